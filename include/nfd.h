@@ -221,6 +221,121 @@ int nfd_attention_noalloc(const void *q, const void *k_pages, const void *v_page
                           int head_dim, int tokens_per_frame, int n_q_frames, int n_kv_frames, int window,
                           void *out, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Calls for callers that bring their own cache, for several sequences at once.
+ * (The paper has no counterpart of them, but for its cross-attention variant of
+ * the conditioning, Section 3.1.)  Like nfd_attention_noalloc they need no
+ * context, allocate nothing and call no allocating library routine; unlike it
+ * they have no working memory at all: calls may overlap on the GPU, on any
+ * streams, and be captured into graphs.  Everything that changes from call to
+ * call -- lengths, page tables, which rows belong to which sequence -- is read
+ * on the device when the call runs, so that a captured call can be replayed for
+ * the next step.  The device of `cuda_stream` has to be current.
+ *
+ * Device-side values are clamped, never trusted: row_start into 0..n_rows,
+ * kv_len into 0..2^30; a page number outside 0..n_pages-1 stands for a page that
+ * is not there: its keys are seen by nobody, and rows that belong in it are
+ * dropped. */
+
+/* Which rows belong to which sequence.  Sequence s has the rows row_start[s] ..
+ * row_start[s+1]-1 of the row buffers, at most max_rows of them (rows past
+ * max_rows in a sequence, and rows behind the last sequence, are left alone), or,
+ * with row_start NULL, max_rows rows each (n_rows == n_seqs * max_rows).
+ * With a paged cache kv_len[s] counts the sequence's tokens with its rows in it:
+ * row i of n is token kv_len[s] - n + i.  Token p lies in page
+ * table[s * table_len + (p / page_tokens) % table_len]: a table that is shorter
+ * than the sequence is a ring, and tokens that have been overwritten in it are
+ * seen by nobody. */
+typedef struct {
+    const int *row_start;    /* dev [n_seqs + 1], or NULL                              */
+    const int *kv_len;       /* dev [n_seqs]; nfd_cross_attention: keys, NULL = all     */
+    const int *table;        /* dev [n_seqs][table_len] (paged cache only)              */
+    int n_seqs, n_rows, max_rows, table_len;
+} nfd_batch;
+
+/* A paged cache: pages [n_pages][n_heads][page_tokens][head_dim] of K and of V.
+ * dtype: NFD_DTYPE_FP32, NFD_DTYPE_BF16 or NFD_DTYPE_KV4.
+ * NFD_DTYPE_KV4 holds 4.5 bits per number.  k and v are [..][head_dim / 2] bytes,
+ * k_scale and v_scale [..][head_dim / 32] 16-bit words, one for 32 numbers.  A
+ * word's upper 12 bits are those of a bf16 number `step` (4 significant bits), its
+ * lower 4 bits a whole number z; a code n stands for (n - z) step, which is a
+ * bf16 number (exactly, as long as it does not leave bf16's range).  Codes: eight numbers to a little-endian 32-bit word,
+ * number i in bits 4 (i / 2) + 16 (i % 2) and up. */
+#define NFD_DTYPE_KV4 2
+typedef struct {
+    void *k, *v;                                        /* dev                          */
+    void *k_scale, *v_scale;                            /* dev, NFD_DTYPE_KV4 only      */
+    int dtype, n_pages, n_heads, page_tokens, head_dim; /* head_dim in {32,64,128}      */
+} nfd_pages;
+
+/* Rotation of queries and keys: the 3D rotary embedding of nfd_cfg (adjacent
+ * pairs; rope_t, rope_h, rope_w even, sum == head_dim).  Token p has the position
+ * (p / frame_tokens, p % frame_tokens / grid_w, p % frame_tokens % grid_w);
+ * frame_tokens = grid_w = 1 and rope_t = head_dim is the embedding of a text. */
+typedef struct {
+    int rope_t, rope_h, rope_w;
+    float theta;
+    int frame_tokens, grid_w;
+} nfd_rope;
+
+/* Append rows to a paged cache: k and v dev [n_rows][n_heads][head_dim] of `dtype`
+ * (NFD_DTYPE_FP32 or NFD_DTYPE_BF16), k_stride and v_stride elements from row to
+ * row, go to their tokens' places, k rotated (rope NULL: as it is).  The pages
+ * hold `dtype` or NFD_DTYPE_KV4.  With n_q_heads > 0 the rows' queries, q dev
+ * [n_rows][n_q_heads][head_dim], q_stride from row to row, are rotated into
+ * q_out dev [n_rows][n_q_heads][head_dim], which may be q itself if q is
+ * contiguous.  The angle of a pair is formed in 64 bits, its sine and cosine are
+ * rounded to fp32, the rotation is computed in fp32.
+ * 4 bits: of 32 numbers, lo = min(0, smallest), hi = max(0, largest), step = the
+ * smallest number of 4 significant bits, at least 2^-100, with 15 step >= hi - lo,
+ * z = lo / -step rounded, n = x / step rounded, plus z, kept in 0..15 (all to
+ * nearest, ties to even).  Where one of the 32 is not finite, or hi - lo is not,
+ * the step is NaN and with it all 32.
+ * Rows of tokens below 0 (a sequence with more rows than kv_len) are dropped.
+ * Two rows for the same place (pages that sequences share) race. */
+int nfd_kv_append(const nfd_pages *pages, const nfd_batch *batch, const nfd_rope *rope, int dtype, const void *k,
+                  long long k_stride, const void *v, long long v_stride, int n_q_heads, const void *q,
+                  long long q_stride, void *q_out, void *cuda_stream);
+
+/* The batch's rows read back out of the pages: k_out and v_out dev
+ * [n_rows][n_heads][head_dim] (either may be NULL) of `dtype`; NFD_DTYPE_KV4 pages
+ * are read as either type, others as their own.  Rows without a place are left
+ * alone. */
+int nfd_pages_read(const nfd_pages *pages, const nfd_batch *batch, int dtype, void *k_out, void *v_out,
+                   void *cuda_stream);
+
+/* Attention over a cache of NFD_DTYPE_KV4 pages.  q dev bf16
+ * [n_rows][n_heads][head_dim], q_stride elements from row to row; out dev bf16
+ * [n_rows][n_heads * head_dim].  n_heads is a multiple of pages->n_heads: head h
+ * reads the pages' head h / (n_heads / pages->n_heads).  The mask is the library's
+ * block-wise causal one: token p belongs to frame p / frame_tokens and sees the
+ * tokens of the frames max(0, frame - window) .. frame that the cache holds
+ * (frame_tokens = 1: a causal mask over the last window + 1 tokens).
+ * The scale is 1 / sqrt(head_dim).  A row that sees nothing, or nothing but scores
+ * of -inf, gives zeros.  Scores, softmax and sums are fp32; probabilities are rounded to bf16 for
+ * the product with V.  Should a device-side wait run out, the rows concerned are NaN. */
+int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,
+                      int frame_tokens, int window, void *out, void *cuda_stream);
+
+/* The states of an encoder, as keys and values: k and v dev, of dtype
+ * NFD_DTYPE_FP32 or NFD_DTYPE_BF16, element strides from sequence to sequence (0:
+ * all sequences share one set), from key to key and from head to head; head_dim is contiguous.
+ * Keys j with mask[s * n_keys + j] == 0 are seen by nobody; what k and v hold there, or
+ * behind a sequence's length, is not looked at.  (n_keys 0: k and v may be NULL.) */
+typedef struct {
+    const void *k, *v;
+    const unsigned char *mask;                          /* dev [n_seqs][n_keys], or NULL */
+    long long seq_stride, key_stride, head_stride;
+    int dtype, n_keys, n_heads, head_dim;
+} nfd_states;
+
+/* Cross attention: every row of a sequence sees the first kv_len[s] (at most
+ * n_keys) states of its sequence, but for masked ones.  q, out, n_heads, scale and
+ * rows that see nothing as in nfd_attention_kv4; q and out of the states' type.
+ * fp32 is computed on the fp32 pipes. */
+int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_heads, const void *q,
+                        long long q_stride, void *out, void *cuda_stream);
+
 /* Device-side status latch: 0, or the first NFD_E_* a kernel recorded.
  * NFD_E_TIMEOUT: a bounded wait inside a kernel (on an mbarrier that a TMA copy or
  * a tensor-core operation completes) ran out after 0.4 s; the kernel skipped the

@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnfd.so")
-SOURCES = ["nfd_api.cu"]
+SOURCES = ["nfd_api.cu", "nfd_paged.cu"]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,223 @@
+// Entry points for callers that bring their own memory: appending to paged caches, attention over 4-bit pages, cross
+// attention.  No context, no working memory; see include/nfd.h.
+#include <math.h>
+#include <stdio.h>
+#include <string.h>
+
+#include "nfd_append.cuh"
+#include "nfd_attn_any.cuh"
+
+#define CK(call)                                                                                   \
+    do {                                                                                           \
+        cudaError_t e_ = (call);                                                                   \
+        if (e_ != cudaSuccess) {                                                                   \
+            fprintf(stderr, "libnfd: %s failed: %s (%s:%d)\n", #call, cudaGetErrorString(e_),      \
+                    __FILE__, __LINE__);                                                           \
+            return NFD_E_CUDA;                                                                     \
+        }                                                                                          \
+    } while (0)
+
+#define RET(expr)                    \
+    do {                             \
+        int r_ = (expr);             \
+        if (r_ != NFD_OK) return r_; \
+    } while (0)
+
+namespace {
+
+bool aligned(const void *p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+size_t type_size(int dtype) { return dtype == NFD_DTYPE_FP32 ? 4 : 2; }
+
+template <typename F> int by_head_dim(int dh, F &&f) {
+    switch (dh) {
+        case 32: return f(std::integral_constant<int, 32>());
+        case 64: return f(std::integral_constant<int, 64>());
+        default: return f(std::integral_constant<int, 128>());
+    }
+}
+
+int check_batch(const nfd_batch *b, bool paged, BatchD &B) {
+    if (!b) return NFD_E_NULLPTR;
+    if (paged && (!b->kv_len || !b->table)) return NFD_E_NULLPTR;
+    if (!aligned(b->row_start, 4) || !aligned(b->kv_len, 4) || !aligned(b->table, 4)) return NFD_E_ALIGN;
+    if (b->n_seqs < 1 || b->n_seqs > 65535 || b->n_rows < 0 || b->n_rows > NFD_MAX_TOKENS) return NFD_E_RANGE;
+    if (b->max_rows < 0 || b->max_rows > b->n_rows) return NFD_E_RANGE;
+    if (!b->row_start && (long long)b->n_seqs * b->max_rows != b->n_rows) return NFD_E_RANGE;
+    if (paged && (b->table_len < 1 || b->table_len > NFD_MAX_TOKENS)) return NFD_E_RANGE;
+    B = {b->row_start, b->kv_len, b->table, b->n_seqs, b->n_rows, b->max_rows, b->table_len};
+    return NFD_OK;
+}
+
+int check_pages(const nfd_pages *p, PagesD &P) {
+    if (!p || !p->k || !p->v) return NFD_E_NULLPTR;
+    if (p->dtype != NFD_DTYPE_FP32 && p->dtype != NFD_DTYPE_BF16 && p->dtype != NFD_DTYPE_KV4) return NFD_E_BADCFG;
+    if (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) return NFD_E_BADCFG;
+    if (p->dtype == NFD_DTYPE_KV4 && (!p->k_scale || !p->v_scale)) return NFD_E_NULLPTR;
+    if (!aligned(p->k, 16) || !aligned(p->v, 16)) return NFD_E_ALIGN;
+    if (p->dtype == NFD_DTYPE_KV4 && (!aligned(p->k_scale, 16) || !aligned(p->v_scale, 16))) return NFD_E_ALIGN;
+    if (p->n_pages < 1 || p->n_heads < 1 || p->n_heads > 1024 || p->page_tokens < 1 || p->page_tokens > (1 << 20)) return NFD_E_RANGE;
+    P = {p->k, p->v, (uint16_t *)p->k_scale, (uint16_t *)p->v_scale, p->n_pages, p->n_heads, p->page_tokens};
+    return NFD_OK;
+}
+
+// rows of `heads` heads, `stride` elements apart, read in 16-byte words
+int check_rows(const void *p, long long stride, int heads, int head_dim, int dtype) {
+    if (!p) return NFD_E_NULLPTR;
+    if (!aligned(p, 16) || (stride * (long long)type_size(dtype)) % 16) return NFD_E_ALIGN;
+    if (stride < (long long)heads * head_dim || stride > (1LL << 40)) return NFD_E_RANGE;
+    return NFD_OK;
+}
+
+int check_heads(int n_heads, int kv_heads) {
+    if (n_heads < 1 || n_heads > 1024 || kv_heads < 1 || n_heads % kv_heads) return NFD_E_RANGE;
+    return NFD_OK;
+}
+
+int sm_count(int &n) {
+    static int n_sms[64];                      // (the same value whichever thread stores it)
+    int dev = -1;
+    CK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return NFD_E_RANGE;
+    if (!n_sms[dev]) CK(cudaDeviceGetAttribute(&n_sms[dev], cudaDevAttrMultiProcessorCount, dev));
+    n = n_sms[dev];
+    return NFD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int nfd_kv_append(const nfd_pages *pages, const nfd_batch *batch, const nfd_rope *rope, int dtype, const void *k,
+                  long long k_stride, const void *v, long long v_stride, int n_q_heads, const void *q,
+                  long long q_stride, void *q_out, void *cuda_stream) {
+    BatchD B;
+    PagesD P;
+    RET(check_pages(pages, P));
+    RET(check_batch(batch, true, B));
+    if (dtype != NFD_DTYPE_FP32 && dtype != NFD_DTYPE_BF16) return NFD_E_BADCFG;
+    if (pages->dtype != dtype && pages->dtype != NFD_DTYPE_KV4) return NFD_E_BADCFG;
+    const int dh = pages->head_dim;
+    RET(check_rows(k, k_stride, P.heads, dh, dtype));
+    RET(check_rows(v, v_stride, P.heads, dh, dtype));
+    if (n_q_heads < 0 || n_q_heads > 1024) return NFD_E_RANGE;
+    if (n_q_heads) {
+        RET(check_rows(q, q_stride, n_q_heads, dh, dtype));
+        if (!q_out) return NFD_E_NULLPTR;
+        if (!aligned(q_out, 16)) return NFD_E_ALIGN;
+    }
+    RopeD R;
+    memset(&R, 0, sizeof(R));
+    if (rope) {
+        const int d[3] = {rope->rope_t, rope->rope_h, rope->rope_w};
+        if (d[0] < 0 || d[1] < 0 || d[2] < 0 || d[0] % 2 || d[1] % 2 || d[2] % 2 || (long long)d[0] + d[1] + d[2] != dh) return NFD_E_BADCFG;
+        if (!(rope->theta > 0.f) || !isfinite(rope->theta)) return NFD_E_BADCFG;
+        if (rope->frame_tokens < 1 || rope->grid_w < 1 || rope->frame_tokens % rope->grid_w) return NFD_E_BADCFG;
+        R.on = 1, R.frame_tokens = rope->frame_tokens, R.grid_w = rope->grid_w;
+        R.half_t = d[0] / 2, R.half_th = (d[0] + d[1]) / 2;
+        for (int a = 0, pair = 0; a < 3; ++a)
+            for (int i = 0; i < d[a] / 2; ++i) R.freq[pair++] = pow((double)rope->theta, -2.0 * i / d[a]);
+    }
+    if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
+    int n_sm = 0;
+    RET(sm_count(n_sm));
+    const AppendIO io = {q, k, v, q_stride, k_stride, v_stride, q_out, n_q_heads};
+    const int rows = B.n_rows >= 2 * APPEND_MAX_ROWS * n_sm ? APPEND_MAX_ROWS : 1;
+    const unsigned grid = (unsigned)((B.n_rows + rows - 1) / rows);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    by_head_dim(dh, [&](auto d) {
+        constexpr int DH = decltype(d)::value;
+        const bool kv4 = pages->dtype == NFD_DTYPE_KV4;
+        if (dtype == NFD_DTYPE_BF16) {
+            if (kv4) k_kv_append<bf16, true, DH><<<grid, APPEND_THREADS, 0, st>>>(R, io, B, P, rows);
+            else k_kv_append<bf16, false, DH><<<grid, APPEND_THREADS, 0, st>>>(R, io, B, P, rows);
+        } else {
+            if (kv4) k_kv_append<float, true, DH><<<grid, APPEND_THREADS, 0, st>>>(R, io, B, P, rows);
+            else k_kv_append<float, false, DH><<<grid, APPEND_THREADS, 0, st>>>(R, io, B, P, rows);
+        }
+        return 0;
+    });
+    CK(cudaGetLastError());
+    return NFD_OK;
+}
+
+int nfd_pages_read(const nfd_pages *pages, const nfd_batch *batch, int dtype, void *k_out, void *v_out, void *cuda_stream) {
+    BatchD B;
+    PagesD P;
+    RET(check_pages(pages, P));
+    RET(check_batch(batch, true, B));
+    if (dtype != NFD_DTYPE_FP32 && dtype != NFD_DTYPE_BF16) return NFD_E_BADCFG;
+    if (pages->dtype != dtype && pages->dtype != NFD_DTYPE_KV4) return NFD_E_BADCFG;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16)) return NFD_E_ALIGN;
+    if (B.n_rows == 0 || B.max_rows == 0 || (!k_out && !v_out)) return NFD_OK;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    by_head_dim(pages->head_dim, [&](auto d) {
+        constexpr int DH = decltype(d)::value;
+        const unsigned grid = (unsigned)B.n_rows;
+        if (pages->dtype == NFD_DTYPE_KV4) {
+            if (dtype == NFD_DTYPE_BF16) k_pages_read<bf16, bf16, true, DH><<<grid, 256, 0, st>>>(B, P, (bf16 *)k_out, (bf16 *)v_out);
+            else k_pages_read<bf16, float, true, DH><<<grid, 256, 0, st>>>(B, P, (float *)k_out, (float *)v_out);
+        } else if (dtype == NFD_DTYPE_BF16) {
+            k_pages_read<bf16, bf16, false, DH><<<grid, 256, 0, st>>>(B, P, (bf16 *)k_out, (bf16 *)v_out);
+        } else {
+            k_pages_read<float, float, false, DH><<<grid, 256, 0, st>>>(B, P, (float *)k_out, (float *)v_out);
+        }
+        return 0;
+    });
+    CK(cudaGetLastError());
+    return NFD_OK;
+}
+
+int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,
+                      int frame_tokens, int window, void *out, void *cuda_stream) {
+    BatchD B;
+    PagesD P;
+    RET(check_pages(pages, P));
+    RET(check_batch(batch, true, B));
+    if (pages->dtype != NFD_DTYPE_KV4) return NFD_E_BADCFG;
+    RET(check_heads(n_heads, P.heads));
+    RET(check_rows(q, q_stride, n_heads, pages->head_dim, NFD_DTYPE_BF16));
+    if (!out) return NFD_E_NULLPTR;
+    if (!aligned(out, 16)) return NFD_E_ALIGN;
+    if (frame_tokens < 1 || frame_tokens > (1 << 20) || window < 0) return NFD_E_RANGE;
+    if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
+    const AttnRows A = {q, out, q_stride, n_heads, n_heads / P.heads};
+    return by_head_dim(pages->head_dim, [&](auto d) -> int {
+        constexpr int DH = decltype(d)::value;
+        return launch_attn_any<bf16, DH>(B, A, Kv4Keys<DH>{P, {frame_tokens, window}}, (cudaStream_t)cuda_stream);
+    });
+}
+
+int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,
+                        void *out, void *cuda_stream) {
+    if (!states || (states->n_keys && (!states->k || !states->v))) return NFD_E_NULLPTR;
+    BatchD B;
+    RET(check_batch(batch, false, B));
+    const int dtype = states->dtype, dh = states->head_dim;
+    if (dtype != NFD_DTYPE_FP32 && dtype != NFD_DTYPE_BF16) return NFD_E_BADCFG;
+    if (dh != 32 && dh != 64 && dh != 128) return NFD_E_BADCFG;
+    if (states->n_keys < 0 || states->n_keys > NFD_MAX_TOKENS) return NFD_E_RANGE;
+    RET(check_heads(n_heads, states->n_heads));
+    const long long unit = 16 / (long long)type_size(dtype), most = 1LL << 40;
+    const long long st[3] = {states->seq_stride, states->key_stride, states->head_stride};
+    for (long long s : st)
+        if (s < 0 || s > most) return NFD_E_RANGE;
+    for (long long s : st)
+        if (s % unit) return NFD_E_ALIGN;
+    if (!aligned(states->k, 16) || !aligned(states->v, 16)) return NFD_E_ALIGN;
+    RET(check_rows(q, q_stride, n_heads, dh, dtype));
+    if (!out) return NFD_E_NULLPTR;
+    if (!aligned(out, 16)) return NFD_E_ALIGN;
+    if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
+    const AttnRows A = {q, out, q_stride, n_heads, n_heads / states->n_heads};
+    return by_head_dim(dh, [&](auto d) -> int {
+        constexpr int DH = decltype(d)::value;
+        auto go = [&](auto *t) -> int {
+            using TS = std::remove_pointer_t<decltype(t)>;
+            const StateKeys<TS, DH> K = {(const TS *)states->k, (const TS *)states->v, states->mask, st[0], st[1], st[2], states->n_keys};
+            return launch_attn_any<TS, DH>(B, A, K, (cudaStream_t)cuda_stream);
+        };
+        return dtype == NFD_DTYPE_BF16 ? go((bf16 *)nullptr) : go((float *)nullptr);
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,96 @@
+// Batches of sequences, paged caches and encoder states as kernels see them: where a row belongs, where a token lies, the
+// 4-bit numbers.  Everything that comes from device memory (row starts, lengths, page numbers) is clamped here.
+#pragma once
+#include "nfd_common.cuh"
+
+#define NFD_MAX_TOKENS (1 << 30)
+
+struct BatchD {
+    const int *row_start, *kv_len, *table;
+    int n_seqs, n_rows, max_rows, table_len;
+    // first row and number of rows of sequence s (of which the first max_rows are computed)
+    __device__ __forceinline__ int2 rows(int s) const {
+        if (!row_start) return make_int2(s * max_rows, max_rows);
+        const int a = min(max(__ldg(row_start + s), 0), n_rows), b = min(__ldg(row_start + s + 1), n_rows);
+        return make_int2(a, max(b - a, 0));
+    }
+    // the sequence of a row, for a whole warp: as many as end at or before it
+    __device__ __forceinline__ int seq_of(int row) const {
+        if (!row_start) return row / max_rows;
+        int s = 0;
+        for (int s0 = 0; s0 < n_seqs; s0 += 32) {
+            const int i = s0 + (threadIdx.x & 31);
+            s += __popc(__ballot_sync(0xffffffffu, i < n_seqs && __ldg(row_start + i + 1) <= row));
+        }
+        return s;
+    }
+    __device__ __forceinline__ int tokens(int s) const { return min(max(__ldg(kv_len + s), 0), NFD_MAX_TOKENS); }
+};
+
+// What a token's place in a paged cache needs.
+struct PagesD {
+    void *k, *v;
+    uint16_t *k_scale, *v_scale;
+    int n_pages, heads, page_tokens;
+    // Place of token p of sequence s: (page * heads) * page_tokens + offset, in rows; head h is h * page_tokens further on.
+    // -1: there is none.
+    __device__ __forceinline__ long long place(const BatchD &B, int s, int p) const {
+        const int pg = p / page_tokens, page = __ldg(B.table + (size_t)s * B.table_len + pg % B.table_len);
+        if ((unsigned)page >= (unsigned)n_pages) return -1;
+        return (long long)page * heads * page_tokens + (p - pg * page_tokens);
+    }
+    // tokens below this one have been overwritten by the ring
+    __device__ __forceinline__ int oldest(const BatchD &B, int tokens) const {
+        const long long o = (long long)tokens - (long long)B.table_len * page_tokens;
+        return o > 0 ? (int)o : 0;
+    }
+};
+
+// ---- 4-bit numbers ------------------------------------------------------------------------------------------
+// Step (upper 12 bits of the word) and zero of a group with range lo..hi (lo <= 0 <= hi).  The fp32 product is within an
+// ulp or two of (hi - lo) / 15; with 4 significant bits 15 step is exact, so that one comparison on either side settles
+// which of two neighbours is the smallest that covers the range.
+__device__ __forceinline__ float kv4_step(float lo, float hi) {
+    const float r = hi - lo;
+    uint32_t b = (__float_as_uint(fmaxf(r * (1.0f / 15.0f), 7.8886090522101181e-31f)) + 0xFFFFFu) & 0xFFF00000u;
+    if (15.0f * __uint_as_float(b) < r) b += 0x100000u;
+    const uint32_t down = b - 0x100000u;
+    if (__uint_as_float(down) >= 7.8886090522101181e-31f && 15.0f * __uint_as_float(down) >= r) b = down;
+    return __uint_as_float(b);
+}
+// x / step to the nearest whole number, ties to even: the product with the reciprocal is off by ulps, the remainder of
+// its rounding is exact in fp32 (whole number of 5 bits x 4 bits, next to x) and corrects it.
+__device__ __forceinline__ float kv4_round(float x, float step, float inv) {
+    float r = rintf(x * inv);
+    const float e = fmaf(-r, step, x), h = 0.5f * step;
+    const bool odd = (int)r & 1;
+    if (e > h || (e == h && odd)) r += 1.0f;
+    else if (e < -h || (e == -h && odd)) r -= 1.0f;
+    return r;
+}
+// bits of code i of a word of eight
+__device__ __forceinline__ constexpr int kv4_shift(int i) { return 4 * (i >> 1) + 16 * (i & 1); }
+__device__ __forceinline__ float kv4_word_step(uint32_t w) { return __uint_as_float((w & 0xFFF0u) << 16); }
+// the eight numbers of a word of codes, exact
+__device__ __forceinline__ void kv4_unpack(uint32_t codes, uint32_t word, float *x) {
+    const float step = kv4_word_step(word);
+    const int z = word & 15;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)((int)(codes >> kv4_shift(i) & 15) - z) * step;
+}
+
+// ---- which keys a row sees ----------------------------------------------------------------------------------
+struct KeyRange {
+    int lo, hi;
+};
+// Block-wise causal: row i of n of a sequence of `len` tokens.
+struct CausalMask {
+    int frame_tokens, window;
+    __device__ __forceinline__ KeyRange range(int len, int oldest, int n, int i) const {
+        const int p = len - n + i;
+        if (p < 0) return {0, 0};
+        const int f = p / frame_tokens;
+        const int lo = max(max(f - window, 0) * frame_tokens, oldest);
+        return {lo, max(lo, min((f + 1) * frame_tokens, len))};
+    }
+};

@@ -17,6 +17,7 @@ import numpy as np
 # dtype codes shared with the C ABI (nfd_cfg.dtype)
 DTYPE_FP32 = 0
 DTYPE_BF16 = 1
+DTYPE_KV4 = 2            # pages of a cache only (nfd_pages.dtype)
 
 
 def _base_cfg(**kw):

@@ -45,7 +45,29 @@ EXPORTS = ["nfd_create", "nfd_destroy", "nfd_reset", "nfd_denoise_step", "nfd_de
            "nfd_launch_count", "nfd_set_option", "nfd_warm_modulation", "nfd_strerror", "nfd_profile_begin",
            "nfd_profile_end",
            "nfd_profile_class_count", "nfd_profile_class_name", "nfd_attention_noalloc", "nfd_cond_cache_stats",
-           "nfd_sample_dpmpp", "nfd_accepted_count", "nfd_debug_read"]
+           "nfd_sample_dpmpp", "nfd_accepted_count", "nfd_debug_read", "nfd_kv_append", "nfd_pages_read",
+           "nfd_attention_kv4", "nfd_cross_attention"]
+
+
+class NfdBatch(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("row_start", "kv_len", "table")]
+                + [(n, C.c_int) for n in ("n_seqs", "n_rows", "max_rows", "table_len")])
+
+
+class NfdPages(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+                + [(n, C.c_int) for n in ("dtype", "n_pages", "n_heads", "page_tokens", "head_dim")])
+
+
+class NfdRope(C.Structure):
+    _fields_ = [("rope_t", C.c_int), ("rope_h", C.c_int), ("rope_w", C.c_int), ("theta", C.c_float),
+                ("frame_tokens", C.c_int), ("grid_w", C.c_int)]
+
+
+class NfdStates(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("k", "v", "mask")]
+                + [(n, C.c_longlong) for n in ("seq_stride", "key_stride", "head_stride")]
+                + [(n, C.c_int) for n in ("dtype", "n_keys", "n_heads", "head_dim")])
 
 
 class NfdError(RuntimeError):
@@ -96,6 +118,11 @@ def load():
     lib.nfd_cond_cache_stats.argtypes = [vp, C.POINTER(C.c_longlong), C.POINTER(C.c_longlong)]
     lib.nfd_accepted_count.argtypes = [ip, C.c_int, C.c_int, C.c_int]
     lib.nfd_debug_read.argtypes = [vp, C.c_char_p, vp, C.c_longlong]
+    ll = C.c_longlong
+    lib.nfd_kv_append.argtypes = [vp, vp, vp, C.c_int, vp, ll, vp, ll, C.c_int, vp, ll, vp, vp]
+    lib.nfd_pages_read.argtypes = [vp, vp, C.c_int, vp, vp, vp]
+    lib.nfd_attention_kv4.argtypes = [vp, vp, C.c_int, vp, ll, C.c_int, C.c_int, vp, vp]
+    lib.nfd_cross_attention.argtypes = [vp, vp, C.c_int, vp, ll, vp, vp]
     lib.nfd_strerror.argtypes = [C.c_int]
     lib.nfd_strerror.restype = C.c_char_p
     _lib = lib
@@ -152,6 +179,178 @@ def attention_noalloc(q, k_pages, v_pages, n_q_frames: int, window: int, out, st
                                      C.c_void_p(v_pages.data_ptr()), dtype, H, dh, T, n_q_frames, n_kv, window,
                                      C.c_void_p(out.data_ptr()), C.c_void_p(st.cuda_stream)),
            "nfd_attention_noalloc")
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# calls for hosts that bring their own memory: paged caches, 4-bit pages, encoder states
+# ---------------------------------------------------------------------------------------------------------------
+_TYPES = {torch.float32: I.DTYPE_FP32, torch.bfloat16: I.DTYPE_BF16}
+
+
+class Batch:
+    """nfd_batch: which rows belong to which sequence, and where its tokens lie.  kv_len [n_seqs], table
+    [n_seqs, table_len] (paged caches) and row_start [n_seqs + 1] (None: n_rows / n_seqs rows each) are contiguous int32
+    tensors on the GPU; their values are read when a call runs and may change between calls.  max_rows: the most rows
+    that a sequence has (None: n_rows)."""
+
+    def __init__(self, n_rows: int, kv_len=None, table=None, row_start=None, max_rows=None, n_seqs=None):
+        given = [t for t in (kv_len, table, row_start) if t is not None]
+        for t in given:
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 and t.device == given[0].device
+        if n_seqs is None:
+            n_seqs = kv_len.shape[0] if kv_len is not None else row_start.shape[0] - 1
+        assert kv_len is None or tuple(kv_len.shape) == (n_seqs,)
+        assert table is None or (table.dim() == 2 and table.shape[0] == n_seqs)
+        assert row_start is None or tuple(row_start.shape) == (n_seqs + 1,)
+        if max_rows is None:
+            max_rows = n_rows if row_start is not None else n_rows // n_seqs
+        self.kv_len, self.table, self.row_start = kv_len, table, row_start
+        self.device = given[0].device if given else None
+        self.n_seqs, self.n_rows = n_seqs, int(n_rows)
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        self.c = NfdBatch(ptr(row_start), ptr(kv_len), ptr(table), n_seqs, self.n_rows, int(max_rows),
+                          table.shape[1] if table is not None else 0)
+        self.ref = C.addressof(self.c)
+
+
+class Pages:
+    """nfd_pages: a paged cache.  k, v [n_pages, n_heads, page_tokens, head_dim] of float32 or bfloat16; or, with 4 bits a
+    number, [.., head_dim / 2] uint8 with k_scale, v_scale [.., head_dim / 32] int16."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        kv4 = k.dtype == torch.uint8
+        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and (kv4 or k.dtype in _TYPES)
+        n_pages, heads, tokens, width = k.shape
+        head_dim = 2 * width if kv4 else width
+        for t in (k, v) + ((k_scale, v_scale) if kv4 else ()):
+            assert t.is_cuda and t.is_contiguous() and t.device == k.device
+        if kv4:
+            for t in (k_scale, v_scale):
+                assert t.dtype == torch.int16 and tuple(t.shape) == (n_pages, heads, tokens, head_dim // 32)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device, self.n_heads, self.head_dim = k.device, heads, head_dim
+        self.dtype = None if kv4 else k.dtype
+        ptr = lambda t: t.data_ptr() if kv4 else None
+        self.c = NfdPages(k.data_ptr(), v.data_ptr(), ptr(k_scale), ptr(v_scale), I.DTYPE_KV4 if kv4 else _TYPES[k.dtype],
+                          n_pages, heads, tokens, head_dim)
+        self.ref = C.addressof(self.c)
+
+    @classmethod
+    def empty(cls, dtype, n_pages: int, n_heads: int, page_tokens: int, head_dim: int, device="cuda:0"):
+        """A new cache; dtype torch.float32, torch.bfloat16 or "kv4"."""
+        shape = (n_pages, n_heads, page_tokens)
+        new = lambda width, dt: torch.zeros(shape + (width,), device=device, dtype=dt)
+        if dtype == "kv4":
+            return cls(new(head_dim // 2, torch.uint8), new(head_dim // 2, torch.uint8),
+                       new(head_dim // 32, torch.int16), new(head_dim // 32, torch.int16))
+        return cls(new(head_dim, dtype), new(head_dim, dtype))
+
+
+class Rope:
+    """nfd_rope: the rotation of queries and keys (3D as in the configuration; of a text: Rope(head_dim, 0, 0))."""
+
+    def __init__(self, rope_t: int, rope_h: int, rope_w: int, theta: float = 10000.0, frame_tokens: int = 1, grid_w: int = 1):
+        self.c = NfdRope(rope_t, rope_h, rope_w, theta, frame_tokens, grid_w)
+        self.ref = C.addressof(self.c)
+
+
+class States:
+    """nfd_states: an encoder's states as keys and values [n_seqs, n_keys, n_heads, head_dim] of float32 or bfloat16, which
+    may be strided (and expanded over sequences) alike; mask [n_seqs, n_keys] bool or uint8, False = not seen."""
+
+    def __init__(self, k, v, mask=None):
+        assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.dtype in _TYPES
+        assert k.is_cuda and v.is_cuda and k.device == v.device and (k.stride(3) == 1 or k.numel() == 0)
+        n, keys, heads, head_dim = k.shape
+        if mask is not None:
+            assert mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and mask.device == k.device
+            assert tuple(mask.shape) == (n, keys)
+        self.k, self.v, self.mask = k, v, mask
+        self.device, self.dtype, self.n_seqs, self.n_heads, self.head_dim = k.device, k.dtype, n, heads, head_dim
+        st = [k.stride(i) if k.shape[i] > 1 and keys else 0 for i in range(3)]        # (the stride of one element says nothing)
+        self.c = NfdStates(k.data_ptr(), v.data_ptr(), mask.data_ptr() if mask is not None else None, st[0], st[1], st[2],
+                           _TYPES[k.dtype], keys, heads, head_dim)
+        self.ref = C.addressof(self.c)
+
+
+def _call(what, device, stream, fn, *args):
+    """A call on `stream` (None: torch's current one) with its device current."""
+    if device.index == torch.cuda.current_device():
+        st = torch.cuda.current_stream() if stream is None else stream
+        code = fn(*args, st.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = torch.cuda.current_stream() if stream is None else stream
+            code = fn(*args, st.cuda_stream)
+    if code != 0:
+        raise NfdError(code, what)
+
+
+def _row_stride(t, n_rows, heads, head_dim, dtype, device):
+    """Elements between the rows of t [n_rows, heads, head_dim] (or [n_rows, heads * head_dim]), whose rows are dense."""
+    assert t.dtype == dtype and t.device == device
+    if t.dim() == 2:
+        assert t.shape[0] == n_rows and t.shape[1] == heads * head_dim and t.stride(1) == 1
+    else:
+        assert tuple(t.shape) == (n_rows, heads, head_dim) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim)
+    return t.stride(0) if n_rows > 1 else heads * head_dim
+
+
+def kv_append(pages: Pages, batch: Batch, k, v, rope: Rope = None, q=None, q_out=None, stream=None):
+    """nfd_kv_append: k, v [n_rows, n_heads, head_dim] go to their tokens' places in the pages, k rotated; with q
+    [n_rows, n_q_heads, head_dim] the rows' queries are rotated into q_out, which is returned.  Rows may be strided."""
+    dev, n, dh = pages.device, batch.n_rows, pages.head_dim
+    assert batch.device == dev and batch.table is not None
+    ks = _row_stride(k, n, pages.n_heads, dh, k.dtype, dev)
+    vs = _row_stride(v, n, pages.n_heads, dh, k.dtype, dev)
+    hq = qs = qp = op = 0
+    if q is not None:
+        hq = q.shape[1] if q.dim() == 3 else q.shape[1] // dh
+        qs, qp = _row_stride(q, n, hq, dh, k.dtype, dev), q.data_ptr()
+        assert q_out.is_contiguous() and q_out.dtype == k.dtype and q_out.device == dev and q_out.numel() == n * hq * dh
+        op = q_out.data_ptr()
+        assert op != qp or qs == hq * dh
+    _call("nfd_kv_append", dev, stream, load().nfd_kv_append, pages.ref, batch.ref, rope.ref if rope is not None else None,
+          _TYPES[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs, hq, qp, qs, op)
+    return q_out
+
+
+def pages_read(pages: Pages, batch: Batch, k_out=None, v_out=None, stream=None):
+    """nfd_pages_read: the batch's rows out of the pages, [n_rows, n_heads, head_dim] each (either may be None)."""
+    dev, n = pages.device, batch.n_rows * pages.n_heads * pages.head_dim
+    assert batch.device == dev and batch.table is not None
+    some = k_out if k_out is not None else v_out
+    for t in (k_out, v_out):
+        assert t is None or (t.is_contiguous() and t.device == dev and t.dtype == some.dtype and t.numel() == n)
+    ptr = lambda t: t.data_ptr() if t is not None else None
+    _call("nfd_pages_read", dev, stream, load().nfd_pages_read, pages.ref, batch.ref, _TYPES[some.dtype], ptr(k_out), ptr(v_out))
+    return k_out, v_out
+
+
+def attention_kv4(pages: Pages, batch: Batch, q, out, frame_tokens: int = 1, window: int = (1 << 31) - 1, stream=None):
+    """nfd_attention_kv4: attention of q [n_rows, n_heads, head_dim] (bfloat16, rows may be strided) over a cache of 4-bit
+    pages into out [n_rows, n_heads * head_dim]; frame_tokens = 1: causal, otherwise block-causal by frames."""
+    dev, n, dh = pages.device, batch.n_rows, pages.head_dim
+    assert batch.device == dev and batch.table is not None
+    h = q.shape[1] if q.dim() == 3 else q.shape[1] // dh
+    qs = _row_stride(q, n, h, dh, torch.bfloat16, dev)
+    assert out.is_contiguous() and out.dtype == torch.bfloat16 and out.device == dev and out.numel() == n * h * dh
+    _call("nfd_attention_kv4", dev, stream, load().nfd_attention_kv4, pages.ref, batch.ref, h, q.data_ptr(), qs, frame_tokens,
+          window, out.data_ptr())
+    return out
+
+
+def cross_attention(states: States, batch: Batch, q, out, stream=None):
+    """nfd_cross_attention: attention of q [n_rows, n_heads, head_dim] (the states' type, rows may be strided) to each row's
+    sequence of encoder states, of which batch.kv_len tells how many there are (None: all), into out [n_rows, n_heads * head_dim]."""
+    dev, n, dh = states.device, batch.n_rows, states.head_dim
+    assert batch.device in (dev, None) and batch.n_seqs == states.n_seqs
+    h = q.shape[1] if q.dim() == 3 else q.shape[1] // dh
+    qs = _row_stride(q, n, h, dh, states.dtype, dev)
+    assert out.is_contiguous() and out.dtype == states.dtype and out.device == dev and out.numel() == n * h * dh
+    _call("nfd_cross_attention", dev, stream, load().nfd_cross_attention, states.ref, batch.ref, h, q.data_ptr(), qs,
+          out.data_ptr())
     return out
 
 

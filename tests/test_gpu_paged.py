@@ -1,0 +1,656 @@
+"""The calls on the caller's own memory against the 64-bit oracle: rows appended to paged caches (bits), attention over 4-bit
+pages, cross attention, and a run of them together.
+
+Bounds.  With S = |q||k| / sqrt(dh), a score is off by at most (dh + 2) 2^-23 S in its fp32 sum (tensor cores may truncate
+where they add), its exponential by that, S 2^-23 (argument) and 2^-21 (function): together e.  A result o = sum p v / sum p
+is off by 2 e M (numerator and denominator), M = sum p |v| / sum p, n 2^-23 M for its sums over n keys and the rounding of
+itself: 2^-23 |o| in fp32, 2^-8 |o| in bf16, where probabilities rounded to bf16 add 2^-8 M.  (1 % on these two is for the
+products of roundings.)
+"""
+import numpy as np
+import pytest
+
+from oracle import paged_oracle as P
+
+pytestmark = pytest.mark.gpu
+
+HALF = 2.0 ** -8
+
+
+def _mods():
+    import torch
+    from paper_2506_01380_b200 import nfd as N
+    return torch, N
+
+
+def _np(t):
+    return t.float().cpu().numpy() if t.dtype.is_floating_point else t.cpu().numpy()
+
+
+def _bits(t):
+    return t.cpu().contiguous().view(-1).view(__import__("torch").uint8).numpy()
+
+
+def _batch(rows, lens, table=None, extra=0, uniform=False, max_rows=None):
+    """(Batch, n_rows) of sequences with `rows` rows and `lens` tokens; `extra` rows behind the last sequence."""
+    torch, N = _mods()
+    start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    n = int(start[-1]) + extra
+    c = lambda a: torch.as_tensor(np.asarray(a, np.int32)).cuda()
+    b = N.Batch(n, c(lens) if lens is not None else None, table=c(table) if table is not None else None,
+                row_start=None if uniform else c(start), max_rows=max_rows if max_rows is not None else max(list(rows) + [0]),
+                n_seqs=len(rows))
+    return b, n
+
+
+def _tables(rng, n_seqs, table_len, spare=3):
+    """Page tables with the pages in no order, and the number of pages."""
+    n = n_seqs * table_len + spare
+    return rng.permutation(n)[:n_seqs * table_len].reshape(n_seqs, table_len).astype(np.int32), n
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# appending
+# ---------------------------------------------------------------------------------------------------------------
+def _pool(kind, n_pages, heads, page, dh, seed):
+    torch, N = _mods()
+    g = torch.Generator("cuda").manual_seed(seed)
+    if kind == "kv4":
+        r = lambda w, dt, hi: torch.randint(0, hi, (n_pages, heads, page, w), generator=g, device="cuda").to(dt)
+        return N.Pages(r(dh // 2, torch.uint8, 256), r(dh // 2, torch.uint8, 256), r(dh // 32, torch.int16, 32000),
+                       r(dh // 32, torch.int16, 32000))
+    r = lambda: torch.randn(n_pages, heads, page, dh, generator=g, device="cuda").to(kind)
+    return N.Pages(r(), r())
+
+
+def _rounded(x, tdt):
+    torch, _ = _mods()
+    return torch.as_tensor(np.ascontiguousarray(x)).to(tdt)
+
+
+def _check_append(kind, tdt, rows, lens, heads, hq, dh, page, table, n_pages, rope, frame, grid_w, q_in_place=False, extra=0,
+                  pad=0, seed=0, poke=None, max_rows=None):
+    torch, N = _mods()
+    rng = np.random.default_rng(seed)
+    pool = _pool(kind, n_pages, heads, page, dh, seed)
+    old = [t.clone() for t in (pool.k, pool.v) + ((pool.k_scale, pool.v_scale) if kind == "kv4" else ())]
+    b, n = _batch(rows, lens, table, extra, max_rows=max_rows)
+    # the projection's output: q | k | v side by side, and `pad` columns nobody reads
+    width = (hq + 2 * heads) * dh + pad
+    x = (rng.standard_normal((n, width)) * np.exp(rng.uniform(-3, 3, (n, 1)))).astype(np.float32)
+    x = _rounded(x, tdt)
+    if poke is not None:
+        poke(x)
+    d = x.cuda()
+    q, k, v = (d[:, a * dh:(a + m) * dh].unflatten(1, (m, dh)) if m else None
+               for a, m in ((0, hq), (hq, heads), (hq + heads, heads)))
+    if q_in_place:
+        q = q.contiguous()
+    q_out = q if q_in_place else torch.full((n, hq, dh), 7.0, device="cuda", dtype=tdt) if hq else None
+    q_old = _np(q_out) if hq else None
+    r = N.Rope(*rope, theta=1e4, frame_tokens=frame, grid_w=grid_w) if rope else None
+    N.kv_append(pool, b, k, v, r, q=q, q_out=q_out)
+    # oracle
+    want = [_np(t) for t in old]
+    xf = _np(x)
+    qf, kf, vf = (xf[:, a * dh:(a + m) * dh].reshape(n, m, dh) for a, m in ((0, hq), (hq, heads), (hq + heads, heads)))
+    q_want, r0 = q_old, 0
+    live = np.zeros(n, bool)
+    for s, (m, length) in enumerate(zip(rows, lens)):
+        cap = m if max_rows is None else min(m, max_rows)
+        pos = length - m + np.arange(cap)
+        here = r0 + np.arange(cap)[pos >= 0]
+        pos = pos[pos >= 0]
+        live[here] = True
+        turn = lambda y: P.rotate(y, pos, rope, 1e4, frame, grid_w) if rope else y
+        if hq:
+            q_want[here] = turn(qf[here])
+        for i, y in ((0, turn(kf[here])), (1, vf[here])):
+            for j, t in enumerate(pos):
+                pg, off = P.place(table[s], t, page)
+                if t < P.held_from(length, len(table[s]), page) or not 0 <= pg < n_pages:
+                    continue
+                if kind == "kv4":
+                    by, words = P.kv4_bytes(*P.kv4_quantise(y[j]))
+                    want[i][pg, :, off], want[2 + i][pg, :, off] = by, words.view(np.int16)
+                else:
+                    want[i][pg, :, off] = y[j]
+        r0 += m
+    got = [t.clone() for t in (pool.k, pool.v) + ((pool.k_scale, pool.v_scale) if kind == "kv4" else ())]
+    for i, (g, w) in enumerate(zip(got, want)):
+        w = torch.as_tensor(w).to(g.dtype)
+        assert np.array_equal(_bits(g), _bits(w)), ("pages", i, int((_bits(g) != _bits(w)).sum()))
+    if hq:
+        assert np.array_equal(_bits(q_out), _bits(torch.as_tensor(q_want).to(tdt)))
+    return pool, b, live
+
+
+TEXT = lambda dh: (dh, 0, 0)
+GRID = {32: (8, 12, 12), 64: (16, 24, 24), 128: (32, 48, 48)}
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("tdt", ["bfloat16", "float32"])
+@pytest.mark.parametrize("pages", ["own", "kv4"])
+def test_append_bits(dh, tdt, pages):
+    """Ragged sequences (one without rows, one longer than its page), pages that end inside a frame: every bit of the pool."""
+    torch, _ = _mods()
+    rng = np.random.default_rng(dh)
+    dt = getattr(torch, tdt)
+    table, n_pages = _tables(rng, 4, 9)
+    _check_append("kv4" if pages == "kv4" else dt, dt, [37, 0, 1, 60], [50, 17, 90, 61], 3, 6, dh, 11, table, n_pages, GRID[dh], 21, 7,
+                  extra=2)
+
+
+@pytest.mark.parametrize("kind", ["bfloat16", "kv4"])
+@pytest.mark.parametrize("rows,lens,page,rope,frame,grid_w,hq", [
+    ([1] * 5, [1, 2, 1000003, 77, 16], 16, "text", 1, 1, 4),       # single tokens, one far out in a ring
+    ([336], [336 * 3], 336, "grid", 336, 14, 2),                   # a frame into its page
+    ([700, 3], [700, 3], 50, "grid", 77, 7, 0),                    # from the start on, no queries; more rows than a ring holds
+    ([5, 4], [3, 4], 8, None, 1, 1, 1),                            # rows of tokens below 0; no rotation
+    ([1500], [1500], 64, "text", 1, 1, 1)])                        # four rows to a CTA
+def test_append_sizes(kind, rows, lens, page, rope, frame, grid_w, hq):
+    torch, _ = _mods()
+    rng = np.random.default_rng(1)
+    table, n_pages = _tables(rng, len(rows), 8)
+    rope = {"text": TEXT(64), "grid": GRID[64], None: None}[rope]
+    _check_append("kv4" if kind == "kv4" else torch.bfloat16, torch.bfloat16, rows, lens, 2, hq, 64, page, table, n_pages, rope, frame, grid_w)
+
+
+def test_append_many_sequences():
+    """More sequences than a warp has lanes; a head count whose chunks leave the last threads idle."""
+    torch, _ = _mods()
+    rng = np.random.default_rng(2)
+    rows = [int(r) for r in rng.integers(0, 4, 75)]
+    table, n_pages = _tables(rng, 75, 2)
+    _check_append("kv4", torch.bfloat16, rows, [r + int(rng.integers(0, 9)) for r in rows], 1, 5, 32, 7, table, n_pages, GRID[32], 12, 4, pad=8)
+
+
+def test_append_holes_in_place_queries_and_capped_rows():
+    """Page numbers that do not exist drop their rows; q rotated in place; rows past max_rows are left alone."""
+    torch, _ = _mods()
+    table = np.array([[0, -1, 2], [3, 1 << 30, 5]], np.int32)
+    _check_append(torch.float32, torch.float32, [20, 20], [25, 30], 2, 3, 64, 10, table, 6, GRID[64], 12, 4, q_in_place=True)
+    table = np.array([[0, 1, 2], [3, 4, 5]], np.int32)
+    _check_append("kv4", torch.bfloat16, [20, 20], [25, 30], 2, 3, 64, 10, table, 6, GRID[64], 12, 4, max_rows=13)
+
+
+def test_append_not_finite():
+    """NaN, infinities and a range beyond fp32 make their group of 32 NaN and no other; tiny and equal numbers hold."""
+    torch, _ = _mods()
+
+    def poke(x):
+        x[0, 64], x[1, 97], x[2, 150], x[3, 64:96] = float("nan"), float("inf"), -float("inf"), 0.0
+        x[4, 64:66] = torch.tensor([3e38, -3e38])
+        x[5, 64:96] = 1e-35
+        x[6, 64:96] = -2.5
+        x[7, 64:192] = 3.0e38
+    _check_append("kv4", torch.float32, [9], [9], 1, 1, 64, 16, np.array([[1]], np.int32), 2, None, 1, 1, poke=poke)
+
+
+def test_append_clamps_what_it_reads_on_the_device():
+    """row_start and kv_len with nonsense in them: nothing is written outside the sequences' places, the good one is right."""
+    torch, N = _mods()
+    pool = _pool(torch.bfloat16, 4, 2, 8, 64, 0)
+    k = torch.randn(12, 2, 64, device="cuda", dtype=torch.bfloat16)
+    b = N.Batch(12, torch.tensor([8, -5, 8], device="cuda", dtype=torch.int32), torch.tensor([[0], [1], [2]], device="cuda", dtype=torch.int32),
+                row_start=torch.tensor([0, 4, 7, 1 << 30], device="cuda", dtype=torch.int32), max_rows=12)
+    old = pool.k.clone()
+    N.kv_append(pool, b, k, k)
+    want = old.clone()
+    want[0, :, 4:8] = k[:4].transpose(0, 1)
+    want[2, :, 3:8] = k[7:].transpose(0, 1)                            # (row_start is taken as n_rows)
+    assert torch.equal(pool.k, want)
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "kv4"])
+def test_read_back(kind):
+    torch, N = _mods()
+    rng = np.random.default_rng(4)
+    table, n_pages = _tables(rng, 3, 4)
+    dt = torch.float32 if kind == "float32" else torch.bfloat16
+    pool, b, live = _check_append("kv4" if kind == "kv4" else dt, dt, [9, 0, 30], [12, 5, 33], 2, 1, 128, 9, table, n_pages, GRID[128], 12, 4, extra=3)
+    outs = [dt, torch.float32] if kind == "kv4" else [dt]
+    for odt in outs:
+        ko, vo = (torch.full((b.n_rows, 2, 128), 7.0, device="cuda", dtype=odt) for _ in range(2))
+        N.pages_read(pool, b, ko, vo)
+        r0 = 0
+        for s, (m, length) in enumerate(zip([9, 0, 30], [12, 5, 33])):
+            for i in range(m):
+                pg, off = P.place(table[s], length - m + i, 9)
+                for o, c, w in ((ko, pool.k, pool.k_scale), (vo, pool.v, pool.v_scale)):
+                    want = P.kv4_values(_np(c[pg, :, off]), _np(w[pg, :, off]).view(np.uint16)) if kind == "kv4" else _np(c[pg, :, off])
+                    assert np.array_equal(_np(o[r0 + i]), want.astype(np.float32))
+            r0 += m
+        assert (ko[~torch.as_tensor(live)] == 7).all()
+        only = torch.zeros_like(vo)
+        N.pages_read(pool, b, None, only)
+        assert torch.equal(only[torch.as_tensor(live)], vo[torch.as_tensor(live)])
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# attention over 4-bit pages
+# ---------------------------------------------------------------------------------------------------------------
+def _kv4_pool(rng, n_pages, heads, page, dh, scale=1.0):
+    """Pages of quantised normal numbers; the same on the host."""
+    torch, N = _mods()
+    parts = []
+    for _ in range(2):
+        x = (rng.standard_normal((n_pages, heads, page, dh)) * scale).astype(np.float32)
+        by, w = P.kv4_bytes(*P.kv4_quantise(x))
+        parts += [by, w]
+    kb, kw, vb, vw = parts
+    t = lambda a: torch.as_tensor(a.view(np.int16) if a.dtype == np.uint16 else a).cuda()
+    return N.Pages(t(kb), t(vb), t(kw), t(vw)), (kb, kw, vb, vw)
+
+
+def _within(got, want, mag, smax, keys, half=HALF):
+    """`half`: half a step of the result (and of probabilities), or 0 for fp32."""
+    dh = want.shape[-1]
+    e = (dh + 2) * 2.0 ** -23 * smax + 2.0 ** -21 + smax * 2.0 ** -23
+    bound = mag * (2 * e + keys * 2.0 ** -23 + 1.01 * half) + np.abs(want) * (1.01 * half + 2.0 ** -23) + 1e-30
+    what = (smax, keys)
+    off = np.abs(got - want)
+    assert np.isfinite(got).all()
+    worst = (off / bound).max() if off.size else 0.0
+    assert worst <= 1.0, (what, worst, np.unravel_index((off / bound).argmax(), off.shape))
+
+
+def _largest_score(q, k):
+    """|q||k| / sqrt(dh) over all rows and keys."""
+    n = lambda x: np.linalg.norm(x, axis=-1).max(initial=0.0)
+    return n(q) * n(k) / np.sqrt(q.shape[-1])
+
+
+def _check_kv4(rows, lens, heads, share, dh, page, table_len, frame, window, seed=0, scale=1.0, extra=0, table=None, n_pages=None, pool=None,
+               uniform=False, pad=0):
+    torch, N = _mods()
+    rng = np.random.default_rng(seed)
+    if table is None:
+        table, n_pages = _tables(rng, len(rows), table_len)
+    pages, host = pool or _kv4_pool(rng, n_pages, heads // share, page, dh)
+    b, n = _batch(rows, lens, table, extra, uniform)
+    q = _rounded((rng.standard_normal((n, heads * dh + pad)) * scale).astype(np.float32), torch.bfloat16)
+    out = torch.full((n, heads * dh), 7.0, device="cuda", dtype=torch.bfloat16)
+    d = q.cuda()[:, :heads * dh]
+    N.attention_kv4(pages, b, d if pad else d.view(n, heads, dh), out, frame_tokens=frame, window=window)
+    live = int(np.sum(rows))
+    want, mag = P.attention_kv4(_np(q)[:live, :heads * dh].reshape(live, heads, dh), dict(rows=rows, lens=lens), table, host, frame, window, share)
+    got = _np(out).reshape(n, heads, dh)
+    _within(got[:live], want, mag, _largest_score(_np(q)[:live, :heads * dh].reshape(live, heads, dh), P.kv4_values(*host[:2])), max(lens))
+    assert (got[live:] == 7).all()
+    return out
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("heads,share", [(3, 1), (8, 4), (6, 6)])
+def test_kv4_single_tokens(dh, heads, share):
+    """One token a sequence: contexts of one token, of less than a tile, of many; a sequence without rows."""
+    _check_kv4([1, 1, 0, 1, 1], [1, 19, 7, 700, 333], heads, share, dh, 16, 44, 1, 1 << 30, seed=dh)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("heads,share,rows,lens,page,table_len,frame,window", [
+    (2, 1, [77, 77], [77 * 5, 77 * 3], 77, 5, 77, 2),              # frames in frame pages, a window
+    (2, 2, [130, 1, 0, 64], [131, 300, 4, 64], 50, 7, 1, 1 << 30), # causal, from the first token on; pages that end inside a tile
+    (4, 2, [40, 12], [200, 190], 16, 13, 20, 3),                   # rows of several frames, the last one not full
+    (2, 1, [200], [1200], 64, 8, 1, 100),                          # a sliding window over a ring that has overwritten the rest
+    (3, 3, [5, 2], [6, 2], 3, 9, 4, 0)])                           # a frame sees itself alone; pages of three tokens
+def test_kv4_many_rows(dh, heads, share, rows, lens, page, table_len, frame, window):
+    _check_kv4(rows, lens, heads, share, dh, page, table_len, frame, window, seed=dh, extra=2)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 4, 5, 8, 9, 16, 17, 31, 33, 64, 127, 129, 257])
+def test_kv4_rows_around_the_tiles(rows):
+    _check_kv4([rows], [rows + 301], 2, 1, 64, 64, 10, 1, 1 << 30, seed=rows, pad=8)
+    _check_kv4([rows], [rows + 90], 6, 3, 64, 48, 10, 16, 3, seed=rows)
+
+
+@pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 255, 256, 257, 640, 1025])
+def test_kv4_lengths_around_the_tiles(length):
+    _check_kv4([1, 1], [length, max(1, length - 1)], 4, 2, 64, 64, 17, 1, 1 << 30, seed=length, uniform=True)
+    _check_kv4([min(length, 40)], [length], 2, 1, 64, 64, 17, 1, 1 << 30, seed=length, uniform=True)
+
+
+@pytest.mark.parametrize("scale", [0.0, 30.0])
+def test_kv4_flat_and_peaked_rows(scale):
+    _check_kv4([1, 1], [900, 513], 4, 1, 64, 64, 16, 1, 1 << 30, scale=scale)
+    _check_kv4([150], [900], 2, 1, 64, 64, 16, 50, 16, scale=scale)
+
+
+def test_kv4_scores_that_rise():
+    """The largest scores come last, far above the first ones."""
+    torch, N = _mods()
+    rng = np.random.default_rng(3)
+    for rows in (1, 140):
+        x = rng.standard_normal((9, 1, 100, 64)).astype(np.float32)
+        x[..., 0] = (np.arange(900) / 20).reshape(9, 1, 100)
+        kb, kw = P.kv4_bytes(*P.kv4_quantise(x))
+        vb, vw = P.kv4_bytes(*P.kv4_quantise(rng.standard_normal(x.shape).astype(np.float32)))
+        t = lambda a: torch.as_tensor(a.view(np.int16) if a.dtype == np.uint16 else a).cuda()
+        b, n = _batch([rows], [900], np.arange(9, dtype=np.int32)[None])
+        q = np.zeros((n, 1, 64), np.float32)
+        q[..., 0], q[..., 1] = 40.0, 1.0
+        out = torch.zeros(n, 64, device="cuda", dtype=torch.bfloat16)
+        N.attention_kv4(N.Pages(t(kb), t(vb), t(kw), t(vw)), b, torch.as_tensor(q).cuda().bfloat16(), out)
+        want, mag = P.attention_kv4(q, dict(rows=[rows], lens=[900]), np.arange(9)[None], (kb, kw, vb, vw), 1, 1 << 30, 1)
+        _within(_np(out).reshape(n, 1, 64), want, mag, _largest_score(q, P.kv4_values(kb, kw)), 900)
+
+
+@pytest.mark.parametrize("rows", [1, 150])
+def test_kv4_rows_that_see_nothing(rows):
+    """No tokens at all, tokens below 0, every page missing: zeros; a hole in the table: its keys are seen by nobody."""
+    torch, N = _mods()
+    rng = np.random.default_rng(5)
+    pool = _kv4_pool(rng, 12, 2, 16, 64)
+    gone = np.full((3, 12), -1, np.int32)
+    out = _check_kv4([rows] * 3, [0, 180, 180], 2, 1, 64, 16, 12, 1, 1 << 30, table=gone, n_pages=12, pool=pool)
+    assert (out == 0).all()
+    holes = np.array([rng.permutation(12) for _ in range(3)], np.int32)
+    holes[0, 3:6], holes[1, 0], holes[2, 11] = -7, 12, 1 << 30
+    _check_kv4([rows] * 3, [180, 170, 192], 2, 1, 64, 16, 12, 1, 1 << 30, table=holes, n_pages=12, pool=pool)
+    out = _check_kv4([rows], [rows // 2], 2, 1, 64, 16, 12, 1, 1 << 30, table=holes[:1], n_pages=12, pool=pool)
+    assert (out[:rows - rows // 2] == 0).all()
+
+
+@pytest.mark.parametrize("rows", [1, 150])
+def test_kv4_what_is_not_seen_is_not_looked_at(rows):
+    """NaN in pages that no row sees, behind the sequence's end and in front of its window, changes nothing; a NaN in a key that is
+    seen makes the rows that see it NaN and no others."""
+    torch, N = _mods()
+    rng = np.random.default_rng(6)
+    pages, host = _kv4_pool(rng, 8, 2, 40, 64)
+    table = np.arange(8, dtype=np.int32)[None]
+    length, window = 290, 130
+    b, n = _batch([rows], [length], table)
+    q = torch.randn(n, 2, 64, device="cuda").bfloat16()
+    out, again = (torch.zeros(n, 128, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    N.attention_kv4(pages, b, q, out, window=window)
+    first = length - rows - window
+    for t in list(range(0, first)) + list(range(length, 320)):
+        for w in (pages.k_scale, pages.v_scale):
+            w[t // 40, :, t % 40] = 0x7FC0
+    N.attention_kv4(pages, b, q, again, window=window)
+    assert torch.equal(out, again)
+    if rows > 1:
+        t = length - 20                                                # seen by the last 20 rows
+        pages.k_scale[t // 40, 1, t % 40] = 0x7FC0
+        N.attention_kv4(pages, b, q, again, window=window)
+        bad = again.isnan().view(n, 2, 64)
+        assert bad[-20:, 1].all() and not bad[:, 0].any() and not bad[:-20].any()
+        assert torch.equal(out.view(n, 2, 64)[:-20], again.view(n, 2, 64)[:-20])
+
+
+def test_kv4_offsets_beyond_32_bits():
+    """A cache of more than 2^32 bytes of codes, with the sequence's pages at its end."""
+    torch, N = _mods()
+    rng = np.random.default_rng(7)
+    page, dh = 512, 128
+    n_pages = (1 << 32) // (page * 8 * dh // 2) + 64
+    z = lambda w, dt: torch.zeros(n_pages, 8, page, w, device="cuda", dtype=dt)
+    pages = N.Pages(z(64, torch.uint8), z(64, torch.uint8), z(4, torch.int16), z(4, torch.int16))
+    table = torch.arange(n_pages - 3, n_pages, device="cuda", dtype=torch.int32).flip(0)[None].contiguous()
+    x = torch.randn(2, 1500, 8, dh, device="cuda").bfloat16()
+    b = N.Batch(1500, torch.tensor([1500], device="cuda", dtype=torch.int32), table)
+    N.kv_append(pages, b, x[0], x[1])
+    small = N.Pages(*[t[-3:].clone() for t in (pages.k, pages.v, pages.k_scale, pages.v_scale)])
+    st = torch.tensor([[2, 1, 0]], device="cuda", dtype=torch.int32)
+    for n in (1, 200):
+        kv = torch.tensor([1500], device="cuda", dtype=torch.int32)
+        q = torch.randn(n, 8, dh, device="cuda").bfloat16()
+        o1, o2 = (torch.zeros(n, 8 * dh, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+        N.attention_kv4(pages, N.Batch(n, kv, table), q, o1)
+        N.attention_kv4(small, N.Batch(n, kv, st), q, o2)
+        assert torch.equal(o1, o2) and o1.abs().sum() > 0
+    assert not pages.k[:-3].any()
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# cross attention
+# ---------------------------------------------------------------------------------------------------------------
+def _check_cross(tdt, rows, lens, heads, share, dh, keys, masked=False, shared=False, seed=0, scale=1.0, extra=0, layout="fused"):
+    torch, N = _mods()
+    rng = np.random.default_rng(seed)
+    S, hk = len(rows), heads // share
+    sets = 1 if shared else S
+    kv = rng.standard_normal((sets, keys, 2, hk, dh)).astype(np.float32)
+    mask = rng.random((S, keys)) < 0.7 if masked else None
+    if masked and S > 1:
+        mask[-1] = False                                               # a sequence whose mask leaves nothing
+    kv = _rounded(kv, tdt)
+    host = _np(kv).copy()
+    hidden = np.arange(keys)[None] >= np.array(lens if lens is not None else [keys] * S)[:, None]
+    if masked:
+        hidden |= ~mask
+    if not shared:
+        kv[torch.as_tensor(hidden)] = float("nan")                     # what nobody sees may hold anything
+    d = kv.cuda()
+    k, v = d[:, :, 0], d[:, :, 1]
+    if layout == "heads":                                              # [S, Hk, L, dh], as attention kernels keep them
+        k, v = (t.transpose(1, 2).contiguous().transpose(1, 2) for t in (k, v))
+    if shared:
+        k, v = k.expand(S, -1, -1, -1), v.expand(S, -1, -1, -1)
+    b, n = _batch(rows, lens, extra=extra)
+    q = _rounded((rng.standard_normal((n, heads, dh)) * scale).astype(np.float32), tdt)
+    out = torch.full((n, heads * dh), 7.0, device="cuda", dtype=tdt)
+    N.cross_attention(N.States(k, v, torch.as_tensor(mask).cuda() if masked else None), b, q.cuda(), out)
+    live = int(np.sum(rows))
+    kf, vf = (np.broadcast_to(host[:, :, i], (S,) + host[:, :, i].shape[1:]) for i in (0, 1))
+    qf = _np(q)
+    want, mag = P.cross_attention(qf[:live], dict(rows=rows, lens=lens if lens is not None else [keys] * S), kf, vf, mask, share)
+    got = _np(out).reshape(n, heads, dh)
+    assert (got[live:] == 7).all()
+    _within(got[:live], want, mag, _largest_score(qf[:live], kf), keys, HALF if tdt == torch.bfloat16 else 0.0)
+    return out
+
+
+@pytest.mark.parametrize("tdt", ["bfloat16", "float32"])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("heads,share,rows,lens,keys,masked", [
+    (4, 1, [1, 1, 1], None, 77, False),                            # single rows
+    (6, 3, [1, 1, 0, 1], [0, 300, 7, 1], 300, True),               # no keys, one key, a mask, an empty mask
+    (2, 1, [130, 40], [220, 61], 220, False),
+    (4, 4, [33, 7, 100], [128, 0, 129], 129, True),
+    (3, 1, [257], None, 1, False)])
+def test_cross(tdt, dh, heads, share, rows, lens, keys, masked):
+    torch, _ = _mods()
+    _check_cross(getattr(torch, tdt), rows, lens, heads, share, dh, keys, masked, seed=dh, extra=2)
+
+
+@pytest.mark.parametrize("tdt", ["bfloat16", "float32"])
+@pytest.mark.parametrize("rows", [1, 3, 8, 9, 16, 17, 60, 127, 128, 129, 300])
+def test_cross_rows_and_keys_around_the_tiles(tdt, rows):
+    torch, _ = _mods()
+    for keys in (1, 15, 64, 127, 128, 129, 256, 500):
+        _check_cross(getattr(torch, tdt), [rows], [keys], 2, 1, 64, keys, seed=rows + keys)
+
+
+@pytest.mark.parametrize("tdt", ["bfloat16", "float32"])
+@pytest.mark.parametrize("rows", [2, 140])
+def test_cross_layouts(tdt, rows):
+    """States laid out by heads, states that all sequences share, lengths beyond the states."""
+    torch, _ = _mods()
+    dt = getattr(torch, tdt)
+    _check_cross(dt, [rows, rows], [90, 40], 4, 2, 64, 90, True, layout="heads")
+    _check_cross(dt, [rows, rows, 1], [90, 40, 90], 4, 2, 64, 90, shared=True)
+    _check_cross(dt, [rows], [1 << 30], 4, 2, 64, 90)
+    _check_cross(dt, [rows], [-3], 4, 2, 64, 90)
+    _check_cross(dt, [rows, 3], [0, 0], 4, 2, 64, 0)
+
+
+@pytest.mark.parametrize("tdt", ["bfloat16", "float32"])
+@pytest.mark.parametrize("rows", [1, 140])
+def test_cross_values(tdt, rows):
+    """NaN in a key that is seen: its rows are NaN.  Scores of -inf: they count for nothing, and alone give zeros."""
+    torch, N = _mods()
+    dt = getattr(torch, tdt)
+    k, v = (torch.randn(1, 200, 1, 64, device="cuda").to(dt) for _ in range(2))
+    q = torch.randn(rows, 1, 64, device="cuda").abs().to(dt)
+    b = N.Batch(rows, n_seqs=1)
+    run = lambda kk: N.cross_attention(N.States(kk, v), b, q, torch.full((rows, 64), 7.0, device="cuda", dtype=dt))
+    bad = k.clone()
+    bad[0, 150, 0, 3] = float("nan")
+    assert run(bad).isnan().all()
+    some, few = k.clone(), N.Batch(rows, torch.tensor([100], device="cuda", dtype=torch.int32))
+    some[0, 100:] = float("-inf")
+    want = N.cross_attention(N.States(k, v), few, q, torch.zeros(rows, 64, device="cuda", dtype=dt))
+    assert (run(some).float() - want.float()).abs().max() <= 2 * HALF * v.float().abs().max()
+    some[0] = float("-inf")
+    assert (run(some) == 0).all()
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# all of them
+# ---------------------------------------------------------------------------------------------------------------
+def test_a_block_step_by_step_equals_all_at_once():
+    """A block's attention as a host runs it, frame by frame: queries, keys and values appended with their rotation, attention over
+    the cache, cross attention to a prompt; against the same rows in one call each."""
+    torch, N = _mods()
+    T, H, dh, F, S = 77, 4, 64, 4, 2
+    g = torch.Generator("cuda").manual_seed(1)
+    qkv = torch.randn(S, F * T, 3 * H * dh, generator=g, device="cuda").bfloat16()
+    enc = torch.randn(S, 50, 2, H, dh, generator=g, device="cuda").bfloat16()
+    rope = N.Rope(*GRID[dh], frame_tokens=T, grid_w=7)
+    i32 = lambda x: torch.tensor(x, device="cuda", dtype=torch.int32)
+    table = i32([[5, 2, 0, 7], [1, 3, 6, 4]])
+    states = N.States(enc[:, :, 0], enc[:, :, 1])
+
+    def run(step):
+        pages = N.Pages.empty("kv4", 8, H, T, dh)
+        out = torch.zeros(2, S, F * T, H * dh, device="cuda", dtype=torch.bfloat16)
+        for f in range(0, F, step):
+            n = step * T
+            rows = qkv[:, f * T:f * T + n].reshape(S * n, 3, H, dh)
+            b = N.Batch(S * n, i32([f * T + n] * S), table)
+            q = torch.empty(S * n, H, dh, device="cuda", dtype=torch.bfloat16)
+            N.kv_append(pages, b, rows[:, 1], rows[:, 2], rope, q=rows[:, 0], q_out=q)
+            o = torch.empty(S * n, H * dh, device="cuda", dtype=torch.bfloat16)
+            N.attention_kv4(pages, b, q, o, frame_tokens=T, window=2)
+            c = torch.empty_like(o)
+            N.cross_attention(states, N.Batch(S * n, n_seqs=S), o, c)
+            out[0, :, f * T:f * T + n], out[1, :, f * T:f * T + n] = o.view(S, n, -1), c.view(S, n, -1)
+        return out, pages
+
+    (one, p1), (many, p2) = run(F), run(1)
+    for a, b in ((p1.k, p2.k), (p1.v, p2.v), (p1.k_scale, p2.k_scale), (p1.v_scale, p2.v_scale)):
+        assert torch.equal(a, b)
+    host = [_np(p1.k), _np(p1.k_scale).view(np.uint16), _np(p1.v), _np(p1.v_scale).view(np.uint16)]
+    turned = P.rotate(_np(qkv).reshape(S * F * T, 3, H, dh)[:, 0], np.tile(np.arange(F * T), S), GRID[dh], 1e4, T, 7)
+    turned = _np(torch.as_tensor(turned).bfloat16())
+    want, mag = P.attention_kv4(turned, dict(rows=[F * T] * S, lens=[F * T] * S), _np(table), host, T, 2, 1)
+    for got in (one, many):
+        _within(_np(got[0]).reshape(S * F * T, H, dh), want, mag, _largest_score(turned, P.kv4_values(*host[:2])), F * T)
+        e = _np(enc)
+        c, m = P.cross_attention(_np(got[0]).reshape(S * F * T, H, dh), dict(rows=[F * T] * S, lens=[50] * S), e[:, :, 0], e[:, :, 1], None, 1)
+        _within(_np(got[1]).reshape(S * F * T, H, dh), c, m, _largest_score(_np(got[0]).reshape(-1, H, dh), e[:, :, 0]), 50)
+
+
+def _one_of_each(seed=0):
+    """Small calls of every kind on the same inputs: a list of (name, call, outputs)."""
+    torch, N = _mods()
+    g = torch.Generator("cuda").manual_seed(seed)
+    i32 = lambda x: torch.tensor(x, device="cuda", dtype=torch.int32)
+    calls = []
+    for rows in (1, 150):
+        pages = N.Pages.empty("kv4", 10, 2, 64, 64)
+        table, start = i32([[0, 2, 4, 6, 8], [9, 7, 5, 3, 1]]), i32([0, rows, 2 * rows])
+        b = N.Batch(2 * rows, i32([300, 280]), table, row_start=start, max_rows=rows)
+        full = N.Batch(580, i32([300, 280]), table, row_start=i32([0, 300, 580]), max_rows=300)
+        x = torch.randn(580, 3, 2, 64, generator=g, device="cuda").bfloat16()
+        q4 = torch.randn(2 * rows, 4, 64, generator=g, device="cuda").bfloat16()
+        qo, o, c = torch.zeros(580, 2, 64, device="cuda").bfloat16(), torch.zeros(2 * rows, 256, device="cuda").bfloat16(), torch.zeros(
+            2 * rows, 256, device="cuda").bfloat16()
+        cf = torch.zeros(2 * rows, 256, device="cuda")
+        ko = torch.zeros(580, 2, 64, device="cuda")
+        st = N.States(x[:300, 1].unsqueeze(0).expand(2, -1, -1, -1), x[:300, 2].unsqueeze(0).expand(2, -1, -1, -1))
+        sf = N.States(x[:300, 1].float().unsqueeze(0).expand(2, -1, -1, -1), x[:300, 2].float().unsqueeze(0).expand(2, -1, -1, -1))
+        rope = N.Rope(64, 0, 0)
+        qf = q4.float()
+        keep = (x, q4, qf)
+        calls += [("append", lambda s=None, p=pages, f=full, x=x, r=rope, qo=qo: N.kv_append(p, f, x[:, 1], x[:, 2], r, q=x[:, 0], q_out=qo, stream=s),
+                   (pages.k, pages.k_scale, pages.v, pages.v_scale, qo), keep),
+                  ("read", lambda s=None, p=pages, f=full, ko=ko: N.pages_read(p, f, ko, None, stream=s), (ko,), keep),
+                  ("kv4", lambda s=None, p=pages, b=b, q=q4, o=o: N.attention_kv4(p, b, q, o, stream=s), (o,), keep),
+                  ("cross", lambda s=None, st=st, b=b, q=q4, c=c: N.cross_attention(st, b, q, c, stream=s), (c,), keep),
+                  ("cross32", lambda s=None, st=sf, b=b, q=qf, c=cf: N.cross_attention(st, b, q, c, stream=s), (cf,), keep)]
+    return calls
+
+
+def test_repeats_are_bitwise_and_nothing_is_allocated():
+    torch, _ = _mods()
+    calls = _one_of_each()
+    for c in calls:
+        c[1]()
+    torch.cuda.synchronize()
+    first = [[t.clone() for t in c[2]] for c in calls]
+    for c in calls:
+        if c[0] != "append":
+            for t in c[2]:
+                t.zero_()
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    for c in calls:
+        c[1]()
+    torch.cuda.synchronize()
+    assert torch.cuda.mem_get_info()[0] == free
+    for c, f in zip(calls, first):
+        assert all(torch.equal(a, b) for a, b in zip(c[2], f)), c[0]
+
+
+def test_captured_and_overlapping_calls():
+    """All calls captured into one graph on a side stream, replayed with other lengths in place; and eager calls on two streams at once."""
+    torch, _ = _mods()
+    calls = _one_of_each(1)
+    for c in calls:
+        c[1]()
+    torch.cuda.synchronize()
+    want = [[t.clone() for t in c[2]] for c in calls]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        for c in calls:
+            c[1]()
+    for c in calls:
+        for t in c[2]:
+            t.zero_()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    for c, f in zip(calls, want):
+        assert all(torch.equal(a, b) for a, b in zip(c[2], f)), c[0]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, c in enumerate(calls):
+            if c[0] != "append":
+                c[1](streams[i % 2])
+    torch.cuda.synchronize()
+    for c, f in zip(calls, want):
+        assert all(torch.equal(a, b) for a, b in zip(c[2], f)), c[0]
+
+
+def test_lengths_are_read_when_the_call_runs():
+    """A captured call, replayed after kv_len, the table and row_start have changed, is the call with the new values."""
+    torch, N = _mods()
+    rng = np.random.default_rng(9)
+    pages, host = _kv4_pool(rng, 12, 2, 32, 64)
+    i32 = lambda x: torch.tensor(x, device="cuda", dtype=torch.int32)
+    for rows in (1, 70):
+        lens, table, start = i32([rows, rows]), i32([[0, 1, 2, 3, 4, 5], [6, 7, 8, 9, 10, 11]]), i32([0, rows, 2 * rows])
+        b = N.Batch(2 * rows, lens, table, row_start=start, max_rows=rows)
+        q = torch.randn(2 * rows, 2, 64, device="cuda").bfloat16()
+        out = torch.zeros(2 * rows, 128, device="cuda").bfloat16()
+        N.attention_kv4(pages, b, q, out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            N.attention_kv4(pages, b, q, out)
+        lens.copy_(i32([190, 77]))
+        table.copy_(table.flip(0))
+        start.copy_(i32([0, rows - 1, 2 * rows - 1]))
+        out.fill_(7.0)
+        graph.replay()
+        got = _np(out).reshape(2 * rows, 2, 64)
+        want, mag = P.attention_kv4(_np(q)[:2 * rows - 1], dict(rows=[rows - 1, rows], lens=[190, 77]), _np(table), host, 1, 1 << 30, 1)
+        _within(got[:-1], want, mag, _largest_score(_np(q), P.kv4_values(*host[:2])), 190)
+        assert (got[-1] == 7).all()
