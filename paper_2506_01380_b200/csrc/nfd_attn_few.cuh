@@ -1,0 +1,481 @@
+// Attention of a few rows to many keys, on 4-bit pages or bf16 states: single tokens, short speculations, a row or two of a
+// decoder against an encoder's states.
+//
+// The rows of a sequence that share a head of keys (rows x heads that share it) are one 16-row operand of mma.m16n8k16; a
+// unit of work is (sequence, head of keys, 16 rows).  The bound is the stream of K and V: a unit is split over the CTAs of a
+// cluster and their warps, each of which takes chunks of KC keys in turn, with a ring of its own in shared memory that
+// cp.async fills NST chunks ahead, an online softmax of its own, and no barrier until the end.  Then the warps of a CTA merge through
+// shared memory and the CTAs of a cluster through distributed shared memory, in a fixed order, each writing its share of the result: no
+// working memory in HBM, one launch.
+//
+// Products take their operands as they lie: the inner index of either product may be permuted as long as both of its
+// operands are, so that a lane's share of a key is a run of its row (for S = Q K^T) and a lane's share of a value a run of dims
+// (for O = P V); 4-bit codes become bf16 numbers in registers: the code goes into the mantissa of 128 + n, 128 + z is
+// subtracted (exact), the step multiplied (exact: 4 by 4 bits).
+#pragma once
+#include "nfd_attn_any.cuh"
+#include "nfd_sm100.cuh"
+
+#define FEW_WARPS 4
+#define FEW_ROWS 16
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, uint32_t bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void *src, uint32_t bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int n> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory"); }
+
+__device__ __forceinline__ void mma_bf16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float few_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// pair i of a word of codes as bf16 numbers: z2 = two bf16 numbers 128 + z, step2 = the step twice
+__device__ __forceinline__ uint32_t kv4_pair(uint32_t codes, int i, uint32_t z2, uint32_t step2) {
+    const uint32_t t = (codes >> (4 * i) & 0x000F000Fu) | 0x43004300u;
+    __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162 *>(&t);
+    a = __hmul2(__hsub2(a, *reinterpret_cast<const __nv_bfloat162 *>(&z2)), *reinterpret_cast<const __nv_bfloat162 *>(&step2));
+    return *reinterpret_cast<const uint32_t *>(&a);
+}
+__device__ __forceinline__ uint32_t kv4_z2(uint32_t w0, uint32_t w1) { return (w0 & 15u) | (w1 & 15u) << 16 | 0x43004300u; }
+__device__ __forceinline__ uint32_t kv4_step2(uint32_t w0, uint32_t w1) { return (w0 & 0xFFF0u) | (w1 & 0xFFF0u) << 16; }
+
+// A warp's chunk of keys in shared memory, for 4-bit pages: codes of K and V, their words, and which keys are there.
+template <int DH> struct FewKv4 {
+    static constexpr bool KV4 = true;
+    static constexpr int KC = 64;
+    static constexpr int RB = DH / 2;                       // bytes of a row of codes
+    static constexpr int WB = DH == 128 ? 8 : 4;            // bytes of a key's words (DH 32: a word and its neighbour)
+    static constexpr int PR = RB / 16;                      // 16-byte pieces of a row
+    static constexpr int STAGE = 2 * KC * (RB + WB) + 16;
+    Kv4Keys<DH> K;
+    long long place[2];                                     // of keys lane, lane + 32 of the chunk after the next one
+
+    __device__ __forceinline__ void look_up(const BatchD &B, int s, int h, int base, int hi) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int p = base + 32 * i + (threadIdx.x & 31);
+            place[i] = -1;
+            if (p < hi) {
+                const long long at = K.P.place(B, s, p);
+                if (at >= 0) place[i] = at + (long long)h * K.P.page_tokens;
+            }
+        }
+    }
+    // the copies of a chunk; its places have been looked up
+    __device__ __forceinline__ void fill(uint8_t *stage, uint32_t st, const BatchD &B, int s, int h, int base, int hi) {
+        const int lane = threadIdx.x & 31;
+        uint32_t *meta = reinterpret_cast<uint32_t *>(stage + 2 * KC * (RB + WB));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t there = __ballot_sync(0xffffffffu, place[i] >= 0), odd = __ballot_sync(0xffffffffu, place[i] & 1);
+            if (lane == 0) meta[i] = there, meta[2 + i] = odd;
+#pragma unroll
+            for (int j = 0; j < PR; ++j) {
+                const int src = j * (32 / PR) + lane / PR, piece = lane % PR;
+                const long long at = __shfl_sync(0xffffffffu, place[i], src);
+                const size_t off = at >= 0 ? (size_t)at * RB + piece * 16 : 0;
+                const uint32_t d = st + (32 * i + src) * RB + piece * 16, n = at >= 0 ? 16 : 0;
+                cp_async16(d, (const uint8_t *)K.P.k + off, n);
+                cp_async16(d + KC * RB, (const uint8_t *)K.P.v + off, n);
+            }
+            const long long at = place[i] >= 0 ? place[i] : 0;
+            const uint32_t d = st + 2 * KC * RB + (32 * i + lane) * WB, n = place[i] >= 0;
+            if (DH == 128) {
+                cp_async8(d, K.P.k_scale + at * 4, n * 8);
+                cp_async8(d + KC * WB, K.P.v_scale + at * 4, n * 8);
+            } else if (DH == 64) {
+                cp_async4(d, K.P.k_scale + at * 2, n * 4);
+                cp_async4(d + KC * WB, K.P.v_scale + at * 2, n * 4);
+            } else {
+                // one word a key: the aligned pair it is in, or, where it is the pair's first, only itself
+                const uint32_t m = n ? 2 + 2 * (uint32_t)(at & 1) : 0;
+                cp_async4(d, K.P.k_scale + (at & ~1LL), m);
+                cp_async4(d + KC * WB, K.P.v_scale + (at & ~1LL), m);
+            }
+        }
+    }
+    __device__ __forceinline__ void masks(const uint8_t *stage, uint32_t *there) const {
+        const uint32_t *meta = reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB));
+        there[0] = meta[0], there[1] = meta[1];
+    }
+    static __device__ __forceinline__ uint32_t word(const uint8_t *w, int key, int group, const uint8_t *stage) {
+        if (DH == 32) {
+            const uint32_t *meta = reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB));
+            return *reinterpret_cast<const uint16_t *>(w + key * WB + 2 * (meta[2 + (key >> 5)] >> (key & 31) & 1));
+        }
+        return *reinterpret_cast<const uint16_t *>(w + key * WB + 2 * group);
+    }
+    // dims of Q that go with this lane's pair i of product step st
+    static __device__ __forceinline__ int q_dim(int step, int c) { return c * (DH / 4) + 4 * step; }
+    // B operand of S for the key of this lane: DH / 16 steps of two registers
+    static __device__ __forceinline__ void k_frag(const uint8_t *stage, int key, int c, uint32_t *b) {
+        constexpr int NW = DH / 32;                         // words of codes of a lane
+        const uint32_t *src = reinterpret_cast<const uint32_t *>(stage + key * RB) + c * NW;
+        uint32_t w[NW];
+        if constexpr (NW == 4) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(src);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else if constexpr (NW == 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(src);
+            w[0] = v.x, w[1] = v.y;
+        } else {
+            w[0] = *src;
+        }
+        const uint32_t sc = word(stage + 2 * KC * RB, key, c * (DH / 4) / 32, stage), z2 = kv4_z2(sc, sc), s2 = kv4_step2(sc, sc);
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[4 * i + j] = kv4_pair(w[i], j, z2, s2);
+    }
+    // dims of the result that this lane's n-th column of product tile t is
+    static __device__ __forceinline__ int o_dim(int t, int n) {
+        if (DH == 32) return 8 * (n >> 1) + 2 * t + (n & 1);
+        return (n * (DH / 64) + t / 8) * 8 + 2 * (t & 3) + ((t >> 2) & 1);
+    }
+    // B operand of O for keys k0 (+4): DH / 8 tiles, one register each
+    static __device__ __forceinline__ void v_frag(const uint8_t *stage, int k0, int n, uint32_t *b) {
+        const uint8_t *v = stage + KC * RB, *w = stage + 2 * KC * RB + KC * WB;
+        const int g = n * (DH / 8) / 32;
+        const uint32_t s0 = word(w, k0, g, stage), s1 = word(w, k0 + 4, g, stage), z2 = kv4_z2(s0, s1), s2 = kv4_step2(s0, s1);
+        if constexpr (DH == 32) {
+            const uint32_t x = *reinterpret_cast<const uint16_t *>(v + k0 * RB + n * 2) |
+                               (uint32_t)*reinterpret_cast<const uint16_t *>(v + (k0 + 4) * RB + n * 2) << 16;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = kv4_pair(x, j, z2, s2);
+        } else {
+            constexpr int NW = DH / 64;
+            uint32_t x[NW], y[NW];
+            if constexpr (NW == 2) {
+                const uint2 p = *reinterpret_cast<const uint2 *>(v + k0 * RB + n * 8), q = *reinterpret_cast<const uint2 *>(v + (k0 + 4) * RB + n * 8);
+                x[0] = p.x, x[1] = p.y, y[0] = q.x, y[1] = q.y;
+            } else {
+                x[0] = *reinterpret_cast<const uint32_t *>(v + k0 * RB + n * 4), y[0] = *reinterpret_cast<const uint32_t *>(v + (k0 + 4) * RB + n * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                const uint32_t even = __byte_perm(x[i], y[i], 0x5410), odd = __byte_perm(x[i], y[i], 0x7632);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) b[8 * i + j] = kv4_pair(even, j, z2, s2), b[8 * i + 4 + j] = kv4_pair(odd, j, z2, s2);
+            }
+        }
+    }
+};
+
+// The same for bf16 states.  Rows are swizzled in 16-byte pieces so that neither operand's reads meet in a bank.
+template <int DH> struct FewStates {
+    static constexpr bool KV4 = false;
+    static constexpr int KC = DH == 128 ? 16 : 32;
+    static constexpr int RB = 2 * DH, PR = RB / 16;
+    static constexpr int STAGE = 2 * KC * RB + 16;
+    StateKeys<bf16, DH> K;
+    uint32_t there;                                         // of the chunk after the next one
+    static __device__ __forceinline__ uint32_t at_k(int key, int piece) { return key * RB + (piece ^ (key & 7 & (PR - 1))) * 16; }
+    static __device__ __forceinline__ uint32_t at_v(int key, int piece) { return KC * RB + key * RB + (piece ^ (2 * key & 7 & (PR - 1))) * 16; }
+
+    __device__ __forceinline__ void look_up(const BatchD &B, int s, int h, int base, int hi) {
+        const int p = base + (threadIdx.x & 31);
+        bool t = p < hi && (threadIdx.x & 31) < KC;
+        if (t && K.mask) t = K.mask[(size_t)s * K.n_keys + p];
+        there = __ballot_sync(0xffffffffu, t);
+    }
+    __device__ __forceinline__ void fill(uint8_t *stage, uint32_t st, const BatchD &B, int s, int h, int base, int hi) {
+        const int lane = threadIdx.x & 31;
+        if (lane == 0) *reinterpret_cast<uint32_t *>(stage + 2 * KC * RB) = there;
+        const long long seq = s * K.seq_stride + h * K.head_stride;
+#pragma unroll
+        for (int j = 0; j < KC * PR / 32; ++j) {
+            const int key = (j * 32 + lane) / PR, piece = lane % PR;
+            const bool t = there >> key & 1;
+            const long long off = t ? seq + (base + key) * K.key_stride + piece * 8 : 0;
+            cp_async16(st + at_k(key, piece), K.k + off, t ? 16 : 0);
+            cp_async16(st + at_v(key, piece), K.v + off, t ? 16 : 0);
+        }
+    }
+    __device__ __forceinline__ void masks(const uint8_t *stage, uint32_t *m) const {
+        m[0] = *reinterpret_cast<const uint32_t *>(stage + 2 * KC * RB), m[1] = 0;
+    }
+    static __device__ __forceinline__ int q_dim(int step, int c) { return 8 * (c + 4 * (step / 2)) + 4 * (step % 2); }
+    static __device__ __forceinline__ void k_frag(const uint8_t *stage, int key, int c, uint32_t *b) {
+#pragma unroll
+        for (int j = 0; j < DH / 32; ++j) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(stage + at_k(key, c + 4 * j));
+            b[4 * j] = v.x, b[4 * j + 1] = v.y, b[4 * j + 2] = v.z, b[4 * j + 3] = v.w;
+        }
+    }
+    static __device__ __forceinline__ int o_dim(int t, int n) { return DH == 32 ? 4 * n + t : 8 * (n + 8 * (t / 8)) + t % 8; }
+    static __device__ __forceinline__ void v_frag(const uint8_t *stage, int k0, int n, uint32_t *b) {
+        if constexpr (DH == 32) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(stage + at_v(k0, n >> 1) + 8 * (n & 1));
+            const uint2 y = *reinterpret_cast<const uint2 *>(stage + at_v(k0 + 4, n >> 1) + 8 * (n & 1));
+            b[0] = __byte_perm(x.x, y.x, 0x5410), b[1] = __byte_perm(x.x, y.x, 0x7632);
+            b[2] = __byte_perm(x.y, y.y, 0x5410), b[3] = __byte_perm(x.y, y.y, 0x7632);
+        } else {
+#pragma unroll
+            for (int i = 0; i < DH / 64; ++i) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(stage + at_v(k0, n + 8 * i)), y = *reinterpret_cast<const uint4 *>(stage + at_v(k0 + 4, n + 8 * i));
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    b[8 * i + 2 * j] = __byte_perm(xs[j], ys[j], 0x5410), b[8 * i + 2 * j + 1] = __byte_perm(xs[j], ys[j], 0x7632);
+            }
+        }
+    }
+};
+
+template <typename Src, int DH> struct FewCfg {
+    static constexpr int NST = 4;
+    static constexpr int STATE = FEW_ROWS * (DH + 2) * 4;                         // O, m, l of a warp or a CTA
+    static constexpr int RING = (NST * Src::STAGE + 15) / 16 * 16;
+    static constexpr int WARP = RING > STATE ? RING : STATE;                      // a warp's ring, then its state
+    static constexpr int SMEM = FEW_WARPS * WARP + STATE;
+};
+
+// grid: (CTAs of a cluster x heads of keys, sequences, tiles of 16 rows)
+template <typename Src, int DH>
+__global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, const AttnRows A, Src src, int split) {
+    using F = FewCfg<Src, DH>;
+    constexpr int KC = Src::KC, NT = DH / 8, NS = DH / 16, KT = KC / 8;
+    extern __shared__ __align__(16) uint8_t few_smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, n = lane >> 2;
+    const int rank = blockIdx.x % split, h = blockIdx.x / split, s = blockIdx.y, r0 = blockIdx.z * FEW_ROWS;
+    const int2 sr = B.rows(s);
+    const int rows = min(sr.y, B.max_rows) * A.share;                             // of the whole unit; row r: row r / share, head h * share + r % share
+    if (r0 >= rows) return;                                                       // (the whole cluster)
+    const int nr = min(FEW_ROWS, rows - r0);
+    // what the rows of this lane see, and all of them together
+    KeyRange kr[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = n + 8 * i;
+        kr[i] = src.K.range(B, s, sr.y, min(r0 + min(r, nr - 1), rows - 1) / A.share);
+    }
+    const KeyRange first = src.K.range(B, s, sr.y, r0 / A.share), last = src.K.range(B, s, sr.y, (r0 + nr - 1) / A.share);
+    // (bounds rise with the row, but for rows of tokens below 0, which see nothing: 0, 0)
+    const int lo = first.lo, hi = last.hi;
+    // queries, scaled for exp2 later: two rows of this lane, DH / 16 steps
+    uint32_t qa[NS][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = n + 8 * i, rr = r0 + min(r, nr - 1);
+        const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (h * A.share + rr % A.share) * DH;
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(q + Src::q_dim(st, c));
+            qa[st][i] = v.x, qa[st][2 + i] = v.y;
+        }
+    }
+    const float cs = 1.4426950408889634f * rsqrtf((float)DH);
+    float o[NT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[t][e] = 0.f;
+    const bool two = nr > 8;                                                      // rows 8 .. 15 are there
+
+    uint8_t *ring = few_smem + warp * F::WARP;
+    const uint32_t ring_s = smem_u32(ring);
+    const int step = split * FEW_WARPS * KC;
+    int next = lo + (rank * FEW_WARPS + warp) * KC;                               // next chunk to fill
+    int base = next;
+    src.look_up(B, s, h, next, hi);
+#pragma unroll
+    for (int i = 0; i < F::NST - 1; ++i) {
+        if (next < hi) {
+            src.fill(ring + i * Src::STAGE, ring_s + i * Src::STAGE, B, s, h, next, hi);
+            next += step;
+            src.look_up(B, s, h, next, hi);
+        }
+        cp_async_commit();
+    }
+    int st = 0;
+    for (; base < hi; base += step) {
+        {
+            const int f = st == 0 ? F::NST - 1 : st - 1;
+            if (next < hi) {
+                src.fill(ring + f * Src::STAGE, ring_s + f * Src::STAGE, B, s, h, next, hi);
+                next += step;
+                src.look_up(B, s, h, next, hi);
+            }
+            cp_async_commit();
+        }
+        cp_async_wait<F::NST - 1>();
+        __syncwarp();
+        const uint8_t *stage = ring + st * Src::STAGE;
+        uint32_t there[2];
+        src.masks(stage, there);
+        float x[KT][4];
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            // column j of tile u is key 8 u + j / 2 + 4 (j % 2): a lane's four keys of a product step over P are 4 apart
+            uint32_t b[2 * NS];
+            Src::k_frag(stage, 8 * u + (n >> 1) + 4 * (n & 1), c, b);
+            x[u][0] = x[u][1] = x[u][2] = x[u][3] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NS; ++k) mma_bf16(x[u], qa[k], b[2 * k], b[2 * k + 1]);
+        }
+        const bool all = (there[0] & (KC >= 32 ? 0xffffffffu : (1u << KC) - 1)) == (KC >= 32 ? 0xffffffffu : (1u << KC) - 1) &&
+                         (KC <= 32 || there[1] == 0xffffffffu);
+        const bool inside = base >= kr[0].lo && base >= kr[1].lo && base + KC <= kr[0].hi && base + KC <= kr[1].hi;
+        if (!__all_sync(0xffffffffu, all && inside)) {
+#pragma unroll
+            for (int u = 0; u < KT; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = 8 * u + c + 4 * (e & 1), p = base + key;
+                    const bool seen = (there[key >> 5] >> (key & 31) & 1) && p >= kr[e >> 1].lo && p < kr[e >> 1].hi;
+                    if (!seen) x[u][e] = -INFINITY;
+                }
+        }
+        // the rows' maxima; what was summed before is rescaled only where one rose
+        float mn[2] = {m[0], m[1]};
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            mn[0] = fmaxf(mn[0], fmaxf(x[u][0], x[u][1]));
+            mn[1] = fmaxf(mn[1], fmaxf(x[u][2], x[u][3]));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            mn[i] = fmaxf(mn[i], __shfl_xor_sync(0xffffffffu, mn[i], 1));
+            mn[i] = fmaxf(mn[i], __shfl_xor_sync(0xffffffffu, mn[i], 2));
+        }
+        if (__any_sync(0xffffffffu, mn[0] != m[0] || mn[1] != m[1])) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float f = mn[i] == m[i] ? 1.0f : few_exp2((m[i] - mn[i]) * cs);
+                m[i] = mn[i], l[i] *= f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) o[t][2 * i] *= f, o[t][2 * i + 1] *= f;
+            }
+        }
+        const float mc[2] = {m[0] == -INFINITY ? 0.f : m[0] * cs, m[1] == -INFINITY ? 0.f : m[1] * cs};
+        uint32_t p[KT][2];
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            const float a = few_exp2(fmaf(x[u][0], cs, -mc[0])), b = few_exp2(fmaf(x[u][1], cs, -mc[0]));
+            l[0] += a + b, p[u][0] = bf16_pair(a, b), p[u][1] = 0;
+            if (two) {
+                const float d = few_exp2(fmaf(x[u][2], cs, -mc[1])), e = few_exp2(fmaf(x[u][3], cs, -mc[1]));
+                l[1] += d + e, p[u][1] = bf16_pair(d, e);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < KT / 2; ++j) {
+            const uint32_t a[4] = {p[2 * j][0], p[2 * j][1], p[2 * j + 1][0], p[2 * j + 1][1]};
+            uint32_t b0[NT], b1[NT];
+            Src::v_frag(stage, 16 * j + c, n, b0);
+            Src::v_frag(stage, 16 * j + 8 + c, n, b1);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma_bf16(o[t], a, b0[t], b1[t]);
+        }
+        __syncwarp();                                                             // the stage may be filled again
+        if (++st == F::NST) st = 0;
+    }
+    cp_async_wait<0>();
+    __syncwarp();
+    // this warp's state into its (drained) ring
+    float *S = reinterpret_cast<float *>(ring);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+        if (c == 0) S[FEW_ROWS * DH + 2 * (n + 8 * i)] = m[i] * cs, S[FEW_ROWS * DH + 2 * (n + 8 * i) + 1] = l[i];
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[(n + 8 * (e >> 1)) * DH + Src::o_dim(t, 2 * c + (e & 1))] = o[t][e];
+    __syncthreads();
+    // the CTA's
+    float *T = reinterpret_cast<float *>(few_smem + FEW_WARPS * F::WARP);
+    auto write = [&](int r, int d, float4 v, float sum) {
+        const int rr = r0 + r;
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + h * A.share + rr % A.share) * DH + d;
+        *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
+    };
+    for (int i = threadIdx.x; i < nr * (DH / 4); i += 32 * FEW_WARPS) {
+        const int r = i / (DH / 4), d = i % (DH / 4) * 4;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w) mx = fmaxf(mx, reinterpret_cast<const float *>(few_smem + w * F::WARP)[FEW_ROWS * DH + 2 * r]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w) {
+            const float *W = reinterpret_cast<const float *>(few_smem + w * F::WARP);
+            const float mw = W[FEW_ROWS * DH + 2 * r], f = mw == -INFINITY ? 0.f : few_exp2(mw - mx);
+            const float4 x = *reinterpret_cast<const float4 *>(W + r * DH + d);
+            sum = fmaf(W[FEW_ROWS * DH + 2 * r + 1], f, sum);
+            v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+        }
+        if (split == 1) {
+            write(r, d, v, sum);
+        } else {
+            *reinterpret_cast<float4 *>(T + r * DH + d) = v;
+            if (d == 0) T[FEW_ROWS * DH + 2 * r] = mx, T[FEW_ROWS * DH + 2 * r + 1] = sum;
+        }
+    }
+    if (split == 1) return;
+    // the cluster's: every CTA a share of the row words
+    cluster_sync_all();
+    const uint32_t Ts = smem_u32(T);
+    for (int i = rank + split * threadIdx.x; i < nr * (DH / 4); i += split * 32 * FEW_WARPS) {
+        const int r = i / (DH / 4), d = i % (DH / 4) * 4;
+        float mx = -INFINITY;
+        for (int k = 0; k < split; ++k) mx = fmaxf(mx, ld_cluster_f2(cluster_map(Ts + (FEW_ROWS * DH + 2 * r) * 4, k)).x);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+        for (int k = 0; k < split; ++k) {
+            const float2 ml = ld_cluster_f2(cluster_map(Ts + (FEW_ROWS * DH + 2 * r) * 4, k));
+            const float4 x = ld_cluster_f4(cluster_map(Ts + (r * DH + d) * 4, k));
+            const float f = ml.x == -INFINITY ? 0.f : few_exp2(ml.x - mx);
+            sum = fmaf(ml.y, f, sum);
+            v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+        }
+        write(r, d, v, sum);
+    }
+    cluster_sync_all();                                                           // nobody leaves while its state is read
+}
+
+// CTAs of a cluster that a unit is split over.
+static int few_split(int units, long long keys, int kc, int n_sm) {
+    const long long chunks = (keys + kc - 1) / kc;
+    int split = 1;
+    while (split < 8 && (long long)units * split * 2 <= 3LL * n_sm && chunks > (long long)split * FEW_WARPS) split *= 2;
+    return split;
+}
+
+template <typename Src, int DH>
+static int launch_attn_few(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int n_sm, cudaStream_t st) {
+    using F = FewCfg<Src, DH>;
+    const int tiles = (B.max_rows * A.share + FEW_ROWS - 1) / FEW_ROWS;
+    const int split = few_split((int)fmin(1e6, (double)kv_heads * B.n_seqs * tiles), keys, Src::KC, n_sm);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kv_heads * split, B.n_seqs, tiles), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = F::SMEM, cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at, cfg.numAttrs = split > 1;
+    if (cudaFuncSetAttribute(k_attn_few<Src, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
+        cudaLaunchKernelEx(&cfg, k_attn_few<Src, DH>, B, A, src, split) != cudaSuccess) {
+        cudaGetLastError();
+        return NFD_E_CUDA;
+    }
+    return NFD_OK;
+}

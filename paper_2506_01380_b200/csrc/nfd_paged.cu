@@ -5,7 +5,7 @@
 #include <string.h>
 
 #include "nfd_append.cuh"
-#include "nfd_attn_any.cuh"
+#include "nfd_attn_few.cuh"
 
 #define CK(call)                                                                                   \
     do {                                                                                           \
@@ -181,9 +181,16 @@ int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_head
     if (frame_tokens < 1 || frame_tokens > (1 << 20) || window < 0) return NFD_E_RANGE;
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
     const AttnRows A = {q, out, q_stride, n_heads, n_heads / P.heads};
+    int n_sm = 0;
+    RET(sm_count(n_sm));
+    // the most keys that a unit's rows can see: what the tables hold, what the window leaves
+    const long long held = (long long)B.table_len * P.page_tokens, seen = ((long long)window + 1) * frame_tokens + B.max_rows;
+    const long long keys = held < seen ? held : seen;
     return by_head_dim(pages->head_dim, [&](auto d) -> int {
         constexpr int DH = decltype(d)::value;
-        return launch_attn_any<bf16, DH>(B, A, Kv4Keys<DH>{P, {frame_tokens, window}}, (cudaStream_t)cuda_stream);
+        FewKv4<DH> src;
+        src.K = {P, {frame_tokens, window}};
+        return launch_attn_few<FewKv4<DH>, DH>(B, A, src, P.heads, keys, n_sm, (cudaStream_t)cuda_stream);
     });
 }
 
@@ -209,11 +216,18 @@ int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_
     if (!aligned(out, 16)) return NFD_E_ALIGN;
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
     const AttnRows A = {q, out, q_stride, n_heads, n_heads / states->n_heads};
+    int n_sm = 0;
+    RET(sm_count(n_sm));
     return by_head_dim(dh, [&](auto d) -> int {
         constexpr int DH = decltype(d)::value;
         auto go = [&](auto *t) -> int {
             using TS = std::remove_pointer_t<decltype(t)>;
             const StateKeys<TS, DH> K = {(const TS *)states->k, (const TS *)states->v, states->mask, st[0], st[1], st[2], states->n_keys};
+            if constexpr (std::is_same_v<TS, bf16>) {
+                FewStates<DH> src;
+                src.K = K;
+                return launch_attn_few<FewStates<DH>, DH>(B, A, src, states->n_heads, states->n_keys, n_sm, (cudaStream_t)cuda_stream);
+            }
             return launch_attn_any<TS, DH>(B, A, K, (cudaStream_t)cuda_stream);
         };
         return dtype == NFD_DTYPE_BF16 ? go((bf16 *)nullptr) : go((float *)nullptr);
