@@ -312,7 +312,7 @@ int nfd_pages_read(const nfd_pages *pages, const nfd_batch *batch, int dtype, vo
  * tokens of the frames max(0, frame - window) .. frame that the cache holds
  * (frame_tokens = 1: a causal mask over the last window + 1 tokens).
  * The scale is 1 / sqrt(head_dim).  A row that sees nothing, or nothing but scores
- * of -inf, gives zeros.  Scores, softmax and sums are fp32; probabilities are rounded to bf16 for
+ * of -inf, gives zeros; a row that sees a value that is not finite is NaN.  Scores, softmax and sums are fp32; probabilities are rounded to bf16 for
  * the product with V.  Should a device-side wait run out, the rows concerned are NaN. */
 int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,
                       int frame_tokens, int window, void *out, void *cuda_stream);

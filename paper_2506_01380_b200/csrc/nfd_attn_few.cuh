@@ -115,6 +115,38 @@ template <int DH> struct FewKv4 {
         const uint32_t *meta = reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB));
         there[0] = meta[0], there[1] = meta[1];
     }
+    // Values whose step is not finite become zeros (a product with the 0 of a row that does not see them would be NaN); a bit for each
+    // of their keys.  True: there are some.
+    static __device__ __forceinline__ bool take_out(uint8_t *stage, uint32_t *bad) {
+        const int lane = threadIdx.x & 31;
+        bool mine[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t *w = reinterpret_cast<uint32_t *>(stage + 2 * KC * RB + KC * WB + (32 * i + lane) * WB);
+            mine[i] = false;
+#pragma unroll
+            for (int j = 0; j < WB / 4; ++j) {
+                const uint32_t v = w[j];
+                const bool b0 = (v & 0x7F80u) == 0x7F80u, b1 = (v >> 16 & 0x7F80u) == 0x7F80u;
+                if (DH == 32) {
+                    const uint32_t *meta = reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB));
+                    mine[i] |= meta[2 + i] >> lane & 1 ? b1 : b0;
+                } else {
+                    mine[i] |= b0 || b1;
+                }
+            }
+        }
+        if (!__any_sync(0xffffffffu, mine[0] || mine[1])) return false;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t *w = reinterpret_cast<uint32_t *>(stage + 2 * KC * RB + KC * WB + (32 * i + lane) * WB);
+            if (mine[i])
+                for (int j = 0; j < WB / 4; ++j) w[j] = 0;
+            bad[i] = __ballot_sync(0xffffffffu, mine[i]);
+        }
+        __syncwarp();
+        return true;
+    }
     static __device__ __forceinline__ uint32_t word(const uint8_t *w, int key, int group, const uint8_t *stage) {
         if (DH == 32) {
             const uint32_t *meta = reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB));
@@ -211,6 +243,7 @@ template <int DH> struct FewStates {
     __device__ __forceinline__ void masks(const uint8_t *stage, uint32_t *m) const {
         m[0] = *reinterpret_cast<const uint32_t *>(stage + 2 * KC * RB), m[1] = 0;
     }
+    static __device__ __forceinline__ bool take_out(uint8_t *, uint32_t *) { return false; }     // (all rows see the same keys)
     static __device__ __forceinline__ int q_dim(int step, int c) { return 8 * (c + 4 * (step / 2)) + 4 * (step % 2); }
     static __device__ __forceinline__ void k_frag(const uint8_t *stage, int key, int c, uint32_t *b) {
 #pragma unroll
@@ -317,8 +350,8 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
         }
         cp_async_wait<F::NST - 1>();
         __syncwarp();
-        const uint8_t *stage = ring + st * Src::STAGE;
-        uint32_t there[2];
+        uint8_t *stage = ring + st * Src::STAGE;
+        uint32_t there[2], bad[2];
         src.masks(stage, there);
         float x[KT][4];
 #pragma unroll
@@ -343,6 +376,11 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
                     if (!seen) x[u][e] = -INFINITY;
                 }
         }
+        if (Src::take_out(stage, bad))
+            for (int key = 0; key < KC; ++key)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if ((bad[key >> 5] >> (key & 31) & 1) && base + key >= kr[i].lo && base + key < kr[i].hi) l[i] = NAN;
         // the rows' maxima; what was summed before is rescaled only where one rose
         float mn[2] = {m[0], m[1]};
 #pragma unroll

@@ -381,6 +381,29 @@ def test_kv4_what_is_not_seen_is_not_looked_at(rows):
         assert torch.equal(out.view(n, 2, 64)[:-20], again.view(n, 2, 64)[:-20])
 
 
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("rows", [2, 150])
+def test_kv4_values_that_are_not_finite(rows, dh):
+    """A NaN in a value makes the rows that see it NaN, and no others: not the rows before it that share its tile."""
+    torch, N = _mods()
+    rng = np.random.default_rng(8)
+    pages, host = _kv4_pool(rng, 8, 2, 40, dh)
+    length, table = 290, np.arange(8, dtype=np.int32)[None]
+    b, n = _batch([rows], [length], table)
+    q = torch.randn(n, 2, dh, device="cuda").bfloat16()
+    out, again = (torch.zeros(n, 2 * dh, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    N.attention_kv4(pages, b, q, out)
+    t = length - 1 if rows == 2 else length - 33
+    for group in range(dh // 32):
+        keep = pages.v_scale[t // 40, 1, t % 40, group].clone()
+        pages.v_scale[t // 40, 1, t % 40, group] = 0x7FC0
+        N.attention_kv4(pages, b, q, again)
+        pages.v_scale[t // 40, 1, t % 40, group] = keep
+        first = t - (length - rows)                                    # the first row that sees it
+        o, a = out.view(n, 2, dh), again.view(n, 2, dh)
+        assert a[first:, 1].isnan().all() and torch.equal(a[:first], o[:first]) and torch.equal(a[:, 0], o[:, 0])
+
+
 def test_kv4_offsets_beyond_32_bits():
     """A cache of more than 2^32 bytes of codes, with the sequence's pages at its end."""
     torch, N = _mods()
