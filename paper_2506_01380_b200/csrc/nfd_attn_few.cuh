@@ -501,7 +501,7 @@ static int few_split(int units, long long keys, int kc, int n_sm) {
 }
 
 template <typename Src, int DH>
-static int launch_attn_few(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int n_sm, cudaStream_t st) {
+static int launch_attn_few(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
     using F = FewCfg<Src, DH>;
     const int tiles = (B.max_rows * A.share + FEW_ROWS - 1) / FEW_ROWS;
     const int split = few_split((int)fmin(1e6, (double)kv_heads * B.n_seqs * tiles), keys, Src::KC, n_sm);
@@ -510,8 +510,12 @@ static int launch_attn_few(const BatchD &B, const AttnRows &A, const Src &src, i
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at, cfg.numAttrs = split > 1;
-    if (cudaFuncSetAttribute(k_attn_few<Src, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
-        cudaLaunchKernelEx(&cfg, k_attn_few<Src, DH>, B, A, src, split) != cudaSuccess) {
+    static bool sized[NFD_PAGED_DEVICES];                                         // (once per device and kernel)
+    if (!sized[dev]) {
+        if (cudaFuncSetAttribute(k_attn_few<Src, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess) return NFD_E_CUDA;
+        sized[dev] = true;
+    }
+    if (cudaLaunchKernelEx(&cfg, k_attn_few<Src, DH>, B, A, src, split) != cudaSuccess) {
         cudaGetLastError();
         return NFD_E_CUDA;
     }

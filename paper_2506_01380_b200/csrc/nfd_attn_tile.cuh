@@ -1,20 +1,22 @@
 // Attention of many rows on tcgen05 / TMEM, on 4-bit pages or bf16 states.
 //
 // The rows of a sequence that share a head of keys (rows x heads that share it) are cut into tiles of 128.  A CTA takes one
-// tile, whose key blocks its two softmax groups take in turn ("by keys"), or two tiles, one to a group, that share every
-// key block ("by rows": half the copies and, for 4-bit pages, half the conversions).  Either way the work is a list of jobs
-// (block, group), and the groups know nothing of one another until the end: each has an S accumulator, P, O, m and l of
+// tile, whose key blocks its softmax groups take in turn, or a tile for every group, which share every
+// key block (a third or half of the copies and, for 4-bit pages, of the conversions).  Either way the work is a list of jobs
+// (block, group), and the groups know nothing of one another until the end: each has its S accumulators, O, m and l of
 // its own.  Per job
 //     S = Q K^T     UMMA 128 x KB x DH, operands in shared memory, accumulator in tensor memory
-//     P = exp2(S c - m)   one thread per row: the whole row of S to registers, which frees S for the group's next job but one,
-//                   maximum, exponentials, P as bf16 to tensor memory
+//     P = exp2(S c - m)   one thread per row: S by columns to registers, exponentials, P as bf16 over the S it came from
 //     O += P V      UMMA 128 x 64 x KB, P from tensor memory, V as it lies (MN-major)
-// m follows the running maximum only when that has risen by more than 8 (a factor of 256, which neither bf16 nor fp32 minds);
-// then the row's O is rescaled in tensor memory by its thread.
+// m is the row's maximum over the group's first block, and no maximum is taken of later blocks: a probability is exact to the
+// same number of bits whatever its size.  Where a block's sum of a row passes 2^60 after all (or is NaN), the warp takes the block
+// again, S being untouched so far: maxima first, and where one has risen by more than 8 (a factor of 256) it becomes m and
+// the row's O is rescaled in tensor memory by its thread.  First blocks and blocks with keys that some row of the warp does not see
+// go the same way.
 //
-// Warps 0-3 fill the rings of K and V blocks: bf16 states with cp.async, several blocks in flight; 4-bit pages through
-// registers, one block ahead, the codes becoming bf16 numbers on the way.  Warp 4 issues the products, warps 8-15 are the softmax
-// groups; registers are split 72 : 184.  Which keys of a block are there is left beside the V block, a bit each.
+// Warps 0 .. PW-1 fill the rings of K and V blocks: bf16 states with cp.async, several blocks in flight; 4-bit pages through
+// registers, one block ahead, the codes becoming bf16 numbers on the way.  Warp PW issues the products, the last 4 NG are the softmax
+// groups.  Which keys of a block are there is left beside the V block, a bit each.
 //
 // A unit (sequence, head of keys, tile) with many keys and few others beside it is split over the CTAs of a cluster, which
 // merge through distributed shared memory.  Every wait is bounded; after one that ran out the rows are NaN.
@@ -32,8 +34,6 @@ __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity) {
         if ((++spins & 0x3ff) == 0 && global_timer_ns() - t0 > NFD_WAIT_LIMIT_NS) return false;
     return true;
 }
-template <int n> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(n)); }
-template <int n> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(n)); }
 // registers that a tensor-memory load has filled are not touched before this point (which comes after its wait)
 __device__ __forceinline__ void loaded32(float *x) {
     asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]),
@@ -41,20 +41,28 @@ __device__ __forceinline__ void loaded32(float *x) {
     asm volatile("" : "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]),
                       "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31]));
 }
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void loaded16(float *x) {
+    asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]),
+                      "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]));
+}
 
 template <int DH> struct TileCfg {
-    static constexpr int KB = DH == 128 ? 64 : 128;        // keys of a block: S, P and O of both groups fill tensor memory
     static constexpr int SUB = DH == 128 ? 2 : 1;          // 64-dim parts of a row
+    static constexpr int NG = DH == 128 ? 2 : 3;           // softmax groups
+    static constexpr int KB = DH == 128 ? 64 : 96;         // keys of a block
+    static constexpr int NB = DH == 128 ? 2 : 1;           // S accumulators of a group
+    static constexpr int PW = DH == 128 ? 4 : 3;           // producer warps
+    static constexpr int SM0 = 16 - 4 * NG;                // first softmax warp
     static constexpr int NST = 4;                          // blocks in the ring of K, and in that of V
     static constexpr int Q_BYTES = SUB * 128 * 128;        // a tile's queries
-    static constexpr int BLK = SUB * KB * 128;             // a block of K or V: 16 KiB
-    static constexpr int AT_Q = 0, AT_K = 2 * Q_BYTES, AT_V = AT_K + NST * BLK, AT_MASK = AT_V + NST * BLK,
+    static constexpr int BLK = SUB * KB * 128;             // a block of K or V
+    static constexpr int AT_Q = 0, AT_K = NG * Q_BYTES, AT_V = AT_K + NST * BLK, AT_MASK = AT_V + NST * BLK,
                          AT_BAR = AT_MASK + NST * 32, SMEM = AT_BAR + 8 * 32 + 1024;
-    static constexpr int TM_P = 2 * KB, TM_O = 3 * KB;     // S of group g at g KB, P at TM_P + g KB / 2, O at TM_O + g 64 SUB
+    static constexpr int TM_O = NG * NB * KB;              // S, and over it P, of group g's buffer i at (g NB + i) KB; O at TM_O + g 64 SUB
     // a group's state, over queries and rings: O as [DH / 4][128] float4, then [128] (m, l)
     static constexpr int STATE = 128 * DH * 4 + 128 * 8;
-    static_assert(TM_O + 2 * 64 * SUB <= 512 && 2 * STATE <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
+    static_assert(TM_O + NG * 64 * SUB <= 512 && NG * STATE <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
+    static_assert(PW * 32 == KB * SUB, "a thread for 64 dims of a key");
 };
 
 struct TileBars {
@@ -64,22 +72,19 @@ struct TileBars {
     __device__ __forceinline__ uint32_t k_empty(int s) const { return b + 32 + 8 * s; }
     __device__ __forceinline__ uint32_t v_full(int s) const { return b + 64 + 8 * s; }
     __device__ __forceinline__ uint32_t v_empty(int s) const { return b + 96 + 8 * s; }
-    // per group
-    __device__ __forceinline__ uint32_t s_full(int g) const { return b + 128 + 8 * g; }
-    __device__ __forceinline__ uint32_t s_free(int g) const { return b + 144 + 8 * g; }
-    __device__ __forceinline__ uint32_t p_full(int g) const { return b + 160 + 8 * g; }
-    __device__ __forceinline__ uint32_t pv_done(int g) const { return b + 176 + 8 * g; }
-    __device__ __forceinline__ uint32_t q_full() const { return b + 192; }
-    __device__ __forceinline__ void init() const {
+    // per accumulator, per group
+    __device__ __forceinline__ uint32_t s_full(int i) const { return b + 128 + 8 * i; }
+    __device__ __forceinline__ uint32_t p_full(int i) const { return b + 160 + 8 * i; }
+    __device__ __forceinline__ uint32_t pv_done(int g) const { return b + 192 + 8 * g; }
+    __device__ __forceinline__ uint32_t q_full() const { return b + 216; }
+    __device__ __forceinline__ void init(int producers) const {
         for (int s = 0; s < 4; ++s) {
-            mbar_init(k_full(s), 4), mbar_init(v_full(s), 4);          // a producer warp each
+            mbar_init(k_full(s), producers), mbar_init(v_full(s), producers);      // a producer warp each
             mbar_init(k_empty(s), 1), mbar_init(v_empty(s), 1);
+            mbar_init(s_full(s), 1), mbar_init(p_full(s), 4);                      // a softmax warp each
         }
-        for (int g = 0; g < 2; ++g) {
-            mbar_init(s_full(g), 1), mbar_init(pv_done(g), 1);
-            mbar_init(s_free(g), 4), mbar_init(p_full(g), 4);          // a softmax warp each
-        }
-        mbar_init(q_full(), 4);
+        for (int g = 0; g < 3; ++g) mbar_init(pv_done(g), 1);
+        mbar_init(q_full(), producers);
         fence_mbar_init();
     }
 };
@@ -95,12 +100,26 @@ __device__ __forceinline__ void tile_publish(uint32_t bar) {
     if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
 }
 
+// The queries of the CTA's tiles; rows that are not there are zeros.
+template <int DH>
+__device__ __forceinline__ void tile_queries(const BatchD &B, const AttnRows &A, uint32_t sq, int first, int r0, int nr, int h, int tiles) {
+    using C = TileCfg<DH>;
+    constexpr int CPR = DH / 8;
+    for (int i = threadIdx.x; i < tiles * 128 * CPR; i += C::PW * 32) {
+        const int r = i / CPR, piece = i % CPR, rr = r0 + min(r, nr - 1);
+        const bf16 *q = (const bf16 *)A.q + (long long)(first + rr / A.share) * A.q_stride + (h * A.share + rr % A.share) * DH + piece * 8;
+        cp_async16(sq + (r >> 7) * C::Q_BYTES + (piece >> 3) * (128 * 128) + tile_at(r & 127, piece & 7), q, r < nr ? 16 : 0);
+    }
+    cp_async_commit();
+}
+
 // ---- producers: bf16 states ---------------------------------------------------------------------------------
 template <int DH> struct TileStates {
     StateKeys<bf16, DH> K;
-    __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok) const {
+    template <typename F> __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok, F &&queries) const {
         using C = TileCfg<DH>;
-        constexpr int CPR = DH / 8, N = C::KB * CPR / 128;            // 16-byte pieces of a row, of a thread
+        constexpr int CPR = DH / 8, NT = C::PW * 32, RS = NT / CPR, N = C::KB / RS;       // 16-byte pieces of a row; threads; rows a step, steps
+        static_assert(C::KB % RS == 0, "pieces");
         const int t = threadIdx.x, piece = t % CPR, row0 = t / CPR, lane = t & 31;
         const uint32_t base = smem_u32(smem);
         const long long seq = w.s * K.seq_stride + w.h * K.head_stride + piece * 8;
@@ -111,16 +130,17 @@ template <int DH> struct TileStates {
             const int p0 = w.lo + b * C::KB;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int p = p0 + row0 + i * (128 / CPR);
+                const int p = p0 + row0 + i * RS;
                 m |= (uint32_t)(p < w.hi && (!mask || mask[p])) << i;
             }
             const int p = p0 + t;
             return m | (uint32_t)(t < C::KB && p < w.hi && (!mask || mask[p])) << 31;
         };
-        int done = 0, item = 0;                                       // items (K of block 0, V of block 0, K ...) published, begun
+        queries();
+        int done = -1, item = 0;                                      // items (queries, K of block 0, V of block 0, K ...) published, begun
         auto publish = [&]() {
             const int st = (done >> 1) % C::NST;
-            tile_publish(done & 1 ? bars.v_full(st) : bars.k_full(st));
+            tile_publish(done < 0 ? bars.q_full() : done & 1 ? bars.v_full(st) : bars.k_full(st));
             ++done;
         };
         uint32_t bits = there(0);
@@ -141,7 +161,7 @@ template <int DH> struct TileStates {
                 const uint32_t dst = base + (kv ? C::AT_V : C::AT_K) + st * C::BLK + (piece >> 3) * (C::KB * 128);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int row = row0 + i * (128 / CPR);
+                    const int row = row0 + i * RS;
                     const bool here = bits >> i & 1;
                     const long long off = here ? seq + (long long)(w.lo + b * C::KB + row) * K.key_stride : 0;
                     cp_async16(dst + tile_at(row, piece & 7), src + off, here ? 16 : 0);
@@ -149,7 +169,8 @@ template <int DH> struct TileStates {
                 cp_async_commit();
                 if (kv) {
                     const uint32_t m = __ballot_sync(0xffffffffu, bits >> 31);
-                    if (lane == 0) reinterpret_cast<uint32_t *>(smem + C::AT_MASK)[st * 8 + (t >> 5)] = m, reinterpret_cast<uint32_t *>(smem + C::AT_MASK)[st * 8 + 4 + (t >> 5)] = 0;
+                    uint32_t *M = reinterpret_cast<uint32_t *>(smem + C::AT_MASK) + st * 8 + (t >> 5);
+                    if (lane == 0) M[0] = m, M[4] = 0;
                 }
                 ++item;
                 if (item - done > 3) {
@@ -197,7 +218,7 @@ template <int DH> struct TileKv4 {
                 make_uint4(kv4_pair(r.c[i], 0, z2, s2), kv4_pair(r.c[i], 1, z2, s2), kv4_pair(r.c[i], 2, z2, s2), kv4_pair(r.c[i], 3, z2, s2));
         }
     }
-    __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok) const {
+    template <typename F> __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok, F &&queries) const {
         using C = TileCfg<DH>;
         const int t = threadIdx.x, key = t / SUBS, sub = t % SUBS, lane = t & 31;
         auto look_up = [&](int b) -> long long {
@@ -210,6 +231,9 @@ template <int DH> struct TileKv4 {
         long long place = look_up(0), next = look_up(1);
         load(k, K.P.k, K.P.k_scale, place, sub);
         load(v, K.P.v, K.P.v_scale, place, sub);
+        queries();
+        cp_async_wait<0>();
+        tile_publish(bars.q_full());
         for (int b = 0; b < w.nb && ok; ++b) {
             const int st = b % C::NST, par = (b / C::NST - 1) & 1;
             const uint32_t m = __ballot_sync(0xffffffffu, place >= 0);
@@ -250,22 +274,86 @@ template <int DH> struct TileKv4 {
     }
 };
 
-// Grid: x = split x (heads of keys), y = sequences, z = tiles (of 128 rows, or of 256 with `pairs`).
-template <typename Src, int DH>
-__global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, const AttnRows A, const Src src, int split, int pairs) {
+// S of a block that some row of the warp does not see in whole, or whose sums have outgrown m, or the group's first: the
+// row's maximum over the keys that it sees, m and what has been summed so far adjusted to it, then P.
+// seen: bits of the keys that the row sees; n: the group's jobs before this one.
+template <int DH>
+static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, uint32_t seen0, uint32_t seen1, uint32_t seen2, float c, int n,
+                                              uint32_t pv_done, float &m_io, float &l_io, bool &ok) {
     using C = TileCfg<DH>;
-    constexpr int KB = C::KB, SUB = C::SUB;
+    float m = m_io, l = l_io, top = -INFINITY;
+    const uint32_t seen[3] = {seen0, seen1, seen2};
+#pragma unroll
+    for (int k = 0; k < C::KB / 32; ++k)
+#pragma unroll 1
+        for (int i = 0; i < 32; i += 16) {
+            float x[16];
+            tmem_ld16(tS + 32 * k + i, reinterpret_cast<uint32_t *>(x));
+            tmem_ld_wait();
+            loaded16(x);
+            const uint32_t s = seen[k] >> i;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s >> e & 1 ? x[e] : -INFINITY);
+        }
+    // (m starts at -inf: the first score that is seen sets it)
+    const bool rise = top * c > m * c + 8.0f || (m == -INFINITY && top != -INFINITY);
+    if (__any_sync(0xffffffffu, rise)) {
+        const float f = !rise ? 1.0f : m == -INFINITY ? 0.f : few_exp2((m - top) * c);
+        if (rise) m = top;
+        l *= f;
+        if (n) {
+            ok = ok && tile_wait(pv_done, (n - 1) & 1);                // O is at rest
+            __syncwarp();
+            tc_fence_after();
+#pragma unroll 1
+            for (int i = 0; i < DH; i += 16) {
+                float o[16];
+                tmem_ld16(tO + i, reinterpret_cast<uint32_t *>(o));
+                tmem_ld_wait();
+                loaded16(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = f == 0.f ? 0.f : o[e] * f;
+                tmem_st16(tO + i, reinterpret_cast<uint32_t *>(o));
+            }
+        }
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < C::KB / 32; ++k)
+#pragma unroll 1
+        for (int i = 0; i < 32; i += 16) {
+            float x[16];
+            tmem_ld16(tS + 32 * k + i, reinterpret_cast<uint32_t *>(x));
+            tmem_ld_wait();
+            loaded16(x);
+            const uint32_t s = seen[k] >> i;
+            uint32_t pk[8];
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const float a = s >> e & 1 ? few_exp2(fmaf(x[e], c, -mc)) : 0.f, b = s >> (e + 1) & 1 ? few_exp2(fmaf(x[e + 1], c, -mc)) : 0.f;
+                sum += a + b, pk[e / 2] = bf16_pair(a, b);
+            }
+            tmem_st8(tS + 16 * k + i / 2, pk);                         // (behind what is still to be read)
+        }
+    m_io = m, l_io = l + sum;
+}
+
+// Grid: x = split x (heads of keys), y = sequences, z = tiles (of `tiles` x 128 rows: 1 or NG).
+template <typename Src, int DH>
+__global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, const AttnRows A, const Src src, int split, int tiles) {
+    using C = TileCfg<DH>;
+    constexpr int KB = C::KB, SUB = C::SUB, NG = C::NG, NB = C::NB;
     extern __shared__ uint8_t tile_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(tile_raw) + 1023) & ~(uintptr_t)1023);
     __shared__ uint32_t s_tmem;
     __shared__ int s_expired;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % split, s = blockIdx.y, r0 = blockIdx.z * (pairs ? 256 : 128);
+    const int rank = blockIdx.x % split, s = blockIdx.y, r0 = blockIdx.z * tiles * 128;
     const int2 sr = B.rows(s);
     const int rows = min(sr.y, B.max_rows) * A.share;
     if (r0 >= rows) return;                                 // (the whole cluster)
-    const int nr = min(pairs ? 256 : 128, rows - r0);
-    const bool by_rows = nr > 128;                          // a tile to a group
+    const int nr = min(tiles * 128, rows - r0);
     TileWork w;
     w.s = s, w.h = blockIdx.x / split;
     {
@@ -275,10 +363,11 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         w.nb = max(0, min(all - rank * per, per));
         w.hi = min(last.hi, w.lo + w.nb * KB);
     }
-    const int jobs = by_rows ? 2 * w.nb : w.nb;
+    // Job j: block j / T, tile and group j % T; with one tile block j, group j % NG.
+    const int T = (nr + 127) / 128, G = T == 1 ? NG : T, jobs = w.nb * T;
     const TileBars bars = {smem_u32(smem + C::AT_BAR)};
-    if (threadIdx.x == 0) bars.init(), s_expired = 0;
-    if (warp == 4) {
+    if (threadIdx.x == 0) bars.init(C::PW), s_expired = 0;
+    if (warp == C::PW) {
         tmem_alloc(smem_u32(&s_tmem), 512);
         tmem_relinquish();
     }
@@ -292,182 +381,137 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
+    const bool merge = split > 1 || (T == 1 && jobs >= 2);  // a row's result is in several groups
     bool ok = true;
 
-    if (warp < 4) {
+    if (warp < C::PW) {
         // ---------------- producers ----------------
-        regs_down<72>();
-        if (w.nb) {
-            constexpr int CPR = DH / 8;
-            const uint32_t sq = smem_u32(smem + C::AT_Q);
-            for (int i = threadIdx.x; i < (by_rows ? 256 : 128) * CPR; i += 128) {
-                const int r = i / CPR, piece = i % CPR, rr = r0 + min(r, nr - 1);
-                const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (w.h * A.share + rr % A.share) * DH + piece * 8;
-                cp_async16(sq + (r >> 7) * C::Q_BYTES + (piece >> 3) * (128 * 128) + tile_at(r & 127, piece & 7), q, r < nr ? 16 : 0);
-            }
-            cp_async_commit();
-            cp_async_wait<0>();
-            tile_publish(bars.q_full());
-            src.produce(B, w, smem, bars, ok);
-        }
+        if (jobs) src.produce(B, w, smem, bars, ok, [&] { tile_queries<DH>(B, A, smem_u32(smem + C::AT_Q), sr.x, r0, nr, w.h, T); });
         if (!ok) s_expired = 1;
-    } else if (warp < 8) {
-        regs_down<72>();
+    } else if (warp < C::SM0) {
         // ---------------- issuer of the products ----------------
-        if (warp == 4 && jobs && elect_one()) {
+        if (warp == C::PW && jobs && elect_one()) {
             constexpr uint32_t idesc_s = umma_idesc_bf16(128, KB), idesc_pv = umma_idesc_bf16(128, 64) | (1u << 16);   // V: MN-major
             const uint32_t sQ = smem_u32(smem + C::AT_Q), sK = smem_u32(smem + C::AT_K), sV = smem_u32(smem + C::AT_V);
             ok = tile_wait(bars.q_full(), 0);
-            auto scores = [&](int j) {
-                const int g = j & 1, b = by_rows ? j >> 1 : j, st = b % C::NST;
-                if (!by_rows || g == 0) ok = ok && tile_wait(bars.k_full(st), (b / C::NST) & 1);
-                if (j >= 2) ok = ok && tile_wait(bars.s_free(g), ((j >> 1) - 1) & 1);
+            // S is issued NB x G jobs ahead of P V, right behind the P V that reads the accumulator's last P: the tensor pipe takes one
+            // thread's instructions in order
+            int js = 0, gs = 0, bs = 0, is = 0;             // next S: job, group, block, buffer of the group
+            auto scores = [&]() {
+                const int st = bs % C::NST;
+                if (T == 1 || gs == 0) ok = ok && tile_wait(bars.k_full(st), (bs / C::NST) & 1);
                 if (!ok) return;
                 tc_fence_after();
-                const uint64_t qd = umma_desc_k128(sQ + (by_rows ? g : 0) * C::Q_BYTES), kd = umma_desc_k128(sK + st * C::BLK);
+                const uint64_t qd = umma_desc_k128(sQ + (T == 1 ? 0 : gs) * C::Q_BYTES), kd = umma_desc_k128(sK + st * C::BLK);
 #pragma unroll
                 for (int i = 0; i < DH / 16; ++i) {
                     const int sub = i >> 2, in = i & 3;
-                    umma_bf16_ss(tmem + g * KB, qd + sub * (128 * 128 >> 4) + 2 * in, kd + sub * (KB * 128 >> 4) + 2 * in, idesc_s, i != 0);
+                    umma_bf16_ss(tmem + (gs * NB + is) * KB, qd + sub * (128 * 128 >> 4) + 2 * in, kd + sub * (KB * 128 >> 4) + 2 * in, idesc_s, i != 0);
                 }
-                umma_commit(bars.s_full(g));
-                if (!by_rows || g == 1) umma_commit(bars.k_empty(st));
+                umma_commit(bars.s_full(gs * NB + is));
+                if (T == 1 || gs == T - 1) umma_commit(bars.k_empty(st)), ++bs;
+                ++js;
+                if (++gs == G) gs = 0, is = is + 1 == NB ? 0 : is + 1;
             };
-            auto values = [&](int j) {
-                const int g = j & 1, b = by_rows ? j >> 1 : j, st = b % C::NST;
-                if (!by_rows || g == 0) ok = ok && tile_wait(bars.v_full(st), (b / C::NST) & 1);
-                ok = ok && tile_wait(bars.p_full(g), (j >> 1) & 1);
-                if (!ok) return;
+            while (js < NB * G && js < jobs && ok) scores();
+            int g = 0, b = 0, n = 0;                        // next P V: group, block, jobs of the group before it
+            for (int j = 0; j < jobs && ok; ++j) {
+                const int st = b % C::NST, buf = g * NB + n % NB;
+                if (T == 1 || g == 0) ok = ok && tile_wait(bars.v_full(st), (b / C::NST) & 1);
+                ok = ok && tile_wait(bars.p_full(buf), (n / NB) & 1);
+                if (!ok) break;
                 tc_fence_after();
 #pragma unroll
                 for (int sub = 0; sub < SUB; ++sub) {
                     const uint64_t vd = umma_desc_k128(sV + st * C::BLK + sub * (KB * 128));
 #pragma unroll
                     for (int i = 0; i < KB / 16; ++i)
-                        umma_bf16_ts(tmem + C::TM_O + g * 64 * SUB + 64 * sub, tmem + C::TM_P + g * (KB / 2) + 8 * i, vd + i * (2048 >> 4),
-                                     idesc_pv, i != 0 || j >= 2);
+                        umma_bf16_ts(tmem + C::TM_O + g * 64 * SUB + 64 * sub, tmem + buf * KB + 8 * i, vd + i * (2048 >> 4), idesc_pv, i != 0 || n != 0);
                 }
                 umma_commit(bars.pv_done(g));
-                if (!by_rows || g == 1) umma_commit(bars.v_empty(st));
-            };
-            for (int j = 0; j < 4 && j < jobs; ++j) scores(j);
-            for (int j = 0; j < jobs && ok; ++j) {
-                values(j);
-                if (j + 4 < jobs && ok) scores(j + 4);
+                if (T == 1 || g == T - 1) umma_commit(bars.v_empty(st)), ++b;
+                if (++g == G) g = 0, ++n;
+                if (js < jobs) scores();
             }
             if (!ok) s_expired = 1;
         }
     } else {
         // ---------------- softmax: a thread per row ----------------
-        regs_up<184>();
-        const int g = (warp - 8) >> 2, quad = warp & 3, trow = quad * 32 + lane, r = (by_rows ? g * 128 : 0) + trow;
-        const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
-        const uint32_t tS = tmem + g * KB + lane_off, tP = tmem + C::TM_P + g * (KB / 2) + lane_off, tO = tmem + C::TM_O + g * 64 * SUB + lane_off;
+        const int g = (warp - C::SM0) >> 2, quad = warp & 3, trow = quad * 32 + lane, r = (T == 1 ? 0 : g * 128) + trow;
+        const uint32_t lane_off = (uint32_t)(quad * 32) << 16, tO = tmem + C::TM_O + g * 64 * SUB + lane_off;
         const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
         const float c = 1.4426950408889634f * rsqrtf((float)DH);
         const KeyRange kr = src.K.range(B, s, sr.y, (r0 + min(r, nr - 1)) / A.share);
         float m = -INFINITY, l = 0.f;                                  // m: reference, in units of scores
         int n = 0;                                                     // the group's jobs so far
-        for (int j = g; j < jobs; j += 2, ++n) {
-            const int b = by_rows ? j >> 1 : j, st = b % C::NST;
+        for (int j = g; g < G && j < jobs; j += G, ++n) {
+            const int b = T == 1 ? j : n, st = b % C::NST, buf = g * NB + n % NB;
+            const uint32_t tS = tmem + buf * KB + lane_off;
             ok = ok && tile_wait(bars.v_full(st), (b / C::NST) & 1);   // (the block's mask)
-            ok = ok && tile_wait(bars.s_full(g), n & 1);
+            ok = ok && tile_wait(bars.s_full(buf), (n / NB) & 1);
             __syncwarp();
             tc_fence_after();
-            if (!some) {
-                // no rows: P may be anything, as what comes of it is not looked at
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bars.s_free(g));
-                if (n) ok = ok && tile_wait(bars.pv_done(g), (n - 1) & 1);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bars.p_full(g));
-                continue;
-            }
-            float x[KB];
+            if (some) {                                                // (of rows that are not there P may be anything)
+                const uint4 mask = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + st * 32);
+                const uint4 bad = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + st * 32 + 16);
+                const int p0 = w.lo + b * KB;
+                bool fast = (mask.x & mask.y & (KB == 96 ? mask.z : 0xffffffffu)) == 0xffffffffu && !(bad.x | bad.y | (KB == 96 ? bad.z : 0u)) && p0 >= kr.lo &&
+                            p0 + KB <= kr.hi && m != -INFINITY;
+                fast = __all_sync(0xffffffffu, fast);
+                if (fast) {
+                    // one pass over S, 16 columns at a time with the next load in flight
+                    const float mc = m * c;
+                    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    float xa[16], xb[16];
+                    uint32_t pk[KB / 2];
+                    tmem_ld16(tS, reinterpret_cast<uint32_t *>(xa));
 #pragma unroll
-            for (int i = 0; i < KB; i += 32) tmem_ld32(tS + i, reinterpret_cast<uint32_t *>(x + i));
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < KB; i += 32) loaded32(x + i);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bars.s_free(g));
-            const uint4 mask = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + st * 32);
-            const uint4 bad = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + st * 32 + 16);
-            const int p0 = w.lo + b * KB;
-            const bool whole = (mask.x & mask.y & (KB == 128 ? mask.z & mask.w : 0xffffffffu)) == 0xffffffffu && p0 >= kr.lo && p0 + KB <= kr.hi;
-            const bool none_bad = !(bad.x | bad.y | (KB == 128 ? bad.z | bad.w : 0u));
-            if (!__all_sync(0xffffffffu, whole && none_bad)) {
-                const uint32_t there[4] = {mask.x, mask.y, mask.z, mask.w}, bads[4] = {bad.x, bad.y, bad.z, bad.w};
-                const int a = kr.lo - p0, e = kr.hi - p0;              // keys a .. e - 1 of the block
-#pragma unroll
-                for (int k = 0; k < KB / 32; ++k) {
-                    const int a1 = min(max(a - 32 * k, 0), 32), e1 = min(max(e - 32 * k, 0), 32);
-                    const uint32_t seen = (e1 == 32 ? 0xffffffffu : (1u << e1) - 1) & ~(a1 == 32 ? 0xffffffffu : (1u << a1) - 1) & there[k];
-                    if (seen & bads[k]) l = NAN;           // the row sees a value that is not finite
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (!(seen >> i & 1)) x[32 * k + i] = -INFINITY;
-                }
-            }
-            float mx[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-            for (int i = 4; i < KB; i += 8)
-#pragma unroll
-                for (int u = 0; u < 4; ++u) mx[u] = i + 4 + u < KB ? fmaxf(fmaxf(mx[u], x[i + u]), x[i + 4 + u]) : fmaxf(mx[u], x[i + u]);
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-            if (n) ok = ok && tile_wait(bars.pv_done(g), (n - 1) & 1);  // P has been read, O is at rest
-            __syncwarp();
-            // (m starts at -inf: the first score that is seen sets it)
-            const bool rise = top * c > m * c + 8.0f || (m == -INFINITY && top != -INFINITY);
-            if (__any_sync(0xffffffffu, rise)) {
-                const float f = rise && m != -INFINITY ? few_exp2((m - top) * c) : rise ? 0.f : 1.0f;
-                if (rise) m = top;
-                l *= f;
-                if (n) {
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int i = 0; i < DH; i += 32) {
-                        float o[32];
-                        tmem_ld32(tO + i, reinterpret_cast<uint32_t *>(o));
+                    for (int i = 0; i < KB; i += 16) {
+                        float *x = i & 16 ? xb : xa, *y = i & 16 ? xa : xb;
                         tmem_ld_wait();
-                        loaded32(o);
+                        loaded16(x);
+                        if (i + 16 < KB) tmem_ld16(tS + i + 16, reinterpret_cast<uint32_t *>(y));
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = f == 0.f ? 0.f : o[e] * f;
-                        tmem_st16(tO + i, reinterpret_cast<uint32_t *>(o));
-                        tmem_st16(tO + i + 16, reinterpret_cast<uint32_t *>(o) + 16);
+                        for (int u = 0; u < 8; ++u) {
+                            const float2 e = ffma2(make_float2(x[2 * u], x[2 * u + 1]), make_float2(c, c), make_float2(-mc, -mc));
+                            const float2 p = make_float2(few_exp2(e.x), few_exp2(e.y));
+                            ls[u & 1] = fadd2(ls[u & 1], p);
+                            pk[i / 2 + u] = bf16_pair(p.x, p.y);
+                        }
+                    }
+                    const float2 l2 = fadd2(ls[0], ls[1]);
+                    const float sum = l2.x + l2.y;
+                    fast = __all_sync(0xffffffffu, sum < 1.152921504606847e18f);
+                    if (fast) {
+                        l += sum;
+#pragma unroll
+                        for (int i = 0; i < KB / 2; i += 16) tmem_st16(tS + i, pk + i);
                     }
                 }
-            }
-            const float mc = m == -INFINITY ? 0.f : m * c;
-            float2 ls[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                if (!fast) {
+                    const uint32_t there[3] = {mask.x, mask.y, mask.z}, bads[3] = {bad.x, bad.y, bad.z};
+                    const int a = kr.lo - p0, e = kr.hi - p0;          // keys a .. e - 1 of the block
+                    uint32_t seen[3] = {0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < KB; i += 32) {
-                uint32_t pk[16];
-#pragma unroll
-                for (int u = 0; u < 16; ++u) {
-                    const float2 y = ffma2(make_float2(x[i + 2 * u], x[i + 2 * u + 1]), make_float2(c, c), make_float2(-mc, -mc));
-                    const float2 p = make_float2(few_exp2(y.x), few_exp2(y.y));
-                    ls[u & 3] = fadd2(ls[u & 3], p);
-                    pk[u] = bf16_pair(p.x, p.y);
+                    for (int k = 0; k < KB / 32; ++k) {
+                        const int a1 = min(max(a - 32 * k, 0), 32), e1 = min(max(e - 32 * k, 0), 32);
+                        seen[k] = (e1 == 32 ? 0xffffffffu : (1u << e1) - 1) & ~(a1 == 32 ? 0xffffffffu : (1u << a1) - 1) & there[k];
+                        if (seen[k] & bads[k]) l = NAN;                // the row sees a value that is not finite
+                    }
+                    tile_slow<DH>(tS, tO, seen[0], seen[1], seen[2], c, n, bars.pv_done(g), m, l, ok);
                 }
-                tmem_st16(tP + i / 2, pk);
+                tmem_st_wait();
             }
-            const float2 l2 = fadd2(fadd2(ls[0], ls[1]), fadd2(ls[2], ls[3]));
-            l += l2.x + l2.y;
-            tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bars.p_full(g));
+            if (lane == 0) mbar_arrive(bars.p_full(buf));
         }
         if (n) ok = ok && tile_wait(bars.pv_done(g), (n - 1) & 1);
         __syncwarp();
         tc_fence_after();
         if (!ok) s_expired = 1;
-        const bool alone = split == 1 && (by_rows || jobs < 2);        // nothing to merge with
-        if (!alone) softmax_sync();                                    // the rings are at rest
-        if (!alone || (some && (by_rows || g == 0))) {
+        if (merge) asm volatile("bar.sync 1, %0;" ::"n"(NG * 128) : "memory");    // queries and rings are at rest
+        if (merge ? g < G : some && (T > 1 ? g < T : g == 0)) {
             const float expired = s_expired || !ok ? NAN : 0.f, inv = (l == 0.f ? 0.f : 1.0f / l) + expired;
             uint8_t *state = smem + g * C::STATE;
             const int rr = r0 + r;
@@ -478,7 +522,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                 tmem_ld32(tO + i, reinterpret_cast<uint32_t *>(o));
                 tmem_ld_wait();
                 loaded32(o);
-                if (!alone) {
+                if (merge) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         *reinterpret_cast<float4 *>(state + ((i / 4 + e) * 128 + trow) * 16) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
@@ -492,21 +536,19 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                     }
                 }
             }
-            if (!alone) *reinterpret_cast<float2 *>(state + 128 * DH * 4 + trow * 8) = make_float2(n ? m * c : -INFINITY, l + expired);
+            if (merge) *reinterpret_cast<float2 *>(state + 128 * DH * 4 + trow * 8) = make_float2(n ? m * c : -INFINITY, l + expired);
         }
     }
     __syncwarp();
     cp_async_wait<0>();
     tc_fence_before();
-    const bool merge = split > 1 || (!by_rows && jobs >= 2);
     if (split > 1) cluster_sync_all();
     else __syncthreads();
     if (merge) {
         // Row words of four columns, 8 rows x 4 of them to a warp (32 bytes of a row, and every bank once); each CTA of a cluster
         // takes every split-th of these.  States count in the order of rank and group; one without scores counts for nothing.
         const uint32_t st0 = smem_u32(smem);
-        const int tiles = by_rows ? 2 : 1, groups = by_rows ? 1 : 2;
-        const int n_words = tiles * 16 * (DH / 16);
+        const int groups = T == 1 ? NG : 1, n_words = T * 16 * (DH / 16);
         for (int i = rank * 16 + warp; i < n_words; i += split * 16) {
             const int tile = i / (16 * (DH / 16)), in = i % (16 * (DH / 16));
             const int trow = (in / (DH / 16)) * 8 + (lane & 7), col4 = (in % (DH / 16)) * 4 + (lane >> 3), r = tile * 128 + trow;
@@ -515,12 +557,12 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < split; ++k)
                 for (int g = 0; g < groups; ++g) {
-                    const uint32_t at = cluster_map(st0 + (by_rows ? tile : g) * C::STATE, k);
+                    const uint32_t at = cluster_map(st0 + (T == 1 ? g : tile) * C::STATE, k);
                     mx = fmaxf(mx, ld_cluster_f2(at + 128 * DH * 4 + trow * 8).x);
                 }
             for (int k = 0; k < split; ++k)
                 for (int g = 0; g < groups; ++g) {
-                    const uint32_t at = cluster_map(st0 + (by_rows ? tile : g) * C::STATE, k);
+                    const uint32_t at = cluster_map(st0 + (T == 1 ? g : tile) * C::STATE, k);
                     const float2 ml = ld_cluster_f2(at + 128 * DH * 4 + trow * 8);
                     if (ml.x == -INFINITY) {
                         sum += ml.y;                        // (0, or the NaN of a wait that ran out)
@@ -538,43 +580,60 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         }
         if (split > 1) cluster_sync_all();                  // nobody leaves while its state is read
     }
-    if (warp == 4) {
+    if (warp == C::PW) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
 }
 
-// CTAs of a cluster that a unit is split over: as many as leave every CTA an SM of its own and a few blocks.
-static int tile_split(long long units, long long keys, int kb, int n_sm) {
-    const long long blocks = (keys + kb - 1) / kb;
-    int split = 1;
-    while (split < 8 && units * (split + 1) <= n_sm && blocks >= 2LL * (split + 1)) ++split;
-    return split;
+// How the work is laid out: tiles of a CTA, CTAs of a cluster that a tile's keys are split over.
+struct TilePlan {
+    int tiles, split;
+};
+// Times in jobs (a key block of a tile): the groups of a CTA share its pipes, so that a CTA's time is its jobs, plus a
+// beginning and an end; waves go by how many clusters the device holds at once.
+template <typename F> static TilePlan tile_plan(long long units, long long rows, long long keys, int kb, int ng, int n_sm, F &&clusters) {
+    const long long blocks = (keys + kb - 1) / kb + 1, t1 = (rows + 127) / 128, tn = (rows + 128 * ng - 1) / (128 * ng);
+    const long long fixed = 8;
+    TilePlan best = {ng, 1};
+    long long least = (units * tn + n_sm - 1) / n_sm * (blocks * (t1 < ng ? t1 : ng) + fixed);
+    for (int split = 1; split <= 8; ++split) {
+        const long long fit = split == 1 ? n_sm : clusters(split);
+        if (fit < 1 || (split > 1 && blocks < 2 * split)) break;
+        const long long cost = (units * t1 + fit - 1) / fit * ((blocks + split - 1) / split + fixed + 2 * (split > 1));
+        if (cost < least) least = cost, best = {1, split};
+    }
+    return best;
 }
 
 template <typename Src, int DH>
-static int launch_attn_tile(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int n_sm, cudaStream_t st) {
+static int launch_attn_tile(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
     using C = TileCfg<DH>;
-    const long long rows = (long long)B.max_rows * A.share, units = (long long)kv_heads * B.n_seqs;
-    const bool pairs = units * ((rows + 255) / 256) >= n_sm;
-    const long long tiles = pairs ? (rows + 255) / 256 : (rows + 127) / 128;
-    if (tiles > 65535) return NFD_E_RANGE;
-    const int split = pairs ? 1 : tile_split(units * tiles, keys, C::KB, n_sm);
-    // the warps' shares of registers add up to what a block is launched with, and no less
-    static int regs = 0;
-    if (!regs) {
-        cudaFuncAttributes fa;
-        if (cudaFuncGetAttributes(&fa, k_attn_tile<Src, DH>) != cudaSuccess) return NFD_E_CUDA;
-        regs = fa.numRegs;
+    auto kern = k_attn_tile<Src, DH>;
+    static bool sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
+    static int fit[NFD_PAGED_DEVICES][9];
+    if (!sized[dev]) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return NFD_E_CUDA;
+        for (int split = 2; split <= 8; ++split) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(split), cfg.blockDim = dim3(TILE_THREADS), cfg.dynamicSmemBytes = C::SMEM;
+            cudaLaunchAttribute at;
+            at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+            cfg.attrs = &at, cfg.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&fit[dev][split], kern, &cfg) != cudaSuccess) fit[dev][split] = 0, cudaGetLastError();
+        }
+        sized[dev] = true;
     }
-    if (regs < 128) return NFD_E_CUDA;
+    const long long rows = (long long)B.max_rows * A.share;
+    const TilePlan pl = tile_plan((long long)kv_heads * B.n_seqs, rows, keys, C::KB, C::NG, n_sm, [&](int k) { return fit[dev][k]; });
+    const long long nz = (rows + 128 * pl.tiles - 1) / (128 * pl.tiles);
+    if (nz > 65535) return NFD_E_RANGE;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kv_heads * split, B.n_seqs, (unsigned)tiles), cfg.blockDim = dim3(TILE_THREADS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
+    cfg.gridDim = dim3(kv_heads * pl.split, B.n_seqs, (unsigned)nz), cfg.blockDim = dim3(TILE_THREADS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
     cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.attrs = &at, cfg.numAttrs = split > 1;
-    if (cudaFuncSetAttribute(k_attn_tile<Src, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess ||
-        cudaLaunchKernelEx(&cfg, k_attn_tile<Src, DH>, B, A, src, split, (int)pairs) != cudaSuccess) {
+    at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = pl.split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at, cfg.numAttrs = pl.split > 1;
+    if (cudaLaunchKernelEx(&cfg, kern, B, A, src, pl.split, pl.tiles) != cudaSuccess) {
         cudaGetLastError();
         return NFD_E_CUDA;
     }

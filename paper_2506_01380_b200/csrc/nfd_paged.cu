@@ -73,13 +73,13 @@ int check_heads(int n_heads, int kv_heads) {
     return NFD_OK;
 }
 
-int sm_count(int &n) {
-    static int n_sms[64];                      // (the same value whichever thread stores it)
-    int dev = -1;
+// the current device and its SMs
+int this_device(int &dev, int &n_sm) {
+    static int n_sms[NFD_PAGED_DEVICES];       // (the same value whichever thread stores it)
     CK(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return NFD_E_RANGE;
+    if (dev < 0 || dev >= NFD_PAGED_DEVICES) return NFD_E_RANGE;
     if (!n_sms[dev]) CK(cudaDeviceGetAttribute(&n_sms[dev], cudaDevAttrMultiProcessorCount, dev));
-    n = n_sms[dev];
+    n_sm = n_sms[dev];
     return NFD_OK;
 }
 
@@ -118,8 +118,8 @@ int nfd_kv_append(const nfd_pages *pages, const nfd_batch *batch, const nfd_rope
             for (int i = 0; i < d[a] / 2; ++i) R.freq[pair++] = pow((double)rope->theta, -2.0 * i / d[a]);
     }
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
-    int n_sm = 0;
-    RET(sm_count(n_sm));
+    int dev = 0, n_sm = 0;
+    RET(this_device(dev, n_sm));
     const AppendIO io = {q, k, v, q_stride, k_stride, v_stride, q_out, n_q_heads};
     const int rows = B.n_rows >= 2 * APPEND_MAX_ROWS * n_sm ? APPEND_MAX_ROWS : 1;
     const unsigned grid = (unsigned)((B.n_rows + rows - 1) / rows);
@@ -181,18 +181,18 @@ int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_head
     if (frame_tokens < 1 || frame_tokens > (1 << 20) || window < 0) return NFD_E_RANGE;
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
     const AttnRows A = {q, out, q_stride, n_heads, n_heads / P.heads};
-    int n_sm = 0;
-    RET(sm_count(n_sm));
+    int dev = 0, n_sm = 0;
+    RET(this_device(dev, n_sm));
     // the most keys that a unit's rows can see: what the tables hold, what the window leaves
     const long long held = (long long)B.table_len * P.page_tokens, seen = ((long long)window + 1) * frame_tokens + B.max_rows;
     const long long keys = held < seen ? held : seen;
     return by_head_dim(pages->head_dim, [&](auto d) -> int {
         constexpr int DH = decltype(d)::value;
         if ((long long)B.max_rows * A.share > FEW_ROWS)
-            return launch_attn_tile<TileKv4<DH>, DH>(B, A, TileKv4<DH>{{P, {frame_tokens, window}}}, P.heads, keys, n_sm, (cudaStream_t)cuda_stream);
+            return launch_attn_tile<TileKv4<DH>, DH>(B, A, TileKv4<DH>{{P, {frame_tokens, window}}}, P.heads, keys, dev, n_sm, (cudaStream_t)cuda_stream);
         FewKv4<DH> src;
         src.K = {P, {frame_tokens, window}};
-        return launch_attn_few<FewKv4<DH>, DH>(B, A, src, P.heads, keys, n_sm, (cudaStream_t)cuda_stream);
+        return launch_attn_few<FewKv4<DH>, DH>(B, A, src, P.heads, keys, dev, n_sm, (cudaStream_t)cuda_stream);
     });
 }
 
@@ -218,8 +218,8 @@ int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_
     if (!aligned(out, 16)) return NFD_E_ALIGN;
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
     const AttnRows A = {q, out, q_stride, n_heads, n_heads / states->n_heads};
-    int n_sm = 0;
-    RET(sm_count(n_sm));
+    int dev = 0, n_sm = 0;
+    RET(this_device(dev, n_sm));
     return by_head_dim(dh, [&](auto d) -> int {
         constexpr int DH = decltype(d)::value;
         auto go = [&](auto *t) -> int {
@@ -227,10 +227,10 @@ int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_
             const StateKeys<TS, DH> K = {(const TS *)states->k, (const TS *)states->v, states->mask, st[0], st[1], st[2], states->n_keys};
             if constexpr (std::is_same_v<TS, bf16>) {
                 if ((long long)B.max_rows * A.share > FEW_ROWS)
-                    return launch_attn_tile<TileStates<DH>, DH>(B, A, TileStates<DH>{K}, states->n_heads, states->n_keys, n_sm, (cudaStream_t)cuda_stream);
+                    return launch_attn_tile<TileStates<DH>, DH>(B, A, TileStates<DH>{K}, states->n_heads, states->n_keys, dev, n_sm, (cudaStream_t)cuda_stream);
                 FewStates<DH> src;
                 src.K = K;
-                return launch_attn_few<FewStates<DH>, DH>(B, A, src, states->n_heads, states->n_keys, n_sm, (cudaStream_t)cuda_stream);
+                return launch_attn_few<FewStates<DH>, DH>(B, A, src, states->n_heads, states->n_keys, dev, n_sm, (cudaStream_t)cuda_stream);
             }
             return launch_attn_any<TS, DH>(B, A, K, (cudaStream_t)cuda_stream);
         };

@@ -4,6 +4,7 @@
 #include "nfd_common.cuh"
 
 #define NFD_MAX_TOKENS (1 << 30)
+#define NFD_PAGED_DEVICES 64
 
 struct BatchD {
     const int *row_start, *kv_len, *table;
