@@ -15,8 +15,8 @@
 // go the same way.
 //
 // Warps 0 .. PW-1 fill the rings of K and V blocks: bf16 states with cp.async, several blocks in flight; 4-bit pages through
-// registers, one block ahead, the codes becoming bf16 numbers on the way.  Warp PW issues the products, the last 4 NG are the softmax
-// groups.  Which keys of a block are there is left beside the V block, a bit each.
+// registers, two blocks ahead, the codes becoming bf16 numbers on the way.  Warp PW issues the products, the last 4 NG are the
+// softmax groups.  Which keys of a block are there is told beside K, a bit each, in a ring of its own: the softmax does not wait for V.
 //
 // A unit (sequence, head of keys, tile) with many keys and few others beside it is split over the CTAs of a cluster, which
 // merge through distributed shared memory.  Every wait is bounded; after one that ran out the rows are NaN.
@@ -34,6 +34,25 @@ __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity) {
         if ((++spins & 0x3ff) == 0 && global_timer_ns() - t0 > NFD_WAIT_LIMIT_NS) return false;
     return true;
 }
+// two of them, their first looks overlapped
+__device__ __forceinline__ bool tile_wait2(uint32_t a, uint32_t pa, uint32_t b, uint32_t pb) {
+    const bool da = mbar_try_wait(a, pa), db = mbar_try_wait(b, pb);
+    return (da || tile_wait(a, pa)) && (db || tile_wait(b, pb));
+}
+// Has the phase completed?  (try_wait may sleep for a while before it says no.)
+__device__ __forceinline__ bool tile_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 // registers that a tensor-memory load has filled are not touched before this point (which comes after its wait)
 __device__ __forceinline__ void loaded32(float *x) {
     asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]),
@@ -49,45 +68,66 @@ __device__ __forceinline__ void loaded16(float *x) {
 template <int DH> struct TileCfg {
     static constexpr int SUB = DH == 128 ? 2 : 1;          // 64-dim parts of a row
     static constexpr int NG = DH == 128 ? 2 : 3;           // softmax groups
-    static constexpr int KB = DH == 128 ? 64 : 96;         // keys of a block
-    static constexpr int NB = DH == 128 ? 2 : 1;           // S accumulators of a group
+    static constexpr int KB = DH == 128 ? 64 : 80;         // keys of a block
+    static constexpr int NB = 4;                           // S accumulators: job j has number j % NB
     static constexpr int PW = DH == 128 ? 4 : 3;           // producer warps
     static constexpr int SM0 = 16 - 4 * NG;                // first softmax warp
-    static constexpr int NST = 4;                          // blocks in the ring of K, and in that of V
+    static constexpr int NST = DH == 128 ? 5 : 6;          // blocks in the ring of K, and in that of V
+    static constexpr int NM = 16;                          // and of their masks: K runs up to NST + NB blocks ahead of the softmax
     static constexpr int Q_BYTES = SUB * 128 * 128;        // a tile's queries
     static constexpr int BLK = SUB * KB * 128;             // a block of K or V
     static constexpr int AT_Q = 0, AT_K = NG * Q_BYTES, AT_V = AT_K + NST * BLK, AT_MASK = AT_V + NST * BLK,
-                         AT_BAR = AT_MASK + NST * 32, SMEM = AT_BAR + 8 * 32 + 1024;
-    static constexpr int TM_O = NG * NB * KB;              // S, and over it P, of group g's buffer i at (g NB + i) KB; O at TM_O + g 64 SUB
+                         AT_BAR = AT_MASK + NM * 32, SMEM = AT_BAR + 448 + 1024;
+    static constexpr int TM_O = NB * KB;                   // S number i, and over it P, at i KB; O of group g at TM_O + g 64 SUB
+    static constexpr uint32_t M1 = 0xffffffffu, M2 = KB >= 96 ? 0xffffffffu : KB > 64 ? (1u << (KB - 64)) - 1 : 0;      // bits of keys 32 .., 64 ..
     // a group's state, over queries and rings: O as [DH / 4][128] float4, then [128] (m, l)
     static constexpr int STATE = 128 * DH * 4 + 128 * 8;
     static_assert(TM_O + NG * 64 * SUB <= 512 && NG * STATE <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
-    static_assert(PW * 32 == KB * SUB, "a thread for 64 dims of a key");
+    static_assert(NST + NB <= NM, "masks");
+    static_assert(NST <= 6 && NB == 4 && NM == 16, "TileBars");
+    static_assert(PW * 32 >= KB * SUB && KB >= 64 && KB <= 96 && KB % 16 == 0, "a thread for 64 dims of a key; three words of bits");
+    static_assert(PW < SM0, "warps");
 };
 
 struct TileBars {
     uint32_t b;
-    // per stage
+    // per stage (up to 6)
     __device__ __forceinline__ uint32_t k_full(int s) const { return b + 8 * s; }
-    __device__ __forceinline__ uint32_t k_empty(int s) const { return b + 32 + 8 * s; }
-    __device__ __forceinline__ uint32_t v_full(int s) const { return b + 64 + 8 * s; }
-    __device__ __forceinline__ uint32_t v_empty(int s) const { return b + 96 + 8 * s; }
-    // per accumulator, per group
-    __device__ __forceinline__ uint32_t s_full(int i) const { return b + 128 + 8 * i; }
-    __device__ __forceinline__ uint32_t p_full(int i) const { return b + 160 + 8 * i; }
-    __device__ __forceinline__ uint32_t pv_done(int g) const { return b + 192 + 8 * g; }
-    __device__ __forceinline__ uint32_t q_full() const { return b + 216; }
-    __device__ __forceinline__ void init(int producers) const {
-        for (int s = 0; s < 4; ++s) {
+    __device__ __forceinline__ uint32_t k_empty(int s) const { return b + 48 + 8 * s; }
+    __device__ __forceinline__ uint32_t v_full(int s) const { return b + 96 + 8 * s; }
+    __device__ __forceinline__ uint32_t v_empty(int s) const { return b + 144 + 8 * s; }
+    // per accumulator (up to 4)
+    __device__ __forceinline__ uint32_t s_full(int i) const { return b + 192 + 8 * i; }
+    __device__ __forceinline__ uint32_t p_full(int i) const { return b + 224 + 8 * i; }
+    // of a group's even and odd jobs: a warp may be done with a job before the product of the one before it is
+    __device__ __forceinline__ uint32_t pv_done(int g, int n) const { return b + 256 + 16 * g + 8 * (n & 1); }
+    __device__ __forceinline__ uint32_t q_full() const { return b + 304; }
+    // per mask (16)
+    __device__ __forceinline__ uint32_t m_full(int s) const { return b + 312 + 8 * s; }
+    static constexpr int BYTES = 440;
+    __device__ __forceinline__ void init(int producers, int q_warps) const {
+        for (int s = 0; s < 6; ++s) {
             mbar_init(k_full(s), producers), mbar_init(v_full(s), producers);      // a producer warp each
             mbar_init(k_empty(s), 1), mbar_init(v_empty(s), 1);
-            mbar_init(s_full(s), 1), mbar_init(p_full(s), 4);                      // a softmax warp each
         }
-        for (int g = 0; g < 3; ++g) mbar_init(pv_done(g), 1);
-        mbar_init(q_full(), producers);
+        for (int i = 0; i < 4; ++i) mbar_init(s_full(i), 1), mbar_init(p_full(i), 4);      // a softmax warp each
+        for (int g = 0; g < 3; ++g) mbar_init(pv_done(g, 0), 1), mbar_init(pv_done(g, 1), 1);
+        for (int s = 0; s < 16; ++s) mbar_init(m_full(s), producers);
+        mbar_init(q_full(), q_warps);                                              // the softmax warps
         fence_mbar_init();
     }
 };
+// at most n groups of this thread's copies are in flight
+__device__ __forceinline__ void cp_async_wait_upto(int n) {
+    switch (n) {
+        case 0: cp_async_wait<0>(); break;
+        case 1: cp_async_wait<1>(); break;
+        case 2: cp_async_wait<2>(); break;
+        case 3: cp_async_wait<3>(); break;
+        case 4: cp_async_wait<4>(); break;
+        default: cp_async_wait<5>();
+    }
+}
 // the CTA's part of its unit's keys
 struct TileWork {
     int s, h, lo, hi, nb;                                   // keys lo .. hi - 1 in nb blocks
@@ -100,29 +140,23 @@ __device__ __forceinline__ void tile_publish(uint32_t bar) {
     if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
 }
 
-// The queries of the CTA's tiles; rows that are not there are zeros.
-template <int DH>
-__device__ __forceinline__ void tile_queries(const BatchD &B, const AttnRows &A, uint32_t sq, int first, int r0, int nr, int h, int tiles) {
-    using C = TileCfg<DH>;
-    constexpr int CPR = DH / 8;
-    for (int i = threadIdx.x; i < tiles * 128 * CPR; i += C::PW * 32) {
-        const int r = i / CPR, piece = i % CPR, rr = r0 + min(r, nr - 1);
-        const bf16 *q = (const bf16 *)A.q + (long long)(first + rr / A.share) * A.q_stride + (h * A.share + rr % A.share) * DH + piece * 8;
-        cp_async16(sq + (r >> 7) * C::Q_BYTES + (piece >> 3) * (128 * 128) + tile_at(r & 127, piece & 7), q, r < nr ? 16 : 0);
-    }
-    cp_async_commit();
-}
-
 // ---- producers: bf16 states ---------------------------------------------------------------------------------
 template <int DH> struct TileStates {
+    static constexpr bool KV4 = false;
     StateKeys<bf16, DH> K;
-    template <typename F> __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok, F &&queries) const {
+    __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok) const {
         using C = TileCfg<DH>;
-        constexpr int CPR = DH / 8, NT = C::PW * 32, RS = NT / CPR, N = C::KB / RS;       // 16-byte pieces of a row; threads; rows a step, steps
-        static_assert(C::KB % RS == 0, "pieces");
+        constexpr int CPR = DH / 8, NT = C::PW * 32, RS = NT / CPR, N = (C::KB + RS - 1) / RS;      // 16-byte pieces of a row; threads; rows a step, steps
+        constexpr int FLY = 5;                                        // items (K of block 0, V of block 0, K ...) whose copies are in flight
         const int t = threadIdx.x, piece = t % CPR, row0 = t / CPR, lane = t & 31;
-        const uint32_t base = smem_u32(smem);
-        const long long seq = w.s * K.seq_stride + w.h * K.head_stride + piece * 8;
+        // this thread's pieces of a block: from its first row on, in steps (few instructions a copy: a producer warp has a scheduler's
+        // slots to itself for the tenth part of the time, and no latency to hide behind)
+        uint32_t to[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) to[i] = smem_u32(smem) + (piece >> 3) * (C::KB * 128) + tile_at(row0 + i * RS, piece & 7);
+        const long long first = w.s * K.seq_stride + w.h * K.head_stride + (long long)(w.lo + row0) * K.key_stride + piece * 8;
+        const bf16 *from[2] = {K.k + first, K.v + first};
+        const long long step = RS * K.key_stride, on = C::KB * K.key_stride;
         const unsigned char *mask = K.mask ? K.mask + (size_t)w.s * K.n_keys : nullptr;
         // bits of this thread's rows of a block, and (the last one) of key t of it
         auto there = [&](int b) -> uint32_t {
@@ -131,17 +165,15 @@ template <int DH> struct TileStates {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int p = p0 + row0 + i * RS;
-                m |= (uint32_t)(p < w.hi && (!mask || mask[p])) << i;
+                m |= (uint32_t)(p < w.hi && row0 + i * RS < C::KB && (!mask || mask[p])) << i;
             }
             const int p = p0 + t;
             return m | (uint32_t)(t < C::KB && p < w.hi && (!mask || mask[p])) << 31;
         };
-        queries();
-        int done = -1, item = 0;                                      // items (queries, K of block 0, V of block 0, K ...) published, begun
+        int done = 0, item = 0;                                       // published, begun
         auto publish = [&]() {
             const int st = (done >> 1) % C::NST;
-            tile_publish(done < 0 ? bars.q_full() : done & 1 ? bars.v_full(st) : bars.k_full(st));
-            ++done;
+            tile_publish(done & 1 ? bars.v_full(st) : bars.k_full(st)), ++done;
         };
         uint32_t bits = there(0);
         for (int b = 0; b < w.nb && ok; ++b) {
@@ -150,49 +182,61 @@ template <int DH> struct TileStates {
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 const uint32_t empty = kv ? bars.v_empty(st) : bars.k_empty(st);
-                if (b >= C::NST && !__all_sync(0xffffffffu, mbar_try_wait(empty, par))) {
-                    // nothing is held back while waiting: what frees this stage may need it
-                    cp_async_wait<0>();
-                    while (done < item) publish();
-                    ok = __all_sync(0xffffffffu, tile_wait(empty, par));
-                    if (!ok) break;
+                // (nothing is held back while waiting: what frees this stage may need it)
+                while (b >= C::NST && !__all_sync(0xffffffffu, tile_test(empty, par))) {
+                    if (done < item) {
+                        cp_async_wait_upto(item - done - 1);
+                        publish();
+                    } else {
+                        ok = __all_sync(0xffffffffu, tile_wait(empty, par));
+                        break;
+                    }
                 }
-                const bf16 *src = kv ? K.v : K.k;
-                const uint32_t dst = base + (kv ? C::AT_V : C::AT_K) + st * C::BLK + (piece >> 3) * (C::KB * 128);
+                if (!ok) break;
+                const uint32_t dst = (kv ? C::AT_V : C::AT_K) + st * C::BLK;
+                const bf16 *src = from[kv];
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int row = row0 + i * RS;
+                for (int i = 0; i < N; ++i, src += step) {
+                    if (C::KB % RS && row0 + i * RS >= C::KB) break;
                     const bool here = bits >> i & 1;
-                    const long long off = here ? seq + (long long)(w.lo + b * C::KB + row) * K.key_stride : 0;
-                    cp_async16(dst + tile_at(row, piece & 7), src + off, here ? 16 : 0);
+                    cp_async16(dst + to[i], here ? src : K.k, here ? 16 : 0);
                 }
+                from[kv] += on;
                 cp_async_commit();
-                if (kv) {
+                if (!kv) {
                     const uint32_t m = __ballot_sync(0xffffffffu, bits >> 31);
-                    uint32_t *M = reinterpret_cast<uint32_t *>(smem + C::AT_MASK) + st * 8 + (t >> 5);
-                    if (lane == 0) M[0] = m, M[4] = 0;
+                    uint32_t *M = reinterpret_cast<uint32_t *>(smem + C::AT_MASK) + b % C::NM * 8 + (t >> 5);
+                    if (lane == 0) M[0] = m, M[4] = 0, mbar_arrive(bars.m_full(b % C::NM));
                 }
-                ++item;
-                if (item - done > 3) {
-                    cp_async_wait<3>();
+                if (++item - done > FLY) {
+                    cp_async_wait<FLY>();
                     publish();
                 }
             }
             bits = next;
         }
-        cp_async_wait<0>();
-        while (ok && done < item) publish();
+        while (ok && done < item) {
+            cp_async_wait_upto(item - done - 1);
+            publish();
+        }
     }
 };
 
 // ---- producers: 4-bit pages ---------------------------------------------------------------------------------
 template <int DH> struct TileKv4 {
+    static constexpr bool KV4 = true;
     Kv4Keys<DH> K;
     // a thread's share of a block: 64 (DH 32: 32) dims of a key of K and of V
     static constexpr int NW = DH == 32 ? 4 : 8, SUBS = DH == 128 ? 2 : 1;
     struct Regs {
-        uint32_t c[NW], w;
+        uint32_t c[NW], w;                                  // codes, words
     };
+    // a word's step is not finite
+    static __device__ __forceinline__ bool infinite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u; }
+    static __device__ __forceinline__ uint32_t load_words(const uint16_t *words, long long place, int sub) {
+        if (DH == 32) return __ldg(words + place);
+        return __ldg(reinterpret_cast<const uint32_t *>(words + place * (DH / 32)) + sub);
+    }
     static __device__ __forceinline__ void load(Regs &r, const void *codes, const uint16_t *words, long long place, int sub) {
         if (place < 0) {
 #pragma unroll
@@ -206,8 +250,7 @@ template <int DH> struct TileKv4 {
             const uint4 v = __ldg(p + i);
             r.c[4 * i] = v.x, r.c[4 * i + 1] = v.y, r.c[4 * i + 2] = v.z, r.c[4 * i + 3] = v.w;
         }
-        if (DH == 32) r.w = __ldg(words + place);
-        else r.w = __ldg(reinterpret_cast<const uint32_t *>(words + place * (DH / 32)) + sub);
+        r.w = load_words(words, place, sub);
     }
     // (a key that is not there has step 0: its row is zeros)
     static __device__ __forceinline__ void convert(const Regs &r, uint8_t *blk, int row) {
@@ -218,42 +261,51 @@ template <int DH> struct TileKv4 {
                 make_uint4(kv4_pair(r.c[i], 0, z2, s2), kv4_pair(r.c[i], 1, z2, s2), kv4_pair(r.c[i], 2, z2, s2), kv4_pair(r.c[i], 3, z2, s2));
         }
     }
-    template <typename F> __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok, F &&queries) const {
+    __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok) const {
         using C = TileCfg<DH>;
         const int t = threadIdx.x, key = t / SUBS, sub = t % SUBS, lane = t & 31;
-        auto look_up = [&](int b) -> long long {
-            const int p = w.lo + b * C::KB + key;
-            if (p >= w.hi) return -1;
-            const long long at = K.P.place(B, w.s, p);
-            return at < 0 ? -1 : at + (long long)w.h * K.P.page_tokens;
+        // This thread's key of the block that is looked up next: token, entry of the table, offset in the page.  (From block to block by
+        // additions: two divisions a block were a sixth of a producer's instructions.)
+        const int P = K.P.page_tokens, L = B.table_len, dq = C::KB / P % L, dr = C::KB % P;
+        const int *table = B.table + (size_t)w.s * L;
+        int p = w.lo + key, off = p % P, pg = p / P % L;
+        auto look_up = [&]() -> long long {
+            long long at = -1;
+            if (p < w.hi && key < C::KB) {
+                const int page = __ldg(table + pg);
+                if ((unsigned)page < (unsigned)K.P.n_pages) at = ((long long)page * K.P.heads + w.h) * P + off;
+            }
+            p += C::KB, off += dr, pg += dq;
+            if (off >= P) off -= P, ++pg;
+            if (pg >= L) pg -= L;
+            return at;
         };
-        Regs k, v;
-        long long place = look_up(0), next = look_up(1);
-        load(k, K.P.k, K.P.k_scale, place, sub);
-        load(v, K.P.v, K.P.v_scale, place, sub);
-        queries();
-        cp_async_wait<0>();
-        tile_publish(bars.q_full());
-        for (int b = 0; b < w.nb && ok; ++b) {
+        Regs k[2], v[2];
+        uint32_t there[2];
+        {
+            const long long a = look_up(), b = look_up();
+            load(k[0], K.P.k, K.P.k_scale, a, sub), load(v[0], K.P.v, K.P.v_scale, a, sub);
+            load(k[1], K.P.k, K.P.k_scale, b, sub), load(v[1], K.P.v, K.P.v_scale, b, sub);
+            there[0] = __ballot_sync(0xffffffffu, a >= 0), there[1] = __ballot_sync(0xffffffffu, b >= 0);
+        }
+        long long next = look_up();
+        // block b, whose codes are in k and v, into the rings; those of block b + 2 take their place
+        auto block = [&](int b, Regs &k, Regs &v, uint32_t &there) {
             const int st = b % C::NST, par = (b / C::NST - 1) & 1;
-            const uint32_t m = __ballot_sync(0xffffffffu, place >= 0);
-            place = next;
-            next = look_up(b + 2);
-            if (b >= C::NST) ok = __all_sync(0xffffffffu, tile_wait(bars.k_empty(st), par));
-            if (!ok) break;
-            convert(k, smem + C::AT_K + st * C::BLK + sub * (C::KB * 128), key);
-            load(k, K.P.k, K.P.k_scale, b + 1 < w.nb ? place : -1, sub);
-            tile_publish(bars.k_full(st));
-            if (b >= C::NST) ok = __all_sync(0xffffffffu, tile_wait(bars.v_empty(st), par));
-            if (!ok) break;
-            // values whose step is not finite go in as zeros: a product with the 0 of a row that does not see them would be NaN
-            const uint32_t inf = 0x7F80u;
-            const bool bad0 = (v.w & inf) == inf, bad1 = DH > 32 && (v.w >> 16 & inf) == inf;
+            const uint32_t m = there;
+            const long long place = next;
+            there = __ballot_sync(0xffffffffu, place >= 0);
+            next = look_up();
+            // Values whose step is not finite go in as zeros (a product with the 0 of a row that does not see them would be NaN), a bit for
+            // each of their keys.
+            const bool bad0 = infinite(v.w), bad1 = DH > 32 && infinite(v.w >> 16);
             uint32_t bad = __ballot_sync(0xffffffffu, bad0 || bad1);
             if (bad0) v.w &= 0xffff0000u;
             if (bad1) v.w &= 0xffffu;
-            convert(v, smem + C::AT_V + st * C::BLK + sub * (C::KB * 128), key);
-            load(v, K.P.v, K.P.v_scale, b + 1 < w.nb ? place : -1, sub);
+            if (b >= C::NST) ok = __all_sync(0xffffffffu, tile_wait(bars.k_empty(st), par));
+            if (!ok) return;
+            if (key < C::KB) convert(k, smem + C::AT_K + st * C::BLK + sub * (C::KB * 128), key);
+            load(k, K.P.k, K.P.k_scale, place, sub);
             if (SUBS == 2) {
                 // two lanes to a key, 16 keys to a warp
                 bad |= bad >> 1;
@@ -262,14 +314,23 @@ template <int DH> struct TileKv4 {
                     x = (x | x >> 1) & 0x33333333u, x = (x | x >> 2) & 0x0F0F0F0Fu, x = (x | x >> 4) & 0x00FF00FFu;
                     return (x | x >> 8) & 0xFFFFu;
                 };
-                uint16_t *M = reinterpret_cast<uint16_t *>(smem + C::AT_MASK) + st * 16 + (t >> 5);
+                uint16_t *M = reinterpret_cast<uint16_t *>(smem + C::AT_MASK) + b % C::NM * 16 + (t >> 5);
                 const uint32_t m16 = every_other(m), b16 = every_other(bad);
-                if (lane == 0) M[0] = (uint16_t)m16, M[8] = (uint16_t)b16;
+                if (lane == 0) M[0] = (uint16_t)m16, M[8] = (uint16_t)b16, mbar_arrive(bars.m_full(b % C::NM));
             } else if (lane == 0) {
-                uint32_t *M = reinterpret_cast<uint32_t *>(smem + C::AT_MASK) + st * 8 + (t >> 5);
-                M[0] = m, M[4] = bad;
+                uint32_t *M = reinterpret_cast<uint32_t *>(smem + C::AT_MASK) + b % C::NM * 8 + (t >> 5);
+                M[0] = m, M[4] = bad, mbar_arrive(bars.m_full(b % C::NM));
             }
+            tile_publish(bars.k_full(st));
+            if (b >= C::NST) ok = __all_sync(0xffffffffu, tile_wait(bars.v_empty(st), par));
+            if (!ok) return;
+            if (key < C::KB) convert(v, smem + C::AT_V + st * C::BLK + sub * (C::KB * 128), key);
+            load(v, K.P.v, K.P.v_scale, place, sub);
             tile_publish(bars.v_full(st));
+        };
+        for (int b = 0; b < w.nb && ok; b += 2) {
+            block(b, k[0], v[0], there[0]);
+            if (ok && b + 1 < w.nb) block(b + 1, k[1], v[1], there[1]);
         }
     }
 };
@@ -282,19 +343,17 @@ static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, uint3
                                               uint32_t pv_done, float &m_io, float &l_io, bool &ok) {
     using C = TileCfg<DH>;
     float m = m_io, l = l_io, top = -INFINITY;
-    const uint32_t seen[3] = {seen0, seen1, seen2};
-#pragma unroll
-    for (int k = 0; k < C::KB / 32; ++k)
+    auto seen = [&](int i) { return (i < 32 ? seen0 : i < 64 ? seen1 : seen2) >> (i & 31); };
 #pragma unroll 1
-        for (int i = 0; i < 32; i += 16) {
-            float x[16];
-            tmem_ld16(tS + 32 * k + i, reinterpret_cast<uint32_t *>(x));
-            tmem_ld_wait();
-            loaded16(x);
-            const uint32_t s = seen[k] >> i;
+    for (int i = 0; i < C::KB; i += 16) {
+        float x[16];
+        tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
+        tmem_ld_wait();
+        loaded16(x);
+        const uint32_t s = seen(i);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s >> e & 1 ? x[e] : -INFINITY);
-        }
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s >> e & 1 ? x[e] : -INFINITY);
+    }
     // (m starts at -inf: the first score that is seen sets it)
     const bool rise = top * c > m * c + 8.0f || (m == -INFINITY && top != -INFINITY);
     if (__any_sync(0xffffffffu, rise)) {
@@ -302,7 +361,7 @@ static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, uint3
         if (rise) m = top;
         l *= f;
         if (n) {
-            ok = ok && tile_wait(pv_done, (n - 1) & 1);                // O is at rest
+            ok = ok && tile_wait(pv_done, ((n - 1) >> 1) & 1);         // O is at rest
             __syncwarp();
             tc_fence_after();
 #pragma unroll 1
@@ -319,24 +378,100 @@ static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, uint3
     }
     const float mc = m == -INFINITY ? 0.f : m * c;
     float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < C::KB / 32; ++k)
 #pragma unroll 1
-        for (int i = 0; i < 32; i += 16) {
-            float x[16];
-            tmem_ld16(tS + 32 * k + i, reinterpret_cast<uint32_t *>(x));
-            tmem_ld_wait();
-            loaded16(x);
-            const uint32_t s = seen[k] >> i;
-            uint32_t pk[8];
+    for (int i = 0; i < C::KB; i += 16) {
+        float x[16];
+        tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
+        tmem_ld_wait();
+        loaded16(x);
+        const uint32_t s = seen(i);
+        uint32_t pk[8];
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                const float a = s >> e & 1 ? few_exp2(fmaf(x[e], c, -mc)) : 0.f, b = s >> (e + 1) & 1 ? few_exp2(fmaf(x[e + 1], c, -mc)) : 0.f;
-                sum += a + b, pk[e / 2] = bf16_pair(a, b);
-            }
-            tmem_st8(tS + 16 * k + i / 2, pk);                         // (behind what is still to be read)
+        for (int e = 0; e < 16; e += 2) {
+            const float a = s >> e & 1 ? few_exp2(fmaf(x[e], c, -mc)) : 0.f, b = s >> (e + 1) & 1 ? few_exp2(fmaf(x[e + 1], c, -mc)) : 0.f;
+            sum += a + b, pk[e / 2] = bf16_pair(a, b);
         }
+        tmem_st8(tS + i / 2, pk);                                      // (behind what is still to be read)
+    }
     m_io = m, l_io = l + sum;
+}
+
+// D (+)= A B^T with descriptors whose upper halves are constants
+__device__ __forceinline__ void tile_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        ".reg .b64 da, db;\n"
+        "mov.b64 da, {%1, %5};\n"
+        "mov.b64 db, {%2, %5};\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n"
+        "}\n" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"((1024 >> 4) | 1 << 14 | 2 << 29)
+        : "memory");
+}
+__device__ __forceinline__ void tile_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        ".reg .b64 db;\n"
+        "mov.b64 db, {%2, %5};\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n"
+        "}\n" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"((1024 >> 4) | 1 << 14 | 2 << 29)
+        : "memory");
+}
+// All products of a CTA, by one thread.  G groups; one: a single tile, whose blocks they share out.  (With a thread for each kind, S waits
+// for the completion of the P V before it: the same times.)
+template <int DH> static __device__ __forceinline__ bool tile_issue(const TileBars &bars, uint32_t base, uint32_t tmem, int jobs, int G, bool one) {
+    using C = TileCfg<DH>;
+    constexpr int KB = C::KB, SUB = C::SUB, NB = C::NB, NST = C::NST;
+    constexpr uint32_t idesc_s = umma_idesc_bf16(128, KB), idesc_pv = umma_idesc_bf16(128, 64) | (1u << 16);       // V: MN-major
+    const uint32_t dQ = (base + C::AT_Q) >> 4, dK = (base + C::AT_K) >> 4, dV = (base + C::AT_V) >> 4;
+    bool ok = tile_wait(bars.q_full(), 0);
+    // S is issued NB jobs ahead of P V, right behind the P V that reads the accumulator's last P: the tensor pipe takes one
+    // thread's instructions in order
+    int is = 0, gs = 0, js = 0, ks = 0, klap = 0;           // next S: accumulator, group, job, stage of K and how often its ring has gone round
+    auto scores = [&]() {
+        if (one || gs == 0) ok = ok && tile_wait(bars.k_full(ks), klap & 1);
+        if (!ok) return;
+        tc_fence_after();
+        const uint32_t q = dQ + (one ? 0 : gs) * (C::Q_BYTES >> 4), k = dK + ks * (C::BLK >> 4), d = tmem + is * KB;
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i)
+            tile_mma_ss(d, q + (i >> 2) * (128 * 128 >> 4) + 2 * (i & 3), k + (i >> 2) * (KB * 128 >> 4) + 2 * (i & 3), idesc_s, i != 0);
+        umma_commit(bars.s_full(is));
+        if (one || gs == G - 1) {
+            umma_commit(bars.k_empty(ks));
+            if (++ks == NST) ks = 0, ++klap;
+        }
+        ++js;
+        if (++is == NB) is = 0;
+        if (++gs == G) gs = 0;
+    };
+    while (js < NB && js < jobs && ok) scores();
+    int ip = 0, par = 0, g = 0, n = 0, vs = 0, vlap = 0;    // next P V: accumulator, its phase, group, its jobs so far, stage of V
+    for (int j = 0; j < jobs && ok; ++j) {
+        if (one || g == 0) ok = ok && tile_wait(bars.v_full(vs), vlap & 1);
+        ok = ok && tile_wait(bars.p_full(ip), par);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub) {
+            const uint32_t d = tmem + C::TM_O + g * 64 * SUB + 64 * sub, a = tmem + ip * KB, v = dV + vs * (C::BLK >> 4) + sub * (KB * 128 >> 4);
+            tile_mma_ts(d, a, v, idesc_pv, n != 0);
+#pragma unroll
+            for (int i = 1; i < KB / 16; ++i) tile_mma_ts(d, a + 8 * i, v + i * (2048 >> 4), idesc_pv, 1);
+        }
+        umma_commit(bars.pv_done(g, n));
+        if (one || g == G - 1) {
+            umma_commit(bars.v_empty(vs));
+            if (++vs == NST) vs = 0, ++vlap;
+        }
+        if (++ip == NB) ip = 0, par ^= 1;
+        if (++g == G) g = 0, ++n;
+        if (js < jobs) scores();
+    }
+    return ok;
 }
 
 // Grid: x = split x (heads of keys), y = sequences, z = tiles (of `tiles` x 128 rows: 1 or NG).
@@ -356,6 +491,19 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
     const int nr = min(tiles * 128, rows - r0);
     TileWork w;
     w.s = s, w.h = blockIdx.x / split;
+    // Job j: block j / T, tile and group j % T; with one tile block j, group j % NG.
+    const int T = (nr + 127) / 128, G = T == 1 ? NG : T;
+    if (warp >= C::SM0) {
+        // softmax warps: the row's queries, into the operand of its tile; with one tile, the groups share them out
+        constexpr int CPR = DH / 8;
+        const int g = (warp - C::SM0) >> 2, trow = (warp & 3) * 32 + lane, r = (T == 1 ? 0 : g * 128) + trow, rr = r0 + min(r, nr - 1);
+        const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (w.h * A.share + rr % A.share) * DH;
+        const uint32_t sq = smem_u32(smem + C::AT_Q) + (T == 1 ? 0 : g) * C::Q_BYTES;
+        if (g < G)
+            for (int i = T == 1 ? g : 0; i < CPR; i += T == 1 ? NG : 1)
+                cp_async16(sq + (i >> 3) * (128 * 128) + tile_at(trow, i & 7), q + 8 * i, r < nr ? 16 : 0);
+        cp_async_commit();
+    }
     {
         const KeyRange first = src.K.range(B, s, sr.y, r0 / A.share), last = src.K.range(B, s, sr.y, (r0 + nr - 1) / A.share);
         const int all = max(0, (last.hi - first.lo + KB - 1) / KB), per = (all + split - 1) / split;
@@ -363,10 +511,9 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         w.nb = max(0, min(all - rank * per, per));
         w.hi = min(last.hi, w.lo + w.nb * KB);
     }
-    // Job j: block j / T, tile and group j % T; with one tile block j, group j % NG.
-    const int T = (nr + 127) / 128, G = T == 1 ? NG : T, jobs = w.nb * T;
+    const int jobs = w.nb * T;
     const TileBars bars = {smem_u32(smem + C::AT_BAR)};
-    if (threadIdx.x == 0) bars.init(C::PW), s_expired = 0;
+    if (threadIdx.x == 0) bars.init(C::PW, 4 * G), s_expired = 0;
     if (warp == C::PW) {
         tmem_alloc(smem_u32(&s_tmem), 512);
         tmem_relinquish();
@@ -384,57 +531,19 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
     const bool merge = split > 1 || (T == 1 && jobs >= 2);  // a row's result is in several groups
     bool ok = true;
 
-    if (warp < C::PW) {
+    if (warp < C::SM0) {
         // ---------------- producers ----------------
-        if (jobs) src.produce(B, w, smem, bars, ok, [&] { tile_queries<DH>(B, A, smem_u32(smem + C::AT_Q), sr.x, r0, nr, w.h, T); });
-        if (!ok) s_expired = 1;
-    } else if (warp < C::SM0) {
+        if (warp < C::PW && jobs) src.produce(B, w, smem, bars, ok);
         // ---------------- issuer of the products ----------------
-        if (warp == C::PW && jobs && elect_one()) {
-            constexpr uint32_t idesc_s = umma_idesc_bf16(128, KB), idesc_pv = umma_idesc_bf16(128, 64) | (1u << 16);   // V: MN-major
-            const uint32_t sQ = smem_u32(smem + C::AT_Q), sK = smem_u32(smem + C::AT_K), sV = smem_u32(smem + C::AT_V);
-            ok = tile_wait(bars.q_full(), 0);
-            // S is issued NB x G jobs ahead of P V, right behind the P V that reads the accumulator's last P: the tensor pipe takes one
-            // thread's instructions in order
-            int js = 0, gs = 0, bs = 0, is = 0;             // next S: job, group, block, buffer of the group
-            auto scores = [&]() {
-                const int st = bs % C::NST;
-                if (T == 1 || gs == 0) ok = ok && tile_wait(bars.k_full(st), (bs / C::NST) & 1);
-                if (!ok) return;
-                tc_fence_after();
-                const uint64_t qd = umma_desc_k128(sQ + (T == 1 ? 0 : gs) * C::Q_BYTES), kd = umma_desc_k128(sK + st * C::BLK);
-#pragma unroll
-                for (int i = 0; i < DH / 16; ++i) {
-                    const int sub = i >> 2, in = i & 3;
-                    umma_bf16_ss(tmem + (gs * NB + is) * KB, qd + sub * (128 * 128 >> 4) + 2 * in, kd + sub * (KB * 128 >> 4) + 2 * in, idesc_s, i != 0);
-                }
-                umma_commit(bars.s_full(gs * NB + is));
-                if (T == 1 || gs == T - 1) umma_commit(bars.k_empty(st)), ++bs;
-                ++js;
-                if (++gs == G) gs = 0, is = is + 1 == NB ? 0 : is + 1;
-            };
-            while (js < NB * G && js < jobs && ok) scores();
-            int g = 0, b = 0, n = 0;                        // next P V: group, block, jobs of the group before it
-            for (int j = 0; j < jobs && ok; ++j) {
-                const int st = b % C::NST, buf = g * NB + n % NB;
-                if (T == 1 || g == 0) ok = ok && tile_wait(bars.v_full(st), (b / C::NST) & 1);
-                ok = ok && tile_wait(bars.p_full(buf), (n / NB) & 1);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll
-                for (int sub = 0; sub < SUB; ++sub) {
-                    const uint64_t vd = umma_desc_k128(sV + st * C::BLK + sub * (KB * 128));
-#pragma unroll
-                    for (int i = 0; i < KB / 16; ++i)
-                        umma_bf16_ts(tmem + C::TM_O + g * 64 * SUB + 64 * sub, tmem + buf * KB + 8 * i, vd + i * (2048 >> 4), idesc_pv, i != 0 || n != 0);
-                }
-                umma_commit(bars.pv_done(g));
-                if (T == 1 || g == T - 1) umma_commit(bars.v_empty(st)), ++b;
-                if (++g == G) g = 0, ++n;
-                if (js < jobs) scores();
-            }
-            if (!ok) s_expired = 1;
+        if (warp == C::PW && jobs) {
+            // (what the products' operands come from is the same in all lanes, and the compiler has to know it: with operands moved to uniform
+            // registers one by one they took 720 clocks a job for 620)
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
+            const int n_jobs = __shfl_sync(0xffffffffu, jobs, 0), n_g = __shfl_sync(0xffffffffu, G, 0);
+            const bool one = __shfl_sync(0xffffffffu, T, 0) == 1;
+            if (elect_one()) ok = tile_issue<DH>(bars, base, tm, n_jobs, n_g, one);
         }
+        if (!ok) s_expired = 1;
     } else {
         // ---------------- softmax: a thread per row ----------------
         const int g = (warp - C::SM0) >> 2, quad = warp & 3, trow = quad * 32 + lane, r = (T == 1 ? 0 : g * 128) + trow;
@@ -442,29 +551,32 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
         const float c = 1.4426950408889634f * rsqrtf((float)DH);
         const KeyRange kr = src.K.range(B, s, sr.y, (r0 + min(r, nr - 1)) / A.share);
+        if (g < G && jobs) {
+            cp_async_wait<0>();
+            tile_publish(bars.q_full());
+        }
         float m = -INFINITY, l = 0.f;                                  // m: reference, in units of scores
         int n = 0;                                                     // the group's jobs so far
         for (int j = g; g < G && j < jobs; j += G, ++n) {
-            const int b = T == 1 ? j : n, st = b % C::NST, buf = g * NB + n % NB;
+            const int b = T == 1 ? j : n, buf = j % NB;
             const uint32_t tS = tmem + buf * KB + lane_off;
-            ok = ok && tile_wait(bars.v_full(st), (b / C::NST) & 1);   // (the block's mask)
-            ok = ok && tile_wait(bars.s_full(buf), (n / NB) & 1);
+            ok = ok && tile_wait2(bars.m_full(b % C::NM), (b / C::NM) & 1, bars.s_full(buf), (j / NB) & 1);
             __syncwarp();
             tc_fence_after();
             if (some) {                                                // (of rows that are not there P may be anything)
-                const uint4 mask = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + st * 32);
-                const uint4 bad = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + st * 32 + 16);
+                float xa[16], xb[16];
+                tmem_ld16(tS, reinterpret_cast<uint32_t *>(xa));       // (of use where the fast path is taken)
+                const uint4 mask = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + b % C::NM * 32);
+                const uint4 bad = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + b % C::NM * 32 + 16);
                 const int p0 = w.lo + b * KB;
-                bool fast = (mask.x & mask.y & (KB == 96 ? mask.z : 0xffffffffu)) == 0xffffffffu && !(bad.x | bad.y | (KB == 96 ? bad.z : 0u)) && p0 >= kr.lo &&
+                bool fast = (mask.x & mask.y) == 0xffffffffu && (mask.z & C::M2) == C::M2 && !(bad.x | bad.y | (C::M2 ? bad.z : 0u)) && p0 >= kr.lo &&
                             p0 + KB <= kr.hi && m != -INFINITY;
                 fast = __all_sync(0xffffffffu, fast);
                 if (fast) {
                     // one pass over S, 16 columns at a time with the next load in flight
                     const float mc = m * c;
                     float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    float xa[16], xb[16];
                     uint32_t pk[KB / 2];
-                    tmem_ld16(tS, reinterpret_cast<uint32_t *>(xa));
 #pragma unroll
                     for (int i = 0; i < KB; i += 16) {
                         float *x = i & 16 ? xb : xa, *y = i & 16 ? xa : xb;
@@ -485,20 +597,21 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                     if (fast) {
                         l += sum;
 #pragma unroll
-                        for (int i = 0; i < KB / 2; i += 16) tmem_st16(tS + i, pk + i);
+                        for (int i = 0; i < KB / 2; i += 8) tmem_st8(tS + i, pk + i);
                     }
                 }
                 if (!fast) {
+                    tmem_ld_wait();
                     const uint32_t there[3] = {mask.x, mask.y, mask.z}, bads[3] = {bad.x, bad.y, bad.z};
                     const int a = kr.lo - p0, e = kr.hi - p0;          // keys a .. e - 1 of the block
                     uint32_t seen[3] = {0, 0, 0};
 #pragma unroll
-                    for (int k = 0; k < KB / 32; ++k) {
+                    for (int k = 0; k < (KB + 31) / 32; ++k) {
                         const int a1 = min(max(a - 32 * k, 0), 32), e1 = min(max(e - 32 * k, 0), 32);
                         seen[k] = (e1 == 32 ? 0xffffffffu : (1u << e1) - 1) & ~(a1 == 32 ? 0xffffffffu : (1u << a1) - 1) & there[k];
                         if (seen[k] & bads[k]) l = NAN;                // the row sees a value that is not finite
                     }
-                    tile_slow<DH>(tS, tO, seen[0], seen[1], seen[2], c, n, bars.pv_done(g), m, l, ok);
+                    tile_slow<DH>(tS, tO, seen[0], seen[1], seen[2], c, n, bars.pv_done(g, n - 1), m, l, ok);
                 }
                 tmem_st_wait();
             }
@@ -506,7 +619,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
             __syncwarp();
             if (lane == 0) mbar_arrive(bars.p_full(buf));
         }
-        if (n) ok = ok && tile_wait(bars.pv_done(g), (n - 1) & 1);
+        if (n) ok = ok && tile_wait(bars.pv_done(g, n - 1), ((n - 1) >> 1) & 1);
         __syncwarp();
         tc_fence_after();
         if (!ok) s_expired = 1;
@@ -586,23 +699,29 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
     }
 }
 
-// How the work is laid out: tiles of a CTA, CTAs of a cluster that a tile's keys are split over.
+// How the work is laid out: tiles of a CTA (1 or NG), CTAs of a cluster that their keys are split over.
 struct TilePlan {
     int tiles, split;
 };
-// Times in jobs (a key block of a tile): the groups of a CTA share its pipes, so that a CTA's time is its jobs, plus a
-// beginning and an end; waves go by how many clusters the device holds at once.
-template <typename F> static TilePlan tile_plan(long long units, long long rows, long long keys, int kb, int ng, int n_sm, F &&clusters) {
-    const long long blocks = (keys + kb - 1) / kb + 1, t1 = (rows + 127) / 128, tn = (rows + 128 * ng - 1) / (128 * ng);
-    const long long fixed = 8;
-    TilePlan best = {ng, 1};
-    long long least = (units * tn + n_sm - 1) / n_sm * (blocks * (t1 < ng ? t1 : ng) + fixed);
-    for (int split = 1; split <= 8; ++split) {
-        const long long fit = split == 1 ? n_sm : clusters(split);
-        if (fit < 1 || (split > 1 && blocks < 2 * split)) break;
-        const long long cost = (units * t1 + fit - 1) / fit * ((blocks + split - 1) / split + fixed + 2 * (split > 1));
-        if (cost < least) least = cost, best = {1, split};
-    }
+// Times in clocks, as measured with all SMs busy: a job (a key block of a tile) takes a CTA's pipes JOB, a block its producers LOAD (few rows
+// are bound by that); a CTA has a beginning and an end (FIXED, and MERGE where there are states to merge); waves go by how many clusters the
+// device holds at once.  16 heads x 64, 336 rows behind 5376 keys in 4-bit pages: a tile to a CTA in 2 pieces 42.7 us, three tiles in 1, 4, 6 and
+// 8 (two waves) 108, 42.7, 35.2, 65; 512 encoder states: a tile in 1, 2 and 4 pieces 17.7, 15.7, 29.7, three tiles in 6 20.7.
+template <int DH, bool KV4, typename F> static TilePlan tile_plan(long long units, long long rows, long long keys, int n_sm, F &&clusters) {
+    constexpr int kb = TileCfg<DH>::KB, ng = TileCfg<DH>::NG;
+    constexpr long long JOB = (DH == 128 ? 17 : 10) * kb, LOAD = (DH == 128 ? (KV4 ? 34 : 37) : KV4 ? 27 : 19) * kb, FIXED = 9000, MERGE = 3000;
+    const long long blocks = (keys + kb - 1) / kb, t1 = (rows + 127) / 128;
+    TilePlan best = {1, 1};
+    long long least = -1;
+    for (int tiles = 1; tiles <= ng; tiles += ng - 1)
+        for (int split = 1; split <= 8; ++split) {
+            const long long fit = split == 1 ? n_sm : clusters(split);
+            if (fit < 1 || (split > 1 && blocks < 2 * split)) break;
+            const long long mine = t1 < tiles ? t1 : tiles, job = JOB * mine, per = (blocks + split - 1) / split;
+            const long long cost = (units * ((t1 + tiles - 1) / tiles) + fit - 1) / fit *
+                                   (per * (job > LOAD ? job : LOAD) + FIXED + (split > 1 || mine == 1 ? MERGE : 0));
+            if (least < 0 || cost < least) least = cost, best = {tiles, split};
+        }
     return best;
 }
 
@@ -625,7 +744,7 @@ static int launch_attn_tile(const BatchD &B, const AttnRows &A, const Src &src, 
         sized[dev] = true;
     }
     const long long rows = (long long)B.max_rows * A.share;
-    const TilePlan pl = tile_plan((long long)kv_heads * B.n_seqs, rows, keys, C::KB, C::NG, n_sm, [&](int k) { return fit[dev][k]; });
+    const TilePlan pl = tile_plan<DH, Src::KV4>((long long)kv_heads * B.n_seqs, rows, keys, n_sm, [&](int k) { return fit[dev][k]; });
     const long long nz = (rows + 128 * pl.tiles - 1) / (128 * pl.tiles);
     if (nz > 65535) return NFD_E_RANGE;
     cudaLaunchConfig_t cfg = {};

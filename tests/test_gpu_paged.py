@@ -306,6 +306,13 @@ def test_kv4_rows_around_the_tiles(rows):
     _check_kv4([rows], [rows + 90], 6, 3, 64, 48, 10, 16, 3, seed=rows)
 
 
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("rows", [100, 200, 336, 400])
+def test_kv4_several_tiles_to_a_cta(rows, dh):
+    """Enough sequences and heads that the tiles of a head share a CTA: one, two and three of them, the last one not full."""
+    _check_kv4([rows] * 5, [rows + 250, rows, rows + 1, rows + 100, 2 * rows], 32, 1, dh, 64, 13, 40, 4, seed=rows)
+
+
 @pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 255, 256, 257, 640, 1025])
 def test_kv4_lengths_around_the_tiles(length):
     _check_kv4([1, 1], [length, max(1, length - 1)], 4, 2, 64, 64, 17, 1, 1 << 30, seed=length, uniform=True)
@@ -486,6 +493,13 @@ def test_cross_rows_and_keys_around_the_tiles(tdt, rows):
     torch, _ = _mods()
     for keys in (1, 15, 64, 127, 128, 129, 256, 500):
         _check_cross(getattr(torch, tdt), [rows], [keys], 2, 1, 64, keys, seed=rows + keys)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("rows", [100, 200, 336, 400])
+def test_cross_several_tiles_to_a_cta(rows, dh):
+    torch, _ = _mods()
+    _check_cross(torch.bfloat16, [rows] * 5, [700, 0, 81, 500, 640], 32, 1, dh, 700, rows == 200, seed=rows)
 
 
 @pytest.mark.parametrize("tdt", ["bfloat16", "float32"])
