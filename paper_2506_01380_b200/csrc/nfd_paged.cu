@@ -114,8 +114,18 @@ int nfd_kv_append(const nfd_pages *pages, const nfd_batch *batch, const nfd_rope
         if (rope->frame_tokens < 1 || rope->grid_w < 1 || rope->frame_tokens % rope->grid_w) return NFD_E_BADCFG;
         R.on = 1, R.frame_tokens = rope->frame_tokens, R.grid_w = rope->grid_w;
         R.half_t = d[0] / 2, R.half_th = (d[0] + d[1]) / 2;
-        for (int a = 0, pair = 0; a < 3; ++a)
-            for (int i = 0; i < d[a] / 2; ++i) R.freq[pair++] = pow((double)rope->theta, -2.0 * i / d[a]);
+        // (the powers of the last rotation of this thread: they took longer than the rest of the call)
+        static thread_local struct {
+            int d[3];
+            float theta;
+            double freq[64];
+        } last = {};
+        if (memcmp(last.d, d, sizeof(d)) || last.theta != rope->theta) {
+            for (int a = 0, pair = 0; a < 3; ++a)
+                for (int i = 0; i < d[a] / 2; ++i) last.freq[pair++] = pow((double)rope->theta, -2.0 * i / d[a]);
+            memcpy(last.d, d, sizeof(d)), last.theta = rope->theta;
+        }
+        memcpy(R.freq, last.freq, dh / 2 * sizeof(double));
     }
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
     int dev = 0, n_sm = 0;

@@ -206,7 +206,7 @@ class Batch:
         if max_rows is None:
             max_rows = n_rows if row_start is not None else n_rows // n_seqs
         self.kv_len, self.table, self.row_start = kv_len, table, row_start
-        self.device = given[0].device if given else None
+        self.dev = given[0].get_device() if given else None
         self.n_seqs, self.n_rows = n_seqs, int(n_rows)
         ptr = lambda t: t.data_ptr() if t is not None else None
         self.c = NfdBatch(ptr(row_start), ptr(kv_len), ptr(table), n_seqs, self.n_rows, int(max_rows),
@@ -229,7 +229,7 @@ class Pages:
             for t in (k_scale, v_scale):
                 assert t.dtype == torch.int16 and tuple(t.shape) == (n_pages, heads, tokens, head_dim // 32)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device, self.n_heads, self.head_dim = k.device, heads, head_dim
+        self.dev, self.n_heads, self.head_dim = k.get_device(), heads, head_dim
         self.dtype = None if kv4 else k.dtype
         ptr = lambda t: t.data_ptr() if kv4 else None
         self.c = NfdPages(k.data_ptr(), v.data_ptr(), ptr(k_scale), ptr(v_scale), I.DTYPE_KV4 if kv4 else _TYPES[k.dtype],
@@ -267,90 +267,95 @@ class States:
             assert mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and mask.device == k.device
             assert tuple(mask.shape) == (n, keys)
         self.k, self.v, self.mask = k, v, mask
-        self.device, self.dtype, self.n_seqs, self.n_heads, self.head_dim = k.device, k.dtype, n, heads, head_dim
+        self.dev, self.dtype, self.n_seqs, self.n_heads, self.head_dim = k.get_device(), k.dtype, n, heads, head_dim
         st = [k.stride(i) if k.shape[i] > 1 and keys else 0 for i in range(3)]        # (the stride of one element says nothing)
         self.c = NfdStates(k.data_ptr(), v.data_ptr(), mask.data_ptr() if mask is not None else None, st[0], st[1], st[2],
                            _TYPES[k.dtype], keys, heads, head_dim)
         self.ref = C.addressof(self.c)
 
 
-def _call(what, device, stream, fn, *args):
-    """A call on `stream` (None: torch's current one) with its device current."""
-    if device.index == torch.cuda.current_device():
-        st = torch.cuda.current_stream() if stream is None else stream
-        code = fn(*args, st.cuda_stream)
+# (Checks and look-ups cost the host as much as a small call costs the GPU: tensors are asked for what is needed, once.)
+def _call(what, dev, stream, fn, *args):
+    """A call on `stream` (None: torch's current one of device number dev) with its device current."""
+    raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if dev == torch.cuda.current_device():
+        code = fn(*args, raw)
     else:
-        with torch.cuda.device(device):
-            st = torch.cuda.current_stream() if stream is None else stream
-            code = fn(*args, st.cuda_stream)
+        with torch.cuda.device(dev):
+            code = fn(*args, raw)
     if code != 0:
         raise NfdError(code, what)
 
 
-def _row_stride(t, n_rows, heads, head_dim, dtype, device):
+def _row_stride(t, n_rows, heads, head_dim, dtype, dev):
     """Elements between the rows of t [n_rows, heads, head_dim] (or [n_rows, heads * head_dim]), whose rows are dense."""
-    assert t.dtype == dtype and t.device == device
-    if t.dim() == 2:
-        assert t.shape[0] == n_rows and t.shape[1] == heads * head_dim and t.stride(1) == 1
+    st = t.stride()
+    assert t.dtype is dtype and t.get_device() == dev
+    if len(st) == 2:
+        assert t.shape == (n_rows, heads * head_dim) and st[1] == 1
     else:
-        assert tuple(t.shape) == (n_rows, heads, head_dim) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim)
-    return t.stride(0) if n_rows > 1 else heads * head_dim
+        assert t.shape == (n_rows, heads, head_dim) and st[2] == 1 and (heads == 1 or st[1] == head_dim)
+    return st[0] if n_rows > 1 else heads * head_dim
+
+
+def _heads(q, head_dim):
+    s = q.shape
+    return s[1] if len(s) == 3 else s[1] // head_dim
+
+
+def _result(t, n, dtype, dev):
+    """The address of a dense result of n elements."""
+    assert t.dtype is dtype and t.get_device() == dev and t.numel() == n and t.is_contiguous()
+    return t.data_ptr()
 
 
 def kv_append(pages: Pages, batch: Batch, k, v, rope: Rope = None, q=None, q_out=None, stream=None):
     """nfd_kv_append: k, v [n_rows, n_heads, head_dim] go to their tokens' places in the pages, k rotated; with q
     [n_rows, n_q_heads, head_dim] the rows' queries are rotated into q_out, which is returned.  Rows may be strided."""
-    dev, n, dh = pages.device, batch.n_rows, pages.head_dim
-    assert batch.device == dev and batch.table is not None
-    ks = _row_stride(k, n, pages.n_heads, dh, k.dtype, dev)
-    vs = _row_stride(v, n, pages.n_heads, dh, k.dtype, dev)
+    dev, n, dh, dtype = pages.dev, batch.n_rows, pages.head_dim, k.dtype
+    assert batch.dev == dev and batch.table is not None
+    ks = _row_stride(k, n, pages.n_heads, dh, dtype, dev)
+    vs = _row_stride(v, n, pages.n_heads, dh, dtype, dev)
     hq = qs = qp = op = 0
     if q is not None:
-        hq = q.shape[1] if q.dim() == 3 else q.shape[1] // dh
-        qs, qp = _row_stride(q, n, hq, dh, k.dtype, dev), q.data_ptr()
-        assert q_out.is_contiguous() and q_out.dtype == k.dtype and q_out.device == dev and q_out.numel() == n * hq * dh
-        op = q_out.data_ptr()
+        hq = _heads(q, dh)
+        qs, qp, op = _row_stride(q, n, hq, dh, dtype, dev), q.data_ptr(), _result(q_out, n * hq * dh, dtype, dev)
         assert op != qp or qs == hq * dh
     _call("nfd_kv_append", dev, stream, load().nfd_kv_append, pages.ref, batch.ref, rope.ref if rope is not None else None,
-          _TYPES[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs, hq, qp, qs, op)
+          _TYPES[dtype], k.data_ptr(), ks, v.data_ptr(), vs, hq, qp, qs, op)
     return q_out
 
 
 def pages_read(pages: Pages, batch: Batch, k_out=None, v_out=None, stream=None):
     """nfd_pages_read: the batch's rows out of the pages, [n_rows, n_heads, head_dim] each (either may be None)."""
-    dev, n = pages.device, batch.n_rows * pages.n_heads * pages.head_dim
-    assert batch.device == dev and batch.table is not None
-    some = k_out if k_out is not None else v_out
-    for t in (k_out, v_out):
-        assert t is None or (t.is_contiguous() and t.device == dev and t.dtype == some.dtype and t.numel() == n)
-    ptr = lambda t: t.data_ptr() if t is not None else None
-    _call("nfd_pages_read", dev, stream, load().nfd_pages_read, pages.ref, batch.ref, _TYPES[some.dtype], ptr(k_out), ptr(v_out))
+    dev, n, dtype = pages.dev, batch.n_rows * pages.n_heads * pages.head_dim, (k_out if k_out is not None else v_out).dtype
+    assert batch.dev == dev and batch.table is not None
+    kp, vp = (_result(t, n, dtype, dev) if t is not None else None for t in (k_out, v_out))
+    _call("nfd_pages_read", dev, stream, load().nfd_pages_read, pages.ref, batch.ref, _TYPES[dtype], kp, vp)
     return k_out, v_out
 
 
 def attention_kv4(pages: Pages, batch: Batch, q, out, frame_tokens: int = 1, window: int = (1 << 31) - 1, stream=None):
     """nfd_attention_kv4: attention of q [n_rows, n_heads, head_dim] (bfloat16, rows may be strided) over a cache of 4-bit
     pages into out [n_rows, n_heads * head_dim]; frame_tokens = 1: causal, otherwise block-causal by frames."""
-    dev, n, dh = pages.device, batch.n_rows, pages.head_dim
-    assert batch.device == dev and batch.table is not None
-    h = q.shape[1] if q.dim() == 3 else q.shape[1] // dh
+    dev, n, dh = pages.dev, batch.n_rows, pages.head_dim
+    assert batch.dev == dev and batch.table is not None
+    h = _heads(q, dh)
     qs = _row_stride(q, n, h, dh, torch.bfloat16, dev)
-    assert out.is_contiguous() and out.dtype == torch.bfloat16 and out.device == dev and out.numel() == n * h * dh
     _call("nfd_attention_kv4", dev, stream, load().nfd_attention_kv4, pages.ref, batch.ref, h, q.data_ptr(), qs, frame_tokens,
-          window, out.data_ptr())
+          window, _result(out, n * h * dh, torch.bfloat16, dev))
     return out
 
 
 def cross_attention(states: States, batch: Batch, q, out, stream=None):
     """nfd_cross_attention: attention of q [n_rows, n_heads, head_dim] (the states' type, rows may be strided) to each row's
     sequence of encoder states, of which batch.kv_len tells how many there are (None: all), into out [n_rows, n_heads * head_dim]."""
-    dev, n, dh = states.device, batch.n_rows, states.head_dim
-    assert batch.device in (dev, None) and batch.n_seqs == states.n_seqs
-    h = q.shape[1] if q.dim() == 3 else q.shape[1] // dh
-    qs = _row_stride(q, n, h, dh, states.dtype, dev)
-    assert out.is_contiguous() and out.dtype == states.dtype and out.device == dev and out.numel() == n * h * dh
+    dev, n, dh, dtype = states.dev, batch.n_rows, states.head_dim, states.dtype
+    assert batch.dev in (dev, None) and batch.n_seqs == states.n_seqs
+    h = _heads(q, dh)
+    qs = _row_stride(q, n, h, dh, dtype, dev)
     _call("nfd_cross_attention", dev, stream, load().nfd_cross_attention, states.ref, batch.ref, h, q.data_ptr(), qs,
-          out.data_ptr())
+          _result(out, n * h * dh, dtype, dev))
     return out
 
 
