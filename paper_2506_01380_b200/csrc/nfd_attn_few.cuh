@@ -1,23 +1,26 @@
 // Attention of a few rows to many keys, on 4-bit pages or bf16 states: single tokens, short speculations, a row or two of a
 // decoder against an encoder's states.
 //
-// The rows of a sequence that share a head of keys (rows x heads that share it) are one 16-row operand of mma.m16n8k16; a
-// unit of work is (sequence, head of keys, 16 rows).  The bound is the stream of K and V: a unit is split over the CTAs of a
+// A unit of work is (sequence, head of keys, up to 8 NR rows: rows x heads that share it).  The bound is the stream of K and V, and with
+// 4-bit pages the instructions that make bf16 numbers of codes; a unit is split over the CTAs of a
 // cluster and their warps, each of which takes chunks of KC keys in turn, with a ring of its own in shared memory that
-// cp.async fills NST chunks ahead, an online softmax of its own, and no barrier until the end.  Then the warps of a CTA merge through
+// cp.async fills NST - 1 chunks ahead, an online softmax of its own, and no barrier until the end.  Then the warps of a CTA merge through
 // shared memory and the CTAs of a cluster through distributed shared memory, in a fixed order, each writing its share of the result: no
 // working memory in HBM, one launch.
 //
-// Products take their operands as they lie: the inner index of either product may be permuted as long as both of its
-// operands are, so that a lane's share of a key is a run of its row (for S = Q K^T) and a lane's share of a value a run of dims
-// (for O = P V); 4-bit codes become bf16 numbers in registers: the code goes into the mantissa of 128 + n, 128 + z is
+// Both products have the keys' operand on the 16-wide side of mma.m16n8k16 and the rows on the 8-wide side:
+//     S^T = K Q^T   (16 keys x 8 rows),   O^T += V^T P^T   (16 dims x 8 rows)
+// so that what a key costs does not grow with the 16 rows of a tile (with the rows on that side: twice the products and twice the registers
+// for rows that are not there).  P^T changes sides by movmatrix.  The inner index of either product may be permuted as long as both of its
+// operands are, so that a lane's share of a key is a run of its row (for S) and a lane's share of a value a run of dims
+// (for O); 4-bit codes become bf16 numbers in registers: the code goes into the mantissa of 128 + n, 128 + z is
 // subtracted (exact), the step multiplied (exact: 4 by 4 bits).
 #pragma once
 #include "nfd_attn_any.cuh"
 #include "nfd_sm100.cuh"
 
-#define FEW_WARPS 4
-#define FEW_ROWS 16
+#define FEW_WARPS 8
+#define FEW_MOST 32               // rows of a unit that this kernel takes
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -35,6 +38,12 @@ __device__ __forceinline__ void mma_bf16(float *d, const uint32_t *a, uint32_t b
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// an 8 x 8 matrix of 16-bit numbers, a pair of a row to a lane, the other way round
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
@@ -59,98 +68,79 @@ __device__ __forceinline__ uint32_t kv4_step2(uint32_t w0, uint32_t w1) { return
 // A warp's chunk of keys in shared memory, for 4-bit pages: codes of K and V, their words, and which keys are there.
 template <int DH> struct FewKv4 {
     static constexpr bool KV4 = true;
-    static constexpr int KC = 64;
+    static constexpr int KC = 32;
+    static constexpr int NST = 4;
     static constexpr int RB = DH / 2;                       // bytes of a row of codes
     static constexpr int WB = DH == 128 ? 8 : 4;            // bytes of a key's words (DH 32: a word and its neighbour)
     static constexpr int PR = RB / 16;                      // 16-byte pieces of a row
     static constexpr int STAGE = 2 * KC * (RB + WB) + 16;
     Kv4Keys<DH> K;
-    long long place[2];                                     // of keys lane, lane + 32 of the chunk after the next one
+    long long place;                                        // of key `lane` of the chunk after the next one
 
     __device__ __forceinline__ void look_up(const BatchD &B, int s, int h, int base, int hi) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int p = base + 32 * i + (threadIdx.x & 31);
-            place[i] = -1;
-            if (p < hi) {
-                const long long at = K.P.place(B, s, p);
-                if (at >= 0) place[i] = at + (long long)h * K.P.page_tokens;
-            }
+        const int p = base + (threadIdx.x & 31);
+        place = -1;
+        if (p < hi) {
+            const long long at = K.P.place(B, s, p);
+            if (at >= 0) place = at + (long long)h * K.P.page_tokens;
         }
     }
     // the copies of a chunk; its places have been looked up
     __device__ __forceinline__ void fill(uint8_t *stage, uint32_t st, const BatchD &B, int s, int h, int base, int hi) {
         const int lane = threadIdx.x & 31;
         uint32_t *meta = reinterpret_cast<uint32_t *>(stage + 2 * KC * (RB + WB));
+        const uint32_t there = __ballot_sync(0xffffffffu, place >= 0), odd = __ballot_sync(0xffffffffu, place & 1);
+        if (lane == 0) meta[0] = there, meta[1] = odd;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t there = __ballot_sync(0xffffffffu, place[i] >= 0), odd = __ballot_sync(0xffffffffu, place[i] & 1);
-            if (lane == 0) meta[i] = there, meta[2 + i] = odd;
-#pragma unroll
-            for (int j = 0; j < PR; ++j) {
-                const int src = j * (32 / PR) + lane / PR, piece = lane % PR;
-                const long long at = __shfl_sync(0xffffffffu, place[i], src);
-                const size_t off = at >= 0 ? (size_t)at * RB + piece * 16 : 0;
-                const uint32_t d = st + (32 * i + src) * RB + piece * 16, n = at >= 0 ? 16 : 0;
-                cp_async16(d, (const uint8_t *)K.P.k + off, n);
-                cp_async16(d + KC * RB, (const uint8_t *)K.P.v + off, n);
-            }
-            const long long at = place[i] >= 0 ? place[i] : 0;
-            const uint32_t d = st + 2 * KC * RB + (32 * i + lane) * WB, n = place[i] >= 0;
-            if (DH == 128) {
-                cp_async8(d, K.P.k_scale + at * 4, n * 8);
-                cp_async8(d + KC * WB, K.P.v_scale + at * 4, n * 8);
-            } else if (DH == 64) {
-                cp_async4(d, K.P.k_scale + at * 2, n * 4);
-                cp_async4(d + KC * WB, K.P.v_scale + at * 2, n * 4);
-            } else {
-                // one word a key: the aligned pair it is in, or, where it is the pair's first, only itself
-                const uint32_t m = n ? 2 + 2 * (uint32_t)(at & 1) : 0;
-                cp_async4(d, K.P.k_scale + (at & ~1LL), m);
-                cp_async4(d + KC * WB, K.P.v_scale + (at & ~1LL), m);
-            }
+        for (int j = 0; j < PR; ++j) {
+            const int src = j * (32 / PR) + lane / PR, piece = lane % PR;
+            const long long at = __shfl_sync(0xffffffffu, place, src);
+            const size_t off = at >= 0 ? (size_t)at * RB + piece * 16 : 0;
+            const uint32_t d = st + src * RB + piece * 16, n = at >= 0 ? 16 : 0;
+            cp_async16(d, (const uint8_t *)K.P.k + off, n);
+            cp_async16(d + KC * RB, (const uint8_t *)K.P.v + off, n);
+        }
+        const long long at = place >= 0 ? place : 0;
+        const uint32_t d = st + 2 * KC * RB + lane * WB, n = place >= 0;
+        if (DH == 128) {
+            cp_async8(d, K.P.k_scale + at * 4, n * 8);
+            cp_async8(d + KC * WB, K.P.v_scale + at * 4, n * 8);
+        } else if (DH == 64) {
+            cp_async4(d, K.P.k_scale + at * 2, n * 4);
+            cp_async4(d + KC * WB, K.P.v_scale + at * 2, n * 4);
+        } else {
+            // one word a key: the aligned pair it is in, or, where it is the pair's first, only itself
+            const uint32_t m = n ? 2 + 2 * (uint32_t)(at & 1) : 0;
+            cp_async4(d, K.P.k_scale + (at & ~1LL), m);
+            cp_async4(d + KC * WB, K.P.v_scale + (at & ~1LL), m);
         }
     }
-    __device__ __forceinline__ void masks(const uint8_t *stage, uint32_t *there) const {
-        const uint32_t *meta = reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB));
-        there[0] = meta[0], there[1] = meta[1];
-    }
+    static __device__ __forceinline__ uint32_t mask(const uint8_t *stage) { return *reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB)); }
     // Values whose step is not finite become zeros (a product with the 0 of a row that does not see them would be NaN); a bit for each
-    // of their keys.  True: there are some.
-    static __device__ __forceinline__ bool take_out(uint8_t *stage, uint32_t *bad) {
+    // of their keys.
+    static __device__ __forceinline__ uint32_t take_out(uint8_t *stage) {
         const int lane = threadIdx.x & 31;
-        bool mine[2];
+        uint32_t *w = reinterpret_cast<uint32_t *>(stage + 2 * KC * RB + KC * WB + lane * WB);
+        bool mine = false;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t *w = reinterpret_cast<uint32_t *>(stage + 2 * KC * RB + KC * WB + (32 * i + lane) * WB);
-            mine[i] = false;
-#pragma unroll
-            for (int j = 0; j < WB / 4; ++j) {
-                const uint32_t v = w[j];
-                const bool b0 = (v & 0x7F80u) == 0x7F80u, b1 = (v >> 16 & 0x7F80u) == 0x7F80u;
-                if (DH == 32) {
-                    const uint32_t *meta = reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB));
-                    mine[i] |= meta[2 + i] >> lane & 1 ? b1 : b0;
-                } else {
-                    mine[i] |= b0 || b1;
-                }
-            }
+        for (int j = 0; j < WB / 4; ++j) {
+            const uint32_t v = w[j];
+            const bool b0 = (v & 0x7F80u) == 0x7F80u, b1 = (v >> 16 & 0x7F80u) == 0x7F80u;
+            if (DH == 32) mine |= reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB))[1] >> lane & 1 ? b1 : b0;
+            else mine |= b0 || b1;
         }
-        if (!__any_sync(0xffffffffu, mine[0] || mine[1])) return false;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t *w = reinterpret_cast<uint32_t *>(stage + 2 * KC * RB + KC * WB + (32 * i + lane) * WB);
-            if (mine[i])
+        const uint32_t bad = __ballot_sync(0xffffffffu, mine);
+        if (bad) {
+            if (mine)
                 for (int j = 0; j < WB / 4; ++j) w[j] = 0;
-            bad[i] = __ballot_sync(0xffffffffu, mine[i]);
+            __syncwarp();
         }
-        __syncwarp();
-        return true;
+        return bad;
     }
     static __device__ __forceinline__ uint32_t word(const uint8_t *w, int key, int group, const uint8_t *stage) {
         if (DH == 32) {
             const uint32_t *meta = reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB));
-            return *reinterpret_cast<const uint16_t *>(w + key * WB + 2 * (meta[2 + (key >> 5)] >> (key & 31) & 1));
+            return *reinterpret_cast<const uint16_t *>(w + key * WB + 2 * (meta[1] >> key & 1));
         }
         return *reinterpret_cast<const uint16_t *>(w + key * WB + 2 * group);
     }
@@ -213,7 +203,8 @@ template <int DH> struct FewKv4 {
 // The same for bf16 states.  Rows are swizzled in 16-byte pieces so that neither operand's reads meet in a bank.
 template <int DH> struct FewStates {
     static constexpr bool KV4 = false;
-    static constexpr int KC = DH == 128 ? 16 : 32;
+    static constexpr int KC = DH == 32 ? 32 : 16;
+    static constexpr int NST = DH == 128 ? 3 : 4;
     static constexpr int RB = 2 * DH, PR = RB / 16;
     static constexpr int STAGE = 2 * KC * RB + 16;
     StateKeys<bf16, DH> K;
@@ -240,10 +231,8 @@ template <int DH> struct FewStates {
             cp_async16(st + at_v(key, piece), K.v + off, t ? 16 : 0);
         }
     }
-    __device__ __forceinline__ void masks(const uint8_t *stage, uint32_t *m) const {
-        m[0] = *reinterpret_cast<const uint32_t *>(stage + 2 * KC * RB), m[1] = 0;
-    }
-    static __device__ __forceinline__ bool take_out(uint8_t *, uint32_t *) { return false; }     // (all rows see the same keys)
+    static __device__ __forceinline__ uint32_t mask(const uint8_t *stage) { return *reinterpret_cast<const uint32_t *>(stage + 2 * KC * RB); }
+    static __device__ __forceinline__ uint32_t take_out(uint8_t *) { return 0; }                // (all rows see the same keys)
     static __device__ __forceinline__ int q_dim(int step, int c) { return 8 * (c + 4 * (step / 2)) + 4 * (step % 2); }
     static __device__ __forceinline__ void k_frag(const uint8_t *stage, int key, int c, uint32_t *b) {
 #pragma unroll
@@ -272,55 +261,31 @@ template <int DH> struct FewStates {
     }
 };
 
-template <typename Src, int DH> struct FewCfg {
-    static constexpr int NST = 4;
-    static constexpr int STATE = FEW_ROWS * (DH + 2) * 4;                         // O, m, l of a warp or a CTA
-    static constexpr int RING = (NST * Src::STAGE + 15) / 16 * 16;
+template <typename Src, int DH, int NR> struct FewCfg {
+    static constexpr int ROWS = 8 * NR;
+    static constexpr int STATE = ROWS * (DH + 2) * 4;                             // O, m, l of a warp or a CTA
+    static constexpr int RING = (Src::NST * Src::STAGE + 15) / 16 * 16;
     static constexpr int WARP = RING > STATE ? RING : STATE;                      // a warp's ring, then its state
     static constexpr int SMEM = FEW_WARPS * WARP + STATE;
+    static_assert(SMEM <= 232448 - 1024, "shared memory of a CTA");
 };
 
-// grid: (CTAs of a cluster x heads of keys, sequences, tiles of 16 rows)
-template <typename Src, int DH>
+// grid: (CTAs of a cluster x heads of keys, sequences, tiles of 8 NR rows)
+template <typename Src, int DH, int NR>
 __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, const AttnRows A, Src src, int split) {
-    using F = FewCfg<Src, DH>;
-    constexpr int KC = Src::KC, NT = DH / 8, NS = DH / 16, KT = KC / 8;
+    using F = FewCfg<Src, DH, NR>;
+    constexpr int KC = Src::KC, NST = Src::NST, NS = DH / 16, KT = KC / 16, ROWS = F::ROWS;
     extern __shared__ __align__(16) uint8_t few_smem[];
+    __shared__ int2 s_range[ROWS];                                                // keys that a row sees
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, n = lane >> 2;
-    const int rank = blockIdx.x % split, h = blockIdx.x / split, s = blockIdx.y, r0 = blockIdx.z * FEW_ROWS;
+    const int rank = blockIdx.x % split, h = blockIdx.x / split, s = blockIdx.y, r0 = blockIdx.z * ROWS;
     const int2 sr = B.rows(s);
     const int rows = min(sr.y, B.max_rows) * A.share;                             // of the whole unit; row r: row r / share, head h * share + r % share
     if (r0 >= rows) return;                                                       // (the whole cluster)
-    const int nr = min(FEW_ROWS, rows - r0);
-    // what the rows of this lane see, and all of them together
-    KeyRange kr[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = n + 8 * i;
-        kr[i] = src.K.range(B, s, sr.y, min(r0 + min(r, nr - 1), rows - 1) / A.share);
-    }
+    const int nr = min(ROWS, rows - r0);
     const KeyRange first = src.K.range(B, s, sr.y, r0 / A.share), last = src.K.range(B, s, sr.y, (r0 + nr - 1) / A.share);
     // (bounds rise with the row, but for rows of tokens below 0, which see nothing: 0, 0)
     const int lo = first.lo, hi = last.hi;
-    // queries, scaled for exp2 later: two rows of this lane, DH / 16 steps
-    uint32_t qa[NS][4];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = n + 8 * i, rr = r0 + min(r, nr - 1);
-        const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (h * A.share + rr % A.share) * DH;
-#pragma unroll
-        for (int st = 0; st < NS; ++st) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(q + Src::q_dim(st, c));
-            qa[st][i] = v.x, qa[st][2 + i] = v.y;
-        }
-    }
-    const float cs = 1.4426950408889634f * rsqrtf((float)DH);
-    float o[NT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[t][e] = 0.f;
-    const bool two = nr > 8;                                                      // rows 8 .. 15 are there
 
     uint8_t *ring = few_smem + warp * F::WARP;
     const uint32_t ring_s = smem_u32(ring);
@@ -329,7 +294,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
     int base = next;
     src.look_up(B, s, h, next, hi);
 #pragma unroll
-    for (int i = 0; i < F::NST - 1; ++i) {
+    for (int i = 0; i < NST - 1; ++i) {
         if (next < hi) {
             src.fill(ring + i * Src::STAGE, ring_s + i * Src::STAGE, B, s, h, next, hi);
             next += step;
@@ -337,10 +302,36 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
         }
         cp_async_commit();
     }
+    if (threadIdx.x < ROWS) {
+        const KeyRange r = src.K.range(B, s, sr.y, (r0 + min((int)threadIdx.x, nr - 1)) / A.share);
+        s_range[threadIdx.x] = make_int2(r.lo, r.hi);
+    }
+    // queries: row n of every tile of 8, in the order of K's inner index
+    uint32_t qb[NR][NS][2];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+        const int rr = r0 + min(8 * t + n, nr - 1);
+        const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (h * A.share + rr % A.share) * DH;
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(q + Src::q_dim(st, c));
+            qb[t][st][0] = v.x, qb[t][st][1] = v.y;
+        }
+    }
+    const float cs = 1.4426950408889634f * rsqrtf((float)DH);
+    // this lane's rows: 2 c and 2 c + 1 of every tile of 8
+    float o[NR][NS][4], m[NR][2], l[NR][2];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+        m[t][0] = m[t][1] = -INFINITY, l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
+    }
+    __syncthreads();
     int st = 0;
     for (; base < hi; base += step) {
         {
-            const int f = st == 0 ? F::NST - 1 : st - 1;
+            const int f = st == 0 ? NST - 1 : st - 1;
             if (next < hi) {
                 src.fill(ring + f * Src::STAGE, ring_s + f * Src::STAGE, B, s, h, next, hi);
                 next += step;
@@ -348,97 +339,115 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
             }
             cp_async_commit();
         }
-        cp_async_wait<F::NST - 1>();
+        cp_async_wait<NST - 1>();
         __syncwarp();
         uint8_t *stage = ring + st * Src::STAGE;
-        uint32_t there[2], bad[2];
-        src.masks(stage, there);
-        float x[KT][4];
+        const uint32_t all = KC == 32 ? 0xffffffffu : (1u << KC) - 1, there = Src::mask(stage), bad = Src::take_out(stage);
+        float x[KT][NR][4];
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            // column j of tile u is key 8 u + j / 2 + 4 (j % 2): a lane's four keys of a product step over P are 4 apart
-            uint32_t b[2 * NS];
-            Src::k_frag(stage, 8 * u + (n >> 1) + 4 * (n & 1), c, b);
-            x[u][0] = x[u][1] = x[u][2] = x[u][3] = 0.f;
+            // row i of half j of tile u is key 16 u + 8 j + i / 2 + 4 (i % 2): a lane's four keys of a product with V are 4 apart
+            uint32_t a[2][2 * NS];
+            Src::k_frag(stage, 16 * u + (n >> 1) + 4 * (n & 1), c, a[0]);
+            Src::k_frag(stage, 16 * u + 8 + (n >> 1) + 4 * (n & 1), c, a[1]);
 #pragma unroll
-            for (int k = 0; k < NS; ++k) mma_bf16(x[u], qa[k], b[2 * k], b[2 * k + 1]);
+            for (int t = 0; t < NR; ++t) {
+                x[u][t][0] = x[u][t][1] = x[u][t][2] = x[u][t][3] = 0.f;
+#pragma unroll
+                for (int k = 0; k < NS; ++k) {
+                    const uint32_t ak[4] = {a[0][2 * k], a[1][2 * k], a[0][2 * k + 1], a[1][2 * k + 1]};
+                    mma_bf16(x[u][t], ak, qb[t][k][0], qb[t][k][1]);
+                }
+            }
         }
-        const bool all = (there[0] & (KC >= 32 ? 0xffffffffu : (1u << KC) - 1)) == (KC >= 32 ? 0xffffffffu : (1u << KC) - 1) &&
-                         (KC <= 32 || there[1] == 0xffffffffu);
-        const bool inside = base >= kr[0].lo && base >= kr[1].lo && base + KC <= kr[0].hi && base + KC <= kr[1].hi;
-        if (!__all_sync(0xffffffffu, all && inside)) {
+        // x[u][t]: keys n' and n' + 8 (0, 1 and 2, 3) of tile u, rows 2 c and 2 c + 1 (0, 2 and 1, 3)
+        if ((there & all) != all || bad || base < s_range[nr - 1].x || base + KC > s_range[0].y) {
+#pragma unroll
+            for (int t = 0; t < NR; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int2 kr = s_range[8 * t + 2 * c + e];
+#pragma unroll
+                    for (int u = 0; u < KT; ++u)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int key = 16 * u + 8 * j + (n >> 1) + 4 * (n & 1), p = base + key;
+                            const bool seen = (there >> key & 1) && p >= kr.x && p < kr.y;
+                            if (!seen) x[u][t][2 * j + e] = -INFINITY;
+                            else if (bad >> key & 1) l[t][e] = NAN;               // the row sees a value that is not finite
+                        }
+                }
+        }
+        // the rows' maxima; what was summed before is rescaled only where one rose
+        float mn[NR][2];
+        bool rise = false;
+#pragma unroll
+        for (int t = 0; t < NR; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float v = m[t][e];
+#pragma unroll
+                for (int u = 0; u < KT; ++u) v = fmaxf(v, fmaxf(x[u][t][e], x[u][t][2 + e]));
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+                mn[t][e] = v, rise |= v != m[t][e];
+            }
+        if (__any_sync(0xffffffffu, rise)) {
+#pragma unroll
+            for (int t = 0; t < NR; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float f = mn[t][e] == m[t][e] ? 1.0f : few_exp2((m[t][e] - mn[t][e]) * cs);
+                    m[t][e] = mn[t][e], l[t][e] *= f;
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) o[t][i][e] *= f, o[t][i][2 + e] *= f;
+                }
+        }
+        uint32_t p[KT][NR][2];                                                    // P^T: keys 2 c.., row n
+#pragma unroll
+        for (int t = 0; t < NR; ++t) {
+            const float m0 = m[t][0] == -INFINITY ? 0.f : m[t][0] * cs, m1 = m[t][1] == -INFINITY ? 0.f : m[t][1] * cs;
 #pragma unroll
             for (int u = 0; u < KT; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int key = 8 * u + c + 4 * (e & 1), p = base + key;
-                    const bool seen = (there[key >> 5] >> (key & 31) & 1) && p >= kr[e >> 1].lo && p < kr[e >> 1].hi;
-                    if (!seen) x[u][e] = -INFINITY;
+                for (int j = 0; j < 2; ++j) {
+                    const float a = few_exp2(fmaf(x[u][t][2 * j], cs, -m0)), b = few_exp2(fmaf(x[u][t][2 * j + 1], cs, -m1));
+                    l[t][0] += a, l[t][1] += b;
+                    p[u][t][j] = transpose8(bf16_pair(a, b));
                 }
         }
-        if (Src::take_out(stage, bad))
-            for (int key = 0; key < KC; ++key)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if ((bad[key >> 5] >> (key & 31) & 1) && base + key >= kr[i].lo && base + key < kr[i].hi) l[i] = NAN;
-        // the rows' maxima; what was summed before is rescaled only where one rose
-        float mn[2] = {m[0], m[1]};
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            mn[0] = fmaxf(mn[0], fmaxf(x[u][0], x[u][1]));
-            mn[1] = fmaxf(mn[1], fmaxf(x[u][2], x[u][3]));
-        }
+            // (columns 2 c and 2 c + 1 of a half are keys c and c + 4 of it)
+            uint32_t b0[2 * NS], b1[2 * NS];
+            Src::v_frag(stage, 16 * u + c, n, b0);
+            Src::v_frag(stage, 16 * u + 8 + c, n, b1);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            mn[i] = fmaxf(mn[i], __shfl_xor_sync(0xffffffffu, mn[i], 1));
-            mn[i] = fmaxf(mn[i], __shfl_xor_sync(0xffffffffu, mn[i], 2));
-        }
-        if (__any_sync(0xffffffffu, mn[0] != m[0] || mn[1] != m[1])) {
+            for (int i = 0; i < NS; ++i) {
+                const uint32_t a[4] = {b0[2 * i], b0[2 * i + 1], b1[2 * i], b1[2 * i + 1]};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float f = mn[i] == m[i] ? 1.0f : few_exp2((m[i] - mn[i]) * cs);
-                m[i] = mn[i], l[i] *= f;
-#pragma unroll
-                for (int t = 0; t < NT; ++t) o[t][2 * i] *= f, o[t][2 * i + 1] *= f;
+                for (int t = 0; t < NR; ++t) mma_bf16(o[t][i], a, p[u][t][0], p[u][t][1]);
             }
-        }
-        const float mc[2] = {m[0] == -INFINITY ? 0.f : m[0] * cs, m[1] == -INFINITY ? 0.f : m[1] * cs};
-        uint32_t p[KT][2];
-#pragma unroll
-        for (int u = 0; u < KT; ++u) {
-            const float a = few_exp2(fmaf(x[u][0], cs, -mc[0])), b = few_exp2(fmaf(x[u][1], cs, -mc[0]));
-            l[0] += a + b, p[u][0] = bf16_pair(a, b), p[u][1] = 0;
-            if (two) {
-                const float d = few_exp2(fmaf(x[u][2], cs, -mc[1])), e = few_exp2(fmaf(x[u][3], cs, -mc[1]));
-                l[1] += d + e, p[u][1] = bf16_pair(d, e);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < KT / 2; ++j) {
-            const uint32_t a[4] = {p[2 * j][0], p[2 * j][1], p[2 * j + 1][0], p[2 * j + 1][1]};
-            uint32_t b0[NT], b1[NT];
-            Src::v_frag(stage, 16 * j + c, n, b0);
-            Src::v_frag(stage, 16 * j + 8 + c, n, b1);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) mma_bf16(o[t], a, b0[t], b1[t]);
         }
         __syncwarp();                                                             // the stage may be filled again
-        if (++st == F::NST) st = 0;
+        if (++st == NST) st = 0;
     }
     cp_async_wait<0>();
     __syncwarp();
-    // this warp's state into its (drained) ring
+    // this warp's state into its (drained) ring: O by rows, then m and l of the rows
     float *S = reinterpret_cast<float *>(ring);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-        if (c == 0) S[FEW_ROWS * DH + 2 * (n + 8 * i)] = m[i] * cs, S[FEW_ROWS * DH + 2 * (n + 8 * i) + 1] = l[i];
+    for (int t = 0; t < NR; ++t) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[t][e] += __shfl_xor_sync(0xffffffffu, l[t][e], d);
+            const int r = 8 * t + 2 * c + e;
+            if (n == 0) S[ROWS * DH + 2 * r] = m[t][e] * cs, S[ROWS * DH + 2 * r + 1] = l[t][e];
+#pragma unroll
+            for (int i = 0; i < NS; ++i) S[r * DH + Src::o_dim(2 * i, n)] = o[t][i][e], S[r * DH + Src::o_dim(2 * i + 1, n)] = o[t][i][2 + e];
+        }
     }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) S[(n + 8 * (e >> 1)) * DH + Src::o_dim(t, 2 * c + (e & 1))] = o[t][e];
     __syncthreads();
     // the CTA's
     float *T = reinterpret_cast<float *>(few_smem + FEW_WARPS * F::WARP);
@@ -452,22 +461,22 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
         const int r = i / (DH / 4), d = i % (DH / 4) * 4;
         float mx = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < FEW_WARPS; ++w) mx = fmaxf(mx, reinterpret_cast<const float *>(few_smem + w * F::WARP)[FEW_ROWS * DH + 2 * r]);
+        for (int w = 0; w < FEW_WARPS; ++w) mx = fmaxf(mx, reinterpret_cast<const float *>(few_smem + w * F::WARP)[ROWS * DH + 2 * r]);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < FEW_WARPS; ++w) {
             const float *W = reinterpret_cast<const float *>(few_smem + w * F::WARP);
-            const float mw = W[FEW_ROWS * DH + 2 * r], f = mw == -INFINITY ? 0.f : few_exp2(mw - mx);
+            const float mw = W[ROWS * DH + 2 * r], f = mw == -INFINITY ? 0.f : few_exp2(mw - mx);
             const float4 x = *reinterpret_cast<const float4 *>(W + r * DH + d);
-            sum = fmaf(W[FEW_ROWS * DH + 2 * r + 1], f, sum);
+            sum = fmaf(W[ROWS * DH + 2 * r + 1], f, sum);
             v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
         }
         if (split == 1) {
             write(r, d, v, sum);
         } else {
             *reinterpret_cast<float4 *>(T + r * DH + d) = v;
-            if (d == 0) T[FEW_ROWS * DH + 2 * r] = mx, T[FEW_ROWS * DH + 2 * r + 1] = sum;
+            if (d == 0) T[ROWS * DH + 2 * r] = mx, T[ROWS * DH + 2 * r + 1] = sum;
         }
     }
     if (split == 1) return;
@@ -477,11 +486,11 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
     for (int i = rank + split * threadIdx.x; i < nr * (DH / 4); i += split * 32 * FEW_WARPS) {
         const int r = i / (DH / 4), d = i % (DH / 4) * 4;
         float mx = -INFINITY;
-        for (int k = 0; k < split; ++k) mx = fmaxf(mx, ld_cluster_f2(cluster_map(Ts + (FEW_ROWS * DH + 2 * r) * 4, k)).x);
+        for (int k = 0; k < split; ++k) mx = fmaxf(mx, ld_cluster_f2(cluster_map(Ts + (ROWS * DH + 2 * r) * 4, k)).x);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         float sum = 0.f;
         for (int k = 0; k < split; ++k) {
-            const float2 ml = ld_cluster_f2(cluster_map(Ts + (FEW_ROWS * DH + 2 * r) * 4, k));
+            const float2 ml = ld_cluster_f2(cluster_map(Ts + (ROWS * DH + 2 * r) * 4, k));
             const float4 x = ld_cluster_f4(cluster_map(Ts + (r * DH + d) * 4, k));
             const float f = ml.x == -INFINITY ? 0.f : few_exp2(ml.x - mx);
             sum = fmaf(ml.y, f, sum);
@@ -492,32 +501,43 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
     cluster_sync_all();                                                           // nobody leaves while its state is read
 }
 
-// CTAs of a cluster that a unit is split over.
-static int few_split(int units, long long keys, int kc, int n_sm) {
+// CTAs of a cluster that a unit is split over: as many as the device holds at once, and no more than give every warp a chunk or two.
+static int few_split(long long units, long long keys, int kc, int n_sm, int per_sm) {
     const long long chunks = (keys + kc - 1) / kc;
     int split = 1;
-    while (split < 8 && (long long)units * split * 2 <= 3LL * n_sm && chunks > (long long)split * FEW_WARPS) split *= 2;
+    while (split < 8 && units * split * 2 <= (long long)n_sm * per_sm && chunks > (long long)split * FEW_WARPS) split *= 2;
     return split;
 }
 
-template <typename Src, int DH>
-static int launch_attn_few(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
-    using F = FewCfg<Src, DH>;
-    const int tiles = (B.max_rows * A.share + FEW_ROWS - 1) / FEW_ROWS;
-    const int split = few_split((int)fmin(1e6, (double)kv_heads * B.n_seqs * tiles), keys, Src::KC, n_sm);
+template <typename Src, int DH, int NR>
+static int launch_attn_few_nr(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
+    using F = FewCfg<Src, DH, NR>;
+    auto kern = k_attn_few<Src, DH, NR>;
+    static int per_sm[NFD_PAGED_DEVICES];                                         // (once per device and kernel)
+    if (!per_sm[dev]) {
+        int n = 0;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 32 * FEW_WARPS, F::SMEM) != cudaSuccess || n < 1)
+            return NFD_E_CUDA;
+        per_sm[dev] = n;
+    }
+    const long long tiles = ((long long)B.max_rows * A.share + F::ROWS - 1) / F::ROWS;
+    if (tiles > 65535) return NFD_E_RANGE;
+    const int split = few_split((long long)kv_heads * B.n_seqs * tiles, keys, Src::KC, n_sm, per_sm[dev]);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kv_heads * split, B.n_seqs, tiles), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = F::SMEM, cfg.stream = st;
+    cfg.gridDim = dim3(kv_heads * split, B.n_seqs, (unsigned)tiles), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = F::SMEM, cfg.stream = st;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at, cfg.numAttrs = split > 1;
-    static bool sized[NFD_PAGED_DEVICES];                                         // (once per device and kernel)
-    if (!sized[dev]) {
-        if (cudaFuncSetAttribute(k_attn_few<Src, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess) return NFD_E_CUDA;
-        sized[dev] = true;
-    }
-    if (cudaLaunchKernelEx(&cfg, k_attn_few<Src, DH>, B, A, src, split) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, kern, B, A, src, split) != cudaSuccess) {
         cudaGetLastError();
         return NFD_E_CUDA;
     }
     return NFD_OK;
+}
+template <typename Src, int DH>
+static int launch_attn_few(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
+    if ((long long)B.max_rows * A.share <= 8) return launch_attn_few_nr<Src, DH, 1>(B, A, src, kv_heads, keys, dev, n_sm, st);
+    if (DH == 128 || (long long)B.max_rows * A.share <= 16) return launch_attn_few_nr<Src, DH, 2>(B, A, src, kv_heads, keys, dev, n_sm, st);
+    return launch_attn_few_nr<Src, DH, DH == 128 ? 2 : 4>(B, A, src, kv_heads, keys, dev, n_sm, st);
 }
