@@ -1,0 +1,237 @@
+// Attention of a batch's rows to fp32 encoder states, on the fp32 pipes.
+//
+// A CTA takes 32 or 64 rows (rows x heads that share a head of keys) of a sequence and walks its keys in tiles of 64, the next tile's copies in
+// flight: S = Q K^T with 4 rows x 4 keys to a thread, an online softmax per row over the 16 lanes that hold it, P through shared memory
+// (a row's 16 lanes write and read it, no barrier), O += P V with 4 rows x DH / 16 dims to a thread.  All operands are read as 16-byte words
+// along their rows, rows are padded by one word so that no two lanes of a quarter warp meet in a bank: 64 FMAs for eight words either way, which keeps
+// the FMA pipe ahead of the shared-memory port.  Keys that are not seen are copied as zeros and take a score of -inf.
+// Few units with many keys are split over the CTAs of a cluster and merged through distributed shared memory.
+// Bound by FMAs for many rows, by the chain of a tile (copy, S, softmax, P V) for few.
+#pragma once
+#include "nfd_attn_few.cuh"
+
+#define F32_KEYS 64
+
+template <int DH, int ROWS> struct F32Cfg {
+    static constexpr int THREADS = 4 * ROWS;
+    static constexpr int LD = DH + 4, LP = F32_KEYS + 4;                // floats of a padded row
+    static constexpr int AT_K = ROWS * LD, AT_V = AT_K + 2 * F32_KEYS * LD, AT_P = AT_V + 2 * F32_KEYS * LD,
+                         AT_M = AT_P + ROWS * LP, FLOATS = AT_M + 2 * F32_KEYS;
+    static constexpr int SMEM = FLOATS * 4;
+    static_assert(ROWS * (DH + 2) <= AT_K + F32_KEYS * LD, "a CTA's state lies over Q and K");
+};
+
+template <int DH, int ROWS>
+__global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const AttnRows A, const StateKeys<float, DH> K, int split) {
+    using C = F32Cfg<DH, ROWS>;
+    constexpr int LD = C::LD, LP = C::LP, ND = DH / 16, W = DH / 4;
+    extern __shared__ __align__(16) float f32_smem[];
+    float *sQ = f32_smem, *sP = f32_smem + C::AT_P;
+    uint32_t *sM = reinterpret_cast<uint32_t *>(f32_smem + C::AT_M);    // keys that are there, of two tiles
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int rank = blockIdx.x % split, h = blockIdx.x / split, s = blockIdx.y, r0 = blockIdx.z * ROWS;
+    const int2 sr = B.rows(s);
+    const int rows = min(sr.y, B.max_rows) * A.share;
+    if (r0 >= rows) return;                                             // (the whole cluster)
+    const int nr = min(ROWS, rows - r0);
+    const int keys = K.range(B, s, sr.y, 0).hi, tiles = (keys + F32_KEYS - 1) / F32_KEYS, per = (tiles + split - 1) / split;
+    const int t0 = min(tiles, rank * per), t1 = min(tiles, t0 + per);
+    const long long seq = s * K.seq_stride + h * K.head_stride;
+    const unsigned char *mask = K.mask ? K.mask + (size_t)s * K.n_keys : nullptr;
+    auto fill = [&](int t) {
+        const int b = t & 1, p0 = t * F32_KEYS;
+        // G threads to a key, a share of its row each
+        constexpr int G = C::THREADS / F32_KEYS, PART = DH / G;
+        const int key = tid / G, part = tid % G, p = p0 + key;
+        const bool here = p < keys && (!mask || mask[p]);
+        const long long at = here ? seq + p * K.key_stride + part * PART : 0;
+        const uint32_t dk = smem_u32(f32_smem + C::AT_K + (b * F32_KEYS + key) * LD + part * PART);
+        const uint32_t dv = smem_u32(f32_smem + C::AT_V + (b * F32_KEYS + key) * LD + part * PART);
+#pragma unroll
+        for (int i = 0; i < PART / 4; ++i) {
+            cp_async16(dk + 16 * i, K.k + at + (here ? 4 * i : 0), here ? 16 : 0);
+            cp_async16(dv + 16 * i, K.v + at + (here ? 4 * i : 0), here ? 16 : 0);
+        }
+        cp_async_commit();
+        if (part == 0) sM[64 * b + key] = here;
+    };
+    for (int i = tid; i < ROWS * W; i += C::THREADS) {
+        const int r = i / W, w = i % W, rr = r0 + min(r, nr - 1);
+        cp_async16(smem_u32(sQ + r * LD + 4 * w), (const float *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (h * A.share + rr % A.share) * DH + 4 * w, 16);
+    }
+    cp_async_commit();
+    if (t0 < t1) fill(t0);
+    const float cs = 1.4426950408889634f * (1.0f / sqrtf((float)DH));
+    float o[4][ND], m[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m[i] = -INFINITY, l[i] = 0.f;
+#pragma unroll
+        for (int e = 0; e < ND; ++e) o[i][e] = 0.f;
+    }
+    for (int t = t0; t < t1; ++t) {
+        if (t + 1 < t1) {
+            fill(t + 1);
+            cp_async_wait<1>();
+        } else {
+            cp_async_wait<0>();
+        }
+        __syncthreads();
+        const float *kt = f32_smem + C::AT_K + (t & 1) * F32_KEYS * LD, *vt = f32_smem + C::AT_V + (t & 1) * F32_KEYS * LD;
+        // S: rows 4 ty + i, keys tx + 16 j
+        float x[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
+#pragma unroll 4
+        for (int w = 0; w < W; ++w) {
+            float4 q[4], k[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = *reinterpret_cast<const float4 *>(sQ + (4 * ty + i) * LD + 4 * w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4 *>(kt + (tx + 16 * j) * LD + 4 * w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    x[i][j] = fmaf(q[i].x, k[j].x, fmaf(q[i].y, k[j].y, fmaf(q[i].z, k[j].z, fmaf(q[i].w, k[j].w, x[i][j]))));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (!sM[64 * (t & 1) + tx + 16 * j])
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i][j] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float mn = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
+            mn = fmaxf(mn, m[i]);
+            const float f = mn == m[i] ? 1.0f : exp2f((m[i] - mn) * cs), mc = mn == -INFINITY ? 0.f : mn;
+            m[i] = mn, l[i] *= f;
+#pragma unroll
+            for (int e = 0; e < ND; ++e) o[i][e] *= f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = exp2f((x[i][j] - mc) * cs);
+                l[i] += p, sP[(4 * ty + i) * LP + tx + 16 * j] = p;
+            }
+        }
+        __syncwarp();
+        // O: rows 4 ty + i, dims: words of up to four, tx-th of every 16 of them
+#pragma unroll 4
+        for (int k = 0; k < F32_KEYS; k += 4) {
+            float4 p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4 *>(sP + (4 * ty + i) * LP + k);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float v[ND];
+                if constexpr (DH == 32) {
+                    const float2 a = *reinterpret_cast<const float2 *>(vt + (k + u) * LD + 2 * tx);
+                    v[0] = a.x, v[1] = a.y;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < ND; e += 4) {
+                        const float4 a = *reinterpret_cast<const float4 *>(vt + (k + u) * LD + 16 * e + 4 * tx);
+                        v[e] = a.x, v[e + 1] = a.y, v[e + 2] = a.z, v[e + 3] = a.w;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float pu = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
+#pragma unroll
+                    for (int e = 0; e < ND; ++e) o[i][e] = fmaf(pu, v[e], o[i][e]);
+                }
+            }
+        }
+        __syncthreads();                                                // the tile may be overwritten
+    }
+    cp_async_wait<0>();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+    auto dim = [&](int e) { return DH == 32 ? 2 * tx + e : 16 * (e & ~3) + 4 * tx + (e & 3); };
+    auto place = [&](int r) {
+        const int rr = r0 + r;
+        return (float *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + h * A.share + rr % A.share) * DH;
+    };
+    if (split == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 4 * ty + i;
+            if (r >= nr) continue;
+            const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];
+            float *out = place(r);
+            if constexpr (DH == 32) {
+                *reinterpret_cast<float2 *>(out + dim(0)) = make_float2(o[i][0] * inv, o[i][1] * inv);
+            } else {
+#pragma unroll
+                for (int e = 0; e < ND; e += 4)
+                    *reinterpret_cast<float4 *>(out + dim(e)) = make_float4(o[i][e] * inv, o[i][e + 1] * inv, o[i][e + 2] * inv, o[i][e + 3] * inv);
+            }
+        }
+        return;
+    }
+    __syncthreads();
+    float *S = f32_smem;                                                // [rows][DH], then m and l of the rows
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 4 * ty + i;
+        if (tx == 0) S[ROWS * DH + 2 * r] = m[i] * cs, S[ROWS * DH + 2 * r + 1] = l[i];
+#pragma unroll
+        for (int e = 0; e < ND; ++e) S[r * DH + dim(e)] = o[i][e];
+    }
+    cluster_sync_all();
+    const uint32_t Ss = smem_u32(S);
+    for (int i = rank + split * tid; i < nr * W; i += split * C::THREADS) {
+        const int r = i / W, d = i % W * 4;
+        float mx = -INFINITY, sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < split; ++k) mx = fmaxf(mx, ld_cluster_f2(cluster_map(Ss + (ROWS * DH + 2 * r) * 4, k)).x);
+        for (int k = 0; k < split; ++k) {
+            const float2 ml = ld_cluster_f2(cluster_map(Ss + (ROWS * DH + 2 * r) * 4, k));
+            const float4 x = ld_cluster_f4(cluster_map(Ss + (r * DH + d) * 4, k));
+            const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mx);
+            sum = fmaf(ml.y, f, sum);
+            v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        *reinterpret_cast<float4 *>(place(r) + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    }
+    cluster_sync_all();                                                 // nobody leaves while its state is read
+}
+
+template <int DH, int ROWS>
+static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
+    using C = F32Cfg<DH, ROWS>;
+    auto kern = k_attn_f32<DH, ROWS>;
+    static bool sized[NFD_PAGED_DEVICES];                               // (once per device and kernel)
+    if (!sized[dev]) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return NFD_E_CUDA;
+        sized[dev] = true;
+    }
+    const long long tiles = ((long long)B.max_rows * A.share + ROWS - 1) / ROWS, units = kv_heads * tiles * B.n_seqs;
+    if (tiles > 65535) return NFD_E_RANGE;
+    const int blocks = (K.n_keys + F32_KEYS - 1) / F32_KEYS;
+    int split = 1;
+    while (split < 8 && units * split * 2 <= 2 * n_sm && blocks > split) split *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kv_heads * split, B.n_seqs, (unsigned)tiles), cfg.blockDim = dim3(C::THREADS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at, cfg.numAttrs = split > 1;
+    if (cudaLaunchKernelEx(&cfg, kern, B, A, K, split) != cudaSuccess) {
+        cudaGetLastError();
+        return NFD_E_CUDA;
+    }
+    return NFD_OK;
+}
+// 64 rows where that leaves no SM idle: twice the warps for the same tiles of keys
+template <int DH>
+static int launch_attn_f32(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
+    if ((((long long)B.max_rows * A.share + 63) / 64) * kv_heads * B.n_seqs >= n_sm) return launch_attn_f32_rows<DH, 64>(B, A, K, kv_heads, dev, n_sm, st);
+    return launch_attn_f32_rows<DH, 32>(B, A, K, kv_heads, dev, n_sm, st);
+}

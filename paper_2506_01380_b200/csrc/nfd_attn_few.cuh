@@ -16,7 +16,7 @@
 // (for O); 4-bit codes become bf16 numbers in registers: the code goes into the mantissa of 128 + n, 128 + z is
 // subtracted (exact), the step multiplied (exact: 4 by 4 bits).
 #pragma once
-#include "nfd_attn_any.cuh"
+#include "nfd_attn_rows.cuh"
 #include "nfd_sm100.cuh"
 
 #define FEW_WARPS 8
@@ -69,21 +69,33 @@ __device__ __forceinline__ uint32_t kv4_step2(uint32_t w0, uint32_t w1) { return
 template <int DH> struct FewKv4 {
     static constexpr bool KV4 = true;
     static constexpr int KC = 32;
-    static constexpr int NST = 4;
+    static constexpr int NST = 3;                           // (with 4, head dimension 128 leaves one CTA to an SM: 138 us for 101)
     static constexpr int RB = DH / 2;                       // bytes of a row of codes
     static constexpr int WB = DH == 128 ? 8 : 4;            // bytes of a key's words (DH 32: a word and its neighbour)
     static constexpr int PR = RB / 16;                      // 16-byte pieces of a row
     static constexpr int STAGE = 2 * KC * (RB + WB) + 16;
     Kv4Keys<DH> K;
-    long long place;                                        // of key `lane` of the chunk after the next one
+    // Key `lane` of the chunk that is looked up next: entry of the table, offset in the page; how far they move from chunk to chunk (additions
+    // instead of two divisions a chunk).
+    const int *table;
+    int pg, off, dq, dr;
+    long long place;                                        // of key `lane` of the chunk that is filled next
 
+    __device__ __forceinline__ void start(const BatchD &B, int s, int h, int first, int step) {
+        const int P = K.P.page_tokens, L = B.table_len, p = first + (threadIdx.x & 31);
+        table = B.table + (size_t)s * L;
+        off = p % P, pg = p / P % L, dr = step % P, dq = step / P % L;
+    }
     __device__ __forceinline__ void look_up(const BatchD &B, int s, int h, int base, int hi) {
-        const int p = base + (threadIdx.x & 31);
+        const int P = K.P.page_tokens, L = B.table_len;
         place = -1;
-        if (p < hi) {
-            const long long at = K.P.place(B, s, p);
-            if (at >= 0) place = at + (long long)h * K.P.page_tokens;
+        if (base + (int)(threadIdx.x & 31) < hi) {
+            const int page = __ldg(table + pg);
+            if ((unsigned)page < (unsigned)K.P.n_pages) place = ((long long)page * K.P.heads + h) * P + off;
         }
+        off += dr, pg += dq;
+        if (off >= P) off -= P, ++pg;
+        if (pg >= L) pg -= L;
     }
     // the copies of a chunk; its places have been looked up
     __device__ __forceinline__ void fill(uint8_t *stage, uint32_t st, const BatchD &B, int s, int h, int base, int hi) {
@@ -208,7 +220,8 @@ template <int DH> struct FewStates {
     static constexpr int RB = 2 * DH, PR = RB / 16;
     static constexpr int STAGE = 2 * KC * RB + 16;
     StateKeys<bf16, DH> K;
-    uint32_t there;                                         // of the chunk after the next one
+    uint32_t there;                                         // of the chunk that is filled next
+    __device__ __forceinline__ void start(const BatchD &, int, int, int, int) {}
     static __device__ __forceinline__ uint32_t at_k(int key, int piece) { return key * RB + (piece ^ (key & 7 & (PR - 1))) * 16; }
     static __device__ __forceinline__ uint32_t at_v(int key, int piece) { return KC * RB + key * RB + (piece ^ (2 * key & 7 & (PR - 1))) * 16; }
 
@@ -292,6 +305,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
     const int step = split * FEW_WARPS * KC;
     int next = lo + (rank * FEW_WARPS + warp) * KC;                               // next chunk to fill
     int base = next;
+    src.start(B, s, h, next, step);
     src.look_up(B, s, h, next, hi);
 #pragma unroll
     for (int i = 0; i < NST - 1; ++i) {
@@ -378,7 +392,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
                         }
                 }
         }
-        // the rows' maxima; what was summed before is rescaled only where one rose
+        // the rows' maxima; the reference m follows only where one rose by more than 8 (a factor of 256), and what was summed before with it
         float mn[NR][2];
         bool rise = false;
 #pragma unroll
@@ -390,14 +404,15 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
                 for (int u = 0; u < KT; ++u) v = fmaxf(v, fmaxf(x[u][t][e], x[u][t][2 + e]));
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-                mn[t][e] = v, rise |= v != m[t][e];
+                mn[t][e] = v, rise |= v * cs > m[t][e] * cs + 8.0f;
             }
         if (__any_sync(0xffffffffu, rise)) {
 #pragma unroll
             for (int t = 0; t < NR; ++t)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float f = mn[t][e] == m[t][e] ? 1.0f : few_exp2((m[t][e] - mn[t][e]) * cs);
+                    if (!(mn[t][e] * cs > m[t][e] * cs + 8.0f)) continue;
+                    const float f = few_exp2((m[t][e] - mn[t][e]) * cs);
                     m[t][e] = mn[t][e], l[t][e] *= f;
 #pragma unroll
                     for (int i = 0; i < NS; ++i) o[t][i][e] *= f, o[t][i][2 + e] *= f;
@@ -505,7 +520,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
 static int few_split(long long units, long long keys, int kc, int n_sm, int per_sm) {
     const long long chunks = (keys + kc - 1) / kc;
     int split = 1;
-    while (split < 8 && units * split * 2 <= (long long)n_sm * per_sm && chunks > (long long)split * FEW_WARPS) split *= 2;
+    while (split < 16 && units * split * 2 <= (long long)n_sm * per_sm && chunks > (long long)(split == 8 ? 48 : split) * FEW_WARPS) split *= 2;
     return split;
 }
 
@@ -517,6 +532,7 @@ static int launch_attn_few_nr(const BatchD &B, const AttnRows &A, const Src &src
     if (!per_sm[dev]) {
         int n = 0;
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
+            cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
             cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 32 * FEW_WARPS, F::SMEM) != cudaSuccess || n < 1)
             return NFD_E_CUDA;
         per_sm[dev] = n;

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include "nfd_append.cuh"
+#include "nfd_attn_f32.cuh"
 #include "nfd_attn_tile.cuh"
 
 #define CK(call)                                                                                   \
@@ -241,8 +242,9 @@ int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_
                 FewStates<DH> src;
                 src.K = K;
                 return launch_attn_few<FewStates<DH>, DH>(B, A, src, states->n_heads, states->n_keys, dev, n_sm, (cudaStream_t)cuda_stream);
+            } else {
+                return launch_attn_f32<DH>(B, A, K, states->n_heads, dev, n_sm, (cudaStream_t)cuda_stream);
             }
-            return launch_attn_any<TS, DH>(B, A, K, (cudaStream_t)cuda_stream);
         };
         return dtype == NFD_DTYPE_BF16 ? go((bf16 *)nullptr) : go((float *)nullptr);
     });
