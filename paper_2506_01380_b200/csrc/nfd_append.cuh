@@ -1,15 +1,15 @@
 // Rows into a paged cache, rotated and, where the pages hold 4 bits, quantised on the way; and back out of it.
 //
-// Bound by memory: every number of the new rows is read once and written once.  A CTA takes `rows` rows (one where that
-// leaves SMs idle otherwise) with all their heads, so that the angles of a row (64-bit arithmetic, head_dim / 2 sines and
-// cosines) are formed once for all of its heads, and each thread eight numbers of a head at a time: 16 bytes of bf16, four
-// pairs of the rotation, a word of 4-bit codes; four neighbouring lanes hold a group of 32.  The first loads are issued
-// before the row's sequence, its place and the angles are looked up.
+// Bound by memory: every number of the new rows is read once and written once; with 4-bit pages by instructions.  A CTA takes `rows` rows (one
+// where that leaves SMs idle otherwise) with all their heads, so that the angles of a row (64-bit arithmetic, head_dim / 2 sines and
+// cosines) are formed once for all of its heads.  A thread has a place in the rows, eight numbers of a head (16 bytes of bf16, four
+// pairs of the rotation, a word of 4-bit codes; four neighbouring lanes hold a group of 32), and takes it in one row after the other: what
+// depends on the place is worked out once.  The first loads are issued before the rows' sequences, places and angles are looked up.
 #pragma once
 #include "nfd_paged.cuh"
 
 #define APPEND_THREADS 256
-#define APPEND_MAX_ROWS 4
+#define APPEND_MAX_ROWS 8
 
 struct RopeD {
     int on, frame_tokens, grid_w;
@@ -51,147 +51,183 @@ template <> __device__ __forceinline__ void store8<bf16>(bf16 *p, const float *x
 }
 
 // The eight numbers of this lane to 4 bits, with the group's other three lanes: codes, and the group's word.
-__device__ __forceinline__ uint32_t kv4_pack(const float *x, uint32_t &word) {
-    float lo = 0.f, hi = 0.f;
-    bool bad = false;
+__device__ __forceinline__ uint32_t kv4_pack(const float *x, uint32_t &word, uint32_t group) {
+    float lo = 0.f, hi = 0.f, zero = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]), bad |= x[i] != x[i];
-    if (bad) hi = INFINITY;
+    for (int i = 0; i < 8; ++i) lo = fminf(lo, x[i]), hi = fmaxf(hi, x[i]), zero = fmaf(x[i], 0.f, zero);
+    if (zero != 0.f) hi = INFINITY;                            // NaN: one of them is not finite
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        lo = fminf(lo, __shfl_xor_sync(group, lo, o));
+        hi = fmaxf(hi, __shfl_xor_sync(group, hi, o));
     }
     if (!(hi - lo < INFINITY)) {
         word = 0x7FC0u;
         return 0;
     }
-    const float step = kv4_step(lo, hi), inv = __frcp_rn(step), z = kv4_round(-lo, step, inv);
-    word = (__float_as_uint(step) >> 16) | (uint32_t)(int)z;
+    const float step = kv4_step(lo, hi), inv = __frcp_rn(step);
+    const int z = __float_as_int(kv4_quotient(-lo, step, inv)) - __float_as_int(KV4_MAGIC), up = z - __float_as_int(KV4_MAGIC);
+    word = (__float_as_uint(step) >> 16) | (uint32_t)z;
     uint32_t codes = 0;
+    // (no code is below 0: x >= lo, and rounding is symmetric; the largest may be 16, where lo and hi are both rounded away from 0)
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        codes |= (uint32_t)(int)fminf(fmaxf(kv4_round(x[i], step, inv) + z, 0.f), 15.f) << kv4_shift(i);
+    for (int i = 0; i < 8; ++i) codes += (uint32_t)min(__float_as_int(kv4_quotient(x[i], step, inv)) + up, 15) << kv4_shift(i);
     return codes;
+}
+
+// The rows of a CTA, a warp to each: token (-1: none, or one that is dropped) and place in the pages (-1: none).
+__device__ __forceinline__ void rows_look_up(const BatchD &B, const PagesD &P, int r0, int nr, int *pos, long long *place) {
+    for (int r = threadIdx.x >> 5; r < nr; r += APPEND_THREADS / 32) {
+        const int s = B.seq_of(r0 + r);
+        int p = -1;
+        long long at = -1;
+        if (s < B.n_seqs) {
+            const int2 sr = B.rows(s);
+            const int i = r0 + r - sr.x, len = B.tokens(s);
+            if (i >= 0 && i < min(sr.y, B.max_rows)) p = max(len - sr.y + i, -1);
+            if (p >= 0 && p >= P.oldest(B, len)) at = P.place(B, s, p);
+        }
+        if ((threadIdx.x & 31) == 0) pos[r] = p, place[r] = at;
+    }
 }
 
 // TS: the rows' type; KV4: pages of 4 bits, otherwise of TS.
 template <typename TS, bool KV4, int DH>
 __global__ void __launch_bounds__(APPEND_THREADS) k_kv_append(const __grid_constant__ RopeD rope, const AppendIO io, const BatchD B,
                                                               const PagesD P, int rows) {
-    constexpr int CPH = DH / 8;                                // chunks of eight numbers of a head
-    constexpr int U = KV4 ? 2 : 4;                             // chunks of a thread in flight
+    constexpr int CPH = DH / 8, U = 4;                         // chunks of eight numbers of a head; rows in flight
     __shared__ float2 s_cs[APPEND_MAX_ROWS][DH / 2];
-    __shared__ long long s_place[APPEND_MAX_ROWS];             // -1: none
-    __shared__ int s_pos[APPEND_MAX_ROWS];                     // -1: dropped
-    const int tid = threadIdx.x, warp = tid >> 5;
-    const int r0 = blockIdx.x * rows, nr = min(rows, B.n_rows - r0);
-    const int qc = io.q_heads * CPH, kc = P.heads * CPH, per_row = qc + 2 * kc, total = nr * per_row;
-    float x[U][8];
-    auto load = [&](int c, float *v) {
-        const int r = c / per_row, j = c - r * per_row;
-        const TS *p = j < qc ? (const TS *)io.q + (r0 + r) * io.q_stride + j * 8
-                    : j < qc + kc ? (const TS *)io.k + (r0 + r) * io.k_stride + (j - qc) * 8
-                                  : (const TS *)io.v + (r0 + r) * io.v_stride + (j - qc - kc) * 8;
-        load8<TS>(p, v);
+    __shared__ long long s_place[APPEND_MAX_ROWS];
+    __shared__ int s_pos[APPEND_MAX_ROWS];
+    const int tid = threadIdx.x, r0 = blockIdx.x * rows, nr = min(rows, B.n_rows - r0);
+    const int qc = io.q_heads * CPH, kc = P.heads * CPH, per_row = qc + 2 * kc;
+    // a thread's place: chunk j of q, k and v side by side, and its numbers in row r0
+    struct Place {
+        const TS *src;
+        long long stride;
+        bool is_q, is_k;
     };
+    auto at = [&](int j) -> Place {
+        Place p;
+        p.is_q = j < qc, p.is_k = !p.is_q && j < qc + kc;
+        p.stride = p.is_q ? io.q_stride : p.is_k ? io.k_stride : io.v_stride;
+        p.src = (p.is_q ? (const TS *)io.q + j * 8 : p.is_k ? (const TS *)io.k + (j - qc) * 8 : (const TS *)io.v + (j - qc - kc) * 8) + r0 * p.stride;
+        return p;
+    };
+    float x[U][8];
+    auto load = [&](const Place &p, int r) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (u * APPEND_THREADS + tid < total) load(u * APPEND_THREADS + tid, x[u]);
-    if (warp < nr) {
-        const int row = r0 + warp, s = B.seq_of(row);
-        int pos = -1;
-        long long place = -1;
-        if (s < B.n_seqs) {
-            const int2 sr = B.rows(s);
-            const int i = row - sr.x, len = B.tokens(s), p = len - sr.y + i;
-            if (i >= 0 && i < min(sr.y, B.max_rows) && p >= 0) {
-                pos = p;
-                if (p >= P.oldest(B, len)) place = P.place(B, s, p);
-            }
-        }
-        if ((tid & 31) == 0) s_pos[warp] = pos, s_place[warp] = place;
-    }
+        for (int u = 0; u < U; ++u)
+            if (r + u < nr) load8<TS>(p.src + (r + u) * p.stride, x[u]);
+    };
+    int j = tid;
+    Place pl = at(j);
+    if (j < per_row) load(pl, 0);
+    rows_look_up(B, P, r0, nr, s_pos, s_place);
     __syncthreads();
     if (rope.on) {
         for (int i = tid; i < nr * (DH / 2); i += APPEND_THREADS) {
             const int r = i / (DH / 2), pair = i - r * (DH / 2), pos = max(s_pos[r], 0);
             const int f = pos / rope.frame_tokens, in = pos - f * rope.frame_tokens, gr = in / rope.grid_w;
-            const int at = pair < rope.half_t ? f : pair < rope.half_th ? gr : in - gr * rope.grid_w;
+            const int a = pair < rope.half_t ? f : pair < rope.half_th ? gr : in - gr * rope.grid_w;
             double sn, cs;
-            sincos((double)at * rope.freq[pair], &sn, &cs);
+            sincos((double)a * rope.freq[pair], &sn, &cs);
             s_cs[r][pair] = make_float2((float)cs, (float)sn);
         }
         __syncthreads();
     }
-    for (int c0 = 0; c0 < total; c0 += U * APPEND_THREADS) {
-        if (c0) {
+    for (; j < per_row; j += APPEND_THREADS) {                 // (a multiple of four: the lanes of a group agree)
+        if (j != tid) pl = at(j), load(pl, 0);
+        const bool turn = rope.on && (pl.is_q || pl.is_k);
+        const int jj = pl.is_q ? j : pl.is_k ? j - qc : j - qc - kc, h = jj / CPH, d = jj - h * CPH;
+        const long long head = (long long)h * P.page_tokens;
+        const uint32_t group = 0xFu << (tid & 28);             // the lanes that hold this group of 32
+        for (int rb = 0; rb < nr; rb += U) {
+            if (rb) load(pl, rb);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (c0 + u * APPEND_THREADS + tid < total) load(c0 + u * APPEND_THREADS + tid, x[u]);
-        }
+            for (int u = 0; u < U; ++u) {
+                const int r = rb + u;
+                if (r >= nr) break;                            // (the same for all threads)
+                if (s_pos[r] < 0) continue;                    // (and this)
+                if (turn) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c = c0 + u * APPEND_THREADS + tid;
-            if (c0 + u * APPEND_THREADS >= total) break;       // (the same for all threads)
-            const bool here = c < total;                       // (a multiple of four: the lanes of a group agree)
-            const int r = here ? c / per_row : 0, j = here ? c - r * per_row : 0;
-            const bool is_q = j < qc, is_k = !is_q && j < qc + kc;
-            if (rope.on && (is_q || is_k)) {
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float2 cs = s_cs[r][(j % CPH) * 4 + e / 2];
-                    const float a = x[u][e], b = x[u][e + 1];
-                    // (every rounding spelled out: a number next to a border of the 4-bit codes falls on the same side in
-                    // every instance of the kernel)
-                    x[u][e] = __fsub_rn(__fmul_rn(a, cs.x), __fmul_rn(b, cs.y));
-                    x[u][e + 1] = __fadd_rn(__fmul_rn(b, cs.x), __fmul_rn(a, cs.y));
+                    for (int e = 0; e < 8; e += 4) {
+                        const float4 cs = *reinterpret_cast<const float4 *>(&s_cs[r][d * 4 + e / 2]);
+                        const float a0 = x[u][e], a1 = x[u][e + 1], b0 = x[u][e + 2], b1 = x[u][e + 3];
+                        // (every rounding spelled out: a number next to a border of the 4-bit codes falls on the same side in
+                        // every instance of the kernel)
+                        x[u][e] = __fsub_rn(__fmul_rn(a0, cs.x), __fmul_rn(a1, cs.y));
+                        x[u][e + 1] = __fadd_rn(__fmul_rn(a1, cs.x), __fmul_rn(a0, cs.y));
+                        x[u][e + 2] = __fsub_rn(__fmul_rn(b0, cs.z), __fmul_rn(b1, cs.w));
+                        x[u][e + 3] = __fadd_rn(__fmul_rn(b1, cs.z), __fmul_rn(b0, cs.w));
+                    }
                 }
-            }
-            uint32_t word = 0, codes = 0;
-            if (KV4) codes = kv4_pack(x[u], word);
-            if (!here || s_pos[r] < 0) continue;
-            if (is_q) {
-                store8<TS>((TS *)io.q_out + ((long long)(r0 + r) * qc + j) * 8, x[u]);
-                continue;
-            }
-            if (s_place[r] < 0) continue;
-            const int jj = is_k ? j - qc : j - qc - kc, h = jj / CPH, d = jj - h * CPH;
-            const size_t at = (size_t)(s_place[r] + (long long)h * P.page_tokens);
-            if (KV4) {
-                reinterpret_cast<uint32_t *>(is_k ? P.k : P.v)[at * CPH + d] = codes;
-                if (!(d & 3)) (is_k ? P.k_scale : P.v_scale)[at * (DH / 32) + d / 4] = (uint16_t)word;
-            } else {
-                store8<TS>((TS *)(is_k ? P.k : P.v) + at * DH + d * 8, x[u]);
+                if (pl.is_q) {
+                    store8<TS>((TS *)io.q_out + ((long long)(r0 + r) * qc + j) * 8, x[u]);
+                    continue;
+                }
+                if (s_place[r] < 0) continue;
+                const size_t to = (size_t)(s_place[r] + head);
+                if (KV4) {
+                    uint32_t word;
+                    const uint32_t codes = kv4_pack(x[u], word, group);
+                    reinterpret_cast<uint32_t *>(pl.is_k ? P.k : P.v)[to * CPH + d] = codes;
+                    if (!(d & 3)) (pl.is_k ? P.k_scale : P.v_scale)[to * (DH / 32) + d / 4] = (uint16_t)word;
+                } else {
+                    store8<TS>((TS *)(pl.is_k ? P.k : P.v) + to * DH + d * 8, x[u]);
+                }
             }
         }
     }
 }
 
-// TP: type of the pages (KV4: 4 bits), TO: of the result.
+// TP: type of the pages (KV4: 4 bits), TO: of the result.  Rows and threads as above.
 template <typename TP, typename TO, bool KV4, int DH>
-__global__ void __launch_bounds__(256) k_pages_read(const BatchD B, const PagesD P, TO *k_out, TO *v_out) {
-    constexpr int CPH = DH / 8;
-    const int row = blockIdx.x, s = B.seq_of(row);
-    if (s >= B.n_seqs) return;
-    const int2 sr = B.rows(s);
-    const int i = row - sr.x, len = B.tokens(s), p = len - sr.y + i;
-    if (i < 0 || i >= min(sr.y, B.max_rows) || p < P.oldest(B, len)) return;
-    const long long place = P.place(B, s, p);
-    if (place < 0) return;
-    const int per = P.heads * CPH;
-    for (int c = threadIdx.x; c < 2 * per; c += blockDim.x) {
+__global__ void __launch_bounds__(APPEND_THREADS) k_pages_read(const BatchD B, const PagesD P, TO *k_out, TO *v_out, int rows) {
+    constexpr int CPH = DH / 8, U = 4;
+    __shared__ long long s_place[APPEND_MAX_ROWS];
+    __shared__ int s_pos[APPEND_MAX_ROWS];
+    const int r0 = blockIdx.x * rows, nr = min(rows, B.n_rows - r0), per = P.heads * CPH;
+    rows_look_up(B, P, r0, nr, s_pos, s_place);
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * per; c += APPEND_THREADS) {
         const bool is_k = c < per;
         TO *out = is_k ? k_out : v_out;
         if (!out) continue;
         const int j = is_k ? c : c - per, h = j / CPH, d = j - h * CPH;
-        const size_t at = (size_t)(place + (long long)h * P.page_tokens);
-        float x[8];
-        if (KV4)
-            kv4_unpack(reinterpret_cast<const uint32_t *>(is_k ? P.k : P.v)[at * CPH + d],
-                       (is_k ? P.k_scale : P.v_scale)[at * (DH / 32) + d / 4], x);
-        else
-            load8<TP>((const TP *)(is_k ? P.k : P.v) + at * DH + d * 8, x);
-        store8<TO>(out + ((size_t)row * per + j) * 8, x);
+        const long long head = (long long)h * P.page_tokens;
+        const void *src = is_k ? P.k : P.v;
+        const uint16_t *words = is_k ? P.k_scale : P.v_scale;
+        out += (size_t)r0 * per * 8 + j * 8;
+        for (int rb = 0; rb < nr; rb += U) {
+            uint32_t codes[U], word[U];
+            float x[U][8];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (rb + u >= nr || s_place[rb + u] < 0) continue;
+                const size_t at = (size_t)(s_place[rb + u] + head);
+                if (KV4) codes[u] = reinterpret_cast<const uint32_t *>(src)[at * CPH + d], word[u] = words[at * (DH / 32) + d / 4];
+                else load8<TP>((const TP *)src + at * DH + d * 8, x[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (rb + u >= nr || s_place[rb + u] < 0) continue;
+                TO *to = out + (size_t)(rb + u) * per * 8;
+                if constexpr (KV4) {
+                    uint32_t b[4];                             // bf16 numbers, exactly
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) b[i] = kv4_pair(codes[u], i, kv4_z2(word[u], word[u]), kv4_step2(word[u], word[u]));
+                    if constexpr (sizeof(TO) == 2) {
+                        *reinterpret_cast<uint4 *>(to) = make_uint4(b[0], b[1], b[2], b[3]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[u][2 * i] = __uint_as_float(b[i] << 16), x[u][2 * i + 1] = __uint_as_float(b[i] & 0xffff0000u);
+                        store8<TO>(to, x[u]);
+                    }
+                } else {
+                    store8<TO>(to, x[u]);
+                }
+            }
+        }
     }
 }

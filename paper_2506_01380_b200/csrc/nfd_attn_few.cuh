@@ -55,16 +55,6 @@ __device__ __forceinline__ float few_exp2(float x) {
     return y;
 }
 
-// pair i of a word of codes as bf16 numbers: z2 = two bf16 numbers 128 + z, step2 = the step twice
-__device__ __forceinline__ uint32_t kv4_pair(uint32_t codes, int i, uint32_t z2, uint32_t step2) {
-    const uint32_t t = (codes >> (4 * i) & 0x000F000Fu) | 0x43004300u;
-    __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162 *>(&t);
-    a = __hmul2(__hsub2(a, *reinterpret_cast<const __nv_bfloat162 *>(&z2)), *reinterpret_cast<const __nv_bfloat162 *>(&step2));
-    return *reinterpret_cast<const uint32_t *>(&a);
-}
-__device__ __forceinline__ uint32_t kv4_z2(uint32_t w0, uint32_t w1) { return (w0 & 15u) | (w1 & 15u) << 16 | 0x43004300u; }
-__device__ __forceinline__ uint32_t kv4_step2(uint32_t w0, uint32_t w1) { return (w0 & 0xFFF0u) | (w1 & 0xFFF0u) << 16; }
-
 // A warp's chunk of keys in shared memory, for 4-bit pages: codes of K and V, their words, and which keys are there.
 template <int DH> struct FewKv4 {
     static constexpr bool KV4 = true;

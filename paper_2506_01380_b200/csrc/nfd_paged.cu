@@ -84,6 +84,13 @@ int this_device(int &dev, int &n_sm) {
     return NFD_OK;
 }
 
+// rows of a CTA: several where every SM has a few CTAs all the same
+int append_rows(int n_rows, int n_sm) {
+    int rows = 1;
+    while (rows < APPEND_MAX_ROWS && n_rows >= 4 * rows * n_sm) rows *= 2;
+    return rows;
+}
+
 }  // namespace
 
 extern "C" {
@@ -132,7 +139,7 @@ int nfd_kv_append(const nfd_pages *pages, const nfd_batch *batch, const nfd_rope
     int dev = 0, n_sm = 0;
     RET(this_device(dev, n_sm));
     const AppendIO io = {q, k, v, q_stride, k_stride, v_stride, q_out, n_q_heads};
-    const int rows = B.n_rows >= 2 * APPEND_MAX_ROWS * n_sm ? APPEND_MAX_ROWS : 1;
+    const int rows = append_rows(B.n_rows, n_sm);
     const unsigned grid = (unsigned)((B.n_rows + rows - 1) / rows);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     by_head_dim(dh, [&](auto d) {
@@ -160,17 +167,20 @@ int nfd_pages_read(const nfd_pages *pages, const nfd_batch *batch, int dtype, vo
     if (pages->dtype != dtype && pages->dtype != NFD_DTYPE_KV4) return NFD_E_BADCFG;
     if (!aligned(k_out, 16) || !aligned(v_out, 16)) return NFD_E_ALIGN;
     if (B.n_rows == 0 || B.max_rows == 0 || (!k_out && !v_out)) return NFD_OK;
+    int dev = 0, n_sm = 0;
+    RET(this_device(dev, n_sm));
+    const int rows = append_rows(B.n_rows, n_sm);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     by_head_dim(pages->head_dim, [&](auto d) {
         constexpr int DH = decltype(d)::value;
-        const unsigned grid = (unsigned)B.n_rows;
+        const unsigned grid = (unsigned)((B.n_rows + rows - 1) / rows);
         if (pages->dtype == NFD_DTYPE_KV4) {
-            if (dtype == NFD_DTYPE_BF16) k_pages_read<bf16, bf16, true, DH><<<grid, 256, 0, st>>>(B, P, (bf16 *)k_out, (bf16 *)v_out);
-            else k_pages_read<bf16, float, true, DH><<<grid, 256, 0, st>>>(B, P, (float *)k_out, (float *)v_out);
+            if (dtype == NFD_DTYPE_BF16) k_pages_read<bf16, bf16, true, DH><<<grid, APPEND_THREADS, 0, st>>>(B, P, (bf16 *)k_out, (bf16 *)v_out, rows);
+            else k_pages_read<bf16, float, true, DH><<<grid, APPEND_THREADS, 0, st>>>(B, P, (float *)k_out, (float *)v_out, rows);
         } else if (dtype == NFD_DTYPE_BF16) {
-            k_pages_read<bf16, bf16, false, DH><<<grid, 256, 0, st>>>(B, P, (bf16 *)k_out, (bf16 *)v_out);
+            k_pages_read<bf16, bf16, false, DH><<<grid, APPEND_THREADS, 0, st>>>(B, P, (bf16 *)k_out, (bf16 *)v_out, rows);
         } else {
-            k_pages_read<float, float, false, DH><<<grid, 256, 0, st>>>(B, P, (float *)k_out, (float *)v_out);
+            k_pages_read<float, float, false, DH><<<grid, APPEND_THREADS, 0, st>>>(B, P, (float *)k_out, (float *)v_out, rows);
         }
         return 0;
     });

@@ -59,26 +59,25 @@ __device__ __forceinline__ float kv4_step(float lo, float hi) {
     if (__uint_as_float(down) >= 7.8886090522101181e-31f && 15.0f * __uint_as_float(down) >= r) b = down;
     return __uint_as_float(b);
 }
-// x / step to the nearest whole number, ties to even: the product with the reciprocal is off by ulps, the remainder of
-// its rounding is exact in fp32 (whole number of 5 bits x 4 bits, next to x) and corrects it.
-__device__ __forceinline__ float kv4_round(float x, float step, float inv) {
-    float r = rintf(x * inv);
-    const float e = fmaf(-r, step, x), h = 0.5f * step;
-    const bool odd = (int)r & 1;
-    if (e > h || (e == h && odd)) r += 1.0f;
-    else if (e < -h || (e == -h && odd)) r -= 1.0f;
-    return r;
+// x / step to the nearest whole number, ties to even, in the low bits of the result's significand (less KV4_MAGIC's bits).  The quotient is
+// corrected by its exact remainder, which makes it the rounded quotient; step having 4 significant bits, a quotient that is not half way
+// between whole numbers is not rounded to one that is (it is off by more than half an ulp), so that rounding once more loses nothing.
+#define KV4_MAGIC 12582912.0f                              // 1.5 x 2^23: an ulp is 1
+__device__ __forceinline__ float kv4_quotient(float x, float step, float inv) {
+    const float q = x * inv;
+    return fmaf(fmaf(-q, step, x), inv, q) + KV4_MAGIC;
 }
 // bits of code i of a word of eight
 __device__ __forceinline__ constexpr int kv4_shift(int i) { return 4 * (i >> 1) + 16 * (i & 1); }
-__device__ __forceinline__ float kv4_word_step(uint32_t w) { return __uint_as_float((w & 0xFFF0u) << 16); }
-// the eight numbers of a word of codes, exact
-__device__ __forceinline__ void kv4_unpack(uint32_t codes, uint32_t word, float *x) {
-    const float step = kv4_word_step(word);
-    const int z = word & 15;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (float)((int)(codes >> kv4_shift(i) & 15) - z) * step;
+// pair i of a word of codes as bf16 numbers: z2 = two bf16 numbers 128 + z, step2 = the step twice
+__device__ __forceinline__ uint32_t kv4_pair(uint32_t codes, int i, uint32_t z2, uint32_t step2) {
+    const uint32_t t = (codes >> (4 * i) & 0x000F000Fu) | 0x43004300u;
+    __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162 *>(&t);
+    a = __hmul2(__hsub2(a, *reinterpret_cast<const __nv_bfloat162 *>(&z2)), *reinterpret_cast<const __nv_bfloat162 *>(&step2));
+    return *reinterpret_cast<const uint32_t *>(&a);
 }
+__device__ __forceinline__ uint32_t kv4_z2(uint32_t w0, uint32_t w1) { return (w0 & 15u) | (w1 & 15u) << 16 | 0x43004300u; }
+__device__ __forceinline__ uint32_t kv4_step2(uint32_t w0, uint32_t w1) { return (w0 & 0xFFF0u) | (w1 & 0xFFF0u) << 16; }
 
 // ---- which keys a row sees ----------------------------------------------------------------------------------
 struct KeyRange {
