@@ -93,7 +93,7 @@ __device__ __forceinline__ void rows_look_up(const BatchD &B, const PagesD &P, i
 
 // TS: the rows' type; KV4: pages of 4 bits, otherwise of TS.
 template <typename TS, bool KV4, int DH>
-__global__ void __launch_bounds__(APPEND_THREADS) k_kv_append(const __grid_constant__ RopeD rope, const AppendIO io, const BatchD B,
+__global__ void __launch_bounds__(APPEND_THREADS, KV4 ? 4 : 1) k_kv_append(const __grid_constant__ RopeD rope, const AppendIO io, const BatchD B,
                                                               const PagesD P, int rows) {
     constexpr int CPH = DH / 8, U = 4;                         // chunks of eight numbers of a head; rows in flight
     __shared__ float2 s_cs[APPEND_MAX_ROWS][DH / 2];
