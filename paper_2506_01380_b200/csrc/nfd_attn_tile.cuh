@@ -9,10 +9,9 @@
 //     P = exp2(S c - m)   one thread per row: S by columns to registers, exponentials, P as bf16 over the S it came from
 //     O += P V      UMMA 128 x 64 x KB, P from tensor memory, V as it lies (MN-major)
 // m is the row's maximum over the group's first block, and no maximum is taken of later blocks: a probability is exact to the
-// same number of bits whatever its size.  Where a block's sum of a row passes 2^60 after all (or is NaN), the warp takes the block
-// again, S being untouched so far: maxima first, and where one has risen by more than 8 (a factor of 256) it becomes m and
-// the row's O is rescaled in tensor memory by its thread.  First blocks and blocks with keys that some row of the warp does not see
-// go the same way.
+// same number of bits whatever its size.  Where a block's sum of a row passes 2^60 after all (or is NaN), or a row has no m yet, the warp
+// takes the block again, S being untouched so far: maxima first, and where one has risen by more than 8 (a factor of 256) it becomes m and
+// the row's O is rescaled in tensor memory by its thread.
 //
 // Warps 0 .. PW-1 fill the rings of K and V blocks: bf16 states with cp.async, several blocks in flight; 4-bit pages through
 // registers, two blocks ahead, the codes becoming bf16 numbers on the way.  Warp PW issues the products, the last 4 NG are the
@@ -335,22 +334,24 @@ template <int DH> struct TileKv4 {
     }
 };
 
-// S of a block that some row of the warp does not see in whole, or whose sums have outgrown m, or the group's first: the
+// S of a group's first block, or of one whose sums have outgrown m, or that finds a row without m: the
 // row's maximum over the keys that it sees, m and what has been summed so far adjusted to it, then P.
 // seen: bits of the keys that the row sees; n: the group's jobs before this one.
 template <int DH>
-static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, uint32_t seen0, uint32_t seen1, uint32_t seen2, float c, int n,
+static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, const uint32_t *seen, float c, int n,
                                               uint32_t pv_done, float &m_io, float &l_io, bool &ok) {
     using C = TileCfg<DH>;
+    constexpr int KB = C::KB;
     float m = m_io, l = l_io, top = -INFINITY;
-    auto seen = [&](int i) { return (i < 32 ? seen0 : i < 64 ? seen1 : seen2) >> (i & 31); };
+    // (by columns, in loops: a whole row in registers is no faster, and its registers are missing elsewhere)
+    auto bits = [&](int i) { return (i < 32 ? seen[0] : i < 64 ? seen[1] : seen[2]) >> (i & 31); };
 #pragma unroll 1
-    for (int i = 0; i < C::KB; i += 16) {
+    for (int i = 0; i < KB; i += 16) {
         float x[16];
         tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
+        const uint32_t s = bits(i);
         tmem_ld_wait();
         loaded16(x);
-        const uint32_t s = seen(i);
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s >> e & 1 ? x[e] : -INFINITY);
     }
@@ -379,12 +380,12 @@ static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, uint3
     const float mc = m == -INFINITY ? 0.f : m * c;
     float sum = 0.f;
 #pragma unroll 1
-    for (int i = 0; i < C::KB; i += 16) {
+    for (int i = 0; i < KB; i += 16) {
         float x[16];
         tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
+        const uint32_t s = bits(i);
         tmem_ld_wait();
         loaded16(x);
-        const uint32_t s = seen(i);
         uint32_t pk[8];
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
@@ -394,6 +395,42 @@ static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, uint3
         tmem_st8(tS + i / 2, pk);                                      // (behind what is still to be read)
     }
     m_io = m, l_io = l + sum;
+}
+// One pass over S against the m that there is, 16 columns at a time with the next load in flight (xa: the first ones).  MASKED: keys that the
+// row does not see count for nothing.  False: a sum has outgrown m, and S is as it was.
+template <int DH, bool MASKED>
+static __device__ __forceinline__ bool tile_fast(uint32_t tS, float *xa, const uint32_t *seen, float c, float m, float &l) {
+    constexpr int KB = TileCfg<DH>::KB;
+    const float mc = m == -INFINITY ? 0.f : m * c;
+    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    float xb[16];
+    uint32_t pk[KB / 2];
+#pragma unroll
+    for (int i = 0; i < KB; i += 16) {
+        float *x = i & 16 ? xb : xa, *y = i & 16 ? xa : xb;
+        tmem_ld_wait();
+        loaded16(x);
+        if (i + 16 < KB) tmem_ld16(tS + i + 16, reinterpret_cast<uint32_t *>(y));
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            float2 s = make_float2(x[2 * u], x[2 * u + 1]);
+            if (MASKED) {
+                const uint32_t bits = seen[i >> 5] >> (i & 31);
+                s.x = bits >> (2 * u) & 1 ? s.x : -INFINITY, s.y = bits >> (2 * u + 1) & 1 ? s.y : -INFINITY;
+            }
+            const float2 e = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
+            const float2 p = make_float2(few_exp2(e.x), few_exp2(e.y));
+            ls[u & 1] = fadd2(ls[u & 1], p);
+            pk[i / 2 + u] = bf16_pair(p.x, p.y);
+        }
+    }
+    const float2 l2 = fadd2(ls[0], ls[1]);
+    const float sum = l2.x + l2.y;
+    if (!__all_sync(0xffffffffu, sum < 1.152921504606847e18f)) return false;
+    l += sum;
+#pragma unroll
+    for (int i = 0; i < KB / 2; i += 8) tmem_st8(tS + i, pk + i);
+    return true;
 }
 
 // D (+)= A B^T with descriptors whose upper halves are constants
@@ -564,54 +601,33 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
             __syncwarp();
             tc_fence_after();
             if (some) {                                                // (of rows that are not there P may be anything)
-                float xa[16], xb[16];
+                float xa[16];
                 tmem_ld16(tS, reinterpret_cast<uint32_t *>(xa));       // (of use where the fast path is taken)
                 const uint4 mask = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + b % C::NM * 32);
                 const uint4 bad = *reinterpret_cast<const uint4 *>(smem + C::AT_MASK + b % C::NM * 32 + 16);
                 const int p0 = w.lo + b * KB;
-                bool fast = (mask.x & mask.y) == 0xffffffffu && (mask.z & C::M2) == C::M2 && !(bad.x | bad.y | (C::M2 ? bad.z : 0u)) && p0 >= kr.lo &&
-                            p0 + KB <= kr.hi && m != -INFINITY;
-                fast = __all_sync(0xffffffffu, fast);
-                if (fast) {
-                    // one pass over S, 16 columns at a time with the next load in flight
-                    const float mc = m * c;
-                    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    uint32_t pk[KB / 2];
-#pragma unroll
-                    for (int i = 0; i < KB; i += 16) {
-                        float *x = i & 16 ? xb : xa, *y = i & 16 ? xa : xb;
-                        tmem_ld_wait();
-                        loaded16(x);
-                        if (i + 16 < KB) tmem_ld16(tS + i + 16, reinterpret_cast<uint32_t *>(y));
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            const float2 e = ffma2(make_float2(x[2 * u], x[2 * u + 1]), make_float2(c, c), make_float2(-mc, -mc));
-                            const float2 p = make_float2(few_exp2(e.x), few_exp2(e.y));
-                            ls[u & 1] = fadd2(ls[u & 1], p);
-                            pk[i / 2 + u] = bf16_pair(p.x, p.y);
-                        }
-                    }
-                    const float2 l2 = fadd2(ls[0], ls[1]);
-                    const float sum = l2.x + l2.y;
-                    fast = __all_sync(0xffffffffu, sum < 1.152921504606847e18f);
-                    if (fast) {
-                        l += sum;
-#pragma unroll
-                        for (int i = 0; i < KB / 2; i += 8) tmem_st8(tS + i, pk + i);
-                    }
-                }
-                if (!fast) {
-                    tmem_ld_wait();
+                const bool whole = (mask.x & mask.y) == 0xffffffffu && (mask.z & C::M2) == C::M2 && !(bad.x | bad.y | (C::M2 ? bad.z : 0u)) &&
+                                   p0 >= kr.lo && p0 + KB <= kr.hi;
+                uint32_t seen[3] = {0xffffffffu, 0xffffffffu, 0xffffffffu};
+                bool done = false;
+                if (__all_sync(0xffffffffu, whole)) {
+                    if (__all_sync(0xffffffffu, m != -INFINITY)) done = tile_fast<DH, false>(tS, xa, seen, c, m, l);
+                } else {
                     const uint32_t there[3] = {mask.x, mask.y, mask.z}, bads[3] = {bad.x, bad.y, bad.z};
                     const int a = kr.lo - p0, e = kr.hi - p0;          // keys a .. e - 1 of the block
-                    uint32_t seen[3] = {0, 0, 0};
+                    uint32_t any = 0;
 #pragma unroll
                     for (int k = 0; k < (KB + 31) / 32; ++k) {
                         const int a1 = min(max(a - 32 * k, 0), 32), e1 = min(max(e - 32 * k, 0), 32);
                         seen[k] = (e1 == 32 ? 0xffffffffu : (1u << e1) - 1) & ~(a1 == 32 ? 0xffffffffu : (1u << a1) - 1) & there[k];
+                        any |= seen[k];
                         if (seen[k] & bads[k]) l = NAN;                // the row sees a value that is not finite
                     }
-                    tile_slow<DH>(tS, tO, seen[0], seen[1], seen[2], c, n, bars.pv_done(g, n - 1), m, l, ok);
+                    if (__all_sync(0xffffffffu, m != -INFINITY || !any)) done = tile_fast<DH, true>(tS, xa, seen, c, m, l);
+                }
+                if (!done) {
+                    tmem_ld_wait();
+                    tile_slow<DH>(tS, tO, seen, c, n, bars.pv_done(g, n - 1), m, l, ok);
                 }
                 tmem_st_wait();
             }
