@@ -8,7 +8,7 @@
 //     S = Q K^T     UMMA 128 x KB x DH, operands in shared memory, accumulator in tensor memory
 //     P = exp2(S c - m)   one thread per row: S by columns to registers, exponentials, P as bf16 over the S it came from
 //     O += P V      UMMA 128 x 64 x KB, P from tensor memory, V as it lies (MN-major)
-// m is the row's maximum over the group's first block, and no maximum is taken of later blocks: a probability is exact to the
+// m is the largest of the first 16 scores of the group's first block, and no other maximum is taken: a probability is exact to the
 // same number of bits whatever its size.  Where a block's sum of a row passes 2^60 after all (or is NaN), or a row has no m yet, the warp
 // takes the block again, S being untouched so far: maxima first, and where one has risen by more than 8 (a factor of 256) it becomes m and
 // the row's O is rescaled in tensor memory by its thread.
@@ -23,6 +23,7 @@
 #include "nfd_attn_few.cuh"
 
 #define TILE_THREADS 512
+#define TILE_SPLIT 8                // most CTAs of a cluster
 
 // (no status word: there is no context whose latch could be read)
 __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity) {
@@ -81,7 +82,7 @@ template <int DH> struct TileCfg {
     static constexpr uint32_t M1 = 0xffffffffu, M2 = KB >= 96 ? 0xffffffffu : KB > 64 ? (1u << (KB - 64)) - 1 : 0;      // bits of keys 32 .., 64 ..
     // a group's state, over queries and rings: O as [DH / 4][128] float4, then [128] (m, l)
     static constexpr int STATE = 128 * DH * 4 + 128 * 8;
-    static_assert(TM_O + NG * 64 * SUB <= 512 && NG * STATE <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
+    static_assert(TM_O + NG * 64 * SUB <= 512 && NG * STATE + 128 * 8 <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
     static_assert(NST + NB <= NM, "masks");
     static_assert(NST <= 6 && NB == 4 && NM == 16, "TileBars");
     static_assert(PW * 32 >= KB * SUB && KB >= 64 && KB <= 96 && KB % 16 == 0, "a thread for 64 dims of a key; three words of bits");
@@ -157,27 +158,33 @@ template <int DH> struct TileStates {
         const bf16 *from[2] = {K.k + first, K.v + first};
         const long long step = RS * K.key_stride, on = C::KB * K.key_stride;
         const unsigned char *mask = K.mask ? K.mask + (size_t)w.s * K.n_keys : nullptr;
-        // bits of this thread's rows of a block, and (the last one) of key t of it
-        auto there = [&](int b) -> uint32_t {
-            uint32_t m = 0;
+        // What the mask says of this thread's rows of a block, and of key t of it (loaded a block ahead); the bits of these that are there.
+        uint32_t raw[N + 1];
+        auto look = [&](int b) {
             const int p0 = w.lo + b * C::KB;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int p = p0 + row0 + i * RS;
-                m |= (uint32_t)(p < w.hi && row0 + i * RS < C::KB && (!mask || mask[p])) << i;
+            for (int i = 0; i <= N; ++i) {
+                const int row = i < N ? row0 + i * RS : t, p = p0 + row;
+                raw[i] = p < w.hi && row < C::KB;
+                if (mask && raw[i]) raw[i] = mask[p];
             }
-            const int p = p0 + t;
-            return m | (uint32_t)(t < C::KB && p < w.hi && (!mask || mask[p])) << 31;
+        };
+        auto there = [&]() -> uint32_t {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i <= N; ++i) m |= (uint32_t)(raw[i] != 0) << (i < N ? i : 31);
+            return m;
         };
         int done = 0, item = 0;                                       // published, begun
         auto publish = [&]() {
             const int st = (done >> 1) % C::NST;
             tile_publish(done & 1 ? bars.v_full(st) : bars.k_full(st)), ++done;
         };
-        uint32_t bits = there(0);
+        look(0);
         for (int b = 0; b < w.nb && ok; ++b) {
             const int st = b % C::NST, par = (b / C::NST - 1) & 1;
-            const uint32_t next = b + 1 < w.nb ? there(b + 1) : 0;
+            const uint32_t bits = there();
+            look(b + 1);
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 const uint32_t empty = kv ? bars.v_empty(st) : bars.k_empty(st);
@@ -207,12 +214,12 @@ template <int DH> struct TileStates {
                     uint32_t *M = reinterpret_cast<uint32_t *>(smem + C::AT_MASK) + b % C::NM * 8 + (t >> 5);
                     if (lane == 0) M[0] = m, M[4] = 0, mbar_arrive(bars.m_full(b % C::NM));
                 }
-                if (++item - done > FLY) {
-                    cp_async_wait<FLY>();
+                // (the first block is wanted at once)
+                if (++item - done > (item < 2 * FLY ? 2 : FLY)) {
+                    cp_async_wait_upto(item - done - 1);
                     publish();
                 }
             }
-            bits = next;
         }
         while (ok && done < item) {
             cp_async_wait_upto(item - done - 1);
@@ -334,7 +341,7 @@ template <int DH> struct TileKv4 {
     }
 };
 
-// S of a group's first block, or of one whose sums have outgrown m, or that finds a row without m: the
+// S of a block whose sums have outgrown m, or that finds a row without one: the
 // row's maximum over the keys that it sees, m and what has been summed so far adjusted to it, then P.
 // seen: bits of the keys that the row sees; n: the group's jobs before this one.
 template <int DH>
@@ -523,13 +530,22 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % split, s = blockIdx.y, r0 = blockIdx.z * tiles * 128;
     const int2 sr = B.rows(s);
+    const TileBars bars = {smem_u32(smem + C::AT_BAR)};
+    if (threadIdx.x == 0) bars.init(C::PW, 4 * NG), s_expired = 0;
+    if (DH == 32) {
+        // V's columns 32 .. 63 belong to nothing, and are zeros
+        for (int i = threadIdx.x; i < C::NST * KB * 4; i += TILE_THREADS)
+            *reinterpret_cast<uint4 *>(smem + C::AT_V + (i / (KB * 4)) * C::BLK + tile_at(i / 4 % KB, 4 + i % 4)) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+    }
     const int rows = min(sr.y, B.max_rows) * A.share;
     if (r0 >= rows) return;                                 // (the whole cluster)
+    __syncthreads();
     const int nr = min(tiles * 128, rows - r0);
-    TileWork w;
-    w.s = s, w.h = blockIdx.x / split;
     // Job j: block j / T, tile and group j % T; with one tile block j, group j % NG.
     const int T = (nr + 127) / 128, G = T == 1 ? NG : T;
+    TileWork w;
+    w.s = s, w.h = blockIdx.x / split;
     if (warp >= C::SM0) {
         // softmax warps: the row's queries, into the operand of its tile; with one tile, the groups share them out
         constexpr int CPR = DH / 8;
@@ -549,23 +565,19 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         w.hi = min(last.hi, w.lo + w.nb * KB);
     }
     const int jobs = w.nb * T;
-    const TileBars bars = {smem_u32(smem + C::AT_BAR)};
-    if (threadIdx.x == 0) bars.init(C::PW, 4 * G), s_expired = 0;
-    if (warp == C::PW) {
-        tmem_alloc(smem_u32(&s_tmem), 512);
-        tmem_relinquish();
-    }
-    if (DH == 32) {
-        // V's columns 32 .. 63 belong to nothing, and are zeros
-        for (int i = threadIdx.x; i < C::NST * KB * 4; i += TILE_THREADS)
-            *reinterpret_cast<uint4 *>(smem + C::AT_V + (i / (KB * 4)) * C::BLK + tile_at(i / 4 % KB, 4 + i % 4)) = make_uint4(0, 0, 0, 0);
-        fence_proxy_async_smem();
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = s_tmem;
     const bool merge = split > 1 || (T == 1 && jobs >= 2);  // a row's result is in several groups
+    uint32_t tmem = 0;
+    if (warp >= C::PW) {
+        // (the producers are on their way; the others wait for tensor memory)
+        if (warp == C::PW) {
+            tmem_alloc(smem_u32(&s_tmem), 512);
+            tmem_relinquish();
+        }
+        tc_fence_before();
+        asm volatile("bar.sync 2, %0;" ::"n"(TILE_THREADS - 32 * C::PW) : "memory");
+        tc_fence_after();
+        tmem = s_tmem;
+    }
     bool ok = true;
 
     if (warp < C::SM0) {
@@ -588,10 +600,8 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
         const float c = 1.4426950408889634f * rsqrtf((float)DH);
         const KeyRange kr = src.K.range(B, s, sr.y, (r0 + min(r, nr - 1)) / A.share);
-        if (g < G && jobs) {
-            cp_async_wait<0>();
-            tile_publish(bars.q_full());
-        }
+        cp_async_wait<0>();
+        tile_publish(bars.q_full());
         float m = -INFINITY, l = 0.f;                                  // m: reference, in units of scores
         int n = 0;                                                     // the group's jobs so far
         for (int j = g; g < G && j < jobs; j += G, ++n) {
@@ -608,14 +618,12 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                 const int p0 = w.lo + b * KB;
                 const bool whole = (mask.x & mask.y) == 0xffffffffu && (mask.z & C::M2) == C::M2 && !(bad.x | bad.y | (C::M2 ? bad.z : 0u)) &&
                                    p0 >= kr.lo && p0 + KB <= kr.hi;
-                uint32_t seen[3] = {0xffffffffu, 0xffffffffu, 0xffffffffu};
-                bool done = false;
-                if (__all_sync(0xffffffffu, whole)) {
-                    if (__all_sync(0xffffffffu, m != -INFINITY)) done = tile_fast<DH, false>(tS, xa, seen, c, m, l);
-                } else {
+                const bool all_whole = __all_sync(0xffffffffu, whole);
+                uint32_t seen[3] = {0xffffffffu, 0xffffffffu, 0xffffffffu}, any = 1;
+                if (!all_whole) {
                     const uint32_t there[3] = {mask.x, mask.y, mask.z}, bads[3] = {bad.x, bad.y, bad.z};
                     const int a = kr.lo - p0, e = kr.hi - p0;          // keys a .. e - 1 of the block
-                    uint32_t any = 0;
+                    any = 0;
 #pragma unroll
                     for (int k = 0; k < (KB + 31) / 32; ++k) {
                         const int a1 = min(max(a - 32 * k, 0), 32), e1 = min(max(e - 32 * k, 0), 32);
@@ -623,8 +631,19 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                         any |= seen[k];
                         if (seen[k] & bads[k]) l = NAN;                // the row sees a value that is not finite
                     }
-                    if (__all_sync(0xffffffffu, m != -INFINITY || !any)) done = tile_fast<DH, true>(tS, xa, seen, c, m, l);
                 }
+                if (__any_sync(0xffffffffu, m == -INFINITY)) {
+                    // a row without m (nothing has been summed for it): the largest of the first scores will do, if it sees one of them
+                    tmem_ld_wait();
+                    loaded16(xa);
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, seen[0] >> e & 1 ? xa[e] : -INFINITY);
+                    if (m == -INFINITY) m = top;
+                }
+                bool done = false;
+                if (__all_sync(0xffffffffu, m != -INFINITY || !any))
+                    done = all_whole ? tile_fast<DH, false>(tS, xa, seen, c, m, l) : tile_fast<DH, true>(tS, xa, seen, c, m, l);
                 if (!done) {
                     tmem_ld_wait();
                     tile_slow<DH>(tS, tO, seen, c, n, bars.pv_done(g, n - 1), m, l, ok);
@@ -640,11 +659,12 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         tc_fence_after();
         if (!ok) s_expired = 1;
         if (merge) asm volatile("bar.sync 1, %0;" ::"n"(NG * 128) : "memory");    // queries and rings are at rest
+        const int rr = r0 + r;
+        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + w.h * A.share + rr % A.share) * DH;
+        const float expired = s_expired || !ok ? NAN : 0.f;
         if (merge ? g < G : some && (T > 1 ? g < T : g == 0)) {
-            const float expired = s_expired || !ok ? NAN : 0.f, inv = (l == 0.f ? 0.f : 1.0f / l) + expired;
+            const float inv = (l == 0.f ? 0.f : 1.0f / l) + expired;
             uint8_t *state = smem + g * C::STATE;
-            const int rr = r0 + r;
-            bf16 *out = (bf16 *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + w.h * A.share + rr % A.share) * DH;
 #pragma unroll 1
             for (int i = 0; i < DH; i += 32) {
                 float o[32];
@@ -667,47 +687,80 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
             }
             if (merge) *reinterpret_cast<float2 *>(state + 128 * DH * 4 + trow * 8) = make_float2(n ? m * c : -INFINITY, l + expired);
         }
+        if (merge && T == 1) {
+            // The groups' states of the one tile become one, over the first (a third or half of the columns to a group), or the result.  They count
+            // in the groups' order; one without scores counts for nothing.
+            asm volatile("bar.sync 1, %0;" ::"n"(NG * 128) : "memory");
+            float f[NG], mx = -INFINITY, sum = 0.f;
+            float2 ml[NG];
+#pragma unroll
+            for (int k = 0; k < NG; ++k) ml[k] = *reinterpret_cast<const float2 *>(smem + k * C::STATE + 128 * DH * 4 + trow * 8), mx = fmaxf(mx, ml[k].x);
+#pragma unroll
+            for (int k = 0; k < NG; ++k) f[k] = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx), sum = fmaf(ml[k].y, f[k], sum);
+            const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+            for (int i = g; i < DH / 8; i += NG) {
+                float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < NG; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (f[k] == 0.f) continue;          // (what is there may be anything)
+                        const float4 o = *reinterpret_cast<const float4 *>(smem + k * C::STATE + ((2 * i + e) * 128 + trow) * 16);
+                        v[4 * e] = fmaf(o.x, f[k], v[4 * e]), v[4 * e + 1] = fmaf(o.y, f[k], v[4 * e + 1]);
+                        v[4 * e + 2] = fmaf(o.z, f[k], v[4 * e + 2]), v[4 * e + 3] = fmaf(o.w, f[k], v[4 * e + 3]);
+                    }
+                if (split > 1) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        *reinterpret_cast<float4 *>(smem + ((2 * i + e) * 128 + trow) * 16) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                } else if (r < nr) {
+                    *reinterpret_cast<uint4 *>(out + 8 * i) = make_uint4(bf16_pair(v[0] * inv, v[1] * inv), bf16_pair(v[2] * inv, v[3] * inv),
+                                                                         bf16_pair(v[4] * inv, v[5] * inv), bf16_pair(v[6] * inv, v[7] * inv));
+                }
+            }
+            if (g == 0) *reinterpret_cast<float2 *>(smem + NG * C::STATE + trow * 8) = make_float2(mx, sum);
+        }
     }
     __syncwarp();
     cp_async_wait<0>();
     tc_fence_before();
-    if (split > 1) cluster_sync_all();
-    else __syncthreads();
-    if (merge) {
-        // Row words of four columns, 8 rows x 4 of them to a warp (32 bytes of a row, and every bank once); each CTA of a cluster
-        // takes every split-th of these.  States count in the order of rank and group; one without scores counts for nothing.
+    if (split > 1) {
+        cluster_sync_all();
+        // The CTAs' states.  Row words of four columns, 8 rows x 4 of them to a warp (32 bytes of a row, and every bank once); each CTA of a
+        // cluster takes every split-th of these.  A word's loads are in flight together (one after the other they were 5 to 9 us of a call).
         const uint32_t st0 = smem_u32(smem);
-        const int groups = T == 1 ? NG : 1, n_words = T * 16 * (DH / 16);
+        const int n_words = T * 16 * (DH / 16);
         for (int i = rank * 16 + warp; i < n_words; i += split * 16) {
             const int tile = i / (16 * (DH / 16)), in = i % (16 * (DH / 16));
             const int trow = (in / (DH / 16)) * 8 + (lane & 7), col4 = (in % (DH / 16)) * 4 + (lane >> 3), r = tile * 128 + trow;
             if (r >= nr) continue;
+            const uint32_t at_ml = st0 + (T == 1 ? NG * C::STATE : tile * C::STATE + 128 * DH * 4) + trow * 8;
+            const uint32_t at_o = st0 + tile * C::STATE + (col4 * 128 + trow) * 16;
+            float2 ml[TILE_SPLIT];
+            float4 o[TILE_SPLIT];
             float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < TILE_SPLIT; ++k) {
+                ml[k] = make_float2(-INFINITY, 0.f), o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k < split) ml[k] = ld_cluster_f2(cluster_map(at_ml, k)), o[k] = ld_cluster_f4(cluster_map(at_o, k));
+            }
+#pragma unroll
+            for (int k = 0; k < TILE_SPLIT; ++k) mx = fmaxf(mx, ml[k].x);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k = 0; k < split; ++k)
-                for (int g = 0; g < groups; ++g) {
-                    const uint32_t at = cluster_map(st0 + (T == 1 ? g : tile) * C::STATE, k);
-                    mx = fmaxf(mx, ld_cluster_f2(at + 128 * DH * 4 + trow * 8).x);
-                }
-            for (int k = 0; k < split; ++k)
-                for (int g = 0; g < groups; ++g) {
-                    const uint32_t at = cluster_map(st0 + (T == 1 ? g : tile) * C::STATE, k);
-                    const float2 ml = ld_cluster_f2(at + 128 * DH * 4 + trow * 8);
-                    if (ml.x == -INFINITY) {
-                        sum += ml.y;                        // (0, or the NaN of a wait that ran out)
-                        continue;
-                    }
-                    const float f = few_exp2(ml.x - mx);
-                    const float4 o = ld_cluster_f4(at + (col4 * 128 + trow) * 16);
-                    sum = fmaf(ml.y, f, sum);
-                    v.x = fmaf(o.x, f, v.x), v.y = fmaf(o.y, f, v.y), v.z = fmaf(o.z, f, v.z), v.w = fmaf(o.w, f, v.w);
-                }
+#pragma unroll
+            for (int k = 0; k < TILE_SPLIT; ++k) {
+                const float f = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx);
+                sum = fmaf(ml[k].y, f, sum);
+                if (f != 0.f) v.x = fmaf(o[k].x, f, v.x), v.y = fmaf(o[k].y, f, v.y), v.z = fmaf(o[k].z, f, v.z), v.w = fmaf(o[k].w, f, v.w);
+            }
             const float inv = sum == 0.f ? 0.f : 1.0f / sum;
             const int rr = r0 + r;
             bf16 *out = (bf16 *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + w.h * A.share + rr % A.share) * DH + col4 * 4;
             *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
         }
-        if (split > 1) cluster_sync_all();                  // nobody leaves while its state is read
+        cluster_sync_all();                                 // nobody leaves while its state is read
+    } else {
+        __syncthreads();
     }
     if (warp == C::PW) {
         tc_fence_after();
@@ -730,7 +783,7 @@ template <int DH, bool KV4, typename F> static TilePlan tile_plan(long long unit
     TilePlan best = {1, 1};
     long long least = -1;
     for (int tiles = 1; tiles <= ng; tiles += ng - 1)
-        for (int split = 1; split <= 8; ++split) {
+        for (int split = 1; split <= TILE_SPLIT; ++split) {
             const long long fit = split == 1 ? n_sm : clusters(split);
             if (fit < 1 || (split > 1 && blocks < 2 * split)) break;
             const long long mine = t1 < tiles ? t1 : tiles, job = JOB * mine, per = (blocks + split - 1) / split;
@@ -746,10 +799,10 @@ static int launch_attn_tile(const BatchD &B, const AttnRows &A, const Src &src, 
     using C = TileCfg<DH>;
     auto kern = k_attn_tile<Src, DH>;
     static bool sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
-    static int fit[NFD_PAGED_DEVICES][9];
+    static int fit[NFD_PAGED_DEVICES][TILE_SPLIT + 1];
     if (!sized[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return NFD_E_CUDA;
-        for (int split = 2; split <= 8; ++split) {
+        for (int split = 2; split <= TILE_SPLIT; ++split) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(split), cfg.blockDim = dim3(TILE_THREADS), cfg.dynamicSmemBytes = C::SMEM;
             cudaLaunchAttribute at;
