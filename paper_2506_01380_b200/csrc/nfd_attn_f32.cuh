@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
     const int rows = min(sr.y, B.max_rows) * A.share;
     if (r0 >= rows) return;                                             // (the whole cluster)
     const int nr = min(ROWS, rows - r0);
-    const int keys = K.range(B, s, sr.y, 0).hi, tiles = (keys + F32_KEYS - 1) / F32_KEYS, per = (tiles + split - 1) / split;
+    const int keys = K.length(B, s), tiles = (keys + F32_KEYS - 1) / F32_KEYS, per = (tiles + split - 1) / split;
     const int t0 = min(tiles, rank * per), t1 = min(tiles, t0 + per);
     const long long seq = s * K.seq_stride + h * K.head_stride;
     const unsigned char *mask = K.mask ? K.mask + (size_t)s * K.n_keys : nullptr;
@@ -56,8 +56,9 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
         if (part == 0) sM[64 * b + key] = here;
     };
     for (int i = tid; i < ROWS * W; i += C::THREADS) {
-        const int r = i / W, w = i % W, rr = r0 + min(r, nr - 1);
-        cp_async16(smem_u32(sQ + r * LD + 4 * w), (const float *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (h * A.share + rr % A.share) * DH + 4 * w, 16);
+        const int r = i / W, w = i % W;
+        const int2 at = A.split(r0 + min(r, nr - 1));
+        cp_async16(smem_u32(sQ + r * LD + 4 * w), (const float *)A.q + (long long)(sr.x + at.x) * A.q_stride + (h * A.share + at.y) * DH + 4 * w, 16);
     }
     cp_async_commit();
     if (t0 < t1) fill(t0);
@@ -155,8 +156,8 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
         for (int d = 1; d < 16; d <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
     auto dim = [&](int e) { return DH == 32 ? 2 * tx + e : 16 * (e & ~3) + 4 * tx + (e & 3); };
     auto place = [&](int r) {
-        const int rr = r0 + r;
-        return (float *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + h * A.share + rr % A.share) * DH;
+        const int2 at = A.split(r0 + r);
+        return (float *)A.out + ((long long)(sr.x + at.x) * A.heads + h * A.share + at.y) * DH;
     };
     if (split == 1) {
 #pragma unroll

@@ -283,10 +283,11 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, n = lane >> 2;
     const int rank = blockIdx.x % split, h = blockIdx.x / split, s = blockIdx.y, r0 = blockIdx.z * ROWS;
     const int2 sr = B.rows(s);
+    const int len = src.K.length(B, s);
     const int rows = min(sr.y, B.max_rows) * A.share;                             // of the whole unit; row r: row r / share, head h * share + r % share
     if (r0 >= rows) return;                                                       // (the whole cluster)
     const int nr = min(ROWS, rows - r0);
-    const KeyRange first = src.K.range(B, s, sr.y, r0 / A.share), last = src.K.range(B, s, sr.y, (r0 + nr - 1) / A.share);
+    const KeyRange first = src.K.range(B, len, sr.y, A.split(r0).x), last = src.K.range(B, len, sr.y, A.split(r0 + nr - 1).x);
     // (bounds rise with the row, but for rows of tokens below 0, which see nothing: 0, 0)
     const int lo = first.lo, hi = last.hi;
 
@@ -307,15 +308,15 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
         cp_async_commit();
     }
     if (threadIdx.x < ROWS) {
-        const KeyRange r = src.K.range(B, s, sr.y, (r0 + min((int)threadIdx.x, nr - 1)) / A.share);
+        const KeyRange r = src.K.range(B, len, sr.y, A.split(r0 + min((int)threadIdx.x, nr - 1)).x);
         s_range[threadIdx.x] = make_int2(r.lo, r.hi);
     }
     // queries: row n of every tile of 8, in the order of K's inner index
     uint32_t qb[NR][NS][2];
 #pragma unroll
     for (int t = 0; t < NR; ++t) {
-        const int rr = r0 + min(8 * t + n, nr - 1);
-        const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (h * A.share + rr % A.share) * DH;
+        const int2 at = A.split(r0 + min(8 * t + n, nr - 1));
+        const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + at.x) * A.q_stride + (h * A.share + at.y) * DH;
 #pragma unroll
         for (int st = 0; st < NS; ++st) {
             const uint2 v = *reinterpret_cast<const uint2 *>(q + Src::q_dim(st, c));
@@ -457,9 +458,9 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
     // the CTA's
     float *T = reinterpret_cast<float *>(few_smem + FEW_WARPS * F::WARP);
     auto write = [&](int r, int d, float4 v, float sum) {
-        const int rr = r0 + r;
+        const int2 at = A.split(r0 + r);
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + h * A.share + rr % A.share) * DH + d;
+        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + h * A.share + at.y) * DH + d;
         *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
     };
     for (int i = threadIdx.x; i < nr * (DH / 4); i += 32 * FEW_WARPS) {

@@ -8,16 +8,21 @@ struct AttnRows {
     void *out;
     long long q_stride;
     int heads, share;                    // heads, heads per head of the keys
+    // row r of a unit (rows x heads that share a head of keys) as row and which of the heads; (without a division where there is none to share)
+    __device__ __forceinline__ int2 split(int r) const {
+        if (share == 1) return make_int2(r, 0);
+        const int i = r / share;
+        return make_int2(i, r - i * share);
+    }
 };
 
 // Keys and values in 4-bit pages.
 template <int DH> struct Kv4Keys {
     PagesD P;
     CausalMask mask;
-    __device__ __forceinline__ KeyRange range(const BatchD &B, int s, int n, int i) const {
-        const int len = B.tokens(s);
-        return mask.range(len, P.oldest(B, len), n, i);
-    }
+    // tokens of sequence s (a load: asked for early); what row i of n of a sequence of that many sees
+    __device__ __forceinline__ int length(const BatchD &B, int s) const { return B.tokens(s); }
+    __device__ __forceinline__ KeyRange range(const BatchD &B, int len, int n, int i) const { return mask.range(len, P.oldest(B, len), n, i); }
 };
 // States of an encoder.
 template <typename TS, int DH> struct StateKeys {
@@ -25,8 +30,7 @@ template <typename TS, int DH> struct StateKeys {
     const unsigned char *mask;
     long long seq_stride, key_stride, head_stride;
     int n_keys;
-    __device__ __forceinline__ KeyRange range(const BatchD &B, int s, int n, int i) const {
-        return {0, B.kv_len ? min(B.tokens(s), n_keys) : n_keys};
-    }
+    __device__ __forceinline__ int length(const BatchD &B, int s) const { return B.kv_len ? min(B.tokens(s), n_keys) : n_keys; }
+    __device__ __forceinline__ KeyRange range(const BatchD &, int len, int, int) const { return {0, len}; }
 };
 

@@ -530,6 +530,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % split, s = blockIdx.y, r0 = blockIdx.z * tiles * 128;
     const int2 sr = B.rows(s);
+    const int len = src.K.length(B, s);
     const TileBars bars = {smem_u32(smem + C::AT_BAR)};
     if (threadIdx.x == 0) bars.init(C::PW, 4 * NG), s_expired = 0;
     if (DH == 32) {
@@ -548,17 +549,21 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
     w.s = s, w.h = blockIdx.x / split;
     if (warp >= C::SM0) {
         // softmax warps: the row's queries, into the operand of its tile; with one tile, the groups share them out
-        constexpr int CPR = DH / 8;
-        const int g = (warp - C::SM0) >> 2, trow = (warp & 3) * 32 + lane, r = (T == 1 ? 0 : g * 128) + trow, rr = r0 + min(r, nr - 1);
-        const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + rr / A.share) * A.q_stride + (w.h * A.share + rr % A.share) * DH;
-        const uint32_t sq = smem_u32(smem + C::AT_Q) + (T == 1 ? 0 : g) * C::Q_BYTES;
+        // (a row's pieces by neighbouring lanes: a row to a lane took 3000 clocks for three tiles)
+        constexpr int CPR = DH / 8, RPI = 32 / CPR;
+        const int g = (warp - C::SM0) >> 2, piece = lane % CPR;
+        const uint32_t sq = smem_u32(smem + C::AT_Q) + (T == 1 ? 0 : g) * C::Q_BYTES + (piece >> 3) * (128 * 128);
         if (g < G)
-            for (int i = T == 1 ? g : 0; i < CPR; i += T == 1 ? NG : 1)
-                cp_async16(sq + (i >> 3) * (128 * 128) + tile_at(trow, i & 7), q + 8 * i, r < nr ? 16 : 0);
+            for (int i = T == 1 ? g : 0; i < CPR; i += T == 1 ? NG : 1) {
+                const int trow = (warp & 3) * 32 + i * RPI + lane / CPR, r = (T == 1 ? 0 : g * 128) + trow;
+                const int2 at = A.split(r0 + min(r, nr - 1));
+                const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + at.x) * A.q_stride + (w.h * A.share + at.y) * DH + piece * 8;
+                cp_async16(sq + tile_at(trow, piece & 7), q, r < nr ? 16 : 0);
+            }
         cp_async_commit();
     }
     {
-        const KeyRange first = src.K.range(B, s, sr.y, r0 / A.share), last = src.K.range(B, s, sr.y, (r0 + nr - 1) / A.share);
+        const KeyRange first = src.K.range(B, len, sr.y, A.split(r0).x), last = src.K.range(B, len, sr.y, A.split(r0 + nr - 1).x);
         const int all = max(0, (last.hi - first.lo + KB - 1) / KB), per = (all + split - 1) / split;
         w.lo = first.lo + min(all, rank * per) * KB;
         w.nb = max(0, min(all - rank * per, per));
@@ -599,7 +604,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         const uint32_t lane_off = (uint32_t)(quad * 32) << 16, tO = tmem + C::TM_O + g * 64 * SUB + lane_off;
         const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
         const float c = 1.4426950408889634f * rsqrtf((float)DH);
-        const KeyRange kr = src.K.range(B, s, sr.y, (r0 + min(r, nr - 1)) / A.share);
+        const KeyRange kr = src.K.range(B, len, sr.y, A.split(r0 + min(r, nr - 1)).x);
         cp_async_wait<0>();
         tile_publish(bars.q_full());
         float m = -INFINITY, l = 0.f;                                  // m: reference, in units of scores
@@ -659,8 +664,8 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         tc_fence_after();
         if (!ok) s_expired = 1;
         if (merge) asm volatile("bar.sync 1, %0;" ::"n"(NG * 128) : "memory");    // queries and rings are at rest
-        const int rr = r0 + r;
-        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + w.h * A.share + rr % A.share) * DH;
+        const int2 at = A.split(r0 + r);
+        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH;
         const float expired = s_expired || !ok ? NAN : 0.f;
         if (merge ? g < G : some && (T > 1 ? g < T : g == 0)) {
             const float inv = (l == 0.f ? 0.f : 1.0f / l) + expired;
@@ -754,8 +759,8 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                 if (f != 0.f) v.x = fmaf(o[k].x, f, v.x), v.y = fmaf(o[k].y, f, v.y), v.z = fmaf(o[k].z, f, v.z), v.w = fmaf(o[k].w, f, v.w);
             }
             const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-            const int rr = r0 + r;
-            bf16 *out = (bf16 *)A.out + ((long long)(sr.x + rr / A.share) * A.heads + w.h * A.share + rr % A.share) * DH + col4 * 4;
+            const int2 at = A.split(r0 + r);
+            bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH + col4 * 4;
             *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
         }
         cluster_sync_all();                                 // nobody leaves while its state is read
