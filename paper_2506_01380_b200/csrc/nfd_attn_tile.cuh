@@ -60,6 +60,9 @@ __device__ __forceinline__ void loaded32(float *x) {
     asm volatile("" : "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]),
                       "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31]));
 }
+__device__ __forceinline__ void loaded8(float *x) {
+    asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]));
+}
 __device__ __forceinline__ void loaded16(float *x) {
     asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]),
                       "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]));
@@ -410,16 +413,22 @@ static __device__ __forceinline__ bool tile_fast(uint32_t tS, float *xa, const u
     constexpr int KB = TileCfg<DH>::KB;
     const float mc = m == -INFINITY ? 0.f : m * c;
     float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-    float xb[16];
+    float xb[8];
     uint32_t pk[KB / 2];
+    tmem_ld_wait();
+    loaded16(xa);
+    tmem_ld8(tS + 16, reinterpret_cast<uint32_t *>(xb));
 #pragma unroll
-    for (int i = 0; i < KB; i += 16) {
-        float *x = i & 16 ? xb : xa, *y = i & 16 ? xa : xb;
-        tmem_ld_wait();
-        loaded16(x);
-        if (i + 16 < KB) tmem_ld16(tS + i + 16, reinterpret_cast<uint32_t *>(y));
+    for (int i = 0; i < KB; i += 8) {
+        // columns 0 .. 15 are in xa; then xb, xa (first half), xb ...
+        float *x = i < 16 ? xa + i : (i >> 3) & 1 ? xa : xb;
+        if (i >= 16) {
+            tmem_ld_wait();
+            loaded8(x);
+            if (i + 8 < KB) tmem_ld8(tS + i + 8, reinterpret_cast<uint32_t *>((i >> 3) & 1 ? xb : xa));
+        }
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
+        for (int u = 0; u < 4; ++u) {
             float2 s = make_float2(x[2 * u], x[2 * u + 1]);
             if (MASKED) {
                 const uint32_t bits = seen[i >> 5] >> (i & 31);
