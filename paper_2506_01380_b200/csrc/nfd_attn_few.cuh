@@ -20,7 +20,10 @@
 #include "nfd_sm100.cuh"
 
 #define FEW_WARPS 8
-#define FEW_MOST 32               // rows of a unit that this kernel takes
+// Rows of a unit that this kernel takes.  Measured against the kernel for many rows, us: 16 heads x 64 behind 5712 tokens in 4-bit pages, 24, 64 and
+// 100 rows 16.9, 17.5, 26.2 here and 21.2, 21.7, 22.6 there; 4 x 16 heads against 512 states 8.3, 9.5, 17.4 and 10.3, 10.5, 11.4;
+// head dimension 128, eight sequences of 4 heads of keys behind 8192, 32 rows 46.4 and 50.1, 96 rows 151 and 51.
+constexpr int few_most(int dh) { return dh == 128 ? 32 : 64; }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -507,30 +510,33 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
     cluster_sync_all();                                                           // nobody leaves while its state is read
 }
 
-// CTAs of a cluster that a unit is split over: as many as the device holds at once, and no more than give every warp a chunk or two.
-static int few_split(long long units, long long keys, int kc, int n_sm, int per_sm) {
+// CTAs of a cluster that a unit is split over: as many as let the device hold all units' clusters at once (fit[i]: clusters of 2^i CTAs), and
+// no more than give every warp a chunk or two; sixteen where they get three and more.  (16 heads x 64, 24 rows behind 5712 tokens, one CTA to an
+// SM: in 8 pieces, of which the device holds 14 at once, 23 us, in 4 pieces 15.  One row: in 8 pieces 10.8, in 16 11.8; 24 heads on 8 behind 32768
+// tokens 39 and 33.)
+static int few_split(long long units, long long keys, int kc, const int *fit) {
     const long long chunks = (keys + kc - 1) / kc;
-    int split = 1;
-    while (split < 16 && units * split * 2 <= (long long)n_sm * per_sm && chunks > (long long)(split == 8 ? 48 : split) * FEW_WARPS) split *= 2;
-    return split;
+    int i = 0;
+    while (i < 4 && units <= fit[i + 1] && chunks > (long long)(i == 3 ? 48 : 1 << i) * FEW_WARPS) ++i;
+    return 1 << i;
 }
 
 template <typename Src, int DH, int NR>
 static int launch_attn_few_nr(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
     using F = FewCfg<Src, DH, NR>;
     auto kern = k_attn_few<Src, DH, NR>;
-    static int per_sm[NFD_PAGED_DEVICES];                                         // (once per device and kernel)
-    if (!per_sm[dev]) {
-        int n = 0;
+    static bool sized[NFD_PAGED_DEVICES];                                         // (once per device and kernel)
+    static int fit[NFD_PAGED_DEVICES][5];
+    if (!sized[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
-            cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 32 * FEW_WARPS, F::SMEM) != cudaSuccess || n < 1)
+            cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
             return NFD_E_CUDA;
-        per_sm[dev] = n;
+        for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * FEW_WARPS, F::SMEM);
+        sized[dev] = true;
     }
     const long long tiles = ((long long)B.max_rows * A.share + F::ROWS - 1) / F::ROWS;
     if (tiles > 65535) return NFD_E_RANGE;
-    const int split = few_split((long long)kv_heads * B.n_seqs * tiles, keys, Src::KC, n_sm, per_sm[dev]);
+    const int split = few_split((long long)kv_heads * B.n_seqs * tiles, keys, Src::KC, fit[dev]);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kv_heads * split, B.n_seqs, (unsigned)tiles), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = F::SMEM, cfg.stream = st;
     cudaLaunchAttribute at;

@@ -34,3 +34,16 @@ template <typename TS, int DH> struct StateKeys {
     __device__ __forceinline__ KeyRange range(const BatchD &, int len, int, int) const { return {0, len}; }
 };
 
+
+// Clusters of `ctas` CTAs that the device holds at once.
+template <typename Kernel> static int clusters_that_fit(Kernel kern, int ctas, int threads, int smem) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas), cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = ctas, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at, cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess) return n;
+    cudaGetLastError();
+    return 0;
+}

@@ -816,14 +816,7 @@ static int launch_attn_tile(const BatchD &B, const AttnRows &A, const Src &src, 
     static int fit[NFD_PAGED_DEVICES][TILE_SPLIT + 1];
     if (!sized[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return NFD_E_CUDA;
-        for (int split = 2; split <= TILE_SPLIT; ++split) {
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(split), cfg.blockDim = dim3(TILE_THREADS), cfg.dynamicSmemBytes = C::SMEM;
-            cudaLaunchAttribute at;
-            at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
-            cfg.attrs = &at, cfg.numAttrs = 1;
-            if (cudaOccupancyMaxActiveClusters(&fit[dev][split], kern, &cfg) != cudaSuccess) fit[dev][split] = 0, cudaGetLastError();
-        }
+        for (int split = 2; split <= TILE_SPLIT; ++split) fit[dev][split] = clusters_that_fit(kern, split, TILE_THREADS, C::SMEM);
         sized[dev] = true;
     }
     const long long rows = (long long)B.max_rows * A.share;

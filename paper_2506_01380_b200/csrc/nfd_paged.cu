@@ -209,7 +209,7 @@ int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_head
     const long long keys = held < seen ? held : seen;
     return by_head_dim(pages->head_dim, [&](auto d) -> int {
         constexpr int DH = decltype(d)::value;
-        if ((long long)B.max_rows * A.share > FEW_MOST)
+        if ((long long)B.max_rows * A.share > few_most(DH))
             return launch_attn_tile<TileKv4<DH>, DH>(B, A, TileKv4<DH>{{P, {frame_tokens, window}}}, P.heads, keys, dev, n_sm, (cudaStream_t)cuda_stream);
         FewKv4<DH> src;
         src.K = {P, {frame_tokens, window}};
@@ -247,7 +247,7 @@ int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_
             using TS = std::remove_pointer_t<decltype(t)>;
             const StateKeys<TS, DH> K = {(const TS *)states->k, (const TS *)states->v, states->mask, st[0], st[1], st[2], states->n_keys};
             if constexpr (std::is_same_v<TS, bf16>) {
-                if ((long long)B.max_rows * A.share > FEW_MOST)
+                if ((long long)B.max_rows * A.share > few_most(DH))
                     return launch_attn_tile<TileStates<DH>, DH>(B, A, TileStates<DH>{K}, states->n_heads, states->n_keys, dev, n_sm, (cudaStream_t)cuda_stream);
                 FewStates<DH> src;
                 src.K = K;
