@@ -307,13 +307,16 @@ int nfd_pages_read(const nfd_pages *pages, const nfd_batch *batch, int dtype, vo
 /* Attention over a cache of NFD_DTYPE_KV4 pages.  q dev bf16
  * [n_rows][n_heads][head_dim], q_stride elements from row to row; out dev bf16
  * [n_rows][n_heads * head_dim].  n_heads is a multiple of pages->n_heads: head h
- * reads the pages' head h / (n_heads / pages->n_heads).  The mask is the library's
+ * reads the pages' head h / (n_heads / pages->n_heads); max_rows times that quotient
+ * is at most 2097120.  The mask is the library's
  * block-wise causal one: token p belongs to frame p / frame_tokens and sees the
  * tokens of the frames max(0, frame - window) .. frame that the cache holds
  * (frame_tokens = 1: a causal mask over the last window + 1 tokens).
  * The scale is 1 / sqrt(head_dim).  A row that sees nothing, or nothing but scores
- * of -inf, gives zeros; a row that sees a value that is not finite is NaN.  Scores, softmax and sums are fp32; probabilities are rounded to bf16 for
- * the product with V.  Should a device-side wait run out, the rows concerned are NaN. */
+ * of -inf, gives zeros; a row that sees a value that is not finite is NaN, and steps of
+ * 2^27 and more (numbers beyond 10^8) count as not finite here.  Scores, softmax and
+ * sums are fp32; probabilities are rounded to bf16 for the product with V.  Should a
+ * device-side wait run out, the rows concerned are NaN. */
 int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,
                       int frame_tokens, int window, void *out, void *cuda_stream);
 

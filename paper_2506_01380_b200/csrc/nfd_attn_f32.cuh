@@ -209,13 +209,12 @@ template <int DH, int ROWS>
 static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
     using C = F32Cfg<DH, ROWS>;
     auto kern = k_attn_f32<DH, ROWS>;
-    static bool sized[NFD_PAGED_DEVICES];                               // (once per device and kernel)
+    static std::atomic<bool> sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
     if (!sized[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return NFD_E_CUDA;
         sized[dev] = true;
     }
     const long long tiles = ((long long)B.max_rows * A.share + ROWS - 1) / ROWS, units = kv_heads * tiles * B.n_seqs;
-    if (tiles > 65535) return NFD_E_RANGE;
     const int blocks = (K.n_keys + F32_KEYS - 1) / F32_KEYS;
     int split = 1;
     while (split < 8 && units * split * 2 <= 2 * n_sm && blocks > split) split *= 2;

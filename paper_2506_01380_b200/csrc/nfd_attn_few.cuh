@@ -13,8 +13,7 @@
 // so that what a key costs does not grow with the 16 rows of a tile (with the rows on that side: twice the products and twice the registers
 // for rows that are not there).  P^T changes sides by movmatrix.  The inner index of either product may be permuted as long as both of its
 // operands are, so that a lane's share of a key is a run of its row (for S) and a lane's share of a value a run of dims
-// (for O); 4-bit codes become bf16 numbers in registers: the code goes into the mantissa of 128 + n, 128 + z is
-// subtracted (exact), the step multiplied (exact: 4 by 4 bits).
+// (for O); 4-bit codes become bf16 numbers in registers (Kv4Scale).
 #pragma once
 #include "nfd_attn_rows.cuh"
 #include "nfd_sm100.cuh"
@@ -61,6 +60,7 @@ __device__ __forceinline__ float few_exp2(float x) {
 // A warp's chunk of keys in shared memory, for 4-bit pages: codes of K and V, their words, and which keys are there.
 template <int DH> struct FewKv4 {
     static constexpr bool KV4 = true;
+    static constexpr float UP = KV4_UP;                     // what scores and results are to be multiplied by
     static constexpr int KC = 32;
     static constexpr int NST = 3;                           // (with 4, head dimension 128 leaves one CTA to an SM: 138 us for 101)
     static constexpr int RB = DH / 2;                       // bytes of a row of codes
@@ -130,7 +130,7 @@ template <int DH> struct FewKv4 {
 #pragma unroll
         for (int j = 0; j < WB / 4; ++j) {
             const uint32_t v = w[j];
-            const bool b0 = (v & 0x7F80u) == 0x7F80u, b1 = (v >> 16 & 0x7F80u) == 0x7F80u;
+            const bool b0 = kv4_not_finite(v), b1 = kv4_not_finite(v >> 16);
             if (DH == 32) mine |= reinterpret_cast<const uint32_t *>(stage + 2 * KC * (RB + WB))[1] >> lane & 1 ? b1 : b0;
             else mine |= b0 || b1;
         }
@@ -165,11 +165,12 @@ template <int DH> struct FewKv4 {
         } else {
             w[0] = *src;
         }
-        const uint32_t sc = word(stage + 2 * KC * RB, key, c * (DH / 4) / 32, stage), z2 = kv4_z2(sc, sc), s2 = kv4_step2(sc, sc);
+        const uint32_t sc = word(stage + 2 * KC * RB, key, c * (DH / 4) / 32, stage);
+        const Kv4Scale scale(sc, sc);
 #pragma unroll
         for (int i = 0; i < NW; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[4 * i + j] = kv4_pair(w[i], j, z2, s2);
+            for (int j = 0; j < 4; ++j) b[4 * i + j] = scale.pair(w[i], j);
     }
     // dims of the result that this lane's n-th column of product tile t is
     static __device__ __forceinline__ int o_dim(int t, int n) {
@@ -180,12 +181,12 @@ template <int DH> struct FewKv4 {
     static __device__ __forceinline__ void v_frag(const uint8_t *stage, int k0, int n, uint32_t *b) {
         const uint8_t *v = stage + KC * RB, *w = stage + 2 * KC * RB + KC * WB;
         const int g = n * (DH / 8) / 32;
-        const uint32_t s0 = word(w, k0, g, stage), s1 = word(w, k0 + 4, g, stage), z2 = kv4_z2(s0, s1), s2 = kv4_step2(s0, s1);
+        const Kv4Scale scale(word(w, k0, g, stage), word(w, k0 + 4, g, stage));
         if constexpr (DH == 32) {
             const uint32_t x = *reinterpret_cast<const uint16_t *>(v + k0 * RB + n * 2) |
                                (uint32_t)*reinterpret_cast<const uint16_t *>(v + (k0 + 4) * RB + n * 2) << 16;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = kv4_pair(x, j, z2, s2);
+            for (int j = 0; j < 4; ++j) b[j] = scale.pair(x, j);
         } else {
             constexpr int NW = DH / 64;
             uint32_t x[NW], y[NW];
@@ -199,7 +200,7 @@ template <int DH> struct FewKv4 {
             for (int i = 0; i < NW; ++i) {
                 const uint32_t even = __byte_perm(x[i], y[i], 0x5410), odd = __byte_perm(x[i], y[i], 0x7632);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) b[8 * i + j] = kv4_pair(even, j, z2, s2), b[8 * i + 4 + j] = kv4_pair(odd, j, z2, s2);
+                for (int j = 0; j < 4; ++j) b[8 * i + j] = scale.pair(even, j), b[8 * i + 4 + j] = scale.pair(odd, j);
             }
         }
     }
@@ -208,6 +209,7 @@ template <int DH> struct FewKv4 {
 // The same for bf16 states.  Rows are swizzled in 16-byte pieces so that neither operand's reads meet in a bank.
 template <int DH> struct FewStates {
     static constexpr bool KV4 = false;
+    static constexpr float UP = 1.0f;
     static constexpr int KC = DH == 32 ? 32 : 16;
     static constexpr int NST = DH == 128 ? 3 : 4;
     static constexpr int RB = 2 * DH, PR = RB / 16;
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
             qb[t][st][0] = v.x, qb[t][st][1] = v.y;
         }
     }
-    const float cs = 1.4426950408889634f * rsqrtf((float)DH);
+    const float cs = 1.4426950408889634f * rsqrtf((float)DH) * Src::UP;
     // this lane's rows: 2 c and 2 c + 1 of every tile of 8
     float o[NR][NS][4], m[NR][2], l[NR][2];
 #pragma unroll
@@ -462,7 +464,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
     float *T = reinterpret_cast<float *>(few_smem + FEW_WARPS * F::WARP);
     auto write = [&](int r, int d, float4 v, float sum) {
         const int2 at = A.split(r0 + r);
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        const float inv = sum == 0.f ? 0.f : Src::UP / sum;
         bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + h * A.share + at.y) * DH + d;
         *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
     };
@@ -525,7 +527,7 @@ template <typename Src, int DH, int NR>
 static int launch_attn_few_nr(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
     using F = FewCfg<Src, DH, NR>;
     auto kern = k_attn_few<Src, DH, NR>;
-    static bool sized[NFD_PAGED_DEVICES];                                         // (once per device and kernel)
+    static std::atomic<bool> sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
     static int fit[NFD_PAGED_DEVICES][5];
     if (!sized[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
@@ -535,7 +537,6 @@ static int launch_attn_few_nr(const BatchD &B, const AttnRows &A, const Src &src
         sized[dev] = true;
     }
     const long long tiles = ((long long)B.max_rows * A.share + F::ROWS - 1) / F::ROWS;
-    if (tiles > 65535) return NFD_E_RANGE;
     const int split = few_split((long long)kv_heads * B.n_seqs * tiles, keys, Src::KC, fit[dev]);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kv_heads * split, B.n_seqs, (unsigned)tiles), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = F::SMEM, cfg.stream = st;

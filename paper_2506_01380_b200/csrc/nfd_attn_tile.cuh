@@ -146,6 +146,7 @@ __device__ __forceinline__ void tile_publish(uint32_t bar) {
 // ---- producers: bf16 states ---------------------------------------------------------------------------------
 template <int DH> struct TileStates {
     static constexpr bool KV4 = false;
+    static constexpr float UP = 1.0f;
     StateKeys<bf16, DH> K;
     __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok) const {
         using C = TileCfg<DH>;
@@ -234,14 +235,13 @@ template <int DH> struct TileStates {
 // ---- producers: 4-bit pages ---------------------------------------------------------------------------------
 template <int DH> struct TileKv4 {
     static constexpr bool KV4 = true;
+    static constexpr float UP = KV4_UP;                     // what scores and results are to be multiplied by
     Kv4Keys<DH> K;
     // a thread's share of a block: 64 (DH 32: 32) dims of a key of K and of V
     static constexpr int NW = DH == 32 ? 4 : 8, SUBS = DH == 128 ? 2 : 1;
     struct Regs {
         uint32_t c[NW], w;                                  // codes, words
     };
-    // a word's step is not finite
-    static __device__ __forceinline__ bool infinite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u; }
     static __device__ __forceinline__ uint32_t load_words(const uint16_t *words, long long place, int sub) {
         if (DH == 32) return __ldg(words + place);
         return __ldg(reinterpret_cast<const uint32_t *>(words + place * (DH / 32)) + sub);
@@ -263,11 +263,11 @@ template <int DH> struct TileKv4 {
     }
     // (a key that is not there has step 0: its row is zeros)
     static __device__ __forceinline__ void convert(const Regs &r, uint8_t *blk, int row) {
+        const Kv4Scale lower(r.w & 0xffffu, r.w & 0xffffu), upper(r.w >> 16, r.w >> 16);
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
-            const uint32_t w = i < 4 ? r.w & 0xffffu : r.w >> 16, z2 = kv4_z2(w, w), s2 = kv4_step2(w, w);
-            *reinterpret_cast<uint4 *>(blk + tile_at(row, i)) =
-                make_uint4(kv4_pair(r.c[i], 0, z2, s2), kv4_pair(r.c[i], 1, z2, s2), kv4_pair(r.c[i], 2, z2, s2), kv4_pair(r.c[i], 3, z2, s2));
+            const Kv4Scale &s = i < 4 ? lower : upper;
+            *reinterpret_cast<uint4 *>(blk + tile_at(row, i)) = make_uint4(s.pair(r.c[i], 0), s.pair(r.c[i], 1), s.pair(r.c[i], 2), s.pair(r.c[i], 3));
         }
     }
     __device__ __forceinline__ void produce(const BatchD &B, const TileWork &w, uint8_t *smem, const TileBars &bars, bool &ok) const {
@@ -307,7 +307,7 @@ template <int DH> struct TileKv4 {
             next = look_up();
             // Values whose step is not finite go in as zeros (a product with the 0 of a row that does not see them would be NaN), a bit for
             // each of their keys.
-            const bool bad0 = infinite(v.w), bad1 = DH > 32 && infinite(v.w >> 16);
+            const bool bad0 = kv4_not_finite(v.w), bad1 = DH > 32 && kv4_not_finite(v.w >> 16);
             uint32_t bad = __ballot_sync(0xffffffffu, bad0 || bad1);
             if (bad0) v.w &= 0xffff0000u;
             if (bad1) v.w &= 0xffffu;
@@ -612,7 +612,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         const int g = (warp - C::SM0) >> 2, quad = warp & 3, trow = quad * 32 + lane, r = (T == 1 ? 0 : g * 128) + trow;
         const uint32_t lane_off = (uint32_t)(quad * 32) << 16, tO = tmem + C::TM_O + g * 64 * SUB + lane_off;
         const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
-        const float c = 1.4426950408889634f * rsqrtf((float)DH);
+        const float c = 1.4426950408889634f * rsqrtf((float)DH) * Src::UP;
         const KeyRange kr = src.K.range(B, len, sr.y, A.split(r0 + min(r, nr - 1)).x);
         cp_async_wait<0>();
         tile_publish(bars.q_full());
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH;
         const float expired = s_expired || !ok ? NAN : 0.f;
         if (merge ? g < G : some && (T > 1 ? g < T : g == 0)) {
-            const float inv = (l == 0.f ? 0.f : 1.0f / l) + expired;
+            const float inv = (l == 0.f ? 0.f : Src::UP / l) + expired;
             uint8_t *state = smem + g * C::STATE;
 #pragma unroll 1
             for (int i = 0; i < DH; i += 32) {
@@ -711,7 +711,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
             for (int k = 0; k < NG; ++k) ml[k] = *reinterpret_cast<const float2 *>(smem + k * C::STATE + 128 * DH * 4 + trow * 8), mx = fmaxf(mx, ml[k].x);
 #pragma unroll
             for (int k = 0; k < NG; ++k) f[k] = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx), sum = fmaf(ml[k].y, f[k], sum);
-            const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+            const float inv = sum == 0.f ? 0.f : Src::UP / sum;
             for (int i = g; i < DH / 8; i += NG) {
                 float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -767,7 +767,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                 sum = fmaf(ml[k].y, f, sum);
                 if (f != 0.f) v.x = fmaf(o[k].x, f, v.x), v.y = fmaf(o[k].y, f, v.y), v.z = fmaf(o[k].z, f, v.z), v.w = fmaf(o[k].w, f, v.w);
             }
-            const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+            const float inv = sum == 0.f ? 0.f : Src::UP / sum;
             const int2 at = A.split(r0 + r);
             bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH + col4 * 4;
             *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
@@ -812,7 +812,7 @@ template <typename Src, int DH>
 static int launch_attn_tile(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
     using C = TileCfg<DH>;
     auto kern = k_attn_tile<Src, DH>;
-    static bool sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
+    static std::atomic<bool> sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
     static int fit[NFD_PAGED_DEVICES][TILE_SPLIT + 1];
     if (!sized[dev]) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return NFD_E_CUDA;
@@ -822,7 +822,6 @@ static int launch_attn_tile(const BatchD &B, const AttnRows &A, const Src &src, 
     const long long rows = (long long)B.max_rows * A.share;
     const TilePlan pl = tile_plan<DH, Src::KV4>((long long)kv_heads * B.n_seqs, rows, keys, n_sm, [&](int k) { return fit[dev][k]; });
     const long long nz = (rows + 128 * pl.tiles - 1) / (128 * pl.tiles);
-    if (nz > 65535) return NFD_E_RANGE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kv_heads * pl.split, B.n_seqs, (unsigned)nz), cfg.blockDim = dim3(TILE_THREADS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
     cudaLaunchAttribute at;

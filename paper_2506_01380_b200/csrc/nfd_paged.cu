@@ -69,8 +69,10 @@ int check_rows(const void *p, long long stride, int heads, int head_dim, int dty
     return NFD_OK;
 }
 
-int check_heads(int n_heads, int kv_heads) {
+// heads that share heads of keys; rows x heads that share one are numbered within a sequence, 32 and more to a CTA of a grid's last dimension
+int check_heads(int n_heads, int kv_heads, const BatchD &B) {
     if (n_heads < 1 || n_heads > 1024 || kv_heads < 1 || n_heads % kv_heads) return NFD_E_RANGE;
+    if ((long long)B.max_rows * (n_heads / kv_heads) > 65535LL * 32) return NFD_E_RANGE;
     return NFD_OK;
 }
 
@@ -195,7 +197,7 @@ int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_head
     RET(check_pages(pages, P));
     RET(check_batch(batch, true, B));
     if (pages->dtype != NFD_DTYPE_KV4) return NFD_E_BADCFG;
-    RET(check_heads(n_heads, P.heads));
+    RET(check_heads(n_heads, P.heads, B));
     RET(check_rows(q, q_stride, n_heads, pages->head_dim, NFD_DTYPE_BF16));
     if (!out) return NFD_E_NULLPTR;
     if (!aligned(out, 16)) return NFD_E_ALIGN;
@@ -226,7 +228,7 @@ int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_
     if (dtype != NFD_DTYPE_FP32 && dtype != NFD_DTYPE_BF16) return NFD_E_BADCFG;
     if (dh != 32 && dh != 64 && dh != 128) return NFD_E_BADCFG;
     if (states->n_keys < 0 || states->n_keys > NFD_MAX_TOKENS) return NFD_E_RANGE;
-    RET(check_heads(n_heads, states->n_heads));
+    RET(check_heads(n_heads, states->n_heads, B));
     const long long unit = 16 / (long long)type_size(dtype), most = 1LL << 40;
     const long long st[3] = {states->seq_stride, states->key_stride, states->head_stride};
     for (long long s : st)

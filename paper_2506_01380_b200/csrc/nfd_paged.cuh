@@ -1,6 +1,7 @@
 // Batches of sequences, paged caches and encoder states as kernels see them: where a row belongs, where a token lies, the
 // 4-bit numbers.  Everything that comes from device memory (row starts, lengths, page numbers) is clamped here.
 #pragma once
+#include <atomic>
 #include "nfd_common.cuh"
 
 #define NFD_MAX_TOKENS (1 << 30)
@@ -78,6 +79,28 @@ __device__ __forceinline__ uint32_t kv4_pair(uint32_t codes, int i, uint32_t z2,
 }
 __device__ __forceinline__ uint32_t kv4_z2(uint32_t w0, uint32_t w1) { return (w0 & 15u) | (w1 & 15u) << 16 | 0x43004300u; }
 __device__ __forceinline__ uint32_t kv4_step2(uint32_t w0, uint32_t w1) { return (w0 & 0xFFF0u) | (w1 & 0xFFF0u) << 16; }
+
+// The same for the operands of products, scaled by 2^-32 (KV4_UP undoes it in fp32): a code in the low bits of a bf16 is the subnormal number
+// n 2^-133, and one fma with step 2^101 and -z step 2^-32 makes (n - z) step 2^-32 of it, exactly for steps from 2^-94 on: two instructions and a
+// shift for two numbers, where kv4_pair takes three.  Steps of 2^27 and more (numbers beyond 10^8) count as not finite here.
+#define KV4_UP 4294967296.0f
+__device__ __forceinline__ bool kv4_not_finite(uint32_t word) { return (word & 0x7F80u) >= 0x4D00u; }
+struct Kv4Scale {
+    uint32_t step2, zero2;
+    __device__ __forceinline__ Kv4Scale(uint32_t w0, uint32_t w1) {
+        auto up = [](uint32_t w) { return kv4_not_finite(w) ? 0x7FC0u : (w & 0xFFF0u) + (101u << 7); };
+        step2 = up(w0) | up(w1) << 16;
+        const uint32_t z = (w0 & 15u) | (w1 & 15u) << 16;
+        const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&z), *reinterpret_cast<const __nv_bfloat162 *>(&step2));
+        zero2 = *reinterpret_cast<const uint32_t *>(&p) ^ 0x80008000u;
+    }
+    __device__ __forceinline__ uint32_t pair(uint32_t codes, int i) const {
+        const uint32_t t = codes >> (4 * i) & 0x000F000Fu;
+        const __nv_bfloat162 a = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&t), *reinterpret_cast<const __nv_bfloat162 *>(&step2),
+                                         *reinterpret_cast<const __nv_bfloat162 *>(&zero2));
+        return *reinterpret_cast<const uint32_t *>(&a);
+    }
+};
 
 // ---- which keys a row sees ----------------------------------------------------------------------------------
 struct KeyRange {

@@ -319,6 +319,14 @@ def test_kv4_lengths_around_the_tiles(length):
     _check_kv4([min(length, 40)], [length], 2, 1, 64, 64, 17, 1, 1 << 30, seed=length, uniform=True)
 
 
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("rows,length,frame", [(1, 13000, 1), (12, 13000, 1), (30, 5000, 7), (60, 3000, 1), (150, 3000, 1), (336, 3100, 336),
+                                               (500, 3100, 100)])
+def test_kv4_few_units_in_many_pieces(rows, length, frame, dh):
+    """One sequence, one or two heads: the keys are split over clusters of two to sixteen CTAs."""
+    _check_kv4([rows], [length], 2, 1 + rows % 2, dh, 64, length // 64 + 1, frame, 1 << 20, seed=rows)
+
+
 @pytest.mark.parametrize("scale", [0.0, 30.0])
 def test_kv4_flat_and_peaked_rows(scale):
     _check_kv4([1, 1], [900, 513], 4, 1, 64, 64, 16, 1, 1 << 30, scale=scale)
@@ -409,6 +417,35 @@ def test_kv4_values_that_are_not_finite(rows, dh):
         first = t - (length - rows)                                    # the first row that sees it
         o, a = out.view(n, 2, dh), again.view(n, 2, dh)
         assert a[first:, 1].isnan().all() and torch.equal(a[:first], o[:first]) and torch.equal(a[:, 0], o[:, 0])
+
+
+@pytest.mark.parametrize("rows", [1, 150])
+def test_kv4_large_and_small_numbers(rows):
+    """Steps up to 2^26 and down to 2^-94 in K and in V; from 2^27 on a step counts as not finite."""
+    torch, N = _mods()
+    rng = np.random.default_rng(11)
+    t = lambda a: torch.as_tensor(a.view(np.int16) if a.dtype == np.uint16 else a).cuda()
+    for power in (26, -94, 5, -40):
+        x = rng.integers(0, 16, (4, 1, 64, 64)).astype(np.float32) - 7
+        x[..., 0::32], x[..., 1::32] = -7, 8                           # (the whole range: the step is 1 and every number a code)
+        (kb, kw), (vb, vw) = P.kv4_bytes(*P.kv4_quantise(x)), P.kv4_bytes(*P.kv4_quantise(x[::-1].copy()))
+        vw = ((vw & 15) | ((127 + power) << 7)).astype(np.uint16)      # V's steps: 2^power; K's: in the first group
+        kw = np.where(np.arange(2) == 0, (kw & 15) | ((127 + power) << 7), kw).astype(np.uint16)
+        b, n = _batch([rows], [256], np.arange(4, dtype=np.int32)[None])
+        q = rng.standard_normal((n, 1, 64)).astype(np.float32)
+        q[..., :32] *= 2.0 ** -power
+        q = _np(torch.as_tensor(q).bfloat16())
+        out = torch.zeros(n, 64, device="cuda", dtype=torch.bfloat16)
+        run = lambda: N.attention_kv4(N.Pages(t(kb), t(vb), t(kw), t(vw)), b, torch.as_tensor(q).cuda().bfloat16(), out)
+        run()
+        want, mag = P.attention_kv4(q, dict(rows=[rows], lens=[256]), np.arange(4)[None], (kb, kw, vb, vw), 1, 1 << 30, 1)
+        k1, half = P.kv4_values(kb, kw), (slice(0, 32), slice(32, 64))
+        smax = sum(np.linalg.norm(q[..., h], axis=-1).max() * np.linalg.norm(k1[..., h], axis=-1).max() for h in half) / 8
+        s = 2.0 ** -power
+        _within(_np(out).astype(np.float64).reshape(n, 1, 64) * s, want * s, mag * s, smax, 256)
+    vw[0, 0, 0, 1] = (127 + 27) << 7                                   # token 0, which every row sees
+    run()
+    assert out.isnan().all()
 
 
 def test_kv4_offsets_beyond_32_bits():

@@ -98,7 +98,9 @@ def test_kv4_attention_refuses():
     for code, kw in [(NULLPTR, dict(q=None)), (NULLPTR, dict(out=None)), (ALIGN, dict(q=A + 2)), (ALIGN, dict(out=A + 8)),
                      (ALIGN, dict(qs=260)), (RANGE, dict(qs=128)), (RANGE, dict(heads=3)), (RANGE, dict(heads=0)),
                      (RANGE, dict(heads=2048)), (RANGE, dict(frame=0)), (RANGE, dict(frame=(1 << 20) + 1)), (RANGE, dict(window=-1)),
-                     (BADCFG, dict(pages=_pages(dtype=1)))]:
+                     (BADCFG, dict(pages=_pages(dtype=1))),
+                     (RANGE, dict(batch=_batch(n_rows=1 << 21, max_rows=1 << 20))),
+                     (RANGE, dict(batch=_batch(n_rows=1 << 30, max_rows=1 << 30)))]:
         assert kv4(**kw) == code, (code, kw)
 
 
@@ -111,7 +113,7 @@ def test_cross_attention_refuses():
                      (RANGE, dict(states=_states(key_stride=-128))), (ALIGN, dict(states=_states(key_stride=132))),
                      (ALIGN, dict(states=_states(seq_stride=1020))), (ALIGN, dict(states=_states(k=A + 8))),
                      (NULLPTR, dict(q=None)), (NULLPTR, dict(out=None)), (ALIGN, dict(q=A + 2)), (RANGE, dict(qs=128)),
-                     (RANGE, dict(heads=3))]:
+                     (RANGE, dict(heads=3)), (RANGE, dict(batch=_batch(n_rows=1 << 30, max_rows=1 << 30)))]:
         assert cross(**kw) == code, (code, kw)
 
 
