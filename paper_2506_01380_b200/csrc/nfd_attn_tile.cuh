@@ -7,7 +7,7 @@
 // its own.  Per job
 //     S = Q K^T     UMMA 128 x KB x DH, operands in shared memory, accumulator in tensor memory
 //     P = exp2(S c - m)   one thread per row: S by columns to registers, exponentials, P as bf16 over the S it came from
-//     O += P V      UMMA 128 x 64 x KB, P from tensor memory, V as it lies (MN-major)
+//     O += P V      UMMA 128 x head_dim x KB, P from tensor memory, V as it lies (MN-major)
 // m is the largest of the first 16 scores of the group's first block, and no other maximum is taken: a probability is exact to the
 // same number of bits whatever its size.  Where a block's sum of a row passes 2^60 after all (or is NaN), or a row has no m yet, the warp
 // takes the block again, S being untouched so far: maxima first, and where one has risen by more than 8 (a factor of 256) it becomes m and
@@ -478,8 +478,9 @@ __device__ __forceinline__ void tile_mma_ts(uint32_t d, uint32_t a, uint32_t b, 
 template <int DH> static __device__ __forceinline__ bool tile_issue(const TileBars &bars, uint32_t base, uint32_t tmem, int jobs, int G, bool one) {
     using C = TileCfg<DH>;
     constexpr int KB = C::KB, SUB = C::SUB, NB = C::NB, NST = C::NST;
-    constexpr uint32_t idesc_s = umma_idesc_bf16(128, KB), idesc_pv = umma_idesc_bf16(128, 64) | (1u << 16);       // V: MN-major
-    const uint32_t dQ = (base + C::AT_Q) >> 4, dK = (base + C::AT_K) >> 4, dV = (base + C::AT_V) >> 4;
+    constexpr uint32_t idesc_s = umma_idesc_bf16(128, KB), idesc_pv = umma_idesc_bf16(128, DH) | (1u << 16);       // V: MN-major
+    // (a cluster's addresses hold the CTA's rank above bit 23; V's other 64 dims are KB rows on: the leading offset)
+    const uint32_t at = base & 0x3ffffu, dQ = (at + C::AT_Q) >> 4, dK = (at + C::AT_K) >> 4, dV = (at + C::AT_V) >> 4 | (KB * 128 >> 4) << 16;
     bool ok = tile_wait(bars.q_full(), 0);
     // S is issued NB jobs ahead of P V, right behind the P V that reads the accumulator's last P: the tensor pipe takes one
     // thread's instructions in order
@@ -508,13 +509,10 @@ template <int DH> static __device__ __forceinline__ bool tile_issue(const TileBa
         ok = ok && tile_wait(bars.p_full(ip), par);
         if (!ok) break;
         tc_fence_after();
+        const uint32_t d = tmem + C::TM_O + g * 64 * SUB, a = tmem + ip * KB, v = dV + vs * (C::BLK >> 4);
+        tile_mma_ts(d, a, v, idesc_pv, n != 0);
 #pragma unroll
-        for (int sub = 0; sub < SUB; ++sub) {
-            const uint32_t d = tmem + C::TM_O + g * 64 * SUB + 64 * sub, a = tmem + ip * KB, v = dV + vs * (C::BLK >> 4) + sub * (KB * 128 >> 4);
-            tile_mma_ts(d, a, v, idesc_pv, n != 0);
-#pragma unroll
-            for (int i = 1; i < KB / 16; ++i) tile_mma_ts(d, a + 8 * i, v + i * (2048 >> 4), idesc_pv, 1);
-        }
+        for (int i = 1; i < KB / 16; ++i) tile_mma_ts(d, a + 8 * i, v + i * (2048 >> 4), idesc_pv, 1);
         umma_commit(bars.pv_done(g, n));
         if (one || g == G - 1) {
             umma_commit(bars.v_empty(vs));
@@ -542,12 +540,6 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
     const int len = src.K.length(B, s);
     const TileBars bars = {smem_u32(smem + C::AT_BAR)};
     if (threadIdx.x == 0) bars.init(C::PW, 4 * NG), s_expired = 0;
-    if (DH == 32) {
-        // V's columns 32 .. 63 belong to nothing, and are zeros
-        for (int i = threadIdx.x; i < C::NST * KB * 4; i += TILE_THREADS)
-            *reinterpret_cast<uint4 *>(smem + C::AT_V + (i / (KB * 4)) * C::BLK + tile_at(i / 4 % KB, 4 + i % 4)) = make_uint4(0, 0, 0, 0);
-        fence_proxy_async_smem();
-    }
     const int rows = min(sr.y, B.max_rows) * A.share;
     if (r0 >= rows) return;                                 // (the whole cluster)
     __syncthreads();
