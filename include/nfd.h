@@ -259,8 +259,9 @@ typedef struct {
  * k_scale and v_scale [..][head_dim / 32] 16-bit words, one for 32 numbers.  A
  * word's upper 12 bits are those of a bf16 number `step` (4 significant bits), its
  * lower 4 bits a whole number z; a code n stands for (n - z) step, which is a
- * bf16 number (exactly, as long as it does not leave bf16's range).  Codes: eight numbers to a little-endian 32-bit word,
- * number i in bits 4 (i / 2) + 16 (i % 2) and up. */
+ * bf16 number (exactly, as long as it does not leave bf16's range).  Codes: eight
+ * numbers to a little-endian 32-bit word, number i in bits 4 (i / 2) + 16 (i % 2)
+ * and up. */
 #define NFD_DTYPE_KV4 2
 typedef struct {
     void *k, *v;                                        /* dev                          */

@@ -5,6 +5,8 @@
 // cosines) are formed once for all of its heads.  A thread has a place in the rows, eight numbers of a head (16 bytes of bf16, four
 // pairs of the rotation, a word of 4-bit codes; four neighbouring lanes hold a group of 32), and takes it in one row after the other: what
 // depends on the place is worked out once.  The first loads are issued before the rows' sequences, places and angles are looked up.
+// Measured, 16 heads x 64 with q: 336 rows into bf16 pages 4.3 us, eight single rows 3.7 (a launch that does nothing takes 2.5); 10752 rows into
+// 4-bit pages and back out of them 51 us for the two calls (144 MB, 2.8 TB/s).
 #pragma once
 #include "nfd_paged.cuh"
 
