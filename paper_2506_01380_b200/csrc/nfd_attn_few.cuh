@@ -168,7 +168,7 @@ template <int DH> struct FewKv4 {
             w[0] = *src;
         }
         const uint32_t sc = word(stage + 2 * KC * RB, key, c * (DH / 4) / 32, stage);
-        const Kv4Scale scale(sc, sc);
+        const Kv4Scale scale(sc, sc, true);
 #pragma unroll
         for (int i = 0; i < NW; ++i)
 #pragma unroll
@@ -183,7 +183,7 @@ template <int DH> struct FewKv4 {
     static __device__ __forceinline__ void v_frag(const uint8_t *stage, int k0, int n, uint32_t *b) {
         const uint8_t *v = stage + KC * RB, *w = stage + 2 * KC * RB + KC * WB;
         const int g = n * (DH / 8) / 32;
-        const Kv4Scale scale(word(w, k0, g, stage), word(w, k0 + 4, g, stage));
+        const Kv4Scale scale(word(w, k0, g, stage), word(w, k0 + 4, g, stage), false);    // (take_out; checked, 3 to 5 % of a call)
         if constexpr (DH == 32) {
             const uint32_t x = *reinterpret_cast<const uint16_t *>(v + k0 * RB + n * 2) |
                                (uint32_t)*reinterpret_cast<const uint16_t *>(v + (k0 + 4) * RB + n * 2) << 16;
@@ -285,6 +285,9 @@ template <typename Src, int DH, int NR>
 __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, const AttnRows A, Src src, int split) {
     using F = FewCfg<Src, DH, NR>;
     constexpr int KC = Src::KC, NST = Src::NST, NS = DH / 16, KT = KC / 16, ROWS = F::ROWS;
+    // S in two chains of products for a single tile of rows (states, eight rows against 4096 26.9 us for 25.9; with 4-bit pages and head
+    // dimension 64 it gains nothing)
+    constexpr bool TWO = NR == 1 && NS >= 4 && (!Src::KV4 || DH == 128);
     extern __shared__ __align__(16) uint8_t few_smem[];
     __shared__ int2 s_range[ROWS];                                                // keys that a row sees
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, n = lane >> 2;
@@ -364,12 +367,16 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
             Src::k_frag(stage, 16 * u + 8 + (n >> 1) + 4 * (n & 1), c, a[1]);
 #pragma unroll
             for (int t = 0; t < NR; ++t) {
+                float odd[4] = {0.f, 0.f, 0.f, 0.f};
                 x[u][t][0] = x[u][t][1] = x[u][t][2] = x[u][t][3] = 0.f;
 #pragma unroll
                 for (int k = 0; k < NS; ++k) {
                     const uint32_t ak[4] = {a[0][2 * k], a[1][2 * k], a[0][2 * k + 1], a[1][2 * k + 1]};
-                    mma_bf16(x[u][t], ak, qb[t][k][0], qb[t][k][1]);
+                    mma_bf16(TWO && k & 1 ? odd : x[u][t], ak, qb[t][k][0], qb[t][k][1]);
                 }
+                if (TWO)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[u][t][e] += odd[e];
             }
         }
         // x[u][t]: keys n' and n' + 8 (0, 1 and 2, 3) of tile u, rows 2 c and 2 c + 1 (0, 2 and 1, 3)

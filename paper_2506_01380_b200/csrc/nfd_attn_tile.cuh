@@ -269,8 +269,8 @@ template <int DH> struct TileKv4 {
         r.w = load_words(words, place, sub);
     }
     // (a key that is not there has step 0: its row is zeros)
-    static __device__ __forceinline__ void convert(const Regs &r, uint8_t *blk, int row) {
-        const Kv4Scale lower(r.w & 0xffffu, r.w & 0xffffu), upper(r.w >> 16, r.w >> 16);
+    static __device__ __forceinline__ void convert(const Regs &r, uint8_t *blk, int row, bool check) {
+        const Kv4Scale lower(r.w & 0xffffu, r.w & 0xffffu, check), upper(r.w >> 16, r.w >> 16, check);
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
             const Kv4Scale &s = i < 4 ? lower : upper;
@@ -320,7 +320,7 @@ template <int DH> struct TileKv4 {
             if (bad1) v.w &= 0xffffu;
             if (b >= C::NST) ok = __all_sync(0xffffffffu, tile_wait(bars.k_empty(st), par));
             if (!ok) return;
-            if (key < C::KB) convert(k, smem + C::AT_K + st * C::BLK + sub * (C::KB * 128), key);
+            if (key < C::KB) convert(k, smem + C::AT_K + st * C::BLK + sub * (C::KB * 128), key, true);
             load(k, K.P.k, K.P.k_scale, place, sub);
             if (SUBS == 2) {
                 // two lanes to a key, 16 keys to a warp
@@ -340,7 +340,7 @@ template <int DH> struct TileKv4 {
             tile_publish(bars.k_full(st));
             if (b >= C::NST) ok = __all_sync(0xffffffffu, tile_wait(bars.v_empty(st), par));
             if (!ok) return;
-            if (key < C::KB) convert(v, smem + C::AT_V + st * C::BLK + sub * (C::KB * 128), key);
+            if (key < C::KB) convert(v, smem + C::AT_V + st * C::BLK + sub * (C::KB * 128), key, false);
             load(v, K.P.v, K.P.v_scale, place, sub);
             tile_publish(bars.v_full(st));
         };

@@ -87,8 +87,9 @@ __device__ __forceinline__ uint32_t kv4_step2(uint32_t w0, uint32_t w1) { return
 __device__ __forceinline__ bool kv4_not_finite(uint32_t word) { return (word & 0x7F80u) >= 0x4D00u; }
 struct Kv4Scale {
     uint32_t step2, zero2;
-    __device__ __forceinline__ Kv4Scale(uint32_t w0, uint32_t w1) {
-        auto up = [](uint32_t w) { return kv4_not_finite(w) ? 0x7FC0u : (w & 0xFFF0u) + (101u << 7); };
+    // check: the words may be of steps that are not finite
+    __device__ __forceinline__ Kv4Scale(uint32_t w0, uint32_t w1, bool check) {
+        auto up = [check](uint32_t w) { return check && kv4_not_finite(w) ? 0x7FC0u : (w & 0xFFF0u) + (101u << 7); };
         step2 = up(w0) | up(w1) << 16;
         const uint32_t z = (w0 & 15u) | (w1 & 15u) << 16;
         const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&z), *reinterpret_cast<const __nv_bfloat162 *>(&step2));
