@@ -80,11 +80,11 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
         __syncthreads();
         const float *kt = f32_smem + C::AT_K + (t & 1) * F32_KEYS * LD, *vt = f32_smem + C::AT_V + (t & 1) * F32_KEYS * LD;
         // S: rows 4 ty + i, keys tx + 16 j
-        float x[4][4];
+        float2 xx[4][4];                                                // sums over even and odd dims
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
+            for (int j = 0; j < 4; ++j) xx[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
         for (int w = 0; w < W; ++w) {
             float4 q[4], k[4];
@@ -96,8 +96,14 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    x[i][j] = fmaf(q[i].x, k[j].x, fmaf(q[i].y, k[j].y, fmaf(q[i].z, k[j].z, fmaf(q[i].w, k[j].w, x[i][j]))));
+                    xx[i][j] = ffma2(make_float2(q[i].x, q[i].y), make_float2(k[j].x, k[j].y),
+                                     ffma2(make_float2(q[i].z, q[i].w), make_float2(k[j].z, k[j].w), xx[i][j]));
         }
+        float x[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i][j] = xx[i][j].x + xx[i][j].y;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (!sM[64 * (t & 1) + tx + 16 * j])
@@ -143,7 +149,10 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
                 for (int i = 0; i < 4; ++i) {
                     const float pu = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
 #pragma unroll
-                    for (int e = 0; e < ND; ++e) o[i][e] = fmaf(pu, v[e], o[i][e]);
+                    for (int e = 0; e < ND; e += 2) {
+                        const float2 y = ffma2(make_float2(pu, pu), make_float2(v[e], v[e + 1]), make_float2(o[i][e], o[i][e + 1]));
+                        o[i][e] = y.x, o[i][e + 1] = y.y;
+                    }
                 }
             }
         }
