@@ -238,9 +238,225 @@ static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const StateK
     }
     return NFD_OK;
 }
+// A few rows (up to 8 of a unit) to fp32 states: bound by the stream of K and V.  Each warp of a cluster's CTAs takes chunks of 1024 / DH keys in turn,
+// with a cp.async ring of its own (8 KB a chunk, two chunks ahead: 128 KB of an SM on their way), an online softmax of its own and no barrier until
+// the end.  S: a lane has a key's share of 32 dims; O: a lane has four dims and eight keys.  Rows of 16-byte words are swizzled by the key, so
+// that neither way of reading meets in a bank.  Measured, four sequences of one row, 16 heads x 64, against up to 2000 states: 14.4 us (131 MB at most, 66 on average: 4.6 TB/s), with the
+// kernel above, whose tile of 32 rows one row has to itself, 50.
+template <int DH, int R> struct F32Few {
+    static constexpr int KC = 1024 / DH, PR = DH / 4, LPK = 32 / KC, NST = 3;
+    static constexpr int QS = LPK * 36;                                 // floats of a query: 32 of each share, and 4 that nobody reads
+    static constexpr int STAGE = 2 * KC * DH * 4;
+    static constexpr int STATE = R * (DH + 2) * 4;
+    static constexpr int AT_Q = FEW_WARPS * NST * STAGE, AT_P = AT_Q + R * QS * 4, AT_T = AT_P + FEW_WARPS * R * KC * 4, SMEM = AT_T + STATE;
+    static_assert(STATE <= NST * STAGE && AT_T % 16 == 0 && SMEM <= 232448 - 1024, "shared memory of a CTA");
+};
+template <int DH, int R>
+__global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B, const AttnRows A, const StateKeys<float, DH> K, int split) {
+    using C = F32Few<DH, R>;
+    constexpr int KC = C::KC, PR = C::PR, NST = C::NST, STEP = 32 / PR;
+    extern __shared__ __align__(16) uint8_t f32_few_smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % split, h = blockIdx.x / split, s = blockIdx.y;
+    const int2 sr = B.rows(s);
+    const int nr = min(min(sr.y, B.max_rows) * A.share, R);
+    if (nr == 0) return;                                                // (the whole cluster)
+    const int hi = K.length(B, s);
+    float *ring = reinterpret_cast<float *>(f32_few_smem + warp * NST * C::STAGE), *sQ = reinterpret_cast<float *>(f32_few_smem + C::AT_Q);
+    float *sP = reinterpret_cast<float *>(f32_few_smem + C::AT_P) + warp * R * KC;
+    const unsigned char *mask = K.mask ? K.mask + (size_t)s * K.n_keys : nullptr;
+    // copies: word `lane % PR` of keys lane / PR, + STEP, ...
+    const int word = lane % PR, key0 = lane / PR, step = split * FEW_WARPS * KC;
+    const long long from = s * K.seq_stride + h * K.head_stride + word * 4;
+    int next = (rank * FEW_WARPS + warp) * KC, base = next;
+    uint32_t raw = 0, bits[2] = {0, 0};                                 // key `lane` of the chunk that is filled next; which keys of the next two chunks are there
+    auto look = [&]() {
+        const int p = next + lane;
+        raw = p < hi && lane < KC;
+        if (mask && raw) raw = mask[p];
+    };
+    auto fill = [&](int st) -> uint32_t {
+        const uint32_t there = __ballot_sync(0xffffffffu, raw != 0), dst = smem_u32(ring) + st * C::STAGE;
+        long long at = from + (long long)(next + key0) * K.key_stride;
+#pragma unroll
+        for (int i = 0; i < KC / STEP; ++i, at += STEP * K.key_stride) {
+            const int key = key0 + i * STEP;
+            const bool here = there >> key & 1;
+            const uint32_t d = dst + (key * PR + (word ^ (key & 7))) * 16;
+            cp_async16(d, here ? K.k + at : K.k, here ? 16 : 0);
+            cp_async16(d + KC * DH * 4, here ? K.v + at : K.v, here ? 16 : 0);
+        }
+        next += step;
+        look();
+        return there;
+    };
+    look();
+#pragma unroll
+    for (int i = 0; i < NST - 1; ++i) {
+        if (next < hi) bits[i] = fill(i);
+        cp_async_commit();
+    }
+    for (int i = threadIdx.x; i < R * PR; i += 32 * FEW_WARPS) {
+        const int r = i / PR, w = i % PR;
+        const int2 at = A.split(min(r, nr - 1));
+        *reinterpret_cast<float4 *>(sQ + r * C::QS + (w >> 3) * 36 + (w & 7) * 4) =
+            *reinterpret_cast<const float4 *>((const float *)A.q + (long long)(sr.x + at.x) * A.q_stride + (h * A.share + at.y) * DH + 4 * w);
+    }
+    const float cs = 1.4426950408889634f * (1.0f / sqrtf((float)DH));
+    const int key = lane % KC, part = lane / KC, g = lane / PR;
+    float o[R][4], m[R], l[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) m[r] = -INFINITY, l[r] = o[r][0] = o[r][1] = o[r][2] = o[r][3] = 0.f;
+    __syncthreads();
+    int st = 0;
+    for (; base < hi; base += step) {
+        const uint32_t there = bits[0];
+        const float *kt = ring + st * (C::STAGE / 4), *vt = kt + KC * DH;
+        bits[0] = bits[1];
+        if (next < hi) bits[1] = fill(st == 0 ? NST - 1 : st - 1);
+        if (++st == NST) st = 0;
+        cp_async_commit();
+        cp_async_wait<NST - 1>();
+        __syncwarp();
+        float2 xx[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) xx[r] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            const float4 k = *reinterpret_cast<const float4 *>(kt + (key * PR + ((part * 8 + w) ^ (key & 7))) * 4);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float4 q = *reinterpret_cast<const float4 *>(sQ + r * C::QS + part * 36 + 4 * w);
+                xx[r] = ffma2(make_float2(q.x, q.y), make_float2(k.x, k.y), ffma2(make_float2(q.z, q.w), make_float2(k.z, k.w), xx[r]));
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float x = xx[r].x + xx[r].y;
+#pragma unroll
+            for (int d = KC; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            if (!(there >> key & 1)) x = -INFINITY;
+            float mn = x;
+#pragma unroll
+            for (int d = 1; d < KC; d <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
+            mn = fmaxf(mn, m[r]);
+            const float f = mn == m[r] ? 1.0f : exp2f((m[r] - mn) * cs), p = exp2f((x - (mn == -INFINITY ? 0.f : mn)) * cs);
+            m[r] = mn, l[r] = fmaf(l[r], f, p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[r][e] *= f;
+            if (part == 0) sP[r * KC + key] = p;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            float4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float4 *>(vt + ((g * 8 + i + u) * PR + (word ^ (i + u))) * 4);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float4 p4 = *reinterpret_cast<const float4 *>(sP + r * KC + g * 8 + i);
+                const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float2 a = ffma2(make_float2(p[u], p[u]), make_float2(v[u].x, v[u].y), make_float2(o[r][0], o[r][1]));
+                    const float2 b = ffma2(make_float2(p[u], p[u]), make_float2(v[u].z, v[u].w), make_float2(o[r][2], o[r][3]));
+                    o[r][0] = a.x, o[r][1] = a.y, o[r][2] = b.x, o[r][3] = b.y;
+                }
+            }
+        }
+        __syncwarp();                                                   // the stage and sP may be written again
+    }
+    cp_async_wait<0>();
+    __syncwarp();
+    // this warp's state into its (drained) ring: O by rows, then m and l of the rows
+    float *S = ring;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int d = 1; d < KC; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+#pragma unroll
+        for (int d = PR; d < 32; d <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[r][e] += __shfl_xor_sync(0xffffffffu, o[r][e], d);
+        if (g == 0) *reinterpret_cast<float4 *>(S + r * DH + word * 4) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+        if (lane == 0) S[R * DH + 2 * r] = m[r] * cs, S[R * DH + 2 * r + 1] = l[r];
+    }
+    __syncthreads();
+    float *T = reinterpret_cast<float *>(f32_few_smem + C::AT_T);
+    auto write = [&](int r, int d, float4 v, float sum) {
+        const int2 at = A.split(r);
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        float *out = (float *)A.out + ((long long)(sr.x + at.x) * A.heads + h * A.share + at.y) * DH + d;
+        *reinterpret_cast<float4 *>(out) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    };
+    auto join = [](float4 &v, float &sum, float4 x, float2 ml, float mx) {
+        const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mx);
+        sum = fmaf(ml.y, f, sum);
+        v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+    };
+    for (int i = threadIdx.x; i < nr * PR; i += 32 * FEW_WARPS) {
+        const int r = i / PR, d = i % PR * 4;
+        float mx = -INFINITY, sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto state = [&](int w) { return reinterpret_cast<const float *>(f32_few_smem + w * NST * C::STAGE); };
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w) mx = fmaxf(mx, state(w)[R * DH + 2 * r]);
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w)
+            join(v, sum, *reinterpret_cast<const float4 *>(state(w) + r * DH + d), *reinterpret_cast<const float2 *>(state(w) + R * DH + 2 * r), mx);
+        if (split == 1) {
+            write(r, d, v, sum);
+        } else {
+            *reinterpret_cast<float4 *>(T + r * DH + d) = v;
+            if (d == 0) T[R * DH + 2 * r] = mx, T[R * DH + 2 * r + 1] = sum;
+        }
+    }
+    if (split == 1) return;
+    cluster_sync_all();
+    const uint32_t Ts = smem_u32(T);
+    for (int i = rank + split * threadIdx.x; i < nr * PR; i += split * 32 * FEW_WARPS) {
+        const int r = i / PR, d = i % PR * 4;
+        float mx = -INFINITY, sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < split; ++k) mx = fmaxf(mx, ld_cluster_f2(cluster_map(Ts + (R * DH + 2 * r) * 4, k)).x);
+        for (int k = 0; k < split; ++k)
+            join(v, sum, ld_cluster_f4(cluster_map(Ts + (r * DH + d) * 4, k)), ld_cluster_f2(cluster_map(Ts + (R * DH + 2 * r) * 4, k)), mx);
+        write(r, d, v, sum);
+    }
+    cluster_sync_all();                                                 // nobody leaves while its state is read
+}
+template <int DH, int R>
+static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, cudaStream_t st) {
+    using C = F32Few<DH, R>;
+    auto kern = k_attn_f32_few<DH, R>;
+    static std::atomic<bool> sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
+    static int fit[NFD_PAGED_DEVICES][5];
+    if (!sized[dev]) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess ||
+            cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+            return NFD_E_CUDA;
+        for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * FEW_WARPS, C::SMEM);
+        sized[dev] = true;
+    }
+    const int split = few_split((long long)kv_heads * B.n_seqs, K.n_keys, C::KC, fit[dev]);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kv_heads * split, B.n_seqs), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at, cfg.numAttrs = split > 1;
+    if (cudaLaunchKernelEx(&cfg, kern, B, A, K, split) != cudaSuccess) {
+        cudaGetLastError();
+        return NFD_E_CUDA;
+    }
+    return NFD_OK;
+}
 // 64 rows where that leaves no SM idle: twice the warps for the same tiles of keys
 template <int DH>
 static int launch_attn_f32(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
+    const long long rows = (long long)B.max_rows * A.share;
+    if (rows <= 1) return launch_attn_f32_few<DH, 1>(B, A, K, kv_heads, dev, st);
+    if (rows <= 4) return launch_attn_f32_few<DH, 4>(B, A, K, kv_heads, dev, st);
+    if (rows <= 8) return launch_attn_f32_few<DH, 8>(B, A, K, kv_heads, dev, st);
     if ((((long long)B.max_rows * A.share + 63) / 64) * kv_heads * B.n_seqs >= n_sm) return launch_attn_f32_rows<DH, 64>(B, A, K, kv_heads, dev, n_sm, st);
     return launch_attn_f32_rows<DH, 32>(B, A, K, kv_heads, dev, n_sm, st);
 }
