@@ -1,12 +1,13 @@
 // Attention of a batch's rows to fp32 encoder states, on the fp32 pipes.
 //
-// A CTA takes 32 or 64 rows (rows x heads that share a head of keys) of a sequence and walks its keys in tiles of 64, the next tile's copies in
+// k_attn_f32: a CTA takes 32 or 64 rows (rows x heads that share a head of keys) of a sequence and walks its keys in tiles of 64, the next tile's copies in
 // flight: S = Q K^T with 4 rows x 4 keys to a thread, an online softmax per row over the 16 lanes that hold it, P through shared memory
 // (a row's 16 lanes write and read it, no barrier), O += P V with 4 rows x DH / 16 dims to a thread.  All operands are read as 16-byte words
 // along their rows, rows are padded by one word so that no two lanes of a quarter warp meet in a bank: 64 FMAs for eight words either way, which keeps
 // the FMA pipe ahead of the shared-memory port.  Keys that are not seen are copied as zeros and take a score of -inf.
 // Few units with many keys are split over the CTAs of a cluster and merged through distributed shared memory.
-// Bound by FMAs for many rows, by the chain of a tile (copy, S, softmax, P V) for few.
+// Bound by FMAs for many rows, by the chain of a tile (copy, S, softmax, P V) for few, which k_attn_f32_few takes.  Measured: four sequences of 1344
+// rows, 16 heads x 64, against up to 1000 states 665 us (33 TFLOP/s of 72); three of 77 rows, 6 heads x 32, against up to 220, 6.9 us.
 #pragma once
 #include "nfd_attn_few.cuh"
 
@@ -238,7 +239,7 @@ static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const StateK
     }
     return NFD_OK;
 }
-// A few rows (up to 8 of a unit) to fp32 states: bound by the stream of K and V.  Each warp of a cluster's CTAs takes chunks of 1024 / DH keys in turn,
+// A few rows (8 of a unit to a cluster) to fp32 states: bound by the stream of K and V.  Each warp of a cluster's CTAs takes chunks of 1024 / DH keys in turn,
 // with a cp.async ring of its own (8 KB a chunk, two chunks ahead: 128 KB of an SM on their way), an online softmax of its own and no barrier until
 // the end.  S: a lane has a key's share of 32 dims; O: a lane has four dims and eight keys.  Rows of 16-byte words are swizzled by the key, so
 // that neither way of reading meets in a bank.  Measured, four sequences of one row, 16 heads x 64, against up to 2000 states: 14.4 us (131 MB at most, 66 on average: 4.6 TB/s), with the
@@ -259,8 +260,8 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B,
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % split, h = blockIdx.x / split, s = blockIdx.y;
     const int2 sr = B.rows(s);
-    const int nr = min(min(sr.y, B.max_rows) * A.share, R);
-    if (nr == 0) return;                                                // (the whole cluster)
+    const int r0 = blockIdx.z * R, nr = min(min(sr.y, B.max_rows) * A.share - r0, R);
+    if (nr <= 0) return;                                                // (the whole cluster)
     const int hi = K.length(B, s);
     float *ring = reinterpret_cast<float *>(f32_few_smem + warp * NST * C::STAGE), *sQ = reinterpret_cast<float *>(f32_few_smem + C::AT_Q);
     float *sP = reinterpret_cast<float *>(f32_few_smem + C::AT_P) + warp * R * KC;
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B,
     }
     for (int i = threadIdx.x; i < R * PR; i += 32 * FEW_WARPS) {
         const int r = i / PR, w = i % PR;
-        const int2 at = A.split(min(r, nr - 1));
+        const int2 at = A.split(r0 + min(r, nr - 1));
         *reinterpret_cast<float4 *>(sQ + r * C::QS + (w >> 3) * 36 + (w & 7) * 4) =
             *reinterpret_cast<const float4 *>((const float *)A.q + (long long)(sr.x + at.x) * A.q_stride + (h * A.share + at.y) * DH + 4 * w);
     }
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B,
     __syncthreads();
     float *T = reinterpret_cast<float *>(f32_few_smem + C::AT_T);
     auto write = [&](int r, int d, float4 v, float sum) {
-        const int2 at = A.split(r);
+        const int2 at = A.split(r0 + r);
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
         float *out = (float *)A.out + ((long long)(sr.x + at.x) * A.heads + h * A.share + at.y) * DH + d;
         *reinterpret_cast<float4 *>(out) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
@@ -438,9 +439,10 @@ static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const StateKe
         for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * FEW_WARPS, C::SMEM);
         sized[dev] = true;
     }
-    const int split = few_split((long long)kv_heads * B.n_seqs, K.n_keys, C::KC, fit[dev]);
+    const int tiles = (int)(((long long)B.max_rows * A.share + R - 1) / R);
+    const int split = few_split((long long)kv_heads * B.n_seqs * tiles, K.n_keys, C::KC, fit[dev]);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kv_heads * split, B.n_seqs), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
+    cfg.gridDim = dim3(kv_heads * split, B.n_seqs, tiles), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at, cfg.numAttrs = split > 1;
@@ -450,13 +452,17 @@ static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const StateKe
     }
     return NFD_OK;
 }
+// Rows of a unit that the kernel for few takes, eight at a time, each reading the keys.  us there and in tiles of 32 rows: four sequences, 16 heads x
+// 64, up to 2000 states, 8, 16 and 24 rows 25.7, 41.5, 79.7 and 51.0, 50.8, 50.7; 64 sequences, up to 512 states, 95.6, 182, 266 and 242, 242,
+// 241; head dimension 128, 32 sequences, 8 heads, up to 600, 16 and 32 rows 88, 154 and 183, 183.
+constexpr int f32_few_most(int dh) { return dh == 128 ? 32 : 16; }
 // 64 rows where that leaves no SM idle: twice the warps for the same tiles of keys
 template <int DH>
 static int launch_attn_f32(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
     const long long rows = (long long)B.max_rows * A.share;
     if (rows <= 1) return launch_attn_f32_few<DH, 1>(B, A, K, kv_heads, dev, st);
     if (rows <= 4) return launch_attn_f32_few<DH, 4>(B, A, K, kv_heads, dev, st);
-    if (rows <= 8) return launch_attn_f32_few<DH, 8>(B, A, K, kv_heads, dev, st);
+    if (rows <= f32_few_most(DH)) return launch_attn_f32_few<DH, 8>(B, A, K, kv_heads, dev, st);
     if ((((long long)B.max_rows * A.share + 63) / 64) * kv_heads * B.n_seqs >= n_sm) return launch_attn_f32_rows<DH, 64>(B, A, K, kv_heads, dev, n_sm, st);
     return launch_attn_f32_rows<DH, 32>(B, A, K, kv_heads, dev, n_sm, st);
 }

@@ -541,9 +541,9 @@ def test_cross_several_tiles_to_a_cta(rows, dh):
 
 @pytest.mark.parametrize("tdt", ["bfloat16", "float32"])
 @pytest.mark.parametrize("dh", [32, 64, 128])
-@pytest.mark.parametrize("rows,share", [(1, 1), (2, 1), (1, 4), (3, 2), (1, 8), (2, 4)])
+@pytest.mark.parametrize("rows,share", [(1, 1), (2, 1), (1, 4), (3, 2), (1, 8), (2, 4), (9, 1), (13, 1), (8, 4)])
 def test_cross_few_rows(rows, share, dh, tdt):
-    """Up to eight rows of a unit, ragged, masked; many keys in the pieces of a cluster, keys that end inside a chunk."""
+    """A few rows of a unit, ragged, masked; many keys in the pieces of a cluster, keys that end inside a chunk."""
     torch, _ = _mods()
     dt = getattr(torch, tdt)
     _check_cross(dt, [rows, 1, 0, rows], [1000, 7, 33, 0], 2 * share, share, dh, 1000, True, seed=rows)
