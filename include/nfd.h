@@ -240,7 +240,8 @@ int nfd_attention_noalloc(const void *q, const void *k_pages, const void *v_page
 /* Which rows belong to which sequence.  Sequence s has the rows row_start[s] ..
  * row_start[s+1]-1 of the row buffers, at most max_rows of them (rows past
  * max_rows in a sequence, and rows behind the last sequence, are left alone), or,
- * with row_start NULL, max_rows rows each (n_rows == n_seqs * max_rows).
+ * with row_start NULL, max_rows rows each (n_rows == n_seqs * max_rows).  With
+ * n_rows 0 a call does nothing, and row buffers may be NULL.
  * With a paged cache kv_len[s] counts the sequence's tokens with its rows in it:
  * row i of n is token kv_len[s] - n + i.  Token p lies in page
  * table[s * table_len + (p / page_tokens) % table_len]: a table that is shorter

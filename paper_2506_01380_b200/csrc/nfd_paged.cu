@@ -61,9 +61,9 @@ int check_pages(const nfd_pages *p, PagesD &P) {
     return NFD_OK;
 }
 
-// rows of `heads` heads, `stride` elements apart, read in 16-byte words
-int check_rows(const void *p, long long stride, int heads, int head_dim, int dtype) {
-    if (!p) return NFD_E_NULLPTR;
+// rows of `heads` heads, `stride` elements apart, read in 16-byte words; where there are no rows they may be nowhere
+int check_rows(const BatchD &B, const void *p, long long stride, int heads, int head_dim, int dtype) {
+    if (!p && B.n_rows) return NFD_E_NULLPTR;
     if (!aligned(p, 16) || (stride * (long long)type_size(dtype)) % 16) return NFD_E_ALIGN;
     if (stride < (long long)heads * head_dim || stride > (1LL << 40)) return NFD_E_RANGE;
     return NFD_OK;
@@ -107,12 +107,12 @@ int nfd_kv_append(const nfd_pages *pages, const nfd_batch *batch, const nfd_rope
     if (dtype != NFD_DTYPE_FP32 && dtype != NFD_DTYPE_BF16) return NFD_E_BADCFG;
     if (pages->dtype != dtype && pages->dtype != NFD_DTYPE_KV4) return NFD_E_BADCFG;
     const int dh = pages->head_dim;
-    RET(check_rows(k, k_stride, P.heads, dh, dtype));
-    RET(check_rows(v, v_stride, P.heads, dh, dtype));
+    RET(check_rows(B, k, k_stride, P.heads, dh, dtype));
+    RET(check_rows(B, v, v_stride, P.heads, dh, dtype));
     if (n_q_heads < 0 || n_q_heads > 1024) return NFD_E_RANGE;
     if (n_q_heads) {
-        RET(check_rows(q, q_stride, n_q_heads, dh, dtype));
-        if (!q_out) return NFD_E_NULLPTR;
+        RET(check_rows(B, q, q_stride, n_q_heads, dh, dtype));
+        if (!q_out && B.n_rows) return NFD_E_NULLPTR;
         if (!aligned(q_out, 16)) return NFD_E_ALIGN;
     }
     RopeD R;
@@ -198,8 +198,8 @@ int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_head
     RET(check_batch(batch, true, B));
     if (pages->dtype != NFD_DTYPE_KV4) return NFD_E_BADCFG;
     RET(check_heads(n_heads, P.heads, B));
-    RET(check_rows(q, q_stride, n_heads, pages->head_dim, NFD_DTYPE_BF16));
-    if (!out) return NFD_E_NULLPTR;
+    RET(check_rows(B, q, q_stride, n_heads, pages->head_dim, NFD_DTYPE_BF16));
+    if (!out && B.n_rows) return NFD_E_NULLPTR;
     if (!aligned(out, 16)) return NFD_E_ALIGN;
     if (frame_tokens < 1 || frame_tokens > (1 << 20) || window < 0) return NFD_E_RANGE;
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
@@ -236,8 +236,8 @@ int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_
     for (long long s : st)
         if (s % unit) return NFD_E_ALIGN;
     if (!aligned(states->k, 16) || !aligned(states->v, 16)) return NFD_E_ALIGN;
-    RET(check_rows(q, q_stride, n_heads, dh, dtype));
-    if (!out) return NFD_E_NULLPTR;
+    RET(check_rows(B, q, q_stride, n_heads, dh, dtype));
+    if (!out && B.n_rows) return NFD_E_NULLPTR;
     if (!aligned(out, 16)) return NFD_E_ALIGN;
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
     const AttnRows A = {q, out, q_stride, n_heads, n_heads / states->n_heads};

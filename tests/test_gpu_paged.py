@@ -448,6 +448,20 @@ def test_kv4_large_and_small_numbers(rows):
     assert out.isnan().all()
 
 
+def test_a_step_without_rows():
+    """A batch of no rows: empty tensors, which have no address."""
+    torch, N = _mods()
+    new = lambda *sh: torch.zeros(sh, device="cuda", dtype=torch.bfloat16)
+    b = N.Batch(0, torch.tensor([5, 9], device="cuda", dtype=torch.int32), torch.zeros(2, 1, device="cuda", dtype=torch.int32))
+    pages = N.Pages.empty("kv4", 1, 2, 16, 64)
+    N.kv_append(pages, b, new(0, 2, 64), new(0, 2, 64), N.Rope(64, 0, 0), new(0, 4, 64), new(0, 4, 64))
+    N.pages_read(pages, b, new(0, 2, 64), new(0, 2, 64))
+    assert N.attention_kv4(pages, b, new(0, 4, 64), new(0, 256)).numel() == 0
+    assert N.cross_attention(N.States(new(2, 7, 2, 64), new(2, 7, 2, 64)), b, new(0, 4, 64), new(0, 256)).numel() == 0
+    torch.cuda.synchronize()
+    assert not pages.k.any() and not pages.v_scale.any()
+
+
 def test_kv4_offsets_beyond_32_bits():
     """A cache of more than 2^32 bytes of codes, with the sequence's pages at its end."""
     torch, N = _mods()

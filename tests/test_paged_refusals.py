@@ -124,6 +124,15 @@ def test_calls_without_rows_do_nothing():
     assert read(k=None, v=None) == 0
 
 
+def test_calls_without_rows_need_no_buffers():
+    none = _batch(n_rows=0, max_rows=0)
+    assert append(batch=none, k=None, v=None, q=None, q_out=None) == 0
+    assert read(batch=none, k=None, v=None) == 0
+    assert kv4(batch=none, q=None, out=None) == 0
+    assert cross(batch=none, q=None, out=None) == 0
+    assert kv4(batch=none, q=A + 2) == ALIGN and append(batch=none, ks=100) == ALIGN
+
+
 def test_structs_match_header():
     import os
     import re
