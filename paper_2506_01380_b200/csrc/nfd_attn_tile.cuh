@@ -22,8 +22,8 @@
 //
 // Bound by the special-function unit and the issue slots beside it (4-bit pages: the producers' conversions; a fifth of the exponentials by a
 // polynomial on the FMA pipe made 202 us 207), with head dimension 128 by the two warps a scheduler has for the chain S - P - P V.
-// Measured, 16 heads x 64: 336 rows behind 5712 tokens in 4-bit pages 28.7 us (273 TFLOP/s: the beginning, 18 blocks, the merge), eight
-// streams of 336 rows behind 11088 203 us (601 TFLOP/s); 16 heads on 4 x 128, eight batches of 1344 rows against up to 2048 states 126 us
+// Measured, 16 heads x 64: 336 rows behind 5712 tokens in 4-bit pages 28.5 us (276 TFLOP/s: the beginning, 18 blocks, the merge), eight
+// streams of 336 rows behind 11088 202 us (604 TFLOP/s); 16 heads on 4 x 128, eight batches of 1344 rows against up to 2048 states 126 us
 // (620 TFLOP/s).
 #pragma once
 #include "nfd_attn_few.cuh"

@@ -728,6 +728,46 @@ def test_captured_and_overlapping_calls():
         assert all(torch.equal(a, b) for a, b in zip(c[2], f)), c[0]
 
 
+FIRST_CALLS = """
+import torch
+from paper_2506_01380_b200 import nfd as N
+i32 = lambda *x: torch.tensor(x, device="cuda", dtype=torch.int32)
+runs, outs = [], []
+for rows in (1, 140):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    new = lambda *sh, dt=torch.bfloat16: torch.randn(sh, device="cuda", generator=g).to(dt)
+    pages, b = N.Pages.empty("kv4", 9, 2, 64, 64), N.Batch(rows, i32(500), torch.arange(9, device="cuda", dtype=torch.int32)[None])
+    k, v, q, o = new(rows, 2, 64), new(rows, 2, 64), new(rows, 4, 64), new(rows, 256)
+    qr = torch.empty_like(q)
+    runs.append(lambda pages=pages, b=b, k=k, v=v, q=q, qr=qr: N.kv_append(pages, b, k, v, N.Rope(64, 0, 0), q, qr))
+    runs.append(lambda pages=pages, b=b, q=qr, o=o: N.attention_kv4(pages, b, q, o))
+    outs.append(o)
+    for dt in (torch.bfloat16, torch.float32):
+        st, qc, oc = N.States(new(1, 700, 2, 64, dt=dt), new(1, 700, 2, 64, dt=dt)), new(rows, 4, 64, dt=dt), new(rows, 256, dt=dt)
+        runs.append(lambda st=st, b=N.Batch(rows, n_seqs=1), qc=qc, oc=oc: N.cross_attention(st, b, qc, oc))
+        outs.append(oc)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    for run in runs:
+        run()
+graph.replay()
+first = [o.clone() for o in outs]
+for run in runs:
+    run()
+assert all(torch.equal(a, o) for a, o in zip(first, outs))
+print("same")
+"""
+
+
+def test_first_calls_may_be_captured():
+    """In a process of its own: nothing has run before the capture."""
+    import subprocess
+    import sys
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=240)
+    assert done.returncode == 0 and done.stdout.strip() == "same", done.stderr[-2000:]
+
+
 def test_lengths_are_read_when_the_call_runs():
     """A captured call, replayed after kv_len, the table and row_start have changed, is the call with the new values."""
     torch, N = _mods()
