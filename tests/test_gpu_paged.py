@@ -440,7 +440,9 @@ def test_kv4_large_and_small_numbers(rows):
         run()
         want, mag = P.attention_kv4(q, dict(rows=[rows], lens=[256]), np.arange(4)[None], (kb, kw, vb, vw), 1, 1 << 30, 1)
         k1, half = P.kv4_values(kb, kw), (slice(0, 32), slice(32, 64))
-        smax = sum(np.linalg.norm(q[..., h], axis=-1).max() * np.linalg.norm(k1[..., h], axis=-1).max() for h in half) / 8
+        norm = lambda x: np.linalg.norm(x.astype(np.float64), axis=-1).max()
+        smax = sum(norm(q[..., h]) * norm(k1[..., h]) for h in half) / 8
+        assert smax < 1e5
         s = 2.0 ** -power
         _within(_np(out).astype(np.float64).reshape(n, 1, 64) * s, want * s, mag * s, smax, 256)
     vw[0, 0, 0, 1] = (127 + 27) << 7                                   # token 0, which every row sees
