@@ -3,6 +3,7 @@
 #pragma once
 #include <atomic>
 #include "nfd_common.cuh"
+#include "nfd_paged_plan.h"
 
 #define NFD_MAX_TOKENS (1 << 30)
 #define NFD_PAGED_DEVICES 64
@@ -13,8 +14,8 @@ struct BatchD {
     // first row and number of rows of sequence s (of which the first max_rows are computed)
     __device__ __forceinline__ int2 rows(int s) const {
         if (!row_start) return make_int2(s * max_rows, max_rows);
-        const int a = min(max(__ldg(row_start + s), 0), n_rows), b = min(__ldg(row_start + s + 1), n_rows);
-        return make_int2(a, max(b - a, 0));
+        const RowSpan r = rows_between(__ldg(row_start + s), __ldg(row_start + s + 1), n_rows);
+        return make_int2(r.first, r.n);
     }
     // the sequence of a row, for a whole warp: as many as end at or before it
     __device__ __forceinline__ int seq_of(int row) const {
