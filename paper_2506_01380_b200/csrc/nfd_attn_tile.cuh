@@ -226,7 +226,8 @@ template <int DH> struct TileStates {
                     if (lane == 0) M[0] = m, M[4] = 0, mbar_arrive(bars.m_full(b % C::NM));
                 }
                 // (the first block is wanted at once)
-                if (++item - done > (item < 2 * FLY ? 2 : FLY)) {
+                ++item;
+                if (item - done > (item < 2 * FLY ? 2 : FLY)) {
                     cp_async_wait_upto(item - done - 1);
                     publish();
                 }
