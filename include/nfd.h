@@ -337,7 +337,9 @@ typedef struct {
 /* Cross attention: every row of a sequence sees the first kv_len[s] (at most
  * n_keys) states of its sequence, but for masked ones.  q, out, n_heads, scale and
  * rows that see nothing as in nfd_attention_kv4; q and out of the states' type.
- * fp32 is computed on the fp32 pipes. */
+ * fp32 is computed on the fp32 pipes.  Values may be as large as their type goes: a
+ * result, being a mean of them, is finite with them.  (Small ones: with up to 2^20
+ * states, values below 2^-80 may lose bits in the sums.) */
 int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_heads, const void *q,
                         long long q_stride, void *out, void *cuda_stream);
 

@@ -5,6 +5,7 @@
 // (a row's 16 lanes write and read it, no barrier), O += P V with 4 rows x DH / 16 dims to a thread.  All operands are read as 16-byte words
 // along their rows, rows are padded by one word so that no two lanes of a quarter warp meet in a bank: 64 FMAs for eight words either way, which keeps
 // the FMA pipe ahead of the shared-memory port.  Keys that are not seen are copied as zeros and take a score of -inf.
+// Probabilities are scaled down by a power of two (sum_bits), which no result shows but those whose sums would have left fp32.
 // Few units with many keys are split over the CTAs of a cluster and merged through distributed shared memory.
 // Bound by FMAs for many rows, by the chain of a tile (copy, S, softmax, P V) for few, which k_attn_f32_few takes.  Measured: four sequences of 1344
 // rows, 16 heads x 64, against up to 1000 states 665 us (33 TFLOP/s of 72); three of 77 rows, 6 heads x 32, against up to 220, 6.9 us.
@@ -64,6 +65,7 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
     cp_async_commit();
     if (t0 < t1) fill(t0);
     const float cs = 1.4426950408889634f * (1.0f / sqrtf((float)DH));
+    const float scale = exp2f(-K.down(1, 1));                           // of probabilities; exact (1: for the roundings of the sums)
     float o[4][ND], m[4], l[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -122,7 +124,7 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
             for (int e = 0; e < ND; ++e) o[i][e] *= f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float p = exp2f((x[i][j] - mc) * cs);
+                const float p = exp2f((x[i][j] - mc) * cs) * scale;
                 l[i] += p, sP[(4 * ty + i) * LP + tx + 16 * j] = p;
             }
         }
@@ -304,6 +306,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B,
             *reinterpret_cast<const float4 *>((const float *)A.q + (long long)(sr.x + at.x) * A.q_stride + (h * A.share + at.y) * DH + 4 * w);
     }
     const float cs = 1.4426950408889634f * (1.0f / sqrtf((float)DH));
+    const float scale = exp2f(-K.down(1, 1));                           // as above
     const int key = lane % KC, part = lane / KC, g = lane / PR;
     float o[R][4], m[R], l[R];
 #pragma unroll
@@ -341,7 +344,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B,
 #pragma unroll
             for (int d = 1; d < KC; d <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
             mn = fmaxf(mn, m[r]);
-            const float f = mn == m[r] ? 1.0f : exp2f((m[r] - mn) * cs), p = exp2f((x - (mn == -INFINITY ? 0.f : mn)) * cs);
+            const float f = mn == m[r] ? 1.0f : exp2f((m[r] - mn) * cs), p = exp2f((x - (mn == -INFINITY ? 0.f : mn)) * cs) * scale;
             m[r] = mn, l[r] = fmaf(l[r], f, p);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[r][e] *= f;

@@ -334,6 +334,8 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
         }
     }
     const float cs = 1.4426950408889634f * rsqrtf((float)DH) * Src::UP;
+    float down = 0.f;                                                             // (probabilities grow to 2^8 before m follows)
+    if constexpr (!Src::KV4) down = src.K.down(8, 1);
     // this lane's rows: 2 c and 2 c + 1 of every tile of 8
     float o[NR][NS][4], m[NR][2], l[NR][2];
 #pragma unroll
@@ -426,7 +428,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
         uint32_t p[KT][NR][2];                                                    // P^T: keys 2 c.., row n
 #pragma unroll
         for (int t = 0; t < NR; ++t) {
-            const float m0 = m[t][0] == -INFINITY ? 0.f : m[t][0] * cs, m1 = m[t][1] == -INFINITY ? 0.f : m[t][1] * cs;
+            const float m0 = m[t][0] == -INFINITY ? 0.f : fmaf(m[t][0], cs, down), m1 = m[t][1] == -INFINITY ? 0.f : fmaf(m[t][1], cs, down);
 #pragma unroll
             for (int u = 0; u < KT; ++u)
 #pragma unroll

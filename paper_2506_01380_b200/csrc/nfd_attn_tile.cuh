@@ -9,9 +9,10 @@
 //     P = exp2(S c - m)   one thread per row: S by columns to registers, exponentials, P as bf16 over the S it came from
 //     O += P V      UMMA 128 x head_dim x KB, P from tensor memory, V as it lies (MN-major)
 // m is the largest of the first 16 scores of the group's first block, and no other maximum is taken: a probability is exact to the
-// same number of bits whatever its size.  Where a block's sum of a row passes 2^60 after all (or is NaN), or a row has no m yet, the warp
-// takes the block again, S being untouched so far: maxima first, and where one has risen by more than 8 (a factor of 256) it becomes m and
-// the row's O is rescaled in tensor memory by its thread.
+// same number of bits whatever its size.  Where a block's sum of a row passes 2^60 (states: 2^24) after all (or is NaN), or a row has no m yet, the
+// warp takes the block again, S being untouched so far: maxima first, and where one has risen by more than 8 (a factor of 256) it becomes m and
+// the row's O is rescaled in tensor memory by its thread.  What P grows to, O does: 4-bit values are scaled to less than 1, and O stays in fp32; states
+// may be as large as bf16 goes, so that their P are scaled down by as much as all blocks together can grow (sum_bits), in the exponent.
 //
 // Warps 0 .. PW-1 fill the rings of K and V blocks: bf16 states with cp.async, several blocks in flight; 4-bit pages through
 // registers, two blocks ahead, the codes becoming bf16 numbers on the way.  Warp PW issues the products, the last 4 NG are the
@@ -30,6 +31,8 @@
 
 #define TILE_THREADS 512
 #define TILE_SPLIT 8                // most CTAs of a cluster
+#define TILE_GROWTH_KV4 60          // bits that a block's sum may grow by before m follows it
+#define TILE_GROWTH 24
 
 // (no status word: there is no context whose latch could be read)
 __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity) {
@@ -356,7 +359,7 @@ template <int DH> struct TileKv4 {
 // row's maximum over the keys that it sees, m and what has been summed so far adjusted to it, then P.
 // seen: bits of the keys that the row sees; n: the group's jobs before this one.
 template <int DH>
-static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, const uint32_t *seen, float c, int n,
+static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, const uint32_t *seen, float c, float down, int n,
                                               uint32_t pv_done, float &m_io, float &l_io, bool &ok) {
     using C = TileCfg<DH>;
     constexpr int KB = C::KB;
@@ -395,7 +398,7 @@ static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, const
             }
         }
     }
-    const float mc = m == -INFINITY ? 0.f : m * c;
+    const float mc = m == -INFINITY ? 0.f : fmaf(m, c, down);
     float sum = 0.f;
 #pragma unroll 1
     for (int i = 0; i < KB; i += 16) {
@@ -415,11 +418,11 @@ static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, const
     m_io = m, l_io = l + sum;
 }
 // One pass over S against the m that there is, 16 columns at a time with the next load in flight (xa: the first ones).  MASKED: keys that the
-// row does not see count for nothing.  False: a sum has outgrown m, and S is as it was.
+// row does not see count for nothing.  down: taken off the exponents.  False: a sum has outgrown m (most: the most that it may be), and S is as it was.
 template <int DH, bool MASKED>
-static __device__ __forceinline__ bool tile_fast(uint32_t tS, float *xa, const uint32_t *seen, float c, float m, float &l) {
+static __device__ __forceinline__ bool tile_fast(uint32_t tS, float *xa, const uint32_t *seen, float c, float down, float most, float m, float &l) {
     constexpr int KB = TileCfg<DH>::KB;
-    const float mc = m == -INFINITY ? 0.f : m * c;
+    const float mc = m == -INFINITY ? 0.f : fmaf(m, c, down);
     float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     float xb[8];
     uint32_t pk[KB / 2];
@@ -450,7 +453,7 @@ static __device__ __forceinline__ bool tile_fast(uint32_t tS, float *xa, const u
     }
     const float2 l2 = fadd2(ls[0], ls[1]);
     const float sum = l2.x + l2.y;
-    if (!__all_sync(0xffffffffu, sum < 1.152921504606847e18f)) return false;
+    if (!__all_sync(0xffffffffu, sum < most)) return false;
     l += sum;
 #pragma unroll
     for (int i = 0; i < KB / 2; i += 8) tmem_st8(tS + i, pk + i);
@@ -613,6 +616,8 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         const uint32_t lane_off = (uint32_t)(quad * 32) << 16, tO = tmem + C::TM_O + g * 64 * SUB + lane_off;
         const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
         const float c = 1.4426950408889634f * rsqrtf((float)DH) * Src::UP;
+        float down = 0.f, most = (float)(1ull << TILE_GROWTH_KV4);     // (4-bit values are below 1 here)
+        if constexpr (!Src::KV4) down = src.K.down(TILE_GROWTH, KB), most = exp2f(TILE_GROWTH - down);
         const KeyRange kr = src.K.range(B, len, sr.y, A.split(r0 + min(r, nr - 1)).x);
         cp_async_wait<0>();
         tile_publish(bars.q_full());
@@ -657,10 +662,10 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                 }
                 bool done = false;
                 if (__all_sync(0xffffffffu, m != -INFINITY || !any))
-                    done = all_whole ? tile_fast<DH, false>(tS, xa, seen, c, m, l) : tile_fast<DH, true>(tS, xa, seen, c, m, l);
+                    done = all_whole ? tile_fast<DH, false>(tS, xa, seen, c, down, most, m, l) : tile_fast<DH, true>(tS, xa, seen, c, down, most, m, l);
                 if (!done) {
                     tmem_ld_wait();
-                    tile_slow<DH>(tS, tO, seen, c, n, bars.pv_done(g, n - 1), m, l, ok);
+                    tile_slow<DH>(tS, tO, seen, c, down, n, bars.pv_done(g, n - 1), m, l, ok);
                 }
                 tmem_st_wait();
             }

@@ -1,0 +1,49 @@
+"""The calls on the caller's own memory at the ends of their numbers' ranges.  Bounds as in test_gpu_paged.py."""
+import numpy as np
+import pytest
+
+from oracle import paged_oracle as P
+from test_gpu_paged import HALF, _largest_score, _mods, _np, _rounded, _within
+
+pytestmark = pytest.mark.gpu
+
+
+def _states_case(tdt, seqs, rows, keys, dh, power, scores, seed):
+    """States whose values have a size of 2^power, and queries whose scores are a function of the key's number (in nats): everything 64 bits
+    needs to judge the call, and its result."""
+    torch, N = _mods()
+    rng = np.random.default_rng(seed)
+    k = rng.standard_normal((seqs, keys, 1, dh)).astype(np.float32)
+    q = np.zeros((seqs * rows, 1, dh), np.float32)
+    q[..., 0], q[..., 1] = np.sqrt(dh), 1.0                            # (and a little of another channel)
+    k[..., 0] = scores[None, :, None]
+    v = rng.uniform(-1.9, 1.9, k.shape)
+    k, q = _rounded(k, tdt), _rounded(q, tdt)
+    v = (_rounded(v.astype(np.float32), tdt).double() * 2.0 ** power).to(tdt)
+    assert torch.isfinite(v).all()
+    b = N.Batch(seqs * rows, n_seqs=seqs)
+    out = torch.full((seqs * rows, dh), 7.0, device="cuda", dtype=tdt)
+    N.cross_attention(N.States(k.cuda(), v.cuda()), b, q.cuda(), out)
+    batch = dict(rows=[rows] * seqs, lens=[keys] * seqs)
+    want, mag = P.cross_attention(_np(q), batch, _np(k), _np(v).astype(np.float64), None, 1)
+    return out, want, mag, _largest_score(_np(q), _np(k))
+
+
+RISES = {"equal": lambda n: np.zeros(n, np.float32),
+         "rising by 41": lambda n: np.where(np.arange(n) < 16, 0, 41 * np.arange(n) / n).astype(np.float32),
+         "late": lambda n: np.where(np.arange(n) < n - 3, 0, 30).astype(np.float32)}
+
+
+@pytest.mark.parametrize("power", [100, 127, -90])
+@pytest.mark.parametrize("scores", list(RISES))
+@pytest.mark.parametrize("seqs,rows", [(1, 1), (3, 24), (1, 140), (150, 300)])
+@pytest.mark.parametrize("tdt,dh", [("bfloat16", 64), ("bfloat16", 128), ("float32", 64)])
+def test_cross_large_and_small_values(tdt, dh, seqs, rows, scores, power):
+    """Results are means of the values: finite where these are, however the scores rise, for every number of rows."""
+    torch, _ = _mods()
+    if seqs > 100 and tdt == "float32":
+        seqs = 5                                                       # (many sequences are for the layouts of the bf16 kernel)
+    keys = 700
+    out, want, mag, smax = _states_case(getattr(torch, tdt), seqs, rows, keys, dh, power, RISES[scores](keys), rows)
+    s = 2.0 ** -power
+    _within(_np(out).astype(np.float64).reshape(want.shape) * s, want * s, mag * s, smax, keys, HALF if tdt == "bfloat16" else 0.0)

@@ -13,6 +13,7 @@ extern "C" void span(int start, int end, int n_rows, int *out) {
     const RowSpan r = rows_between(start, end, n_rows);
     out[0] = r.first, out[1] = r.n;
 }
+extern "C" int bits(int growth, int n) { return sum_bits(growth, n); }
 """
 
 
@@ -38,3 +39,12 @@ def test_row_starts_of_any_value_stay_in_the_buffer(lib):
                 assert 0 <= first <= n_rows and 0 <= n <= n_rows - first, (a, b, n_rows)
                 inside = [min(max(x, 0), n_rows) for x in (a, b)]
                 assert (first, n) == (inside[0], max(0, inside[1] - inside[0]))
+
+
+def test_probabilities_of_all_keys_add_up_to_one_at_most(lib):
+    """n probabilities of 2^growth, scaled: the next power of two of n, and no bit more."""
+    for n in list(range(1, 5000)) + [(1 << b) + d for b in range(13, 30) for d in (-1, 0, 1)] + [1 << 30]:
+        for growth in (1, 8, 24):
+            b = lib.bits(growth, n) - growth
+            assert n <= 1 << b and (b == 0 or n > 1 << b - 1), n
+    assert lib.bits(8, 0) == 8
