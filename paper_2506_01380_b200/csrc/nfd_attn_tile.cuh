@@ -393,7 +393,7 @@ static __device__ __forceinline__ void tile_slow(uint32_t tS, uint32_t tO, const
                 tmem_ld_wait();
                 loaded16(o);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = f == 0.f ? 0.f : o[e] * f;
+                for (int e = 0; e < 16; ++e) o[e] *= f;               // (f may be 0: a value that is not finite stays one)
                 tmem_st16(tO + i, reinterpret_cast<uint32_t *>(o));
             }
         }
@@ -693,7 +693,8 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                 if (merge) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        *reinterpret_cast<float4 *>(state + ((i / 4 + e) * 128 + trow) * 16) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        *reinterpret_cast<float4 *>(state + ((i / 4 + e) * 128 + trow) * 16) =
+                            n ? make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
                 } else if (r < nr) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -708,7 +709,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         }
         if (merge && T == 1) {
             // The groups' states of the one tile become one, over the first (a third or half of the columns to a group), or the result.  They count
-            // in the groups' order; one without scores counts for nothing.
+            // in the groups' order; one without scores has zeros, and none is left out: a value that is not finite counts however small its factor.
             asm volatile("bar.sync 1, %0;" ::"n"(NG * 128) : "memory");
             float f[NG], mx = -INFINITY, sum = 0.f;
             float2 ml[NG];
@@ -723,7 +724,6 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
                 for (int k = 0; k < NG; ++k)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        if (f[k] == 0.f) continue;          // (what is there may be anything)
                         const float4 o = *reinterpret_cast<const float4 *>(smem + k * C::STATE + ((2 * i + e) * 128 + trow) * 16);
                         v[4 * e] = fmaf(o.x, f[k], v[4 * e]), v[4 * e + 1] = fmaf(o.y, f[k], v[4 * e + 1]);
                         v[4 * e + 2] = fmaf(o.z, f[k], v[4 * e + 2]), v[4 * e + 3] = fmaf(o.w, f[k], v[4 * e + 3]);
@@ -770,7 +770,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
             for (int k = 0; k < TILE_SPLIT; ++k) {
                 const float f = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx);
                 sum = fmaf(ml[k].y, f, sum);
-                if (f != 0.f) v.x = fmaf(o[k].x, f, v.x), v.y = fmaf(o[k].y, f, v.y), v.z = fmaf(o[k].z, f, v.z), v.w = fmaf(o[k].w, f, v.w);
+                v.x = fmaf(o[k].x, f, v.x), v.y = fmaf(o[k].y, f, v.y), v.z = fmaf(o[k].z, f, v.z), v.w = fmaf(o[k].w, f, v.w);
             }
             const float inv = sum == 0.f ? 0.f : Src::UP / sum;
             const int2 at = A.split(r0 + r);

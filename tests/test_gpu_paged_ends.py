@@ -47,3 +47,27 @@ def test_cross_large_and_small_values(tdt, dh, seqs, rows, scores, power):
     out, want, mag, smax = _states_case(getattr(torch, tdt), seqs, rows, keys, dh, power, RISES[scores](keys), rows)
     s = 2.0 ** -power
     _within(_np(out).astype(np.float64).reshape(want.shape) * s, want * s, mag * s, smax, keys, HALF if tdt == "bfloat16" else 0.0)
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+@pytest.mark.parametrize("at", [0, 90, 699])
+@pytest.mark.parametrize("seqs,rows", [(1, 1), (3, 24), (1, 140), (1, 336), (150, 300)])
+@pytest.mark.parametrize("tdt,dh", [("bfloat16", 64), ("bfloat16", 128), ("float32", 64)])
+def test_cross_values_that_are_not_finite(tdt, dh, seqs, rows, at, what):
+    """A value that is not finite makes its column of the rows that see it not finite, however small the probability: here the scores of
+    later keys are 120 nats above those of earlier ones.  Other columns hold."""
+    torch, N = _mods()
+    dt = getattr(torch, tdt)
+    keys, g = 700, torch.Generator("cuda").manual_seed(rows)
+    k, v = (torch.randn(seqs, keys, 1, dh, device="cuda", generator=g).to(dt) for _ in range(2))
+    k[..., 0] = torch.where(torch.arange(keys, device="cuda") < 100, 0.0, 120.0)[None, :, None].to(dt)
+    q = torch.zeros(seqs * rows, 1, dh, device="cuda", dtype=dt)
+    q[..., 0], q[..., 1] = dh ** 0.5, 1.0
+    b = N.Batch(seqs * rows, n_seqs=seqs)
+    run = lambda vv: N.cross_attention(N.States(k, vv), b, q, torch.full((seqs * rows, dh), 7.0, device="cuda", dtype=dt))
+    good, bad = run(v), v.clone()
+    bad[:, at, 0, 5] = what
+    got = run(bad)
+    assert not got[:, 5].isfinite().any()
+    rest = torch.arange(dh, device="cuda") != 5
+    assert good.isfinite().all() and torch.equal(got[:, rest], good[:, rest])
