@@ -340,7 +340,7 @@ typedef struct {
  * fp32 is computed on the fp32 pipes.  Values may be as large as their type goes: a
  * result, being a mean of them, is finite with them.  A NaN or an infinity among them
  * makes its column of the rows that see it NaN or infinite, however small its
- * probability.  (Small values: with up to 2^20 states, values below 2^-80 may lose
+ * probability.  (Small values: with up to 2^20 states, values below 2^-56 may lose
  * bits in the sums.) */
 int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_heads, const void *q,
                         long long q_stride, void *out, void *cuda_stream);

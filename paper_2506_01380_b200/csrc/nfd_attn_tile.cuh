@@ -9,7 +9,7 @@
 //     P = exp2(S c - m)   one thread per row: S by columns to registers, exponentials, P as bf16 over the S it came from
 //     O += P V      UMMA 128 x head_dim x KB, P from tensor memory, V as it lies (MN-major)
 // m is the largest of the first 16 scores of the group's first block, and no other maximum is taken: a probability is exact to the
-// same number of bits whatever its size.  Where a block's sum of a row passes 2^60 (states: 2^24) after all (or is NaN), or a row has no m yet, the
+// same number of bits whatever its size.  Where a block's sum of a row passes 2^60 (states: 2^50) after all (or is NaN), or a row has no m yet, the
 // warp takes the block again, S being untouched so far: maxima first, and where one has risen by more than 8 (a factor of 256) it becomes m and
 // the row's O is rescaled in tensor memory by its thread.  What P grows to, O does: 4-bit values are scaled to less than 1, and O stays in fp32; states
 // may be as large as bf16 goes, so that their P are scaled down by as much as all blocks together can grow (sum_bits), in the exponent.
@@ -32,7 +32,8 @@
 #define TILE_THREADS 512
 #define TILE_SPLIT 8                // most CTAs of a cluster
 #define TILE_GROWTH_KV4 60          // bits that a block's sum may grow by before m follows it
-#define TILE_GROWTH 24
+#define TILE_GROWTH 50              // of states, whose probabilities start as many bits lower.  8 x 1344 rows against up to 2048 states, 16 heads on 4 x 128,
+                                    // scores with a deviation of 10 nats, us: 24 bits 156, 40 135, 50 128, 60 127; with a deviation of 1 all 126 to 127
 
 // (no status word: there is no context whose latch could be read)
 __device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity) {

@@ -15,7 +15,7 @@ NFD_HD RowSpan rows_between(int start, int end, int n_rows) {
 
 // Probabilities of states are formed 2^-bits of their size: with a reference m of a row that may be short of its largest score, n of them of up to
 // 2^growth have a sum of 1 at most then, so that O, a sum of values times them, is no larger than the largest value and leaves fp32 for no
-// finite one; the quotient of O and the sum does not know of it.  (What it costs is at the other end: values next to fp32's smallest ones
+// finite one; the quotient of O and the sum does not know of it.  (What it costs is at the other end: small values
 // lose bits in O, which ends at 2^-149 whatever the scale.)
 NFD_HD int sum_bits(int growth, int n) {
     if (n <= 1) return growth;
