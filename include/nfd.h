@@ -291,8 +291,9 @@ typedef struct {
  * 4 bits: of 32 numbers, lo = min(0, smallest), hi = max(0, largest), step = the
  * smallest number of 4 significant bits, at least 2^-100, with 15 step >= hi - lo,
  * z = lo / -step rounded, n = x / step rounded, plus z, kept in 0..15 (all to
- * nearest, ties to even).  Where one of the 32 is not finite, or hi - lo is not,
- * the step is NaN and with it all 32.
+ * nearest, ties to even), all of it exactly, whatever fp32 would make of hi - lo.
+ * Where one of the 32 is not finite, or hi - lo is above fp32's largest number, the
+ * step is NaN and with it all 32.
  * Rows of tokens below 0 (a sequence with more rows than kv_len) are dropped.
  * Two rows for the same place (pages that sequences share) race. */
 int nfd_kv_append(const nfd_pages *pages, const nfd_batch *batch, const nfd_rope *rope, int dtype, const void *k,

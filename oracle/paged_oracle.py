@@ -12,12 +12,14 @@ def kv4_quantise(x):
     """x [..., dh] (fp32 values) -> whole numbers n [..., dh], z and step [..., dh / 32] (64 bits; step NaN: not finite)."""
     g = np.asarray(x, np.float64).reshape(x.shape[:-1] + (-1, 32))
     lo, hi = np.minimum(g.min(-1), 0.0), np.maximum(g.max(-1), 0.0)
-    with np.errstate(invalid="ignore", over="ignore"):
-        r = np.asarray(hi.astype(np.float32) - lo.astype(np.float32), np.float64)      # the range is an fp32 number
-    ok = np.isfinite(r) & np.isfinite(g).all(-1)
-    r = np.where(ok, r, 0.0)
-    m, e = np.frexp(r / 15)
-    step = np.maximum(np.ldexp(np.ceil(m * 16) / 16, e), 2.0 ** -100)
+    ok = np.isfinite(g).all(-1)
+    # r >= hi - lo as r - big >= small: a difference that 64 bits hold, r being a number of few bits that is not far from big (or far above)
+    big, small = np.where(ok, np.maximum(hi, -lo), 0.0), np.where(ok, np.minimum(hi, -lo), 0.0)
+    ok &= float(np.finfo(np.float32).max) - big >= small
+    big, small = np.where(ok, big, 0.0), np.where(ok, small, 0.0)
+    up = lambda y: (lambda m, e: np.ldexp(np.ceil(m * 16) / 16, e))(*np.frexp(y))
+    step = np.maximum(up((big + small) / 15), 2.0 ** -100)
+    step = np.where(15 * step - big >= small, step, up(step * (1 + 2.0 ** -20)))
     g, lo = np.where(ok[..., None], g, 0.0), np.where(ok, lo, 0.0)
     z = np.rint(-lo / step)
     n = np.clip(np.rint(g / step[..., None]) + z[..., None], 0, 15)

@@ -63,11 +63,12 @@ __device__ __forceinline__ uint32_t kv4_pack(const float *x, uint32_t &word, uin
         lo = fminf(lo, __shfl_xor_sync(group, lo, o));
         hi = fmaxf(hi, __shfl_xor_sync(group, hi, o));
     }
-    if (!(hi - lo < INFINITY)) {
+    const float range = kv4_range(lo, hi);
+    if (!(range < INFINITY)) {
         word = 0x7FC0u;
         return 0;
     }
-    const float step = kv4_step(lo, hi), inv = __frcp_rn(step);
+    const float step = kv4_step(range), inv = __frcp_rn(step);
     const int z = __float_as_int(kv4_quotient(-lo, step, inv)) - __float_as_int(KV4_MAGIC), up = z - __float_as_int(KV4_MAGIC);
     word = (__float_as_uint(step) >> 16) | (uint32_t)z;
     uint32_t codes = 0;

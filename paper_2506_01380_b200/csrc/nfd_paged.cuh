@@ -50,17 +50,6 @@ struct PagesD {
 };
 
 // ---- 4-bit numbers ------------------------------------------------------------------------------------------
-// Step (upper 12 bits of the word) and zero of a group with range lo..hi (lo <= 0 <= hi).  The fp32 product is within an
-// ulp or two of (hi - lo) / 15; with 4 significant bits 15 step is exact, so that one comparison on either side settles
-// which of two neighbours is the smallest that covers the range.
-__device__ __forceinline__ float kv4_step(float lo, float hi) {
-    const float r = hi - lo;
-    uint32_t b = (__float_as_uint(fmaxf(r * (1.0f / 15.0f), 7.8886090522101181e-31f)) + 0xFFFFFu) & 0xFFF00000u;
-    if (15.0f * __uint_as_float(b) < r) b += 0x100000u;
-    const uint32_t down = b - 0x100000u;
-    if (__uint_as_float(down) >= 7.8886090522101181e-31f && 15.0f * __uint_as_float(down) >= r) b = down;
-    return __uint_as_float(b);
-}
 // x / step to the nearest whole number, ties to even, in the low bits of the result's significand (less KV4_MAGIC's bits).  The quotient is
 // corrected by its exact remainder, which makes it the rounded quotient; step having 4 significant bits, a quotient that is not half way
 // between whole numbers is not rounded to one that is (it is off by more than half an ulp), so that rounding once more loses nothing.

@@ -1,5 +1,6 @@
 // Arithmetic of the calls on the caller's own memory on numbers alone, for the host and the kernels (and for a plain C++ compiler).
 #pragma once
+#include <string.h>
 #include "nfd_attn_plan.h"
 
 // Rows start .. end - 1 of a buffer of n_rows, whatever device memory says: both ends are clamped into 0 .. n_rows before anything is formed of
@@ -24,4 +25,41 @@ NFD_HD int sum_bits(int growth, int n) {
 #else
     return growth + 32 - __builtin_clz((unsigned int)n - 1);
 #endif
+}
+
+// ---- the step of 4-bit numbers ------------------------------------------------------------------------------
+NFD_HD uint32_t bits_of(float x) {
+#ifdef __CUDA_ARCH__
+    return __float_as_uint(x);
+#else
+    uint32_t b;
+    memcpy(&b, &x, 4);
+    return b;
+#endif
+}
+NFD_HD float float_of(uint32_t b) {
+#ifdef __CUDA_ARCH__
+    return __uint_as_float(b);
+#else
+    float x;
+    memcpy(&x, &b, 4);
+    return x;
+#endif
+}
+// The smallest fp32 number that is at least hi - lo (lo <= 0 <= hi): the rounded difference, and the next number where what the rounding took away
+// (exactly the second sum, the larger number standing first in it) is above 0.  An fp32 number is at least hi - lo exactly where it is at least this one.
+NFD_HD float kv4_range(float lo, float hi) {
+    const float big = hi > -lo ? hi : -lo, small = hi > -lo ? -lo : hi, r = big + small;
+    return small - (r - big) > 0.f ? float_of(bits_of(r) + 1) : r;
+}
+// Step (upper 12 bits of the word) of a group with that range: the smallest number of 4 significant bits, at least 2^-100, 15 of which cover it.
+// The fp32 product is within an ulp or two of range / 15; 15 step is exact with 4 significant bits (or infinite), so that one comparison on either
+// side settles which of two neighbours it is.
+NFD_HD float kv4_step(float range) {
+    const float least = 7.8886090522101181e-31f, t = range * (1.0f / 15.0f);
+    uint32_t b = (bits_of(t > least ? t : least) + 0xFFFFFu) & 0xFFF00000u;
+    if (15.0f * float_of(b) < range) b += 0x100000u;
+    const uint32_t down = b - 0x100000u;
+    if (float_of(down) >= least && 15.0f * float_of(down) >= range) b = down;
+    return float_of(b);
 }

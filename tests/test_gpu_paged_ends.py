@@ -1,4 +1,6 @@
 """The calls on the caller's own memory at the ends of their numbers' ranges.  Bounds as in test_gpu_paged.py."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 
@@ -71,3 +73,32 @@ def test_cross_values_that_are_not_finite(tdt, dh, seqs, rows, at, what):
     assert not got[:, 5].isfinite().any()
     rest = torch.arange(dh, device="cuda") != 5
     assert good.isfinite().all() and torch.equal(got[:, rest], good[:, rest])
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# 4-bit numbers
+# ---------------------------------------------------------------------------------------------------------------
+def _step(lo, hi):
+    """The smallest number of 4 significant bits, at least 2^-100, with 15 of it at least hi - lo, in fractions."""
+    r, e = Fraction(float(hi)) - Fraction(float(lo)), -100
+    while Fraction(2) ** e * 15 * 15 / 8 < r:
+        e += 1
+    return next(float(Fraction(2) ** e * m / 8) for m in range(8, 16) if Fraction(2) ** e * m / 8 * 15 >= r)
+
+
+@pytest.mark.parametrize("hi,lo", [(15.0, -1e-8), (15.0, -1e-30), (1e-9, -15.0), (15.0, 0.0), (30.0 - 2.0 ** -19, -2.0 ** -19), (7.5, -7.5 - 2.0 ** -21),
+                                   (16.875 * 2.0 ** 40, -1.0)])
+def test_append_steps_by_the_definition(hi, lo):
+    """Ranges that lie next to 15 steps: what fp32 rounds away of hi - lo decides."""
+    torch, N = _mods()
+    x = torch.zeros(1, 1, 64)
+    x[0, 0, 3], x[0, 0, 9], x[0, 0, 32:] = hi, lo, torch.linspace(-1, 1, 32)
+    hi, lo = float(x[0, 0, 3]), float(x[0, 0, 9])
+    pages = N.Pages.empty("kv4", 1, 1, 1, 64)
+    b = N.Batch(1, torch.ones(1, device="cuda", dtype=torch.int32), torch.zeros(1, 1, device="cuda", dtype=torch.int32))
+    N.kv_append(pages, b, x.cuda(), x.cuda())
+    step = _step(lo, hi)
+    for words in (pages.k_scale, pages.v_scale):
+        w = int(words[0, 0, 0, 0]) & 0xFFFF
+        got = float(np.uint32((w & 0xFFF0) << 16).view(np.float32))
+        assert got == step and w & 15 == round(Fraction(-lo) / Fraction(step))
