@@ -260,7 +260,8 @@ typedef struct {
  * k_scale and v_scale [..][head_dim / 32] 16-bit words, one for 32 numbers.  A
  * word's upper 12 bits are those of a bf16 number `step` (4 significant bits), its
  * lower 4 bits a whole number z; a code n stands for (n - z) step, which is a
- * bf16 number (exactly, as long as it does not leave bf16's range).  Codes: eight
+ * bf16 number (exactly, as long as it does not leave bf16's range; what
+ * nfd_attention_kv4 takes of that range stands there).  Codes: eight
  * numbers to a little-endian 32-bit word, number i in bits 4 (i / 2) + 16 (i % 2)
  * and up. */
 #define NFD_DTYPE_KV4 2
@@ -316,8 +317,10 @@ int nfd_pages_read(const nfd_pages *pages, const nfd_batch *batch, int dtype, vo
  * tokens of the frames max(0, frame - window) .. frame that the cache holds
  * (frame_tokens = 1: a causal mask over the last window + 1 tokens).
  * The scale is 1 / sqrt(head_dim).  A row that sees nothing, or nothing but scores
- * of -inf, gives zeros; a row that sees a value that is not finite is NaN, and steps of
- * 2^27 and more (numbers beyond 10^8) count as not finite here.  Scores, softmax and
+ * of -inf, gives zeros; a row that sees a value that is not finite is NaN.  Of a
+ * step, 2^-98 to below 2^27 is taken as it is: steps of 2^27 and more (numbers beyond
+ * 10^8) count as not finite here, and a number of a smaller step (2^-100 is the
+ * smallest) is taken to within 2^-101; nfd_pages_read reads them all.  Scores, softmax and
  * sums are fp32; probabilities are rounded to bf16 for the product with V.  Should a
  * device-side wait run out, the rows concerned are NaN. */
 int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,

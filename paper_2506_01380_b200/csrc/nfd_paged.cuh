@@ -71,8 +71,9 @@ __device__ __forceinline__ uint32_t kv4_z2(uint32_t w0, uint32_t w1) { return (w
 __device__ __forceinline__ uint32_t kv4_step2(uint32_t w0, uint32_t w1) { return (w0 & 0xFFF0u) | (w1 & 0xFFF0u) << 16; }
 
 // The same for the operands of products, scaled by 2^-32 (KV4_UP undoes it in fp32): a code in the low bits of a bf16 is the subnormal number
-// n 2^-133, and one fma with step 2^101 and -z step 2^-32 makes (n - z) step 2^-32 of it, exactly for steps from 2^-94 on: two instructions and a
-// shift for two numbers, where kv4_pair takes three.  Steps of 2^27 and more (numbers beyond 10^8) count as not finite here.
+// n 2^-133, and one fma with step 2^101 and -z step 2^-32 makes (n - z) step 2^-32 of it: two instructions and a
+// shift for two numbers, where kv4_pair takes three.  Exactly for steps from 2^-98 on, whose numbers are whole multiples of 2^-101; the quantiser's smaller
+// ones (2^-100 and 2^-99) lose half of 2^-101 in z step and half in the fma.  Steps of 2^27 and more (numbers beyond 10^8) count as not finite here.
 #define KV4_UP 4294967296.0f
 __device__ __forceinline__ bool kv4_not_finite(uint32_t word) { return (word & 0x7F80u) >= 0x4D00u; }
 struct Kv4Scale {

@@ -102,3 +102,24 @@ def test_append_steps_by_the_definition(hi, lo):
         w = int(words[0, 0, 0, 0]) & 0xFFFF
         got = float(np.uint32((w & 0xFFF0) << 16).view(np.float32))
         assert got == step and w & 15 == round(Fraction(-lo) / Fraction(step))
+
+
+@pytest.mark.parametrize("rows", [1, 150])
+@pytest.mark.parametrize("power", [-100, -99, -98, -97, -94])
+def test_kv4_smallest_steps(rows, power):
+    """Steps from 2^-98 on are taken as they are; a value of a smaller one to within 2^-101 (half of it by the zero, half by the number)."""
+    torch, N = _mods()
+    rng = np.random.default_rng(12)
+    t = lambda a: torch.as_tensor(a.view(np.int16) if a.dtype == np.uint16 else a).cuda()
+    x = rng.standard_normal((4, 1, 64, 64)).astype(np.float32)
+    (kb, kw), (vb, vw) = P.kv4_bytes(*P.kv4_quantise(x)), P.kv4_bytes(*P.kv4_quantise(x[::-1].copy()))
+    vw = ((vw & 0x7F) | ((127 + power) << 7)).astype(np.uint16)        # (steps of 4 bits, as they come)
+    b = N.Batch(rows, torch.tensor([256], device="cuda", dtype=torch.int32), torch.arange(4, device="cuda", dtype=torch.int32)[None])
+    q = _np(_rounded(rng.standard_normal((rows, 1, 64)).astype(np.float32), torch.bfloat16))
+    out = torch.zeros(rows, 64, device="cuda", dtype=torch.bfloat16)
+    N.attention_kv4(N.Pages(t(kb), t(vb), t(kw), t(vw)), b, torch.as_tensor(q).cuda().bfloat16(), out)
+    want, mag = P.attention_kv4(q, dict(rows=[rows], lens=[256]), np.arange(4)[None], (kb, kw, vb, vw), 1, 1 << 30, 1)
+    off = np.abs(_np(out).astype(np.float64).reshape(rows, 1, 64) - want)
+    # (2^-109: 256 sums of numbers scaled by 2^-32 that may be below fp32's normal ones, to 2^-149 each)
+    bound = (2.0 ** -101 if power < -98 else 0) + 2.0 ** -109 + 1.02 * HALF * (mag + np.abs(want))
+    assert (off <= bound).all(), float((off / bound).max())
