@@ -221,11 +221,8 @@ template <int DH, int ROWS>
 static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
     using C = F32Cfg<DH, ROWS>;
     auto kern = k_attn_f32<DH, ROWS>;
-    static std::atomic<bool> sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
-    if (!sized[dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return NFD_E_CUDA;
-        sized[dev] = true;
-    }
+    static OncePerDevice once;
+    if (!once.run(dev, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess; })) return NFD_E_CUDA;
     const long long tiles = ((long long)B.max_rows * A.share + ROWS - 1) / ROWS, units = kv_heads * tiles * B.n_seqs;
     const int blocks = (K.n_keys + F32_KEYS - 1) / F32_KEYS;
     int split = 1;
@@ -433,15 +430,16 @@ template <int DH, int R>
 static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, cudaStream_t st) {
     using C = F32Few<DH, R>;
     auto kern = k_attn_f32_few<DH, R>;
-    static std::atomic<bool> sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
+    static OncePerDevice once;
     static int fit[NFD_PAGED_DEVICES][5];
-    if (!sized[dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess ||
-            cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
-            return NFD_E_CUDA;
-        for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * FEW_WARPS, C::SMEM);
-        sized[dev] = true;
-    }
+    if (!once.run(dev, [&] {
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess ||
+                cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+                return false;
+            for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * FEW_WARPS, C::SMEM);
+            return true;
+        }))
+        return NFD_E_CUDA;
     const int tiles = (int)(((long long)B.max_rows * A.share + R - 1) / R);
     const int split = few_split((long long)kv_heads * B.n_seqs * tiles, K.n_keys, C::KC, fit[dev]);
     cudaLaunchConfig_t cfg = {};

@@ -538,15 +538,16 @@ template <typename Src, int DH, int NR>
 static int launch_attn_few_nr(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
     using F = FewCfg<Src, DH, NR>;
     auto kern = k_attn_few<Src, DH, NR>;
-    static std::atomic<bool> sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
+    static OncePerDevice once;
     static int fit[NFD_PAGED_DEVICES][5];
-    if (!sized[dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
-            cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
-            return NFD_E_CUDA;
-        for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * FEW_WARPS, F::SMEM);
-        sized[dev] = true;
-    }
+    if (!once.run(dev, [&] {
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
+                cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+                return false;
+            for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * FEW_WARPS, F::SMEM);
+            return true;
+        }))
+        return NFD_E_CUDA;
     const long long tiles = ((long long)B.max_rows * A.share + F::ROWS - 1) / F::ROWS;
     const int split = few_split((long long)kv_heads * B.n_seqs * tiles, keys, Src::KC, fit[dev]);
     cudaLaunchConfig_t cfg = {};

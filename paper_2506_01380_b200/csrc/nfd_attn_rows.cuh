@@ -1,5 +1,6 @@
 // The rows of an attention call, and what they attend to: 4-bit pages or encoder states.
 #pragma once
+#include <mutex>
 #include "nfd_append.cuh"
 
 // The rows of a call.
@@ -37,6 +38,24 @@ template <typename TS, int DH> struct StateKeys {
 };
 
 
+// What a kernel's first call on a device finds out, once for all threads: nobody reads it before it is complete.
+struct OncePerDevice {
+    std::atomic<bool> done[NFD_PAGED_DEVICES];
+    std::mutex mutex;
+    // f() returns false where it failed: the next call tries again
+    template <typename F> bool run(int dev, F &&f) {
+        if (done[dev]) return true;
+        std::lock_guard<std::mutex> lock(mutex);
+        if (!done[dev]) {
+            if (!f()) {
+                cudaGetLastError();                         // (the call's code tells)
+                return false;
+            }
+            done[dev] = true;
+        }
+        return true;
+    }
+};
 // Clusters of `ctas` CTAs that the device holds at once.
 template <typename Kernel> static int clusters_that_fit(Kernel kern, int ctas, int threads, int smem) {
     cudaLaunchConfig_t cfg = {};

@@ -818,13 +818,14 @@ template <typename Src, int DH>
 static int launch_attn_tile(const BatchD &B, const AttnRows &A, const Src &src, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
     using C = TileCfg<DH>;
     auto kern = k_attn_tile<Src, DH>;
-    static std::atomic<bool> sized[NFD_PAGED_DEVICES];                  // (once per device and kernel)
+    static OncePerDevice once;
     static int fit[NFD_PAGED_DEVICES][TILE_SPLIT + 1];
-    if (!sized[dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return NFD_E_CUDA;
-        for (int split = 2; split <= TILE_SPLIT; ++split) fit[dev][split] = clusters_that_fit(kern, split, TILE_THREADS, C::SMEM);
-        sized[dev] = true;
-    }
+    if (!once.run(dev, [&] {
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return false;
+            for (int split = 2; split <= TILE_SPLIT; ++split) fit[dev][split] = clusters_that_fit(kern, split, TILE_THREADS, C::SMEM);
+            return true;
+        }))
+        return NFD_E_CUDA;
     const long long rows = (long long)B.max_rows * A.share;
     const TilePlan pl = tile_plan<DH, Src::KV4>((long long)kv_heads * B.n_seqs, rows, keys, n_sm, [&](int k) { return fit[dev][k]; });
     const long long nz = (rows + 128 * pl.tiles - 1) / (128 * pl.tiles);

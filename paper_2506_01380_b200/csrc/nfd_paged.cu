@@ -78,11 +78,14 @@ int check_heads(int n_heads, int kv_heads, const BatchD &B) {
 
 // the current device and its SMs
 int this_device(int &dev, int &n_sm) {
-    static int n_sms[NFD_PAGED_DEVICES];       // (the same value whichever thread stores it)
+    static std::atomic<int> n_sms[NFD_PAGED_DEVICES];      // (the same value whichever thread stores it)
     CK(cudaGetDevice(&dev));
     if (dev < 0 || dev >= NFD_PAGED_DEVICES) return NFD_E_RANGE;
-    if (!n_sms[dev]) CK(cudaDeviceGetAttribute(&n_sms[dev], cudaDevAttrMultiProcessorCount, dev));
     n_sm = n_sms[dev];
+    if (!n_sm) {
+        CK(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev));
+        n_sms[dev] = n_sm;
+    }
     return NFD_OK;
 }
 
