@@ -14,6 +14,12 @@
 
 #define F32_KEYS 64
 
+// States, and the power of two by which probabilities are scaled: exact, one bit for the roundings of the sums.
+template <int DH> struct F32States : StateKeys<float, DH> {
+    float scale;
+    explicit F32States(const StateKeys<float, DH> &k) : StateKeys<float, DH>(k), scale(ldexpf(1.0f, -sum_bits(1, k.n_keys))) {}
+};
+
 template <int DH, int ROWS> struct F32Cfg {
     static constexpr int THREADS = 4 * ROWS;
     static constexpr int LD = DH + 4, LP = F32_KEYS + 4;                // floats of a padded row
@@ -24,7 +30,7 @@ template <int DH, int ROWS> struct F32Cfg {
 };
 
 template <int DH, int ROWS>
-__global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const AttnRows A, const StateKeys<float, DH> K, int split) {
+__global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const AttnRows A, const F32States<DH> K, int split) {
     using C = F32Cfg<DH, ROWS>;
     constexpr int LD = C::LD, LP = C::LP, ND = DH / 16, W = DH / 4;
     extern __shared__ __align__(16) float f32_smem[];
@@ -65,7 +71,6 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
     cp_async_commit();
     if (t0 < t1) fill(t0);
     const float cs = 1.4426950408889634f * (1.0f / sqrtf((float)DH));
-    const float scale = exp2f(-K.down(1, 1));                           // of probabilities; exact (1: for the roundings of the sums)
     float o[4][ND], m[4], l[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -124,7 +129,7 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
             for (int e = 0; e < ND; ++e) o[i][e] *= f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float p = exp2f((x[i][j] - mc) * cs) * scale;
+                const float p = exp2f((x[i][j] - mc) * cs) * K.scale;
                 l[i] += p, sP[(4 * ty + i) * LP + tx + 16 * j] = p;
             }
         }
@@ -218,7 +223,7 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
 }
 
 template <int DH, int ROWS>
-static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
+static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const F32States<DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
     using C = F32Cfg<DH, ROWS>;
     auto kern = k_attn_f32<DH, ROWS>;
     static OncePerDevice once;
@@ -241,7 +246,7 @@ static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const StateK
 // A few rows (8 of a unit to a cluster) to fp32 states: bound by the stream of K and V.  Each warp of a cluster's CTAs takes chunks of 1024 / DH keys in turn,
 // with a cp.async ring of its own (8 KB a chunk, two chunks ahead: 128 KB of an SM on their way), an online softmax of its own and no barrier until
 // the end.  S: a lane has a key's share of 32 dims; O: a lane has four dims and eight keys.  Rows of 16-byte words are swizzled by the key, so
-// that neither way of reading meets in a bank.  Measured, four sequences of one row, 16 heads x 64, against up to 2000 states: 14.4 us (131 MB at most, 66 on average: 4.6 TB/s), with the
+// that neither way of reading meets in a bank.  Measured, four sequences of one row, 16 heads x 64, against 2000 states each: 14.6 us (66 MB: 4.5 TB/s), with the
 // kernel above, whose tile of 32 rows one row has to itself, 50.
 template <int DH, int R> struct F32Few {
     static constexpr int KC = 1024 / DH, PR = DH / 4, LPK = 32 / KC, NST = 3;
@@ -251,8 +256,9 @@ template <int DH, int R> struct F32Few {
     static constexpr int AT_Q = FEW_WARPS * NST * STAGE, AT_P = AT_Q + R * QS * 4, AT_T = AT_P + FEW_WARPS * R * KC * 4, SMEM = AT_T + STATE;
     static_assert(STATE <= NST * STAGE && AT_T % 16 == 0 && SMEM <= 232448 - 1024, "shared memory of a CTA");
 };
+// (The rings leave one CTA to an SM, and so it may have all registers: not told so, the compiler took 128 and spilled, and eight rows took 25.6 us for 21.5.)
 template <int DH, int R>
-__global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B, const AttnRows A, const StateKeys<float, DH> K, int split) {
+__global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD B, const AttnRows A, const F32States<DH> K, int split) {
     using C = F32Few<DH, R>;
     constexpr int KC = C::KC, PR = C::PR, NST = C::NST, STEP = 32 / PR;
     extern __shared__ __align__(16) uint8_t f32_few_smem[];
@@ -303,7 +309,6 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B,
             *reinterpret_cast<const float4 *>((const float *)A.q + (long long)(sr.x + at.x) * A.q_stride + (h * A.share + at.y) * DH + 4 * w);
     }
     const float cs = 1.4426950408889634f * (1.0f / sqrtf((float)DH));
-    const float scale = exp2f(-K.down(1, 1));                           // as above
     const int key = lane % KC, part = lane / KC, g = lane / PR;
     float o[R][4], m[R], l[R];
 #pragma unroll
@@ -341,7 +346,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B,
 #pragma unroll
             for (int d = 1; d < KC; d <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
             mn = fmaxf(mn, m[r]);
-            const float f = mn == m[r] ? 1.0f : exp2f((m[r] - mn) * cs), p = exp2f((x - (mn == -INFINITY ? 0.f : mn)) * cs) * scale;
+            const float f = mn == m[r] ? 1.0f : exp2f((m[r] - mn) * cs), p = exp2f((x - (mn == -INFINITY ? 0.f : mn)) * cs) * K.scale;
             m[r] = mn, l[r] = fmaf(l[r], f, p);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[r][e] *= f;
@@ -427,7 +432,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_f32_few(const BatchD B,
     cluster_sync_all();                                                 // nobody leaves while its state is read
 }
 template <int DH, int R>
-static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, cudaStream_t st) {
+static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const F32States<DH> &K, int kv_heads, int dev, cudaStream_t st) {
     using C = F32Few<DH, R>;
     auto kern = k_attn_f32_few<DH, R>;
     static OncePerDevice once;
@@ -453,13 +458,14 @@ static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const StateKe
     }
     return NFD_OK;
 }
-// Rows of a unit that the kernel for few takes, eight at a time, each reading the keys.  us there and in tiles of 32 rows: four sequences, 16 heads x
-// 64, up to 2000 states, 8, 16 and 24 rows 25.7, 41.5, 79.7 and 51.0, 50.8, 50.7; 64 sequences, up to 512 states, 95.6, 182, 266 and 242, 242,
-// 241; head dimension 128, 32 sequences, 8 heads, up to 600, 16 and 32 rows 88, 154 and 183, 183.
+// Rows of a unit that the kernel for few takes, eight at a time, each eight reading the keys.  us there and in tiles of 32 rows: four sequences, 16 heads x
+// 64, 2000 states, 8 and 16 rows 21.6, 32.7 and 51.0, 50.8 (24, when that kernel still spilled, 79.7 and 50.7); 64 sequences, 512 states, 81.7,
+// 154 and 242, 242; head dimension 128, 32 sequences, 8 heads, 600 states, 16 and 32 rows 80, 139 and 183, 183.
 constexpr int f32_few_most(int dh) { return dh == 128 ? 32 : 16; }
 // 64 rows where that leaves no SM idle: twice the warps for the same tiles of keys
 template <int DH>
-static int launch_attn_f32(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
+static int launch_attn_f32(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &states, int kv_heads, int dev, int n_sm, cudaStream_t st) {
+    const F32States<DH> K(states);
     const long long rows = (long long)B.max_rows * A.share;
     if (rows <= 1) return launch_attn_f32_few<DH, 1>(B, A, K, kv_heads, dev, st);
     if (rows <= 4) return launch_attn_f32_few<DH, 4>(B, A, K, kv_heads, dev, st);

@@ -63,6 +63,7 @@ __device__ __forceinline__ float few_exp2(float x) {
 template <int DH> struct FewKv4 {
     static constexpr bool KV4 = true;
     static constexpr float UP = KV4_UP;                     // what scores and results are to be multiplied by
+    static __device__ __forceinline__ float down() { return 0.f; }        // taken off the exponents (sum_bits; values below 1 need nothing)
     static constexpr int KC = 32;
     static constexpr int NST = 3;                           // (with 4, head dimension 128 leaves one CTA to an SM: 138 us for 101)
     static constexpr int RB = DH / 2;                       // bytes of a row of codes
@@ -217,6 +218,8 @@ template <int DH> struct FewStates {
     static constexpr int RB = 2 * DH, PR = RB / 16;
     static constexpr int STAGE = 2 * KC * RB + 16;
     StateKeys<bf16, DH> K;
+    float bits;
+    __device__ __forceinline__ float down() const { return bits; }
     uint32_t there;                                         // of the chunk that is filled next
     __device__ __forceinline__ void start(const BatchD &, int, int, int, int) {}
     static __device__ __forceinline__ uint32_t at_k(int key, int piece) { return key * RB + (piece ^ (key & 7 & (PR - 1))) * 16; }
@@ -280,9 +283,10 @@ template <typename Src, int DH, int NR> struct FewCfg {
     static_assert(SMEM <= 232448 - 1024, "shared memory of a CTA");
 };
 
-// grid: (CTAs of a cluster x heads of keys, sequences, tiles of 8 NR rows)
+// grid: (CTAs of a cluster x heads of keys, sequences, tiles of 8 NR rows).  (States: their ring leaves one CTA to an SM, and so it may have all registers: not
+// told so, the compiler spilled in 80.)
 template <typename Src, int DH, int NR>
-__global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, const AttnRows A, Src src, int split) {
+__global__ void __launch_bounds__(32 * FEW_WARPS, Src::KV4 ? 0 : 1) k_attn_few(const BatchD B, const AttnRows A, Src src, int split) {
     using F = FewCfg<Src, DH, NR>;
     constexpr int KC = Src::KC, NST = Src::NST, NS = DH / 16, KT = KC / 16, ROWS = F::ROWS;
     // S in two chains of products for a single tile of rows (states, eight rows against 4096 26.9 us for 25.9; with 4-bit pages and head
@@ -334,8 +338,6 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
         }
     }
     const float cs = 1.4426950408889634f * rsqrtf((float)DH) * Src::UP;
-    float down = 0.f;                                                             // (probabilities grow to 2^8 before m follows)
-    if constexpr (!Src::KV4) down = src.K.down(8, 1);
     // this lane's rows: 2 c and 2 c + 1 of every tile of 8
     float o[NR][NS][4], m[NR][2], l[NR][2];
 #pragma unroll
@@ -428,7 +430,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) k_attn_few(const BatchD B, con
         uint32_t p[KT][NR][2];                                                    // P^T: keys 2 c.., row n
 #pragma unroll
         for (int t = 0; t < NR; ++t) {
-            const float m0 = m[t][0] == -INFINITY ? 0.f : fmaf(m[t][0], cs, down), m1 = m[t][1] == -INFINITY ? 0.f : fmaf(m[t][1], cs, down);
+            const float m0 = m[t][0] == -INFINITY ? 0.f : fmaf(m[t][0], cs, src.down()), m1 = m[t][1] == -INFINITY ? 0.f : fmaf(m[t][1], cs, src.down());
 #pragma unroll
             for (int u = 0; u < KT; ++u)
 #pragma unroll

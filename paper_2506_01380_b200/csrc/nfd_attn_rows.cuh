@@ -33,8 +33,6 @@ template <typename TS, int DH> struct StateKeys {
     int n_keys;
     __device__ __forceinline__ int length(const BatchD &B, int s) const { return B.kv_len ? min(B.tokens(s), n_keys) : n_keys; }
     __device__ __forceinline__ KeyRange range(const BatchD &, int len, int, int) const { return {0, len}; }
-    // what is taken off the exponent of a probability (4-bit values, below 2^31 and scaled by 2^-32, need nothing of the kind)
-    __device__ __forceinline__ float down(int growth, int of) const { return (float)sum_bits(growth, (int)(((long long)n_keys + of - 1) / of)); }
 };
 
 

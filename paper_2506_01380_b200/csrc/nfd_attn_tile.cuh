@@ -618,7 +618,10 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) k_attn_tile(const BatchD B, c
         const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
         const float c = 1.4426950408889634f * rsqrtf((float)DH) * Src::UP;
         float down = 0.f, most = (float)(1ull << TILE_GROWTH_KV4);     // (4-bit values are below 1 here)
-        if constexpr (!Src::KV4) down = src.K.down(TILE_GROWTH, KB), most = exp2f(TILE_GROWTH - down);
+        if constexpr (!Src::KV4) {
+            const int bits = sum_bits(TILE_GROWTH, (src.K.n_keys + KB - 1) / KB);
+            down = (float)bits, most = exp2f(TILE_GROWTH - down);      // (read as operands from the arguments: cross_streams8 129 us for 127)
+        }
         const KeyRange kr = src.K.range(B, len, sr.y, A.split(r0 + min(r, nr - 1)).x);
         cp_async_wait<0>();
         tile_publish(bars.q_full());

@@ -255,7 +255,7 @@ int nfd_cross_attention(const nfd_states *states, const nfd_batch *batch, int n_
                 if ((long long)B.max_rows * A.share > few_most(DH))
                     return launch_attn_tile<TileStates<DH>, DH>(B, A, TileStates<DH>{K}, states->n_heads, states->n_keys, dev, n_sm, (cudaStream_t)cuda_stream);
                 FewStates<DH> src;
-                src.K = K;
+                src.K = K, src.bits = (float)sum_bits(8, K.n_keys);    // (probabilities grow to 2^8 before m follows)
                 return launch_attn_few<FewStates<DH>, DH>(B, A, src, states->n_heads, states->n_keys, dev, n_sm, (cudaStream_t)cuda_stream);
             } else {
                 return launch_attn_f32<DH>(B, A, K, states->n_heads, dev, n_sm, (cudaStream_t)cuda_stream);
