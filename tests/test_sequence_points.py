@@ -6,14 +6,17 @@ CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
 
 
 def _conditions(text):
-    """What stands in the parentheses of every if, while and for, comments removed."""
+    """What stands in the parentheses of every if, while and for, comments and the bodies of functions in them removed."""
     text = re.sub(r"//[^\n]*", "", text)
     for m in re.finditer(r"\b(?:if(?: constexpr)?|while|for)\s*\(", text):
         depth, j = 1, m.end()
         while depth:
             depth += {"(": 1, ")": -1}.get(text[j], 0)
             j += 1
-        yield text[m.end():j - 1]
+        condition = text[m.end():j - 1]
+        while "{" in condition:
+            condition = re.sub(r"\{[^{}]*\}", "", condition)
+        yield condition
 
 
 def test_no_condition_counts_on_and_reads_a_counter_in_no_order():
