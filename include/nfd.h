@@ -223,8 +223,9 @@ int nfd_attention_noalloc(const void *q, const void *k_pages, const void *v_page
 
 /* ---------------------------------------------------------------------------
  * Calls for callers that bring their own cache, for several sequences at once.
- * (The paper has no counterpart of them, but for its cross-attention variant of
- * the conditioning, Section 3.1.)  Like nfd_attention_noalloc they need no
+ * (The paper has no counterpart of them: cross attention it considers for the
+ * conditioning on time and action, Section 3.1, and takes adaLN-zero instead.  No pass of
+ * a context calls them.)  Like nfd_attention_noalloc they need no
  * context, allocate nothing and call no allocating library routine; unlike it
  * they have no working memory at all: calls may overlap on the GPU, on any
  * streams, and be captured into graphs.  Everything that changes from call to

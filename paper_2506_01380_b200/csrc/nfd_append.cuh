@@ -1,12 +1,14 @@
 // Rows into a paged cache, rotated and, where the pages hold 4 bits, quantised on the way; and back out of it.
 //
-// Bound by memory: every number of the new rows is read once and written once; with 4-bit pages by instructions.  A CTA takes `rows` rows (one
+// Every number of the new rows is read once and written once; what bounds it is latency, not a rate (figures below).  A CTA takes `rows` rows (one
 // where that leaves SMs idle otherwise) with all their heads, so that the angles of a row (64-bit arithmetic, head_dim / 2 sines and
 // cosines) are formed once for all of its heads.  A thread has a place in the rows, eight numbers of a head (16 bytes of bf16, four
 // pairs of the rotation, a word of 4-bit codes; four neighbouring lanes hold a group of 32), and takes it in one row after the other: what
 // depends on the place is worked out once.  The first loads are issued before the rows' sequences, places and angles are looked up.
-// Measured, 16 heads x 64 with q: 336 rows into bf16 pages 4.3 us, eight single rows 3.7 (a launch that does nothing takes 2.5); 10752 rows into
-// 4-bit pages and back out of them 51 us for the two calls (144 MB, 2.8 TB/s).
+// Measured, 16 heads x 64 with q: 336 rows into bf16 pages 4.3 us, eight single rows 3.7 (a launch that does nothing takes 2.5).  10752 rows, in and back
+// out: fp32 pages 51 us (5.1 TB/s) and 33 (5.3), bf16 36 (3.7) and 24 (3.7), bf16 rows in 4-bit pages 40 (2.5) and 14 (4.0), fp32 rows in them 45 (4.2)
+// and 29 (3.5).  Under the profiler both kernels of 4-bit pages issue in 62 % of the clocks and their warps wait for loads and for shared memory as long; the
+// append has 40 % of an SM's warps, 64 registers a thread (with bf16 rows it spills 8 bytes of them).
 #pragma once
 #include "nfd_paged.cuh"
 

@@ -3,12 +3,12 @@
 // k_attn_f32: a CTA takes 32 or 64 rows (rows x heads that share a head of keys) of a sequence and walks its keys in tiles of 64, the next tile's copies in
 // flight: S = Q K^T with 4 rows x 4 keys to a thread, an online softmax per row over the 16 lanes that hold it, P through shared memory
 // (a row's 16 lanes write and read it, no barrier), O += P V with 4 rows x DH / 16 dims to a thread.  All operands are read as 16-byte words
-// along their rows, rows are padded by one word so that no two lanes of a quarter warp meet in a bank: 64 FMAs for eight words either way, which keeps
-// the FMA pipe ahead of the shared-memory port.  Keys that are not seen are copied as zeros and take a score of -inf.
+// along their rows, rows are padded by one word so that no two lanes of a quarter warp meet in a bank.  Keys that are not seen are copied as zeros and take a score of -inf.
 // Probabilities are scaled down by a power of two (sum_bits), which no result shows but those whose sums would have left fp32.
 // Few units with many keys are split over the CTAs of a cluster and merged through distributed shared memory.
-// Bound by FMAs for many rows, by the chain of a tile (copy, S, softmax, P V) for few, which k_attn_f32_few takes.  Measured: four sequences of 1344
-// rows, 16 heads x 64, against up to 1000 states 665 us (33 TFLOP/s of 72); three of 77 rows, 6 heads x 32, against up to 220, 6.9 us.
+// For many rows at 46 % of the FMA pipes' rate (eight 16-byte words from shared memory for 64 FMAs either way; what else holds it has not been taken
+// apart), for few bound by the chain of a tile (copy, S, softmax, P V), and so k_attn_f32_few takes them.  Measured: four sequences of 1344
+// rows, 16 heads x 64, against 1000 states 667 us (33 TFLOP/s of 72); three of 77 rows, 6 heads x 32, against up to 220, 7.0 us.
 #pragma once
 #include "nfd_attn_few.cuh"
 

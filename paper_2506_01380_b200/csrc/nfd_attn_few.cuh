@@ -13,9 +13,10 @@
 // so that what a key costs does not grow with the 16 rows of a tile (with the rows on that side: twice the products and twice the registers
 // for rows that are not there).  P^T changes sides by movmatrix.  The inner index of either product may be permuted as long as both of its
 // operands are, so that a lane's share of a key is a run of its row (for S) and a lane's share of a value a run of dims
-// (for O); 4-bit codes become bf16 numbers in registers (Kv4Scale).
-// Measured: one row, 16 heads x 64, behind 5712 tokens in 4-bit pages 9.9 us (pieces, merge and launch; 6.6 MB); eight sequences of up to 32768
-// tokens, 24 heads on 8 x 128, 84 us (185 MB, 2.2 TB/s); bf16 states, eight rows, 16 heads x 64 against 4096 26 us (134 MB, 5.2 TB/s).
+// (for O); 4-bit codes become bf16 numbers in registers (Kv4Scale).  P is rounded to one bf16 number, as in the kernel for many rows.
+// Measured: one row, 16 heads x 64, behind 5712 tokens in 4-bit pages 10.0 us (pieces, merge and launch; 6.6 MB); eight sequences of up to 32768
+// tokens, 24 heads on 8 x 128, 84.5 us (185 MB, 2.2 TB/s: nothing is saturated, 48 % of the issue slots, 28 % of the copy rate; latency, and lengths that
+// differ); bf16 states, eight rows, 16 heads x 64 against 4096 25.4 us (134 MB, 5.3 TB/s).
 #pragma once
 #include "nfd_attn_rows.cuh"
 #include "nfd_sm100.cuh"

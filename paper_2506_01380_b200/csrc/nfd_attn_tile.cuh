@@ -19,13 +19,19 @@
 // softmax groups.  Which keys of a block are there is told beside K, a bit each, in a ring of its own: the softmax does not wait for V.
 //
 // A unit (sequence, head of keys, tile) with many keys and few others beside it is split over the CTAs of a cluster, which
-// merge through distributed shared memory.  Every wait is bounded; after one that ran out the rows are NaN.
+// merge through distributed shared memory.  Every wait on a barrier in memory is bounded; after one that ran out the rows are NaN.  (The cluster's own
+// barrier has no bound and needs none: every CTA comes to it, its other waits being bounded, or has left as a whole cluster.)
 //
-// Bound by the special-function unit and the issue slots beside it (4-bit pages: the producers' conversions; a fifth of the exponentials by a
-// polynomial on the FMA pipe made 202 us 207), with head dimension 128 by the two warps a scheduler has for the chain S - P - P V.
-// Measured, 16 heads x 64: 336 rows behind 5712 tokens in 4-bit pages 28.5 us (276 TFLOP/s: the beginning, 18 blocks, the merge), eight
-// streams of 336 rows behind 11088 202 us (604 TFLOP/s); 16 heads on 4 x 128, eight batches of 1344 rows against up to 2048 states 126 us
-// (620 TFLOP/s).
+// P is one bf16 number.  (k_attn_tc carries it as two and doubles its second product for that, 9 to 16 % of its time; here the error of a result is 2.3e-3,
+// 2-norm, normal data, for 1.66e-3 of one that is only rounded at the end.  4-bit numbers are themselves off by some 8 % of their group's deviation.)
+//
+// Nothing is saturated: with 4-bit pages and head dimension 64 an SM that has a CTA gives the special-function unit 62 % of its clocks and issues in 54 %
+// of them (a fifth of the exponentials by a polynomial on the FMA pipe made 202 us 207), with head dimension 128 it issues in 44 % and the tensor pipe
+// has 30 %.  What is left is the chain S - P - P V of few warps: three to a scheduler, two with head dimension 128.  (512 threads
+// have 128 registers each; head dimensions 32 and 64 spill 16 to 24 bytes of them.)
+// Measured, 16 heads x 64: 336 rows behind 5712 tokens in 4-bit pages 28.7 us (274 TFLOP/s: 96 CTAs, 12 blocks of three tiles each, the merge), eight
+// streams of 336 rows behind 11088 202 us (604 TFLOP/s; 128 CTAs on 148 SMs); 16 heads on 4 x 128, eight batches of 1344 rows against up to 2048 states
+// 126.5 us (620 TFLOP/s).
 #pragma once
 #include "nfd_attn_few.cuh"
 
