@@ -327,6 +327,85 @@ int nfd_pages_read(const nfd_pages *pages, const nfd_batch *batch, int dtype, vo
 int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,
                       int frame_tokens, int window, void *out, void *cuda_stream);
 
+/* The same over a cache of NFD_DTYPE_BF16 or NFD_DTYPE_FP32 pages, from single rows
+ * to chunks of any length: q, out, n_heads, mask, scale and rows that see nothing as
+ * in nfd_attention_kv4, q and out of the pages' type.  What a row does not see may
+ * be anything, NaN included; a NaN or an infinity among the values that it does see makes
+ * its column of that row NaN or infinite, however small its probability.  Values
+ * may be as large as their type goes: a result, being a mean of them, is finite
+ * with them.  (Small values: with up to 2^20 keys, values below 2^-56 may lose bits in
+ * the sums.)  fp32 is computed on the fp32 pipes; with bf16, scores, softmax and sums are fp32
+ * and probabilities are rounded to bf16 for the product with V. */
+int nfd_attention_pages(const nfd_pages *pages, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,
+                        int frame_tokens, int window, void *out, void *cuda_stream);
+
+/* Attention over whole prompts: the rows of a sequence are its tokens 0, 1, ..., and
+ * every row sees rows of its own sequence under the same mask (token p sees the
+ * tokens of the frames max(0, p / frame_tokens - window) .. p / frame_tokens that there
+ * are; frame_tokens = 1: causal; a frame as long as the sequence: all of it).  The batch's
+ * row_start says where sequences begin, in ascending order; kv_len and table are not looked
+ * at.  A sequence may have more rows than max_rows: the first max_rows are
+ * computed, and what they see of the others counts.  q dev [n_rows][n_heads][head_dim],
+ * k and v dev [n_rows][kv_heads][head_dim] of `dtype` (NFD_DTYPE_FP32 or
+ * NFD_DTYPE_BF16), each with a stride in elements from row to row, so that the three
+ * may be parts of one projection's output; out dev [n_rows][n_heads * head_dim], not one of
+ * them.  n_heads is a multiple of kv_heads, head_dim in {32,64,128}.  Everything else as in
+ * nfd_attention_pages. */
+int nfd_attention_packed(const nfd_batch *batch, int dtype, int n_heads, int kv_heads, int head_dim, const void *q, long long q_stride,
+                         const void *k, long long k_stride, const void *v, long long v_stride, int frame_tokens, int window, void *out,
+                         void *cuda_stream);
+
+/* Rotary embedding of rows whose positions are given: positions dev [n_rows][3] (whole numbers, of
+ * either sign: time, height, width of a token), rope_t, rope_h, rope_w of `rope` numbers of
+ * every head turning with each (even, sum == head_dim; frame_tokens and grid_w are not looked
+ * at).  Pair i of an axis of n numbers turns by position * theta^(-2 i / n).  x dev
+ * [n_rows][n_heads][head_dim] of `dtype` (NFD_DTYPE_FP32 or NFD_DTYPE_BF16) goes to x_out, x2
+ * [n_rows][n_heads2][head_dim] to x2_out (queries and keys; either may have 0 heads), each with
+ * its stride in elements from row to row; an output may be its own input (with the same stride),
+ * and shares no memory with the inputs otherwise.  head_dim: a multiple of 16, up to 256.
+ * flags: NFD_ROTATE_HALVES: pair i is numbers i and i + head_dim / 2 of a head, otherwise the
+ * library's adjacent pairs 2 i and 2 i + 1 (the axes share the pairs in order either way);
+ * NFD_ROTATE_BACK: by the angle's negative, which undoes the rotation and is its
+ * gradient.  The angle of a pair is formed and reduced to a turn in 64 bits; sine, cosine and rotation are
+ * fp32. */
+#define NFD_ROTATE_HALVES 1
+#define NFD_ROTATE_BACK 2
+int nfd_rotate(const nfd_rope *rope, int flags, int dtype, int head_dim, int n_rows, const int *positions, int n_heads, const void *x,
+               long long x_stride, void *x_out, long long x_out_stride, int n_heads2, const void *x2, long long x2_stride, void *x2_out,
+               long long x2_out_stride, void *cuda_stream);
+
+/* The norms around a block, its gate and its residual scale, row by row:
+ *     t = post(y),   x_out = x + res_scale * gate * t,   h = pre(x_out) * (1 + scale) + shift
+ * x and x_out dev [n_rows][width] of x_dtype (the residual stream; x_out may be x), y (what the
+ * block's projection gave) and h (the next projection's operand; may be y) of `dtype`, both
+ * NFD_DTYPE_FP32 or NFD_DTYPE_BF16, each with a stride in elements from row to row.  Without
+ * y (NULL) there is no residual: h = pre(x) * (1 + scale) + shift, x_out, post and
+ * gate are not looked at; without h the call ends at x_out.  post NULL: t = y.  pre and post:
+ * LayerNorm (mean and variance) or RMSNorm (mean square), eps inside the root, times `weight`, plus `bias`
+ * (dev [width] of the norm's dtype, either may be NULL).  gate, scale and shift: dev [n_mods][width] of the modulation's
+ * dtype, `stride` elements from row to row (parts of one projection's output), any of them
+ * NULL: 1, 0, 0; row r has modulation index[r] (dev; kept into 0 .. n_mods - 1) or, with index NULL,
+ * r / rows_per_mod; mod NULL: none.  width: a multiple of 8, up to NFD_MAX_WIDTH.  Everything is
+ * computed in fp32, from the numbers as they are given, and rounded once where it is stored: h is the norm of the
+ * sum before x_out's rounding. */
+#define NFD_NORM_LAYER 0
+#define NFD_NORM_RMS 1
+#define NFD_MAX_WIDTH 16384
+typedef struct {
+    int kind, dtype;                                    /* NFD_NORM_*, NFD_DTYPE_FP32 or _BF16   */
+    float eps;
+    const void *weight, *bias;                          /* dev [width], or NULL                 */
+} nfd_norm;
+typedef struct {
+    const void *gate, *scale, *shift;                   /* dev [n_mods][width], or NULL         */
+    long long stride;
+    const int *index;                                   /* dev [n_rows], or NULL                */
+    int n_mods, rows_per_mod, dtype;
+} nfd_modulation;
+int nfd_gate_norm(int n_rows, int width, int x_dtype, const void *x, long long x_stride, int dtype, const void *y, long long y_stride,
+                  void *x_out, long long x_out_stride, void *h, long long h_stride, const nfd_norm *post, const nfd_norm *pre,
+                  const nfd_modulation *mod, float res_scale, void *cuda_stream);
+
 /* The states of an encoder, as keys and values: k and v dev, of dtype
  * NFD_DTYPE_FP32 or NFD_DTYPE_BF16, element strides from sequence to sequence (0:
  * all sequences share one set), from key to key and from head to head; head_dim is contiguous.

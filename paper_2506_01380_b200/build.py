@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnfd.so")
-SOURCES = ["nfd_api.cu", "nfd_paged.cu"]
+SOURCES = ["nfd_api.cu", "nfd_paged.cu", "nfd_attn_pages.cu", "nfd_rows.cu"]
 
 
 def _nvcc() -> str:
@@ -37,7 +37,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     cmd = [
         _nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-        "-shared", "-Xcompiler", "-fPIC",
+        "-shared", "-Xcompiler", "-fPIC", "-t", "0",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC,
         "-o", LIB,
     ] + [os.path.join(CSRC, s) for s in SOURCES]

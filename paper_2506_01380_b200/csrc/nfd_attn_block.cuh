@@ -1,0 +1,708 @@
+// Attention of many rows under the block-wise causal mask on tcgen05 / TMEM, to bf16 pages or to the rows of packed prompts.
+//
+// The rows of a sequence that share a head of keys (rows x heads that share it) are cut into tiles of 128; a CTA takes two of them, which share
+// every copied block of keys, or one, whose blocks its two softmax groups take in turn.  Each group has S accumulators, O, m and l of its own:
+//     S = Q K^T     UMMA 128 x KB x DH, operands in shared memory, accumulator in tensor memory
+//     P = exp2(S c - m)   one thread per row: S to registers, exponentials, P as bf16 over the S it came from
+//     O += P V      UMMA 128 x head_dim x KB, P from tensor memory, V as it lies (MN-major)
+// m is the largest of the first 16 scores that a row sees, and no other maximum is taken: a probability is exact to the same number of bits whatever its
+// size.  Where a sum of a row passes 2^50 after all (or is NaN), or a row has no m yet, the warp takes its keys again, S being untouched so far: the
+// maximum first, and where it has risen by more than 8 (a factor of 256) it becomes m and the row's O is rescaled in tensor memory.  What P grows to, O
+// does, and values may be as large as bf16 goes, so that P is scaled down by as much as all blocks together can grow (sum_bits), in the exponent.
+//
+// A tile walks the blocks that its own rows see, and no others; in a block that only some rows see the others' scores become -inf.  There P is 0, which
+// keeps keys out and not values: 0 x NaN is NaN.  So in blocks that not all rows of a CTA see, the producers take values that are not finite out of V and
+// note where; a row that does see one adds it to its result at the end.
+//
+// Warps 0 .. 3 fill a ring of K and V blocks in turn with cp.async, several blocks in flight, a lane looking up the place of each key; warp 4 issues the
+// products; the last 8 are the softmax groups.  Which keys of a block are there is told beside K, a bit each, in a ring of its own.
+//
+// A unit (sequence, head of keys, tiles) with many keys and few others beside it is split over the CTAs of a cluster, which merge through distributed
+// shared memory in a fixed order.  Every wait on a barrier in memory is bounded; after one that ran out the rows are NaN.  (The cluster's own barrier needs
+// no bound: every CTA comes to it, its other waits being bounded, or has left as a whole cluster.)
+#pragma once
+#include "nfd_attn_tile.cuh"
+
+#define BLOCK_THREADS 512
+#define BLOCK_SPLIT 8               // most CTAs of a cluster
+#define BLOCK_SORTED 128            // sequences whose tiles are dealt out deepest first
+#define BLOCK_GROWTH 50             // bits that a sum may grow by before m follows it
+
+template <int DH> struct BlockCfg {
+    static constexpr int SUB = DH == 128 ? 2 : 1;          // 64-dim parts of a row
+    static constexpr int KB = DH == 128 ? 128 : 96;        // keys of a block
+    static constexpr int NBG = DH == 128 ? 1 : 2;          // S accumulators of a group
+    static constexpr int PARTS = DH == 128 ? 2 : 1;        // a block's P goes to its product in so many parts
+    static constexpr int HK = KB / PARTS;
+    static constexpr int PW = 4, KPW = KB / PW;            // producer warps, keys of each
+    static constexpr int SM0 = 8;                          // first softmax warp
+    static constexpr int NST = DH == 128 ? 5 : 12;         // stages of the ring: K and V of the first block, of the second ...
+    static constexpr int FLY = DH == 128 ? 3 : 5;          // of which the copies are in flight
+    static constexpr int NM = 16;                          // masks
+    static constexpr int Q_BYTES = SUB * 128 * 128;        // a tile's queries
+    static constexpr int BLK = SUB * KB * 128;             // a block of K or V
+    static constexpr int AT_Q = 0, AT_R = 2 * Q_BYTES, AT_MASK = AT_R + NST * BLK, AT_BAR = AT_MASK + NM * 16, SMEM = AT_BAR + 512 + 1024;
+    static constexpr int TM_O = 2 * NBG * KB;              // S of group g, number i, and over it P, at (g NBG + i) KB; O of group g at TM_O + g 64 SUB
+    static constexpr int STATE = 128 * DH * 4 + 128 * 8;   // a group's state, over queries and ring: O as [DH / 4][128] float4, then [128] (m, l)
+    static_assert(TM_O + 2 * 64 * SUB <= 512 && 2 * STATE + 128 * 8 <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
+    static_assert(SMEM > 232448 / 2, "a CTA has an SM, and its tensor memory, to itself: nobody in a cluster waits for what another cluster holds");
+    static_assert(2 * NBG + NST / 2 + 1 <= NM, "K runs so many blocks ahead of the softmax");
+    static_assert(KPW * (DH / 8) % 32 == 0 && KPW <= 32 && KPW % 8 == 0 && HK % 32 == 0, "copies; bits of a warp's keys are whole bytes; S by 32 columns");
+};
+
+struct BlockBars {
+    uint32_t b;
+    __device__ __forceinline__ uint32_t full(int s) const { return b + 8 * s; }                  // stages (up to 12)
+    __device__ __forceinline__ uint32_t empty(int s) const { return b + 96 + 8 * s; }
+    __device__ __forceinline__ uint32_t m_full(int s) const { return b + 192 + 8 * s; }          // masks (16)
+    __device__ __forceinline__ uint32_t s_full(int g, int i) const { return b + 320 + 16 * g + 8 * i; }
+    __device__ __forceinline__ uint32_t p_full(int g, int i) const { return b + 352 + 16 * g + 8 * i; }   // of an accumulator, or of its parts
+    // of a group's even and odd parts: a warp may be done with one before the product of the one before it is
+    __device__ __forceinline__ uint32_t pv_done(int g, int n) const { return b + 384 + 16 * g + 8 * (n & 1); }
+    __device__ __forceinline__ uint32_t q_full() const { return b + 416; }
+    __device__ __forceinline__ void init(int stages, int producers) const {
+        for (int s = 0; s < stages; ++s) mbar_init(full(s), producers), mbar_init(empty(s), 1);
+        for (int s = 0; s < 16; ++s) mbar_init(m_full(s), producers);
+        for (int g = 0; g < 2; ++g)
+            for (int i = 0; i < 2; ++i) mbar_init(s_full(g, i), 1), mbar_init(p_full(g, i), 4), mbar_init(pv_done(g, i), 1);
+        mbar_init(q_full(), 8);
+        fence_mbar_init();
+    }
+};
+
+// What a CTA works on: keys lo .. hi - 1 of a sequence in nb blocks; keys that not all rows see: those below
+// edge_lo, those from edge_hi on.
+struct BlockWork {
+    int s, h, first_row, lo, hi, nb, T, edge_lo, edge_hi;
+    int end0, begin1;                                       // two tiles: the first takes the blocks before end0, the second those from begin1 on
+    // does group g take block b (one tile: they take turns)
+    __device__ __forceinline__ bool takes(int g, int b) const { return T == 2 ? (g ? b >= begin1 : b < end0) : (b & 1) == g; }
+};
+template <int n> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(n)); }
+template <int n> __device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(n)); }
+
+// ---- producers ----------------------------------------------------------------------------------------------
+template <int DH, typename Keys>
+static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD &B, const BlockWork &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
+    using C = BlockCfg<DH>;
+    constexpr int CPR = DH / 8, N = C::KPW * CPR / 32;       // 16-byte pieces of a row; a lane's of a block
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % CPR, sub = lane / CPR;
+    // (rows sub, sub + RPI, ... of the warp's, whose first is a multiple of 8: bits of the row above sub only flip bits of the piece)
+    constexpr int RPI = 32 / CPR;
+    const uint32_t to0 = (piece >> 3) * (C::KB * 128) + tile_at(warp * C::KPW + sub, piece & 7);
+    auto to = [&](int i) -> uint32_t { return (to0 ^ ((i * RPI & 7) << 4)) + i * RPI * 128; };
+    int p = w.lo + warp * C::KPW + lane;
+    auto cur = K.cursor(B, w.s, w.first_row, p, C::KB);
+    auto look_up = [&]() -> long long {
+        const long long row = K.next(cur, B, w.h, lane < C::KPW && p < w.hi);
+        p += C::KB;
+        return row;
+    };
+    long long next = look_up();
+    int done = 0, item = 0;                                  // published, begun
+    auto publish = [&]() {
+        const int st = done % C::NST, p0 = w.lo + (done >> 1) * C::KB;
+        cp_async_wait_upto(item - done - 1);
+        if ((done & 1) && (p0 < w.edge_lo || p0 + C::KB > w.edge_hi)) {
+            bool some = false;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint4 *v = reinterpret_cast<uint4 *>(smem + C::AT_R + st * C::BLK + to(i));
+                const uint4 x = *v;
+                const uint4 f = make_uint4(finite_bits(x.x), finite_bits(x.y), finite_bits(x.z), finite_bits(x.w));
+                if ((f.x & f.y & f.z & f.w) != 0xffffffffu) *v = make_uint4(x.x & f.x, x.y & f.y, x.z & f.z, x.w & f.w), some = true;
+            }
+            if (some) atomicMin(bad, p0), atomicMax(bad + 1, p0 + C::KB);
+        }
+        tile_publish(bars.full(st)), ++done;
+    };
+    for (int b = 0; b < w.nb && ok; ++b) {
+        const long long row = next;
+        const uint32_t there = __ballot_sync(0xffffffffu, row >= 0);
+        next = look_up();
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            const int st = item % C::NST;
+            if (item >= C::NST) {
+                const uint32_t par = (item / C::NST - 1) & 1;
+                // (nothing is held back while waiting: what frees this stage may need it)
+                while (!__all_sync(0xffffffffu, tile_test(bars.empty(st), par))) {
+                    if (done < item) {
+                        publish();
+                    } else {
+                        ok = __all_sync(0xffffffffu, tile_wait(bars.empty(st), par));
+                        break;
+                    }
+                }
+                if (!ok) break;
+            }
+            const uint32_t dst = smem_u32(smem) + C::AT_R + st * C::BLK;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const long long r = __shfl_sync(0xffffffffu, row, i * RPI + sub);
+                const bf16 *src = (kv ? K.v_row(r < 0 ? 0 : r, w.h) : K.k_row(r < 0 ? 0 : r, w.h)) + piece * 8;
+                cp_async16(dst + to(i), src, r < 0 ? 0 : 16);
+            }
+            cp_async_commit();
+            if (!kv) {
+                uint8_t *M = smem + C::AT_MASK + b % C::NM * 16 + warp * (C::KPW / 8);
+                if (lane < C::KPW / 8) M[lane] = (uint8_t)(there >> (8 * lane));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars.m_full(b % C::NM));
+            }
+            // (the first block is wanted at once)
+            ++item;
+            if (item - done > (item < 2 * C::FLY ? 2 : C::FLY)) publish();
+        }
+    }
+    while (ok && done < item) publish();
+}
+
+// ---- issuer -------------------------------------------------------------------------------------------------
+// All products of a CTA, by one thread.  A job is a block of a group, by blocks and then by groups; the S of a job is issued as soon as the P V that
+// reads its accumulator's last P has been: the tensor pipe takes one thread's instructions in order.
+template <int DH> static __device__ __forceinline__ bool block_issue(const BlockWork &w, const BlockBars &bars, uint32_t base, uint32_t tmem) {
+    using C = BlockCfg<DH>;
+    constexpr int KB = C::KB, SUB = C::SUB, NST = C::NST, NBG = C::NBG;
+    constexpr uint32_t idesc_s = umma_idesc_bf16(128, KB), idesc_pv = umma_idesc_bf16(128, DH) | (1u << 16);       // V: MN-major
+    // (a cluster's addresses hold the CTA's rank above bit 23; V's other 64 dims are KB rows on: the leading offset)
+    const uint32_t at = base & 0x3ffffu, dQ = (at + C::AT_Q) >> 4, dR = (at + C::AT_R) >> 4, lead = (KB * 128 >> 4) << 16;
+    bool ok = tile_wait(bars.q_full(), 0);
+    int sb = 0, sg = 0, ns0 = 0, ns1 = 0, np0 = 0, np1 = 0; // next S: block, group; jobs of a group so far
+    auto scores = [&]() {                                    // issues what may be issued
+        while (ok && sb < w.nb) {
+            if (!w.takes(sg, sb)) {
+                if (++sg == 2) sg = 0, ++sb;
+                continue;
+            }
+            int &n = sg ? ns1 : ns0;
+            if (n >= (sg ? np1 : np0) + NBG) return;
+            const int item = 2 * sb, st = item % NST;
+            if (!(sg == 1 && w.takes(0, sb))) ok = ok && tile_wait(bars.full(st), (item / NST) & 1);
+            if (!ok) return;
+            tc_fence_after();
+            const int i = NBG == 1 ? 0 : n & 1;
+            const uint32_t q = dQ + (w.T == 1 ? 0 : sg) * (C::Q_BYTES >> 4), k = dR + st * (C::BLK >> 4), d = tmem + (sg * NBG + i) * KB;
+#pragma unroll
+            for (int e = 0; e < (DH + 15) / 16; ++e)
+                tile_mma_ss(d, q + (e >> 2) * (128 * 128 >> 4) + 2 * (e & 3), k + (e >> 2) * (KB * 128 >> 4) + 2 * (e & 3), idesc_s, e != 0);
+            umma_commit(bars.s_full(sg, i));
+            if (!(sg == 0 && w.takes(1, sb))) umma_commit(bars.empty(st));
+            ++n;
+            if (++sg == 2) sg = 0, ++sb;
+        }
+    };
+    scores();
+    for (int b = 0; b < w.nb && ok; ++b) {
+        const int item = 2 * b + 1, st = item % NST;
+        const uint32_t v = (dR + st * (C::BLK >> 4)) | lead;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            if (!ok || !w.takes(g, b)) continue;
+            if (!(g == 1 && w.takes(0, b))) ok = ok && tile_wait(bars.full(st), (item / NST) & 1);
+            int &n = g ? np1 : np0;
+            const int i = NBG == 1 ? 0 : n & 1;
+            const uint32_t d = tmem + C::TM_O + g * 64 * SUB, a = tmem + (g * NBG + i) * KB;
+#pragma unroll
+            for (int part = 0; part < C::PARTS; ++part) {
+                ok = ok && tile_wait(bars.p_full(g, C::PARTS == 1 ? i : part), (n / NBG) & 1);
+                if (!ok) break;
+                tc_fence_after();
+                constexpr int E = C::HK / 16;
+#pragma unroll
+                for (int e = part * E; e < (part + 1) * E; ++e) tile_mma_ts(d, a + 8 * e, v + e * (2048 >> 4), idesc_pv, n != 0 || e != 0);
+                umma_commit(bars.pv_done(g, n * C::PARTS + part));
+            }
+            if (!ok) break;
+            if (!(g == 0 && w.takes(1, b))) umma_commit(bars.empty(st));
+            ++n;
+            scores();
+        }
+    }
+    return ok;
+}
+
+// ---- softmax ------------------------------------------------------------------------------------------------
+// A part of a block whose sums have outgrown m, or that finds a row without one: the row's maximum over the keys that it sees, m and what has been
+// summed so far adjusted to it, then P.  seen: bits of the keys that the row sees; n: the group's parts before this one; pv_done: of the last of them.
+template <int DH>
+static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint32_t tO, const uint32_t *seen, float c, float down, int n, uint32_t pv_done,
+                                               float &m_io, float &l_io, bool &ok) {
+    constexpr int HK = BlockCfg<DH>::HK;
+    float m = m_io, l = l_io, top = -INFINITY;
+    auto bits = [&](int i) { return (i < 32 ? seen[0] : i < 64 ? seen[1] : seen[2]) >> (i & 31); };
+#pragma unroll 1
+    for (int i = 0; i < HK; i += 16) {
+        float x[16];
+        tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
+        const uint32_t s = bits(i);
+        tmem_ld_wait();
+        loaded16(x);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s >> e & 1 ? x[e] : -INFINITY);
+    }
+    // (m starts at -inf: the first score that is seen sets it)
+    const bool rise = top * c > m * c + 8.0f || (m == -INFINITY && top != -INFINITY);
+    if (__any_sync(0xffffffffu, rise)) {
+        const float f = !rise ? 1.0f : m == -INFINITY ? 0.f : few_exp2((m - top) * c);
+        if (rise) m = top;
+        l *= f;
+        if (n) {
+            ok = ok && tile_wait(pv_done, ((n - 1) >> 1) & 1);         // O is at rest
+            __syncwarp();
+            tc_fence_after();
+#pragma unroll 1
+            for (int i = 0; i < DH; i += 16) {
+                float o[16];
+                tmem_ld16(tO + i, reinterpret_cast<uint32_t *>(o));
+                tmem_ld_wait();
+                loaded16(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] *= f;               // (f may be 0: a value that is not finite stays one)
+                tmem_st16(tO + i, reinterpret_cast<uint32_t *>(o));
+            }
+        }
+    }
+    const float mc = m == -INFINITY ? 0.f : fmaf(m, c, down);
+    float sum = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < HK; i += 16) {
+        float x[16];
+        tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
+        const uint32_t s = bits(i);
+        tmem_ld_wait();
+        loaded16(x);
+        uint32_t pk[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float a = s >> e & 1 ? few_exp2(fmaf(x[e], c, -mc)) : 0.f, b = s >> (e + 1) & 1 ? few_exp2(fmaf(x[e + 1], c, -mc)) : 0.f;
+            sum += a + b, pk[e / 2] = bf16_pair(a, b);
+        }
+        tmem_st8(tP + i / 2, pk);                                      // (behind what is still to be read)
+    }
+    m_io = m, l_io = l + sum;
+}
+// One pass over S against the m that there is, 32 columns at a time with the next load in flight (xa: the first ones, on their way).  MASKED: keys that
+// the row does not see count for nothing.  False: a sum has outgrown m (most: the most that it may be), and S is as it was.
+template <int DH, bool MASKED>
+static __device__ __forceinline__ bool block_fast(uint32_t tS, uint32_t tP, float *xa, const uint32_t *seen, float c, float mc, float most, float &l) {
+    constexpr int HK = BlockCfg<DH>::HK;
+    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    float xb[32];
+    uint32_t pk[HK / 2];
+#pragma unroll
+    for (int i = 0; i < HK; i += 32) {
+        float *x = (i >> 5) & 1 ? xb : xa;
+        tmem_ld_wait();
+        loaded32(x);
+        if (i + 32 < HK) tmem_ld32(tS + i + 32, reinterpret_cast<uint32_t *>((i >> 5) & 1 ? xa : xb));
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            float2 s = make_float2(x[2 * u], x[2 * u + 1]);
+            if (MASKED) s.x = seen[i >> 5] >> (2 * u) & 1 ? s.x : -INFINITY, s.y = seen[i >> 5] >> (2 * u + 1) & 1 ? s.y : -INFINITY;
+            const float2 e = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
+            const float2 p = make_float2(few_exp2(e.x), few_exp2(e.y));
+            ls[u & 1] = fadd2(ls[u & 1], p);
+            pk[i / 2 + u] = bf16_pair(p.x, p.y);
+        }
+    }
+    const float2 l2 = fadd2(ls[0], ls[1]);
+    const float sum = l2.x + l2.y;
+    if (!__all_sync(0xffffffffu, sum < most)) return false;
+    l += sum;
+#pragma unroll
+    for (int i = 0; i < HK / 2; i += 16) tmem_st16(tP + i, pk + i);
+    return true;
+}
+
+// ---- which tiles a CTA takes --------------------------------------------------------------------------------
+// Work item `slot` as (sequence, number of its unit of R rows); sequence -1: there is none.  The deepest units of all sequences come first: they
+// see the most keys, and what is dealt out last should be short.  Up to BLOCK_SORTED sequences of different lengths there are as many items as units;
+// otherwise as many as if all sequences had max_rows.
+static __device__ __forceinline__ int2 block_unit(const BatchD &B, int share, int R, long long slot) {
+    const int most = (int)(((long long)B.max_rows * share + R - 1) / R);
+    if (!B.row_start || B.n_seqs > BLOCK_SORTED) {
+        const int t = (int)(slot / B.n_seqs);
+        return make_int2(t < most ? (int)(slot - (long long)t * B.n_seqs) : -1, most - 1 - t);
+    }
+    const int lane = threadIdx.x & 31;
+    constexpr int N = BLOCK_SORTED / 32;
+    int t[N], all = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        t[i] = 0;
+        if (i * 32 < B.n_seqs && i * 32 + lane < B.n_seqs) t[i] = (int)(((long long)min(B.rows(i * 32 + lane).y, B.max_rows) * share + R - 1) / R);
+        all += t[i];
+    }
+    if (slot >= __reduce_add_sync(0xffffffffu, (unsigned)all)) return make_int2(-1, 0);
+    // the smallest depth j with no more than `slot` units deeper than it
+    int lo = 0, hi = most - 1;
+    auto deeper = [&](int j) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += max(0, t[i] - 1 - j);
+        return (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
+    };
+    while (lo < hi) {
+        const int j = (lo + hi) >> 1;
+        if (deeper(j) <= slot) hi = j;
+        else lo = j + 1;
+    }
+    int left = (int)slot - deeper(lo), s = -1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t m = __ballot_sync(0xffffffffu, t[i] > lo);
+        const int n = __popc(m);
+        if (s < 0 && left < n) {
+            const bool me = (m >> lane & 1) && __popc(m & ((1u << lane) - 1)) == left;
+            s = i * 32 + __ffs(__ballot_sync(0xffffffffu, me)) - 1;
+        }
+        left -= n;
+    }
+    return make_int2(s, lo);
+}
+
+// Grid: items x heads of keys x split (a cluster's CTAs).
+template <int DH, typename Keys>
+__global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B, const AttnRows A, const Keys K, int kv_heads, int split, int tiles, float down) {
+    using C = BlockCfg<DH>;
+    constexpr int KB = C::KB, SUB = C::SUB, NBG = C::NBG, HK = C::HK, PARTS = C::PARTS;
+    extern __shared__ uint8_t block_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(block_raw) + 1023) & ~(uintptr_t)1023);
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_expired, s_bad[2];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % split, hs = blockIdx.x / split;
+    const BlockBars bars = {smem_u32(smem + C::AT_BAR)};
+    if (threadIdx.x == 0) bars.init(C::NST, C::PW), s_expired = 0, s_bad[0] = INT_MAX, s_bad[1] = 0;
+    const int2 unit = block_unit(B, A.share, tiles * 128, hs / kv_heads);
+    if (unit.x < 0) return;                                 // (the whole cluster)
+    BlockWork w;
+    w.s = unit.x, w.h = hs % kv_heads;
+    const int r0 = unit.y * tiles * 128;
+    const int2 sr = B.rows(w.s);
+    const int len = K.length(B, w.s);
+    const int rows = min(sr.y, B.max_rows) * A.share;
+    if (r0 >= rows) return;                                 // (the whole cluster)
+    __syncthreads();
+    const int nr = min(tiles * 128, rows - r0), T = (nr + 127) / 128;
+    w.T = T, w.first_row = sr.x;
+    if (warp >= C::SM0) {
+        // softmax warps: the row's queries, into the operand of its tile, a row's pieces by neighbouring lanes; of one tile each group half
+        constexpr int CPR = DH / 8, RPI = 32 / CPR;
+        const int g = (warp - C::SM0) >> 2, piece = lane % CPR;
+        const uint32_t sq = smem_u32(smem + C::AT_Q) + (T == 1 ? 0 : g) * C::Q_BYTES + (piece >> 3) * (128 * 128);
+        for (int i = T == 1 ? g : 0; i < CPR; i += T == 1 ? 2 : 1) {
+            const int trow = (warp & 3) * 32 + i * RPI + lane / CPR, r = (T == 1 ? 0 : g * 128) + trow;
+            const int2 at = A.split(r0 + min(r, nr - 1));
+            const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + at.x) * A.q_stride + (w.h * A.share + at.y) * DH + piece * 8;
+            cp_async16(sq + tile_at(trow, piece & 7), q, r < nr ? 16 : 0);
+        }
+        cp_async_commit();
+    }
+    {
+        const KeyRange first = K.range(B, len, sr.y, A.split(r0).x), last = K.range(B, len, sr.y, A.split(r0 + nr - 1).x);
+        const int all = max(0, (last.hi - first.lo + KB - 1) / KB), per = (all + split - 1) / split;
+        w.lo = first.lo + min(all, rank * per) * KB;
+        w.nb = max(0, min(all - rank * per, per));
+        w.hi = min(last.hi, w.lo + w.nb * KB);
+        w.edge_lo = last.lo, w.edge_hi = first.hi;
+        if (T == 2) {
+            const KeyRange a = K.range(B, len, sr.y, A.split(r0 + 127).x), b = K.range(B, len, sr.y, A.split(r0 + 128).x);
+            // (no block is left out between the tiles' ranges: rows see themselves, and those before them what comes before)
+            w.end0 = min(w.nb, max(0, a.hi - w.lo + KB - 1) / KB), w.begin1 = min(max(0, b.lo - w.lo) / KB, w.end0);
+        }
+    }
+    const bool merge = split > 1 || (T == 1 && w.nb >= 2);  // a row's result is in several groups
+    uint32_t tmem = 0;
+    if (warp >= C::PW) {
+        // (the producers are on their way; the others wait for tensor memory)
+        if (warp == C::PW) {
+            tmem_alloc(smem_u32(&s_tmem), 512);
+            tmem_relinquish();
+        }
+        tc_fence_before();
+        asm volatile("bar.sync 2, %0;" ::"n"(BLOCK_THREADS - 32 * C::PW) : "memory");
+        tc_fence_after();
+        tmem = s_tmem;
+    }
+    bool ok = true;
+
+    // (registers of a thread: 64 + 48 + 2 x 200 of the 512 that four warps' threads were launched with)
+    if (warp < C::SM0) {
+        if (warp < C::PW) {
+            leave_registers<64>();
+            if (w.nb) block_produce<DH>(K, B, w, smem, bars, s_bad, ok);
+            if (!ok) s_expired = 1;
+            asm volatile("bar.arrive 1, %0;" ::"n"(256 + 32 * C::PW) : "memory");
+        } else {
+            leave_registers<48>();
+            if (warp == C::PW && w.nb) {
+                // (what the products' operands come from is the same in all lanes, and the compiler has to know it)
+                const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
+                BlockWork u;
+                u.nb = __shfl_sync(0xffffffffu, w.nb, 0), u.T = __shfl_sync(0xffffffffu, w.T, 0);
+                u.end0 = __shfl_sync(0xffffffffu, w.end0, 0), u.begin1 = __shfl_sync(0xffffffffu, w.begin1, 0);
+                if (elect_one()) {
+                    if (!block_issue<DH>(u, bars, base, tm)) s_expired = 1;
+                }
+            }
+        }
+    } else {
+        take_registers<200>();
+        // ---------------- softmax: a thread per row ----------------
+        const int g = (warp - C::SM0) >> 2, quad = warp & 3, trow = quad * 32 + lane, r = (T == 1 ? 0 : g * 128) + trow;
+        const uint32_t lane_off = (uint32_t)(quad * 32) << 16, tO = tmem + C::TM_O + g * 64 * SUB + lane_off;
+        const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
+        const float c = 1.4426950408889634f * rsqrtf((float)DH);
+        const float most = exp2f(BLOCK_GROWTH - down);
+        const KeyRange kr = K.range(B, len, sr.y, A.split(r0 + min(r, nr - 1)).x);
+        cp_async_wait<0>();
+        tile_publish(bars.q_full());
+        float m = -INFINITY, l = 0.f;                                  // m: reference, in units of scores
+        int n = 0;                                                     // the group's jobs so far
+        const int b_first = T == 1 ? g : g ? w.begin1 : 0, b_end = T == 2 && !g ? w.end0 : w.nb, b_step = T == 2 ? 1 : 2;
+        for (int b = b_first; b < b_end; b += b_step, ++n) {
+            const int i = NBG == 1 ? 0 : n & 1;
+            const uint32_t tJ = tmem + (g * NBG + i) * KB + lane_off;
+            ok = ok && tile_wait(bars.s_full(g, i), (n / NBG) & 1);
+            ok = ok && tile_wait(bars.m_full(b % C::NM), (b / C::NM) & 1);
+            __syncwarp();
+            tc_fence_after();
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+                if (some) {                                            // (of rows that are not there P may be anything)
+                    const uint32_t tS = tJ + part * HK, tP = tJ + part * (HK / 2);
+                    float xa[32];
+                    tmem_ld32(tS, reinterpret_cast<uint32_t *>(xa));   // (of use where the fast path is taken)
+                    const uint32_t *mask = reinterpret_cast<const uint32_t *>(smem + C::AT_MASK + b % C::NM * 16) + part * (HK / 32);
+                    const int p0 = w.lo + b * KB + part * HK;
+                    uint32_t seen[HK / 32], every = 0xffffffffu, any = 0;
+#pragma unroll
+                    for (int k = 0; k < HK / 32; ++k) seen[k] = mask[k], every &= seen[k];
+                    const bool all_whole = __all_sync(0xffffffffu, every == 0xffffffffu && p0 >= kr.lo && p0 + HK <= kr.hi);
+                    if (!all_whole) {
+                        const int a = kr.lo - p0, e = kr.hi - p0;      // keys a .. e - 1 of the part
+#pragma unroll
+                        for (int k = 0; k < HK / 32; ++k) {
+                            const int a1 = min(max(a - 32 * k, 0), 32), e1 = min(max(e - 32 * k, 0), 32);
+                            seen[k] &= (e1 == 32 ? 0xffffffffu : (1u << e1) - 1) & ~(a1 == 32 ? 0xffffffffu : (1u << a1) - 1);
+                            any |= seen[k];
+                        }
+                    } else {
+                        any = 1;
+                    }
+                    if (__any_sync(0xffffffffu, m == -INFINITY)) {
+                        // a row without m (nothing has been summed for it): the largest of the first scores will do, if it sees one of them
+                        tmem_ld_wait();
+                        loaded32(xa);
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) top = fmaxf(top, seen[0] >> e & 1 ? xa[e] : -INFINITY);
+                        if (m == -INFINITY) m = top;
+                    }
+                    bool done = false;
+                    if (__all_sync(0xffffffffu, m != -INFINITY || !any)) {
+                        const float mc = m == -INFINITY ? 0.f : fmaf(m, c, down);
+                        if (all_whole) {
+                            done = block_fast<DH, false>(tS, tP, xa, seen, c, mc, most, l);
+                        } else if (__any_sync(0xffffffffu, any)) {
+                            done = block_fast<DH, true>(tS, tP, xa, seen, c, mc, most, l);
+                        } else {                                       // none of the warp's rows sees any of these keys
+                            const uint32_t zero[16] = {};
+                            tmem_ld_wait();
+                            loaded32(xa);
+#pragma unroll
+                            for (int k = 0; k < HK / 2; k += 16) tmem_st16(tP + k, zero);
+                            done = true;
+                        }
+                    }
+                    if (!done) {
+                        tmem_ld_wait();
+                        block_slow<DH>(tS, tP, tO, seen, c, down, n * PARTS + part, bars.pv_done(g, n * PARTS + part - 1), m, l, ok);
+                    }
+                    tmem_st_wait();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars.p_full(g, PARTS == 1 ? i : part));
+            }
+        }
+        const int parts = n * PARTS;
+        if (n) ok = ok && tile_wait(bars.pv_done(g, parts - 1), ((parts - 1) >> 1) & 1);
+        __syncwarp();
+        tc_fence_after();
+        if (!ok) s_expired = 1;
+        asm volatile("bar.sync 1, %0;" ::"n"(256 + 32 * C::PW) : "memory");           // queries and ring are at rest, and what the producers found is told
+        const int2 at = A.split(r0 + r);
+        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH;
+        const float expired = s_expired || !ok ? NAN : 0.f;
+        const int late_lo = max(s_bad[0], kr.lo), late_hi = min(s_bad[1], kr.hi);      // keys among which there are values that were taken out
+        if (merge || (some && (T == 2 || g == 0))) {
+            const float inv = (l == 0.f ? 0.f : 1.0f / l) + expired;
+            uint8_t *state = smem + g * C::STATE;
+#pragma unroll 1
+            for (int i = 0; i < DH; i += 32) {
+                float o[32];
+                tmem_ld32(tO + i, reinterpret_cast<uint32_t *>(o));
+                tmem_ld_wait();
+                loaded32(o);
+                if (!n)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                for (int p = late_lo; p < late_hi && r < nr; ++p) {
+                    auto cur = K.cursor(B, w.s, sr.x, p, 1);
+                    const long long row = K.next(cur, B, w.h, true);
+                    if (row < 0) continue;
+                    const uint32_t *v = reinterpret_cast<const uint32_t *>(K.v_row(row, w.h) + i);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t x = v[e], f = finite_bits(x);
+                        o[2 * e] += f & 0xFFFFu ? 0.f : __uint_as_float(x << 16);
+                        o[2 * e + 1] += f >> 16 ? 0.f : __uint_as_float(x & 0xffff0000u);
+                    }
+                }
+                if (merge) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        *reinterpret_cast<float4 *>(state + ((i / 4 + e) * 128 + trow) * 16) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                } else if (r < nr) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) v[u] = bf16_pair(o[8 * e + 2 * u] * inv, o[8 * e + 2 * u + 1] * inv);
+                        *reinterpret_cast<uint4 *>(out + i + 8 * e) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                }
+            }
+            if (merge) *reinterpret_cast<float2 *>(state + 128 * DH * 4 + trow * 8) = make_float2(n ? m * c : -INFINITY, l + expired);
+        }
+        if (merge && T == 1) {
+            // The groups' states of the one tile become one, over the first (half of the columns to a group), or the result.  None is left out: a
+            // value that is not finite counts however small its factor.
+            asm volatile("bar.sync 3, 256;" ::: "memory");
+            float f[2], mx = -INFINITY, sum = 0.f;
+            float2 ml[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) ml[k] = *reinterpret_cast<const float2 *>(smem + k * C::STATE + 128 * DH * 4 + trow * 8), mx = fmaxf(mx, ml[k].x);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) f[k] = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx), sum = fmaf(ml[k].y, f[k], sum);
+            const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+            for (int i = g; i < DH / 8; i += 2) {
+                float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float4 o = *reinterpret_cast<const float4 *>(smem + k * C::STATE + ((2 * i + e) * 128 + trow) * 16);
+                        v[4 * e] = fmaf(o.x, f[k], v[4 * e]), v[4 * e + 1] = fmaf(o.y, f[k], v[4 * e + 1]);
+                        v[4 * e + 2] = fmaf(o.z, f[k], v[4 * e + 2]), v[4 * e + 3] = fmaf(o.w, f[k], v[4 * e + 3]);
+                    }
+                if (split > 1) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        *reinterpret_cast<float4 *>(smem + ((2 * i + e) * 128 + trow) * 16) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                } else if (r < nr) {
+                    *reinterpret_cast<uint4 *>(out + 8 * i) = make_uint4(bf16_pair(v[0] * inv, v[1] * inv), bf16_pair(v[2] * inv, v[3] * inv),
+                                                                         bf16_pair(v[4] * inv, v[5] * inv), bf16_pair(v[6] * inv, v[7] * inv));
+                }
+            }
+            if (g == 0) *reinterpret_cast<float2 *>(smem + 2 * C::STATE + trow * 8) = make_float2(mx, sum);
+        }
+        if (split > 1) {
+            __syncwarp();
+            cluster_sync_all();
+            // The CTAs' states.  Row words of four columns, 8 rows x 4 of them to a warp (32 bytes of a row, and every bank once); each CTA of a
+            // cluster takes every split-th of these.  A word's loads are in flight together.
+            const uint32_t st0 = smem_u32(smem);
+            const int n_words = T * 16 * (DH / 16);
+            for (int i = rank * 8 + warp - C::SM0; i < n_words; i += split * 8) {
+                const int tile = i / (16 * (DH / 16)), in = i % (16 * (DH / 16));
+                const int trow = (in / (DH / 16)) * 8 + (lane & 7), col4 = (in % (DH / 16)) * 4 + (lane >> 3), r = tile * 128 + trow;
+                if (r >= nr) continue;
+                const uint32_t at_ml = st0 + (T == 1 ? 2 * C::STATE : tile * C::STATE + 128 * DH * 4) + trow * 8;
+                const uint32_t at_o = st0 + tile * C::STATE + (col4 * 128 + trow) * 16;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                float mx = -INFINITY, sum = 0.f;
+                for (int k = 0; k < split; ++k) mx = fmaxf(mx, ld_cluster_f2(cluster_map(at_ml, k)).x);
+                for (int k = 0; k < split; ++k) {
+                    const float2 ml = ld_cluster_f2(cluster_map(at_ml, k));
+                    const float4 o = ld_cluster_f4(cluster_map(at_o, k));
+                    const float f = ml.x == -INFINITY ? 0.f : few_exp2(ml.x - mx);
+                    sum = fmaf(ml.y, f, sum);
+                    v.x = fmaf(o.x, f, v.x), v.y = fmaf(o.y, f, v.y), v.z = fmaf(o.z, f, v.z), v.w = fmaf(o.w, f, v.w);
+                }
+                const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+                const int2 at = A.split(r0 + r);
+                bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH + col4 * 4;
+                *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
+            }
+            cluster_sync_all();                                 // nobody leaves while its state is read
+        }
+    }
+    // (the other warps have too few registers for any of the above)
+    __syncwarp();
+    cp_async_wait<0>();
+    tc_fence_before();
+    if (split > 1) {
+        if (warp < C::SM0) cluster_sync_all(), cluster_sync_all();
+    } else {
+        __syncthreads();
+    }
+    if (warp == C::PW) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// How the work is laid out: tiles of a CTA (1 or 2), CTAs of a cluster that their keys are split over, by times in clocks as measured with all SMs busy: a
+// job (a key block of a tile) takes a CTA's pipes JOB, a block its producers LOAD; a CTA has a beginning and an end (FIXED, and MERGE where there are
+// states to merge); waves go by how many clusters the device holds at once.
+template <int DH, typename F> static TilePlan block_plan(long long kv_heads, long long seqs, long long rows, long long all_rows, long long keys, int n_sm, F &&clusters) {
+    constexpr int kb = BlockCfg<DH>::KB;
+    constexpr long long JOB = (DH == 128 ? 10 : 9) * kb, LOAD = 6 * kb, FIXED = 6000, MERGE = 3000;
+    const long long blocks = (keys + kb - 1) / kb;
+    TilePlan best = {1, 1};
+    long long least = -1;
+    for (int tiles = 1; tiles <= 2; ++tiles)
+        for (int split = 1; split <= BLOCK_SPLIT; ++split) {
+            const long long fit = split == 1 ? n_sm : clusters(split);
+            if (fit < 1 || (split > 1 && blocks < 2 * split)) break;
+            const long long R = 128 * tiles, mine = rows < R ? (rows + 127) / 128 : tiles, job = JOB * mine, per = (blocks + split - 1) / split;
+            const long long most = seqs * ((rows + R - 1) / R), real = all_rows / R + seqs, units = kv_heads * (most < real ? most : real);
+            const long long cost = (units + fit - 1) / fit * (per * (job > LOAD ? job : LOAD) + FIXED + (split > 1 || mine == 1 ? MERGE : 0));
+            if (least < 0 || cost < least) least = cost, best = {tiles, split};
+        }
+    return best;
+}
+
+template <int DH, typename Keys>
+static int launch_attn_block(const BatchD &B, const AttnRows &A, const Keys &K, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
+    using C = BlockCfg<DH>;
+    auto kern = k_attn_block<DH, Keys>;
+    static OncePerDevice once;
+    static int fit[NFD_PAGED_DEVICES][BLOCK_SPLIT + 1];
+    if (!once.run(dev, [&] {
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return false;
+            for (int split = 2; split <= BLOCK_SPLIT; ++split) fit[dev][split] = clusters_that_fit(kern, split, BLOCK_THREADS, C::SMEM);
+            return true;
+        }))
+        return NFD_E_CUDA;
+    const long long rows = (long long)B.max_rows * A.share, all_rows = (long long)B.n_rows * A.share;
+    const TilePlan pl = block_plan<DH>(kv_heads, B.n_seqs, rows, all_rows, keys, n_sm, [&](int k) { return fit[dev][k]; });
+    const long long R = 128 * pl.tiles, most = B.n_seqs * ((rows + R - 1) / R), real = all_rows / R + B.n_seqs;
+    const long long units = B.row_start && B.n_seqs <= BLOCK_SORTED && real < most ? real : most, grid = units * kv_heads * pl.split;
+    if (grid > INT_MAX) return NFD_E_RANGE;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid), cfg.blockDim = dim3(BLOCK_THREADS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = pl.split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at, cfg.numAttrs = pl.split > 1;
+    const float down = (float)sum_bits(BLOCK_GROWTH, (int)((keys + C::HK - 1) / C::HK));
+    if (cudaLaunchKernelEx(&cfg, kern, B, A, K, kv_heads, pl.split, pl.tiles, down) != cudaSuccess) {
+        cudaGetLastError();
+        return NFD_E_CUDA;
+    }
+    return NFD_OK;
+}

@@ -14,10 +14,20 @@
 
 #define F32_KEYS 64
 
-// States, and the power of two by which probabilities are scaled: exact, one bit for the roundings of the sums.
+// Keys, and the power of two by which probabilities are scaled: exact, one bit for the roundings of the sums.
 template <int DH> struct F32States : StateKeys<float, DH> {
+    static constexpr bool RANGES = false;                               // all rows see the same keys
+    int most;                                                           // keys of a row
     float scale;
-    explicit F32States(const StateKeys<float, DH> &k) : StateKeys<float, DH>(k), scale(ldexpf(1.0f, -sum_bits(1, k.n_keys))) {}
+    explicit F32States(const StateKeys<float, DH> &k) : StateKeys<float, DH>(k), most(k.n_keys), scale(ldexpf(1.0f, -sum_bits(1, k.n_keys))) {}
+};
+// Pages, or the rows of packed prompts: under a mask, and what a row does not see may be anything, so that in tiles that not all rows see a product
+// with a value is left out where the row does not see it.
+template <typename Keys, int DH> struct F32Rows : Keys {
+    static constexpr bool RANGES = true;
+    int most;
+    float scale;
+    F32Rows(const Keys &k, long long keys) : Keys(k), most((int)keys), scale(ldexpf(1.0f, -sum_bits(1, (int)keys))) {}
 };
 
 template <int DH, int ROWS> struct F32Cfg {
@@ -29,8 +39,8 @@ template <int DH, int ROWS> struct F32Cfg {
     static_assert(ROWS * (DH + 2) <= AT_K + F32_KEYS * LD, "a CTA's state lies over Q and K");
 };
 
-template <int DH, int ROWS>
-__global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const AttnRows A, const F32States<DH> K, int split) {
+template <typename Src, int DH, int ROWS>
+__global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const AttnRows A, const Src K, int split) {
     using C = F32Cfg<DH, ROWS>;
     constexpr int LD = C::LD, LP = C::LP, ND = DH / 16, W = DH / 4;
     extern __shared__ __align__(16) float f32_smem[];
@@ -42,23 +52,46 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
     const int rows = min(sr.y, B.max_rows) * A.share;
     if (r0 >= rows) return;                                             // (the whole cluster)
     const int nr = min(ROWS, rows - r0);
-    const int keys = K.length(B, s), tiles = (keys + F32_KEYS - 1) / F32_KEYS, per = (tiles + split - 1) / split;
+    // keys lo .. hi - 1; of which those below edge_lo and from edge_hi on are not seen by all rows
+    int lo = 0, hi = 0, edge_lo = 0, edge_hi = INT_MAX;
+    const int len = K.length(B, s);
+    KeyRange kr[4];                                                     // what rows 4 ty + i see
+    if constexpr (Src::RANGES) {
+        const KeyRange first = K.range(B, len, sr.y, A.split(r0).x), last = K.range(B, len, sr.y, A.split(r0 + nr - 1).x);
+        lo = first.lo, hi = last.hi, edge_lo = last.lo, edge_hi = first.hi;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kr[i] = K.range(B, len, sr.y, A.split(r0 + min(4 * ty + i, nr - 1)).x);
+    } else {
+        hi = len;
+    }
+    const int tiles = max(0, (hi - lo + F32_KEYS - 1) / F32_KEYS), per = (tiles + split - 1) / split;
     const int t0 = min(tiles, rank * per), t1 = min(tiles, t0 + per);
-    const long long seq = s * K.seq_stride + h * K.head_stride;
-    const unsigned char *mask = K.mask ? K.mask + (size_t)s * K.n_keys : nullptr;
-    auto fill = [&](int t) {
-        const int b = t & 1, p0 = t * F32_KEYS;
-        // G threads to a key, a share of its row each
-        constexpr int G = C::THREADS / F32_KEYS, PART = DH / G;
-        const int key = tid / G, part = tid % G, p = p0 + key;
-        const bool here = p < keys && (!mask || mask[p]);
-        const long long at = here ? seq + p * K.key_stride + part * PART : 0;
+    // G threads to a key, a share of its row each
+    constexpr int G = C::THREADS / F32_KEYS, PART = DH / G;
+    const int key = tid / G, part = tid % G;
+    auto cursor = [&]() {
+        if constexpr (Src::RANGES) return K.cursor(B, s, sr.x, lo + t0 * F32_KEYS + key, F32_KEYS);
+        else return 0;
+    }();
+    auto fill = [&](int t) {                                            // (t0, t0 + 1, ...)
+        const int b = t & 1, p = lo + t * F32_KEYS + key;
+        bool here = p < hi;
+        const float *k = K.first_k(), *v = K.first_v();
+        if constexpr (Src::RANGES) {
+            const long long row = K.next(cursor, B, h, here);
+            here = row >= 0;
+            k = K.k_row(here ? row : 0, h) + part * PART, v = K.v_row(here ? row : 0, h) + part * PART;
+        } else {
+            here = here && (!K.mask || K.mask[(size_t)s * K.n_keys + p]);
+            const long long at = here ? s * K.seq_stride + h * K.head_stride + p * K.key_stride + part * PART : 0;
+            k += at, v += at;
+        }
         const uint32_t dk = smem_u32(f32_smem + C::AT_K + (b * F32_KEYS + key) * LD + part * PART);
         const uint32_t dv = smem_u32(f32_smem + C::AT_V + (b * F32_KEYS + key) * LD + part * PART);
 #pragma unroll
         for (int i = 0; i < PART / 4; ++i) {
-            cp_async16(dk + 16 * i, K.k + at + (here ? 4 * i : 0), here ? 16 : 0);
-            cp_async16(dv + 16 * i, K.v + at + (here ? 4 * i : 0), here ? 16 : 0);
+            cp_async16(dk + 16 * i, k + (here ? 4 * i : 0), here ? 16 : 0);
+            cp_async16(dv + 16 * i, v + (here ? 4 * i : 0), here ? 16 : 0);
         }
         cp_async_commit();
         if (part == 0) sM[64 * b + key] = here;
@@ -117,6 +150,18 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
             if (!sM[64 * (t & 1) + tx + 16 * j])
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i][j] = -INFINITY;
+        const int p0 = lo + t * F32_KEYS;
+        const bool edge = Src::RANGES && (p0 < edge_lo || p0 + F32_KEYS > edge_hi);
+        if constexpr (Src::RANGES) {
+            if (edge)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int p = p0 + tx + 16 * j;
+                        if (p < kr[i].lo || p >= kr[i].hi) x[i][j] = -INFINITY;
+                    }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float mn = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
@@ -135,6 +180,7 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
         }
         __syncwarp();
         // O: rows 4 ty + i, dims: words of up to four, tx-th of every 16 of them
+        auto sum = [&](auto masked) {
 #pragma unroll 4
         for (int k = 0; k < F32_KEYS; k += 4) {
             float4 p[4];
@@ -155,6 +201,9 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    if constexpr (decltype(masked)::value) {
+                        if (p0 + k + u < kr[i].lo || p0 + k + u >= kr[i].hi) continue;
+                    }
                     const float pu = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
 #pragma unroll
                     for (int e = 0; e < ND; e += 2) {
@@ -164,6 +213,9 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
                 }
             }
         }
+        };
+        if (Src::RANGES && edge) sum(std::integral_constant<bool, Src::RANGES>());
+        else sum(std::false_type());
         __syncthreads();                                                // the tile may be overwritten
     }
     cp_async_wait<0>();
@@ -222,14 +274,14 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
     cluster_sync_all();                                                 // nobody leaves while its state is read
 }
 
-template <int DH, int ROWS>
-static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const F32States<DH> &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
+template <typename Src, int DH, int ROWS>
+static int launch_attn_f32_rows(const BatchD &B, const AttnRows &A, const Src &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
     using C = F32Cfg<DH, ROWS>;
-    auto kern = k_attn_f32<DH, ROWS>;
+    auto kern = k_attn_f32<Src, DH, ROWS>;
     static OncePerDevice once;
     if (!once.run(dev, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess; })) return NFD_E_CUDA;
     const long long tiles = ((long long)B.max_rows * A.share + ROWS - 1) / ROWS, units = kv_heads * tiles * B.n_seqs;
-    const int blocks = (K.n_keys + F32_KEYS - 1) / F32_KEYS;
+    const int blocks = (K.most + F32_KEYS - 1) / F32_KEYS;
     int split = 1;
     while (split < 8 && units * split * 2 <= 2 * n_sm && blocks > split) split *= 2;
     cudaLaunchConfig_t cfg = {};
@@ -257,8 +309,8 @@ template <int DH, int R> struct F32Few {
     static_assert(STATE <= NST * STAGE && AT_T % 16 == 0 && SMEM <= 232448 - 1024, "shared memory of a CTA");
 };
 // (The rings leave one CTA to an SM, and so it may have all registers: not told so, the compiler took 128 and spilled, and eight rows took 25.6 us for 21.5.)
-template <int DH, int R>
-__global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD B, const AttnRows A, const F32States<DH> K, int split) {
+template <typename Src, int DH, int R>
+__global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD B, const AttnRows A, const Src K, int split) {
     using C = F32Few<DH, R>;
     constexpr int KC = C::KC, PR = C::PR, NST = C::NST, STEP = 32 / PR;
     extern __shared__ __align__(16) uint8_t f32_few_smem[];
@@ -267,30 +319,54 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD
     const int2 sr = B.rows(s);
     const int r0 = blockIdx.z * R, nr = min(min(sr.y, B.max_rows) * A.share - r0, R);
     if (nr <= 0) return;                                                // (the whole cluster)
-    const int hi = K.length(B, s);
+    const int len = K.length(B, s);
+    int lo = 0, hi = len, edge_lo = 0, edge_hi = INT_MAX;               // (as in the kernel above)
+    KeyRange kr[R];
+    if constexpr (Src::RANGES) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) kr[r] = K.range(B, len, sr.y, A.split(r0 + min(r, nr - 1)).x);
+        lo = kr[0].lo, hi = kr[R - 1].hi, edge_lo = kr[R - 1].lo, edge_hi = kr[0].hi;
+    }
     float *ring = reinterpret_cast<float *>(f32_few_smem + warp * NST * C::STAGE), *sQ = reinterpret_cast<float *>(f32_few_smem + C::AT_Q);
     float *sP = reinterpret_cast<float *>(f32_few_smem + C::AT_P) + warp * R * KC;
-    const unsigned char *mask = K.mask ? K.mask + (size_t)s * K.n_keys : nullptr;
     // copies: word `lane % PR` of keys lane / PR, + STEP, ...
     const int word = lane % PR, key0 = lane / PR, step = split * FEW_WARPS * KC;
-    const long long from = s * K.seq_stride + h * K.head_stride + word * 4;
-    int next = (rank * FEW_WARPS + warp) * KC, base = next;
+    int next = lo + (rank * FEW_WARPS + warp) * KC, base = next;
     uint32_t raw = 0, bits[2] = {0, 0};                                 // key `lane` of the chunk that is filled next; which keys of the next two chunks are there
+    long long place = -1;                                               // its row
+    auto cursor = [&]() {
+        if constexpr (Src::RANGES) return K.cursor(B, s, sr.x, next + lane, step);
+        else return 0;
+    }();
     auto look = [&]() {
         const int p = next + lane;
         raw = p < hi && lane < KC;
-        if (mask && raw) raw = mask[p];
+        if constexpr (Src::RANGES) {
+            place = K.next(cursor, B, h, raw);
+            raw = place >= 0;
+        } else {
+            if (K.mask && raw) raw = K.mask[(size_t)s * K.n_keys + p];
+        }
     };
     auto fill = [&](int st) -> uint32_t {
         const uint32_t there = __ballot_sync(0xffffffffu, raw != 0), dst = smem_u32(ring) + st * C::STAGE;
-        long long at = from + (long long)(next + key0) * K.key_stride;
+        long long at = 0;
+        if constexpr (!Src::RANGES) at = s * K.seq_stride + h * K.head_stride + word * 4 + (long long)(next + key0) * K.key_stride;
 #pragma unroll
-        for (int i = 0; i < KC / STEP; ++i, at += STEP * K.key_stride) {
+        for (int i = 0; i < KC / STEP; ++i) {
             const int key = key0 + i * STEP;
             const bool here = there >> key & 1;
             const uint32_t d = dst + (key * PR + (word ^ (key & 7))) * 16;
-            cp_async16(d, here ? K.k + at : K.k, here ? 16 : 0);
-            cp_async16(d + KC * DH * 4, here ? K.v + at : K.v, here ? 16 : 0);
+            const float *k = K.first_k(), *v = K.first_v();
+            if constexpr (Src::RANGES) {
+                const long long row = __shfl_sync(0xffffffffu, place, key);
+                if (here) k = K.k_row(row, h) + word * 4, v = K.v_row(row, h) + word * 4;
+            } else {
+                if (here) k += at, v += at;
+                at += STEP * K.key_stride;
+            }
+            cp_async16(d, k, here ? 16 : 0);
+            cp_async16(d + KC * DH * 4, v, here ? 16 : 0);
         }
         next += step;
         look();
@@ -342,6 +418,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD
 #pragma unroll
             for (int d = KC; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
             if (!(there >> key & 1)) x = -INFINITY;
+            if (Src::RANGES && (base + key < kr[r].lo || base + key >= kr[r].hi)) x = -INFINITY;
             float mn = x;
 #pragma unroll
             for (int d = 1; d < KC; d <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, d));
@@ -353,6 +430,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD
             if (part == 0) sP[r * KC + key] = p;
         }
         __syncwarp();
+        const bool edge = Src::RANGES && (base < edge_lo || base + KC > edge_hi);
 #pragma unroll
         for (int i = 0; i < 8; i += 4) {
             float4 v[4];
@@ -364,6 +442,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD
                 const float p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
+                    if (Src::RANGES && edge && (base + g * 8 + i + u < kr[r].lo || base + g * 8 + i + u >= kr[r].hi)) continue;
                     const float2 a = ffma2(make_float2(p[u], p[u]), make_float2(v[u].x, v[u].y), make_float2(o[r][0], o[r][1]));
                     const float2 b = ffma2(make_float2(p[u], p[u]), make_float2(v[u].z, v[u].w), make_float2(o[r][2], o[r][3]));
                     o[r][0] = a.x, o[r][1] = a.y, o[r][2] = b.x, o[r][3] = b.y;
@@ -431,10 +510,10 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD
     }
     cluster_sync_all();                                                 // nobody leaves while its state is read
 }
-template <int DH, int R>
-static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const F32States<DH> &K, int kv_heads, int dev, cudaStream_t st) {
+template <typename Src, int DH, int R>
+static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const Src &K, int kv_heads, int dev, cudaStream_t st) {
     using C = F32Few<DH, R>;
-    auto kern = k_attn_f32_few<DH, R>;
+    auto kern = k_attn_f32_few<Src, DH, R>;
     static OncePerDevice once;
     static int fit[NFD_PAGED_DEVICES][5];
     if (!once.run(dev, [&] {
@@ -446,7 +525,7 @@ static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const F32Stat
         }))
         return NFD_E_CUDA;
     const int tiles = (int)(((long long)B.max_rows * A.share + R - 1) / R);
-    const int split = few_split((long long)kv_heads * B.n_seqs * tiles, K.n_keys, C::KC, fit[dev]);
+    const int split = few_split((long long)kv_heads * B.n_seqs * tiles, K.most, C::KC, fit[dev]);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kv_heads * split, B.n_seqs, tiles), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
     cudaLaunchAttribute at;
@@ -463,13 +542,12 @@ static int launch_attn_f32_few(const BatchD &B, const AttnRows &A, const F32Stat
 // 154 and 242, 242; head dimension 128, 32 sequences, 8 heads, 600 states, 16 and 32 rows 80, 139 and 183, 183.
 constexpr int f32_few_most(int dh) { return dh == 128 ? 32 : 16; }
 // 64 rows where that leaves no SM idle: twice the warps for the same tiles of keys
-template <int DH>
-static int launch_attn_f32(const BatchD &B, const AttnRows &A, const StateKeys<float, DH> &states, int kv_heads, int dev, int n_sm, cudaStream_t st) {
-    const F32States<DH> K(states);
+template <int DH, typename Src>
+static int launch_attn_f32(const BatchD &B, const AttnRows &A, const Src &K, int kv_heads, int dev, int n_sm, cudaStream_t st) {
     const long long rows = (long long)B.max_rows * A.share;
-    if (rows <= 1) return launch_attn_f32_few<DH, 1>(B, A, K, kv_heads, dev, st);
-    if (rows <= 4) return launch_attn_f32_few<DH, 4>(B, A, K, kv_heads, dev, st);
-    if (rows <= f32_few_most(DH)) return launch_attn_f32_few<DH, 8>(B, A, K, kv_heads, dev, st);
-    if ((((long long)B.max_rows * A.share + 63) / 64) * kv_heads * B.n_seqs >= n_sm) return launch_attn_f32_rows<DH, 64>(B, A, K, kv_heads, dev, n_sm, st);
-    return launch_attn_f32_rows<DH, 32>(B, A, K, kv_heads, dev, n_sm, st);
+    if (rows <= 1) return launch_attn_f32_few<Src, DH, 1>(B, A, K, kv_heads, dev, st);
+    if (rows <= 4) return launch_attn_f32_few<Src, DH, 4>(B, A, K, kv_heads, dev, st);
+    if (rows <= f32_few_most(DH)) return launch_attn_f32_few<Src, DH, 8>(B, A, K, kv_heads, dev, st);
+    if ((((long long)B.max_rows * A.share + 63) / 64) * kv_heads * B.n_seqs >= n_sm) return launch_attn_f32_rows<Src, DH, 64>(B, A, K, kv_heads, dev, n_sm, st);
+    return launch_attn_f32_rows<Src, DH, 32>(B, A, K, kv_heads, dev, n_sm, st);
 }

@@ -62,7 +62,7 @@ __device__ __forceinline__ float few_exp2(float x) {
 
 // A warp's chunk of keys in shared memory, for 4-bit pages: codes of K and V, their words, and which keys are there.
 template <int DH> struct FewKv4 {
-    static constexpr bool KV4 = true;
+    static constexpr bool KV4 = true, RANGES = false;
     static constexpr float UP = KV4_UP;                     // what scores and results are to be multiplied by
     static __device__ __forceinline__ float down() { return 0.f; }        // taken off the exponents (sum_bits; values below 1 need nothing)
     static constexpr int KC = 32;
@@ -210,43 +210,20 @@ template <int DH> struct FewKv4 {
     }
 };
 
-// The same for bf16 states.  Rows are swizzled in 16-byte pieces so that neither operand's reads meet in a bank.
-template <int DH> struct FewStates {
+// The same for bf16 numbers.  Rows are swizzled in 16-byte pieces so that neither operand's reads meet in a bank.
+template <int DH> struct FewBf16 {
     static constexpr bool KV4 = false;
     static constexpr float UP = 1.0f;
     static constexpr int KC = DH == 32 ? 32 : 16;
     static constexpr int NST = DH == 128 ? 3 : 4;
     static constexpr int RB = 2 * DH, PR = RB / 16;
     static constexpr int STAGE = 2 * KC * RB + 16;
-    StateKeys<bf16, DH> K;
     float bits;
     __device__ __forceinline__ float down() const { return bits; }
-    uint32_t there;                                         // of the chunk that is filled next
-    __device__ __forceinline__ void start(const BatchD &, int, int, int, int) {}
     static __device__ __forceinline__ uint32_t at_k(int key, int piece) { return key * RB + (piece ^ (key & 7 & (PR - 1))) * 16; }
     static __device__ __forceinline__ uint32_t at_v(int key, int piece) { return KC * RB + key * RB + (piece ^ (2 * key & 7 & (PR - 1))) * 16; }
-
-    __device__ __forceinline__ void look_up(const BatchD &B, int s, int h, int base, int hi) {
-        const int p = base + (threadIdx.x & 31);
-        bool t = p < hi && (threadIdx.x & 31) < KC;
-        if (t && K.mask) t = K.mask[(size_t)s * K.n_keys + p];
-        there = __ballot_sync(0xffffffffu, t);
-    }
-    __device__ __forceinline__ void fill(uint8_t *stage, uint32_t st, const BatchD &B, int s, int h, int base, int hi) {
-        const int lane = threadIdx.x & 31;
-        if (lane == 0) *reinterpret_cast<uint32_t *>(stage + 2 * KC * RB) = there;
-        const long long seq = s * K.seq_stride + h * K.head_stride;
-#pragma unroll
-        for (int j = 0; j < KC * PR / 32; ++j) {
-            const int key = (j * 32 + lane) / PR, piece = lane % PR;
-            const bool t = there >> key & 1;
-            const long long off = t ? seq + (base + key) * K.key_stride + piece * 8 : 0;
-            cp_async16(st + at_k(key, piece), K.k + off, t ? 16 : 0);
-            cp_async16(st + at_v(key, piece), K.v + off, t ? 16 : 0);
-        }
-    }
     static __device__ __forceinline__ uint32_t mask(const uint8_t *stage) { return *reinterpret_cast<const uint32_t *>(stage + 2 * KC * RB); }
-    static __device__ __forceinline__ uint32_t take_out(uint8_t *) { return 0; }                // (all rows see the same keys)
+    static __device__ __forceinline__ uint32_t take_out(uint8_t *) { return 0; }
     static __device__ __forceinline__ int q_dim(int step, int c) { return 8 * (c + 4 * (step / 2)) + 4 * (step % 2); }
     static __device__ __forceinline__ void k_frag(const uint8_t *stage, int key, int c, uint32_t *b) {
 #pragma unroll
@@ -272,6 +249,93 @@ template <int DH> struct FewStates {
                     b[8 * i + 2 * j] = __byte_perm(xs[j], ys[j], 0x5410), b[8 * i + 2 * j + 1] = __byte_perm(xs[j], ys[j], 0x7632);
             }
         }
+    }
+};
+
+// States of an encoder: all rows see the same keys.
+template <int DH> struct FewStates : FewBf16<DH> {
+    using F = FewBf16<DH>;
+    static constexpr bool RANGES = false;
+    static constexpr int KC = F::KC, RB = F::RB, PR = F::PR;
+    StateKeys<bf16, DH> K;
+    uint32_t there;                                         // of the chunk that is filled next
+    __device__ __forceinline__ void start(const BatchD &, int, int, int, int) {}
+    __device__ __forceinline__ void look_up(const BatchD &B, int s, int h, int base, int hi) {
+        const int p = base + (threadIdx.x & 31);
+        bool t = p < hi && (threadIdx.x & 31) < KC;
+        if (t && K.mask) t = K.mask[(size_t)s * K.n_keys + p];
+        there = __ballot_sync(0xffffffffu, t);
+    }
+    __device__ __forceinline__ void fill(uint8_t *stage, uint32_t st, const BatchD &B, int s, int h, int base, int hi) {
+        const int lane = threadIdx.x & 31;
+        if (lane == 0) *reinterpret_cast<uint32_t *>(stage + 2 * KC * RB) = there;
+        const long long seq = s * K.seq_stride + h * K.head_stride;
+#pragma unroll
+        for (int j = 0; j < KC * PR / 32; ++j) {
+            const int key = (j * 32 + lane) / PR, piece = lane % PR;
+            const bool t = there >> key & 1;
+            const long long off = t ? seq + (base + key) * K.key_stride + piece * 8 : 0;
+            cp_async16(st + F::at_k(key, piece), K.k + off, t ? 16 : 0);
+            cp_async16(st + F::at_v(key, piece), K.v + off, t ? 16 : 0);
+        }
+    }
+};
+
+// Bf16 pages and the rows of packed prompts: the rows of a unit do not all see the same keys, and what a row does not see may be anything.
+template <typename Keys, int DH> struct FewRows : FewBf16<DH> {
+    using F = FewBf16<DH>;
+    static constexpr bool RANGES = true;
+    static constexpr int KC = F::KC, RB = F::RB, PR = F::PR;
+    Keys K;
+    typename Keys::Cursor cur;
+    long long place;                                        // of key `lane` of the chunk that is filled next
+    __device__ __forceinline__ void start(const BatchD &B, int s, int h, int first, int step) { cur = K.cursor(B, s, B.rows(s).x, first + (threadIdx.x & 31), step); }
+    __device__ __forceinline__ void look_up(const BatchD &B, int s, int h, int base, int hi) {
+        const int lane = threadIdx.x & 31;
+        place = K.next(cur, B, h, lane < KC && base + lane < hi);
+    }
+    __device__ __forceinline__ void fill(uint8_t *stage, uint32_t st, const BatchD &B, int s, int h, int base, int hi) {
+        const int lane = threadIdx.x & 31;
+        const uint32_t there = __ballot_sync(0xffffffffu, place >= 0);
+        if (lane == 0) *reinterpret_cast<uint32_t *>(stage + 2 * KC * RB) = there;
+#pragma unroll
+        for (int j = 0; j < KC * PR / 32; ++j) {
+            const int key = (j * 32 + lane) / PR, piece = lane % PR;
+            const long long r = __shfl_sync(0xffffffffu, place, key);
+            cp_async16(st + F::at_k(key, piece), K.k_row(r < 0 ? 0 : r, h) + piece * 8, r < 0 ? 0 : 16);
+            cp_async16(st + F::at_v(key, piece), K.v_row(r < 0 ? 0 : r, h) + piece * 8, r < 0 ? 0 : 16);
+        }
+    }
+    // Values of a chunk that are not finite become zeros (a product with the 0 of a row that does not see them would be NaN), after add(key, dim,
+    // value) has been called for each of the dims of this lane: o_dim(t, n) of all t.
+    template <typename Add> static __device__ __forceinline__ void take_out_values(uint8_t *stage, int n, Add &&add) {
+        const int lane = threadIdx.x & 31;
+        uint32_t keys = 0;
+#pragma unroll 1
+        for (int j = 0; j < KC * PR / 32; ++j) {
+            const int key = (j * 32 + lane) / PR;
+            const uint4 x = *reinterpret_cast<const uint4 *>(stage + F::at_v(key, lane % PR));
+            if ((finite_bits(x.x) & finite_bits(x.y) & finite_bits(x.z) & finite_bits(x.w)) != 0xffffffffu) keys |= 1u << key;
+        }
+        keys = __reduce_or_sync(0xffffffffu, keys);
+        if (!keys) return;
+        for (uint32_t left = keys; left; left &= left - 1) {
+            const int key = __ffs(left) - 1;
+#pragma unroll 1
+            for (int t = 0; t < DH / 8; ++t) {
+                const int d = F::o_dim(t, n);
+                const uint32_t x = *reinterpret_cast<const uint16_t *>(stage + F::at_v(key, d / 8) + d % 8 * 2);
+                if ((x & 0x7F80u) == 0x7F80u) add(key, t, __uint_as_float(x << 16));
+            }
+        }
+        __syncwarp();
+#pragma unroll 1
+        for (int j = 0; j < KC * PR / 32; ++j) {
+            uint4 *v = reinterpret_cast<uint4 *>(stage + F::at_v((j * 32 + lane) / PR, lane % PR));
+            const uint4 x = *v;
+            *v = make_uint4(x.x & finite_bits(x.x), x.y & finite_bits(x.y), x.z & finite_bits(x.z), x.w & finite_bits(x.w));
+        }
+        __syncwarp();
     }
 };
 
@@ -383,6 +447,24 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, Src::KV4 ? 0 : 1) k_attn_few(c
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[u][t][e] += odd[e];
             }
+        }
+        if constexpr (Src::RANGES) {
+            if (base < s_range[nr - 1].x || base + KC > s_range[0].y)
+                Src::take_out_values(stage, n, [&](int key, int d, float v) {
+                    const int p = base + key;
+#pragma unroll
+                    for (int t = 0; t < NR; ++t)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int2 kr = s_range[8 * t + 2 * c + e];
+                            if (p < kr.x || p >= kr.y) continue;
+#pragma unroll
+                            for (int i = 0; i < NS; ++i) {
+                                if (d == 2 * i) o[t][i][e] += v;
+                                if (d == 2 * i + 1) o[t][i][2 + e] += v;
+                            }
+                        }
+                });
         }
         // x[u][t]: keys n' and n' + 8 (0, 1 and 2, 3) of tile u, rows 2 c and 2 c + 1 (0, 2 and 1, 3)
         if ((there & all) != all || bad || base < s_range[nr - 1].x || base + KC > s_range[0].y) {

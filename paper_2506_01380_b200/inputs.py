@@ -18,6 +18,8 @@ import numpy as np
 DTYPE_FP32 = 0
 DTYPE_BF16 = 1
 DTYPE_KV4 = 2            # pages of a cache only (nfd_pages.dtype)
+NORM_LAYER, NORM_RMS = 0, 1
+ROTATE_HALVES, ROTATE_BACK = 1, 2        # flags of nfd_rotate
 
 
 def _base_cfg(**kw):

@@ -46,7 +46,8 @@ EXPORTS = ["nfd_create", "nfd_destroy", "nfd_reset", "nfd_denoise_step", "nfd_de
            "nfd_profile_end",
            "nfd_profile_class_count", "nfd_profile_class_name", "nfd_attention_noalloc", "nfd_cond_cache_stats",
            "nfd_sample_dpmpp", "nfd_accepted_count", "nfd_debug_read", "nfd_kv_append", "nfd_pages_read",
-           "nfd_attention_kv4", "nfd_cross_attention"]
+           "nfd_attention_kv4", "nfd_cross_attention", "nfd_attention_pages", "nfd_attention_packed", "nfd_rotate",
+           "nfd_gate_norm"]
 
 
 class NfdBatch(C.Structure):
@@ -68,6 +69,15 @@ class NfdStates(C.Structure):
     _fields_ = ([(n, C.c_void_p) for n in ("k", "v", "mask")]
                 + [(n, C.c_longlong) for n in ("seq_stride", "key_stride", "head_stride")]
                 + [(n, C.c_int) for n in ("dtype", "n_keys", "n_heads", "head_dim")])
+
+
+class NfdNorm(C.Structure):
+    _fields_ = [("kind", C.c_int), ("dtype", C.c_int), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class NfdModulation(C.Structure):
+    _fields_ = [("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("stride", C.c_longlong),
+                ("index", C.c_void_p), ("n_mods", C.c_int), ("rows_per_mod", C.c_int), ("dtype", C.c_int)]
 
 
 class NfdError(RuntimeError):
@@ -123,6 +133,10 @@ def load():
     lib.nfd_pages_read.argtypes = [vp, vp, C.c_int, vp, vp, vp]
     lib.nfd_attention_kv4.argtypes = [vp, vp, C.c_int, vp, ll, C.c_int, C.c_int, vp, vp]
     lib.nfd_cross_attention.argtypes = [vp, vp, C.c_int, vp, ll, vp, vp]
+    lib.nfd_attention_pages.argtypes = [vp, vp, C.c_int, vp, ll, C.c_int, C.c_int, vp, vp]
+    lib.nfd_attention_packed.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, ll, vp, ll, vp, ll, C.c_int, C.c_int, vp, vp]
+    lib.nfd_rotate.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, C.c_int, vp, ll, vp, ll, C.c_int, vp, ll, vp, ll, vp]
+    lib.nfd_gate_norm.argtypes = [C.c_int, C.c_int, C.c_int, vp, ll, C.c_int, vp, ll, vp, ll, vp, ll, vp, vp, vp, C.c_float, vp]
     lib.nfd_strerror.argtypes = [C.c_int]
     lib.nfd_strerror.restype = C.c_char_p
     _lib = lib
@@ -183,7 +197,7 @@ def attention_noalloc(q, k_pages, v_pages, n_q_frames: int, window: int, out, st
 
 
 # ---------------------------------------------------------------------------------------------------------------
-# calls for hosts that bring their own memory: paged caches, 4-bit pages, encoder states
+# calls for hosts that bring their own memory: paged caches, packed prompts, encoder states, rows between projections
 # ---------------------------------------------------------------------------------------------------------------
 _TYPES = {torch.float32: I.DTYPE_FP32, torch.bfloat16: I.DTYPE_BF16}
 
@@ -274,6 +288,44 @@ class States:
         self.ref = C.addressof(self.c)
 
 
+class Norm:
+    """nfd_norm: "layer" or "rms", eps inside the root, weight and bias [width] (float32 or bfloat16, of one type) or None."""
+
+    def __init__(self, kind: str, eps: float = 1e-6, weight=None, bias=None):
+        given = [t for t in (weight, bias) if t is not None]
+        for t in given:
+            assert t.is_cuda and t.dim() == 1 and t.is_contiguous() and t.dtype in _TYPES and t.dtype is given[0].dtype
+            assert t.shape == given[0].shape and t.device == given[0].device
+        self.weight, self.bias = weight, bias
+        self.width, self.dev = (given[0].shape[0], given[0].get_device()) if given else (None, None)
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        self.c = NfdNorm({"layer": I.NORM_LAYER, "rms": I.NORM_RMS}[kind], _TYPES[given[0].dtype] if given else I.DTYPE_FP32, eps,
+                         ptr(weight), ptr(bias))
+        self.ref = C.addressof(self.c)
+
+
+class Modulation:
+    """nfd_modulation: gate, scale and shift [n_mods, width] (any of them None; float32 or bfloat16, of one type), whose rows
+    may be strided alike (parts of one projection's output).  Which row of them a row has: index [n_rows] int32 on the GPU
+    (read when a call runs), or row // rows_per_mod."""
+
+    def __init__(self, gate=None, scale=None, shift=None, index=None, rows_per_mod=None):
+        given = [t for t in (gate, scale, shift) if t is not None]
+        assert given and (index is None) != (rows_per_mod is None)
+        n_mods, width = given[0].shape
+        for t in given:
+            assert t.is_cuda and t.device == given[0].device and t.dtype in _TYPES and t.dtype is given[0].dtype
+            assert t.shape == given[0].shape and (t.stride(1) == 1 or width == 1) and (n_mods == 1 or t.stride(0) == given[0].stride(0))
+        if index is not None:
+            assert index.is_cuda and index.dtype == torch.int32 and index.dim() == 1 and index.is_contiguous() and index.device == given[0].device
+        self.gate, self.scale, self.shift, self.index = gate, scale, shift, index
+        self.width, self.dev = width, given[0].get_device()
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        self.c = NfdModulation(ptr(gate), ptr(scale), ptr(shift), given[0].stride(0) if n_mods > 1 else width, ptr(index), n_mods,
+                               0 if rows_per_mod is None else rows_per_mod, _TYPES[given[0].dtype])
+        self.ref = C.addressof(self.c)
+
+
 # (Checks and look-ups cost the host as much as a small call costs the GPU: tensors are asked for what is needed, once.)
 def _call(what, dev, stream, fn, *args):
     """A call on `stream` (None: torch's current one of device number dev) with its device current."""
@@ -357,6 +409,72 @@ def cross_attention(states: States, batch: Batch, q, out, stream=None):
     _call("nfd_cross_attention", dev, stream, load().nfd_cross_attention, states.ref, batch.ref, h, q.data_ptr(), qs,
           _result(out, n * h * dh, dtype, dev))
     return out
+
+
+def attention_pages(pages: Pages, batch: Batch, q, out, frame_tokens: int = 1, window: int = (1 << 31) - 1, stream=None):
+    """nfd_attention_pages: attention of q [n_rows, n_heads, head_dim] (the pages' type, rows may be strided) over a cache of
+    float32 or bfloat16 pages into out [n_rows, n_heads * head_dim]; frame_tokens = 1: causal, otherwise block-causal by frames."""
+    dev, n, dh, dtype = pages.dev, batch.n_rows, pages.head_dim, pages.dtype
+    assert batch.dev == dev and batch.table is not None and dtype is not None
+    h = _heads(q, dh)
+    qs = _row_stride(q, n, h, dh, dtype, dev)
+    _call("nfd_attention_pages", dev, stream, load().nfd_attention_pages, pages.ref, batch.ref, h, q.data_ptr(), qs, frame_tokens,
+          window, _result(out, n * h * dh, dtype, dev))
+    return out
+
+
+def attention_packed(batch: Batch, q, k, v, out, frame_tokens: int = 1, window: int = (1 << 31) - 1, stream=None):
+    """nfd_attention_packed: attention over whole prompts, packed one behind the other as batch.row_start says (its kv_len and
+    table are not looked at).  q [n_rows, n_heads, head_dim], k and v [n_rows, kv_heads, head_dim], float32 or bfloat16, each
+    with rows that may be strided, into out [n_rows, n_heads * head_dim]; the mask as in attention_pages."""
+    n, (_, hk, dh), dtype, dev = batch.n_rows, k.shape, q.dtype, q.get_device()
+    assert batch.dev in (dev, None) and dtype in _TYPES and q.is_cuda
+    h = _heads(q, dh)
+    qs, ks, vs = (_row_stride(t, n, m, dh, dtype, dev) for t, m in ((q, h), (k, hk), (v, hk)))
+    _call("nfd_attention_packed", dev, stream, load().nfd_attention_packed, batch.ref, _TYPES[dtype], h, hk, dh, q.data_ptr(), qs,
+          k.data_ptr(), ks, v.data_ptr(), vs, frame_tokens, window, _result(out, n * h * dh, dtype, dev))
+    return out
+
+
+def rotate(rope: Rope, positions, x, x_out=None, x2=None, x2_out=None, halves: bool = False, back: bool = False, stream=None):
+    """nfd_rotate: rotary embedding of x [n_rows, n_heads, head_dim] (and x2, of another number of heads) at positions
+    [n_rows, 3] (int32: time, height, width) into x_out and x2_out (None: in place).  halves: pairs are (i, i + head_dim / 2)
+    instead of (2 i, 2 i + 1); back: by the negative angle.  All rows may be strided."""
+    (n, h, dh), dtype, dev = x.shape, x.dtype, x.get_device()
+    assert x.is_cuda and dtype in _TYPES
+    assert positions.dtype == torch.int32 and tuple(positions.shape) == (n, 3) and positions.is_contiguous() and positions.get_device() == dev
+    x_out = x if x_out is None else x_out
+    args = [h, x.data_ptr(), _row_stride(x, n, h, dh, dtype, dev), x_out.data_ptr(), _row_stride(x_out, n, h, dh, dtype, dev)]
+    if x2 is None:
+        args += [0, None, 0, None, 0]
+    else:
+        x2_out = x2 if x2_out is None else x2_out
+        h2 = x2.shape[1]
+        args += [h2, x2.data_ptr(), _row_stride(x2, n, h2, dh, dtype, dev), x2_out.data_ptr(), _row_stride(x2_out, n, h2, dh, dtype, dev)]
+    _call("nfd_rotate", dev, stream, load().nfd_rotate, rope.ref, I.ROTATE_HALVES * halves + I.ROTATE_BACK * back, _TYPES[dtype], dh, n,
+          positions.data_ptr(), *args)
+    return x_out, x2_out
+
+
+def gate_norm(x, y=None, x_out=None, h=None, pre: Norm = None, post: Norm = None, mod: Modulation = None, res_scale: float = 1.0,
+              stream=None):
+    """nfd_gate_norm: t = post(y), x_out = x + res_scale * gate * t, h = pre(x_out) * (1 + scale) + shift, row by row.  x and
+    x_out [n_rows, width] (the residual stream; x_out None: in place) are of one type, y and h of one type, float32 or bfloat16; rows may
+    be strided.  Without y: h = pre(x) * (1 + scale) + shift.  Returns (x_out, h)."""
+    (n, width), dev = x.shape, x.get_device()
+    assert x.is_cuda and x.dtype in _TYPES and (y is not None or h is not None)
+    other = (y if y is not None else h).dtype
+    x_out = x if x_out is None and y is not None else x_out
+    args = []
+    for t, dtype in ((x, x.dtype), (y, other), (x_out if y is not None else None, x.dtype), (h, other)):
+        args += [None, 0] if t is None else [t.data_ptr(), _row_stride(t, n, 1, width, dtype, dev)]
+    for p in (pre, post, mod):
+        assert p is None or (p.width in (width, None) and p.dev in (dev, None))
+    assert mod is None or mod.index is None or mod.index.shape[0] == n
+    ref = lambda p: p.ref if p is not None else None
+    _call("nfd_gate_norm", dev, stream, load().nfd_gate_norm, n, width, _TYPES[x.dtype], args[0], args[1], _TYPES[other], *args[2:],
+          ref(post), ref(pre), ref(mod), res_scale)
+    return x_out, h
 
 
 class NFD:
