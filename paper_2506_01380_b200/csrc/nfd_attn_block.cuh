@@ -14,14 +14,16 @@
 // keeps keys out and not values: 0 x NaN is NaN.  So in blocks that not all rows of a CTA see, the producers take values that are not finite out of V and
 // note where; a row that does see one adds it to its result at the end.
 //
-// Warps 0 .. 3 fill a ring of K and V blocks in turn with cp.async, several blocks in flight, a lane looking up the place of each key; warp 4 issues the
-// products; the last 8 are the softmax groups.  Which keys of a block are there is told beside K, a bit each, in a ring of its own.
+// Warp 0 fills a ring of K and V blocks in turn by TMA, a lane looking up the place of each box of keys, and warps 1 .. 3 look through values where that is
+// needed; where pages do not consist of boxes (or with head dimension 32) the four of them copy by cp.async, a lane looking up the place of each key.  Warp 4 issues
+// the products; the last 8 are the softmax groups.  Which keys of a block are there is told beside K, a bit each, in a ring of its own.
 //
 // A unit (sequence, head of keys, tiles) with many keys and few others beside it is split over the CTAs of a cluster, which merge through distributed
 // shared memory in a fixed order.  Every wait on a barrier in memory is bounded; after one that ran out the rows are NaN.  (The cluster's own barrier needs
 // no bound: every CTA comes to it, its other waits being bounded, or has left as a whole cluster.)
 #pragma once
 #include "nfd_attn_tile.cuh"
+#include <cuda.h>
 
 #define BLOCK_THREADS 512
 #define BLOCK_SPLIT 8               // most CTAs of a cluster
@@ -41,7 +43,7 @@ template <int DH> struct BlockCfg {
     static constexpr int NM = 16;                          // masks
     static constexpr int Q_BYTES = SUB * 128 * 128;        // a tile's queries
     static constexpr int BLK = SUB * KB * 128;             // a block of K or V
-    static constexpr int AT_Q = 0, AT_R = 2 * Q_BYTES, AT_MASK = AT_R + NST * BLK, AT_BAR = AT_MASK + NM * 16, SMEM = AT_BAR + 512 + 1024;
+    static constexpr int AT_Q = 0, AT_R = 2 * Q_BYTES, AT_MASK = AT_R + NST * BLK, AT_BAR = AT_MASK + NM * 16, SMEM = AT_BAR + 528 + 1024;
     static constexpr int TM_O = 2 * NBG * KB;              // S of group g, number i, and over it P, at (g NBG + i) KB; O of group g at TM_O + g 64 SUB
     static constexpr int STATE = 128 * DH * 4 + 128 * 8;   // a group's state, over queries and ring: O as [DH / 4][128] float4, then [128] (m, l)
     static_assert(TM_O + 2 * 64 * SUB <= 512 && 2 * STATE + 128 * 8 <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
@@ -60,8 +62,10 @@ struct BlockBars {
     // of a group's even and odd parts: a warp may be done with one before the product of the one before it is
     __device__ __forceinline__ uint32_t pv_done(int g, int n) const { return b + 384 + 16 * g + 8 * (n & 1); }
     __device__ __forceinline__ uint32_t q_full() const { return b + 416; }
+    __device__ __forceinline__ uint32_t landed(int s) const { return b + 424 + 8 * s; }          // stages: values that are looked through before they are used
+    static constexpr int BYTES = 424 + 96;
     __device__ __forceinline__ void init(int stages, int producers) const {
-        for (int s = 0; s < stages; ++s) mbar_init(full(s), producers), mbar_init(empty(s), 1);
+        for (int s = 0; s < stages; ++s) mbar_init(full(s), producers), mbar_init(empty(s), 1), mbar_init(landed(s), 1);
         for (int s = 0; s < 16; ++s) mbar_init(m_full(s), producers);
         for (int g = 0; g < 2; ++g)
             for (int i = 0; i < 2; ++i) mbar_init(s_full(g, i), 1), mbar_init(p_full(g, i), 4), mbar_init(pv_done(g, i), 1);
@@ -74,14 +78,130 @@ struct BlockBars {
 // edge_lo, those from edge_hi on.
 struct BlockWork {
     int s, h, first_row, lo, hi, nb, T, edge_lo, edge_hi;
+    // are there rows of the CTA that do not see all of block b (of KB keys)
+    __device__ __forceinline__ bool edge(int b, int KB) const { return lo + b * KB < edge_lo || lo + b * KB + KB > edge_hi; }
     int end0, begin1;                                       // two tiles: the first takes the blocks before end0, the second those from begin1 on
     // does group g take block b (one tile: they take turns)
     __device__ __forceinline__ bool takes(int g, int b) const { return T == 2 ? (g ? b >= begin1 : b < end0) : (b & 1) == g; }
+    // and which of its jobs is that
+    __device__ __forceinline__ int job(int g, int b) const { return T == 1 ? b >> 1 : g ? b - begin1 : b; }
 };
 template <int n> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(n)); }
 template <int n> __device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(n)); }
 
+// ---- keys that TMA brings ------------------------------------------------------------------------------------
+// Pages: tensor [pages x heads][page_tokens][DH], a box of `rows` keys (a power of two that a page consists of, so that no box crosses its end).
+template <int DH> struct PageBoxes : PageKeys<bf16, DH> {
+    static constexpr bool TMA = true;
+    CUtensorMap maps[2];
+    int rows;
+    __device__ __forceinline__ int box() const { return rows; }
+    __device__ __forceinline__ int begin(int lo) const { return lo & -rows; }
+    // offset in its page and page of the next box (page -1: it is not there)
+    __device__ __forceinline__ int2 next_box(typename PageKeys<bf16, DH>::Cursor &c, const BatchD &B, int h, bool there) const {
+        const int T = this->P.page_tokens, L = B.table_len;
+        int2 at = make_int2(c.off, -1);
+        if (there) {
+            const int page = __ldg(c.table + c.pg);
+            if ((unsigned)page < (unsigned)this->P.n_pages) at.y = page * this->P.heads + h;
+        }
+        c.off += c.dr, c.pg += c.dq;
+        if (c.off >= T) c.off -= T, ++c.pg;
+        if (c.pg >= L) c.pg -= L;
+        return at;
+    }
+    // (a page behind the last one is filled in as zeros)
+    __device__ __forceinline__ void load(int kv, uint32_t dst, uint32_t bar, int part, int, int2 at) const {
+        tma_load_3d(dst, &maps[kv], bar, 64 * part, at.x, at.y < 0 ? this->P.n_pages * this->P.heads : at.y);
+    }
+};
+// The rows of packed prompts: tensor [rows][heads x DH], a box of a block's keys (what lies behind a sequence's end is the next one's, and masked).
+template <int DH> struct PackedBoxes : PackedKeys<bf16, DH> {
+    static constexpr bool TMA = true;
+    CUtensorMap maps[2];
+    __device__ __forceinline__ int box() const { return BlockCfg<DH>::KB; }
+    __device__ __forceinline__ int begin(int lo) const { return lo; }
+    __device__ __forceinline__ int2 next_box(typename PackedKeys<bf16, DH>::Cursor &c, const BatchD &, int, bool) const {
+        const int row = c.row;
+        c.row += c.step;
+        return make_int2(row, 0);
+    }
+    __device__ __forceinline__ void load(int kv, uint32_t dst, uint32_t bar, int part, int h, int2 at) const {
+        tma_load_2d(dst, &maps[kv], bar, h * DH + 64 * part, at.x);
+    }
+};
+
 // ---- producers ----------------------------------------------------------------------------------------------
+// Values of a piece of a block that are not finite become zeros; was there one?
+__device__ __forceinline__ bool block_take_out(uint8_t *at) {
+    uint4 *v = reinterpret_cast<uint4 *>(at);
+    const uint4 x = *v;
+    const uint4 f = make_uint4(finite_bits(x.x), finite_bits(x.y), finite_bits(x.z), finite_bits(x.w));
+    if ((f.x & f.y & f.z & f.w) == 0xffffffffu) return false;
+    *v = make_uint4(x.x & f.x, x.y & f.y, x.z & f.z, x.w & f.w);
+    return true;
+}
+// By TMA, one warp: a lane's copy of a block is a box of 64 dims and `box` keys, looked up on the way.
+template <int DH, typename Keys>
+static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B, const BlockWork &w, uint8_t *smem, const BlockBars &bars, bool &ok) {
+    using C = BlockCfg<DH>;
+    const int lane = threadIdx.x & 31, box = K.box(), groups = C::KB / box, part = lane / groups, group = lane - part * groups;
+    const bool mine = part < C::SUB;
+    const uint32_t to = smem_u32(smem) + C::AT_R + part * (C::KB * 128) + group * box * 128;
+    int p = w.lo + group * box;
+    auto cur = K.cursor(B, w.s, w.first_row, p, C::KB);
+    auto look_up = [&]() -> int2 {
+        const int2 at = K.next_box(cur, B, w.h, mine && p < w.hi);
+        p += C::KB;
+        return at;
+    };
+    int2 next = look_up();
+    int st = 0;
+    uint32_t par = 1;                                        // (the first lap waits for nothing)
+    int items = 0;
+    for (int b = 0; b < w.nb && ok; ++b) {
+        const int2 at = next;
+        if constexpr (Keys::HOLES) {
+            const uint32_t there = __ballot_sync(0xffffffffu, at.y >= 0);
+            uint8_t *M = smem + C::AT_MASK + b % C::NM * 16;
+            if (lane < C::KB / 8) M[lane] = there >> (lane * 8 / box) & 1 ? 0xFF : 0;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars.m_full(b % C::NM));
+        }
+        next = look_up();
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            ok = __all_sync(0xffffffffu, tile_wait(bars.empty(st), par));
+            if (!ok) break;
+            const uint32_t bar = kv && w.edge(b, C::KB) ? bars.landed(st) : bars.full(st);
+            if (lane == 0) mbar_expect_tx(bar, C::BLK);
+            __syncwarp();
+            if (mine) K.load(kv, to + st * C::BLK, bar, part, w.h, at);
+            if (++st == C::NST) st = 0, par ^= 1;
+            ++items;
+        }
+    }
+    // (nobody leaves with copies in flight, whoever has given up waiting)
+    for (int i = max(0, items - C::NST); i < items; ++i) ok = tile_wait(bars.full(i % C::NST), (i / C::NST) & 1) && ok;
+}
+// and three warps that look through the values of blocks that not all rows see
+template <int DH> static __device__ __forceinline__ void block_look_through(const BlockWork &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
+    using C = BlockCfg<DH>;
+    uint32_t laps = 0;                                       // phases of the stages' barriers
+    for (int b = 0; b < w.nb; ++b) {                         // (all of it, whatever runs out: the threads meet at a barrier)
+        if (!w.edge(b, C::KB)) continue;
+        const int st = (2 * b + 1) % C::NST;
+        if (ok) ok = tile_wait(bars.landed(st), laps >> st & 1);
+        laps ^= 1u << st;
+        bool some = false;
+        for (int i = (threadIdx.x - 32) * 16; i < C::BLK; i += 96 * 16) some |= block_take_out(smem + C::AT_R + st * C::BLK + i);
+        if (some) atomicMin(bad, w.lo + b * C::KB), atomicMax(bad + 1, w.lo + b * C::KB + C::KB);
+        fence_proxy_async_smem();
+        asm volatile("bar.sync 4, 96;" ::: "memory");
+        if (threadIdx.x == 32) mbar_arrive(bars.full(st));
+    }
+}
+// By cp.async, four warps.
 template <int DH, typename Keys>
 static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD &B, const BlockWork &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
     using C = BlockCfg<DH>;
@@ -103,15 +223,10 @@ static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD
     auto publish = [&]() {
         const int st = done % C::NST, p0 = w.lo + (done >> 1) * C::KB;
         cp_async_wait_upto(item - done - 1);
-        if ((done & 1) && (p0 < w.edge_lo || p0 + C::KB > w.edge_hi)) {
+        if ((done & 1) && w.edge(done >> 1, C::KB)) {
             bool some = false;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                uint4 *v = reinterpret_cast<uint4 *>(smem + C::AT_R + st * C::BLK + to(i));
-                const uint4 x = *v;
-                const uint4 f = make_uint4(finite_bits(x.x), finite_bits(x.y), finite_bits(x.z), finite_bits(x.w));
-                if ((f.x & f.y & f.z & f.w) != 0xffffffffu) *v = make_uint4(x.x & f.x, x.y & f.y, x.z & f.z, x.w & f.w), some = true;
-            }
+            for (int i = 0; i < N; ++i) some |= block_take_out(smem + C::AT_R + st * C::BLK + to(i));
             if (some) atomicMin(bad, p0), atomicMax(bad + 1, p0 + C::KB);
         }
         tile_publish(bars.full(st)), ++done;
@@ -144,7 +259,7 @@ static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD
                 cp_async16(dst + to(i), src, r < 0 ? 0 : 16);
             }
             cp_async_commit();
-            if (!kv) {
+            if (Keys::HOLES && !kv) {
                 uint8_t *M = smem + C::AT_MASK + b % C::NM * 16 + warp * (C::KPW / 8);
                 if (lane < C::KPW / 8) M[lane] = (uint8_t)(there >> (8 * lane));
                 __syncwarp();
@@ -159,8 +274,10 @@ static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD
 }
 
 // ---- issuer -------------------------------------------------------------------------------------------------
-// All products of a CTA, by one thread.  A job is a block of a group, by blocks and then by groups; the S of a job is issued as soon as the P V that
-// reads its accumulator's last P has been: the tensor pipe takes one thread's instructions in order.
+// All products of a CTA, by one thread: block by block, for either group P V of its block and then S of the one that takes the same accumulator next
+// (the tensor pipe takes one thread's instructions in order).  Nothing here branches on whether a wait has run out (what follows then is computed from whatever is
+// there, and thrown away): with control flow that is the same for all lanes the operands stay in uniform registers.  Otherwise, moved there one by one for
+// every product, they cost more than the products.
 template <int DH> static __device__ __forceinline__ bool block_issue(const BlockWork &w, const BlockBars &bars, uint32_t base, uint32_t tmem) {
     using C = BlockCfg<DH>;
     constexpr int KB = C::KB, SUB = C::SUB, NST = C::NST, NBG = C::NBG;
@@ -168,71 +285,71 @@ template <int DH> static __device__ __forceinline__ bool block_issue(const Block
     // (a cluster's addresses hold the CTA's rank above bit 23; V's other 64 dims are KB rows on: the leading offset)
     const uint32_t at = base & 0x3ffffu, dQ = (at + C::AT_Q) >> 4, dR = (at + C::AT_R) >> 4, lead = (KB * 128 >> 4) << 16;
     bool ok = tile_wait(bars.q_full(), 0);
-    int sb = 0, sg = 0, ns0 = 0, ns1 = 0, np0 = 0, np1 = 0; // next S: block, group; jobs of a group so far
-    auto scores = [&]() {                                    // issues what may be issued
-        while (ok && sb < w.nb) {
-            if (!w.takes(sg, sb)) {
-                if (++sg == 2) sg = 0, ++sb;
-                continue;
-            }
-            int &n = sg ? ns1 : ns0;
-            if (n >= (sg ? np1 : np0) + NBG) return;
-            const int item = 2 * sb, st = item % NST;
-            if (!(sg == 1 && w.takes(0, sb))) ok = ok && tile_wait(bars.full(st), (item / NST) & 1);
-            if (!ok) return;
-            tc_fence_after();
-            const int i = NBG == 1 ? 0 : n & 1;
-            const uint32_t q = dQ + (w.T == 1 ? 0 : sg) * (C::Q_BYTES >> 4), k = dR + st * (C::BLK >> 4), d = tmem + (sg * NBG + i) * KB;
-#pragma unroll
-            for (int e = 0; e < (DH + 15) / 16; ++e)
-                tile_mma_ss(d, q + (e >> 2) * (128 * 128 >> 4) + 2 * (e & 3), k + (e >> 2) * (KB * 128 >> 4) + 2 * (e & 3), idesc_s, e != 0);
-            umma_commit(bars.s_full(sg, i));
-            if (!(sg == 0 && w.takes(1, sb))) umma_commit(bars.empty(st));
-            ++n;
-            if (++sg == 2) sg = 0, ++sb;
-        }
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (ok) ok = tile_wait(bar, parity);
     };
-    scores();
-    for (int b = 0; b < w.nb && ok; ++b) {
-        const int item = 2 * b + 1, st = item % NST;
-        const uint32_t v = (dR + st * (C::BLK >> 4)) | lead;
+    auto scores = [&](int g, int b, int st, uint32_t par) {  // stage of the block's K and its phase
+        if (g == 0 || !w.takes(0, b)) wait(bars.full(st), par);
+        tc_fence_after();
+        const int i = NBG == 1 ? 0 : w.job(g, b) & 1;
+        const uint32_t q = dQ + (w.T == 1 ? 0 : g) * (C::Q_BYTES >> 4), k = dR + st * (C::BLK >> 4), d = tmem + (g * NBG + i) * KB;
+#pragma unroll
+        for (int e = 0; e < (DH + 15) / 16; ++e)
+            tile_mma_ss(d, q + (e >> 2) * (128 * 128 >> 4) + 2 * (e & 3), k + (e >> 2) * (KB * 128 >> 4) + 2 * (e & 3), idesc_s, e != 0);
+        umma_commit(bars.s_full(g, i));
+        if (g == 1 || !w.takes(1, b)) umma_commit(bars.empty(st));
+    };
+    const int ahead = w.T == 1 ? 2 * NBG : NBG;              // blocks
+    int sk = 0, sv = 1;                                      // stages of the next K and the next V, and their phases
+    uint32_t pk = 0, pv = 0;
+    auto on = [&](int &st, uint32_t &par) {
+        st += 2;
+        if (st >= NST) st -= NST, par ^= 1;
+    };
+    for (int b = 0; b < ahead && b < w.nb; ++b) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+            if (w.takes(g, b)) scores(g, b, sk, pk);
+        on(sk, pk);
+    }
+    for (int b = 0; b < w.nb; ++b) {
+        const uint32_t v = (dR + sv * (C::BLK >> 4)) | lead;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            if (!ok || !w.takes(g, b)) continue;
-            if (!(g == 1 && w.takes(0, b))) ok = ok && tile_wait(bars.full(st), (item / NST) & 1);
-            int &n = g ? np1 : np0;
-            const int i = NBG == 1 ? 0 : n & 1;
-            const uint32_t d = tmem + C::TM_O + g * 64 * SUB, a = tmem + (g * NBG + i) * KB;
+            if (w.takes(g, b)) {
+                if (g == 0 || !w.takes(0, b)) wait(bars.full(sv), pv);
+                const int n = w.job(g, b), i = NBG == 1 ? 0 : n & 1;
+                const uint32_t d = tmem + C::TM_O + g * 64 * SUB, a = tmem + (g * NBG + i) * KB;
 #pragma unroll
-            for (int part = 0; part < C::PARTS; ++part) {
-                ok = ok && tile_wait(bars.p_full(g, C::PARTS == 1 ? i : part), (n / NBG) & 1);
-                if (!ok) break;
-                tc_fence_after();
-                constexpr int E = C::HK / 16;
+                for (int part = 0; part < C::PARTS; ++part) {
+                    wait(bars.p_full(g, C::PARTS == 1 ? i : part), (n / NBG) & 1);
+                    tc_fence_after();
+                    constexpr int E = C::HK / 16;
 #pragma unroll
-                for (int e = part * E; e < (part + 1) * E; ++e) tile_mma_ts(d, a + 8 * e, v + e * (2048 >> 4), idesc_pv, n != 0 || e != 0);
-                umma_commit(bars.pv_done(g, n * C::PARTS + part));
+                    for (int e = part * E; e < (part + 1) * E; ++e) tile_mma_ts(d, a + 8 * e, v + e * (2048 >> 4), idesc_pv, n != 0 || e != 0);
+                    umma_commit(bars.pv_done(g, n * C::PARTS + part));
+                }
+                if (g == 1 || !w.takes(1, b)) umma_commit(bars.empty(sv));
             }
-            if (!ok) break;
-            if (!(g == 0 && w.takes(1, b))) umma_commit(bars.empty(st));
-            ++n;
-            scores();
+            if (b + ahead < w.nb && w.takes(g, b + ahead)) scores(g, b + ahead, sk, pk);
         }
+        on(sk, pk), on(sv, pv);
     }
     return ok;
 }
 
 // ---- softmax ------------------------------------------------------------------------------------------------
-// A part of a block whose sums have outgrown m, or that finds a row without one: the row's maximum over the keys that it sees, m and what has been
-// summed so far adjusted to it, then P.  seen: bits of the keys that the row sees; n: the group's parts before this one; pv_done: of the last of them.
+// The rest of a part whose sums have outgrown m: the row's maximum over the keys that it sees from column `from` on, m and what has been
+// summed so far adjusted to it (O, and P of the part's first columns), then P.  seen: bits of the keys that the row sees; n: the group's parts before this one;
+// pv_done: of the last of them.  A row without an m comes here as well.
 template <int DH>
-static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint32_t tO, const uint32_t *seen, float c, float down, int n, uint32_t pv_done,
+static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint32_t tO, const uint32_t *seen, int from, float c, float down, int n, uint32_t pv_done,
                                                float &m_io, float &l_io, bool &ok) {
     constexpr int HK = BlockCfg<DH>::HK;
     float m = m_io, l = l_io, top = -INFINITY;
-    auto bits = [&](int i) { return (i < 32 ? seen[0] : i < 64 ? seen[1] : seen[2]) >> (i & 31); };
+    auto bits = [&](int i) { return (i < 32 ? seen[0] : i < 64 ? seen[1] : seen[HK / 32 - 1]) >> (i & 31); };
 #pragma unroll 1
-    for (int i = 0; i < HK; i += 16) {
+    for (int i = from; i < HK; i += 16) {
         float x[16];
         tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
         const uint32_t s = bits(i);
@@ -247,6 +364,17 @@ static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint
         const float f = !rise ? 1.0f : m == -INFINITY ? 0.f : few_exp2((m - top) * c);
         if (rise) m = top;
         l *= f;
+        tmem_st_wait();
+#pragma unroll 1
+        for (int i = 0; i < from / 2; i += 16) {
+            uint32_t p[16];
+            tmem_ld16(tP + i, p);
+            tmem_ld_wait();
+            loaded16(reinterpret_cast<float *>(p));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] = bf16_pair(__uint_as_float(p[e] << 16) * f, __uint_as_float(p[e] & 0xffff0000u) * f);
+            tmem_st16(tP + i, p);
+        }
         if (n) {
             ok = ok && tile_wait(pv_done, ((n - 1) >> 1) & 1);         // O is at rest
             __syncwarp();
@@ -266,7 +394,7 @@ static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint
     const float mc = m == -INFINITY ? 0.f : fmaf(m, c, down);
     float sum = 0.f;
 #pragma unroll 1
-    for (int i = 0; i < HK; i += 16) {
+    for (int i = from; i < HK; i += 16) {
         float x[16];
         tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
         const uint32_t s = bits(i);
@@ -282,39 +410,75 @@ static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint
     }
     m_io = m, l_io = l + sum;
 }
-// One pass over S against the m that there is, 32 columns at a time with the next load in flight (xa: the first ones, on their way).  MASKED: keys that
-// the row does not see count for nothing.  False: a sum has outgrown m (most: the most that it may be), and S is as it was.
-template <int DH, bool MASKED>
-static __device__ __forceinline__ bool block_fast(uint32_t tS, uint32_t tP, float *xa, const uint32_t *seen, float c, float mc, float most, float &l) {
-    constexpr int HK = BlockCfg<DH>::HK;
-    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-    float xb[32];
-    uint32_t pk[HK / 2];
-#pragma unroll
-    for (int i = 0; i < HK; i += 32) {
-        float *x = (i >> 5) & 1 ? xb : xa;
-        tmem_ld_wait();
-        loaded32(x);
-        if (i + 32 < HK) tmem_ld32(tS + i + 32, reinterpret_cast<uint32_t *>((i >> 5) & 1 ? xa : xb));
-#pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            float2 s = make_float2(x[2 * u], x[2 * u + 1]);
-            if (MASKED) s.x = seen[i >> 5] >> (2 * u) & 1 ? s.x : -INFINITY, s.y = seen[i >> 5] >> (2 * u + 1) & 1 ? s.y : -INFINITY;
-            const float2 e = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
-            const float2 p = make_float2(few_exp2(e.x), few_exp2(e.y));
-            ls[u & 1] = fadd2(ls[u & 1], p);
-            pk[i / 2 + u] = bf16_pair(p.x, p.y);
-        }
-    }
-    const float2 l2 = fadd2(ls[0], ls[1]);
-    const float sum = l2.x + l2.y;
-    if (!__all_sync(0xffffffffu, sum < most)) return false;
-    l += sum;
-#pragma unroll
-    for (int i = 0; i < HK / 2; i += 16) tmem_st16(tP + i, pk + i);
-    return true;
+// subnormal numbers to 0
+__device__ __forceinline__ float2 flush2(float2 a) {
+    unsigned long long ra, rd;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(ra) : "f"(a.x), "f"(a.y));
+    asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(rd) : "l"(ra), "l"(0ull));
+    float2 d;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(rd));
+    return d;
 }
-
+// 2^x of two numbers on the fp32 pipes: x = n + f with n whole, a polynomial of degree 3 in f (fitted for the least relative error on [-1/2, 1/2], 1.0e-4; P
+// is rounded to bf16, 2^-9 = 2e-3, anyway), n added to the exponent.  Below 2^-125 it is 2^-125.
+__device__ __forceinline__ float2 block_exp2_poly(float2 x) {
+    const float magic = 12582912.0f;                                   // 1.5 x 2^23: an ulp is 1
+    x.x = fmaxf(x.x, -127.4f), x.y = fmaxf(x.y, -127.4f);
+    const float2 t = fadd2(x, make_float2(magic, magic)), n = fadd2(t, make_float2(-magic, -magic));
+    const float2 f = ffma2(n, make_float2(-1.0f, -1.0f), x);
+    float2 p = ffma2(f, make_float2(0.05517166852951050f, 0.05517166852951050f), make_float2(0.2426111251115799f, 0.2426111251115799f));
+    p = ffma2(p, f, make_float2(0.6932609677314758f, 0.6932609677314758f));
+    p = ffma2(p, f, make_float2(0.9999280571937561f, 0.9999280571937561f));
+    p = make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+    return flush2(p);
+}
+#ifndef NPOLY
+#define NPOLY 2
+#endif
+// sixteen scores to P, as pairs, and their sum
+template <bool MASKED> __device__ __forceinline__ void block_exp16(const float *x, uint32_t bits, float c, float mc, uint32_t *pk, float2 (&ls)[2]) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        float2 s = make_float2(x[2 * u], x[2 * u + 1]);
+        if (MASKED) s.x = bits >> (2 * u) & 1 ? s.x : -INFINITY, s.y = bits >> (2 * u + 1) & 1 ? s.y : -INFINITY;
+        const float2 e = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
+        const float2 p = !MASKED && ((u + 1) * NPOLY / 8 != u * NPOLY / 8) ? block_exp2_poly(e) : make_float2(few_exp2(e.x), few_exp2(e.y));
+        ls[u & 1] = fadd2(ls[u & 1], p);
+        pk[u] = bf16_pair(p.x, p.y);
+    }
+}
+// One pass over a part of S against the m that there is, 32 columns a turn (a loop, so that its code stays near: unrolled, the exponentials of a part waited for
+// instructions a fifth of their time), halves of them loaded while the others are worked on.  MASKED: keys that the row does not see count for nothing; ready:
+// whether there is an m, or nothing to see.  Returns the columns that are done: fewer than all where a sum has outgrown m (most: the most that it may be),
+// and what is not done is as it was.
+template <int DH, bool MASKED>
+static __device__ __forceinline__ int block_fast(uint32_t tS, uint32_t tP, float (&xa)[16], const uint32_t *seen, bool ready, float c, float mc, float most, float &l) {
+    constexpr int HK = BlockCfg<DH>::HK;
+    float xb[16];
+#pragma unroll 1
+    for (int i = 0; i < HK; i += 32) {
+        const uint32_t bits = MASKED ? (i == 0 ? seen[0] : i == 32 ? seen[1] : seen[HK / 32 - 1]) : 0;
+        float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        uint32_t pk[16];
+        tmem_ld_wait();
+        loaded16(xa);
+        tmem_ld16(tS + i + 16, reinterpret_cast<uint32_t *>(xb));
+        block_exp16<MASKED>(xa, bits, c, mc, pk, ls);
+        tmem_ld_wait();
+        loaded16(xb);
+        if (i + 32 < HK) tmem_ld16(tS + i + 32, reinterpret_cast<uint32_t *>(xa));
+        block_exp16<MASKED>(xb, bits >> 16, c, mc, pk + 8, ls);
+        const float2 l2 = fadd2(ls[0], ls[1]);
+        const float sum = l2.x + l2.y;
+        if (!__all_sync(0xffffffffu, sum < most && (!MASKED || ready))) {
+            tmem_ld_wait();
+            return i;
+        }
+        l += sum;
+        tmem_st16(tP + i / 2, pk);
+    }
+    return HK;
+}
 // ---- which tiles a CTA takes --------------------------------------------------------------------------------
 // Work item `slot` as (sequence, number of its unit of R rows); sequence -1: there is none.  The deepest units of all sequences come first: they
 // see the most keys, and what is dealt out last should be short.  Up to BLOCK_SORTED sequences of different lengths there are as many items as units;
@@ -364,7 +528,7 @@ static __device__ __forceinline__ int2 block_unit(const BatchD &B, int share, in
 
 // Grid: items x heads of keys x split (a cluster's CTAs).
 template <int DH, typename Keys>
-__global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B, const AttnRows A, const Keys K, int kv_heads, int split, int tiles, float down) {
+__global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B, const AttnRows A, const __grid_constant__ Keys K, int kv_heads, int split, int tiles, float down) {
     using C = BlockCfg<DH>;
     constexpr int KB = C::KB, SUB = C::SUB, NBG = C::NBG, HK = C::HK, PARTS = C::PARTS;
     extern __shared__ uint8_t block_raw[];
@@ -374,7 +538,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % split, hs = blockIdx.x / split;
     const BlockBars bars = {smem_u32(smem + C::AT_BAR)};
-    if (threadIdx.x == 0) bars.init(C::NST, C::PW), s_expired = 0, s_bad[0] = INT_MAX, s_bad[1] = 0;
+    if (threadIdx.x == 0) bars.init(C::NST, Keys::TMA ? 1 : C::PW), s_expired = 0, s_bad[0] = INT_MAX, s_bad[1] = 0;
     const int2 unit = block_unit(B, A.share, tiles * 128, hs / kv_heads);
     if (unit.x < 0) return;                                 // (the whole cluster)
     BlockWork w;
@@ -402,8 +566,10 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
     }
     {
         const KeyRange first = K.range(B, len, sr.y, A.split(r0).x), last = K.range(B, len, sr.y, A.split(r0 + nr - 1).x);
-        const int all = max(0, (last.hi - first.lo + KB - 1) / KB), per = (all + split - 1) / split;
-        w.lo = first.lo + min(all, rank * per) * KB;
+        int lo = first.lo;
+        if constexpr (Keys::TMA) lo = K.begin(lo);
+        const int all = max(0, (last.hi - lo + KB - 1) / KB), per = (all + split - 1) / split;
+        w.lo = lo + min(all, rank * per) * KB;
         w.nb = max(0, min(all - rank * per, per));
         w.hi = min(last.hi, w.lo + w.nb * KB);
         w.edge_lo = last.lo, w.edge_hi = first.hi;
@@ -432,7 +598,12 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
     if (warp < C::SM0) {
         if (warp < C::PW) {
             leave_registers<64>();
-            if (w.nb) block_produce<DH>(K, B, w, smem, bars, s_bad, ok);
+            if constexpr (Keys::TMA) {
+                if (warp == 0) block_copy<DH>(K, B, w, smem, bars, ok);
+                else block_look_through<DH>(w, smem, bars, s_bad, ok);
+            } else {
+                if (w.nb) block_produce<DH>(K, B, w, smem, bars, s_bad, ok);
+            }
             if (!ok) s_expired = 1;
             asm volatile("bar.arrive 1, %0;" ::"n"(256 + 32 * C::PW) : "memory");
         } else {
@@ -462,71 +633,78 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
         float m = -INFINITY, l = 0.f;                                  // m: reference, in units of scores
         int n = 0;                                                     // the group's jobs so far
         const int b_first = T == 1 ? g : g ? w.begin1 : 0, b_end = T == 2 && !g ? w.end0 : w.nb, b_step = T == 2 ? 1 : 2;
+        uint32_t there[KB / 32];                                       // keys of the next block that are there
+        auto look = [&](int b) {
+            if constexpr (Keys::HOLES) {
+                ok = ok && tile_wait(bars.m_full(b % C::NM), (b / C::NM) & 1);
+                const uint32_t *mask = reinterpret_cast<const uint32_t *>(smem + C::AT_MASK + b % C::NM * 16);
+#pragma unroll
+                for (int k = 0; k < KB / 32; ++k) there[k] = mask[k];
+            } else {
+#pragma unroll
+                for (int k = 0; k < KB / 32; ++k) there[k] = 0xffffffffu;
+            }
+        };
         for (int b = b_first; b < b_end; b += b_step, ++n) {
             const int i = NBG == 1 ? 0 : n & 1;
             const uint32_t tJ = tmem + (g * NBG + i) * KB + lane_off;
-            ok = ok && tile_wait(bars.s_full(g, i), (n / NBG) & 1);
-            ok = ok && tile_wait(bars.m_full(b % C::NM), (b / C::NM) & 1);
+            // (the masks of a group's first block may be laps of their ring ahead; S says that they are there)
+            if (n == 0) {
+                ok = ok && tile_wait(bars.s_full(g, i), 0);
+                look(b);
+            }
+            uint32_t every = 0xffffffffu;
+#pragma unroll
+            for (int k = 0; k < KB / 32; ++k) every &= there[k];
+            const int p0 = w.lo + b * KB;
+            const bool plain = __all_sync(0xffffffffu, every == 0xffffffffu && p0 >= kr.lo && p0 + KB <= kr.hi && m != -INFINITY) && some;
+            if (n) ok = ok && tile_wait(bars.s_full(g, i), (n / NBG) & 1);
             __syncwarp();
             tc_fence_after();
-#pragma unroll
+#pragma unroll 1
             for (int part = 0; part < PARTS; ++part) {
-                if (some) {                                            // (of rows that are not there P may be anything)
-                    const uint32_t tS = tJ + part * HK, tP = tJ + part * (HK / 2);
-                    float xa[32];
-                    tmem_ld32(tS, reinterpret_cast<uint32_t *>(xa));   // (of use where the fast path is taken)
-                    const uint32_t *mask = reinterpret_cast<const uint32_t *>(smem + C::AT_MASK + b % C::NM * 16) + part * (HK / 32);
-                    const int p0 = w.lo + b * KB + part * HK;
-                    uint32_t seen[HK / 32], every = 0xffffffffu, any = 0;
+                const uint32_t tS = tJ + part * HK, tP = tJ + part * (HK / 2);
+                float x[16];
+                if (some) tmem_ld16(tS, reinterpret_cast<uint32_t *>(x));
+                if (plain) {                                           // all rows have an m and see all of these keys
+                    const int done = block_fast<DH, false>(tS, tP, x, there, true, c, fmaf(m, c, down), most, l);
+                    if (done < HK)
+                        block_slow<DH>(tS, tP, tO, there, done, c, down, n * PARTS + part, bars.pv_done(g, n * PARTS + part - 1), m, l, ok);
+                } else if (some) {                                     // (of rows that are not there P may be anything)
+                    const int a = kr.lo - p0 - part * HK, e = kr.hi - p0 - part * HK;            // keys a .. e - 1 of the part
+                    uint32_t seen[HK / 32], any = 0;
 #pragma unroll
-                    for (int k = 0; k < HK / 32; ++k) seen[k] = mask[k], every &= seen[k];
-                    const bool all_whole = __all_sync(0xffffffffu, every == 0xffffffffu && p0 >= kr.lo && p0 + HK <= kr.hi);
-                    if (!all_whole) {
-                        const int a = kr.lo - p0, e = kr.hi - p0;      // keys a .. e - 1 of the part
+                    for (int k = 0; k < HK / 32; ++k) {
+                        const int a1 = min(max(a - 32 * k, 0), 32), e1 = min(max(e - 32 * k, 0), 32);
+                        seen[k] = (part ? there[KB / 32 - HK / 32 + k] : there[k]) & (e1 == 32 ? 0xffffffffu : (1u << e1) - 1) &
+                                  ~(a1 == 32 ? 0xffffffffu : (1u << a1) - 1);
+                        any |= seen[k];
+                    }
+                    tmem_ld_wait();
+                    loaded16(x);
+                    if (!__any_sync(0xffffffffu, any)) {               // none of the warp's rows sees any of these keys
+                        const uint32_t zero[16] = {};
 #pragma unroll
-                        for (int k = 0; k < HK / 32; ++k) {
-                            const int a1 = min(max(a - 32 * k, 0), 32), e1 = min(max(e - 32 * k, 0), 32);
-                            seen[k] &= (e1 == 32 ? 0xffffffffu : (1u << e1) - 1) & ~(a1 == 32 ? 0xffffffffu : (1u << a1) - 1);
-                            any |= seen[k];
-                        }
+                        for (int k = 0; k < HK / 2; k += 16) tmem_st16(tP + k, zero);
                     } else {
-                        any = 1;
-                    }
-                    if (__any_sync(0xffffffffu, m == -INFINITY)) {
-                        // a row without m (nothing has been summed for it): the largest of the first scores will do, if it sees one of them
-                        tmem_ld_wait();
-                        loaded32(xa);
-                        float top = -INFINITY;
+                        if (__any_sync(0xffffffffu, m == -INFINITY)) {
+                            // a row without m (nothing has been summed for it): the largest of the first scores will do, if it sees one of them
+                            float top = -INFINITY;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) top = fmaxf(top, seen[0] >> e & 1 ? xa[e] : -INFINITY);
-                        if (m == -INFINITY) m = top;
-                    }
-                    bool done = false;
-                    if (__all_sync(0xffffffffu, m != -INFINITY || !any)) {
-                        const float mc = m == -INFINITY ? 0.f : fmaf(m, c, down);
-                        if (all_whole) {
-                            done = block_fast<DH, false>(tS, tP, xa, seen, c, mc, most, l);
-                        } else if (__any_sync(0xffffffffu, any)) {
-                            done = block_fast<DH, true>(tS, tP, xa, seen, c, mc, most, l);
-                        } else {                                       // none of the warp's rows sees any of these keys
-                            const uint32_t zero[16] = {};
-                            tmem_ld_wait();
-                            loaded32(xa);
-#pragma unroll
-                            for (int k = 0; k < HK / 2; k += 16) tmem_st16(tP + k, zero);
-                            done = true;
+                            for (int e = 0; e < 16; ++e) top = fmaxf(top, seen[0] >> e & 1 ? x[e] : -INFINITY);
+                            if (m == -INFINITY) m = top;
                         }
+                        const int done = block_fast<DH, true>(tS, tP, x, seen, m != -INFINITY || !any, c, m == -INFINITY ? 0.f : fmaf(m, c, down), most, l);
+                        if (done < HK)
+                            block_slow<DH>(tS, tP, tO, seen, done, c, down, n * PARTS + part, bars.pv_done(g, n * PARTS + part - 1), m, l, ok);
                     }
-                    if (!done) {
-                        tmem_ld_wait();
-                        block_slow<DH>(tS, tP, tO, seen, c, down, n * PARTS + part, bars.pv_done(g, n * PARTS + part - 1), m, l, ok);
-                    }
-                    tmem_st_wait();
                 }
+                tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars.p_full(g, PARTS == 1 ? i : part));
             }
+            if (b + b_step < b_end) look(b + b_step);
         }
         const int parts = n * PARTS;
         if (n) ok = ok && tile_wait(bars.pv_done(g, parts - 1), ((parts - 1) >> 1) & 1);
@@ -677,6 +855,27 @@ template <int DH, typename F> static TilePlan block_plan(long long kv_heads, lon
     return best;
 }
 
+// A map of bf16 numbers for boxes of 64 x `rows`, swizzled as the products' operands are; dims and strides (bytes; of all but the first) from the innermost on.
+static int block_map(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides, int rows) {
+    typedef CUresult (*Encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                               CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<Encode> known;                      // (the same whichever thread stores it)
+    Encode encode = known;
+    if (!encode) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess || !fn || found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return NFD_E_CUDA;
+        }
+        known = encode = (Encode)fn;
+    }
+    const cuuint32_t box[3] = {64, (cuuint32_t)rows, 1}, steps[3] = {1, 1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? NFD_OK : NFD_E_CUDA;
+}
+
 template <int DH, typename Keys>
 static int launch_attn_block(const BatchD &B, const AttnRows &A, const Keys &K, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
     using C = BlockCfg<DH>;
@@ -705,4 +904,38 @@ static int launch_attn_block(const BatchD &B, const AttnRows &A, const Keys &K, 
         return NFD_E_CUDA;
     }
     return NFD_OK;
+}
+
+// The rows of a call to the kernel that suits the keys: by TMA where head dimension, pages and strides allow it.
+template <int DH> static int attn_block(const BatchD &B, const AttnRows &A, const PageKeys<bf16, DH> &K, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
+    const long long planes = (long long)K.P.n_pages * K.P.heads;
+    int rows = BlockCfg<DH>::KB & -BlockCfg<DH>::KB;        // the largest power of two that blocks and pages consist of
+    while (K.P.page_tokens % rows) rows /= 2;
+    if constexpr (DH >= 64) {
+        if (rows >= 8 && planes < INT_MAX) {
+            PageBoxes<DH> boxes;
+            static_cast<PageKeys<bf16, DH> &>(boxes) = K;
+            boxes.rows = rows;
+            const cuuint64_t dims[3] = {DH, (cuuint64_t)K.P.page_tokens, (cuuint64_t)planes}, strides[2] = {DH * 2, (cuuint64_t)K.P.page_tokens * DH * 2};
+            for (int i = 0; i < 2; ++i)
+                if (const int r = block_map(&boxes.maps[i], i ? K.P.v : K.P.k, 3, dims, strides, rows)) return r;
+            return launch_attn_block<DH>(B, A, boxes, kv_heads, keys, dev, n_sm, st);
+        }
+    }
+    return launch_attn_block<DH>(B, A, K, kv_heads, keys, dev, n_sm, st);
+}
+template <int DH> static int attn_block(const BatchD &B, const AttnRows &A, const PackedKeys<bf16, DH> &K, int kv_heads, long long keys, int dev, int n_sm, cudaStream_t st) {
+    if constexpr (DH >= 64) {
+        PackedBoxes<DH> boxes;
+        static_cast<PackedKeys<bf16, DH> &>(boxes) = K;
+        const cuuint64_t dims[2] = {(cuuint64_t)kv_heads * DH, (cuuint64_t)B.n_rows};
+        for (int i = 0; i < 2; ++i) {
+            const cuuint64_t stride = (cuuint64_t)(i ? K.v_stride : K.k_stride) * 2;
+            if (stride >= 1ull << 40) return NFD_E_RANGE;
+            if (const int r = block_map(&boxes.maps[i], i ? K.v : K.k, 2, dims, &stride, BlockCfg<DH>::KB)) return r;
+        }
+        return launch_attn_block<DH>(B, A, boxes, kv_heads, keys, dev, n_sm, st);
+    } else {
+        return launch_attn_block<DH>(B, A, K, kv_heads, keys, dev, n_sm, st);
+    }
 }

@@ -19,7 +19,7 @@ int launch_rows(const BatchD &B, const AttnRows &A, int dtype, int head_dim, int
             return launch_attn_f32<DH>(B, A, F32Rows<K, DH>(make.template operator()<K>(), keys), kv_heads, dev, n_sm, st);
         }
         using K = Keys<bf16, DH>;
-        if ((long long)B.max_rows * A.share > few_most(DH)) return launch_attn_block<DH>(B, A, make.template operator()<K>(), kv_heads, keys, dev, n_sm, st);
+        if ((long long)B.max_rows * A.share > few_most(DH)) return attn_block<DH>(B, A, make.template operator()<K>(), kv_heads, keys, dev, n_sm, st);
         FewRows<K, DH> src;
         src.K = make.template operator()<K>(), src.bits = (float)sum_bits(8, (int)keys);       // (probabilities grow to 2^8 before m follows)
         return launch_attn_few<FewRows<K, DH>, DH>(B, A, src, kv_heads, keys, dev, n_sm, st);

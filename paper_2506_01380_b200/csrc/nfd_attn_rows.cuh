@@ -40,6 +40,7 @@ template <typename TS, int DH> struct StateKeys {
 // Pages of TS and the rows of packed sequences, both under the block-wise causal mask.  A reader walks keys p, p + step, ... with a cursor, which
 // tells a key's row (-1: there is none): of the pages, (page, head, offset), or of the row buffers.
 template <typename TS, int DH> struct PageKeys {
+    static constexpr bool TMA = false, HOLES = true;                     // a key within the range may not be there
     PagesD P;
     CausalMask mask;
     __device__ __forceinline__ int length(const BatchD &B, int s) const { return B.tokens(s); }
@@ -70,6 +71,7 @@ template <typename TS, int DH> struct PageKeys {
     __device__ __forceinline__ const TS *v_row(long long row, int) const { return (const TS *)P.v + row * DH; }
 };
 template <typename TS, int DH> struct PackedKeys {
+    static constexpr bool TMA = false, HOLES = false;
     const TS *k, *v;
     long long k_stride, v_stride;
     CausalMask mask;
