@@ -455,30 +455,29 @@ template <int DH, bool MASKED>
 static __device__ __forceinline__ int block_fast(uint32_t tS, uint32_t tP, float (&xa)[16], const uint32_t *seen, bool ready, float c, float mc, float most, float &l) {
     constexpr int HK = BlockCfg<DH>::HK;
     float xb[16];
-#pragma unroll 1
+    float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    uint32_t pk[HK / 2];
+#pragma unroll
     for (int i = 0; i < HK; i += 32) {
-        const uint32_t bits = MASKED ? (i == 0 ? seen[0] : i == 32 ? seen[1] : seen[HK / 32 - 1]) : 0;
-        float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        uint32_t pk[16];
+        const uint32_t bits = MASKED ? seen[i / 32] : 0;
         tmem_ld_wait();
         loaded16(xa);
         tmem_ld16(tS + i + 16, reinterpret_cast<uint32_t *>(xb));
-        block_exp16<MASKED>(xa, bits, c, mc, pk, ls);
+        block_exp16<MASKED>(xa, bits, c, mc, pk + i / 2, ls);
         tmem_ld_wait();
         loaded16(xb);
         if (i + 32 < HK) tmem_ld16(tS + i + 32, reinterpret_cast<uint32_t *>(xa));
-        block_exp16<MASKED>(xb, bits >> 16, c, mc, pk + 8, ls);
-        const float2 l2 = fadd2(ls[0], ls[1]);
-        const float sum = l2.x + l2.y;
-        if (!__all_sync(0xffffffffu, sum < most && (!MASKED || ready))) {
-            tmem_ld_wait();
-            return i;
-        }
-        l += sum;
-        tmem_st16(tP + i / 2, pk);
+        block_exp16<MASKED>(xb, bits >> 16, c, mc, pk + i / 2 + 8, ls);
     }
+    const float2 l2 = fadd2(ls[0], ls[1]);
+    const float sum = l2.x + l2.y;
+    if (!__all_sync(0xffffffffu, sum < most && (!MASKED || ready))) return 0;
+    l += sum;
+#pragma unroll
+    for (int i = 0; i < HK / 2; i += 16) tmem_st16(tP + i, pk + i);
     return HK;
 }
+
 // ---- which tiles a CTA takes --------------------------------------------------------------------------------
 // Work item `slot` as (sequence, number of its unit of R rows); sequence -1: there is none.  The deepest units of all sequences come first: they
 // see the most keys, and what is dealt out last should be short.  Up to BLOCK_SORTED sequences of different lengths there are as many items as units;
