@@ -32,23 +32,25 @@
 
 template <int DH> struct BlockCfg {
     static constexpr int SUB = DH == 128 ? 2 : 1;          // 64-dim parts of a row
+    static constexpr int NG = DH == 128 ? 2 : 3;           // softmax groups
     static constexpr int KB = DH == 128 ? 128 : 96;        // keys of a block
-    static constexpr int NBG = DH == 128 ? 1 : 2;          // S accumulators of a group
     static constexpr int PARTS = DH == 128 ? 2 : 1;        // a block's P goes to its product in so many parts
     static constexpr int HK = KB / PARTS;
-    static constexpr int PW = 4, KPW = KB / PW;            // producer warps, keys of each
-    static constexpr int SM0 = 8;                          // first softmax warp
+    static constexpr int PW = DH == 128 ? 4 : 3, KPW = KB / PW;        // producer warps, keys of each; the next one is the issuer
+    static constexpr int SM0 = 16 - 4 * NG;                // first softmax warp
+    static constexpr int REGS_LOW = DH == 128 ? 56 : 80, REGS_SOFTMAX = DH == 128 ? 200 : 144;      // registers of a thread: 4 x 128 to share out
     static constexpr int NST = DH == 128 ? 5 : 12;         // stages of the ring: K and V of the first block, of the second ...
     static constexpr int FLY = DH == 128 ? 3 : 5;          // of which the copies are in flight
     static constexpr int NM = 16;                          // masks
     static constexpr int Q_BYTES = SUB * 128 * 128;        // a tile's queries
     static constexpr int BLK = SUB * KB * 128;             // a block of K or V
-    static constexpr int AT_Q = 0, AT_R = 2 * Q_BYTES, AT_MASK = AT_R + NST * BLK, AT_BAR = AT_MASK + NM * 16, SMEM = AT_BAR + 528 + 1024;
-    static constexpr int TM_O = 2 * NBG * KB;              // S of group g, number i, and over it P, at (g NBG + i) KB; O of group g at TM_O + g 64 SUB
+    static constexpr int AT_Q = 0, AT_R = NG * Q_BYTES, AT_MASK = AT_R + NST * BLK, AT_BAR = AT_MASK + NM * 16, SMEM = AT_BAR + 544 + 1024;
+    static constexpr int TM_O = NG * KB;                   // S of group g, and over it P, at g KB; O at TM_O + g 64 SUB
     static constexpr int STATE = 128 * DH * 4 + 128 * 8;   // a group's state, over queries and ring: O as [DH / 4][128] float4, then [128] (m, l)
-    static_assert(TM_O + 2 * 64 * SUB <= 512 && 2 * STATE + 128 * 8 <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
+    static_assert(TM_O + NG * 64 * SUB <= 512 && NG * STATE + 128 * 8 <= AT_MASK && SMEM <= 232448, "tensor and shared memory");
     static_assert(SMEM > 232448 / 2, "a CTA has an SM, and its tensor memory, to itself: nobody in a cluster waits for what another cluster holds");
-    static_assert(2 * NBG + NST / 2 + 1 <= NM, "K runs so many blocks ahead of the softmax");
+    static_assert(NG + NST / 2 + 1 <= NM, "K runs so many blocks ahead of the softmax");
+    static_assert((SM0 / 4) * REGS_LOW + NG * REGS_SOFTMAX <= 512 && PW < SM0, "registers; warps");
     static_assert(KPW * (DH / 8) % 32 == 0 && KPW <= 32 && KPW % 8 == 0 && HK % 32 == 0, "copies; bits of a warp's keys are whole bytes; S by 32 columns");
 };
 
@@ -57,34 +59,48 @@ struct BlockBars {
     __device__ __forceinline__ uint32_t full(int s) const { return b + 8 * s; }                  // stages (up to 12)
     __device__ __forceinline__ uint32_t empty(int s) const { return b + 96 + 8 * s; }
     __device__ __forceinline__ uint32_t m_full(int s) const { return b + 192 + 8 * s; }          // masks (16)
-    __device__ __forceinline__ uint32_t s_full(int g, int i) const { return b + 320 + 16 * g + 8 * i; }
-    __device__ __forceinline__ uint32_t p_full(int g, int i) const { return b + 352 + 16 * g + 8 * i; }   // of an accumulator, or of its parts
+    __device__ __forceinline__ uint32_t s_full(int g) const { return b + 320 + 8 * g; }          // groups (up to 3)
+    __device__ __forceinline__ uint32_t p_full(int g, int part) const { return b + 344 + 16 * g + 8 * part; }
     // of a group's even and odd parts: a warp may be done with one before the product of the one before it is
-    __device__ __forceinline__ uint32_t pv_done(int g, int n) const { return b + 384 + 16 * g + 8 * (n & 1); }
-    __device__ __forceinline__ uint32_t q_full() const { return b + 416; }
-    __device__ __forceinline__ uint32_t landed(int s) const { return b + 424 + 8 * s; }          // stages: values that are looked through before they are used
-    static constexpr int BYTES = 424 + 96;
-    __device__ __forceinline__ void init(int stages, int producers) const {
-        for (int s = 0; s < stages; ++s) mbar_init(full(s), producers), mbar_init(empty(s), 1), mbar_init(landed(s), 1);
-        for (int s = 0; s < 16; ++s) mbar_init(m_full(s), producers);
-        for (int g = 0; g < 2; ++g)
-            for (int i = 0; i < 2; ++i) mbar_init(s_full(g, i), 1), mbar_init(p_full(g, i), 4), mbar_init(pv_done(g, i), 1);
-        mbar_init(q_full(), 8);
-        fence_mbar_init();
+    __device__ __forceinline__ uint32_t pv_done(int g, int n) const { return b + 392 + 16 * g + 8 * (n & 1); }
+    __device__ __forceinline__ uint32_t q_full() const { return b + 440; }
+    __device__ __forceinline__ uint32_t landed(int s) const { return b + 448 + 8 * s; }          // stages: values that are looked through before they are used
+    // (a barrier to a thread: one after the other they took a thousand clocks)
+    __device__ __forceinline__ void init(int producers, int groups) const {
+        const int i = threadIdx.x;
+        if (i < 12) mbar_init(full(i), producers);
+        else if (i < 24) mbar_init(empty(i - 12), 1);
+        else if (i < 36) mbar_init(landed(i - 24), 1);
+        else if (i < 52) mbar_init(m_full(i - 36), producers);
+        else if (i < 55) mbar_init(s_full(i - 52), 1);
+        else if (i < 61) mbar_init(p_full((i - 55) >> 1, (i - 55) & 1), 4);
+        else if (i < 67) mbar_init(pv_done((i - 61) >> 1, i - 61), 1);
+        else if (i == 67) mbar_init(q_full(), 4 * groups);
+        if (i < 68) fence_mbar_init();
     }
 };
 
-// What a CTA works on: keys lo .. hi - 1 of a sequence in nb blocks; keys that not all rows see: those below
-// edge_lo, those from edge_hi on.
-struct BlockWork {
+// What a CTA works on: keys lo .. hi - 1 of a sequence in nb blocks, T tiles; keys that not all rows see: those below edge_lo, those from edge_hi on.
+template <int NG> struct BlockWork {
     int s, h, first_row, lo, hi, nb, T, edge_lo, edge_hi;
+    int b0[NG], b1[NG];                                     // several tiles: each takes blocks b0 .. b1 - 1
     // are there rows of the CTA that do not see all of block b (of KB keys)
     __device__ __forceinline__ bool edge(int b, int KB) const { return lo + b * KB < edge_lo || lo + b * KB + KB > edge_hi; }
-    int end0, begin1;                                       // two tiles: the first takes the blocks before end0, the second those from begin1 on
-    // does group g take block b (one tile: they take turns)
-    __device__ __forceinline__ bool takes(int g, int b) const { return T == 2 ? (g ? b >= begin1 : b < end0) : (b & 1) == g; }
-    // and which of its jobs is that
-    __device__ __forceinline__ int job(int g, int b) const { return T == 1 ? b >> 1 : g ? b - begin1 : b; }
+    // does group g take block b (one tile: they take turns); which of its jobs is that; is it the first, the last to take it
+    __device__ __forceinline__ bool takes(int g, int b) const { return T > 1 ? b >= b0[g] && b < b1[g] : b % NG == g; }
+    __device__ __forceinline__ int job(int g, int b) const { return T > 1 ? b - b0[g] : b / NG; }
+    __device__ __forceinline__ bool first(int g, int b) const {
+        bool f = true;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) f = f && !(k < g && takes(k, b));
+        return f;
+    }
+    __device__ __forceinline__ bool last(int g, int b) const {
+        bool f = true;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) f = f && !(k > g && takes(k, b));
+        return f;
+    }
 };
 template <int n> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(n)); }
 template <int n> __device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(n)); }
@@ -143,7 +159,7 @@ __device__ __forceinline__ bool block_take_out(uint8_t *at) {
 }
 // By TMA, one warp: a lane's copy of a block is a box of 64 dims and `box` keys, looked up on the way.
 template <int DH, typename Keys>
-static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B, const BlockWork &w, uint8_t *smem, const BlockBars &bars, bool &ok) {
+static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B, const BlockWork<BlockCfg<DH>::NG> &w, uint8_t *smem, const BlockBars &bars, bool &ok) {
     using C = BlockCfg<DH>;
     const int lane = threadIdx.x & 31, box = K.box(), groups = C::KB / box, part = lane / groups, group = lane - part * groups;
     const bool mine = part < C::SUB;
@@ -184,8 +200,8 @@ static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B
     // (nobody leaves with copies in flight, whoever has given up waiting)
     for (int i = max(0, items - C::NST); i < items; ++i) ok = tile_wait(bars.full(i % C::NST), (i / C::NST) & 1) && ok;
 }
-// and three warps that look through the values of blocks that not all rows see
-template <int DH> static __device__ __forceinline__ void block_look_through(const BlockWork &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
+// and the other producer warps look through the values of blocks that not all rows see
+template <int DH> static __device__ __forceinline__ void block_look_through(const BlockWork<BlockCfg<DH>::NG> &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
     using C = BlockCfg<DH>;
     uint32_t laps = 0;                                       // phases of the stages' barriers
     for (int b = 0; b < w.nb; ++b) {                         // (all of it, whatever runs out: the threads meet at a barrier)
@@ -194,16 +210,16 @@ template <int DH> static __device__ __forceinline__ void block_look_through(cons
         if (ok) ok = tile_wait(bars.landed(st), laps >> st & 1);
         laps ^= 1u << st;
         bool some = false;
-        for (int i = (threadIdx.x - 32) * 16; i < C::BLK; i += 96 * 16) some |= block_take_out(smem + C::AT_R + st * C::BLK + i);
+        for (int i = (threadIdx.x - 32) * 16; i < C::BLK; i += (C::PW - 1) * 32 * 16) some |= block_take_out(smem + C::AT_R + st * C::BLK + i);
         if (some) atomicMin(bad, w.lo + b * C::KB), atomicMax(bad + 1, w.lo + b * C::KB + C::KB);
         fence_proxy_async_smem();
-        asm volatile("bar.sync 4, 96;" ::: "memory");
+        asm volatile("bar.sync 4, %0;" ::"n"((C::PW - 1) * 32) : "memory");
         if (threadIdx.x == 32) mbar_arrive(bars.full(st));
     }
 }
-// By cp.async, four warps.
+// By cp.async, all of them.
 template <int DH, typename Keys>
-static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD &B, const BlockWork &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
+static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD &B, const BlockWork<BlockCfg<DH>::NG> &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
     using C = BlockCfg<DH>;
     constexpr int CPR = DH / 8, N = C::KPW * CPR / 32;       // 16-byte pieces of a row; a lane's of a block
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % CPR, sub = lane / CPR;
@@ -278,9 +294,9 @@ static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD
 // (the tensor pipe takes one thread's instructions in order).  Nothing here branches on whether a wait has run out (what follows then is computed from whatever is
 // there, and thrown away): with control flow that is the same for all lanes the operands stay in uniform registers.  Otherwise, moved there one by one for
 // every product, they cost more than the products.
-template <int DH> static __device__ __forceinline__ bool block_issue(const BlockWork &w, const BlockBars &bars, uint32_t base, uint32_t tmem) {
+template <int DH> static __device__ __forceinline__ bool block_issue(const BlockWork<BlockCfg<DH>::NG> &w, const BlockBars &bars, uint32_t base, uint32_t tmem) {
     using C = BlockCfg<DH>;
-    constexpr int KB = C::KB, SUB = C::SUB, NST = C::NST, NBG = C::NBG;
+    constexpr int KB = C::KB, SUB = C::SUB, NST = C::NST, NG = C::NG;
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, KB), idesc_pv = umma_idesc_bf16(128, DH) | (1u << 16);       // V: MN-major
     // (a cluster's addresses hold the CTA's rank above bit 23; V's other 64 dims are KB rows on: the leading offset)
     const uint32_t at = base & 0x3ffffu, dQ = (at + C::AT_Q) >> 4, dR = (at + C::AT_R) >> 4, lead = (KB * 128 >> 4) << 16;
@@ -289,17 +305,16 @@ template <int DH> static __device__ __forceinline__ bool block_issue(const Block
         if (ok) ok = tile_wait(bar, parity);
     };
     auto scores = [&](int g, int b, int st, uint32_t par) {  // stage of the block's K and its phase
-        if (g == 0 || !w.takes(0, b)) wait(bars.full(st), par);
+        if (w.first(g, b)) wait(bars.full(st), par);
         tc_fence_after();
-        const int i = NBG == 1 ? 0 : w.job(g, b) & 1;
-        const uint32_t q = dQ + (w.T == 1 ? 0 : g) * (C::Q_BYTES >> 4), k = dR + st * (C::BLK >> 4), d = tmem + (g * NBG + i) * KB;
+        const uint32_t q = dQ + (w.T == 1 ? 0 : g) * (C::Q_BYTES >> 4), k = dR + st * (C::BLK >> 4), d = tmem + g * KB;
 #pragma unroll
         for (int e = 0; e < (DH + 15) / 16; ++e)
             tile_mma_ss(d, q + (e >> 2) * (128 * 128 >> 4) + 2 * (e & 3), k + (e >> 2) * (KB * 128 >> 4) + 2 * (e & 3), idesc_s, e != 0);
-        umma_commit(bars.s_full(g, i));
-        if (g == 1 || !w.takes(1, b)) umma_commit(bars.empty(st));
+        umma_commit(bars.s_full(g));
+        if (w.last(g, b)) umma_commit(bars.empty(st));
     };
-    const int ahead = w.T == 1 ? 2 * NBG : NBG;              // blocks
+    const int ahead = w.T == 1 ? NG : 1;                     // blocks
     int sk = 0, sv = 1;                                      // stages of the next K and the next V, and their phases
     uint32_t pk = 0, pv = 0;
     auto on = [&](int &st, uint32_t &par) {
@@ -308,28 +323,28 @@ template <int DH> static __device__ __forceinline__ bool block_issue(const Block
     };
     for (int b = 0; b < ahead && b < w.nb; ++b) {
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+        for (int g = 0; g < NG; ++g)
             if (w.takes(g, b)) scores(g, b, sk, pk);
         on(sk, pk);
     }
     for (int b = 0; b < w.nb; ++b) {
         const uint32_t v = (dR + sv * (C::BLK >> 4)) | lead;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
+        for (int g = 0; g < NG; ++g) {
             if (w.takes(g, b)) {
-                if (g == 0 || !w.takes(0, b)) wait(bars.full(sv), pv);
-                const int n = w.job(g, b), i = NBG == 1 ? 0 : n & 1;
-                const uint32_t d = tmem + C::TM_O + g * 64 * SUB, a = tmem + (g * NBG + i) * KB;
+                if (w.first(g, b)) wait(bars.full(sv), pv);
+                const int n = w.job(g, b);
+                const uint32_t d = tmem + C::TM_O + g * 64 * SUB, a = tmem + g * KB;
 #pragma unroll
                 for (int part = 0; part < C::PARTS; ++part) {
-                    wait(bars.p_full(g, C::PARTS == 1 ? i : part), (n / NBG) & 1);
+                    wait(bars.p_full(g, part), n & 1);
                     tc_fence_after();
                     constexpr int E = C::HK / 16;
 #pragma unroll
                     for (int e = part * E; e < (part + 1) * E; ++e) tile_mma_ts(d, a + 8 * e, v + e * (2048 >> 4), idesc_pv, n != 0 || e != 0);
                     umma_commit(bars.pv_done(g, n * C::PARTS + part));
                 }
-                if (g == 1 || !w.takes(1, b)) umma_commit(bars.empty(sv));
+                if (w.last(g, b)) umma_commit(bars.empty(sv));
             }
             if (b + ahead < w.nb && w.takes(g, b + ahead)) scores(g, b + ahead, sk, pk);
         }
@@ -479,14 +494,19 @@ static __device__ __forceinline__ int block_fast(uint32_t tS, uint32_t tP, float
 }
 
 // ---- which tiles a CTA takes --------------------------------------------------------------------------------
-// Work item `slot` as (sequence, number of its unit of R rows); sequence -1: there is none.  The deepest units of all sequences come first: they
+// Units of `tiles` x 128 rows that n rows of a sequence make.
+__device__ __forceinline__ int block_units(int n, int share, int tiles) {
+    const int t = (n * share + 127) >> 7;
+    return tiles == 1 ? t : tiles == 2 ? (t + 1) >> 1 : (t + 2) / 3;
+}
+// Work item `slot` as (sequence, number of its unit); sequence -1: there is none.  The deepest units of all sequences come first: they
 // see the most keys, and what is dealt out last should be short.  Up to BLOCK_SORTED sequences of different lengths there are as many items as units;
 // otherwise as many as if all sequences had max_rows.
-static __device__ __forceinline__ int2 block_unit(const BatchD &B, int share, int R, long long slot) {
-    const int most = (int)(((long long)B.max_rows * share + R - 1) / R);
+static __device__ __forceinline__ int2 block_unit(const BatchD &B, int share, int tiles, int slot) {
+    const int most = block_units(B.max_rows, share, tiles);
     if (!B.row_start || B.n_seqs > BLOCK_SORTED) {
-        const int t = (int)(slot / B.n_seqs);
-        return make_int2(t < most ? (int)(slot - (long long)t * B.n_seqs) : -1, most - 1 - t);
+        const int t = slot / B.n_seqs;
+        return make_int2(t < most ? slot - t * B.n_seqs : -1, most - 1 - t);
     }
     const int lane = threadIdx.x & 31;
     constexpr int N = BLOCK_SORTED / 32;
@@ -494,10 +514,10 @@ static __device__ __forceinline__ int2 block_unit(const BatchD &B, int share, in
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         t[i] = 0;
-        if (i * 32 < B.n_seqs && i * 32 + lane < B.n_seqs) t[i] = (int)(((long long)min(B.rows(i * 32 + lane).y, B.max_rows) * share + R - 1) / R);
+        if (i * 32 < B.n_seqs && i * 32 + lane < B.n_seqs) t[i] = block_units(min(B.rows(i * 32 + lane).y, B.max_rows), share, tiles);
         all += t[i];
     }
-    if (slot >= __reduce_add_sync(0xffffffffu, (unsigned)all)) return make_int2(-1, 0);
+    if (slot >= (int)__reduce_add_sync(0xffffffffu, (unsigned)all)) return make_int2(-1, 0);
     // the smallest depth j with no more than `slot` units deeper than it
     int lo = 0, hi = most - 1;
     auto deeper = [&](int j) {
@@ -511,7 +531,7 @@ static __device__ __forceinline__ int2 block_unit(const BatchD &B, int share, in
         if (deeper(j) <= slot) hi = j;
         else lo = j + 1;
     }
-    int left = (int)slot - deeper(lo), s = -1;
+    int left = slot - deeper(lo), s = -1;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const uint32_t m = __ballot_sync(0xffffffffu, t[i] > lo);
@@ -527,9 +547,9 @@ static __device__ __forceinline__ int2 block_unit(const BatchD &B, int share, in
 
 // Grid: items x heads of keys x split (a cluster's CTAs).
 template <int DH, typename Keys>
-__global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B, const AttnRows A, const __grid_constant__ Keys K, int kv_heads, int split, int tiles, float down) {
+__global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B, const AttnRows A, const __grid_constant__ Keys K, int kv_heads, int split, int tiles, FastDiv by_share, float down) {
     using C = BlockCfg<DH>;
-    constexpr int KB = C::KB, SUB = C::SUB, NBG = C::NBG, HK = C::HK, PARTS = C::PARTS;
+    constexpr int KB = C::KB, SUB = C::SUB, NG = C::NG, HK = C::HK, PARTS = C::PARTS;
     extern __shared__ uint8_t block_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(block_raw) + 1023) & ~(uintptr_t)1023);
     __shared__ uint32_t s_tmem;
@@ -537,11 +557,13 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % split, hs = blockIdx.x / split;
     const BlockBars bars = {smem_u32(smem + C::AT_BAR)};
-    if (threadIdx.x == 0) bars.init(C::NST, Keys::TMA ? 1 : C::PW), s_expired = 0, s_bad[0] = INT_MAX, s_bad[1] = 0;
-    const int2 unit = block_unit(B, A.share, tiles * 128, hs / kv_heads);
+    bars.init(Keys::TMA ? 1 : C::PW, NG);
+    if (threadIdx.x == 96) s_expired = 0, s_bad[0] = INT_MAX, s_bad[1] = 0;
+    const int slot = hs / kv_heads;
+    const int2 unit = block_unit(B, A.share, tiles, slot);
     if (unit.x < 0) return;                                 // (the whole cluster)
-    BlockWork w;
-    w.s = unit.x, w.h = hs % kv_heads;
+    BlockWork<NG> w;
+    w.s = unit.x, w.h = hs - slot * kv_heads;
     const int r0 = unit.y * tiles * 128;
     const int2 sr = B.rows(w.s);
     const int len = K.length(B, w.s);
@@ -549,33 +571,47 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
     if (r0 >= rows) return;                                 // (the whole cluster)
     __syncthreads();
     const int nr = min(tiles * 128, rows - r0), T = (nr + 127) / 128;
+    // row r of the CTA: row of the sequence, which of the heads
+    auto split_row = [&](int r) {
+        const int i = by_share.div(r0 + r);
+        return make_int2(i, r0 + r - i * A.share);
+    };
     w.T = T, w.first_row = sr.x;
     if (warp >= C::SM0) {
-        // softmax warps: the row's queries, into the operand of its tile, a row's pieces by neighbouring lanes; of one tile each group half
+        // softmax warps: the row's queries, into the operand of its tile, a row's pieces by neighbouring lanes; of one tile each group a share
         constexpr int CPR = DH / 8, RPI = 32 / CPR;
         const int g = (warp - C::SM0) >> 2, piece = lane % CPR;
         const uint32_t sq = smem_u32(smem + C::AT_Q) + (T == 1 ? 0 : g) * C::Q_BYTES + (piece >> 3) * (128 * 128);
-        for (int i = T == 1 ? g : 0; i < CPR; i += T == 1 ? 2 : 1) {
+#pragma unroll 1
+        for (int i = T == 1 ? g : g < T ? 0 : CPR; i < CPR; i += T == 1 ? NG : 1) {
             const int trow = (warp & 3) * 32 + i * RPI + lane / CPR, r = (T == 1 ? 0 : g * 128) + trow;
-            const int2 at = A.split(r0 + min(r, nr - 1));
+            const int2 at = split_row(min(r, nr - 1));
             const bf16 *q = (const bf16 *)A.q + (long long)(sr.x + at.x) * A.q_stride + (w.h * A.share + at.y) * DH + piece * 8;
             cp_async16(sq + tile_at(trow, piece & 7), q, r < nr ? 16 : 0);
         }
         cp_async_commit();
     }
     {
-        const KeyRange first = K.range(B, len, sr.y, A.split(r0).x), last = K.range(B, len, sr.y, A.split(r0 + nr - 1).x);
-        int lo = first.lo;
+        // What the first and the last rows of the tiles see, a row to a lane.  (A CTA's beginning waits for its instructions: few of them, and loops.)
+        const int g0 = lane >> 1, row = min(nr, g0 * 128 + (lane & 1 ? 128 : 1)) - 1;
+        const KeyRange mine = K.range(B, len, sr.y, split_row(g0 < T ? row : nr - 1).x);
+        int lo = __shfl_sync(0xffffffffu, mine.lo, 0);
+        w.edge_lo = __shfl_sync(0xffffffffu, mine.lo, 2 * T - 1), w.edge_hi = __shfl_sync(0xffffffffu, mine.hi, 0);
+        const int end = __shfl_sync(0xffffffffu, mine.hi, 2 * T - 1);
         if constexpr (Keys::TMA) lo = K.begin(lo);
-        const int all = max(0, (last.hi - lo + KB - 1) / KB), per = (all + split - 1) / split;
+        const int all = max(0, (end - lo + KB - 1) / KB), per = split == 1 ? all : (all + split - 1) / split;
         w.lo = lo + min(all, rank * per) * KB;
         w.nb = max(0, min(all - rank * per, per));
-        w.hi = min(last.hi, w.lo + w.nb * KB);
-        w.edge_lo = last.lo, w.edge_hi = first.hi;
-        if (T == 2) {
-            const KeyRange a = K.range(B, len, sr.y, A.split(r0 + 127).x), b = K.range(B, len, sr.y, A.split(r0 + 128).x);
-            // (no block is left out between the tiles' ranges: rows see themselves, and those before them what comes before)
-            w.end0 = min(w.nb, max(0, a.hi - w.lo + KB - 1) / KB), w.begin1 = min(max(0, b.lo - w.lo) / KB, w.end0);
+        w.hi = min(end, w.lo + w.nb * KB);
+        // (no block is left out between the tiles' ranges: rows see themselves, and those before them what comes before)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const int a = __shfl_sync(0xffffffffu, mine.lo, 2 * g), e = __shfl_sync(0xffffffffu, mine.hi, 2 * g + 1);
+            w.b0[g] = w.b1[g] = 0;
+            if (T > 1 && g < T) {
+                w.b1[g] = g == T - 1 ? w.nb : min(w.nb, max(0, e - w.lo + KB - 1) / KB);
+                w.b0[g] = g == 0 ? 0 : min(max(0, a - w.lo) / KB, w.b1[g ? g - 1 : 0]);
+            }
         }
     }
     const bool merge = split > 1 || (T == 1 && w.nb >= 2);  // a row's result is in several groups
@@ -593,10 +629,9 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
     }
     bool ok = true;
 
-    // (registers of a thread: 64 + 48 + 2 x 200 of the 512 that four warps' threads were launched with)
     if (warp < C::SM0) {
+        leave_registers<C::REGS_LOW>();
         if (warp < C::PW) {
-            leave_registers<64>();
             if constexpr (Keys::TMA) {
                 if (warp == 0) block_copy<DH>(K, B, w, smem, bars, ok);
                 else block_look_through<DH>(w, smem, bars, s_bad, ok);
@@ -604,34 +639,36 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
                 if (w.nb) block_produce<DH>(K, B, w, smem, bars, s_bad, ok);
             }
             if (!ok) s_expired = 1;
-            asm volatile("bar.arrive 1, %0;" ::"n"(256 + 32 * C::PW) : "memory");
-        } else {
-            leave_registers<48>();
-            if (warp == C::PW && w.nb) {
-                // (what the products' operands come from is the same in all lanes, and the compiler has to know it)
-                const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
-                BlockWork u;
-                u.nb = __shfl_sync(0xffffffffu, w.nb, 0), u.T = __shfl_sync(0xffffffffu, w.T, 0);
-                u.end0 = __shfl_sync(0xffffffffu, w.end0, 0), u.begin1 = __shfl_sync(0xffffffffu, w.begin1, 0);
-                if (elect_one()) {
-                    if (!block_issue<DH>(u, bars, base, tm)) s_expired = 1;
-                }
+            asm volatile("bar.arrive 1, %0;" ::"n"(NG * 128 + 32 * C::PW) : "memory");
+        } else if (warp == C::PW && w.nb) {
+            // (what the products' operands come from is the same in all lanes, and the compiler has to know it)
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
+            BlockWork<NG> u;
+            u.nb = __shfl_sync(0xffffffffu, w.nb, 0), u.T = __shfl_sync(0xffffffffu, w.T, 0);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) u.b0[g] = __shfl_sync(0xffffffffu, w.b0[g], 0), u.b1[g] = __shfl_sync(0xffffffffu, w.b1[g], 0);
+            if (elect_one()) {
+                if (!block_issue<DH>(u, bars, base, tm)) s_expired = 1;
             }
         }
     } else {
-        take_registers<200>();
+        take_registers<C::REGS_SOFTMAX>();
         // ---------------- softmax: a thread per row ----------------
         const int g = (warp - C::SM0) >> 2, quad = warp & 3, trow = quad * 32 + lane, r = (T == 1 ? 0 : g * 128) + trow;
         const uint32_t lane_off = (uint32_t)(quad * 32) << 16, tO = tmem + C::TM_O + g * 64 * SUB + lane_off;
         const bool some = __any_sync(0xffffffffu, r < nr);             // the warp has rows
         const float c = 1.4426950408889634f * rsqrtf((float)DH);
         const float most = exp2f(BLOCK_GROWTH - down);
-        const KeyRange kr = K.range(B, len, sr.y, A.split(r0 + min(r, nr - 1)).x);
+        const KeyRange kr = K.range(B, len, sr.y, split_row(min(r, nr - 1)).x);
         cp_async_wait<0>();
         tile_publish(bars.q_full());
         float m = -INFINITY, l = 0.f;                                  // m: reference, in units of scores
         int n = 0;                                                     // the group's jobs so far
-        const int b_first = T == 1 ? g : g ? w.begin1 : 0, b_end = T == 2 && !g ? w.end0 : w.nb, b_step = T == 2 ? 1 : 2;
+        int b_first = g, b_end = w.nb;
+        const int b_step = T > 1 ? 1 : NG;
+#pragma unroll
+        for (int k = 0; k < NG; ++k)
+            if (T > 1 && g == k) b_first = w.b0[k], b_end = w.b1[k];
         uint32_t there[KB / 32];                                       // keys of the next block that are there
         auto look = [&](int b) {
             if constexpr (Keys::HOLES) {
@@ -645,11 +682,10 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
             }
         };
         for (int b = b_first; b < b_end; b += b_step, ++n) {
-            const int i = NBG == 1 ? 0 : n & 1;
-            const uint32_t tJ = tmem + (g * NBG + i) * KB + lane_off;
+            const uint32_t tJ = tmem + g * KB + lane_off;
             // (the masks of a group's first block may be laps of their ring ahead; S says that they are there)
             if (n == 0) {
-                ok = ok && tile_wait(bars.s_full(g, i), 0);
+                ok = ok && tile_wait(bars.s_full(g), 0);
                 look(b);
             }
             uint32_t every = 0xffffffffu;
@@ -657,7 +693,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
             for (int k = 0; k < KB / 32; ++k) every &= there[k];
             const int p0 = w.lo + b * KB;
             const bool plain = __all_sync(0xffffffffu, every == 0xffffffffu && p0 >= kr.lo && p0 + KB <= kr.hi && m != -INFINITY) && some;
-            if (n) ok = ok && tile_wait(bars.s_full(g, i), (n / NBG) & 1);
+            if (n) ok = ok && tile_wait(bars.s_full(g), n & 1);
             __syncwarp();
             tc_fence_after();
 #pragma unroll 1
@@ -701,7 +737,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bars.p_full(g, PARTS == 1 ? i : part));
+                if (lane == 0) mbar_arrive(bars.p_full(g, part));
             }
             if (b + b_step < b_end) look(b + b_step);
         }
@@ -710,12 +746,10 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
         __syncwarp();
         tc_fence_after();
         if (!ok) s_expired = 1;
-        asm volatile("bar.sync 1, %0;" ::"n"(256 + 32 * C::PW) : "memory");           // queries and ring are at rest, and what the producers found is told
-        const int2 at = A.split(r0 + r);
-        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH;
+        asm volatile("bar.sync 1, %0;" ::"n"(NG * 128 + 32 * C::PW) : "memory");           // queries and ring are at rest, and what the producers found is told
         const float expired = s_expired || !ok ? NAN : 0.f;
         const int late_lo = max(s_bad[0], kr.lo), late_hi = min(s_bad[1], kr.hi);      // keys among which there are values that were taken out
-        if (merge || (some && (T == 2 || g == 0))) {
+        if (merge ? T == 1 || g < T : some && (T > 1 ? g < T : g == 0)) {
             const float inv = (l == 0.f ? 0.f : 1.0f / l) + expired;
             uint8_t *state = smem + g * C::STATE;
 #pragma unroll 1
@@ -743,33 +777,49 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         *reinterpret_cast<float4 *>(state + ((i / 4 + e) * 128 + trow) * 16) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                } else if (r < nr) {
+                } else {
+                    // over the tile's queries, as these lie
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         uint32_t v[4];
 #pragma unroll
                         for (int u = 0; u < 4; ++u) v[u] = bf16_pair(o[8 * e + 2 * u] * inv, o[8 * e + 2 * u + 1] * inv);
-                        *reinterpret_cast<uint4 *>(out + i + 8 * e) = make_uint4(v[0], v[1], v[2], v[3]);
+                        const int piece = i / 8 + e;
+                        *reinterpret_cast<uint4 *>(smem + C::AT_Q + g * C::Q_BYTES + (piece >> 3) * (128 * 128) + tile_at(trow, piece & 7)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
+                }
+            }
+            if (!merge) {
+                // the warp's rows, a row's pieces by neighbouring lanes (a row to a lane, the stores took four times as long)
+                __syncwarp();
+                constexpr int CPR = DH / 8, RPI = 32 / CPR;
+                const int piece = lane % CPR;
+#pragma unroll 4
+                for (int k = 0; k < CPR; ++k) {
+                    const int row = quad * 32 + k * RPI + lane / CPR, rr = (T == 1 ? 0 : g * 128) + row;
+                    if (rr >= nr) break;
+                    const int2 at = split_row(rr);
+                    bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH + piece * 8;
+                    *reinterpret_cast<uint4 *>(out) = *reinterpret_cast<const uint4 *>(smem + C::AT_Q + g * C::Q_BYTES + (piece >> 3) * (128 * 128) + tile_at(row, piece & 7));
                 }
             }
             if (merge) *reinterpret_cast<float2 *>(state + 128 * DH * 4 + trow * 8) = make_float2(n ? m * c : -INFINITY, l + expired);
         }
         if (merge && T == 1) {
-            // The groups' states of the one tile become one, over the first (half of the columns to a group), or the result.  None is left out: a
+            // The groups' states of the one tile become one, over the first (a share of the columns to a group), or the result.  None is left out: a
             // value that is not finite counts however small its factor.
-            asm volatile("bar.sync 3, 256;" ::: "memory");
-            float f[2], mx = -INFINITY, sum = 0.f;
-            float2 ml[2];
+            asm volatile("bar.sync 3, %0;" ::"n"(NG * 128) : "memory");
+            float f[NG], mx = -INFINITY, sum = 0.f;
+            float2 ml[NG];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) ml[k] = *reinterpret_cast<const float2 *>(smem + k * C::STATE + 128 * DH * 4 + trow * 8), mx = fmaxf(mx, ml[k].x);
+            for (int k = 0; k < NG; ++k) ml[k] = *reinterpret_cast<const float2 *>(smem + k * C::STATE + 128 * DH * 4 + trow * 8), mx = fmaxf(mx, ml[k].x);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) f[k] = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx), sum = fmaf(ml[k].y, f[k], sum);
+            for (int k = 0; k < NG; ++k) f[k] = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx), sum = fmaf(ml[k].y, f[k], sum);
             const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-            for (int i = g; i < DH / 8; i += 2) {
+            for (int i = g; i < DH / 8; i += NG) {
                 float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < NG; ++k)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const float4 o = *reinterpret_cast<const float4 *>(smem + k * C::STATE + ((2 * i + e) * 128 + trow) * 16);
@@ -781,11 +831,13 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
                     for (int e = 0; e < 2; ++e)
                         *reinterpret_cast<float4 *>(smem + ((2 * i + e) * 128 + trow) * 16) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
                 } else if (r < nr) {
+                    const int2 at = split_row(r);
+                    bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH;
                     *reinterpret_cast<uint4 *>(out + 8 * i) = make_uint4(bf16_pair(v[0] * inv, v[1] * inv), bf16_pair(v[2] * inv, v[3] * inv),
                                                                          bf16_pair(v[4] * inv, v[5] * inv), bf16_pair(v[6] * inv, v[7] * inv));
                 }
             }
-            if (g == 0) *reinterpret_cast<float2 *>(smem + 2 * C::STATE + trow * 8) = make_float2(mx, sum);
+            if (g == 0) *reinterpret_cast<float2 *>(smem + NG * C::STATE + trow * 8) = make_float2(mx, sum);
         }
         if (split > 1) {
             __syncwarp();
@@ -794,11 +846,11 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
             // cluster takes every split-th of these.  A word's loads are in flight together.
             const uint32_t st0 = smem_u32(smem);
             const int n_words = T * 16 * (DH / 16);
-            for (int i = rank * 8 + warp - C::SM0; i < n_words; i += split * 8) {
+            for (int i = rank * 4 * NG + warp - C::SM0; i < n_words; i += split * 4 * NG) {
                 const int tile = i / (16 * (DH / 16)), in = i % (16 * (DH / 16));
                 const int trow = (in / (DH / 16)) * 8 + (lane & 7), col4 = (in % (DH / 16)) * 4 + (lane >> 3), r = tile * 128 + trow;
                 if (r >= nr) continue;
-                const uint32_t at_ml = st0 + (T == 1 ? 2 * C::STATE : tile * C::STATE + 128 * DH * 4) + trow * 8;
+                const uint32_t at_ml = st0 + (T == 1 ? NG * C::STATE : tile * C::STATE + 128 * DH * 4) + trow * 8;
                 const uint32_t at_o = st0 + tile * C::STATE + (col4 * 128 + trow) * 16;
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
                 float mx = -INFINITY, sum = 0.f;
@@ -811,7 +863,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
                     v.x = fmaf(o.x, f, v.x), v.y = fmaf(o.y, f, v.y), v.z = fmaf(o.z, f, v.z), v.w = fmaf(o.w, f, v.w);
                 }
                 const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-                const int2 at = A.split(r0 + r);
+                const int2 at = split_row(r);
                 bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH + col4 * 4;
                 *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
             }
@@ -833,22 +885,24 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
     }
 }
 
-// How the work is laid out: tiles of a CTA (1 or 2), CTAs of a cluster that their keys are split over, by times in clocks as measured with all SMs busy: a
-// job (a key block of a tile) takes a CTA's pipes JOB, a block its producers LOAD; a CTA has a beginning and an end (FIXED, and MERGE where there are
-// states to merge); waves go by how many clusters the device holds at once.
-template <int DH, typename F> static TilePlan block_plan(long long kv_heads, long long seqs, long long rows, long long all_rows, long long keys, int n_sm, F &&clusters) {
-    constexpr int kb = BlockCfg<DH>::KB;
-    constexpr long long JOB = (DH == 128 ? 10 : 9) * kb, LOAD = 6 * kb, FIXED = 6000, MERGE = 3000;
-    const long long blocks = (keys + kb - 1) / kb;
+// How the work is laid out: tiles of a CTA (1 or NG), CTAs of a cluster that their keys are split over, by times in clocks as measured with all SMs busy: a
+// block of keys takes a CTA's pipes as long as its tiles say (JOB); a CTA has a beginning and an end (FIXED, and MERGE where there are states to merge).
+// Units that see as many keys (mean = keys) go in waves of as many clusters as the device holds at once; where they differ the last ones are short, and what
+// counts is the sum, or the longest.
+template <int DH, typename Units, typename Clusters>
+static TilePlan block_plan(long long rows, long long keys, long long mean, int n_sm, Units &&units, Clusters &&clusters) {
+    constexpr int kb = BlockCfg<DH>::KB, ng = BlockCfg<DH>::NG;
+    constexpr long long JOB[4] = {0, DH == 128 ? 1700 : 1000, DH == 128 ? 3300 : 2000, 2750}, FIXED = 5000, MERGE1 = 2000, MERGE = 10000;
     TilePlan best = {1, 1};
     long long least = -1;
-    for (int tiles = 1; tiles <= 2; ++tiles)
+    for (int tiles = 1; tiles <= ng; tiles += ng - 1)
         for (int split = 1; split <= BLOCK_SPLIT; ++split) {
-            const long long fit = split == 1 ? n_sm : clusters(split);
+            const long long fit = split == 1 ? n_sm : clusters(split), blocks = (keys + kb - 1) / kb, average = (mean + kb - 1) / kb;
             if (fit < 1 || (split > 1 && blocks < 2 * split)) break;
-            const long long R = 128 * tiles, mine = rows < R ? (rows + 127) / 128 : tiles, job = JOB * mine, per = (blocks + split - 1) / split;
-            const long long most = seqs * ((rows + R - 1) / R), real = all_rows / R + seqs, units = kv_heads * (most < real ? most : real);
-            const long long cost = (units + fit - 1) / fit * (per * (job > LOAD ? job : LOAD) + FIXED + (split > 1 || mine == 1 ? MERGE : 0));
+            const long long mine = rows < 128 * tiles ? (rows + 127) / 128 : tiles, rest = FIXED + (split > 1 ? MERGE : mine == 1 ? MERGE1 : 0);
+            const long long longest = (blocks + split - 1) / split * JOB[mine] + rest, n = units(tiles);
+            const long long sum = n * (average * JOB[mine] / split + rest) / fit + longest / 3;
+            const long long cost = mean == keys ? (n + fit - 1) / fit * longest : sum > longest ? sum : longest;
             if (least < 0 || cost < least) least = cost, best = {tiles, split};
         }
     return best;
@@ -888,9 +942,20 @@ static int launch_attn_block(const BatchD &B, const AttnRows &A, const Keys &K, 
         }))
         return NFD_E_CUDA;
     const long long rows = (long long)B.max_rows * A.share, all_rows = (long long)B.n_rows * A.share;
-    const TilePlan pl = block_plan<DH>(kv_heads, B.n_seqs, rows, all_rows, keys, n_sm, [&](int k) { return fit[dev][k]; });
-    const long long R = 128 * pl.tiles, most = B.n_seqs * ((rows + R - 1) / R), real = all_rows / R + B.n_seqs;
-    const long long units = B.row_start && B.n_seqs <= BLOCK_SORTED && real < most ? real : most, grid = units * kv_heads * pl.split;
+    // units of a head: as many as the sequences' rows can make, or as if all had max_rows (block_unit)
+    auto units = [&](int tiles) -> long long {
+        const long long R = 128 * tiles, most = B.n_seqs * ((rows + R - 1) / R), real = all_rows / R + B.n_seqs;
+        return B.row_start && B.n_seqs <= BLOCK_SORTED && real < most ? real : most;
+    };
+    // what a row sees on the average: of a prompt, as far as its window does not end before, half of it and half of its own frame
+    long long mean = keys;
+    if (!Keys::HOLES) {
+        const long long frame = K.mask.frame_tokens, window = ((long long)K.mask.window + 1) * frame, n = B.max_rows;
+        mean = n <= window ? (n + frame) / 2 : window - window * window / (2 * n) + frame / 2;
+        mean = mean < keys ? mean : keys;
+    }
+    const TilePlan pl = block_plan<DH>(rows, keys, mean, n_sm, [&](int tiles) { return kv_heads * units(tiles); }, [&](int k) { return fit[dev][k]; });
+    const long long grid = units(pl.tiles) * kv_heads * pl.split;
     if (grid > INT_MAX) return NFD_E_RANGE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid), cfg.blockDim = dim3(BLOCK_THREADS), cfg.dynamicSmemBytes = C::SMEM, cfg.stream = st;
@@ -898,7 +963,9 @@ static int launch_attn_block(const BatchD &B, const AttnRows &A, const Keys &K, 
     at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = pl.split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at, cfg.numAttrs = pl.split > 1;
     const float down = (float)sum_bits(BLOCK_GROWTH, (int)((keys + C::HK - 1) / C::HK));
-    if (cudaLaunchKernelEx(&cfg, kern, B, A, K, kv_heads, pl.split, pl.tiles, down) != cudaSuccess) {
+    FastDiv by_share;
+    by_share.set(A.share);
+    if (cudaLaunchKernelEx(&cfg, kern, B, A, K, kv_heads, pl.split, pl.tiles, by_share, down) != cudaSuccess) {
         cudaGetLastError();
         return NFD_E_CUDA;
     }

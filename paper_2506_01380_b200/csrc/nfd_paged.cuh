@@ -104,6 +104,10 @@ struct CausalMask {
     __device__ __forceinline__ KeyRange range(int len, int oldest, int n, int i) const {
         const int p = len - n + i;
         if (p < 0) return {0, 0};
+        if (frame_tokens == 1) {                               // (two divisions less)
+            const int lo = max(p > window ? p - window : 0, oldest);
+            return {lo, max(lo, min(p + 1, len))};
+        }
         const int f = p / frame_tokens;
         const int lo = max(max(f - window, 0) * frame_tokens, oldest);
         return {lo, max(lo, min((f + 1) * frame_tokens, len))};
