@@ -354,17 +354,17 @@ template <int DH> static __device__ __forceinline__ bool block_issue(const Block
 }
 
 // ---- softmax ------------------------------------------------------------------------------------------------
-// The rest of a part whose sums have outgrown m: the row's maximum over the keys that it sees from column `from` on, m and what has been
-// summed so far adjusted to it (O, and P of the part's first columns), then P.  seen: bits of the keys that the row sees; n: the group's parts before this one;
-// pv_done: of the last of them.  A row without an m comes here as well.
+// A part of a block whose sums have outgrown m, or that finds a row without one: the row's maximum over the keys that it sees, m and what has been
+// summed so far adjusted to it, then P.  seen: bits of the keys that the row sees; n: the group's parts before this one; pv_done: of the last of them.
 template <int DH>
-static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint32_t tO, const uint32_t *seen, int from, float c, float down, int n, uint32_t pv_done,
+static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint32_t tO, const uint32_t *seen, float c, float down, int n, uint32_t pv_done,
                                                float &m_io, float &l_io, bool &ok) {
     constexpr int HK = BlockCfg<DH>::HK;
     float m = m_io, l = l_io, top = -INFINITY;
-    auto bits = [&](int i) { return (i < 32 ? seen[0] : i < 64 ? seen[1] : seen[HK / 32 - 1]) >> (i & 31); };
+    constexpr int W = HK / 32;
+    auto bits = [&](int i) { return (i < 32 ? seen[0] : i < 64 ? seen[1] : seen[W - 1]) >> (i & 31); };
 #pragma unroll 1
-    for (int i = from; i < HK; i += 16) {
+    for (int i = 0; i < HK; i += 16) {
         float x[16];
         tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
         const uint32_t s = bits(i);
@@ -379,17 +379,6 @@ static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint
         const float f = !rise ? 1.0f : m == -INFINITY ? 0.f : few_exp2((m - top) * c);
         if (rise) m = top;
         l *= f;
-        tmem_st_wait();
-#pragma unroll 1
-        for (int i = 0; i < from / 2; i += 16) {
-            uint32_t p[16];
-            tmem_ld16(tP + i, p);
-            tmem_ld_wait();
-            loaded16(reinterpret_cast<float *>(p));
-#pragma unroll
-            for (int e = 0; e < 16; ++e) p[e] = bf16_pair(__uint_as_float(p[e] << 16) * f, __uint_as_float(p[e] & 0xffff0000u) * f);
-            tmem_st16(tP + i, p);
-        }
         if (n) {
             ok = ok && tile_wait(pv_done, ((n - 1) >> 1) & 1);         // O is at rest
             __syncwarp();
@@ -409,7 +398,7 @@ static __device__ __forceinline__ void block_slow(uint32_t tS, uint32_t tP, uint
     const float mc = m == -INFINITY ? 0.f : fmaf(m, c, down);
     float sum = 0.f;
 #pragma unroll 1
-    for (int i = from; i < HK; i += 16) {
+    for (int i = 0; i < HK; i += 16) {
         float x[16];
         tmem_ld16(tS + i, reinterpret_cast<uint32_t *>(x));
         const uint32_t s = bits(i);
@@ -462,35 +451,31 @@ template <bool MASKED> __device__ __forceinline__ void block_exp16(const float *
         pk[u] = bf16_pair(p.x, p.y);
     }
 }
-// One pass over a part of S against the m that there is, 32 columns a turn (a loop, so that its code stays near: unrolled, the exponentials of a part waited for
-// instructions a fifth of their time), halves of them loaded while the others are worked on.  MASKED: keys that the row does not see count for nothing; ready:
-// whether there is an m, or nothing to see.  Returns the columns that are done: fewer than all where a sum has outgrown m (most: the most that it may be),
-// and what is not done is as it was.
+// One pass over a part of S against the m that there is, 16 columns at a time with the next load in flight (xa: the first ones, on their way).  MASKED: keys
+// that the row does not see count for nothing; ready: whether there is an m, or nothing to see.  False: a sum has outgrown m (most: the most that it may
+// be), and S is as it was.
 template <int DH, bool MASKED>
-static __device__ __forceinline__ int block_fast(uint32_t tS, uint32_t tP, float (&xa)[16], const uint32_t *seen, bool ready, float c, float mc, float most, float &l) {
+static __device__ __forceinline__ bool block_fast(uint32_t tS, uint32_t tP, float (&xa)[16], const uint32_t *seen, bool ready, float c, float mc, float most, float &l) {
     constexpr int HK = BlockCfg<DH>::HK;
     float xb[16];
     float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     uint32_t pk[HK / 2];
 #pragma unroll
-    for (int i = 0; i < HK; i += 32) {
-        const uint32_t bits = MASKED ? seen[i / 32] : 0;
+    for (int i = 0; i < HK; i += 16) {
+        float (&x)[16] = i / 16 % 2 ? xb : xa;
         tmem_ld_wait();
-        loaded16(xa);
-        tmem_ld16(tS + i + 16, reinterpret_cast<uint32_t *>(xb));
-        block_exp16<MASKED>(xa, bits, c, mc, pk + i / 2, ls);
-        tmem_ld_wait();
-        loaded16(xb);
-        if (i + 32 < HK) tmem_ld16(tS + i + 32, reinterpret_cast<uint32_t *>(xa));
-        block_exp16<MASKED>(xb, bits >> 16, c, mc, pk + i / 2 + 8, ls);
+        loaded16(x);
+        if (i + 16 < HK) tmem_ld16(tS + i + 16, reinterpret_cast<uint32_t *>(i / 16 % 2 ? xa : xb));
+        block_exp16<MASKED>(x, MASKED ? seen[i / 32] >> (i & 16) : 0, c, mc, pk + i / 2, ls);
     }
     const float2 l2 = fadd2(ls[0], ls[1]);
     const float sum = l2.x + l2.y;
-    if (!__all_sync(0xffffffffu, sum < most && (!MASKED || ready))) return 0;
+    if (!__all_sync(0xffffffffu, sum < most && (!MASKED || ready))) return false;
     l += sum;
 #pragma unroll
-    for (int i = 0; i < HK / 2; i += 16) tmem_st16(tP + i, pk + i);
-    return HK;
+    for (int i = 0; i + 16 <= HK / 2; i += 16) tmem_st16(tP + i, pk + i);
+    if (HK / 2 % 16) tmem_st8(tP + HK / 2 - 8, pk + HK / 2 - 8);
+    return true;
 }
 
 // ---- which tiles a CTA takes --------------------------------------------------------------------------------
@@ -702,11 +687,10 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
                 float x[16];
                 if (some) tmem_ld16(tS, reinterpret_cast<uint32_t *>(x));
                 if (plain) {                                           // all rows have an m and see all of these keys
-                    const int done = block_fast<DH, false>(tS, tP, x, there, true, c, fmaf(m, c, down), most, l);
-                    if (done < HK)
-                        block_slow<DH>(tS, tP, tO, there, done, c, down, n * PARTS + part, bars.pv_done(g, n * PARTS + part - 1), m, l, ok);
+                    if (!block_fast<DH, false>(tS, tP, x, there, true, c, fmaf(m, c, down), most, l))
+                        block_slow<DH>(tS, tP, tO, there, c, down, n * PARTS + part, bars.pv_done(g, n * PARTS + part - 1), m, l, ok);
                 } else if (some) {                                     // (of rows that are not there P may be anything)
-                    const int a = kr.lo - p0 - part * HK, e = kr.hi - p0 - part * HK;            // keys a .. e - 1 of the part
+                    const int a = kr.lo - p0 - part * HK, e = min(kr.hi - p0 - part * HK, HK);   // keys a .. e - 1 of the part
                     uint32_t seen[HK / 32], any = 0;
 #pragma unroll
                     for (int k = 0; k < HK / 32; ++k) {
@@ -720,7 +704,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
                     if (!__any_sync(0xffffffffu, any)) {               // none of the warp's rows sees any of these keys
                         const uint32_t zero[16] = {};
 #pragma unroll
-                        for (int k = 0; k < HK / 2; k += 16) tmem_st16(tP + k, zero);
+                        for (int k = 0; k < HK / 2; k += 8) tmem_st8(tP + k, zero);
                     } else {
                         if (__any_sync(0xffffffffu, m == -INFINITY)) {
                             // a row without m (nothing has been summed for it): the largest of the first scores will do, if it sees one of them
@@ -729,9 +713,8 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
                             for (int e = 0; e < 16; ++e) top = fmaxf(top, seen[0] >> e & 1 ? x[e] : -INFINITY);
                             if (m == -INFINITY) m = top;
                         }
-                        const int done = block_fast<DH, true>(tS, tP, x, seen, m != -INFINITY || !any, c, m == -INFINITY ? 0.f : fmaf(m, c, down), most, l);
-                        if (done < HK)
-                            block_slow<DH>(tS, tP, tO, seen, done, c, down, n * PARTS + part, bars.pv_done(g, n * PARTS + part - 1), m, l, ok);
+                        if (!block_fast<DH, true>(tS, tP, x, seen, m != -INFINITY || !any, c, m == -INFINITY ? 0.f : fmaf(m, c, down), most, l))
+                            block_slow<DH>(tS, tP, tO, seen, c, down, n * PARTS + part, bars.pv_done(g, n * PARTS + part - 1), m, l, ok);
                     }
                 }
                 tmem_st_wait();
