@@ -835,15 +835,22 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
                 if (r >= nr) continue;
                 const uint32_t at_ml = st0 + (T == 1 ? NG * C::STATE : tile * C::STATE + 128 * DH * 4) + trow * 8;
                 const uint32_t at_o = st0 + tile * C::STATE + (col4 * 128 + trow) * 16;
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                float2 ml[BLOCK_SPLIT];
+                float4 o[BLOCK_SPLIT];
                 float mx = -INFINITY, sum = 0.f;
-                for (int k = 0; k < split; ++k) mx = fmaxf(mx, ld_cluster_f2(cluster_map(at_ml, k)).x);
-                for (int k = 0; k < split; ++k) {
-                    const float2 ml = ld_cluster_f2(cluster_map(at_ml, k));
-                    const float4 o = ld_cluster_f4(cluster_map(at_o, k));
-                    const float f = ml.x == -INFINITY ? 0.f : few_exp2(ml.x - mx);
-                    sum = fmaf(ml.y, f, sum);
-                    v.x = fmaf(o.x, f, v.x), v.y = fmaf(o.y, f, v.y), v.z = fmaf(o.z, f, v.z), v.w = fmaf(o.w, f, v.w);
+#pragma unroll
+                for (int k = 0; k < BLOCK_SPLIT; ++k) {
+                    ml[k] = make_float2(-INFINITY, 0.f), o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (k < split) ml[k] = ld_cluster_f2(cluster_map(at_ml, k)), o[k] = ld_cluster_f4(cluster_map(at_o, k));
+                }
+#pragma unroll
+                for (int k = 0; k < BLOCK_SPLIT; ++k) mx = fmaxf(mx, ml[k].x);
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < BLOCK_SPLIT; ++k) {
+                    const float f = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx);
+                    sum = fmaf(ml[k].y, f, sum);
+                    v.x = fmaf(o[k].x, f, v.x), v.y = fmaf(o[k].y, f, v.y), v.z = fmaf(o[k].z, f, v.z), v.w = fmaf(o[k].w, f, v.w);
                 }
                 const float inv = sum == 0.f ? 0.f : 1.0f / sum;
                 const int2 at = split_row(r);
@@ -875,7 +882,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
 template <int DH, typename Units, typename Clusters>
 static TilePlan block_plan(long long rows, long long keys, long long mean, int n_sm, Units &&units, Clusters &&clusters) {
     constexpr int kb = BlockCfg<DH>::KB, ng = BlockCfg<DH>::NG;
-    constexpr long long JOB[4] = {0, DH == 128 ? 1700 : 1000, DH == 128 ? 3300 : 2000, 2750}, FIXED = 5000, MERGE1 = 2000, MERGE = 10000;
+    constexpr long long JOB[4] = {0, DH == 128 ? 1800 : 1350, DH == 128 ? 3250 : 2550, 2650}, FIXED = 9000, MERGE1 = 2000, MERGE = 7000;
     TilePlan best = {1, 1};
     long long least = -1;
     for (int tiles = 1; tiles <= ng; tiles += ng - 1)
