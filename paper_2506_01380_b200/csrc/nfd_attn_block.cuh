@@ -80,15 +80,16 @@ struct BlockBars {
     }
 };
 
-// What a CTA works on: keys lo .. hi - 1 of a sequence in nb blocks, T tiles; keys that not all rows see: those below edge_lo, those from edge_hi on.
+// What a CTA works on: keys lo .. hi - 1 of a sequence in nb blocks; keys that not all rows see: those below edge_lo, those from edge_hi on.
 template <int NG> struct BlockWork {
-    int s, h, first_row, lo, hi, nb, T, edge_lo, edge_hi;
-    int b0[NG], b1[NG];                                     // several tiles: each takes blocks b0 .. b1 - 1
+    int s, h, first_row, lo, hi, nb, edge_lo, edge_hi;
+    bool turns;                                             // the groups take one tile's blocks in turn
+    int b0[NG], b1[NG];                                     // otherwise each has a tile, and takes blocks b0 .. b1 - 1
     // are there rows of the CTA that do not see all of block b (of KB keys)
     __device__ __forceinline__ bool edge(int b, int KB) const { return lo + b * KB < edge_lo || lo + b * KB + KB > edge_hi; }
-    // does group g take block b (one tile: they take turns); which of its jobs is that; is it the first, the last to take it
-    __device__ __forceinline__ bool takes(int g, int b) const { return T > 1 ? b >= b0[g] && b < b1[g] : b % NG == g; }
-    __device__ __forceinline__ int job(int g, int b) const { return T > 1 ? b - b0[g] : b / NG; }
+    // does group g take block b; which of its jobs is that; is it the first, the last to take it
+    __device__ __forceinline__ bool takes(int g, int b) const { return turns ? b % NG == g : b >= b0[g] && b < b1[g]; }
+    __device__ __forceinline__ int job(int g, int b) const { return turns ? b / NG : b - b0[g]; }
     __device__ __forceinline__ bool first(int g, int b) const {
         bool f = true;
 #pragma unroll
@@ -251,6 +252,11 @@ static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD
         const long long row = next;
         const uint32_t there = __ballot_sync(0xffffffffu, row >= 0);
         next = look_up();
+        // (rows of 64 bytes and more: memory has fewer than 2^32 - 1 of them)
+        constexpr uint32_t NONE = 0xffffffffu;
+        uint32_t rows[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) rows[i] = __shfl_sync(0xffffffffu, (uint32_t)row, i * RPI + sub);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
             const int st = item % C::NST;
@@ -270,9 +276,8 @@ static __device__ __forceinline__ void block_produce(const Keys &K, const BatchD
             const uint32_t dst = smem_u32(smem) + C::AT_R + st * C::BLK;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const long long r = __shfl_sync(0xffffffffu, row, i * RPI + sub);
-                const bf16 *src = (kv ? K.v_row(r < 0 ? 0 : r, w.h) : K.k_row(r < 0 ? 0 : r, w.h)) + piece * 8;
-                cp_async16(dst + to(i), src, r < 0 ? 0 : 16);
+                const bf16 *src = (kv ? K.v_row(rows[i] == NONE ? 0 : rows[i], w.h) : K.k_row(rows[i] == NONE ? 0 : rows[i], w.h)) + piece * 8;
+                cp_async16(dst + to(i), src, rows[i] == NONE ? 0 : 16);
             }
             cp_async_commit();
             if (Keys::HOLES && !kv) {
@@ -307,14 +312,14 @@ template <int DH> static __device__ __forceinline__ bool block_issue(const Block
     auto scores = [&](int g, int b, int st, uint32_t par) {  // stage of the block's K and its phase
         if (w.first(g, b)) wait(bars.full(st), par);
         tc_fence_after();
-        const uint32_t q = dQ + (w.T == 1 ? 0 : g) * (C::Q_BYTES >> 4), k = dR + st * (C::BLK >> 4), d = tmem + g * KB;
+        const uint32_t q = dQ + (w.turns ? 0 : g) * (C::Q_BYTES >> 4), k = dR + st * (C::BLK >> 4), d = tmem + g * KB;
 #pragma unroll
         for (int e = 0; e < (DH + 15) / 16; ++e)
             tile_mma_ss(d, q + (e >> 2) * (128 * 128 >> 4) + 2 * (e & 3), k + (e >> 2) * (KB * 128 >> 4) + 2 * (e & 3), idesc_s, e != 0);
         umma_commit(bars.s_full(g));
         if (w.last(g, b)) umma_commit(bars.empty(st));
     };
-    const int ahead = w.T == 1 ? NG : 1;                     // blocks
+    const int ahead = w.turns ? NG : 1;                      // blocks
     int sk = 0, sv = 1;                                      // stages of the next K and the next V, and their phases
     uint32_t pk = 0, pv = 0;
     auto on = [&](int &st, uint32_t &par) {
@@ -561,7 +566,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
         const int i = by_share.div(r0 + r);
         return make_int2(i, r0 + r - i * A.share);
     };
-    w.T = T, w.first_row = sr.x;
+    w.first_row = sr.x;
     if (warp >= C::SM0) {
         // softmax warps: the row's queries, into the operand of its tile, a row's pieces by neighbouring lanes; of one tile each group a share
         constexpr int CPR = DH / 8, RPI = 32 / CPR;
@@ -587,19 +592,20 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
         const int all = max(0, (end - lo + KB - 1) / KB), per = split == 1 ? all : (all + split - 1) / split;
         w.lo = lo + min(all, rank * per) * KB;
         w.nb = max(0, min(all - rank * per, per));
+        w.turns = T == 1 && w.nb > 1;
         w.hi = min(end, w.lo + w.nb * KB);
         // (no block is left out between the tiles' ranges: rows see themselves, and those before them what comes before)
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             const int a = __shfl_sync(0xffffffffu, mine.lo, 2 * g), e = __shfl_sync(0xffffffffu, mine.hi, 2 * g + 1);
             w.b0[g] = w.b1[g] = 0;
-            if (T > 1 && g < T) {
+            if (!w.turns && g < T) {
                 w.b1[g] = g == T - 1 ? w.nb : min(w.nb, max(0, e - w.lo + KB - 1) / KB);
                 w.b0[g] = g == 0 ? 0 : min(max(0, a - w.lo) / KB, w.b1[g ? g - 1 : 0]);
             }
         }
     }
-    const bool merge = split > 1 || (T == 1 && w.nb >= 2);  // a row's result is in several groups
+    const bool merge = split > 1 || w.turns;                // a row's result is in several groups
     uint32_t tmem = 0;
     if (warp >= C::PW) {
         // (the producers are on their way; the others wait for tensor memory)
@@ -629,7 +635,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
             // (what the products' operands come from is the same in all lanes, and the compiler has to know it)
             const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), base = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
             BlockWork<NG> u;
-            u.nb = __shfl_sync(0xffffffffu, w.nb, 0), u.T = __shfl_sync(0xffffffffu, w.T, 0);
+            u.nb = __shfl_sync(0xffffffffu, w.nb, 0), u.turns = __shfl_sync(0xffffffffu, (int)w.turns, 0);
 #pragma unroll
             for (int g = 0; g < NG; ++g) u.b0[g] = __shfl_sync(0xffffffffu, w.b0[g], 0), u.b1[g] = __shfl_sync(0xffffffffu, w.b1[g], 0);
             if (elect_one()) {
@@ -650,10 +656,10 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
         float m = -INFINITY, l = 0.f;                                  // m: reference, in units of scores
         int n = 0;                                                     // the group's jobs so far
         int b_first = g, b_end = w.nb;
-        const int b_step = T > 1 ? 1 : NG;
+        const int b_step = w.turns ? NG : 1;
 #pragma unroll
         for (int k = 0; k < NG; ++k)
-            if (T > 1 && g == k) b_first = w.b0[k], b_end = w.b1[k];
+            if (!w.turns && g == k) b_first = w.b0[k], b_end = w.b1[k];
         uint32_t there[KB / 32];                                       // keys of the next block that are there
         auto look = [&](int b) {
             if constexpr (Keys::HOLES) {
@@ -826,37 +832,52 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
             __syncwarp();
             cluster_sync_all();
             // The CTAs' states.  Row words of four columns, 8 rows x 4 of them to a warp (32 bytes of a row, and every bank once); each CTA of a
-            // cluster takes every split-th of these.  A word's loads are in flight together.
+            // cluster takes every split-th of these.  Eight states' loads are in flight together: of several words where the CTAs are fewer (a word at a
+            // time the merge of two CTAs took 17000 clocks).
             const uint32_t st0 = smem_u32(smem);
-            const int n_words = T * 16 * (DH / 16);
-            for (int i = rank * 4 * NG + warp - C::SM0; i < n_words; i += split * 4 * NG) {
-                const int tile = i / (16 * (DH / 16)), in = i % (16 * (DH / 16));
-                const int trow = (in / (DH / 16)) * 8 + (lane & 7), col4 = (in % (DH / 16)) * 4 + (lane >> 3), r = tile * 128 + trow;
-                if (r >= nr) continue;
-                const uint32_t at_ml = st0 + (T == 1 ? NG * C::STATE : tile * C::STATE + 128 * DH * 4) + trow * 8;
-                const uint32_t at_o = st0 + tile * C::STATE + (col4 * 128 + trow) * 16;
-                float2 ml[BLOCK_SPLIT];
-                float4 o[BLOCK_SPLIT];
-                float mx = -INFINITY, sum = 0.f;
+            const int n_words = T * 16 * (DH / 16), stride = split * 4 * NG;
+            auto join = [&](auto most_ctas) {
+                constexpr int S = decltype(most_ctas)::value, U = 8 / S;
+                for (int i0 = rank * 4 * NG + warp - C::SM0; i0 < n_words; i0 += U * stride) {
+                    float2 ml[U][S];
+                    float4 o[U][S];
 #pragma unroll
-                for (int k = 0; k < BLOCK_SPLIT; ++k) {
-                    ml[k] = make_float2(-INFINITY, 0.f), o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (k < split) ml[k] = ld_cluster_f2(cluster_map(at_ml, k)), o[k] = ld_cluster_f4(cluster_map(at_o, k));
+                    for (int u = 0; u < U; ++u) {
+                        const int i = min(i0 + u * stride, n_words - 1), tile = i / (16 * (DH / 16)), in = i % (16 * (DH / 16));
+                        const int mrow = (in / (DH / 16)) * 8 + (lane & 7), col4 = (in % (DH / 16)) * 4 + (lane >> 3);
+                        const uint32_t at_ml = st0 + (T == 1 ? NG * C::STATE : tile * C::STATE + 128 * DH * 4) + mrow * 8;
+                        const uint32_t at_o = st0 + tile * C::STATE + (col4 * 128 + mrow) * 16;
+#pragma unroll
+                        for (int k = 0; k < S; ++k) {
+                            ml[u][k] = make_float2(-INFINITY, 0.f), o[u][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (k < split) ml[u][k] = ld_cluster_f2(cluster_map(at_ml, k)), o[u][k] = ld_cluster_f4(cluster_map(at_o, k));
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int i = i0 + u * stride, tile = i / (16 * (DH / 16)), in = i % (16 * (DH / 16));
+                        const int col4 = (in % (DH / 16)) * 4 + (lane >> 3), mr = tile * 128 + (in / (DH / 16)) * 8 + (lane & 7);
+                        if (i >= n_words || mr >= nr) continue;
+                        float mx = -INFINITY, sum = 0.f;
+                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int k = 0; k < S; ++k) mx = fmaxf(mx, ml[u][k].x);
+#pragma unroll
+                        for (int k = 0; k < S; ++k) {
+                            const float f = ml[u][k].x == -INFINITY ? 0.f : few_exp2(ml[u][k].x - mx);
+                            sum = fmaf(ml[u][k].y, f, sum);
+                            v.x = fmaf(o[u][k].x, f, v.x), v.y = fmaf(o[u][k].y, f, v.y), v.z = fmaf(o[u][k].z, f, v.z), v.w = fmaf(o[u][k].w, f, v.w);
+                        }
+                        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+                        const int2 at = split_row(mr);
+                        bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH + col4 * 4;
+                        *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
+                    }
                 }
-#pragma unroll
-                for (int k = 0; k < BLOCK_SPLIT; ++k) mx = fmaxf(mx, ml[k].x);
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int k = 0; k < BLOCK_SPLIT; ++k) {
-                    const float f = ml[k].x == -INFINITY ? 0.f : few_exp2(ml[k].x - mx);
-                    sum = fmaf(ml[k].y, f, sum);
-                    v.x = fmaf(o[k].x, f, v.x), v.y = fmaf(o[k].y, f, v.y), v.z = fmaf(o[k].z, f, v.z), v.w = fmaf(o[k].w, f, v.w);
-                }
-                const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-                const int2 at = split_row(r);
-                bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + w.h * A.share + at.y) * DH + col4 * 4;
-                *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
-            }
+            };
+            if (split == 2) join(std::integral_constant<int, 2>());
+            else if (split <= 4) join(std::integral_constant<int, 4>());
+            else join(std::integral_constant<int, 8>());
             cluster_sync_all();                                 // nobody leaves while its state is read
         }
     }

@@ -63,6 +63,7 @@ __device__ __forceinline__ float few_exp2(float x) {
 // A warp's chunk of keys in shared memory, for 4-bit pages: codes of K and V, their words, and which keys are there.
 template <int DH> struct FewKv4 {
     static constexpr bool KV4 = true, RANGES = false;
+    static constexpr int WARPS = FEW_WARPS;
     static constexpr float UP = KV4_UP;                     // what scores and results are to be multiplied by
     static __device__ __forceinline__ float down() { return 0.f; }        // taken off the exponents (sum_bits; values below 1 need nothing)
     static constexpr int KC = 32;
@@ -256,6 +257,7 @@ template <int DH> struct FewBf16 {
 template <int DH> struct FewStates : FewBf16<DH> {
     using F = FewBf16<DH>;
     static constexpr bool RANGES = false;
+    static constexpr int WARPS = FEW_WARPS;
     static constexpr int KC = F::KC, RB = F::RB, PR = F::PR;
     StateKeys<bf16, DH> K;
     uint32_t there;                                         // of the chunk that is filled next
@@ -285,6 +287,7 @@ template <int DH> struct FewStates : FewBf16<DH> {
 template <typename Keys, int DH> struct FewRows : FewBf16<DH> {
     using F = FewBf16<DH>;
     static constexpr bool RANGES = true;
+    static constexpr int WARPS = 4;                         // (two CTAs to an SM: one merges while the other streams.  With 8 warps the figures at few_split_rows are 178, 176, 170, 199)
     static constexpr int KC = F::KC, RB = F::RB, PR = F::PR;
     Keys K;
     typename Keys::Cursor cur;
@@ -344,14 +347,14 @@ template <typename Src, int DH, int NR> struct FewCfg {
     static constexpr int STATE = ROWS * (DH + 2) * 4;                             // O, m, l of a warp or a CTA
     static constexpr int RING = (Src::NST * Src::STAGE + 15) / 16 * 16;
     static constexpr int WARP = RING > STATE ? RING : STATE;                      // a warp's ring, then its state
-    static constexpr int SMEM = FEW_WARPS * WARP + STATE;
+    static constexpr int SMEM = Src::WARPS * WARP + STATE;
     static_assert(SMEM <= 232448 - 1024, "shared memory of a CTA");
 };
 
 // grid: (CTAs of a cluster x heads of keys, sequences, tiles of 8 NR rows).  (States: their ring leaves one CTA to an SM, and so it may have all registers: not
 // told so, the compiler spilled in 80.)
 template <typename Src, int DH, int NR>
-__global__ void __launch_bounds__(32 * FEW_WARPS, Src::KV4 ? 0 : 1) k_attn_few(const BatchD B, const AttnRows A, Src src, int split) {
+__global__ void __launch_bounds__(32 * Src::WARPS, Src::KV4 ? 0 : Src::RANGES ? 2 : 1) k_attn_few(const BatchD B, const AttnRows A, Src src, int split) {
     using F = FewCfg<Src, DH, NR>;
     constexpr int KC = Src::KC, NST = Src::NST, NS = DH / 16, KT = KC / 16, ROWS = F::ROWS;
     // S in two chains of products for a single tile of rows (states, eight rows against 4096 26.9 us for 25.9; with 4-bit pages and head
@@ -372,8 +375,8 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, Src::KV4 ? 0 : 1) k_attn_few(c
 
     uint8_t *ring = few_smem + warp * F::WARP;
     const uint32_t ring_s = smem_u32(ring);
-    const int step = split * FEW_WARPS * KC;
-    int next = lo + (rank * FEW_WARPS + warp) * KC;                               // next chunk to fill
+    const int step = split * Src::WARPS * KC;
+    int next = lo + (rank * Src::WARPS + warp) * KC;                               // next chunk to fill
     int base = next;
     src.start(B, s, h, next, step);
     src.look_up(B, s, h, next, hi);
@@ -557,22 +560,22 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, Src::KV4 ? 0 : 1) k_attn_few(c
     }
     __syncthreads();
     // the CTA's
-    float *T = reinterpret_cast<float *>(few_smem + FEW_WARPS * F::WARP);
+    float *T = reinterpret_cast<float *>(few_smem + Src::WARPS * F::WARP);
     auto write = [&](int r, int d, float4 v, float sum) {
         const int2 at = A.split(r0 + r);
         const float inv = sum == 0.f ? 0.f : Src::UP / sum;
         bf16 *out = (bf16 *)A.out + ((long long)(sr.x + at.x) * A.heads + h * A.share + at.y) * DH + d;
         *reinterpret_cast<uint2 *>(out) = make_uint2(bf16_pair(v.x * inv, v.y * inv), bf16_pair(v.z * inv, v.w * inv));
     };
-    for (int i = threadIdx.x; i < nr * (DH / 4); i += 32 * FEW_WARPS) {
+    for (int i = threadIdx.x; i < nr * (DH / 4); i += 32 * Src::WARPS) {
         const int r = i / (DH / 4), d = i % (DH / 4) * 4;
         float mx = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < FEW_WARPS; ++w) mx = fmaxf(mx, reinterpret_cast<const float *>(few_smem + w * F::WARP)[ROWS * DH + 2 * r]);
+        for (int w = 0; w < Src::WARPS; ++w) mx = fmaxf(mx, reinterpret_cast<const float *>(few_smem + w * F::WARP)[ROWS * DH + 2 * r]);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < FEW_WARPS; ++w) {
+        for (int w = 0; w < Src::WARPS; ++w) {
             const float *W = reinterpret_cast<const float *>(few_smem + w * F::WARP);
             const float mw = W[ROWS * DH + 2 * r], f = mw == -INFINITY ? 0.f : few_exp2(mw - mx);
             const float4 x = *reinterpret_cast<const float4 *>(W + r * DH + d);
@@ -590,7 +593,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, Src::KV4 ? 0 : 1) k_attn_few(c
     // the cluster's: every CTA a share of the row words
     cluster_sync_all();
     const uint32_t Ts = smem_u32(T);
-    for (int i = rank + split * threadIdx.x; i < nr * (DH / 4); i += split * 32 * FEW_WARPS) {
+    for (int i = rank + split * threadIdx.x; i < nr * (DH / 4); i += split * 32 * Src::WARPS) {
         const int r = i / (DH / 4), d = i % (DH / 4) * 4;
         float mx = -INFINITY;
         for (int k = 0; k < split; ++k) mx = fmaxf(mx, ld_cluster_f2(cluster_map(Ts + (ROWS * DH + 2 * r) * 4, k)).x);
@@ -612,11 +615,18 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, Src::KV4 ? 0 : 1) k_attn_few(c
 // no more than give every warp a chunk or two; sixteen where they get three and more.  (16 heads x 64, 24 rows behind 5712 tokens, one CTA to an
 // SM: in 8 pieces, of which the device holds 14 at once, 23 us, in 4 pieces 15.  One row: in 8 pieces 10.8, in 16 11.8; 24 heads on 8 behind 32768
 // tokens 39 and 33.)
-static int few_split(long long units, long long keys, int kc, const int *fit) {
+static int few_split(long long units, long long keys, int kc, const int *fit, int warps = FEW_WARPS) {
     const long long chunks = (keys + kc - 1) / kc;
     int i = 0;
-    while (i < 4 && units <= fit[i + 1] && chunks > (long long)(i == 3 ? 48 : 1 << i) * FEW_WARPS) ++i;
+    while (i < 4 && units <= fit[i + 1] && chunks > (long long)(i == 3 ? 48 : 1 << i) * warps) ++i;
     return 1 << i;
+}
+// With bf16 pages and small CTAs (two to an SM) one and two pieces are doubled where they are long: what the device does not hold at once evens out sequences
+// of different lengths.  (One row, 1, 2, 4 and 8 pieces, us: 16 sequences of up to 16384 tokens, 24 heads on 8 x 128, 217, 164, 158, 164; 64 of 4096, 16 heads on 4 x
+// 128, 113, 109, 121, 145, 16 x 64 197, 190, 215, 295.)
+static int few_split_rows(long long units, long long keys, int kc, const int *fit, int warps) {
+    const int split = few_split(units, keys, kc, fit, warps);
+    return split <= 2 && keys >= 32LL * split * kc * warps ? 2 * split : split;
 }
 
 template <typename Src, int DH, int NR>
@@ -629,14 +639,15 @@ static int launch_attn_few_nr(const BatchD &B, const AttnRows &A, const Src &src
             if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM) != cudaSuccess ||
                 cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
                 return false;
-            for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * FEW_WARPS, F::SMEM);
+            for (int i = 1; i < 5; ++i) fit[dev][i] = clusters_that_fit(kern, 1 << i, 32 * Src::WARPS, F::SMEM);
             return true;
         }))
         return NFD_E_CUDA;
     const long long tiles = ((long long)B.max_rows * A.share + F::ROWS - 1) / F::ROWS;
-    const int split = few_split((long long)kv_heads * B.n_seqs * tiles, keys, Src::KC, fit[dev]);
+    const long long units = (long long)kv_heads * B.n_seqs * tiles;
+    const int split = Src::RANGES ? few_split_rows(units, keys, Src::KC, fit[dev], Src::WARPS) : few_split(units, keys, Src::KC, fit[dev]);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kv_heads * split, B.n_seqs, (unsigned)tiles), cfg.blockDim = dim3(32 * FEW_WARPS), cfg.dynamicSmemBytes = F::SMEM, cfg.stream = st;
+    cfg.gridDim = dim3(kv_heads * split, B.n_seqs, (unsigned)tiles), cfg.blockDim = dim3(32 * Src::WARPS), cfg.dynamicSmemBytes = F::SMEM, cfg.stream = st;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at, cfg.numAttrs = split > 1;
