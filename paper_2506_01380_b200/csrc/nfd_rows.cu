@@ -115,8 +115,8 @@ int nfd_gate_norm(int n_rows, int width, int x_dtype, const void *x, long long x
     RET(this_device(dev, n_sm));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (x_dtype == NFD_DTYPE_FP32)
-        return dtype == NFD_DTYPE_FP32 ? launch_gate_norm<float, float>(N, n_sm, st) : launch_gate_norm<float, bf16>(N, n_sm, st);
-    return dtype == NFD_DTYPE_FP32 ? launch_gate_norm<bf16, float>(N, n_sm, st) : launch_gate_norm<bf16, bf16>(N, n_sm, st);
+        return dtype == NFD_DTYPE_FP32 ? launch_gate_norm<float, float>(N, dev, n_sm, st) : launch_gate_norm<float, bf16>(N, dev, n_sm, st);
+    return dtype == NFD_DTYPE_FP32 ? launch_gate_norm<bf16, float>(N, dev, n_sm, st) : launch_gate_norm<bf16, bf16>(N, dev, n_sm, st);
 }
 
 }  // extern "C"

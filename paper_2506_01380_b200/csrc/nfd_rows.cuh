@@ -1,7 +1,8 @@
 // Rows on their way from one projection of a block to the next: rotary embedding with a position on several axes, and the norms around a block with
 // its gate and residual scale.  Both read and write every number once; what bounds them is memory, or for few rows the launch and a chain of loads.
 #pragma once
-#include "nfd_append.cuh"
+#include "nfd_attn_rows.cuh"
+#include "nfd_sm100.cuh"
 
 // ---- rotation -----------------------------------------------------------------------------------------------
 #define ROTATE_THREADS 256
@@ -21,13 +22,33 @@ struct RotateIO {
     int n_rows;
 };
 // A CTA takes `rows` rows: sine and cosine of their pairs once for all heads (the angle, in turns, is formed and reduced in 64 bits, so that far
-// positions keep their fraction; sine and cosine of what is left are fp32), then eight pairs to a thread: 16 numbers in a row, or eight of either half of a head.
+// positions keep their fraction; sine and cosine of what is left are fp32), then eight pairs to a thread: 16 numbers in a row, or eight of either half of a
+// head.  A thread keeps its place in the rows; the first loads are issued before the angles are known.  (With four in flight and eight rows to
+// unpack there were 142 registers, a CTA to an SM, and 21504 rows of 32 heads x 64 took 121 us.)
 template <typename TS, bool HALVES>
-__global__ void __launch_bounds__(ROTATE_THREADS) k_rotate(const __grid_constant__ RotateD R, const RotateIO io, int rows, float sign) {
-    constexpr int U = 4;                                       // rows in flight
+__global__ void __launch_bounds__(ROTATE_THREADS, 5) k_rotate(const __grid_constant__ RotateD R, const RotateIO io, int rows, float sign) {
     __shared__ float2 s_cs[ROTATE_MAX_ROWS * (ROTATE_MAX_DIM / 2)];
     const int tid = threadIdx.x, r0 = blockIdx.x * rows, nr = min(rows, io.n_rows - r0), pairs = R.dim / 2, per_head = R.dim / 16;
     const int n0 = io.heads[0] * per_head, n = n0 + io.heads[1] * per_head;
+    // a thread's place (of n to a row), and the rows that it takes: row, row + by, ...
+    const int by = n < ROTATE_THREADS ? ROTATE_THREADS / n : 1, row = n < ROTATE_THREADS ? tid / n : 0;
+    int j = n < ROTATE_THREADS ? tid - row * n : tid;
+    struct Place {
+        const TS *in;
+        TS *out;
+        long long in_stride, out_stride;
+        int second, pair;                                      // the other eight numbers, the first pair
+    };
+    auto at = [&](int j) -> Place {
+        const int w = j >= n0, jj = w ? j - n0 : j, h = jj / per_head, d = jj - h * per_head, first = h * R.dim + (HALVES ? 8 * d : 16 * d);
+        return {(const TS *)io.in[w] + r0 * io.in_stride[w] + first, (TS *)io.out[w] + r0 * io.out_stride[w] + first, io.in_stride[w], io.out_stride[w],
+                HALVES ? pairs : 8, 8 * d};
+    };
+    float a[8], b[8];
+    auto load = [&](const Place &p, int r) { load8<TS>(p.in + r * p.in_stride, a), load8<TS>(p.in + r * p.in_stride + p.second, b); };
+    const bool mine = row < by && row < nr && j < n;
+    Place p = at(mine ? j : 0);
+    if (mine) load(p, row);
     for (int i = tid; i < nr * pairs; i += ROTATE_THREADS) {
         const int r = i / pairs, pair = i - r * pairs, axis = pair < R.half_t ? 0 : pair < R.half_th ? 1 : 2;
         const double turns = (double)__ldg(io.pos + 3LL * (r0 + r) + axis) * R.freq[pair];
@@ -36,41 +57,36 @@ __global__ void __launch_bounds__(ROTATE_THREADS) k_rotate(const __grid_constant
         s_cs[i] = make_float2(cs, sign * sn);
     }
     __syncthreads();
-    for (int j = tid; j < n; j += ROTATE_THREADS) {
-        const int w = j >= n0, jj = w ? j - n0 : j, h = jj / per_head, d = jj - h * per_head;
-        const int first = h * R.dim + (HALVES ? 8 * d : 16 * d), second = first + (HALVES ? pairs : 8);
-        const TS *in = (const TS *)io.in[w] + r0 * io.in_stride[w];
-        TS *out = (TS *)io.out[w] + r0 * io.out_stride[w];
-        for (int rb = 0; rb < nr; rb += U) {
-            float a[U][8], b[U][8];
+    if (!mine) return;
+    for (; j < n; j += ROTATE_THREADS) {
+        if (j >= ROTATE_THREADS) p = at(j), load(p, row);
+        for (int r = row; r < nr; r += by) {
+            if (r != row) load(p, r);
+            const float4 *cs = reinterpret_cast<const float4 *>(s_cs + r * pairs + p.pair);
+            auto turn = [](float &x, float &y, float co, float si) {
+                const float t = x * co - y * si;
+                y = y * co + x * si, x = t;
+            };
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (rb + u < nr) load8<TS>(in + (rb + u) * io.in_stride[w] + first, a[u]), load8<TS>(in + (rb + u) * io.in_stride[w] + second, b[u]);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (rb + u >= nr) break;
-                const float4 *cs = reinterpret_cast<const float4 *>(s_cs + (rb + u) * pairs + 8 * d);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float4 c = cs[e];
-                    auto turn = [](float &x, float &y, float co, float si) {
-                        const float t = x * co - y * si;
-                        y = y * co + x * si, x = t;
-                    };
-                    if (HALVES) {
-                        turn(a[u][2 * e], b[u][2 * e], c.x, c.y), turn(a[u][2 * e + 1], b[u][2 * e + 1], c.z, c.w);
-                    } else {
-                        float *x = e < 2 ? a[u] + 4 * e : b[u] + 4 * (e - 2);
-                        turn(x[0], x[1], c.x, c.y), turn(x[2], x[3], c.z, c.w);
-                    }
+            for (int e = 0; e < 4; ++e) {
+                const float4 c = cs[e];
+                if (HALVES) {
+                    turn(a[2 * e], b[2 * e], c.x, c.y), turn(a[2 * e + 1], b[2 * e + 1], c.z, c.w);
+                } else {
+                    float *x = e < 2 ? a + 4 * e : b + 4 * (e - 2);
+                    turn(x[0], x[1], c.x, c.y), turn(x[2], x[3], c.z, c.w);
                 }
-                store8<TS>(out + (rb + u) * io.out_stride[w] + first, a[u]), store8<TS>(out + (rb + u) * io.out_stride[w] + second, b[u]);
             }
+            store8<TS>(p.out + r * p.out_stride, a), store8<TS>(p.out + r * p.out_stride + p.second, b);
         }
+        if (n < ROTATE_THREADS) break;
     }
 }
 
 // ---- norms around a block -----------------------------------------------------------------------------------
+#define NORM_STAGES 6                    // rows of a CTA that are ahead, at most
+#define NORM_SHARED 225280               // shared memory of an SM for them
+#define NORM_MOST 196608                 // and of a CTA
 struct NormD {
     int on, layer, bf;                   // layer: LayerNorm, otherwise RMSNorm; bf: weight and bias are bf16, otherwise fp32
     float eps;
@@ -85,49 +101,149 @@ struct GateNormD {
     float res_scale;
     NormD post, pre;
 };
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bulk_wait(uint32_t bar, uint32_t parity) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long t0 = global_timer_ns();
+    uint32_t spins = 0;
+    while (!mbar_try_wait(bar, parity))
+        if ((++spins & 0x3ff) == 0 && global_timer_ns() - t0 > NFD_WAIT_LIMIT_NS) return false;
+    return true;
+}
 // eight parameters
 __device__ __forceinline__ void load8_par(const void *p, int bf, long long at, float *x) {
     if (bf) load8<bf16>((const bf16 *)p + at, x);
     else load8<float>((const float *)p + at, x);
 }
-// Sum over the threads of a row (T of them: a warp, or a CTA).
-template <int T> __device__ __forceinline__ float row_sum(float x, float *shared, int &turn) {
+// eight numbers as they are in memory
+template <typename TS> struct Raw8;
+template <> struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) { a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4); }
+    __device__ __forceinline__ void get(float *x) const { x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w; }
+};
+template <> struct Raw8<bf16> {
+    uint4 a;
+    __device__ __forceinline__ void load(const bf16 *p) { a = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void get(float *x) const {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+};
+// Sum over the threads of a row: a warp, or a CTA of up to 16.
+template <bool WARP> __device__ __forceinline__ float row_sum(float x, float *shared, int &turn) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    if constexpr (T > 32) {
-        float *s = shared + (turn ^= 1) * (T / 32);            // (who writes one half again has been through the barrier of the other)
-        if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
+    if constexpr (!WARP) {
+        float *s = shared + (turn ^= 16);                      // (who writes one half again has been through the barrier of the other)
+        const int lane = threadIdx.x & 31;
+        if (lane == 0) s[threadIdx.x >> 5] = x;
         __syncthreads();
-        x = s[threadIdx.x & (T / 32 - 1)];
+        x = lane < (int)blockDim.x / 32 ? s[lane] : 0.f;
 #pragma unroll
-        for (int d = T / 64; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        for (int d = 8; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        x = __shfl_sync(0xffffffffu, x, 0);
     }
     return x;
 }
-// t = post(y), x' = x + res_scale gate t, h = pre(x') (1 + scale) + shift, statistics in fp32 over numbers that stay in registers: the mean first, then
-// the squares of what is left.  T threads to a row, V pieces of eight numbers to a thread.
-template <typename TX, typename TY, int T, int V>
-__global__ void __launch_bounds__(T == 32 ? 256 : T) k_gate_norm(const __grid_constant__ GateNormD N) {
-    constexpr int RPC = T == 32 ? 8 : 1;                       // rows of a CTA
-    __shared__ float shared[2 * (T / 32)];
-    const int t = threadIdx.x % T, row = blockIdx.x * RPC + threadIdx.x / T, pieces = N.width / 8;
-    if (row >= N.n_rows) return;                               // (whole warps; a CTA of T > 32 has one row)
-    int turn = 0;
-    float x[V][8], y[V][8];
-    const TX *px = (const TX *)N.x + row * N.x_stride;
-    const TY *py = (const TY *)N.y + row * N.y_stride;
+// What a row's numbers are multiplied by and what is added, of a piece of eight: x' = x + y f ym + ya, h = x' f hm + ha.
+struct NormFactors {
+    float ym[8], ya[8], hm[8], ha[8];
+    __device__ __forceinline__ void load(const GateNormD &N, int m, int at) {
+        const long long mod = m * N.mod_stride + at;
+        float w[8];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+        for (int e = 0; e < 8; ++e) ym[e] = N.res_scale, ya[e] = 0.f, hm[e] = 1.f, ha[e] = 0.f;
+        if (N.y) {
+            if (N.gate) {
+                load8_par(N.gate, N.mod_bf, mod, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = 0.f;
-        if (i * T + t < pieces) {
-            load8<TX>(px + (i * T + t) * 8, x[i]);
-            if (N.y) load8<TY>(py + (i * T + t) * 8, y[i]);
+                for (int e = 0; e < 8; ++e) ym[e] *= w[e];
+            }
+            if (N.post.bias) {
+                load8_par(N.post.bias, N.post.bf, at, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ya[e] = ym[e] * w[e];
+            }
+            if (N.post.weight) {
+                load8_par(N.post.weight, N.post.bf, at, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ym[e] *= w[e];
+            }
+        }
+        if (!N.h) return;
+        if (N.scale) {
+            load8_par(N.scale, N.mod_bf, mod, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) hm[e] += w[e];
+        }
+        if (N.shift) load8_par(N.shift, N.mod_bf, mod, ha);
+        if (N.pre.bias) {
+            load8_par(N.pre.bias, N.pre.bf, at, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ha[e] = fmaf(w[e], hm[e], ha[e]);
+        }
+        if (N.pre.weight) {
+            load8_par(N.pre.weight, N.pre.bf, at, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) hm[e] *= w[e];
         }
     }
-    const int m = min(max(N.index ? __ldg(N.index + row) : row / N.rows_per_mod, 0), N.n_mods - 1);
-    const long long mod = m * N.mod_stride;
+};
+// t = post(y), x' = x + res_scale gate t, h = pre(x') (1 + scale) + shift, statistics in fp32 over numbers that stay in registers: the mean first, then
+// the squares of what is left.  A warp (WARP: up to 256 numbers a row) or a CTA takes `rows` rows one after the other, V pieces of eight numbers to a thread.
+// Weights, gate, scale and shift become one factor and one summand for either norm, kept from row to row as long as the modulation is the same (V = 1; wider
+// rows form them anew).  Where a CTA has several rows, bulk copies bring `stages` of them ahead into shared memory: with the next row in registers the bytes on
+// their way were too few.  Bound by the copy rate with many rows, by the launch and one chain of loads with few.  MEASURED
+template <typename TX, typename TY, bool WARP, int V>
+__global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_constant__ GateNormD N, int rows, int stages) {
+    extern __shared__ __align__(16) uint8_t norm_smem[];       // [stages] rows of x and y
+    __shared__ float shared[32];
+    __shared__ __align__(8) uint64_t s_full[NORM_STAGES];
+    const int t = WARP ? threadIdx.x & 31 : threadIdx.x, T = WARP ? 32 : blockDim.x, pieces = N.width / 8;
+    const long long first = (long long)(WARP ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x) * rows;
+    if (first >= N.n_rows) return;                             // (whole warps, or the whole CTA)
+    const int end = (int)min(first + rows, (long long)N.n_rows);
+    const bool ring = !WARP && stages;
+    const uint32_t bytes_x = N.width * sizeof(TX), bytes_y = N.y ? N.width * sizeof(TY) : 0, bar = smem_u32(s_full), to = smem_u32(norm_smem);
+    uint32_t laps = 0;                                         // copies into the stages so far, odd or even
+    auto bring = [&](int row, int st) {                        // (one thread)
+        laps ^= 1u << st;
+        const uint32_t dst = to + st * (bytes_x + bytes_y);
+        mbar_expect_tx(bar + 8 * st, bytes_x + bytes_y);
+        bulk_load(dst, (const TX *)N.x + row * N.x_stride, bytes_x, bar + 8 * st);
+        if (N.y) bulk_load(dst + bytes_x, (const TY *)N.y + row * N.y_stride, bytes_y, bar + 8 * st);
+    };
+    if (ring) {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < stages; ++i) mbar_init(bar + 8 * i, 1);
+            fence_mbar_init();
+            for (int i = 0; i < stages && first + i < end; ++i) bring((int)first + i, i);
+        }
+        __syncthreads();
+    }
+    int turn = 0, st = 0, m = -1;
+    uint32_t par = 0;
+    bool ok = true;
     const float per = 1.0f / (float)N.width;
+    Raw8<TX> rx[V];
+    Raw8<TY> ry[V];
+    auto fetch = [&](const TX *px, const TY *py) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i * T + t < pieces) {
+                rx[i].load(px + (i * T + t) * 8);
+                if (N.y) ry[i].load(py + (i * T + t) * 8);
+            }
+    };
+    auto fetch_row = [&](int row) { fetch((const TX *)N.x + row * N.x_stride, (const TY *)N.y + row * N.y_stride); };
+    auto mod_of = [&](int row) { return min(max(N.index ? __ldg(N.index + row) : row / N.rows_per_mod, 0), N.n_mods - 1); };
+    int next_m = mod_of((int)first);
+    if (!ring) fetch_row((int)first);
+    NormFactors kept;
     // numbers to what they are off the mean, and the factor that makes their mean square 1
     auto stats = [&](float (&v)[V][8], const NormD &n) -> float {
         if (n.layer) {
@@ -136,7 +252,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) k_gate_norm(const __grid_co
             for (int i = 0; i < V; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum += v[i][e];
-            const float mean = row_sum<T>(sum, shared, turn) * per;
+            const float mean = row_sum<WARP>(sum, shared, turn) * per;
 #pragma unroll
             for (int i = 0; i < V; ++i)
                 if (i * T + t < pieces)
@@ -148,72 +264,100 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) k_gate_norm(const __grid_co
         for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) sq = fmaf(v[i][e], v[i][e], sq);
-        return rsqrtf(row_sum<T>(sq, shared, turn) * per + n.eps);
+        return rsqrtf(row_sum<WARP>(sq, shared, turn) * per + n.eps);
     };
-    auto affine = [&](float *v, const NormD &n, int at, float f) {
-        float w[8];
-        if (n.weight) load8_par(n.weight, n.bf, at, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= n.weight ? f * w[e] : f;
-        if (n.bias) {
-            load8_par(n.bias, n.bf, at, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += w[e];
+#pragma unroll 1
+    for (int row = (int)first; row < end; ++row) {
+        if (ring) {
+            ok = ok && bulk_wait(bar + 8 * st, par);
+            const uint8_t *at = norm_smem + st * (bytes_x + bytes_y);
+            fetch(reinterpret_cast<const TX *>(at), reinterpret_cast<const TY *>(at + bytes_x));
         }
-    };
-    if (N.y) {
-        float f = 1.f;
-        if (N.post.on) f = stats(y, N.post);
-        TX *po = (TX *)N.x_out + row * N.x_out_stride;
+        float x[V][8], y[V][8];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int at = (i * T + t) * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = 0.f;
+            if (i * T + t < pieces) {
+                rx[i].get(x[i]);
+                if (N.y) ry[i].get(y[i]);
+            }
+        }
+        if (!ok) x[0][0] = NAN;                                // (a copy that did not come: the row is NaN)
+        // (behind a barrier of the CTA: the stage has been read)
+        bool again = ring;
+        auto refill = [&]() {
+            if (!again) return;
+            again = false;
+            if (threadIdx.x == 0 && ok && row + stages < end) bring(row + stages, st);
+            if (++st == stages) st = 0, par ^= 1;
+        };
+        if (ring && !N.h && !N.post.on) {
+            __syncthreads();
+            refill();
+        }
+        if (V == 1 && next_m != m && t < pieces) kept.load(N, next_m, t * 8);
+        m = next_m;
+        if (row + 1 < end) {
+            next_m = mod_of(row + 1);
+            if (!ring) fetch_row(row + 1);
+        }
+        if (N.y) {
+            const float f = N.post.on ? stats(y, N.post) : 1.f;
+            if (N.post.on) refill();
+            TX *po = (TX *)N.x_out + row * N.x_out_stride;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (i * T + t >= pieces) continue;
+                if (V > 1) kept.load(N, m, (i * T + t) * 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] = fmaf(y[i][e] * f, kept.ym[e], x[i][e] + kept.ya[e]);
+                store8<TX>(po + (i * T + t) * 8, x[i]);
+            }
+        }
+        if (!N.h) continue;
+        const float f = stats(x, N.pre);
+        refill();
+        TY *ph = (TY *)N.h + row * N.h_stride;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
             if (i * T + t >= pieces) continue;
-            if (N.post.on) affine(y[i], N.post, at, f);
-            float g[8];
-            if (N.gate) load8_par(N.gate, N.mod_bf, mod + at, g);
+            if (V > 1) kept.load(N, m, (i * T + t) * 8);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = fmaf(N.gate ? N.res_scale * g[e] : N.res_scale, y[i][e], x[i][e]);
-            store8<TX>(po + at, x[i]);
+            for (int e = 0; e < 8; ++e) x[i][e] = fmaf(x[i][e] * f, kept.hm[e], kept.ha[e]);
+            store8<TY>(ph + (i * T + t) * 8, x[i]);
         }
     }
-    if (!N.h) return;
-    const float f = stats(x, N.pre);
-    TY *ph = (TY *)N.h + row * N.h_stride;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int at = (i * T + t) * 8;
-        if (i * T + t >= pieces) continue;
-        affine(x[i], N.pre, at, f);
-        float w[8];
-        if (N.scale) {
-            load8_par(N.scale, N.mod_bf, mod + at, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = fmaf(x[i][e], w[e], x[i][e]);
-        }
-        if (N.shift) {
-            load8_par(N.shift, N.mod_bf, mod + at, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] += w[e];
-        }
-        store8<TY>(ph + at, x[i]);
-    }
+    if (ring && threadIdx.x == 0 && !ok)                       // (nobody leaves with copies in flight)
+        for (int i = 0; i < stages && first + i < end; ++i) bulk_wait(bar + 8 * i, laps >> i & 1 ^ 1);
 }
-template <typename TX, typename TY, int T, int V> static int launch_gate_norm_as(const GateNormD &N, cudaStream_t st) {
-    constexpr int RPC = T == 32 ? 8 : 1;
-    k_gate_norm<TX, TY, T, V><<<(unsigned)((N.n_rows + RPC - 1) / RPC), T == 32 ? 256 : T, 0, st>>>(N);
+// One wave of CTAs, the rows shared out evenly: a CTA for each row where the device holds them all at once.
+template <typename TX, typename TY, bool WARP, int V> static int launch_gate_norm_as(const GateNormD &N, int threads, int dev, int n_sm, cudaStream_t st) {
+    auto kern = k_gate_norm<TX, TY, WARP, V>;
+    static OncePerDevice once;
+    static int regs[NFD_PAGED_DEVICES];
+    if (!once.run(dev, [&] {
+            cudaFuncAttributes at;
+            if (cudaFuncGetAttributes(&at, kern) != cudaSuccess || cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_MOST) != cudaSuccess) return false;
+            regs[dev] = (at.numRegs + 7) / 8 * 8;
+            return true;
+        }))
+        return NFD_E_CUDA;
+    const int bytes = N.width * (int)(sizeof(TX) + (N.y ? sizeof(TY) : 0)), by_regs = 65536 / (regs[dev] * threads);
+    // rows ahead: as many as leave the CTAs that the registers allow (two of the widest fp32 rows do not fit: such a CTA loads the next row into registers)
+    int stages = WARP ? 0 : NORM_SHARED / by_regs / bytes;
+    stages = stages > NORM_STAGES ? NORM_STAGES : stages < 2 && !WARP && 2 * bytes <= NORM_MOST ? 2 : stages < 2 ? 0 : stages;
+    const int ctas = stages && NORM_SHARED / (stages * bytes) < by_regs ? NORM_SHARED / (stages * bytes) : by_regs;
+    const long long per = WARP ? threads / 32 : 1, held = (long long)(ctas < 1 ? 1 : ctas) * n_sm * per, rows = (N.n_rows + held - 1) / held;
+    if (rows == 1) stages = 0;
+    kern<<<(unsigned)((N.n_rows + rows * per - 1) / (rows * per)), threads, stages * bytes, st>>>(N, (int)rows, stages);
     return cudaGetLastError() == cudaSuccess ? NFD_OK : NFD_E_CUDA;
 }
-template <typename TX, typename TY> static int launch_gate_norm(const GateNormD &N, int n_sm, cudaStream_t st) {
+template <typename TX, typename TY> static int launch_gate_norm(const GateNormD &N, int dev, int n_sm, cudaStream_t st) {
     const int pieces = N.width / 8;
-    if (pieces <= 128 && (pieces <= 32 || N.n_rows >= 16 * n_sm)) {
-        if (pieces <= 32) return launch_gate_norm_as<TX, TY, 32, 1>(N, st);
-        if (pieces <= 64) return launch_gate_norm_as<TX, TY, 32, 2>(N, st);
-        return launch_gate_norm_as<TX, TY, 32, 4>(N, st);
-    }
-    if (pieces <= 128) return launch_gate_norm_as<TX, TY, 128, 1>(N, st);
-    if (pieces <= 256) return launch_gate_norm_as<TX, TY, 128, 2>(N, st);
-    if (pieces <= 512) return launch_gate_norm_as<TX, TY, 128, 4>(N, st);
-    if (pieces <= 1024) return launch_gate_norm_as<TX, TY, 512, 2>(N, st);
-    return launch_gate_norm_as<TX, TY, 512, 4>(N, st);
+    if (pieces <= 32) return launch_gate_norm_as<TX, TY, true, 1>(N, 128, dev, n_sm, st);
+    const int v = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : 4, threads = ((pieces + v - 1) / v + 31) / 32 * 32;
+    if (v == 1) return launch_gate_norm_as<TX, TY, false, 1>(N, threads, dev, n_sm, st);
+    if (v == 2) return launch_gate_norm_as<TX, TY, false, 2>(N, threads, dev, n_sm, st);
+    return launch_gate_norm_as<TX, TY, false, 4>(N, threads, dev, n_sm, st);
 }
