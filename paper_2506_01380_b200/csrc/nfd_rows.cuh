@@ -84,6 +84,7 @@ __global__ void __launch_bounds__(ROTATE_THREADS, 5) k_rotate(const __grid_const
 }
 
 // ---- norms around a block -----------------------------------------------------------------------------------
+#define NORM_FEW 8                       // rows to an SM up to which a CTA reads its own as it comes to it
 #define NORM_STAGES 6                    // rows of a CTA that are ahead, at most
 #define NORM_SHARED 225280               // shared memory of an SM for them
 #define NORM_MOST 196608                 // and of a CTA
@@ -152,29 +153,32 @@ template <bool WARP> __device__ __forceinline__ float row_sum(float x, float *sh
 // What a row's numbers are multiplied by and what is added, of a piece of eight: x' = x + y f ym + ya, h = x' f hm + ha.
 struct NormFactors {
     float ym[8], ya[8], hm[8], ha[8];
-    __device__ __forceinline__ void load(const GateNormD &N, int m, int at) {
+    __device__ __forceinline__ void load_y(const GateNormD &N, int m, int at) {
         const long long mod = m * N.mod_stride + at;
         float w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ym[e] = N.res_scale, ya[e] = 0.f, hm[e] = 1.f, ha[e] = 0.f;
-        if (N.y) {
-            if (N.gate) {
-                load8_par(N.gate, N.mod_bf, mod, w);
+        for (int e = 0; e < 8; ++e) ym[e] = N.res_scale, ya[e] = 0.f;
+        if (N.gate) {
+            load8_par(N.gate, N.mod_bf, mod, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ym[e] *= w[e];
-            }
-            if (N.post.bias) {
-                load8_par(N.post.bias, N.post.bf, at, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ya[e] = ym[e] * w[e];
-            }
-            if (N.post.weight) {
-                load8_par(N.post.weight, N.post.bf, at, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ym[e] *= w[e];
-            }
+            for (int e = 0; e < 8; ++e) ym[e] *= w[e];
         }
-        if (!N.h) return;
+        if (N.post.bias) {
+            load8_par(N.post.bias, N.post.bf, at, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ya[e] = ym[e] * w[e];
+        }
+        if (N.post.weight) {
+            load8_par(N.post.weight, N.post.bf, at, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ym[e] *= w[e];
+        }
+    }
+    __device__ __forceinline__ void load_h(const GateNormD &N, int m, int at) {
+        const long long mod = m * N.mod_stride + at;
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) hm[e] = 1.f, ha[e] = 0.f;
         if (N.scale) {
             load8_par(N.scale, N.mod_bf, mod, w);
 #pragma unroll
@@ -198,8 +202,10 @@ struct NormFactors {
 // Weights, gate, scale and shift become one factor and one summand for either norm, kept from row to row as long as the modulation is the same (V = 1; wider
 // rows form them anew).  Where a CTA has several rows, bulk copies bring `stages` of them ahead into shared memory: with the next row in registers the bytes on
 // their way were too few.  Bound by the copy rate with many rows, by the launch and one chain of loads with few.  MEASURED
-template <typename TX, typename TY, bool WARP, int V>
-__global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_constant__ GateNormD N, int rows, int stages) {
+enum { NORM_WARP, NORM_CTA, NORM_RING };
+template <typename TX, typename TY, int HOW, int V>
+__global__ void __launch_bounds__(HOW == NORM_WARP ? 128 : 512, HOW == NORM_RING && V == 1 ? 2 : 1) k_gate_norm(const __grid_constant__ GateNormD N, int rows, int stages) {
+    constexpr bool WARP = HOW == NORM_WARP, ring = HOW == NORM_RING;
     extern __shared__ __align__(16) uint8_t norm_smem[];       // [stages] rows of x and y
     __shared__ float shared[32];
     __shared__ __align__(8) uint64_t s_full[NORM_STAGES];
@@ -207,7 +213,6 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_con
     const long long first = (long long)(WARP ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x) * rows;
     if (first >= N.n_rows) return;                             // (whole warps, or the whole CTA)
     const int end = (int)min(first + rows, (long long)N.n_rows);
-    const bool ring = !WARP && stages;
     const uint32_t bytes_x = N.width * sizeof(TX), bytes_y = N.y ? N.width * sizeof(TY) : 0, bar = smem_u32(s_full), to = smem_u32(norm_smem);
     uint32_t laps = 0;                                         // copies into the stages so far, odd or even
     auto bring = [&](int row, int st) {                        // (one thread)
@@ -242,29 +247,29 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_con
     auto fetch_row = [&](int row) { fetch((const TX *)N.x + row * N.x_stride, (const TY *)N.y + row * N.y_stride); };
     auto mod_of = [&](int row) { return min(max(N.index ? __ldg(N.index + row) : row / N.rows_per_mod, 0), N.n_mods - 1); };
     int next_m = mod_of((int)first);
-    if (!ring) fetch_row((int)first);
+    if (WARP) fetch_row((int)first);
     NormFactors kept;
     // numbers to what they are off the mean, and the factor that makes their mean square 1
     auto stats = [&](float (&v)[V][8], const NormD &n) -> float {
         if (n.layer) {
-            float sum = 0.f;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < V; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += v[i][e];
-            const float mean = row_sum<WARP>(sum, shared, turn) * per;
+                for (int e = 0; e < 8; ++e) sum[e & 3] += v[i][e];
+            const float mean = row_sum<WARP>((sum[0] + sum[1]) + (sum[2] + sum[3]), shared, turn) * per;
 #pragma unroll
             for (int i = 0; i < V; ++i)
                 if (i * T + t < pieces)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[i][e] -= mean;
         }
-        float sq = 0.f;
+        float sq[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sq = fmaf(v[i][e], v[i][e], sq);
-        return rsqrtf(row_sum<WARP>(sq, shared, turn) * per + n.eps);
+            for (int e = 0; e < 8; ++e) sq[e & 3] = fmaf(v[i][e], v[i][e], sq[e & 3]);
+        return rsqrtf(row_sum<WARP>((sq[0] + sq[1]) + (sq[2] + sq[3]), shared, turn) * per + n.eps);
     };
 #pragma unroll 1
     for (int row = (int)first; row < end; ++row) {
@@ -272,6 +277,8 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_con
             ok = ok && bulk_wait(bar + 8 * st, par);
             const uint8_t *at = norm_smem + st * (bytes_x + bytes_y);
             fetch(reinterpret_cast<const TX *>(at), reinterpret_cast<const TY *>(at + bytes_x));
+        } else if (!WARP) {
+            fetch_row(row);
         }
         float x[V][8], y[V][8];
 #pragma unroll
@@ -296,11 +303,14 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_con
             __syncthreads();
             refill();
         }
-        if (V == 1 && next_m != m && t < pieces) kept.load(N, next_m, t * 8);
+        if (V == 1 && next_m != m && t < pieces) {
+            if (N.y) kept.load_y(N, next_m, t * 8);
+            if (N.h) kept.load_h(N, next_m, t * 8);
+        }
         m = next_m;
         if (row + 1 < end) {
             next_m = mod_of(row + 1);
-            if (!ring) fetch_row(row + 1);
+            if (WARP) fetch_row(row + 1);
         }
         if (N.y) {
             const float f = N.post.on ? stats(y, N.post) : 1.f;
@@ -309,7 +319,7 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_con
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 if (i * T + t >= pieces) continue;
-                if (V > 1) kept.load(N, m, (i * T + t) * 8);
+                if (V > 1) kept.load_y(N, m, (i * T + t) * 8);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[i][e] = fmaf(y[i][e] * f, kept.ym[e], x[i][e] + kept.ya[e]);
                 store8<TX>(po + (i * T + t) * 8, x[i]);
@@ -322,7 +332,7 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_con
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (i * T + t >= pieces) continue;
-            if (V > 1) kept.load(N, m, (i * T + t) * 8);
+            if (V > 1) kept.load_h(N, m, (i * T + t) * 8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[i][e] = fmaf(x[i][e] * f, kept.hm[e], kept.ha[e]);
             store8<TY>(ph + (i * T + t) * 8, x[i]);
@@ -332,8 +342,8 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) k_gate_norm(const __grid_con
         for (int i = 0; i < stages && first + i < end; ++i) bulk_wait(bar + 8 * i, laps >> i & 1 ^ 1);
 }
 // One wave of CTAs, the rows shared out evenly: a CTA for each row where the device holds them all at once.
-template <typename TX, typename TY, bool WARP, int V> static int launch_gate_norm_as(const GateNormD &N, int threads, int dev, int n_sm, cudaStream_t st) {
-    auto kern = k_gate_norm<TX, TY, WARP, V>;
+template <typename TX, typename TY, int HOW, int V> static int launch_gate_norm_as(const GateNormD &N, int threads, int bytes, int dev, int n_sm, cudaStream_t st) {
+    auto kern = k_gate_norm<TX, TY, HOW, V>;
     static OncePerDevice once;
     static int regs[NFD_PAGED_DEVICES];
     if (!once.run(dev, [&] {
@@ -343,21 +353,27 @@ template <typename TX, typename TY, bool WARP, int V> static int launch_gate_nor
             return true;
         }))
         return NFD_E_CUDA;
-    const int bytes = N.width * (int)(sizeof(TX) + (N.y ? sizeof(TY) : 0)), by_regs = 65536 / (regs[dev] * threads);
-    // rows ahead: as many as leave the CTAs that the registers allow (two of the widest fp32 rows do not fit: such a CTA loads the next row into registers)
-    int stages = WARP ? 0 : NORM_SHARED / by_regs / bytes;
-    stages = stages > NORM_STAGES ? NORM_STAGES : stages < 2 && !WARP && 2 * bytes <= NORM_MOST ? 2 : stages < 2 ? 0 : stages;
-    const int ctas = stages && NORM_SHARED / (stages * bytes) < by_regs ? NORM_SHARED / (stages * bytes) : by_regs;
-    const long long per = WARP ? threads / 32 : 1, held = (long long)(ctas < 1 ? 1 : ctas) * n_sm * per, rows = (N.n_rows + held - 1) / held;
-    if (rows == 1) stages = 0;
+    int ctas = 65536 / (regs[dev] * threads), stages = 0;
+    ctas = ctas < 1 ? 1 : ctas > 2048 / threads ? 2048 / threads : ctas;
+    if (HOW == NORM_RING) {
+        // as many rows ahead as leave the CTAs that the registers allow, two at least
+        stages = NORM_SHARED / ctas / bytes;
+        stages = stages > NORM_STAGES ? NORM_STAGES : stages < 2 ? 2 : stages;
+        ctas = NORM_SHARED / (stages * bytes) < ctas ? NORM_SHARED / (stages * bytes) : ctas;
+    }
+    const long long per = HOW == NORM_WARP ? threads / 32 : 1, held = (long long)ctas * n_sm * per, rows = (N.n_rows + held - 1) / held;
     kern<<<(unsigned)((N.n_rows + rows * per - 1) / (rows * per)), threads, stages * bytes, st>>>(N, (int)rows, stages);
     return cudaGetLastError() == cudaSuccess ? NFD_OK : NFD_E_CUDA;
 }
 template <typename TX, typename TY> static int launch_gate_norm(const GateNormD &N, int dev, int n_sm, cudaStream_t st) {
-    const int pieces = N.width / 8;
-    if (pieces <= 32) return launch_gate_norm_as<TX, TY, true, 1>(N, 128, dev, n_sm, st);
-    const int v = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : 4, threads = ((pieces + v - 1) / v + 31) / 32 * 32;
-    if (v == 1) return launch_gate_norm_as<TX, TY, false, 1>(N, threads, dev, n_sm, st);
-    if (v == 2) return launch_gate_norm_as<TX, TY, false, 2>(N, threads, dev, n_sm, st);
-    return launch_gate_norm_as<TX, TY, false, 4>(N, threads, dev, n_sm, st);
+    const int pieces = N.width / 8, v = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : 4, threads = ((pieces + v - 1) / v + 31) / 32 * 32;
+    const int bytes = N.width * (int)(sizeof(TX) + (N.y ? sizeof(TY) : 0));
+    if (pieces <= 32) return launch_gate_norm_as<TX, TY, NORM_WARP, 1>(N, 128, bytes, dev, n_sm, st);
+    auto go = [&](auto pieces_of_a_thread) -> int {
+        constexpr int V = decltype(pieces_of_a_thread)::value;
+        // (two of the widest fp32 rows do not fit into shared memory)
+        if (N.n_rows >= NORM_FEW * n_sm && 2 * bytes <= NORM_MOST) return launch_gate_norm_as<TX, TY, NORM_RING, V>(N, threads, bytes, dev, n_sm, st);
+        return launch_gate_norm_as<TX, TY, NORM_CTA, V>(N, threads, bytes, dev, n_sm, st);
+    };
+    return v == 1 ? go(std::integral_constant<int, 1>()) : v == 2 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 4>());
 }
