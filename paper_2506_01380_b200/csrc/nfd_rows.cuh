@@ -4,6 +4,23 @@
 #include "nfd_attn_rows.cuh"
 #include "nfd_sm100.cuh"
 
+// eight numbers as they are in memory
+template <typename TS> struct Raw8;
+template <> struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) { a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4); }
+    __device__ __forceinline__ void get(float *x) const { x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w; }
+};
+template <> struct Raw8<bf16> {
+    uint4 a;
+    __device__ __forceinline__ void load(const bf16 *p) { a = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void get(float *x) const {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+};
+
 // ---- rotation -----------------------------------------------------------------------------------------------
 #define ROTATE_THREADS 256
 #define ROTATE_MAX_ROWS 8
@@ -23,7 +40,7 @@ struct RotateIO {
 };
 // A CTA takes `rows` rows: sine and cosine of their pairs once for all heads (the angle, in turns, is formed and reduced in 64 bits, so that far
 // positions keep their fraction; sine and cosine of what is left are fp32), then eight pairs to a thread: 16 numbers in a row, or eight of either half of a
-// head.  A thread keeps its place in the rows; the first loads are issued before the angles are known.  (With four in flight and eight rows to
+// head.  A thread keeps its place in the rows and has the next of them on its way, the first before the angles are known.  (With four in flight and eight rows to
 // unpack there were 142 registers, a CTA to an SM, and 21504 rows of 32 heads x 64 took 121 us.)
 template <typename TS, bool HALVES>
 __global__ void __launch_bounds__(ROTATE_THREADS, 5) k_rotate(const __grid_constant__ RotateD R, const RotateIO io, int rows, float sign) {
@@ -44,8 +61,8 @@ __global__ void __launch_bounds__(ROTATE_THREADS, 5) k_rotate(const __grid_const
         return {(const TS *)io.in[w] + r0 * io.in_stride[w] + first, (TS *)io.out[w] + r0 * io.out_stride[w] + first, io.in_stride[w], io.out_stride[w],
                 HALVES ? pairs : 8, 8 * d};
     };
-    float a[8], b[8];
-    auto load = [&](const Place &p, int r) { load8<TS>(p.in + r * p.in_stride, a), load8<TS>(p.in + r * p.in_stride + p.second, b); };
+    Raw8<TS> ra, rb;                                           // the next row's numbers
+    auto load = [&](const Place &p, int r) { ra.load(p.in + r * p.in_stride), rb.load(p.in + r * p.in_stride + p.second); };
     const bool mine = row < by && row < nr && j < n;
     Place p = at(mine ? j : 0);
     if (mine) load(p, row);
@@ -61,7 +78,9 @@ __global__ void __launch_bounds__(ROTATE_THREADS, 5) k_rotate(const __grid_const
     for (; j < n; j += ROTATE_THREADS) {
         if (j >= ROTATE_THREADS) p = at(j), load(p, row);
         for (int r = row; r < nr; r += by) {
-            if (r != row) load(p, r);
+            float a[8], b[8];
+            ra.get(a), rb.get(b);
+            if (r + by < nr) load(p, r + by);
             const float4 *cs = reinterpret_cast<const float4 *>(s_cs + r * pairs + p.pair);
             auto turn = [](float &x, float &y, float co, float si) {
                 const float t = x * co - y * si;
@@ -113,27 +132,14 @@ __device__ __forceinline__ bool bulk_wait(uint32_t bar, uint32_t parity) {
         if ((++spins & 0x3ff) == 0 && global_timer_ns() - t0 > NFD_WAIT_LIMIT_NS) return false;
     return true;
 }
+__device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
 // eight parameters
 __device__ __forceinline__ void load8_par(const void *p, int bf, long long at, float *x) {
     if (bf) load8<bf16>((const bf16 *)p + at, x);
     else load8<float>((const float *)p + at, x);
 }
-// eight numbers as they are in memory
-template <typename TS> struct Raw8;
-template <> struct Raw8<float> {
-    float4 a, b;
-    __device__ __forceinline__ void load(const float *p) { a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4); }
-    __device__ __forceinline__ void get(float *x) const { x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w; }
-};
-template <> struct Raw8<bf16> {
-    uint4 a;
-    __device__ __forceinline__ void load(const bf16 *p) { a = *reinterpret_cast<const uint4 *>(p); }
-    __device__ __forceinline__ void get(float *x) const {
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-};
 // Sum over the threads of a row: a warp, or a CTA of up to 16.
 template <bool WARP> __device__ __forceinline__ float row_sum(float x, float *shared, int &turn) {
 #pragma unroll
@@ -213,12 +219,12 @@ __global__ void __launch_bounds__(HOW == NORM_WARP ? 128 : 512, HOW == NORM_RING
     const long long first = (long long)(WARP ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x) * rows;
     if (first >= N.n_rows) return;                             // (whole warps, or the whole CTA)
     const int end = (int)min(first + rows, (long long)N.n_rows);
-    const uint32_t bytes_x = N.width * sizeof(TX), bytes_y = N.y ? N.width * sizeof(TY) : 0, bar = smem_u32(s_full), to = smem_u32(norm_smem);
+    const uint32_t bytes_x = N.width * sizeof(TX), bytes_y = N.width * sizeof(TY), bytes = bytes_x + bytes_y, bar = smem_u32(s_full), to = smem_u32(norm_smem);
     uint32_t laps = 0;                                         // copies into the stages so far, odd or even
     auto bring = [&](int row, int st) {                        // (one thread)
         laps ^= 1u << st;
-        const uint32_t dst = to + st * (bytes_x + bytes_y);
-        mbar_expect_tx(bar + 8 * st, bytes_x + bytes_y);
+        const uint32_t dst = to + st * bytes;
+        mbar_expect_tx(bar + 8 * st, N.y ? bytes : bytes_x);
         bulk_load(dst, (const TX *)N.x + row * N.x_stride, bytes_x, bar + 8 * st);
         if (N.y) bulk_load(dst + bytes_x, (const TY *)N.y + row * N.y_stride, bytes_y, bar + 8 * st);
     };
@@ -245,7 +251,8 @@ __global__ void __launch_bounds__(HOW == NORM_WARP ? 128 : 512, HOW == NORM_RING
             }
     };
     auto fetch_row = [&](int row) { fetch((const TX *)N.x + row * N.x_stride, (const TY *)N.y + row * N.y_stride); };
-    auto mod_of = [&](int row) { return min(max(N.index ? __ldg(N.index + row) : row / N.rows_per_mod, 0), N.n_mods - 1); };
+    // (clamped when it is used, a row later: a warp stops at the first instruction that asks for a load's result)
+    auto mod_of = [&](int row) { return N.index ? __ldg(N.index + row) : row / N.rows_per_mod; };
     int next_m = mod_of((int)first);
     if (WARP) fetch_row((int)first);
     NormFactors kept;
@@ -275,7 +282,7 @@ __global__ void __launch_bounds__(HOW == NORM_WARP ? 128 : 512, HOW == NORM_RING
     for (int row = (int)first; row < end; ++row) {
         if (ring) {
             ok = ok && bulk_wait(bar + 8 * st, par);
-            const uint8_t *at = norm_smem + st * (bytes_x + bytes_y);
+            const uint8_t *at = norm_smem + st * bytes;
             fetch(reinterpret_cast<const TX *>(at), reinterpret_cast<const TY *>(at + bytes_x));
         } else if (!WARP) {
             fetch_row(row);
@@ -291,31 +298,19 @@ __global__ void __launch_bounds__(HOW == NORM_WARP ? 128 : 512, HOW == NORM_RING
             }
         }
         if (!ok) x[0][0] = NAN;                                // (a copy that did not come: the row is NaN)
-        // (behind a barrier of the CTA: the stage has been read)
-        bool again = ring;
-        auto refill = [&]() {
-            if (!again) return;
-            again = false;
-            if (threadIdx.x == 0 && ok && row + stages < end) bring(row + stages, st);
-            if (++st == stages) st = 0, par ^= 1;
-        };
-        if (ring && !N.h && !N.post.on) {
-            __syncthreads();
-            refill();
+        const int now = min(max(next_m, 0), N.n_mods - 1);
+        if (V == 1 && now != m && t < pieces) {
+            if (N.y) kept.load_y(N, now, t * 8);
+            if (N.h) kept.load_h(N, now, t * 8);
         }
-        if (V == 1 && next_m != m && t < pieces) {
-            if (N.y) kept.load_y(N, next_m, t * 8);
-            if (N.h) kept.load_h(N, next_m, t * 8);
-        }
-        m = next_m;
+        m = now;
         if (row + 1 < end) {
             next_m = mod_of(row + 1);
             if (WARP) fetch_row(row + 1);
         }
         if (N.y) {
             const float f = N.post.on ? stats(y, N.post) : 1.f;
-            if (N.post.on) refill();
-            TX *po = (TX *)N.x_out + row * N.x_out_stride;
+            TX *po = ring ? reinterpret_cast<TX *>(norm_smem + st * bytes) : (TX *)N.x_out + row * N.x_out_stride;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 if (i * T + t >= pieces) continue;
@@ -325,10 +320,9 @@ __global__ void __launch_bounds__(HOW == NORM_WARP ? 128 : 512, HOW == NORM_RING
                 store8<TX>(po + (i * T + t) * 8, x[i]);
             }
         }
-        if (!N.h) continue;
+        if (N.h) {
         const float f = stats(x, N.pre);
-        refill();
-        TY *ph = (TY *)N.h + row * N.h_stride;
+        TY *ph = ring ? reinterpret_cast<TY *>(norm_smem + st * bytes + bytes_x) : (TY *)N.h + row * N.h_stride;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (i * T + t >= pieces) continue;
@@ -337,9 +331,31 @@ __global__ void __launch_bounds__(HOW == NORM_WARP ? 128 : 512, HOW == NORM_RING
             for (int e = 0; e < 8; ++e) x[i][e] = fmaf(x[i][e] * f, kept.hm[e], kept.ha[e]);
             store8<TY>(ph + (i * T + t) * 8, x[i]);
         }
+        }
+        if (ring) {
+            // The results lie where the row lay (a thread writes what it alone has read), and go out from there; a stage is filled again a row later, when
+            // its results have been read.
+            fence_proxy_async_smem();
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                const uint32_t from = to + st * bytes;
+                if (N.y) bulk_store((TX *)N.x_out + row * N.x_out_stride, from, bytes_x);
+                if (N.h) bulk_store((TY *)N.h + row * N.h_stride, from + bytes_x, bytes_y);
+                bulk_commit();
+                const int last = st ? st - 1 : stages - 1, again = row - 1 + stages;
+                if (row > (int)first && ok && again < end) {
+                    bulk_wait_read<1>();
+                    bring(again, last);
+                }
+            }
+            if (++st == stages) st = 0, par ^= 1;
+        }
     }
-    if (ring && threadIdx.x == 0 && !ok)                       // (nobody leaves with copies in flight)
-        for (int i = 0; i < stages && first + i < end; ++i) bulk_wait(bar + 8 * i, laps >> i & 1 ^ 1);
+    if (ring && threadIdx.x == 0) {                            // (nobody leaves with copies in flight)
+        if (!ok)
+            for (int i = 0; i < stages && first + i < end; ++i) bulk_wait(bar + 8 * i, laps >> i & 1 ^ 1);
+        bulk_wait_all();
+    }
 }
 // One wave of CTAs, the rows shared out evenly: a CTA for each row where the device holds them all at once.
 template <typename TX, typename TY, int HOW, int V> static int launch_gate_norm_as(const GateNormD &N, int threads, int bytes, int dev, int n_sm, cudaStream_t st) {
@@ -367,7 +383,7 @@ template <typename TX, typename TY, int HOW, int V> static int launch_gate_norm_
 }
 template <typename TX, typename TY> static int launch_gate_norm(const GateNormD &N, int dev, int n_sm, cudaStream_t st) {
     const int pieces = N.width / 8, v = pieces <= 512 ? 1 : pieces <= 1024 ? 2 : 4, threads = ((pieces + v - 1) / v + 31) / 32 * 32;
-    const int bytes = N.width * (int)(sizeof(TX) + (N.y ? sizeof(TY) : 0));
+    const int bytes = N.width * (int)(sizeof(TX) + sizeof(TY));
     if (pieces <= 32) return launch_gate_norm_as<TX, TY, NORM_WARP, 1>(N, 128, bytes, dev, n_sm, st);
     auto go = [&](auto pieces_of_a_thread) -> int {
         constexpr int V = decltype(pieces_of_a_thread)::value;
