@@ -69,6 +69,12 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
     // G threads to a key, a share of its row each
     constexpr int G = C::THREADS / F32_KEYS, PART = DH / G;
     const int key = tid / G, part = tid % G;
+    long long seq = 0;                                                  // of states: where the sequence's begin, and what the mask says
+    const unsigned char *mask = nullptr;
+    if constexpr (!Src::RANGES) {
+        seq = s * K.seq_stride + h * K.head_stride;
+        mask = K.mask ? K.mask + (size_t)s * K.n_keys : nullptr;
+    }
     auto cursor = [&]() {
         if constexpr (Src::RANGES) return K.cursor(B, s, sr.x, lo + t0 * F32_KEYS + key, F32_KEYS);
         else return 0;
@@ -82,8 +88,8 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
             here = row >= 0;
             k = K.k_row(here ? row : 0, h) + part * PART, v = K.v_row(here ? row : 0, h) + part * PART;
         } else {
-            here = here && (!K.mask || K.mask[(size_t)s * K.n_keys + p]);
-            const long long at = here ? s * K.seq_stride + h * K.head_stride + p * K.key_stride + part * PART : 0;
+            here = here && (!mask || mask[p]);
+            const long long at = here ? seq + p * K.key_stride + part * PART : 0;
             k += at, v += at;
         }
         const uint32_t dk = smem_u32(f32_smem + C::AT_K + (b * F32_KEYS + key) * LD + part * PART);
@@ -334,6 +340,12 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD
     int next = lo + (rank * FEW_WARPS + warp) * KC, base = next;
     uint32_t raw = 0, bits[2] = {0, 0};                                 // key `lane` of the chunk that is filled next; which keys of the next two chunks are there
     long long place = -1;                                               // its row
+    long long from = 0;                                                 // of states: where the sequence's begin, and what the mask says
+    const unsigned char *mask = nullptr;
+    if constexpr (!Src::RANGES) {
+        from = s * K.seq_stride + h * K.head_stride + word * 4;
+        mask = K.mask ? K.mask + (size_t)s * K.n_keys : nullptr;
+    }
     auto cursor = [&]() {
         if constexpr (Src::RANGES) return K.cursor(B, s, sr.x, next + lane, step);
         else return 0;
@@ -345,13 +357,13 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) k_attn_f32_few(const BatchD
             place = K.next(cursor, B, h, raw);
             raw = place >= 0;
         } else {
-            if (K.mask && raw) raw = K.mask[(size_t)s * K.n_keys + p];
+            if (mask && raw) raw = mask[p];
         }
     };
     auto fill = [&](int st) -> uint32_t {
         const uint32_t there = __ballot_sync(0xffffffffu, raw != 0), dst = smem_u32(ring) + st * C::STAGE;
         long long at = 0;
-        if constexpr (!Src::RANGES) at = s * K.seq_stride + h * K.head_stride + word * 4 + (long long)(next + key0) * K.key_stride;
+        if constexpr (!Src::RANGES) at = from + (long long)(next + key0) * K.key_stride;
 #pragma unroll
         for (int i = 0; i < KC / STEP; ++i) {
             const int key = key0 + i * STEP;
