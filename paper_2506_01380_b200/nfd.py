@@ -441,19 +441,32 @@ def rotate(rope: Rope, positions, x, x_out=None, x2=None, x2_out=None, halves: b
     [n_rows, 3] (int32: time, height, width) into x_out and x2_out (None: in place).  halves: pairs are (i, i + head_dim / 2)
     instead of (2 i, 2 i + 1); back: by the negative angle.  All rows may be strided."""
     (n, h, dh), dtype, dev = x.shape, x.dtype, x.get_device()
-    assert x.is_cuda and dtype in _TYPES
-    assert positions.dtype == torch.int32 and tuple(positions.shape) == (n, 3) and positions.is_contiguous() and positions.get_device() == dev
-    x_out = x if x_out is None else x_out
-    args = [h, x.data_ptr(), _row_stride(x, n, h, dh, dtype, dev), x_out.data_ptr(), _row_stride(x_out, n, h, dh, dtype, dev)]
-    if x2 is None:
-        args += [0, None, 0, None, 0]
-    else:
-        x2_out = x2 if x2_out is None else x2_out
+    assert dtype in _TYPES and dev >= 0
+    assert positions.dtype is torch.int32 and positions.shape == (n, 3) and positions.is_contiguous() and positions.get_device() == dev
+    xs = os_ = _row_stride(x, n, h, dh, dtype, dev)
+    if x_out is None:
+        x_out = x
+    elif x_out is not x:
+        os_ = _row_stride(x_out, n, h, dh, dtype, dev)
+    h2 = xs2 = os2 = xp2 = op2 = 0
+    if x2 is not None:
         h2 = x2.shape[1]
-        args += [h2, x2.data_ptr(), _row_stride(x2, n, h2, dh, dtype, dev), x2_out.data_ptr(), _row_stride(x2_out, n, h2, dh, dtype, dev)]
+        xs2 = os2 = _row_stride(x2, n, h2, dh, dtype, dev)
+        if x2_out is None:
+            x2_out = x2
+        elif x2_out is not x2:
+            os2 = _row_stride(x2_out, n, h2, dh, dtype, dev)
+        xp2, op2 = x2.data_ptr(), x2_out.data_ptr()
     _call("nfd_rotate", dev, stream, load().nfd_rotate, rope.ref, I.ROTATE_HALVES * halves + I.ROTATE_BACK * back, _TYPES[dtype], dh, n,
-          positions.data_ptr(), *args)
+          positions.data_ptr(), h, x.data_ptr(), xs, x_out.data_ptr(), os_, h2, xp2, xs2, op2, os2)
     return x_out, x2_out
+
+
+def _plain_rows(t, shape, dtype, dev):
+    """Elements between the rows of t, whose numbers are dense."""
+    st = t.stride()
+    assert t.dtype is dtype and t.shape == shape and t.get_device() == dev and st[1] == 1
+    return st[0] if shape[0] > 1 else shape[1]
 
 
 def gate_norm(x, y=None, x_out=None, h=None, pre: Norm = None, post: Norm = None, mod: Modulation = None, res_scale: float = 1.0,
@@ -461,19 +474,31 @@ def gate_norm(x, y=None, x_out=None, h=None, pre: Norm = None, post: Norm = None
     """nfd_gate_norm: t = post(y), x_out = x + res_scale * gate * t, h = pre(x_out) * (1 + scale) + shift, row by row.  x and
     x_out [n_rows, width] (the residual stream; x_out None: in place) are of one type, y and h of one type, float32 or bfloat16; rows may
     be strided.  Without y: h = pre(x) * (1 + scale) + shift.  Returns (x_out, h)."""
-    (n, width), dev = x.shape, x.get_device()
-    assert x.is_cuda and x.dtype in _TYPES and (y is not None or h is not None)
-    other = (y if y is not None else h).dtype
-    x_out = x if x_out is None and y is not None else x_out
-    args = []
-    for t, dtype in ((x, x.dtype), (y, other), (x_out if y is not None else None, x.dtype), (h, other)):
-        args += [None, 0] if t is None else [t.data_ptr(), _row_stride(t, n, 1, width, dtype, dev)]
-    for p in (pre, post, mod):
-        assert p is None or (p.width in (width, None) and p.dev in (dev, None))
-    assert mod is None or mod.index is None or mod.index.shape[0] == n
-    ref = lambda p: p.ref if p is not None else None
-    _call("nfd_gate_norm", dev, stream, load().nfd_gate_norm, n, width, _TYPES[x.dtype], args[0], args[1], _TYPES[other], *args[2:],
-          ref(post), ref(pre), ref(mod), res_scale)
+    shape, dtype, dev = x.shape, x.dtype, x.get_device()
+    n, width = shape
+    assert dev >= 0 and (y is not None or h is not None)
+    other = y.dtype if y is not None else h.dtype
+    xs = os_ = _plain_rows(x, shape, dtype, dev)
+    yp = ys = op = hp = hs = ref_post = ref_pre = ref_mod = None
+    if y is not None:
+        yp, ys = y.data_ptr(), _plain_rows(y, shape, other, dev)
+        if x_out is None:
+            x_out = x
+        elif x_out is not x:
+            os_ = _plain_rows(x_out, shape, dtype, dev)
+        op = x_out.data_ptr()
+        if post is not None:
+            assert post.width is None or (post.width == width and post.dev == dev)
+            ref_post = post.ref
+    if h is not None:
+        hp, hs = h.data_ptr(), _plain_rows(h, shape, other, dev)
+        assert pre is not None and (pre.width is None or (pre.width == width and pre.dev == dev))
+        ref_pre = pre.ref
+    if mod is not None:
+        assert mod.width == width and mod.dev == dev and (mod.index is None or mod.index.shape[0] == n)
+        ref_mod = mod.ref
+    _call("nfd_gate_norm", dev, stream, load().nfd_gate_norm, n, width, _TYPES[dtype], x.data_ptr(), xs, _TYPES[other], yp, ys or 0, op, os_,
+          hp, hs or 0, ref_post, ref_pre, ref_mod, res_scale)
     return x_out, h
 
 
