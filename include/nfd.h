@@ -387,7 +387,8 @@ int nfd_rotate(const nfd_rope *rope, int flags, int dtype, int head_dim, int n_r
  * NULL: 1, 0, 0; row r has modulation index[r] (dev; kept into 0 .. n_mods - 1) or, with index NULL,
  * r / rows_per_mod; mod NULL: none.  width: a multiple of 8, up to NFD_MAX_WIDTH.  Everything is
  * computed in fp32, from the numbers as they are given, and rounded once where it is stored: h is the norm of the
- * sum before x_out's rounding. */
+ * sum before x_out's rounding.  x_out is x, and h is y, with the same stride or not at all: outputs share no memory
+ * with inputs, nor with one another, otherwise. */
 #define NFD_NORM_LAYER 0
 #define NFD_NORM_RMS 1
 #define NFD_MAX_WIDTH 16384

@@ -1,10 +1,12 @@
 // Attention of many rows under the block-wise causal mask on tcgen05 / TMEM, to bf16 pages or to the rows of packed prompts.
 //
-// The rows of a sequence that share a head of keys (rows x heads that share it) are cut into tiles of 128; a CTA takes two of them, which share
-// every copied block of keys, or one, whose blocks its two softmax groups take in turn.  Each group has S accumulators, O, m and l of its own:
+// The rows of a sequence that share a head of keys (rows x heads that share it) are cut into tiles of 128; a CTA takes as many of them as it has softmax
+// groups (two with head dimension 128, three below), which share every copied block of keys, or one, whose blocks its groups take in turn.  Each group has
+// an accumulator for S and one for O, m and l of its own:
 //     S = Q K^T     UMMA 128 x KB x DH, operands in shared memory, accumulator in tensor memory
 //     P = exp2(S c - m)   one thread per row: S to registers, exponentials, P as bf16 over the S it came from
 //     O += P V      UMMA 128 x head_dim x KB, P from tensor memory, V as it lies (MN-major)
+// P is rounded to bf16 because that product's operands are of one type, V's; its relative error of 2^-9 a key is of the size of V's own.  Sums, m and O are fp32.
 // m is the largest of the first 16 scores that a row sees, and no other maximum is taken: a probability is exact to the same number of bits whatever its
 // size.  Where a sum of a row passes 2^50 after all (or is NaN), or a row has no m yet, the warp takes its keys again, S being untouched so far: the
 // maximum first, and where it has risen by more than 8 (a factor of 256) it becomes m and the row's O is rescaled in tensor memory.  What P grows to, O
@@ -14,13 +16,20 @@
 // keeps keys out and not values: 0 x NaN is NaN.  So in blocks that not all rows of a CTA see, the producers take values that are not finite out of V and
 // note where; a row that does see one adds it to its result at the end.
 //
-// Warp 0 fills a ring of K and V blocks in turn by TMA, a lane looking up the place of each box of keys, and warps 1 .. 3 look through values where that is
-// needed; where pages do not consist of boxes (or with head dimension 32) the four of them copy by cp.async, a lane looking up the place of each key.  Warp 4 issues
-// the products; the last 8 are the softmax groups.  Which keys of a block are there is told beside K, a bit each, in a ring of its own.
+// Producer warps come first.  Warp 0 fills a ring of K and V blocks in turn by TMA, a lane looking up the place of each box of keys, and the others look
+// through values where that is needed; where pages do not consist of boxes (or with head dimension 32) all of them copy by cp.async, a lane looking up the
+// place of each key (four chunks of 512 rows behind 15872, 16 heads on 4 x 128: 380 us so, 246 us by TMA).  The next warp issues the products, the last ones are the softmax
+// groups.  Which keys of a block are there is told beside K, a bit each, in a ring of its own.
 //
 // A unit (sequence, head of keys, tiles) with many keys and few others beside it is split over the CTAs of a cluster, which merge through distributed
 // shared memory in a fixed order.  Every wait on a barrier in memory is bounded; after one that ran out the rows are NaN.  (The cluster's own barrier needs
 // no bound: every CTA comes to it, its other waits being bounded, or has left as a whole cluster.)
+//
+// What bounds it.  With head dimension 128 the tensor pipe: two causal prompts of 8192 rows, 16 heads on 4, take 457 us alone (1200 TFLOP/s) and 536 us after
+// many of their kind, when the clock has fallen (1030).  With 64 a block is 10 short products, which their one thread issues in 600 to 700 clocks, and the
+// chain S, P, O of each group (four prompts of 5376 rows in frames of 336, 16 heads: 336 us; the exponentials alone would take 211): hence three groups there,
+// whose chains overlap; with 128 tensor memory holds two.  Groups with an issuing thread each, or that wait for their turn at the pipes, were slower.
+// Short prompts are their CTAs' beginning (5 to 7 thousand clocks) and end (5).
 #pragma once
 #include "nfd_attn_tile.cuh"
 #include <cuda.h>
@@ -28,6 +37,7 @@
 #define BLOCK_THREADS 512
 #define BLOCK_SPLIT 8               // most CTAs of a cluster
 #define BLOCK_SORTED 128            // sequences whose tiles are dealt out deepest first
+#define BLOCK_POLY 2                // pairs of eight whose exponentials are polynomials
 #define BLOCK_GROWTH 50             // bits that a sum may grow by before m follows it
 
 template <int DH> struct BlockCfg {
@@ -441,17 +451,15 @@ __device__ __forceinline__ float2 block_exp2_poly(float2 x) {
     p = make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
     return flush2(p);
 }
-#ifndef NPOLY
-#define NPOLY 2
-#endif
-// sixteen scores to P, as pairs, and their sum
+// sixteen scores to P, as pairs, and their sum.  BLOCK_POLY of eight pairs go to the fp32 pipes: with two warps to a scheduler a pair of columns takes 18.3
+// clocks with none, 18.2 with one, 16.6 with two and with three.
 template <bool MASKED> __device__ __forceinline__ void block_exp16(const float *x, uint32_t bits, float c, float mc, uint32_t *pk, float2 (&ls)[2]) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
         float2 s = make_float2(x[2 * u], x[2 * u + 1]);
         if (MASKED) s.x = bits >> (2 * u) & 1 ? s.x : -INFINITY, s.y = bits >> (2 * u + 1) & 1 ? s.y : -INFINITY;
         const float2 e = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
-        const float2 p = !MASKED && ((u + 1) * NPOLY / 8 != u * NPOLY / 8) ? block_exp2_poly(e) : make_float2(few_exp2(e.x), few_exp2(e.y));
+        const float2 p = !MASKED && ((u + 1) * BLOCK_POLY / 8 != u * BLOCK_POLY / 8) ? block_exp2_poly(e) : make_float2(few_exp2(e.x), few_exp2(e.y));
         ls[u & 1] = fadd2(ls[u & 1], p);
         pk[u] = bf16_pair(p.x, p.y);
     }

@@ -1,4 +1,4 @@
-// Attention of a batch's rows to fp32 encoder states, on the fp32 pipes.
+// Attention of a batch's rows to fp32 keys, on the fp32 pipes: an encoder's states, pages, the rows of packed prompts.
 //
 // k_attn_f32: a CTA takes 32 or 64 rows (rows x heads that share a head of keys) of a sequence and walks its keys in tiles of 64, the next tile's copies in
 // flight: S = Q K^T with 4 rows x 4 keys to a thread, an online softmax per row over the 16 lanes that hold it, P through shared memory
@@ -188,37 +188,37 @@ __global__ void __launch_bounds__(4 * ROWS) k_attn_f32(const BatchD B, const Att
         // O: rows 4 ty + i, dims: words of up to four, tx-th of every 16 of them
         auto sum = [&](auto masked) {
 #pragma unroll 4
-        for (int k = 0; k < F32_KEYS; k += 4) {
-            float4 p[4];
+            for (int k = 0; k < F32_KEYS; k += 4) {
+                float4 p[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4 *>(sP + (4 * ty + i) * LP + k);
+                for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4 *>(sP + (4 * ty + i) * LP + k);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                float v[ND];
-                if constexpr (DH == 32) {
-                    const float2 a = *reinterpret_cast<const float2 *>(vt + (k + u) * LD + 2 * tx);
-                    v[0] = a.x, v[1] = a.y;
-                } else {
+                for (int u = 0; u < 4; ++u) {
+                    float v[ND];
+                    if constexpr (DH == 32) {
+                        const float2 a = *reinterpret_cast<const float2 *>(vt + (k + u) * LD + 2 * tx);
+                        v[0] = a.x, v[1] = a.y;
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < ND; e += 4) {
-                        const float4 a = *reinterpret_cast<const float4 *>(vt + (k + u) * LD + 16 * e + 4 * tx);
-                        v[e] = a.x, v[e + 1] = a.y, v[e + 2] = a.z, v[e + 3] = a.w;
+                        for (int e = 0; e < ND; e += 4) {
+                            const float4 a = *reinterpret_cast<const float4 *>(vt + (k + u) * LD + 16 * e + 4 * tx);
+                            v[e] = a.x, v[e + 1] = a.y, v[e + 2] = a.z, v[e + 3] = a.w;
+                        }
                     }
-                }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (decltype(masked)::value) {
-                        if (p0 + k + u < kr[i].lo || p0 + k + u >= kr[i].hi) continue;
-                    }
-                    const float pu = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (decltype(masked)::value) {
+                            if (p0 + k + u < kr[i].lo || p0 + k + u >= kr[i].hi) continue;
+                        }
+                        const float pu = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
 #pragma unroll
-                    for (int e = 0; e < ND; e += 2) {
-                        const float2 y = ffma2(make_float2(pu, pu), make_float2(v[e], v[e + 1]), make_float2(o[i][e], o[i][e + 1]));
-                        o[i][e] = y.x, o[i][e + 1] = y.y;
+                        for (int e = 0; e < ND; e += 2) {
+                            const float2 y = ffma2(make_float2(pu, pu), make_float2(v[e], v[e + 1]), make_float2(o[i][e], o[i][e + 1]));
+                            o[i][e] = y.x, o[i][e + 1] = y.y;
+                        }
                     }
                 }
             }
-        }
         };
         if (Src::RANGES && edge) sum(std::integral_constant<bool, Src::RANGES>());
         else sum(std::false_type());
