@@ -1,4 +1,4 @@
-// Attention of a few rows to many keys, on 4-bit pages or bf16 states: single tokens, short speculations, a row or two of a
+// Attention of a few rows to many keys, on 4-bit pages, bf16 pages, bf16 states or the rows of packed prompts: single tokens, short speculations, a row or two of a
 // decoder against an encoder's states.
 //
 // A unit of work is (sequence, head of keys, up to 8 NR rows: rows x heads that share it).  The bound is the stream of K and V, and with
@@ -16,12 +16,14 @@
 // (for O); 4-bit codes become bf16 numbers in registers (Kv4Scale).  P is rounded to one bf16 number, as in the kernel for many rows.
 // Measured: one row, 16 heads x 64, behind 5712 tokens in 4-bit pages 10.0 us (pieces, merge and launch; 6.6 MB); eight sequences of up to 32768
 // tokens, 24 heads on 8 x 128, 84.5 us (185 MB, 2.2 TB/s: nothing is saturated, 48 % of the issue slots, 28 % of the copy rate; latency, and lengths that
-// differ); bf16 states, eight rows, 16 heads x 64 against 4096 25.4 us (134 MB, 5.3 TB/s).
+// differ); bf16 states, eight rows, 16 heads x 64 against 4096 25.4 us (134 MB, 5.3 TB/s);
+// bf16 pages, 16 sequences of one row behind up to 16384 tokens, 24 heads on 8 x 128, 146 to 159 us (701 MB, 4.4 to 4.8 TB/s).
 #pragma once
 #include "nfd_attn_rows.cuh"
 #include "nfd_sm100.cuh"
 
 #define FEW_WARPS 8
+#define FEW_SORTED 128              // sequences that are taken longest first, at most
 // Rows of a unit that this kernel takes.  Measured against the kernel for many rows, us: 16 heads x 64 behind 5712 tokens in 4-bit pages, 24, 64 and
 // 100 rows 16.9, 17.5, 26.2 here and 21.2, 21.7, 22.6 there; 4 x 16 heads against 512 states 8.3, 9.5, 17.4 and 10.3, 10.5, 11.4;
 // head dimension 128, eight sequences of 4 heads of keys behind 8192, 32 rows 46.4 and 50.1, 96 rows 151 and 51.
@@ -62,7 +64,7 @@ __device__ __forceinline__ float few_exp2(float x) {
 
 // A warp's chunk of keys in shared memory, for 4-bit pages: codes of K and V, their words, and which keys are there.
 template <int DH> struct FewKv4 {
-    static constexpr bool KV4 = true, RANGES = false;
+    static constexpr bool KV4 = true, RANGES = false, SORTED = false;
     static constexpr int WARPS = FEW_WARPS;
     static constexpr float UP = KV4_UP;                     // what scores and results are to be multiplied by
     static __device__ __forceinline__ float down() { return 0.f; }        // taken off the exponents (sum_bits; values below 1 need nothing)
@@ -256,7 +258,7 @@ template <int DH> struct FewBf16 {
 // States of an encoder: all rows see the same keys.
 template <int DH> struct FewStates : FewBf16<DH> {
     using F = FewBf16<DH>;
-    static constexpr bool RANGES = false;
+    static constexpr bool RANGES = false, SORTED = false;
     static constexpr int WARPS = FEW_WARPS;
     static constexpr int KC = F::KC, RB = F::RB, PR = F::PR;
     StateKeys<bf16, DH> K;
@@ -286,8 +288,10 @@ template <int DH> struct FewStates : FewBf16<DH> {
 // Bf16 pages and the rows of packed prompts: the rows of a unit do not all see the same keys, and what a row does not see may be anything.
 template <typename Keys, int DH> struct FewRows : FewBf16<DH> {
     using F = FewBf16<DH>;
-    static constexpr bool RANGES = true;
-    static constexpr int WARPS = 4;                         // (two CTAs to an SM: one merges while the other streams.  With 8 warps the figures at few_split_rows are 178, 176, 170, 199)
+    static constexpr bool RANGES = true, SORTED = Keys::HOLES;         // (of packed prompts no row sees more than a few)
+    // two CTAs to an SM: one merges while the other streams (with eight warps 16 sequences of up to 16384 tokens, 24 heads on 8 x 128, took 178, 176, 170 and
+    // 199 us in 1, 2, 4 and 8 pieces, where few_split_rows has its figures)
+    static constexpr int WARPS = 4;
     static constexpr int KC = F::KC, RB = F::RB, PR = F::PR;
     Keys K;
     typename Keys::Cursor cur;
@@ -351,6 +355,42 @@ template <typename Src, int DH, int NR> struct FewCfg {
     static_assert(SMEM <= 232448 - 1024, "shared memory of a CTA");
 };
 
+// The sequence of place `i` where they go by the tokens that they hold, the longest first: what takes longest begins first.  (For a whole warp; own: room for
+// FEW_SORTED words that nobody else uses.  16 sequences of up to 16384 tokens, 24 heads on 8 x 128, 157 -> 139 us.)
+static __device__ __forceinline__ int few_longest(const BatchD &B, int i, uint32_t *own) {
+    if (B.n_seqs == 1 || B.n_seqs > FEW_SORTED) return i;
+    constexpr int N = FEW_SORTED / 32;
+    const int lane = threadIdx.x & 31;
+    uint32_t word[N];                                       // length (as far as 24 bits go) and sequence: no two alike
+    int most = 0, least = INT_MAX, before[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        word[k] = before[k] = 0;
+        if (k * 32 + lane < B.n_seqs) {
+            const int n = B.tokens(k * 32 + lane);
+            most = max(most, n), least = min(least, n), word[k] = (uint32_t)min(n, 1 << 24) * FEW_SORTED + FEW_SORTED - 1 - (k * 32 + lane);
+        }
+        own[k * 32 + lane] = word[k];
+    }
+    if (__reduce_max_sync(0xffffffffu, most) == __reduce_min_sync(0xffffffffu, least)) return i;
+    __syncwarp();
+#pragma unroll 4
+    for (int j = 0; j < B.n_seqs; j += 4) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(own + j);          // (zeros behind the last)
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (k * 32 < B.n_seqs) before[k] += (w.x > word[k]) + (w.y > word[k]) + (w.z > word[k]) + (w.w > word[k]);
+    }
+    __syncwarp();                                           // (the words may be overwritten)
+    int s = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const uint32_t here = __ballot_sync(0xffffffffu, k * 32 + lane < B.n_seqs && before[k] == i);
+        if (here) s = k * 32 + __ffs(here) - 1;
+    }
+    return s;
+}
+
 // grid: (CTAs of a cluster x heads of keys, sequences, tiles of 8 NR rows).  (States: their ring leaves one CTA to an SM, and so it may have all registers: not
 // told so, the compiler spilled in 80.)
 template <typename Src, int DH, int NR>
@@ -363,7 +403,10 @@ __global__ void __launch_bounds__(32 * Src::WARPS, Src::KV4 ? 0 : Src::RANGES ? 
     extern __shared__ __align__(16) uint8_t few_smem[];
     __shared__ int2 s_range[ROWS];                                                // keys that a row sees
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3, n = lane >> 2;
-    const int rank = blockIdx.x % split, h = blockIdx.x / split, s = blockIdx.y, r0 = blockIdx.z * ROWS;
+    uint8_t *ring = few_smem + warp * F::WARP;
+    int s = blockIdx.y;
+    if constexpr (Src::SORTED) s = few_longest(B, s, reinterpret_cast<uint32_t *>(ring));
+    const int rank = blockIdx.x % split, h = blockIdx.x / split, r0 = blockIdx.z * ROWS;
     const int2 sr = B.rows(s);
     const int len = src.K.length(B, s);
     const int rows = min(sr.y, B.max_rows) * A.share;                             // of the whole unit; row r: row r / share, head h * share + r % share
@@ -373,7 +416,6 @@ __global__ void __launch_bounds__(32 * Src::WARPS, Src::KV4 ? 0 : Src::RANGES ? 
     // (bounds rise with the row, but for rows of tokens below 0, which see nothing: 0, 0)
     const int lo = first.lo, hi = last.hi;
 
-    uint8_t *ring = few_smem + warp * F::WARP;
     const uint32_t ring_s = smem_u32(ring);
     const int step = split * Src::WARPS * KC;
     int next = lo + (rank * Src::WARPS + warp) * KC;                               // next chunk to fill
