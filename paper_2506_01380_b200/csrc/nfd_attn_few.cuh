@@ -24,6 +24,7 @@
 
 #define FEW_WARPS 8
 #define FEW_SORTED 128              // sequences that are taken longest first, at most
+#define FEW_PIECE (768 << 10)       // of a long sequence, at least
 // Rows of a unit that this kernel takes.  Measured against the kernel for many rows, us: 16 heads x 64 behind 5712 tokens in 4-bit pages, 24, 64 and
 // 100 rows 16.9, 17.5, 26.2 here and 21.2, 21.7, 22.6 there; 4 x 16 heads against 512 states 8.3, 9.5, 17.4 and 10.3, 10.5, 11.4;
 // head dimension 128, eight sequences of 4 heads of keys behind 8192, 32 rows 46.4 and 50.1, 96 rows 151 and 51.
@@ -663,12 +664,14 @@ static int few_split(long long units, long long keys, int kc, const int *fit, in
     while (i < 4 && units <= fit[i + 1] && chunks > (long long)(i == 3 ? 48 : 1 << i) * warps) ++i;
     return 1 << i;
 }
-// With bf16 pages and small CTAs (two to an SM) one and two pieces are doubled where they are long: what the device does not hold at once evens out sequences
-// of different lengths.  (One row, 1, 2, 4 and 8 pieces, us: 16 sequences of up to 16384 tokens, 24 heads on 8 x 128, 217, 164, 158, 164; 64 of 4096, 16 heads on 4 x
-// 128, 113, 109, 121, 145, 16 x 64 197, 190, 215, 295.)
-static int few_split_rows(long long units, long long keys, int kc, const int *fit, int warps) {
+// With bf16 pages and small CTAs (two to an SM) up to four pieces are doubled where the halves are still long (FEW_PIECE bytes of K and V): what the device does
+// not hold at once evens out sequences of different lengths.  (One row, 1, 2, 4, 8 and 16 pieces, us.  24 heads on 8 x 128: 16 sequences of up to 16384
+// tokens 217, 164, 139, 164 (8); 8 of up to 32768 409, 223, 162, 139, 158, all as long 416, 231, 217, 217, 250; 5 of up to 16384 207, 115, 80, 64, 78, all
+// as long 211, 117, 90, 102, 94, of 8192 111, 66, 51, 66, 64.  16 heads x 64: 4 of up to 32768 307, 172, 115, 90, 102; 4 of 8192 84, 53, 43, 53, 61; 9 of
+// up to 16384 162, 108, 90, 100, 129, of 8192 88, 76, 84, 82, 109.)
+static int few_split_rows(long long units, long long keys, int kc, int dh, const int *fit, int warps) {
     const int split = few_split(units, keys, kc, fit, warps);
-    return split <= 2 && keys >= 32LL * split * kc * warps ? 2 * split : split;
+    return split <= 4 && keys * dh * 4 >= 2LL * split * FEW_PIECE ? 2 * split : split;
 }
 
 template <typename Src, int DH, int NR>
@@ -687,7 +690,7 @@ static int launch_attn_few_nr(const BatchD &B, const AttnRows &A, const Src &src
         return NFD_E_CUDA;
     const long long tiles = ((long long)B.max_rows * A.share + F::ROWS - 1) / F::ROWS;
     const long long units = (long long)kv_heads * B.n_seqs * tiles;
-    const int split = Src::RANGES ? few_split_rows(units, keys, Src::KC, fit[dev], Src::WARPS) : few_split(units, keys, Src::KC, fit[dev]);
+    const int split = Src::RANGES ? few_split_rows(units, keys, Src::KC, DH, fit[dev], Src::WARPS) : few_split(units, keys, Src::KC, fit[dev]);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kv_heads * split, B.n_seqs, (unsigned)tiles), cfg.blockDim = dim3(32 * Src::WARPS), cfg.dynamicSmemBytes = F::SMEM, cfg.stream = st;
     cudaLaunchAttribute at;
