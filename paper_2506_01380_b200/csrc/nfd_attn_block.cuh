@@ -497,50 +497,61 @@ __device__ __forceinline__ int block_units(int n, int share, int tiles) {
     const int t = (n * share + 127) >> 7;
     return tiles == 1 ? t : tiles == 2 ? (t + 1) >> 1 : (t + 2) / 3;
 }
-// Work item `slot` as (sequence, number of its unit); sequence -1: there is none.  The deepest units of all sequences come first: they
-// see the most keys, and what is dealt out last should be short.  Up to BLOCK_SORTED sequences of different lengths there are as many items as units;
-// otherwise as many as if all sequences had max_rows.
-static __device__ __forceinline__ int2 block_unit(const BatchD &B, int share, int tiles, int slot) {
+// Work item `slot` as (sequence, number of its unit); sequence -1: there is none.  The units that see the most keys come first, since what is dealt out last
+// should be short: a unit's place is its depth in its sequence and, with pages, what the sequence holds before its rows (in units; about, but the same for
+// every CTA).  Up to BLOCK_SORTED sequences there are as many items as units; otherwise, and for prompts of one length, as many as if all had max_rows.
+// (24 sequences of up to 336 rows behind up to 33 frames, 16 heads x 64: 338 us by depth alone, 272 so; 12 of 512 behind up to 15872, 16 on 4 x 128: 377, 287.)
+template <typename Keys> static __device__ __forceinline__ int2 block_unit(const Keys &K, const BatchD &B, int share, int tiles, int slot) {
     const int most = block_units(B.max_rows, share, tiles);
-    if (!B.row_start || B.n_seqs > BLOCK_SORTED) {
+    if (B.n_seqs > BLOCK_SORTED || (!B.row_start && (!Keys::HOLES || B.n_seqs == 1))) {
         const int t = slot / B.n_seqs;
         return make_int2(t < most ? slot - t * B.n_seqs : -1, most - 1 - t);
     }
     const int lane = threadIdx.x & 31;
     constexpr int N = BLOCK_SORTED / 32;
-    int t[N], all = 0;
+    int t[N], at[N], all = 0, lo = INT_MAX, hi = 0;         // a sequence's units, the first one's place
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        t[i] = 0;
-        if (i * 32 < B.n_seqs && i * 32 + lane < B.n_seqs) t[i] = block_units(min(B.rows(i * 32 + lane).y, B.max_rows), share, tiles);
+        t[i] = at[i] = 0;
+        const int s = i * 32 + lane;
+        if (i * 32 < B.n_seqs && s < B.n_seqs) {
+            const int n = B.rows(s).y;
+            t[i] = block_units(min(n, B.max_rows), share, tiles);
+            if constexpr (Keys::HOLES) {
+                const float before = fminf((float)max(K.length(B, s) - n, 0), ((float)K.mask.window + 1.0f) * (float)K.mask.frame_tokens);
+                at[i] = (int)fminf(before * (float)share / (float)(128 * tiles), 268435456.0f);
+            }
+            if (t[i]) lo = min(lo, at[i]), hi = max(hi, at[i] + t[i] - 1);
+        }
         all += t[i];
     }
     if (slot >= (int)__reduce_add_sync(0xffffffffu, (unsigned)all)) return make_int2(-1, 0);
-    // the smallest depth j with no more than `slot` units deeper than it
-    int lo = 0, hi = most - 1;
-    auto deeper = [&](int j) {
+    lo = Keys::HOLES ? __reduce_min_sync(0xffffffffu, lo) : 0, hi = Keys::HOLES ? __reduce_max_sync(0xffffffffu, hi) : most - 1;
+    // the first place j with no more than `slot` units behind it
+    auto behind = [&](int j) {
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) n += max(0, t[i] - 1 - j);
+        for (int i = 0; i < N; ++i) n += min(max(0, at[i] + t[i] - 1 - j), t[i]);
         return (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
     };
     while (lo < hi) {
         const int j = (lo + hi) >> 1;
-        if (deeper(j) <= slot) hi = j;
+        if (behind(j) <= slot) hi = j;
         else lo = j + 1;
     }
-    int left = slot - deeper(lo), s = -1;
+    int left = slot - behind(lo), s = -1, unit = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const uint32_t m = __ballot_sync(0xffffffffu, t[i] > lo);
+        const uint32_t m = __ballot_sync(0xffffffffu, lo >= at[i] && lo - at[i] < t[i]);
         const int n = __popc(m);
         if (s < 0 && left < n) {
             const bool me = (m >> lane & 1) && __popc(m & ((1u << lane) - 1)) == left;
-            s = i * 32 + __ffs(__ballot_sync(0xffffffffu, me)) - 1;
+            const int l = __ffs(__ballot_sync(0xffffffffu, me)) - 1;
+            s = i * 32 + l, unit = lo - __shfl_sync(0xffffffffu, at[i], l);
         }
         left -= n;
     }
-    return make_int2(s, lo);
+    return make_int2(s, unit);
 }
 
 // Grid: items x heads of keys x split (a cluster's CTAs).
@@ -558,7 +569,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
     bars.init(Keys::TMA ? 1 : C::PW, NG);
     if (threadIdx.x == 96) s_expired = 0, s_bad[0] = INT_MAX, s_bad[1] = 0;
     const int slot = hs / kv_heads;
-    const int2 unit = block_unit(B, A.share, tiles, slot);
+    const int2 unit = block_unit(K, B, A.share, tiles, slot);
     if (unit.x < 0) return;                                 // (the whole cluster)
     BlockWork<NG> w;
     w.s = unit.x, w.h = hs - slot * kv_heads;

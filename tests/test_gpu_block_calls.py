@@ -149,6 +149,28 @@ def test_pages_of_every_kind_of_box(page):
             _check_pages("bfloat16", [rows], [1500], 2, 1, dh, page, 1500 // page + 1, 77, 3, seed=page)
 
 
+@pytest.mark.parametrize("seqs", [2, 33, 128, 130])
+@pytest.mark.parametrize("rows", [3, 90])
+def test_sequences_of_any_length_in_any_order(seqs, rows):
+    """What is dealt out longest first reaches every row, with row starts and without, sequences without rows or tokens among them."""
+    torch, N = _mods()
+    rng = np.random.default_rng(seqs + rows)
+    lens = rng.integers(0, 700, seqs)
+    lens[rng.integers(0, seqs, seqs // 3)] = 650
+    n = rng.integers(0, rows + 1, seqs)
+    n[0] = rows
+    _check_pages("bfloat16", list(n), list(lens), 4, 2, 64, 32, 22, 1, EVER, seed=seqs, extra=5)
+    _check_pages("bfloat16", list(n), list(lens), 4, 2, 128, 32, 10, 50, 2, seed=seqs, extra=5, max_rows=rows - 1)
+    g = torch.Generator("cuda").manual_seed(rows)
+    pages = N.Pages(*(torch.randn(22 * seqs, 2, 32, 64, device="cuda", generator=g).bfloat16() for _ in range(2)))
+    q = torch.randn(seqs * rows, 4, 64, device="cuda", generator=g).bfloat16()
+    table, held = torch.randperm(22 * seqs, device="cuda").int().view(seqs, 22), _int(lens)
+    outs = [torch.full((seqs * rows, 256), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    N.attention_pages(pages, N.Batch(seqs * rows, held, table=table), q, outs[0])
+    N.attention_pages(pages, N.Batch(seqs * rows, held, table=table, row_start=_int(np.arange(seqs + 1) * rows), max_rows=rows), q, outs[1])
+    assert torch.equal(*outs)
+
+
 @pytest.mark.parametrize("dh", [32, 64, 128])
 def test_the_same_call_again(dh):
     """Tiles that begin and end in other blocks, groups in turn, pieces: the same bits whenever it runs."""
