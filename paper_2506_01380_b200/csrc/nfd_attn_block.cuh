@@ -16,7 +16,7 @@
 // keeps keys out and not values: 0 x NaN is NaN.  So in blocks that not all rows of a CTA see, the producers take values that are not finite out of V and
 // note where; a row that does see one adds it to its result at the end.
 //
-// Producer warps come first.  Warp 0 fills a ring of K and V blocks in turn by TMA, a lane looking up the place of each box of keys, and the others look
+// Producer warps come first.  One or two of them fill a ring of K and V blocks in turn by TMA, a lane looking up the place of each box of keys, and the others look
 // through values where that is needed; where pages do not consist of boxes (or with head dimension 32) all of them copy by cp.async, a lane looking up the
 // place of each key (four chunks of 512 rows behind 15872, 16 heads on 4 x 128: 380 us so, 246 us by TMA).  The next warp issues the products, the last ones are the softmax
 // groups.  Which keys of a block are there is told beside K, a bit each, in a ring of its own.
@@ -120,6 +120,7 @@ template <int n> __device__ __forceinline__ void leave_registers() { asm volatil
 // Pages: tensor [pages x heads][page_tokens][DH], a box of `rows` keys (a power of two that a page consists of, so that no box crosses its end).
 template <int DH> struct PageBoxes : PageKeys<bf16, DH> {
     static constexpr bool TMA = true;
+    static constexpr int COPIERS = 2;                       // warps that issue copies
     CUtensorMap maps[2];
     int rows;
     __device__ __forceinline__ int box() const { return rows; }
@@ -145,6 +146,7 @@ template <int DH> struct PageBoxes : PageKeys<bf16, DH> {
 // The rows of packed prompts: tensor [rows][heads x DH], a box of a block's keys (what lies behind a sequence's end is the next one's, and masked).
 template <int DH> struct PackedBoxes : PackedKeys<bf16, DH> {
     static constexpr bool TMA = true;
+    static constexpr int COPIERS = 1;
     CUtensorMap maps[2];
     __device__ __forceinline__ int box() const { return BlockCfg<DH>::KB; }
     __device__ __forceinline__ int begin(int lo) const { return lo; }
@@ -168,10 +170,14 @@ __device__ __forceinline__ bool block_take_out(uint8_t *at) {
     *v = make_uint4(x.x & f.x, x.y & f.y, x.z & f.z, x.w & f.w);
     return true;
 }
-// By TMA, one warp: a lane's copy of a block is a box of 64 dims and `box` keys, looked up on the way.
+// By TMA, a warp for K (first 0) and one for V of pages, one for both of packed rows: a lane's copy of a block is a box of 64 dims and `box` keys, looked up on
+// the way.  (An issued box takes some 80 clocks, its operands going into uniform registers one by one; one thread for all of them, by shuffles, was slower
+// still.  Four chunks of 512 rows behind 15872, 16 heads on 4 x 128, in pages of 8, 16 and 64 tokens, by one warp 401, 283, 246 us, by two 258, 248, 246.
+// Packed rows are a box to a block, and look through more values: four prompts of 5376 rows in frames of 336, 16 heads x 64, by one 344, by two 352.)
 template <int DH, typename Keys>
-static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B, const BlockWork<BlockCfg<DH>::NG> &w, uint8_t *smem, const BlockBars &bars, bool &ok) {
+static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B, const BlockWork<BlockCfg<DH>::NG> &w, int first, uint8_t *smem, const BlockBars &bars, bool &ok) {
     using C = BlockCfg<DH>;
+    constexpr int STEP = Keys::COPIERS;                      // every so many items (K and V in turn) are this warp's
     const int lane = threadIdx.x & 31, box = K.box(), groups = C::KB / box, part = lane / groups, group = lane - part * groups;
     const bool mine = part < C::SUB;
     const uint32_t to = smem_u32(smem) + C::AT_R + part * (C::KB * 128) + group * box * 128;
@@ -183,12 +189,11 @@ static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B
         return at;
     };
     int2 next = look_up();
-    int st = 0;
+    int st = first, item = first;
     uint32_t par = 1;                                        // (the first lap waits for nothing)
-    int items = 0;
     for (int b = 0; b < w.nb && ok; ++b) {
         const int2 at = next;
-        if constexpr (Keys::HOLES) {
+        if (Keys::HOLES && first == 0) {
             const uint32_t there = __ballot_sync(0xffffffffu, at.y >= 0);
             uint8_t *M = smem + C::AT_MASK + b % C::NM * 16;
             if (lane < C::KB / 8) M[lane] = there >> (lane * 8 / box) & 1 ? 0xFF : 0;
@@ -197,22 +202,23 @@ static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B
         }
         next = look_up();
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
+        for (int i = 0; i < 2; i += STEP, item += STEP) {
+            const int kv = STEP == 2 ? first : i;
             ok = __all_sync(0xffffffffu, tile_wait(bars.empty(st), par));
             if (!ok) break;
             const uint32_t bar = kv && w.edge(b, C::KB) ? bars.landed(st) : bars.full(st);
             if (lane == 0) mbar_expect_tx(bar, C::BLK);
             __syncwarp();
             if (mine) K.load(kv, to + st * C::BLK, bar, part, w.h, at);
-            if (++st == C::NST) st = 0, par ^= 1;
-            ++items;
+            if ((st += STEP) >= C::NST) st -= C::NST, par ^= 1;
         }
     }
-    // (nobody leaves with copies in flight, whoever has given up waiting)
-    for (int i = max(0, items - C::NST); i < items; ++i) ok = tile_wait(bars.full(i % C::NST), (i / C::NST) & 1) && ok;
+    // Nobody leaves with copies in flight, whoever has given up waiting: of the last NST items, this warp's.  (After a wait that ran out a stage may
+    // have been filled once more by the other warp, its earlier copies having landed before, and its barrier be a phase on: that wait runs out, too.)
+    for (int i = item - STEP; i >= max(0, item - first - C::NST); i -= STEP) ok = tile_wait(bars.full(i % C::NST), (i / C::NST) & 1) && ok;
 }
 // and the other producer warps look through the values of blocks that not all rows see
-template <int DH> static __device__ __forceinline__ void block_look_through(const BlockWork<BlockCfg<DH>::NG> &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
+template <int DH, int COPIERS> static __device__ __forceinline__ void block_look_through(const BlockWork<BlockCfg<DH>::NG> &w, uint8_t *smem, const BlockBars &bars, int *bad, bool &ok) {
     using C = BlockCfg<DH>;
     uint32_t laps = 0;                                       // phases of the stages' barriers
     for (int b = 0; b < w.nb; ++b) {                         // (all of it, whatever runs out: the threads meet at a barrier)
@@ -221,11 +227,11 @@ template <int DH> static __device__ __forceinline__ void block_look_through(cons
         if (ok) ok = tile_wait(bars.landed(st), laps >> st & 1);
         laps ^= 1u << st;
         bool some = false;
-        for (int i = (threadIdx.x - 32) * 16; i < C::BLK; i += (C::PW - 1) * 32 * 16) some |= block_take_out(smem + C::AT_R + st * C::BLK + i);
+        for (int i = (threadIdx.x - 32 * COPIERS) * 16; i < C::BLK; i += (C::PW - COPIERS) * 32 * 16) some |= block_take_out(smem + C::AT_R + st * C::BLK + i);
         if (some) atomicMin(bad, w.lo + b * C::KB), atomicMax(bad + 1, w.lo + b * C::KB + C::KB);
         fence_proxy_async_smem();
-        asm volatile("bar.sync 4, %0;" ::"n"((C::PW - 1) * 32) : "memory");
-        if (threadIdx.x == 32) mbar_arrive(bars.full(st));
+        asm volatile("bar.sync 4, %0;" ::"n"((C::PW - COPIERS) * 32) : "memory");
+        if (threadIdx.x == 32 * COPIERS) mbar_arrive(bars.full(st));
     }
 }
 // By cp.async, all of them.
@@ -643,8 +649,8 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 1) k_attn_block(const BatchD B,
         leave_registers<C::REGS_LOW>();
         if (warp < C::PW) {
             if constexpr (Keys::TMA) {
-                if (warp == 0) block_copy<DH>(K, B, w, smem, bars, ok);
-                else block_look_through<DH>(w, smem, bars, s_bad, ok);
+                if (warp < Keys::COPIERS) block_copy<DH>(K, B, w, warp, smem, bars, ok);
+                else block_look_through<DH, Keys::COPIERS>(w, smem, bars, s_bad, ok);
             } else {
                 if (w.nb) block_produce<DH>(K, B, w, smem, bars, s_bad, ok);
             }
