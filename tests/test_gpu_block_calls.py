@@ -114,6 +114,21 @@ def test_a_step_without_rows():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+def test_fewer_rows_than_a_block_has_keys(dh):
+    """Tensors smaller than the boxes that are copied."""
+    torch, N = _mods()
+    for rows in (9, 50):
+        q, k, v = (torch.randn(rows, h, dh, device="cuda").bfloat16() for h in (32, 1, 1))
+        out = torch.zeros(rows, 32 * dh, device="cuda", dtype=torch.bfloat16)
+        N.attention_packed(N.Batch(rows, n_seqs=1), q, k, v, out)
+        s = torch.einsum("ihd,jgd->hij", q.double(), k.double()) / dh ** 0.5
+        s.masked_fill_(torch.ones(rows, rows, device="cuda").triu(1).bool(), -torch.inf)
+        want = torch.einsum("hij,jgd->ihd", s.softmax(-1), v.double()).reshape(rows, -1)
+        # (P's rounding and the result's, half a step of bf16 each of at most the largest value, and as much again for exponentials and sums)
+        assert (out.double() - want).abs().max() <= 4 * 2.0 ** -8 * v.abs().max()
+
+
 def test_rows_far_apart():
     """Strides that take the rows beyond 2^32 bytes."""
     torch, N = _mods()
