@@ -173,7 +173,7 @@ __device__ __forceinline__ bool block_take_out(uint8_t *at) {
 // By TMA, a warp for K (first 0) and one for V of pages, one for both of packed rows: a lane's copy of a block is a box of 64 dims and `box` keys, looked up on
 // the way.  (An issued box takes some 80 clocks, its operands going into uniform registers one by one; one thread for all of them, by shuffles, was slower
 // still.  Four chunks of 512 rows behind 15872, 16 heads on 4 x 128, in pages of 8, 16 and 64 tokens, by one warp 401, 283, 246 us, by two 258, 248, 246.
-// Packed rows are a box to a block, and look through more values: four prompts of 5376 rows in frames of 336, 16 heads x 64, by one 344, by two 352.)
+// Packed rows are a box to a block, which one thread copies (two prompts of 8192, 467 us by two lanes, 461 so), and look through more values: four prompts of 5376 rows in frames of 336, 16 heads x 64, by one 344, by two 352.)
 template <int DH, typename Keys>
 static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B, const BlockWork<BlockCfg<DH>::NG> &w, int first, uint8_t *smem, const BlockBars &bars, bool &ok) {
     using C = BlockCfg<DH>;
@@ -207,9 +207,20 @@ static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B
             ok = __all_sync(0xffffffffu, tile_wait(bars.empty(st), par));
             if (!ok) break;
             const uint32_t bar = kv && w.edge(b, C::KB) ? bars.landed(st) : bars.full(st);
-            if (lane == 0) mbar_expect_tx(bar, C::BLK);
-            __syncwarp();
-            if (mine) K.load(kv, to + st * C::BLK, bar, part, w.h, at);
+            if constexpr (Keys::HOLES) {
+                if (lane == 0) mbar_expect_tx(bar, C::BLK);
+                __syncwarp();
+                if (mine) K.load(kv, to + st * C::BLK, bar, part, w.h, at);
+            } else {
+                // (one box: its place is the same in all lanes, and one thread copies it)
+                const uint32_t dst = __shfl_sync(0xffffffffu, to, 0) + st * C::BLK;
+                const int2 from = make_int2(__shfl_sync(0xffffffffu, at.x, 0), 0);
+                if (elect_one()) {
+                    mbar_expect_tx(bar, C::BLK);
+#pragma unroll
+                    for (int half = 0; half < C::SUB; ++half) K.load(kv, dst + half * (C::KB * 128), bar, half, w.h, from);
+                }
+            }
             if ((st += STEP) >= C::NST) st -= C::NST, par ^= 1;
         }
     }
