@@ -25,9 +25,9 @@
 // shared memory in a fixed order.  Every wait on a barrier in memory is bounded; after one that ran out the rows are NaN.  (The cluster's own barrier needs
 // no bound: every CTA comes to it, its other waits being bounded, or has left as a whole cluster.)
 //
-// What bounds it.  With head dimension 128 the tensor pipe: two causal prompts of 8192 rows, 16 heads on 4, take 457 us alone (1200 TFLOP/s) and 536 us after
-// many of their kind, when the clock has fallen (1030).  With 64 a block is 10 short products, which their one thread issues in 600 to 700 clocks, and the
-// chain S, P, O of each group (four prompts of 5376 rows in frames of 336, 16 heads: 336 us; the exponentials alone would take 211): hence three groups there,
+// What bounds it.  With head dimension 128 the tensor pipe: two causal prompts of 8192 rows, 16 heads on 4, take 461 us alone (1190 TFLOP/s) and 541 us after
+// many of their kind, when the clock has fallen (1020).  With 64 a block is 10 short products, which their one thread issues in 600 to 700 clocks, and the
+// chain S, P, O of each group (four prompts of 5376 rows in frames of 336, 16 heads: 344 us; the exponentials alone would take 211): hence three groups there,
 // whose chains overlap; with 128 tensor memory holds two.  Groups with an issuing thread each, or that wait for their turn at the pipes, were slower.
 // Short prompts are their CTAs' beginning (5 to 7 thousand clocks) and end (5).
 #pragma once
@@ -173,7 +173,8 @@ __device__ __forceinline__ bool block_take_out(uint8_t *at) {
 // By TMA, a warp for K (first 0) and one for V of pages, one for both of packed rows: a lane's copy of a block is a box of 64 dims and `box` keys, looked up on
 // the way.  (An issued box takes some 80 clocks, its operands going into uniform registers one by one; one thread for all of them, by shuffles, was slower
 // still.  Four chunks of 512 rows behind 15872, 16 heads on 4 x 128, in pages of 8, 16 and 64 tokens, by one warp 401, 283, 246 us, by two 258, 248, 246.
-// Packed rows are a box to a block, which one thread copies (two prompts of 8192, 467 us by two lanes, 461 so), and look through more values: four prompts of 5376 rows in frames of 336, 16 heads x 64, by one 344, by two 352.)
+// Packed rows are a box to a block, which one thread copies (two prompts of 8192, 467 us by two lanes, 461 so), and look through more values: four prompts
+// of 5376 rows in frames of 336, 16 heads x 64, by one warp 344, by two 352.)
 template <int DH, typename Keys>
 static __device__ __forceinline__ void block_copy(const Keys &K, const BatchD &B, const BlockWork<BlockCfg<DH>::NG> &w, int first, uint8_t *smem, const BlockBars &bars, bool &ok) {
     using C = BlockCfg<DH>;
