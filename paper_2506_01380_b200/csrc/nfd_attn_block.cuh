@@ -456,11 +456,13 @@ __device__ __forceinline__ float2 flush2(float2 a) {
     asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(rd));
     return d;
 }
-// 2^x of two numbers on the fp32 pipes: x = n + f with n whole, a polynomial of degree 3 in f (fitted for the least relative error on [-1/2, 1/2], 1.0e-4; P
-// is rounded to bf16, 2^-9 = 2e-3, anyway), n added to the exponent.  Below 2^-125 it is 2^-125.
-__device__ __forceinline__ float2 block_exp2_poly(float2 x) {
+// 2^x, x = s c - mc, of two numbers on the fp32 pipes: x = n + f with n whole, a polynomial of degree 3 in f (fitted for the least relative error on [-1/2, 1/2],
+// 1.0e-4; P is rounded to bf16, 2^-9 = 2e-3, anyway), n added to the exponent.  Below 2^-125 it is 2^-125.  From 2^127 on, and of NaN, it is 2^127, so that
+// the part's sum has outgrown m (added to a larger n the exponent would wrap into the sign): fminf first, which takes NaN to its limit.
+__device__ __forceinline__ float2 block_exp2_poly(float2 s, float c, float mc) {
     const float magic = 12582912.0f;                                   // 1.5 x 2^23: an ulp is 1
-    x.x = fmaxf(x.x, -127.4f), x.y = fmaxf(x.y, -127.4f);
+    float2 x = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
+    x.x = fmaxf(fminf(x.x, 127.0f), -127.4f), x.y = fmaxf(fminf(x.y, 127.0f), -127.4f);
     const float2 t = fadd2(x, make_float2(magic, magic)), n = fadd2(t, make_float2(-magic, -magic));
     const float2 f = ffma2(n, make_float2(-1.0f, -1.0f), x);
     float2 p = ffma2(f, make_float2(0.05517166852951050f, 0.05517166852951050f), make_float2(0.2426111251115799f, 0.2426111251115799f));
@@ -477,7 +479,7 @@ template <bool MASKED> __device__ __forceinline__ void block_exp16(const float *
         float2 s = make_float2(x[2 * u], x[2 * u + 1]);
         if (MASKED) s.x = bits >> (2 * u) & 1 ? s.x : -INFINITY, s.y = bits >> (2 * u + 1) & 1 ? s.y : -INFINITY;
         const float2 e = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
-        const float2 p = !MASKED && ((u + 1) * BLOCK_POLY / 8 != u * BLOCK_POLY / 8) ? block_exp2_poly(e) : make_float2(few_exp2(e.x), few_exp2(e.y));
+        const float2 p = !MASKED && ((u + 1) * BLOCK_POLY / 8 != u * BLOCK_POLY / 8) ? block_exp2_poly(s, c, mc) : make_float2(few_exp2(e.x), few_exp2(e.y));
         ls[u & 1] = fadd2(ls[u & 1], p);
         pk[u] = bf16_pair(p.x, p.y);
     }

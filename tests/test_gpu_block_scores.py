@@ -1,0 +1,81 @@
+"""Scores far apart in the attention of many rows to bf16 keys, against the 64-bit oracle: one key far above or below the others, at each place of the
+sixteen columns that are taken at a time; a key that is not a number.
+
+Bounds: as in test_gpu_block.py, with 1.2e-4 more of a probability for those exponentials that are polynomials (1.0e-4, and 1.6e-5 of their arguments).
+"""
+import numpy as np
+import pytest
+
+from oracle import block_oracle as O
+from test_gpu_block import EVER, HALF, _batch, _int, _mods, _randn, _smax
+
+pytestmark = pytest.mark.gpu
+
+PLACES = 16                                                # a head of keys each
+ABOVE = [60, 120, 130, 150, 170, 185, 250, 330, 390]       # a sequence each, the score, of which probabilities are the exponential
+CALLS = [("boxes", 1, 150), ("boxes", 1, 400), ("boxes", 4, 40), ("odd pages", 1, 150), ("odd pages", 4, 110), ("packed", 1, 0), ("packed", 2, 0)]
+POLY = 1.2e-4
+
+
+def _close(got, want, mag, smax, n, dh):
+    torch, _ = _mods()
+    e = (dh + 4) * 2.0 ** -23 * smax + 2.0 ** -21 + POLY
+    bound = (2 * e + n * 2.0 ** -23 + 1.01 * HALF) * mag + 1.01 * HALF * want.abs() + 1e-30
+    nan = want.isnan()
+    assert torch.equal(got.isnan(), nan)
+    assert ((got.double() - want).abs() <= bound)[~nan].all(), torch.where(nan, 0.0, (got.double() - want).abs() - bound).max().item()
+
+
+def _check(kind, dh, share, rows, length, poke, n_seqs, window=EVER, seed=0):
+    """n_seqs sequences of `length` tokens, PLACES heads of keys; the rows are the last `rows` of them (packed: all).  poke(q, k, v) has q [seqs, rows, heads of
+    keys, share, dh] and k, v [seqs, length, heads of keys, dh] with ordinary numbers in them."""
+    torch, N = _mods()
+    g = torch.Generator("cuda").manual_seed(seed)
+    rows = length if kind == "packed" else rows
+    q = _randn(g, n_seqs, rows, PLACES, share, dh, dtype=torch.float32) * 0.3
+    k = _randn(g, n_seqs, length, PLACES, dh, dtype=torch.float32) * 0.3
+    v = _randn(g, n_seqs, length, PLACES, dh, dtype=torch.float32)
+    poke(q, k, v)
+    q, k, v = q.flatten(2, 3).bfloat16(), k.bfloat16(), v.bfloat16()
+    out = torch.full((n_seqs * rows, PLACES * share * dh), 7.0, device="cuda", dtype=torch.bfloat16)
+    if kind == "packed":
+        b, _, _ = _batch([rows] * n_seqs)
+        N.attention_packed(b, q.flatten(0, 1), k.flatten(0, 1), v.flatten(0, 1), out, window=window)
+    else:
+        page = 64 if kind == "boxes" else 50
+        per = -(-length // page)
+        table = torch.randperm(n_seqs * per, generator=g, device="cuda").view(n_seqs, per)
+        pages = []
+        for t in (k, v):
+            t = torch.nn.functional.pad(t, (0, 0, 0, 0, 0, per * page - length)).unflatten(1, (per, page)).transpose(2, 3)
+            p = torch.empty(n_seqs * per, PLACES, page, dh, device="cuda", dtype=torch.bfloat16)
+            p[table.flatten()] = t.flatten(0, 1)
+            pages.append(p)
+        b, _, _ = _batch([rows] * n_seqs, [length] * n_seqs, table.int())
+        N.attention_pages(N.Pages(*pages), b, q.flatten(0, 1), out, window=window)
+    got = out.view(n_seqs, rows, PLACES * share, dh)
+    seen = O.seen_tokens(rows, length, 1, window)
+    for s in range(n_seqs):
+        want, mag = O.attend(q[s], k[s], v[s], seen)
+        _close(got[s], want, mag, _smax(q[s], k[s]), length, dh)
+
+
+def _lone(above):
+    """Key 288 + place (in the middle of the blocks; their columns are tokens modulo 16) `above` over the others, with a value of its own."""
+    def poke(q, k, v):
+        dh = q.shape[-1]
+        q[..., 0], k[..., 0] = 16.0, 0.0
+        for s, a in enumerate(above):
+            for place in range(PLACES):
+                k[s, 288 + place, place, 0] = a * dh ** 0.5 / 16
+        v[:, 288:304] = 5.0
+    return poke
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("kind,share,rows", CALLS)
+def test_one_key_far_above_the_others(kind, dh, share, rows):
+    """A call of all of them, and (keys split over clusters) of one sequence at a time."""
+    _check(kind, dh, share, rows, 800, _lone(ABOVE), len(ABOVE))
+    for a in ABOVE if share == 1 else ABOVE[3:4]:
+        _check(kind, dh, share, rows, 1500, _lone([a]), 1)
