@@ -457,17 +457,19 @@ __device__ __forceinline__ float2 flush2(float2 a) {
     return d;
 }
 // 2^x, x = s c - mc, of two numbers on the fp32 pipes: x = n + f with n whole, a polynomial of degree 3 in f (fitted for the least relative error on [-1/2, 1/2],
-// 1.0e-4; P is rounded to bf16, 2^-9 = 2e-3, anyway), n added to the exponent.  Below 2^-125 it is 2^-125.  From 2^127 on, and of NaN, it is 2^127, so that
-// the part's sum has outgrown m (added to a larger n the exponent would wrap into the sign): fminf first, which takes NaN to its limit.
+// 1.0e-4; P is rounded to bf16, 2^-9 = 2e-3, anyway), n added to the exponent, which must not leave its field.  So x is formed as 127 - 253.4 u with u cut off
+// at 0 and 1 by the instruction that makes it (two minima and maxima in its place cost 2 % of a call): below 2^-126 the result is 0, and from 2^127 on, and of
+// NaN, whose u is 0, it is 2^127, so that the part's sum has outgrown m.  The steps of u are 1.5e-5 of x.  p has 2^127 in its coefficients, n is counted from there.
 __device__ __forceinline__ float2 block_exp2_poly(float2 s, float c, float mc) {
-    const float magic = 12582912.0f;                                   // 1.5 x 2^23: an ulp is 1
-    float2 x = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
-    x.x = fmaxf(fminf(x.x, 127.0f), -127.4f), x.y = fmaxf(fminf(x.y, 127.0f), -127.4f);
-    const float2 t = fadd2(x, make_float2(magic, magic)), n = fadd2(t, make_float2(-magic, -magic));
-    const float2 f = ffma2(n, make_float2(-1.0f, -1.0f), x);
-    float2 p = ffma2(f, make_float2(0.05517166852951050f, 0.05517166852951050f), make_float2(0.2426111251115799f, 0.2426111251115799f));
-    p = ffma2(p, f, make_float2(0.6932609677314758f, 0.6932609677314758f));
-    p = ffma2(p, f, make_float2(0.9999280571937561f, 0.9999280571937561f));
+    constexpr float top = 127.0f, range = 253.4f;                      // (127 - 253.4 = -126 - 0.4: n = -126, p < 1, a subnormal number)
+    const float magic = 12582912.0f, one = 1.7014118346046923e38f;     // 1.5 x 2^23: an ulp is 1; 2^127
+    const float k = c * (-1.0f / range), a = fmaf(mc, 1.0f / range, top / range);
+    const float2 u = make_float2(__saturatef(fmaf(s.x, k, a)), __saturatef(fmaf(s.y, k, a)));
+    const float2 t = ffma2(u, make_float2(-range, -range), make_float2(magic, magic)), n = ffma2(t, make_float2(-1.0f, -1.0f), make_float2(magic, magic));
+    const float2 f = ffma2(u, make_float2(-range, -range), n);         // (n: the whole part's negative)
+    float2 p = ffma2(f, make_float2(0.05517166852951050f * one, 0.05517166852951050f * one), make_float2(0.2426111251115799f * one, 0.2426111251115799f * one));
+    p = ffma2(p, f, make_float2(0.6932609677314758f * one, 0.6932609677314758f * one));
+    p = ffma2(p, f, make_float2(0.9999280571937561f * one, 0.9999280571937561f * one));
     p = make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
     return flush2(p);
 }

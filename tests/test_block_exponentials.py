@@ -69,3 +69,11 @@ def test_above_its_range_a_sum_cannot_pass_for_a_small_one(exp2):
                                                         np.inf, np.nan]])
     y = exp2(x)
     assert not (y < 2.0 ** 126).any(), x[(y < 2.0 ** 126).any(1)]
+
+
+def test_below_its_range_it_is_nothing(exp2):
+    """Not a number that sends the warp to its keys again, nor one that counts beside large values."""
+    x = np.concatenate([np.linspace(-600, -126, 100001), [-126.4, -126.5, -127, -127.4, -127.5, -128, -129, -150, -253, -256, -383, -500, -1e5, -4194304, -1.3e7, -1e30,
+                                                          -3e38, -np.inf]])
+    y = exp2(x)
+    assert ((y >= 0) & (y <= 2.0 ** -126)).all() and (y[x < -126.1] == 0).all()

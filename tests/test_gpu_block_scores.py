@@ -79,3 +79,40 @@ def test_one_key_far_above_the_others(kind, dh, share, rows):
     _check(kind, dh, share, rows, 800, _lone(ABOVE), len(ABOVE))
     for a in ABOVE if share == 1 else ABOVE[3:4]:
         _check(kind, dh, share, rows, 1500, _lone([a]), 1)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("kind,share,rows", CALLS)
+def test_a_first_key_far_above_the_others(kind, dh, share, rows):
+    """What a first token that takes most of the weight leaves the rest: 200 and 60 above, and 45, where theirs is still in the sums; beside the largest values there are, which
+    must not show where their probability is nothing."""
+    above = [200.0, 60.0, 45.0]
+
+    def poke(q, k, v):
+        q[..., 0], k[..., 0] = 16.0, 0.0
+        for s, a in enumerate(above):
+            k[s, 0, :, 0] = a * dh ** 0.5 / 16
+        v[0, 290:420:3] = 3e38
+        v[0, 291:420:3] = -3e38
+    _check(kind, dh, share, rows, 800, poke, len(above))
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("kind,share,rows", CALLS)
+def test_scores_spread_over_a_hundred(kind, dh, share, rows):
+    def poke(q, k, v):
+        q *= 10
+        k *= 10
+    _check(kind, dh, share, rows, 800, poke, 3)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("kind,share,rows", CALLS)
+def test_a_seen_key_that_is_not_a_number(kind, dh, share, rows):
+    """In one place of sixteen for each head, in a block that all rows of a tile see and in one that some do: the rows that see it are NaN, and no others."""
+    def poke(q, k, v):
+        for place in range(PLACES):
+            k[0, 288 + place, place, 3] = float("nan")
+            k[1, 740 + place, place, 3] = float("nan")
+    _check(kind, dh, share, rows, 800, poke, 3)
+    _check(kind, dh, share, rows, 800, poke, 3, window=400)
