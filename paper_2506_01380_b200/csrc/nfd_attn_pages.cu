@@ -7,7 +7,7 @@
 namespace {
 
 // Attention of a batch's rows to keys under the block-wise causal mask, of the rows' type: by what their number and type ask for.  keys: the most that
-// a row's unit can see.
+// the rows of a sequence can see, all together.
 template <template <typename, int> class Keys, typename Make>
 int launch_rows(const BatchD &B, const AttnRows &A, int dtype, int head_dim, int kv_heads, long long keys, Make &&make, cudaStream_t st) {
     int dev = 0, n_sm = 0;
@@ -41,11 +41,6 @@ struct MakePackedKeys {
 };
 
 int check_mask(int frame_tokens, int window) { return frame_tokens < 1 || frame_tokens > (1 << 20) || window < 0 ? NFD_E_RANGE : NFD_OK; }
-// keys that the rows of a sequence of up to `held` tokens can see, all together
-long long most_keys(long long held, int frame_tokens, int window, int rows) {
-    const long long seen = ((long long)window + 1) * frame_tokens + rows;
-    return held < seen ? held : seen;
-}
 
 }  // namespace
 
@@ -66,7 +61,7 @@ int nfd_attention_pages(const nfd_pages *pages, const nfd_batch *batch, int n_he
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
     const AttnRows A = {q, out, q_stride, n_heads, n_heads / P.heads};
     const long long held = (long long)B.table_len * P.page_tokens, most = held < NFD_MAX_TOKENS ? held : NFD_MAX_TOKENS;
-    return launch_rows<PageKeys>(B, A, pages->dtype, pages->head_dim, P.heads, most_keys(most, frame_tokens, window, B.max_rows),
+    return launch_rows<PageKeys>(B, A, pages->dtype, pages->head_dim, P.heads, keys_seen(most, frame_tokens, window, B.max_rows),
                                  MakePageKeys{P, {frame_tokens, window}}, (cudaStream_t)cuda_stream);
 }
 
@@ -87,7 +82,7 @@ int nfd_attention_packed(const nfd_batch *batch, int dtype, int n_heads, int kv_
     if (B.n_rows == 0 || B.max_rows == 0) return NFD_OK;
     const AttnRows A = {q, out, q_stride, n_heads, n_heads / kv_heads};
     // (a sequence may have more rows than are computed, and these may see them: the rest of a frame)
-    return launch_rows<PackedKeys>(B, A, dtype, head_dim, kv_heads, most_keys(B.n_rows, frame_tokens, window, B.max_rows),
+    return launch_rows<PackedKeys>(B, A, dtype, head_dim, kv_heads, prompt_keys_seen(B.n_rows, frame_tokens, window, B.max_rows),
                                    MakePackedKeys{k, v, k_stride, v_stride, {frame_tokens, window}}, (cudaStream_t)cuda_stream);
 }
 

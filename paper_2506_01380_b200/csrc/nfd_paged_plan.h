@@ -14,6 +14,18 @@ NFD_HD RowSpan rows_between(int start, int end, int n_rows) {
     return {a, b > a ? b - a : 0};
 }
 
+// Keys that `rows` (one at least) tokens of a sequence, one behind the other, see under the block-wise causal mask, all together: those of the frames that the rows
+// lie in (of as many as they can touch) and of `window` before, of `held` that there are.
+NFD_HD long long keys_seen(long long held, int frame_tokens, int window, int rows) {
+    const long long frames = (rows + (long long)frame_tokens - 2) / frame_tokens + 1, span = (window + frames) * frame_tokens;
+    return held < span ? held : span;
+}
+// The same of a prompt's first `rows` rows, whose tokens begin at 0, in a buffer of n_rows: none sees further than the end of its frame, whatever other prompts there are.
+NFD_HD long long prompt_keys_seen(int n_rows, int frame_tokens, int window, int rows) {
+    const long long end = ((long long)rows + frame_tokens - 1) / frame_tokens * frame_tokens;
+    return keys_seen(n_rows < end ? n_rows : end, frame_tokens, window, rows);
+}
+
 // Probabilities of states are formed 2^-bits of their size: with a reference m of a row that may be short of its largest score, n of them of up to
 // 2^growth have a sum of 1 at most then, so that O, a sum of values times them, is no larger than the largest value and leaves fp32 for no
 // finite one; the quotient of O and the sum does not know of it.  (What it costs is at the other end: small values

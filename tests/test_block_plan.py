@@ -1,0 +1,60 @@
+"""Arithmetic of the calls around a block's projections (csrc/nfd_paged_plan.h), on the CPU."""
+import ctypes as C
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SOURCE = r"""
+#include "nfd_paged_plan.h"
+extern "C" long long seen(long long held, int frame_tokens, int window, int rows) { return keys_seen(held, frame_tokens, window, rows); }
+extern "C" long long prompt(int n_rows, int frame_tokens, int window, int rows) { return prompt_keys_seen(n_rows, frame_tokens, window, rows); }
+"""
+LAST = (1 << 31) - 1
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    d = tmp_path_factory.mktemp("block")
+    (d / "plan.cpp").write_text(SOURCE)
+    subprocess.run([shutil.which("g++") or "g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-fsanitize=undefined", "-fno-sanitize-recover", "-I",
+                    os.path.join(ROOT, "paper_2506_01380_b200", "csrc"), "-o", str(d / "plan.so"), str(d / "plan.cpp")], check=True)
+    lib = C.CDLL(str(d / "plan.so"))
+    lib.seen.restype, lib.seen.argtypes = C.c_longlong, [C.c_longlong] + 3 * [C.c_int]
+    lib.prompt.restype, lib.prompt.argtypes = C.c_longlong, 4 * [C.c_int]
+    return lib
+
+
+def _span(first, rows, frame, window, length):
+    """Keys from the first that token `first` sees to the last that token first + rows - 1 of a sequence of `length` sees."""
+    last = first + rows - 1
+    return min(length, (last // frame + 1) * frame) - max(0, first // frame - window) * frame
+
+
+def test_keys_that_a_chunk_sees(lib):
+    """The most over all places of the chunk: no less, or a plan would be for fewer keys than there are, and no more than are held."""
+    for frame in (1, 2, 3, 7, 50, 77):
+        for window in (0, 1, 2, 9):
+            for rows in (1, 2, 3, 8, 50, 51, 76, 77, 78, 79, 200):
+                span = max(_span(p, rows, frame, window, 10 ** 6) for p in range(20 * frame, 21 * frame))
+                assert lib.seen(10 ** 6, frame, window, rows) == span, (frame, window, rows)
+                assert lib.seen(span - 1, frame, window, rows) == span - 1
+    assert lib.seen(1 << 30, 1 << 20, LAST, 1 << 30) == 1 << 30 and lib.seen(1 << 60, 1 << 20, LAST, 1) == 1 << 51
+
+
+def test_keys_that_a_prompt_sees(lib):
+    """Of one prompt, however many there are in the batch; of one whose first rows only are computed, to the end of their frame."""
+    for frame in (1, 2, 7, 77, 500):
+        for window in (0, 1, 5, LAST):
+            for length in (1, 2, 6, 7, 8, 153, 154, 155, 400):
+                for rows in {1, 2, length // 2 or 1, length}:
+                    if rows > length:
+                        continue
+                    most = max(_span(p, 1, frame, window, length) for p in range(rows))
+                    for others in (0, 1, 100000):
+                        got = lib.prompt(length + others, frame, window, rows)
+                        assert most <= _span(0, rows, frame, window, length) <= got <= length + others
+                        assert got <= -(-rows // frame) * frame and got <= (window + (rows + frame - 2) // frame + 1) * frame
+    assert lib.prompt(1353, 1, LAST, 200) == 200 and lib.prompt(1 << 30, 1 << 20, LAST, 1 << 30) == 1 << 30
