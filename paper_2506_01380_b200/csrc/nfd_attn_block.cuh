@@ -1014,7 +1014,9 @@ static int launch_attn_block(const BatchD &B, const AttnRows &A, const Keys &K, 
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension, at.val.clusterDim.x = pl.split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at, cfg.numAttrs = pl.split > 1;
-    const float down = (float)sum_bits(BLOCK_GROWTH, (int)((keys + C::HK - 1) / C::HK));
+    // the parts that a row's keys are in, each of which may grow: the first key may lie anywhere in one (a window's, a ring's oldest, in boxes of a page)
+    const long long row_keys = ((long long)K.mask.window + 1) * K.mask.frame_tokens;
+    const float down = (float)sum_bits(BLOCK_GROWTH, parts_touched(keys < row_keys ? keys : row_keys, C::HK));
     FastDiv by_share;
     by_share.set(A.share);
     if (cudaLaunchKernelEx(&cfg, kern, B, A, K, kv_heads, pl.split, pl.tiles, by_share, down) != cudaSuccess) {

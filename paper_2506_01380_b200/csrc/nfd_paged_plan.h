@@ -25,6 +25,8 @@ NFD_HD long long prompt_keys_seen(int n_rows, int frame_tokens, int window, int 
     const long long end = ((long long)rows + frame_tokens - 1) / frame_tokens * frame_tokens;
     return keys_seen(n_rows < end ? n_rows : end, frame_tokens, window, rows);
 }
+// Parts of so many keys that a run of `keys` touches, wherever in a part it begins.
+NFD_HD int parts_touched(long long keys, int part) { return keys < 2 ? (int)keys : (int)((keys - 2) / part) + 2; }
 
 // Probabilities of states are formed 2^-bits of their size: with a reference m of a row that may be short of its largest score, n of them of up to
 // 2^growth have a sum of 1 at most then, so that O, a sum of values times them, is no larger than the largest value and leaves fp32 for no

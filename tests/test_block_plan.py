@@ -11,6 +11,7 @@ SOURCE = r"""
 #include "nfd_paged_plan.h"
 extern "C" long long seen(long long held, int frame_tokens, int window, int rows) { return keys_seen(held, frame_tokens, window, rows); }
 extern "C" long long prompt(int n_rows, int frame_tokens, int window, int rows) { return prompt_keys_seen(n_rows, frame_tokens, window, rows); }
+extern "C" int parts(long long keys, int part) { return parts_touched(keys, part); }
 """
 LAST = (1 << 31) - 1
 
@@ -24,6 +25,7 @@ def lib(tmp_path_factory):
     lib = C.CDLL(str(d / "plan.so"))
     lib.seen.restype, lib.seen.argtypes = C.c_longlong, [C.c_longlong] + 3 * [C.c_int]
     lib.prompt.restype, lib.prompt.argtypes = C.c_longlong, 4 * [C.c_int]
+    lib.parts.argtypes = [C.c_longlong, C.c_int]
     return lib
 
 
@@ -58,3 +60,11 @@ def test_keys_that_a_prompt_sees(lib):
                         assert most <= _span(0, rows, frame, window, length) <= got <= length + others
                         assert got <= -(-rows // frame) * frame and got <= (window + (rows + frame - 2) // frame + 1) * frame
     assert lib.prompt(1353, 1, LAST, 200) == 200 and lib.prompt(1 << 30, 1 << 20, LAST, 1 << 30) == 1 << 30
+
+
+def test_parts_that_keys_touch(lib):
+    for part in (1, 2, 64, 96):
+        for keys in (0, 1, 2, 3, 63, 64, 65, 66, 96, 97, 98, 500):
+            most = max(len({(a + i) // part for i in range(keys)}) for a in range(part))
+            assert lib.parts(keys, part) == most, (keys, part)
+    assert lib.parts(1 << 30, 64) == (1 << 24) + 1

@@ -116,3 +116,37 @@ def test_a_seen_key_that_is_not_a_number(kind, dh, share, rows):
             k[1, 740 + place, place, 3] = float("nan")
     _check(kind, dh, share, rows, 800, poke, 3)
     _check(kind, dh, share, rows, 800, poke, 3, window=400)
+
+
+@pytest.mark.parametrize("dh,part,page,pages,rows", [(128, 64, 64, 4, 40), (64, 96, 32, 12, 80), (32, 96, 32, 12, 80)])
+@pytest.mark.parametrize("share", [1, 4])
+def test_sums_that_have_grown_in_every_part_stay_finite(dh, part, page, pages, rows, share):
+    """What a sum may grow by before its reference follows, in each part of a row's keys, which a ring of pages has begin inside one: keys of a power of two of
+    parts, in one part more.  The values are as large as they go, and so is their mean."""
+    torch, N = _mods()
+    held, shift = page * pages, 8
+    length = held + shift
+    growth = torch.zeros(length, dtype=torch.float64)
+    for a in range(0, length, part):
+        growth[a + 16:a + part] = 50 - np.log2(part - 16) - 0.02       # (the first sixteen are the reference where it is the row's first part)
+    growth[held:] = 50 - np.log2(shift) - 0.02
+    c = np.log2(np.e) / np.sqrt(dh)
+    score = growth / c                                                 # as 2 k0 + k1 / 16, of bf16 numbers
+    k0 = (score / 2).floor()
+    kk = torch.zeros(length, 1, dh, dtype=torch.float64)
+    kk[:, 0, 0], kk[:, 0, 1] = k0.bfloat16().double(), ((score - 2 * k0.bfloat16().double()) * 16).bfloat16().double()
+    big = torch.finfo(torch.bfloat16).max * 0.99
+    kk, vv = kk.bfloat16().cuda(), torch.full((length, 1, dh), big, device="cuda").bfloat16()
+    k, v = (torch.zeros(pages, 1, page, dh, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    t = np.arange(length)[shift:]
+    k[t // page % pages, :, t % page], v[t // page % pages, :, t % page] = kk[shift:], vv[shift:]
+    q = torch.zeros(rows, share, dh, device="cuda", dtype=torch.bfloat16)
+    q[..., 0], q[..., 1] = 2.0, 1 / 16
+    out = torch.zeros(rows, share * dh, device="cuda", dtype=torch.bfloat16)
+    b, _, _ = _batch([rows], [length], _int(np.arange(pages)[None]))
+    N.attention_pages(N.Pages(k, v), b, q, out)
+    got = out.view(rows, share, dh)
+    want, mag = O.attend(q, kk[shift:], vv[shift:], O.seen_tokens(rows, length, 1, EVER)[:, shift:])
+    s = 2.0 ** -100
+    assert torch.isfinite(got).all()
+    _close(got.double() * s, want * s, mag * s, _smax(q, kk), length, dh)
