@@ -380,7 +380,7 @@ int nfd_rotate(const nfd_rope *rope, int flags, int dtype, int head_dim, int n_r
  * block's projection gave) and h (the next projection's operand; may be y) of `dtype`, both
  * NFD_DTYPE_FP32 or NFD_DTYPE_BF16, each with a stride in elements from row to row.  Without
  * y (NULL) there is no residual: h = pre(x) * (1 + scale) + shift, x_out, post and
- * gate are not looked at; without h the call ends at x_out.  post NULL: t = y.  pre and post:
+ * gate are not looked at; without h the call ends at x_out, and pre, scale and shift are not.  post NULL: t = y.  pre and post:
  * LayerNorm (mean and variance) or RMSNorm (mean square), eps inside the root, times `weight`, plus `bias`
  * (dev [width] of the norm's dtype, either may be NULL).  gate, scale and shift: dev [n_mods][width] of the modulation's
  * dtype, `stride` elements from row to row (parts of one projection's output), any of them

@@ -94,10 +94,12 @@ int nfd_gate_norm(int n_rows, int width, int x_dtype, const void *x, long long x
     if (mod) {
         if (mod->dtype != NFD_DTYPE_FP32 && mod->dtype != NFD_DTYPE_BF16) return NFD_E_BADCFG;
         if (mod->n_mods < 1 || (!mod->index && mod->rows_per_mod < 1)) return NFD_E_RANGE;
-        for (const void *p : {mod->gate, mod->scale, mod->shift})
+        // (a gate goes with y, scale and shift with h: without those they are not looked at)
+        N.gate = y ? mod->gate : NULL, N.scale = h ? mod->scale : NULL, N.shift = h ? mod->shift : NULL;
+        for (const void *p : {N.gate, N.scale, N.shift})
             if (p) RET(check_plain_rows(p, mod->stride, width, mod->dtype));
         if (!aligned(mod->index, 4)) return NFD_E_ALIGN;
-        N.gate = mod->gate, N.scale = mod->scale, N.shift = mod->shift, N.mod_stride = mod->stride, N.mod_bf = mod->dtype == NFD_DTYPE_BF16;
+        N.mod_stride = mod->stride, N.mod_bf = mod->dtype == NFD_DTYPE_BF16;
         N.index = mod->index, N.n_mods = mod->n_mods;
         if (!mod->index) N.rows_per_mod = mod->rows_per_mod;
     }
