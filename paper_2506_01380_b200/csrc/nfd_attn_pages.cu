@@ -68,8 +68,11 @@ int nfd_attention_pages(const nfd_pages *pages, const nfd_batch *batch, int n_he
 int nfd_attention_packed(const nfd_batch *batch, int dtype, int n_heads, int kv_heads, int head_dim, const void *q, long long q_stride,
                          const void *k, long long k_stride, const void *v, long long v_stride, int frame_tokens, int window, void *out,
                          void *cuda_stream) {
+    if (!batch) return NFD_E_NULLPTR;
+    nfd_batch prompts = *batch;
+    prompts.kv_len = prompts.table = NULL;                 // (not looked at, aligned or not)
     BatchD B;
-    RET(check_batch(batch, false, B));
+    RET(check_batch(&prompts, false, B));
     if (dtype != NFD_DTYPE_FP32 && dtype != NFD_DTYPE_BF16) return NFD_E_BADCFG;
     if (head_dim != 32 && head_dim != 64 && head_dim != 128) return NFD_E_BADCFG;
     RET(check_heads(n_heads, kv_heads, B));
