@@ -373,8 +373,8 @@ static __device__ __forceinline__ int few_longest(const BatchD &B, int i, uint32
         }
         own[k * 32 + lane] = word[k];
     }
+    __syncwarp();                                           // (before the words are read, or, where all are as long, overwritten)
     if (__reduce_max_sync(0xffffffffu, most) == __reduce_min_sync(0xffffffffu, least)) return i;
-    __syncwarp();
 #pragma unroll 4
     for (int j = 0; j < B.n_seqs; j += 4) {
         const uint4 w = *reinterpret_cast<const uint4 *>(own + j);          // (zeros behind the last)
