@@ -277,7 +277,7 @@ template <typename TS>
 __global__ void __launch_bounds__(256) k_patch_embed(const StepParams *sp, Dims D, const TS *W_pe, const TS *b_pe,
                                                      float *z, TS *a_out, float2 *stats, const float *scale0,
                                                      size_t mod_row_stride, const RopeTab *rt, float2 *rope_tab) {
-    extern __shared__ float s_patch[];          // [PE_TOK][P]
+    extern __shared__ __align__(16) float s_patch[];          // [PE_TOK][P]
     NFD_TRACE_T0();
     pdl_wait();
     pdl_launch();

@@ -44,7 +44,7 @@ struct RotateIO {
 // unpack there were 142 registers, a CTA to an SM, and 21504 rows of 32 heads x 64 took 121 us.)
 template <typename TS, bool HALVES>
 __global__ void __launch_bounds__(ROTATE_THREADS, 5) k_rotate(const __grid_constant__ RotateD R, const RotateIO io, int rows, float sign) {
-    __shared__ float2 s_cs[ROTATE_MAX_ROWS * (ROTATE_MAX_DIM / 2)];
+    __shared__ __align__(16) float2 s_cs[ROTATE_MAX_ROWS * (ROTATE_MAX_DIM / 2)];
     const int tid = threadIdx.x, r0 = blockIdx.x * rows, nr = min(rows, io.n_rows - r0), pairs = R.dim / 2, per_head = R.dim / 16;
     const int n0 = io.heads[0] * per_head, n = n0 + io.heads[1] * per_head;
     // a thread's place (of n to a row), and the rows that it takes: row, row + by, ...
