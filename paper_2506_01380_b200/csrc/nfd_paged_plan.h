@@ -41,6 +41,27 @@ NFD_HD int sum_bits(int growth, int n) {
 #endif
 }
 
+// ---- one wave of CTAs for rows that go through shared memory -------------------------------------------------
+#define NORM_STAGES 6                    // rows of a CTA that are ahead, at most
+#define NORM_MOST 196608                 // shared memory of a CTA for them
+#define SM_SHARED 233472                 // of an SM; each CTA takes 1 KB beside its own, and whole units of 128 bytes
+struct NormPlan {
+    int ctas, stages;                    // CTAs that an SM holds at once; rows ahead of each
+};
+// regs: of a thread, in steps of 8; row_bytes: of a row in shared memory (0: rows do not go through it), of which two fit into NORM_MOST; own: a CTA's other shared memory.
+NFD_HD NormPlan norm_plan(int regs, int threads, int row_bytes, int own) {
+    NormPlan p = {65536 / (regs * threads), 0};
+    p.ctas = p.ctas < 1 ? 1 : p.ctas > 2048 / threads ? 2048 / threads : p.ctas;
+    if (!row_bytes) return p;
+    // as many rows ahead as leave the CTAs that the registers allow, two at least
+    const int fixed = own + 1024 + 128, share = SM_SHARED / p.ctas - fixed;
+    p.stages = (share < NORM_MOST ? share : NORM_MOST) / row_bytes;
+    p.stages = p.stages > NORM_STAGES ? NORM_STAGES : p.stages < 2 ? 2 : p.stages;
+    const int fit = SM_SHARED / (p.stages * row_bytes + fixed);
+    if (fit < p.ctas) p.ctas = fit;
+    return p;
+}
+
 // ---- the step of 4-bit numbers ------------------------------------------------------------------------------
 NFD_HD uint32_t bits_of(float x) {
 #ifdef __CUDA_ARCH__

@@ -104,9 +104,6 @@ __global__ void __launch_bounds__(ROTATE_THREADS, 5) k_rotate(const __grid_const
 
 // ---- norms around a block -----------------------------------------------------------------------------------
 #define NORM_FEW 8                       // rows to an SM up to which a CTA reads its own as it comes to it
-#define NORM_STAGES 6                    // rows of a CTA that are ahead, at most
-#define NORM_SHARED 225280               // shared memory of an SM for them
-#define NORM_MOST 196608                 // and of a CTA
 struct NormD {
     int on, layer, bf;                   // layer: LayerNorm, otherwise RMSNorm; bf: weight and bias are bf16, otherwise fp32
     float eps;
@@ -362,23 +359,17 @@ __global__ void __launch_bounds__(HOW == NORM_WARP ? 128 : 512, HOW == NORM_RING
 template <typename TX, typename TY, int HOW, int V> static int launch_gate_norm_as(const GateNormD &N, int threads, int bytes, int dev, int n_sm, cudaStream_t st) {
     auto kern = k_gate_norm<TX, TY, HOW, V>;
     static OncePerDevice once;
-    static int regs[NFD_PAGED_DEVICES];
+    static int regs[NFD_PAGED_DEVICES], own[NFD_PAGED_DEVICES];
     if (!once.run(dev, [&] {
             cudaFuncAttributes at;
             if (cudaFuncGetAttributes(&at, kern) != cudaSuccess || cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_MOST) != cudaSuccess) return false;
             regs[dev] = (at.numRegs + 7) / 8 * 8;
+            own[dev] = (int)at.sharedSizeBytes;
             return true;
         }))
         return NFD_E_CUDA;
-    int ctas = 65536 / (regs[dev] * threads), stages = 0;
-    ctas = ctas < 1 ? 1 : ctas > 2048 / threads ? 2048 / threads : ctas;
-    if (HOW == NORM_RING) {
-        // as many rows ahead as leave the CTAs that the registers allow, two at least (two rows fit: the caller's rule)
-        const int share = NORM_SHARED / ctas < NORM_MOST ? NORM_SHARED / ctas : NORM_MOST;
-        stages = share / bytes;
-        stages = stages > NORM_STAGES ? NORM_STAGES : stages < 2 ? 2 : stages;
-        ctas = NORM_SHARED / (stages * bytes) < ctas ? NORM_SHARED / (stages * bytes) : ctas;
-    }
+    // (two rows fit into shared memory: the caller's rule)
+    const auto [ctas, stages] = norm_plan(regs[dev], threads, HOW == NORM_RING ? bytes : 0, own[dev]);
     const long long per = HOW == NORM_WARP ? threads / 32 : 1, held = (long long)ctas * n_sm * per, rows = (N.n_rows + held - 1) / held;
     kern<<<(unsigned)((N.n_rows + rows * per - 1) / (rows * per)), threads, stages * bytes, st>>>(N, (int)rows, stages);
     return cudaGetLastError() == cudaSuccess ? NFD_OK : NFD_E_CUDA;

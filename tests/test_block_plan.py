@@ -12,6 +12,10 @@ SOURCE = r"""
 extern "C" long long seen(long long held, int frame_tokens, int window, int rows) { return keys_seen(held, frame_tokens, window, rows); }
 extern "C" long long prompt(int n_rows, int frame_tokens, int window, int rows) { return prompt_keys_seen(n_rows, frame_tokens, window, rows); }
 extern "C" int parts(long long keys, int part) { return parts_touched(keys, part); }
+extern "C" void norm(int regs, int threads, int row_bytes, int own, int *out) {
+    const NormPlan p = norm_plan(regs, threads, row_bytes, own);
+    out[0] = p.ctas, out[1] = p.stages;
+}
 """
 LAST = (1 << 31) - 1
 
@@ -68,3 +72,26 @@ def test_parts_that_keys_touch(lib):
             most = max(len({(a + i) // part for i in range(keys)}) for a in range(part))
             assert lib.parts(keys, part) == most, (keys, part)
     assert lib.parts(1 << 30, 64) == (1 << 24) + 1
+
+
+def test_a_wave_of_norms_is_what_the_device_holds(lib):
+    """All widths that go through shared memory, of two rows of 2 or 4 bytes a number: an SM has 64 K registers, 2048 threads and 228 KB, of which a CTA takes 1 KB and whole
+    units of 128 bytes beside its own.  No CTA is counted that has to wait for another one to leave, and no room for two more is left over."""
+    out = (C.c_int * 2)()
+    for size in (4, 6, 8):
+        for width in range(264, 16385, 8):
+            row, pieces = width * size, width // 8
+            if 2 * row > 196608:
+                continue
+            v = 1 if pieces <= 512 else 2 if pieces <= 1024 else 4
+            threads = (-(-pieces // v) + 31) // 32 * 32
+            for regs in (40, 64, 80, 128):
+                for own in (0, 176, 1000):
+                    lib.norm(regs, threads, row, own, out)
+                    ctas, stages = out
+                    assert 2 <= stages <= 6 and stages * row <= 196608
+                    taken = -(-(stages * row + own) // 128) * 128 + 1024
+                    held = min(65536 // (regs * threads), 2048 // threads, 233472 // taken)
+                    assert 1 <= ctas <= max(held, 1) and held - ctas <= 1, (size, width, regs, ctas, held)
+    lib.norm(32, 128, 0, 0, out)
+    assert tuple(out) == (16, 0)
