@@ -331,11 +331,14 @@ int nfd_attention_kv4(const nfd_pages *pages, const nfd_batch *batch, int n_head
  * to chunks of any length: q, out, n_heads, mask, scale and rows that see nothing as
  * in nfd_attention_kv4, q and out of the pages' type.  What a row does not see may
  * be anything, NaN included; a NaN or an infinity among the values that it does see makes
- * its column of that row NaN or infinite, however small its probability.  Values
- * may be as large as their type goes: a result, being a mean of them, is finite
- * with them.  (Small values: with up to 2^20 keys, values below 2^-56 may lose bits in
- * the sums.)  fp32 is computed on the fp32 pipes; with bf16, scores, softmax and sums are fp32
- * and probabilities are rounded to bf16 for the product with V. */
+ * its column of that row NaN or infinite, however small its probability.  A score of
+ * -inf is a probability of 0; a row that sees one that is NaN or inf is NaN.  Values
+ * may be as large as their type goes, but for 1 % of it (what roundings may add to a
+ * mean): a result, being a mean of them, is finite with them.  (Small values: with up to
+ * 2^20 keys, values below 2^-56 may lose bits in the sums.)  fp32 is computed on the fp32
+ * pipes; with bf16, scores, softmax and sums are fp32 and probabilities are rounded to bf16
+ * for the product with V, and where there are more than 64 rows x sharing heads (32 with
+ * head_dim 128) a quarter of them are formed to 1.2e-4 before that. */
 int nfd_attention_pages(const nfd_pages *pages, const nfd_batch *batch, int n_heads, const void *q, long long q_stride,
                         int frame_tokens, int window, void *out, void *cuda_stream);
 
@@ -422,8 +425,8 @@ typedef struct {
 /* Cross attention: every row of a sequence sees the first kv_len[s] (at most
  * n_keys) states of its sequence, but for masked ones.  q, out, n_heads, scale and
  * rows that see nothing as in nfd_attention_kv4; q and out of the states' type.
- * fp32 is computed on the fp32 pipes.  Values may be as large as their type goes: a
- * result, being a mean of them, is finite with them.  A NaN or an infinity among them
+ * fp32 is computed on the fp32 pipes.  Values may be as large as their type goes, but for
+ * 1 % of it (what roundings may add to a mean): a result is finite with them.  A NaN or an infinity among them
  * makes its column of the rows that see it NaN or infinite, however small its
  * probability.  (Small values: with up to 2^20 states, values below 2^-56 may lose
  * bits in the sums.) */

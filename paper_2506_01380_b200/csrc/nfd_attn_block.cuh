@@ -25,9 +25,9 @@
 // shared memory in a fixed order.  Every wait on a barrier in memory is bounded; after one that ran out the rows are NaN.  (The cluster's own barrier needs
 // no bound: every CTA comes to it, its other waits being bounded, or has left as a whole cluster.)
 //
-// What bounds it.  With head dimension 128 the tensor pipe: two causal prompts of 8192 rows, 16 heads on 4, take 461 us alone (1190 TFLOP/s) and 541 us after
+// What bounds it.  With head dimension 128 the tensor pipe: two causal prompts of 8192 rows, 16 heads on 4, take 462 us alone (1190 TFLOP/s) and 537 us after
 // many of their kind, when the clock has fallen (1020).  With 64 a block is 10 short products, which their one thread issues in 600 to 700 clocks, and the
-// chain S, P, O of each group (four prompts of 5376 rows in frames of 336, 16 heads: 344 us; the exponentials alone would take 211): hence three groups there,
+// chain S, P, O of each group (four prompts of 5376 rows in frames of 336, 16 heads: 346 us; the exponentials alone would take 211): hence three groups there,
 // whose chains overlap; with 128 tensor memory holds two.  Groups with an issuing thread each, or that wait for their turn at the pipes, were slower.
 // Short prompts are their CTAs' beginning (5 to 7 thousand clocks) and end (5).
 #pragma once
@@ -473,8 +473,9 @@ __device__ __forceinline__ float2 block_exp2_poly(float2 s, float c, float mc) {
     p = make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
     return flush2(p);
 }
-// sixteen scores to P, as pairs, and their sum.  BLOCK_POLY of eight pairs go to the fp32 pipes: with two warps to a scheduler a pair of columns takes 18.3
-// clocks with none, 18.2 with one, 16.6 with two and with three.
+// sixteen scores to P, as pairs, and their sum.  BLOCK_POLY of eight pairs go to the fp32 pipes.  With none, one, two, three and four: two prompts of 8192 rows, 16
+// heads on 4 x 128, 488, 467, 465, 459 and 475 us; four of 5376 in frames of 336, 16 heads x 64, 370, 348, 346, 348 and 367; four of 4096, 16 heads x 32, each in
+// one frame, 365, 343, 334, 347 and 369.
 template <bool MASKED> __device__ __forceinline__ void block_exp16(const float *x, uint32_t bits, float c, float mc, uint32_t *pk, float2 (&ls)[2]) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {

@@ -17,7 +17,7 @@
 // Measured: one row, 16 heads x 64, behind 5712 tokens in 4-bit pages 10.0 us (pieces, merge and launch; 6.6 MB); eight sequences of up to 32768
 // tokens, 24 heads on 8 x 128, 84.5 us (185 MB, 2.2 TB/s: nothing is saturated, 48 % of the issue slots, 28 % of the copy rate; latency, and lengths that
 // differ); bf16 states, eight rows, 16 heads x 64 against 4096 25.4 us (134 MB, 5.3 TB/s);
-// bf16 pages, 16 sequences of one row behind up to 16384 tokens, 24 heads on 8 x 128, 146 to 159 us (701 MB, 4.4 to 4.8 TB/s).
+// bf16 pages, 16 sequences of one row behind up to 16384 tokens, 24 heads on 8 x 128, 128 to 139 us (701 MB, 5.0 to 5.5 TB/s).
 #pragma once
 #include "nfd_attn_rows.cuh"
 #include "nfd_sm100.cuh"
