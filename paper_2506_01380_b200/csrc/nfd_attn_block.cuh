@@ -457,14 +457,15 @@ __device__ __forceinline__ float2 flush2(float2 a) {
     return d;
 }
 // 2^x, x = s c - mc, of two numbers on the fp32 pipes: x = n + f with n whole, a polynomial of degree 3 in f (fitted for the least relative error on [-1/2, 1/2],
-// 1.0e-4; P is rounded to bf16, 2^-9 = 2e-3, anyway), n added to the exponent, which must not leave its field.  So x is formed as 127 - 253.4 u with u cut off
-// at 0 and 1 by the instruction that makes it (two minima and maxima in its place cost 2 % of a call): below 2^-126 the result is 0, and from 2^127 on, and of
-// NaN, whose u is 0, it is 2^127, so that the part's sum has outgrown m.  The steps of u are 1.5e-5 of x.  p has 2^127 in its coefficients, n is counted from there.
+// 1.0e-4; P is rounded to bf16, 2^-9 = 2e-3, anyway), n added to the exponent, which must not leave its field.  So x, which is the other columns' to the bit, goes on
+// as 127 - 253.4 u with u cut off at 0 and 1 by the instruction that makes it (a minimum and a maximum in its place cost 2 % of a call): below 2^-126 the
+// result is 0, and from 2^127 on, and of NaN, whose u is 0, it is 2^127, so that the part's sum has outgrown m.  The steps of u are 1.5e-5 of x.  p has 2^127 in its
+// coefficients, n is counted from there.
 __device__ __forceinline__ float2 block_exp2_poly(float2 s, float c, float mc) {
     constexpr float top = 127.0f, range = 253.4f;                      // (127 - 253.4 = -126 - 0.4: n = -126, p < 1, a subnormal number)
     const float magic = 12582912.0f, one = 1.7014118346046923e38f;     // 1.5 x 2^23: an ulp is 1; 2^127
-    const float k = c * (-1.0f / range), a = fmaf(mc, 1.0f / range, top / range);
-    const float2 u = make_float2(__saturatef(fmaf(s.x, k, a)), __saturatef(fmaf(s.y, k, a)));
+    const float2 x = ffma2(s, make_float2(c, c), make_float2(-mc, -mc));
+    const float2 u = make_float2(__saturatef(fmaf(x.x, -1.0f / range, top / range)), __saturatef(fmaf(x.y, -1.0f / range, top / range)));
     const float2 t = ffma2(u, make_float2(-range, -range), make_float2(magic, magic)), n = ffma2(t, make_float2(-1.0f, -1.0f), make_float2(magic, magic));
     const float2 f = ffma2(u, make_float2(-range, -range), n);         // (n: the whole part's negative)
     float2 p = ffma2(f, make_float2(0.05517166852951050f * one, 0.05517166852951050f * one), make_float2(0.2426111251115799f * one, 0.2426111251115799f * one));
@@ -474,8 +475,8 @@ __device__ __forceinline__ float2 block_exp2_poly(float2 s, float c, float mc) {
     return flush2(p);
 }
 // sixteen scores to P, as pairs, and their sum.  BLOCK_POLY of eight pairs go to the fp32 pipes.  With none, one, two, three and four: two prompts of 8192 rows, 16
-// heads on 4 x 128, 488, 467, 465, 459 and 475 us; four of 5376 in frames of 336, 16 heads x 64, 370, 348, 346, 348 and 367; four of 4096, 16 heads x 32, each in
-// one frame, 365, 343, 334, 347 and 369.
+// heads on 4 x 128, 485, 463, 457, 449 and 473 us; four of 5376 in frames of 336, 16 heads x 64, 369, 348, 344, 354 and 377; four of 4096, 16 heads x 32, each in
+// one frame, 362, 340, 336, 354 and 383.
 template <bool MASKED> __device__ __forceinline__ void block_exp16(const float *x, uint32_t bits, float c, float mc, uint32_t *pk, float2 (&ls)[2]) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {

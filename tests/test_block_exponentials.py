@@ -32,6 +32,9 @@ extern "C" void run(const float *x, float *y, int n) {
         y[2 * i] = p.x, y[2 * i + 1] = q.y;
     }
 }
+extern "C" void scores(const float *s, float c, float mc, float *y, float *x, int n) {
+    for (int i = 0; i < n; ++i) y[i] = block_exp2_poly(make_float2(s[i], s[i]), c, mc).x, x[i] = fmaf(s[i], c, -mc);
+}
 """
 # Relative: the polynomial's own 1.0e-4; an argument that may be formed in steps of 2^-24 of a range of 2^8 and of constants rounded to that: off by three
 # half steps, 3 x 2^-17 ln 2; three roundings of 2^-24, and one of x + 3.
@@ -54,6 +57,14 @@ def exp2(tmp_path_factory):
         y = np.zeros((len(x), 2), np.float32)
         lib.run(x.ctypes.data_as(C.c_void_p), y.ctypes.data_as(C.c_void_p), len(x))
         return y
+
+    def scores(s, c, mc):
+        """2^(s c - mc), and the argument as the other columns form it."""
+        s = np.ascontiguousarray(s, np.float32)
+        y, x = np.zeros_like(s), np.zeros_like(s)
+        lib.scores(s.ctypes.data_as(C.c_void_p), C.c_float(c), C.c_float(mc), y.ctypes.data_as(C.c_void_p), x.ctypes.data_as(C.c_void_p), len(s))
+        return y, x
+    run.scores = scores
     return run
 
 
@@ -77,3 +88,15 @@ def test_below_its_range_it_is_nothing(exp2):
                                                           -3e38, -np.inf]])
     y = exp2(x)
     assert ((y >= 0) & (y <= 2.0 ** -126)).all() and (y[x < -126.1] == 0).all()
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_its_argument_is_that_of_the_other_columns_whatever_the_scores(exp2, dh):
+    """Scores that all have a large part in common, which their reference takes away: what is left is rounded once, as in the columns beside."""
+    c = float(np.float32(np.log2(np.e) / np.sqrt(dh)))
+    for common in (0.0, 1e3, -1e4, 1e5, -3e6):
+        s = (common + np.linspace(-200, 0, 4001)).astype(np.float32)
+        y, x = exp2.scores(s, c, float(np.float32(common * c + 57)))
+        inside = x > -125.9
+        want = np.exp2(x.astype(np.float64))
+        assert inside.any() and (np.abs(y - want)[inside] <= ERROR * want[inside]).all() and (y[x < -126.1] == 0).all(), common
